@@ -38,7 +38,10 @@ typedef enum {
 } sp_status;
 
 typedef enum { SP_DENSE = 0, SP_COMPRESSED = 1 } sp_level_type;
-typedef enum { SP_F32 = 0, SP_F64 = 1 } sp_dtype;
+typedef enum {
+    SP_F32 = 0, SP_F64 = 1,  /* the values of a tensor and the operands of its products     */
+    SP_F16 = 2, SP_BF16 = 3  /* operands of sp_attention only: sp_pack refuses them         */
+} sp_dtype;
 #define SP_MAX_RANK 8
 
 typedef struct sp_encoding sp_encoding;   /* HOST, immutable                                */
@@ -160,6 +163,77 @@ sp_status sp_unpack(const sp_tensor *t, int64_t *const *coords, void *values, vo
  * Enqueues on `stream`; does not synchronise when the allocator is stream-ordered (see sp_alloc_fn). */
 sp_status sp_sddmm(const sp_tensor *S, const void *A, int64_t lda, const void *B, int64_t ldb, int b_is_transposed,
                    int64_t K, void *X, void *stream);
+
+/* Attention over a stored pattern: a sampled product, a softmax over each row's stored entries and a product with dense rows in
+ * one pass (sp_sddmm's scores never leave the chip).  Rows of S (m x n) are queries, columns are keys; S's values are not read.
+ * Query i attends to the columns j that row i stores, with causal set only where kpos[j] <= qpos[i].  For every head h, which
+ * reads head g = h / (heads / kvHeads) of K and V:
+ *     s[i,j] = scale * sum_d Q[i,h,d] * K[j,g,d] + table[bucket(kpos[j] - qpos[i]), h]
+ *     lse[h,i] = log sum_j exp(s[i,j]),   O[i,h,d] = sum_j exp(s[i,j] - lse[h,i]) * V[j,g,d]
+ * A row that attends to nothing, or whose scores are all minus infinity, gives O = 0 and lse = minus infinity.  What a row does not
+ * attend to has no influence on it, whatever it holds (infinities and NaN included).
+ * A batch is a block-diagonal pattern: cross attention stores a rectangle for each sequence, of queries times states; tokens that
+ * share a prefix store the same columns, which are then read once for all rows of a block.
+ *
+ * The learned relative position bias (buckets = 0: none) has one row of `table` for each bucket of distances r = kpos[j] - qpos[i].
+ * bidirectional = 1: the upper half of the buckets is for r > 0, the distance is |r|; 0: the distance is max(-r, 0).  With N buckets
+ * a side and e = N / 2, distances below e have a bucket each, and distance d >= e has min(N - 1, e + floor((N - e) * log(d / e) /
+ * log(maxDistance / e))), borders that are whole numbers taken exactly.  At most 64 buckets, at least 2 a side,
+ * e < maxDistance <= 4096. */
+typedef struct sp_attention_problem {
+    int dtype;                          /* SP_F32, SP_F16 or SP_BF16: of Q, K, V, O, table and all gradients.  Sums are in f32. */
+    int heads, kvHeads;                 /* heads: a multiple of kvHeads                                                  */
+    int headDim;                        /* 1 .. 256                                                                      */
+    int causal;                         /* 1: only keys with kpos[j] <= qpos[i]                                          */
+    int buckets, maxDistance, bidirectional;
+    double scale;
+    const void *Q; int64_t ldq, hdq;    /* DEVICE: element (i, h, d) at Q[i * ldq + h * hdq + d]; strides >= 0           */
+    const void *K; int64_t ldk, hdk;    /* DEVICE: element (j, g, d) at K[j * ldk + g * hdk + d]                         */
+    const void *V; int64_t ldv, hdv;
+    const int32_t *qpos, *kpos;         /* DEVICE, m and n positions; read only with a bias or causal                    */
+    const void *table; int64_t ldt;     /* DEVICE: buckets x heads, row-major, ldt >= heads                              */
+} sp_attention_problem;
+
+/* The inspector step: looks at the pattern once and keeps with the handle what sp_attention (and, with grad = 1, sp_attention_grad)
+ * reads instead of pos and crd: the distinct columns of every block of rows with a bit for each pair, and how the blocks are
+ * cut into work items.  It serves any number of heads, any head size and type.  Synchronises `stream`; calling it again is a no-op.
+ * S: a packed rank-2 tensor, row-major with a compressed innermost level (CSR or DCSR); other encodings give SP_ERR_UNSUPPORTED
+ * (convert first).  Errors: NULL, RANK, UNSUPPORTED, TOO_LARGE (2^31 rows, columns or pairs of blocks and column windows), ALLOC, HIP. */
+sp_status sp_prepare_attention(sp_tensor *S, int grad, void *stream);
+
+/* Bytes of workspace that sp_attention (grad = 0) or sp_attention_grad (grad = 1) needs for this problem.  S must have been
+ * prepared (SP_ERR_UNSUPPORTED otherwise).  Reads the sizes in *p, none of its pointers. */
+sp_status sp_attention_workspace(const sp_tensor *S, const sp_attention_problem *p, int grad, size_t *bytes);
+
+/* O and lse for the problem above.
+ *   O    DEVICE: element (i, h, d) at O[i * ldo + h * hdo + d]; rows must not overlap each other or an input.
+ *   lse  DEVICE, heads x m, f32; may be NULL.
+ *   workspace  DEVICE, aligned to 256 bytes, at least as large as sp_attention_workspace says; used until the call's work on
+ *        `stream` is done.  Calls that may overlap (other streams, graphs that are replayed at the same time) need one each.
+ * S must have been prepared with sp_prepare_attention (SP_ERR_UNSUPPORTED otherwise).  Enqueues on `stream`; neither allocates nor
+ * synchronises, and keeps no state in the handle, so that calls may overlap and may be recorded into a HIP graph.  Results are the
+ * same bits on every call.  Errors: NULL, RANK, DTYPE, SHAPE, UNSUPPORTED, HIP. */
+sp_status sp_attention(const sp_tensor *S, const sp_attention_problem *p, void *O, int64_t ldo, int64_t hdo, float *lse,
+                       void *workspace, size_t workspaceBytes, void *stream);
+
+/* Gradients of a loss with respect to Q, K, V and the table, given dO = its gradient with respect to O (with D[i,h] = sum_d
+ * dO[i,h,d] * O[i,h,d] and p, s as above):
+ *     dV[j,g] = sum_{h of g} sum_i p[i,j] dO[i,h],   ds[i,j] = p[i,j] (sum_d dO[i,h,d] V[j,g,d] - D[i,h])
+ *     dQ[i,h] = scale sum_j ds[i,j] K[j,g],   dK[j,g] = scale sum_{h of g} sum_i ds[i,j] Q[i,h],
+ *     dTable[b,h] = sum over the pairs (i,j) of bucket b of ds[i,j]
+ * O and lse are sp_attention's; the gradients are overwritten (rows and columns without pairs become zero).  dTable may be NULL.
+ * S must have been prepared with grad = 1.  Workspace, streams and reproducibility as for sp_attention. */
+typedef struct sp_attention_grads {
+    const void *O; int64_t ldo, hdo;
+    const float *lse;                   /* DEVICE, heads x m                                                             */
+    const void *dO; int64_t lddo, hddo;
+    void *dQ; int64_t lddq, hddq;
+    void *dK; int64_t lddk, hddk;
+    void *dV; int64_t lddv, hddv;
+    void *dTable; int64_t lddt;         /* DEVICE: buckets x heads                                                       */
+} sp_attention_grads;
+sp_status sp_attention_grad(const sp_tensor *S, const sp_attention_problem *p, const sp_attention_grads *g,
+                            void *workspace, size_t workspaceBytes, void *stream);
 
 /* Matricized tensor times Khatri-Rao product A[i,j] = sum_{k,l} B[i,k,l] * D[l,j] * C[k,j] (Section 6.3, the MTTKRP
  * kernel), B a packed rank-3 tensor of shape I x K x L.

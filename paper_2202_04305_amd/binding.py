@@ -7,7 +7,7 @@ import torch
 from . import build as _build
 
 SP_DENSE, SP_COMPRESSED = 0, 1
-SP_F32, SP_F64 = 0, 1
+SP_F32, SP_F64, SP_F16, SP_BF16 = 0, 1, 2, 3
 SP_TUNE_SPMV_KERNEL, SP_TUNE_CSC_MODE, SP_TUNE_SPMM_KERNEL, SP_TUNE_PROFILE, SP_TUNE_SPGEMM_KERNEL = 1, 2, 3, 4, 5
 SP_MAX_RANK = 8
 
@@ -16,7 +16,7 @@ STATUS_NAMES = ["SP_OK", "SP_ERR_NULL", "SP_ERR_RANK", "SP_ERR_LEVEL_TYPE", "SP_
                 "SP_ERR_TOO_LARGE", "SP_ERR_ALLOC", "SP_ERR_HIP"]
 
 EXPORTS = ["sp_encode", "sp_encoding_free", "sp_pack", "sp_tensor_free", "sp_prepare", "sp_matmul", "sp_matmul_noalloc", "sp_pos", "sp_crd", "sp_values",
-           "sp_unpack", "sp_convert", "sp_sddmm", "sp_mttkrp", "sp_spgemm", "sp_add", "sp_tensor_info", "sp_tensor_tune", "sp_profile_read", "sp_stream_copy", "sp_stream_read", "sp_pack_sort_mode", "sp_status_str", "sp_last_hip_error"]
+           "sp_unpack", "sp_convert", "sp_sddmm", "sp_prepare_attention", "sp_attention_workspace", "sp_attention", "sp_attention_grad", "sp_mttkrp", "sp_spgemm", "sp_add", "sp_tensor_info", "sp_tensor_tune", "sp_profile_read", "sp_stream_copy", "sp_stream_read", "sp_pack_sort_mode", "sp_status_str", "sp_last_hip_error"]
 
 _ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p)
 _FREE_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_void_p)
@@ -28,6 +28,24 @@ class SpInfo(ctypes.Structure):
                 ("shape", ctypes.c_int64 * SP_MAX_RANK), ("nnz", ctypes.c_int64), ("nvalues", ctypes.c_int64),
                 ("maxSegment", ctypes.c_int64), ("storageBytes", ctypes.c_int64), ("derivedBytes", ctypes.c_int64),
                 ("spmvKernel", ctypes.c_int), ("lazyPrepares", ctypes.c_int)]
+
+
+class SpAttentionProblem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("heads", ctypes.c_int), ("kvHeads", ctypes.c_int), ("headDim", ctypes.c_int), ("causal", ctypes.c_int),
+                ("buckets", ctypes.c_int), ("maxDistance", ctypes.c_int), ("bidirectional", ctypes.c_int), ("scale", ctypes.c_double),
+                ("Q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("hdq", ctypes.c_int64),
+                ("K", ctypes.c_void_p), ("ldk", ctypes.c_int64), ("hdk", ctypes.c_int64),
+                ("V", ctypes.c_void_p), ("ldv", ctypes.c_int64), ("hdv", ctypes.c_int64),
+                ("qpos", ctypes.c_void_p), ("kpos", ctypes.c_void_p), ("table", ctypes.c_void_p), ("ldt", ctypes.c_int64)]
+
+
+class SpAttentionGrads(ctypes.Structure):
+    _fields_ = [("O", ctypes.c_void_p), ("ldo", ctypes.c_int64), ("hdo", ctypes.c_int64), ("lse", ctypes.c_void_p),
+                ("dO", ctypes.c_void_p), ("lddo", ctypes.c_int64), ("hddo", ctypes.c_int64),
+                ("dQ", ctypes.c_void_p), ("lddq", ctypes.c_int64), ("hddq", ctypes.c_int64),
+                ("dK", ctypes.c_void_p), ("lddk", ctypes.c_int64), ("hddk", ctypes.c_int64),
+                ("dV", ctypes.c_void_p), ("lddv", ctypes.c_int64), ("hddv", ctypes.c_int64),
+                ("dTable", ctypes.c_void_p), ("lddt", ctypes.c_int64)]
 
 
 class SpError(RuntimeError):
@@ -82,6 +100,15 @@ def load_library():
     L.sp_mttkrp.argtypes = [vp, vp, i64, vp, i64, i64, vp, i64, ci, vp]
     L.sp_sddmm.restype = ci
     L.sp_sddmm.argtypes = [vp, vp, i64, vp, i64, ci, i64, vp, vp]
+    problem, grads, size = ctypes.POINTER(SpAttentionProblem), ctypes.POINTER(SpAttentionGrads), ctypes.c_size_t
+    L.sp_prepare_attention.restype = ci
+    L.sp_prepare_attention.argtypes = [vp, ci, vp]
+    L.sp_attention_workspace.restype = ci
+    L.sp_attention_workspace.argtypes = [vp, problem, ci, ctypes.POINTER(size)]
+    L.sp_attention.restype = ci
+    L.sp_attention.argtypes = [vp, problem, vp, i64, i64, vp, vp, size, vp]
+    L.sp_attention_grad.restype = ci
+    L.sp_attention_grad.argtypes = [vp, problem, grads, vp, size, vp]
     L.sp_convert.restype = ci
     L.sp_convert.argtypes = [vp, vp, vp, ctypes.POINTER(vp)]
     L.sp_tensor_info.restype = ci
@@ -298,6 +325,126 @@ def sp_sddmm(S, A, B, X=None, b_is_transposed=False):
     _check(L.sp_sddmm(S._h, A.data_ptr(), int(A.stride(0)), B.data_ptr(), int(B.stride(0)), int(bool(b_is_transposed)), K,
                       X.data_ptr(), _stream_ptr()), "in sp_sddmm")
     return X
+
+
+_ATTENTION_DT = {torch.float32: SP_F32, torch.float16: SP_F16, torch.bfloat16: SP_BF16}
+
+
+def sp_prepare_attention(S, grad=False):
+    """The inspector step of sp_attention (grad: and of sp_attention_grad) on the pattern of S; synchronises."""
+    L = load_library()
+    _check(L.sp_prepare_attention(S._h, int(bool(grad)), _stream_ptr()), "in sp_prepare_attention")
+    return S
+
+
+def _rows_of_heads(t, name, S, dtype):
+    """The strides of a (tokens, heads, d) tensor: the last dimension is contiguous, the other two are free."""
+    if t.dim() != 3 or t.dtype != dtype or t.device != S.device or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError("%s: a (tokens, heads, d) tensor of %s on %s with a contiguous last dimension, not %s %s strides %s on %s" % (
+            name, dtype, S.device, t.dtype, tuple(t.shape), tuple(t.stride()), t.device))
+    return t.data_ptr(), int(t.stride(0)), int(t.stride(1))
+
+
+def _attention_problem(S, Q, K, V, scale, causal, qpos, kpos, bias, max_distance, bidirectional):
+    info = sp_tensor_info(S)
+    if info.rank != 2:
+        raise SpError(2, "in sp_attention")
+    m, n = info.shape[0], info.shape[1]
+    if Q.dtype not in _ATTENTION_DT:
+        raise SpError(9, "in sp_attention: %s" % Q.dtype)
+    p = SpAttentionProblem()
+    p.Q, p.ldq, p.hdq = _rows_of_heads(Q, "Q", S, Q.dtype)
+    p.K, p.ldk, p.hdk = _rows_of_heads(K, "K", S, Q.dtype)
+    p.V, p.ldv, p.hdv = _rows_of_heads(V, "V", S, Q.dtype)
+    if Q.shape[0] != m or K.shape[0] != n or V.shape != K.shape or K.shape[2] != Q.shape[2]:
+        raise ValueError("Q %s, K %s, V %s for a pattern of %d x %d" % (tuple(Q.shape), tuple(K.shape), tuple(V.shape), m, n))
+    p.dtype, p.heads, p.kvHeads, p.headDim = _ATTENTION_DT[Q.dtype], int(Q.shape[1]), int(K.shape[1]), int(Q.shape[2])
+    p.scale = float(Q.shape[2]) ** -0.5 if scale is None else float(scale)
+    p.causal = int(bool(causal))
+    if causal or bias is not None:
+        for name, t, size in (("qpos", qpos, m), ("kpos", kpos, n)):
+            if t is None or t.dtype != torch.int32 or t.device != S.device or tuple(t.shape) != (size,) or not t.is_contiguous():
+                raise ValueError("%s: %d contiguous int32 positions on %s" % (name, size, S.device))
+        p.qpos, p.kpos = qpos.data_ptr(), kpos.data_ptr()
+    if bias is not None:
+        if bias.dim() != 2 or bias.dtype != Q.dtype or bias.device != S.device or bias.shape[1] != Q.shape[1] or (bias.shape[1] > 1 and bias.stride(1) != 1):
+            raise ValueError("bias: a (buckets, heads) tensor of %s on %s" % (Q.dtype, S.device))
+        if bias.shape[0] == 0:
+            raise SpError(8, "in sp_attention: no buckets")
+        p.table, p.ldt, p.buckets = bias.data_ptr(), max(int(bias.stride(0)), int(bias.shape[1])) if bias.shape[0] == 1 else int(bias.stride(0)), int(bias.shape[0])
+        p.maxDistance, p.bidirectional = int(max_distance), int(bool(bidirectional))
+    return p
+
+
+def _attention_call(S, f):
+    """f() with S's device current: the stream, the workspace and the launches are that device's."""
+    if S.device.index is None or S.device.index == torch.cuda.current_device():
+        return f()
+    with torch.cuda.device(S.device):
+        return f()
+
+
+def _attention_workspace(L, S, p, grad):
+    need = ctypes.c_size_t()
+    _check(L.sp_attention_workspace(S._h, ctypes.byref(p), grad, ctypes.byref(need)), "in sp_attention_workspace")
+    return torch.empty(need.value, dtype=torch.uint8, device=S.device) if need.value else None, need.value
+
+
+def _attention_output(t, like, name):
+    """An output of `like`'s shape: a new one, or the caller's (its rows must not overlap)."""
+    if t is None:
+        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    if t.shape != like.shape:
+        raise ValueError("%s: shape %s, not %s" % (name, tuple(like.shape), tuple(t.shape)))
+    return t
+
+
+def sp_attention(S, Q, K, V, scale=None, causal=False, qpos=None, kpos=None, bias=None, max_distance=128, bidirectional=True, O=None, lse=None):
+    """Attention of the rows of S (queries) to the columns each stores (keys).  Q: (m, heads, d); K, V: (n, kv heads, d), f32, f16 or bf16;
+    scale: 1 / sqrt(d) unless given.  bias: (buckets, heads), the learned relative position bias; qpos (m), kpos (n): int32 positions,
+    for the bias and for causal (only keys at positions up to the query's).  Returns O (m, heads, d) and lse (heads, m) f32."""
+    L = load_library()
+
+    def call():
+        p = _attention_problem(S, Q, K, V, scale, causal, qpos, kpos, bias, max_distance, bidirectional)
+        out = _attention_output(O, Q, "O")
+        logs = torch.empty((Q.shape[1], Q.shape[0]), dtype=torch.float32, device=S.device) if lse is None else lse
+        if tuple(logs.shape) != (Q.shape[1], Q.shape[0]) or logs.dtype != torch.float32 or not logs.is_contiguous() or logs.device != S.device:
+            raise ValueError("lse: a contiguous f32 tensor of (heads, m)")
+        o, ldo, hdo = _rows_of_heads(out, "O", S, Q.dtype)
+        work, size = _attention_workspace(L, S, p, 0)
+        _check(L.sp_attention(S._h, ctypes.byref(p), o, ldo, hdo, logs.data_ptr(), work.data_ptr() if size else None, size, _stream_ptr()), "in sp_attention")
+        return out, logs
+    return _attention_call(S, call)
+
+
+def sp_attention_grad(S, Q, K, V, O, lse, dO, scale=None, causal=False, qpos=None, kpos=None, bias=None, max_distance=128, bidirectional=True,
+                      dQ=None, dK=None, dV=None):
+    """Gradients (dQ, dK, dV, dBias) for dO, the gradient with respect to O; O and lse are sp_attention's for the same arguments.
+    dBias is None without a bias."""
+    L = load_library()
+
+    def call():
+        p = _attention_problem(S, Q, K, V, scale, causal, qpos, kpos, bias, max_distance, bidirectional)
+        if O.shape != Q.shape or dO.shape != Q.shape or tuple(lse.shape) != (Q.shape[1], Q.shape[0]) or lse.dtype != torch.float32 or \
+                not lse.is_contiguous() or lse.device != S.device:
+            raise ValueError("O and dO: Q's shape; lse: a contiguous f32 tensor of (heads, m)")
+        g = SpAttentionGrads()
+        out = [_attention_output(t, like, name) for t, like, name in ((dQ, Q, "dQ"), (dK, K, "dK"), (dV, V, "dV"))]
+        g.O, g.ldo, g.hdo = _rows_of_heads(O, "O", S, Q.dtype)
+        g.dO, g.lddo, g.hddo = _rows_of_heads(dO, "dO", S, Q.dtype)
+        g.lse = lse.data_ptr()
+        g.dQ, g.lddq, g.hddq = _rows_of_heads(out[0], "dQ", S, Q.dtype)
+        g.dK, g.lddk, g.hddk = _rows_of_heads(out[1], "dK", S, Q.dtype)
+        g.dV, g.lddv, g.hddv = _rows_of_heads(out[2], "dV", S, Q.dtype)
+        dbias = None
+        if bias is not None:
+            dbias = torch.empty(bias.shape, dtype=bias.dtype, device=S.device)
+            g.dTable, g.lddt = dbias.data_ptr(), int(bias.shape[1])
+        work, size = _attention_workspace(L, S, p, 1)
+        _check(L.sp_attention_grad(S._h, ctypes.byref(p), ctypes.byref(g), work.data_ptr() if size else None, size, _stream_ptr()), "in sp_attention_grad")
+        return out[0], out[1], out[2], dbias
+    return _attention_call(S, call)
 
 
 def sp_mttkrp(B, C, D, A=None, accumulate=False):

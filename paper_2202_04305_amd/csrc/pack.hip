@@ -986,6 +986,7 @@ extern "C" void sp_tensor_free(sp_tensor *t)
     if (t->transposed) sp_tensor_free(t->transposed);
     free_segments(t);
     free_bins(t);
+    spmi_free_attention(t);
     release_tensor_arrays(t);
     if (t->prof_events) {
         for (hipEvent_t e : *t->prof_events) (void)hipEventDestroy(e);

@@ -117,6 +117,7 @@ struct sp_tensor {
     mutable void *mttkrp_windows;            // DEVICE int32[2 * windows]: fibre and slice holding the first entry of each window (rank 3)
     mutable sp_kept mttkrp_carry;            // scratch of the MTTKRP (J values per window)
     mutable sp_kept mttkrp_pad[2];           // scratch of the MTTKRP: inner / mid factor matrix with rows padded to whole cache lines
+    mutable struct sp_attn_plan *attention[2];   // sp_prepare_attention's: rows of queries, rows of keys (the pattern transposed); owned
     mutable std::vector<void *> *outgrown;   // scratch that was outgrown while it was shared, owned
     mutable size_t outgrown_bytes;
     mutable int tables_pending;              // rowblocks / non-empty rows not built yet (a result of sp_spgemm): built on first use by a product
@@ -428,6 +429,9 @@ sp_status spmi_sweep_emit(const sp_tensor *t, const uint64_t *keys, int64_t n, c
 // holds the sum of the first n-1 inputs.
 sp_status spmi_exclusive_scan(void *data, int64_t n, int bits, sp_scratch &tmp, hipStream_t st);
 sp_status spmi_fill_zero(void *p, size_t bytes, hipStream_t st);
+// ---- attention_plan.hip ----
+void spmi_free_attention(sp_tensor *t);
+size_t spmi_attention_bytes(const sp_tensor *t);
 // ---- sort.hip ----
 // Stable radix sort, least significant digit first, of (key, payload) pairs on the low `key_bits` bits taken as whole 8-bit
 // digits (so ceil(key_bits / 8) * 8 bits decide), payload of 4 or 8 bytes.  keys: a temporary of `tmp`, overwritten; vals: only
