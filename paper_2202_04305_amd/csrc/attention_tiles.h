@@ -1,0 +1,222 @@
+// Tiles of 32 x 32 scores on the matrix cores, for attention.hip and attention_grad.hip.
+//
+// Every product is laid out so that the 32 rows that a wave works for (queries; keys in the gradients of K and V) are the lanes:
+// the transposed scores S^T = K Q^T come out with row lane % 32 of the wave in each lane, and 16 of the 32 columns in its registers
+// (column 8 b + 4 (lane / 32) + c in register 4 b + c).  Maxima, sums, masks and scale factors of a row are then private to a lane
+// and its partner 32 lanes on, and the weights are, register by register, what the next product O^T = V^T P^T takes as its second
+// operand: a matrix instruction sums over 8 numbers of each half wave, in any order that both operands agree on, so registers 0-7
+// are the operand of the first 16 columns and 8-15 of the last 16.  V^T needs the columns' numbers transposed, which the LDS does
+// on reading (ds_read_b64_tr_b16; plain 4-byte reads for f32).
+//
+// A tile of dense rows lies in LDS in granules of 16 bytes, granule g of row r at place g ^ attn_swizzle(r).  The exchange keeps
+// both readers off each other's banks: 16 consecutive rows at one granule (first operand), and 4 consecutive rows at 4 granules
+// (transposed).
+#pragma once
+#include "attention.h"
+
+typedef float attn_f32x16 __attribute__((ext_vector_type(16)));
+typedef float attn_f32x4 __attribute__((ext_vector_type(4)));
+typedef short attn_s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char attn_lds;
+
+template <typename T> struct attn_mma;
+template <> struct attn_mma<attn_bf16> {
+    typedef attn_bf16 frag __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ attn_f32x16 mul(frag a, frag b, attn_f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct attn_mma<attn_f16> {
+    typedef attn_f16 frag __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ attn_f32x16 mul(frag a, frag b, attn_f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct attn_mma<float> {
+    typedef attn_f32x4 frag;
+    static __device__ __forceinline__ attn_f32x16 mul(frag a, frag b, attn_f32x16 c)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[k], b[k], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// What a tile of rows of DT numbers (the head size rounded up) looks like in LDS.
+template <typename T, int DT>
+struct attn_tile {
+    typedef typename attn_mma<T>::frag frag;
+    static constexpr int kRow = DT * (int)sizeof(T);     // bytes of a row
+    static constexpr int kGranules = kRow / 16;
+    static constexpr int kPer = 16 / (int)sizeof(T);     // numbers of a granule
+    static constexpr int kSteps = kGranules / 2;         // products a score is summed up in: 2 granules each, one for each half wave
+    static constexpr int kBlocks = DT / 32;              // blocks of 32 numbers of a transposed product
+
+    static __device__ __forceinline__ int swizzle(int r)
+    {
+        if (sizeof(T) == 4) return kGranules >= 16 ? (r & 3) | ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 : (r >> 1) & 7;
+        return kGranules >= 16 ? (r & 3) << 2 | ((r >> 2) & 3) : kGranules == 8 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r >> 2) & 3;
+    }
+    static __device__ __forceinline__ int place(int r, int g) { return r * kRow + ((g ^ swizzle(r)) << 4); }
+
+    // 32 rows from row0 (a multiple of 32) on as the first operand, step s
+    static __device__ __forceinline__ frag rows(const attn_lds *t, int row0, int s, int lane)
+    {
+        return *(const __attribute__((address_space(3))) frag *)(t + row0 * kRow + place(lane & 31, 2 * s + (lane >> 5)));
+    }
+    // acc (32 rows x 32 lanes) = the tile's rows row0 ... times the lanes' rows `b`
+    static __device__ __forceinline__ attn_f32x16 scores(const attn_lds *t, int row0, const frag (&b)[kSteps], int lane)
+    {
+        attn_f32x16 acc = (attn_f32x16)(0.f);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) acc = attn_mma<T>::mul(rows(t, row0, s, lane), b[s], acc);
+        return acc;
+    }
+    // acc[x] (numbers 32 x ... of a head, 32 lanes) += sum over the tile's 32 rows from row0 on of row[number] * w[row of the lane]
+    static __device__ __forceinline__ void add_rows(attn_f32x16 (&acc)[kBlocks], const attn_lds *t, int row0, const attn_f32x16 &w, int lane)
+    {
+        const int half = lane >> 5;
+        if constexpr (sizeof(T) == 4) {
+            const int l = lane & 31;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int row = 8 * (r >> 2) + 4 * half + (r & 3);
+#pragma unroll
+                for (int x = 0; x < kBlocks; ++x) {
+                    const float v = *(const __attribute__((address_space(3))) float *)(t + row0 * kRow + place(row, x * 8 + (l >> 2)) + (l & 3) * 4);
+                    acc[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[r], acc[x], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                frag p;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) p[k] = (T)w[8 * u + k];
+#pragma unroll
+                for (int x = 0; x < kBlocks; ++x) {
+                    union { attn_s16x4 q[2]; frag f; } v;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int row = 16 * u + 8 * k + 4 * half + ((lane & 15) >> 2);
+                        const int at = place(row, x * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8;
+                        v.q[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) attn_s16x4 *)(t + row0 * kRow + at));
+                    }
+                    acc[x] = attn_mma<T>::mul(v.f, p, acc[x]);
+                }
+            }
+        }
+    }
+    // one lane's row as the second operand: numbers past D are zero
+    static __device__ __forceinline__ void load_lane(const T *row, int D, bool vec, bool valid, float sign, frag (&b)[kSteps], int lane)
+    {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            b[s] = granule(row, (2 * s + (lane >> 5)) * kPer, D, vec, valid);
+            if (sign < 0) b[s] = -b[s];
+        }
+    }
+    // numbers d .. d + kPer - 1 of a row.  vec: rows are 16-byte aligned and D is a multiple of kPer
+    static __device__ __forceinline__ frag granule(const T *row, int d, int D, bool vec, bool valid)
+    {
+        frag f;
+        if (vec) {
+            if (valid && d < D) f = *(const frag *)(row + d);
+            else f = (frag)((T)0.f);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) f[k] = valid && d + k < D ? row[d + k] : (T)0.f;
+        }
+        return f;
+    }
+    static __device__ __forceinline__ void put(attn_lds *t, int r, int g, frag f) { *(__attribute__((address_space(3))) frag *)(t + place(r, g)) = f; }
+};
+
+// The larger of a lane's value and its partner's 32 lanes on; their sum.
+__device__ __forceinline__ float attn_pair_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const unsigned lo = r[0], hi = r[1];
+    return fmaxf(__uint_as_float(lo), __uint_as_float(hi));
+}
+__device__ __forceinline__ float attn_pair_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const unsigned lo = r[0], hi = r[1];
+    return __uint_as_float(lo) + __uint_as_float(hi);
+}
+
+// Where a work item's columns come from: a plan's list of a block, or a row's stretch of crd.
+struct attn_columns {
+    const int32_t *at;
+    int64_t last;                        // the last one's place; behind it: that one again
+    __device__ __forceinline__ int32_t get(int64_t x) const { return at[x < last ? x : last]; }
+};
+
+struct attn_item {
+    int64_t block;
+    int chunk0, c0, c1;                  // the block's first chunk, the item's chunks
+    int64_t part;                        // number among all items
+    bool whole;                          // the block's only item
+    attn_columns cols;
+    int64_t count;                       // br = 1: columns of the row
+
+    __device__ __forceinline__ attn_item(const attn_plan_view &p, int64_t item)
+    {
+        part = item;
+        block = p.item_block[item];
+        const int first = p.item0[block];
+        chunk0 = p.chunk0[block];
+        const int end = p.chunk0[block + 1];
+        whole = p.item0[block + 1] - first == 1;
+        c0 = chunk0 + (int)(item - first) * p.per_item;
+        c1 = c0 + p.per_item < end ? c0 + p.per_item : end;
+        if (p.br == 1) {
+            const int64_t s = p.rowptr[block];
+            count = p.rowptr[block + 1] - s;
+            cols = {p.crd + s, count - 1};
+        } else {
+            count = 0;
+            cols = {p.cols + (int64_t)chunk0 * kAttnChunk, (int64_t)(end - chunk0) * kAttnChunk - 1};
+        }
+    }
+    // the pairs of chunk c and row r of the block, and whether the 32 rows around r have none (0), some (1) or all (2) of them
+    __device__ __forceinline__ uint64_t word(const attn_plan_view &p, int c, int r) const
+    {
+        if (p.br != 1) return p.bits[(int64_t)c * p.br + r];
+        const int64_t left = count - (int64_t)(c - chunk0) * kAttnChunk;
+        return left >= kAttnChunk ? ~(uint64_t)0 : ((uint64_t)1 << left) - 1;
+    }
+    __device__ __forceinline__ int state(const attn_plan_view &p, int c, int r) const
+    {
+        if (p.br != 1) return p.state[(int64_t)c * (p.br >> 5) + (r >> 5)];
+        return count - (int64_t)(c - chunk0) * kAttnChunk >= kAttnChunk ? 2 : 1;
+    }
+};
+
+// The position bias in LDS: the bucket of every distance up to the last border, and the table's columns of the heads at hand.
+struct attn_bias {
+    const uint8_t *lut;                  // [2 last + 1]
+    const float *table;                  // [buckets][slots]
+    int last, slots, slot;
+    __device__ __forceinline__ int bucket(int kp, int qp) const
+    {
+        int r = attn_distance(kp, qp);
+        r = r < -last ? -last : r > last ? last : r;
+        return lut[r + last];
+    }
+    __device__ __forceinline__ float at(int bucket) const { return table[bucket * slots + slot]; }
+};
+static inline size_t attn_bias_bytes(const attn_args &a, int slots)
+{
+    return a.buckets ? (size_t)((2 * a.last + 1 + 15) & ~15) + (size_t)a.buckets * slots * 4 : 0;
+}
+// by the whole workgroup; the caller synchronises.  head(slot): the head of a slot, or -1
+template <typename T, typename HEAD>
+__device__ __forceinline__ attn_bias attn_make_bias(const attn_args &a, char *lds, int slots, HEAD head)
+{
+    uint8_t *lut = (uint8_t *)lds;
+    float *table = (float *)(lds + ((2 * a.last + 1 + 15) & ~15));
+    for (int x = threadIdx.x; x <= 2 * a.last; x += blockDim.x) lut[x] = (uint8_t)attn_bucket(a, x - a.last);
+    for (int x = threadIdx.x; x < a.buckets * slots; x += blockDim.x) {
+        const int h = head(x % slots);
+        table[x] = h < 0 ? 0.f : (float)((const T *)a.table)[(int64_t)(x / slots) * a.ldt + h];
+    }
+    return {lut, table, a.last, slots, 0};
+}
