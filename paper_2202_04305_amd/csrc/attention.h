@@ -1,4 +1,4 @@
-// Shared by the sources of attention over a stored pattern (attention_plan.hip, attention.hip, attention_grad.hip).
+// Shared by the sources of attention over a stored pattern (attention_plan.hip, attention.hip, attention_forward_*.hip, attention_backward_*.hip).
 #pragma once
 #include "spmi_internal.h"
 
@@ -59,8 +59,6 @@ struct attn_args {
     int buckets, side, exact, borders, last, bidirectional, causal;
     int16_t border[64];                  // far bucket k begins at distance border[k - 1]; distances from `last` on share a bucket
 };
-
-sp_status spmi_attention_check(const sp_tensor *S, const sp_attention_problem *p, int grad, attn_args *a);
 
 // The level whose items keep the chip busy: at least `want` workgroups where the pattern has as many, and as few parts to be joined
 // as that allows.
@@ -172,10 +170,10 @@ __device__ __forceinline__ void attn_row_forward(const attn_args &a, const attn_
     });
 }
 
-// sum over the stretch of ds K (not yet scaled); each(j, ds) is called for every pair
-template <typename T, typename F>
+// sum over the stretch of ds K (not yet scaled)
+template <typename T>
 __device__ __forceinline__ void attn_row_dq(const attn_args &a, const attn_plan_view &p, int64_t b, int r, int c0, int c1, int64_t i, int h, int lane,
-                                            const T *dO, float lse, float delta, float (&acc)[kAttnPer], F each)
+                                            const T *dO, float lse, float delta, float (&acc)[kAttnPer])
 {
     const int g = h / a.G;
     float q[kAttnPer], go[kAttnPer];
@@ -192,7 +190,6 @@ __device__ __forceinline__ void attn_row_dq(const attn_args &a, const attn_plan_
         const float s = attn_score<T>(a, attn_dot(q, x), i, j, h);
         if (s == -INFINITY) return;
         const float ds = attn_weight(s, lse) * (attn_dot(go, y) - delta);
-        each(j, ds);
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) acc[k] += ds * x[k];
     });

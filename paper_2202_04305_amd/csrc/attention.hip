@@ -1,420 +1,34 @@
-// Attention over a stored pattern, forward: argument checks, the kernel that makes O and lse, the join of rows that were cut.
+// Attention over a stored pattern: the entry points, their checks, and what a call launches (a rule on the plan and the heads, the same
+// for the workspace's size and for the call).
 #include "attention_tiles.h"
 #include <math.h>
 
 namespace {
 
-// How the 32 rows of a wave's tile are made of queries and heads.
-enum { kRowsOfHead,                      // br = 128: the workgroup's waves take 32 rows each, of one head
-       kHeadsOfRows,                     // br = 32: the workgroup's waves take a head each, of the same 32 rows
-       kRowsTogether,                    // br = 32: one tile, 32 rows of one head; the waves share its columns out
-       kHeadsTogether };                 // br = 1: one tile, up to 32 heads of one row; the waves share its columns out
-
-struct forward_args {
-    attn_args a;
-    attn_plan_view p;
-    void *O;
-    int64_t ldo, hdo;
-    float *lse;
-    float *part, *part_stat;             // of rows that are cut: [item][head][row of the block][D] and [..][2] (maximum, total)
-    int groups, mode, vec;               // workgroups of an item; mapping; whether rows are made of whole aligned granules
-};
-
-// A workgroup takes an item (a block of rows and a stretch of the columns that they store) and one head or a few that share K and V.
-// Per step KT columns' rows of K and V come through registers into LDS, gathered by the plan's list, while the step before is
-// computed; every wave makes the 32 x KW scores of its tile, masks them with the plan's bits, keeps each row's running maximum and sum
-// (f32), and adds the weighted rows of V to its 32 x D sums, which stay in registers.  Weights are rounded to the operands' type
-// for that product (half a step of 16-bit types, as every operand of the matrix cores is); the sum that divides takes them unrounded.
-//
-// WM waves take different tiles over the same columns; WN waves share the columns of one tile and are joined through LDS at the end.
-// POS: with positions (bias, causal); scores are held in units of e then, so that a bias of the type's lowest value stays a number,
-// and as plain products of q and k otherwise.
-template <typename T, int DT, int WM, int WN, int KW, bool POS>
-__global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kernel(forward_args f)
-{
-    typedef attn_tile<T, DT> tile;
-    typedef typename tile::frag frag;
-    constexpr int NT = 64 * WM * WN, KT = KW * WN, TILES = KW / 32;
-    constexpr int PIECES = KT * tile::kGranules / NT;    // granules of K (and of V) a thread fetches for a step
-    constexpr int ROWSTEP = NT / tile::kGranules;
-    constexpr int STEP = KT > kAttnChunk ? KT / kAttnChunk : 1;         // chunks of a step (or one chunk in 64 / KT steps)
-    constexpr int SUB = KT < kAttnChunk ? kAttnChunk / KT : 1;
-    static_assert(KT * tile::kGranules % NT == 0 && NT % tile::kGranules == 0, "every thread fetches the same number of granules");
-    extern __shared__ __align__(16) char lds[];
-    attn_lds *sK = (attn_lds *)lds, *sV = sK + KT * tile::kRow;
-    int *s_kpos = (int *)(lds + 2 * KT * tile::kRow);    // POS: [KT]
-    const attn_args &a = f.a;
-    const attn_plan_view &p = f.p;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = WN > 1 ? wave : 0;
-    const int64_t item_no = blockIdx.x / f.groups;
-    const int group = blockIdx.x % f.groups;
-    const attn_item item(p, item_no);
-
-    // this lane's query and head
-    int head, r = lane & 31, kv;
-    bool valid = true;
-    if (f.mode == kRowsOfHead) { head = group; kv = head / a.G; r += 32 * wave; }
-    else if (f.mode == kRowsTogether) { head = group; kv = head / a.G; }
-    else {
-        const int per = f.mode == kHeadsOfRows ? WM : 32, parts = (a.G + per - 1) / per;
-        kv = group / parts;
-        int x = (group % parts) * per + (f.mode == kHeadsOfRows ? wave : lane & 31);
-        valid = x < a.G;
-        if (!valid) x = a.G - 1;
-        head = kv * a.G + x;
-        if (f.mode == kHeadsTogether) r = 0;
-    }
-    int64_t row = item.block * p.br + r;
-    valid = valid && row < a.m;
-    if (row >= a.m) row = a.m - 1;
-    const bool busy = __builtin_amdgcn_ballot_w64(valid) != 0;
-    const float cc = POS ? kLog2e : fabsf(a.c);
-
-    frag q[tile::kSteps];
-    tile::load_lane((const T *)a.Q + row * a.ldq + head * a.hdq, a.D, f.vec, valid && item.c1 > item.c0, POS ? 1.f : a.c, q, lane);
-    int qp = 0;
-    attn_bias bias = {nullptr, nullptr, 0, 1, 0};
-    if (POS) {
-        if (a.qpos) qp = a.qpos[row];
-        if (a.buckets) {
-            const int slots = f.mode == kHeadsTogether ? 32 : f.mode == kHeadsOfRows ? WM : 1;
-            bias = attn_make_bias<T>(a, lds + 2 * KT * tile::kRow + KT * 4, slots, [&](int s) {
-                if (slots == 1) return group;
-                const int per = slots, parts = (a.G + per - 1) / per, x = (group % parts) * per + s;
-                return x < a.G ? (group / parts) * a.G + x : -1;
-            });
-            bias.slot = f.mode == kHeadsTogether ? lane & 31 : f.mode == kHeadsOfRows ? wave : 0;
-        }
-    }
-
-    attn_f32x16 acc[tile::kBlocks];
-#pragma unroll
-    for (int x = 0; x < tile::kBlocks; ++x) acc[x] = (attn_f32x16)(0.f);
-    float top = -INFINITY, total = 0;
-
-    const T *Kh = (const T *)a.K + (int64_t)kv * a.hdk, *Vh = (const T *)a.V + (int64_t)kv * a.hdv;
-    const int my_row = tid / tile::kGranules, my_g = tid % tile::kGranules;
-    const int64_t first = (int64_t)(item.c0 - item.chunk0) * kAttnChunk, steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
-    int32_t at[PIECES], pos_at = 0;
-    frag kf[PIECES], vf[PIECES];
-    int kp_next = 0;
-    auto fetch_columns = [&](int64_t step) {
-        const int64_t x = first + step * KT;
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) at[k] = item.cols.get(x + my_row + k * ROWSTEP);
-        if (POS && tid < KT) pos_at = item.cols.get(x + tid);
-    };
-    auto fetch_rows = [&]() {
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-            kf[k] = tile::granule(Kh + (int64_t)at[k] * a.ldk, my_g * tile::kPer, a.D, f.vec, true);
-            vf[k] = tile::granule(Vh + (int64_t)at[k] * a.ldv, my_g * tile::kPer, a.D, f.vec, true);
-        }
-        if (POS && a.kpos && tid < KT) kp_next = a.kpos[pos_at];
-    };
-    if (steps > 0) {
-        fetch_columns(0);
-        fetch_rows();
-        if (steps > 1) fetch_columns(1);
-    }
-    for (int64_t step = 0; step < steps; ++step) {
-        __syncthreads();                                 // the step before has been computed
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-            tile::put(sK, my_row + k * ROWSTEP, my_g, kf[k]);
-            tile::put(sV, my_row + k * ROWSTEP, my_g, vf[k]);
-        }
-        if (POS && tid < KT) s_kpos[tid] = kp_next;
-        __syncthreads();
-        if (step + 1 < steps) {
-            fetch_rows();
-            if (step + 2 < steps) fetch_columns(step + 2);
-        }
-        const int col0 = (int)(step % SUB) * KT + wn * KW;               // of this wave, from the step's first chunk on
-        const int chunk = item.c0 + (int)(step / SUB) * STEP + col0 / kAttnChunk;
-        if (!busy || chunk >= item.c1) continue;
-        const int state = item.state(p, chunk, r);
-        if (__builtin_amdgcn_readfirstlane(state) == 0) continue;
-        const uint64_t word = item.word(p, chunk, r) >> (col0 % kAttnChunk);
-        const bool all = __builtin_amdgcn_readfirstlane(state) == 2 && !(POS && a.causal);
-
-        attn_f32x16 s[TILES];
-        float up = top;
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-            s[t] = tile::scores(sK, wn * KW + 32 * t, q, lane);
-            if (POS) {
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const int *kp = s_kpos + wn * KW + 32 * t + 8 * b + 4 * (lane >> 5);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float v = s[t][4 * b + c] * a.scale;
-                        if (a.buckets) v += bias.at(bias.bucket(kp[c], qp));
-                        if (a.causal && kp[c] > qp) v = -INFINITY;
-                        s[t][4 * b + c] = v;
-                    }
-                }
-            }
-            if (!all) {
-                const uint32_t bits = (uint32_t)(word >> (32 * t)) >> (4 * (lane >> 5));
-#pragma unroll
-                for (int x = 0; x < 16; ++x) s[t][x] = bits >> (8 * (x >> 2) + (x & 3)) & 1 ? s[t][x] : -INFINITY;
-            }
-#pragma unroll
-            for (int x = 0; x < 16; ++x) up = fmaxf(up, s[t][x]);
-        }
-        up = attn_pair_max(up);
-        const float base = up == -INFINITY ? 0.f : up;
-        if (__builtin_amdgcn_ballot_w64(up != top) != 0) {
-            const float old = __builtin_amdgcn_exp2f((top - base) * cc);
-            total *= old;
-#pragma unroll
-            for (int x = 0; x < tile::kBlocks; ++x) acc[x] *= old;
-            top = up;
-        }
-        const float off = -base * cc;
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                s[t][x] = __builtin_amdgcn_exp2f(POS ? (s[t][x] - base) * cc : __builtin_fmaf(s[t][x], cc, off));
-                total += s[t][x];
-            }
-            tile::add_rows(acc, sV, wn * KW + 32 * t, s[t], lane);
-        }
-    }
-    total = attn_pair_sum(total);
-    // a row whose sums are not all finite is made again by itself: see attn_row_forward
-    float odd = total * 0.f;
-#pragma unroll
-    for (int x = 0; x < tile::kBlocks; ++x)
-#pragma unroll
-        for (int k = 0; k < 16; ++k) odd += acc[x][k] * 0.f;
-    uint64_t again = __builtin_amdgcn_ballot_w64(valid && !(odd == 0.f));
-    if (!POS && top != -INFINITY) top *= fabsf(a.scale);                  // from here on in units of e
-
-    const int64_t place = ((item.part * a.H + head) * p.br + r);          // of a part
-    float *stat = f.part_stat + 2 * place;
-    T *out = (T *)f.O + row * f.ldo + head * f.hdo;
-    if (WN == 1) {
-        again |= again >> 32;
-        if (valid && !(again >> (lane & 31) & 1)) {
-            const float inv = total == 0 ? 0.f : 1.f / total;
-            if (lane < 32) {
-                if (!item.whole) { stat[0] = top; stat[1] = total; }
-                else if (f.lse) f.lse[head * a.m + row] = total == 0 ? -INFINITY : top + __builtin_amdgcn_logf(total) * kLn2;
-            }
-#pragma unroll
-            for (int x = 0; x < tile::kBlocks; ++x)
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const int d = 32 * x + 8 * b + 4 * (lane >> 5);
-                    if (item.whole) {
-                        if (f.vec && d < a.D) {
-                            typedef T out4 __attribute__((ext_vector_type(4)));
-                            out4 o;
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) o[c] = (T)(acc[x][4 * b + c] * inv);
-                            *(out4 *)(out + d) = o;
-                        } else if (!f.vec) {
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) if (d + c < a.D) out[d + c] = (T)(acc[x][4 * b + c] * inv);
-                        }
-                    } else if (total != 0) {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) if (d + c < a.D) f.part[place * a.D + d + c] = acc[x][4 * b + c];
-                    }
-                }
-        }
-    } else {
-        // the waves' shares of the tile meet in LDS, over K and V
-        __syncthreads();
-        float *sums = (float *)lds, *stats = (float *)lds + WN * 32 * DT;        // [WN][32][DT], numbers exchanged by row; [WN][32][3]
-#pragma unroll
-        for (int x = 0; x < tile::kBlocks; ++x)
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int g = (8 * x + 2 * b + (lane >> 5)) ^ (lane & 7);
-                *(attn_f32x4 *)(sums + (wn * 32 + (lane & 31)) * DT + 4 * g) = (attn_f32x4){acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
-            }
-        if (lane < 32) {
-            float *st = stats + (wn * 32 + lane) * 3;
-            st[0] = top; st[1] = total;
-            st[2] = (again | again >> 32) >> lane & 1 ? 1.f : 0.f;
-        }
-        __syncthreads();
-        // a row at a time for NT / 32 threads
-        constexpr int LANES = NT / 32, EACH = DT / LANES;
-        const int mine = tid / LANES, part = tid % LANES;
-        float high = -INFINITY, sum = 0, w[WN], bad = 0;
-#pragma unroll
-        for (int x = 0; x < WN; ++x) { high = fmaxf(high, stats[(x * 32 + mine) * 3]); bad += stats[(x * 32 + mine) * 3 + 2]; }
-#pragma unroll
-        for (int x = 0; x < WN; ++x) {
-            w[x] = attn_weight(stats[(x * 32 + mine) * 3], high == -INFINITY ? 0.f : high);
-            sum += stats[(x * 32 + mine) * 3 + 1] * w[x];
-        }
-        // the row's query and head are those of lane `mine` of any wave
-        const int64_t row2 = ((int64_t)__shfl((int)(row >> 32), mine, 64) << 32) | (uint32_t)__shfl((int)row, mine, 64);
-        const int head2 = __shfl(head, mine, 64), r2 = __shfl(r, mine, 64);
-        const bool valid2 = __shfl((int)valid, mine, 64) != 0;
-        const int64_t place2 = (item.part * a.H + head2) * p.br + r2;
-        T *out2 = (T *)f.O + row2 * f.ldo + head2 * f.hdo;
-        if (valid2 && bad == 0) {
-            const float inv = sum == 0 ? 0.f : 1.f / sum;
-            if (part == 0) {
-                if (!item.whole) { f.part_stat[2 * place2] = high; f.part_stat[2 * place2 + 1] = sum; }
-                else if (f.lse) f.lse[head2 * a.m + row2] = sum == 0 ? -INFINITY : high + __builtin_amdgcn_logf(sum) * kLn2;
-            }
-#pragma unroll
-            for (int k = 0; k < EACH; k += 4) {
-                const int d = part * EACH + k;
-                attn_f32x4 v = (attn_f32x4)(0.f);
-#pragma unroll
-                for (int x = 0; x < WN; ++x) v += *(attn_f32x4 *)(sums + (x * 32 + mine) * DT + 4 * ((d >> 2) ^ (mine & 7))) * w[x];
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (d + c < a.D) {
-                        if (item.whole) out2[d + c] = (T)(v[c] * inv);
-                        else if (sum != 0) f.part[place2 * a.D + d + c] = v[c];
-                    }
-            }
-        }
-        again = 0;
-        for (int x = 0; x < 32; ++x) {
-            float any = 0;
-            for (int y = 0; y < WN; ++y) any += stats[(y * 32 + x) * 3 + 2];
-            if (any != 0 && x % WN == wn) again |= (uint64_t)1 << x;
-        }
-    }
-    for (again &= 0xffffffffu; again; again &= again - 1) {
-        const int x = __builtin_ctzll(again);
-        const int64_t i = ((int64_t)__builtin_amdgcn_readlane((int)(row >> 32), x) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)row, x);
-        const int h = __builtin_amdgcn_readlane(head, x), rr = __builtin_amdgcn_readlane(r, x);
-        float one[kAttnPer], hi, sum;
-        attn_row_forward<T>(a, p, item.block, rr, item.c0, item.c1, i, h, lane, hi, sum, one);
-        const int64_t at1 = (item.part * a.H + h) * p.br + rr;
-        const float inv = sum == 0 ? 0.f : 1.f / sum;
-        if (lane == 0) {
-            if (!item.whole) { f.part_stat[2 * at1] = hi; f.part_stat[2 * at1 + 1] = sum; }
-            else if (f.lse) f.lse[h * a.m + i] = sum == 0 ? -INFINITY : hi + __builtin_amdgcn_logf(sum) * kLn2;
-        }
-#pragma unroll
-        for (int k = 0; k < kAttnPer; ++k) {
-            const int d = lane + 64 * k;
-            if (d >= a.D) continue;
-            if (item.whole) ((T *)f.O)[i * f.ldo + h * f.hdo + d] = (T)(one[k] * inv);
-            else f.part[at1 * a.D + d] = one[k];
-        }
-    }
-}
-
-// Rows whose columns were cut into several items: a wave for a row and head.  Each part has its maximum and total; the parts' sums are
-// weighted to the largest maximum, in the items' order.
-template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(forward_args f)
-{
-    const attn_args &a = f.a;
-    const attn_plan_view &p = f.p;
-    const int lane = threadIdx.x & 63;
-    const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (x >= a.m * a.H) return;
-    const int64_t i = x / a.H, b = i / p.br;
-    const int h = (int)(x % a.H), r = (int)(i % p.br), first = p.item0[b], parts = p.item0[b + 1] - first;
-    if (parts == 1) return;
-    auto place = [&](int k) { return ((int64_t)(first + k) * a.H + h) * p.br + r; };
-    float top = -INFINITY;
-    for (int k = lane; k < parts; k += 64) top = fmaxf(top, f.part_stat[2 * place(k)]);
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    const float base = top == -INFINITY ? 0.f : top;
-    float acc[kAttnPer] = {0}, total = 0;
-    for (int k = 0; k < parts; ++k) {
-        const float t = f.part_stat[2 * place(k) + 1];
-        if (t == 0) continue;                            // this stretch has nothing of the row, and wrote nothing
-        const float w = attn_weight(f.part_stat[2 * place(k)], base);
-        total += t * w;
-#pragma unroll
-        for (int y = 0; y < kAttnPer; ++y)
-            if (lane + 64 * y < a.D) acc[y] += f.part[place(k) * a.D + lane + 64 * y] * w;
-    }
-    const float inv = total == 0 ? 0.f : 1.f / total;
-#pragma unroll
-    for (int y = 0; y < kAttnPer; ++y)
-        if (lane + 64 * y < a.D) ((T *)f.O)[i * f.ldo + h * f.hdo + lane + 64 * y] = (T)(acc[y] * inv);
-    if (f.lse && lane == 0) f.lse[h * a.m + i] = total == 0 ? -INFINITY : top + __builtin_amdgcn_logf(total) * kLn2;
-}
-
-// What a call launches: a rule on the plan and the heads, the same for the workspace's size and for the call.
-struct forward_choice {
-    int mode, wm, wn, groups, level;
-    bool cut;                            // some rows have several items
-    size_t part, part_stat;              // bytes
-};
 forward_choice choose(const sp_attn_plan *plan, const attn_args &a)
 {
     forward_choice c;
-    // a block of 32 rows: with three heads or more to a key, the waves take the heads and K and V are fetched once for them; with
-    // fewer, they share the columns out
-    if (plan->br == 128) { c.mode = kRowsOfHead; c.groups = a.H; }
-    else if (plan->br == 32 && a.G >= 3) { c.mode = kHeadsOfRows; c.groups = a.Hk * (int)ceil_div(a.G, 4); }
-    else if (plan->br == 32) { c.mode = kRowsTogether; c.groups = a.H; }
-    else { c.mode = kHeadsTogether; c.groups = a.Hk * (int)ceil_div(a.G, 32); }
-    const bool share = c.mode == kRowsTogether || c.mode == kHeadsTogether;
-    c.wm = share ? 1 : 4;
-    c.wn = share ? 4 : 1;
-    c.level = attn_pick_level(plan, c.groups, 1024);
-    c.cut = plan->items[c.level] > plan->nblocks;
+    (attn_mapping &)c = attn_map(plan, a);
     const size_t rows = c.cut ? (size_t)plan->items[c.level] * a.H * plan->br : 0;
     c.part = (rows * a.D * 4 + 255) & ~(size_t)255;
     c.part_stat = (rows * 8 + 255) & ~(size_t)255;
     return c;
 }
 
-template <typename T, int DT, int WM, int WN, int KW, bool POS>
-sp_status launch(const forward_args &f, const forward_choice &c, int64_t items, hipStream_t st)
+grad_choice choose(const sp_tensor *S, const attn_args &a)
 {
-    constexpr int KT = KW * WN;
-    const int slots = c.mode == kHeadsTogether ? 32 : c.mode == kHeadsOfRows ? WM : 1;
-    size_t lds = 2 * (size_t)KT * DT * sizeof(T) + (POS ? KT * 4 + attn_bias_bytes(f.a, slots) : 0);
-    const size_t join = WN > 1 ? (size_t)WN * 32 * (DT + 3) * 4 : 0;
-    if (join > lds) lds = join;
-    auto kernel = forward_kernel<T, DT, WM, WN, KW, POS>;
-    if (lds > 65536) SP_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(items * c.groups)), dim3(64 * WM * WN), lds, st, f);
-    SP_HIP(hipGetLastError());
-    return SP_OK;
-}
-
-template <typename T, int DT, bool POS>
-sp_status launch_mode(const forward_args &f, const forward_choice &c, int64_t items, hipStream_t st)
-{
-    constexpr bool wide = sizeof(T) == 4 && DT == 256;   // K and V of 128 columns would not fit the LDS
-    if (c.wn > 1) return launch<T, DT, 1, wide ? 2 : 4, 32, POS>(f, c, items, st);
-    return launch<T, DT, 4, 1, (DT * (int)sizeof(T) <= 256 ? 64 : 32), POS>(f, c, items, st);
-}
-
-template <typename T>
-sp_status forward_t(const sp_attn_plan *plan, forward_args &f, const forward_choice &c, hipStream_t st)
-{
-    // scale 0 goes with the positions: products of q and k by themselves would be scaled by zero after the mask's infinities
-    const bool pos = f.a.buckets || f.a.causal || f.a.scale == 0;
-    const int64_t items = plan->items[c.level];
-    if (items * c.groups >= ((int64_t)1 << 31)) return SP_ERR_TOO_LARGE;
-    sp_status s;
-#define SPMI_FORWARD(DT) s = pos ? launch_mode<T, DT, true>(f, c, items, st) : launch_mode<T, DT, false>(f, c, items, st)
-    if (f.a.D <= 32) SPMI_FORWARD(32);
-    else if (f.a.D <= 64) SPMI_FORWARD(64);
-    else if (f.a.D <= 128) SPMI_FORWARD(128);
-    else SPMI_FORWARD(256);
-#undef SPMI_FORWARD
-    SP_TRY(s);
-    if (c.cut) {
-        hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)ceil_div(f.a.m * f.a.H, 4)), dim3(256), 0, st, f);
-        SP_HIP(hipGetLastError());
-    }
-    return SP_OK;
+    const sp_attn_plan *rows = S->attention[0], *keys = S->attention[1];
+    grad_choice c;
+    c.rows = attn_map(rows, a);
+    c.keys_level = attn_pick_level(keys, a.Hk, 1024);
+    c.keys_cut = keys->items[c.keys_level] > keys->nblocks;
+    const size_t p1 = c.rows.cut ? (size_t)rows->items[c.rows.level] * a.H * rows->br * a.D * 4 : 0;
+    const size_t p2 = c.keys_cut ? (size_t)keys->items[c.keys_level] * a.Hk * keys->br * 2 * a.D * 4 : 0;
+    auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    c.delta = up((size_t)a.m * a.H * 4);
+    c.part = up(p1 > p2 ? p1 : p2);
+    c.table = up(a.buckets ? (size_t)rows->items[c.rows.level] * a.H * a.buckets * 4 : 0);
+    return c;
 }
 
 }  // namespace
@@ -436,7 +50,7 @@ static void make_borders(const sp_attention_problem *p, attn_args *a)
     }
 }
 
-sp_status spmi_attention_check(const sp_tensor *S, const sp_attention_problem *p, int grad, attn_args *a)
+static sp_status check_problem(const sp_tensor *S, const sp_attention_problem *p, int grad, attn_args *a)
 {
     if (!S || !p) return SP_ERR_NULL;
     if (S->enc.rank != 2) return SP_ERR_RANK;
@@ -468,9 +82,11 @@ extern "C" sp_status sp_attention_workspace(const sp_tensor *S, const sp_attenti
     if (!bytes) return SP_ERR_NULL;
     *bytes = 0;
     attn_args a;
-    SP_TRY(spmi_attention_check(S, p, grad, &a));
-    if (grad) *bytes = (size_t)a.m * a.H * 4;
-    else {
+    SP_TRY(check_problem(S, p, grad, &a));
+    if (grad) {
+        const grad_choice c = choose(S, a);
+        *bytes = c.delta + c.part + c.table;
+    } else {
         const forward_choice c = choose(S->attention[0], a);
         *bytes = c.part + c.part_stat;
     }
@@ -483,7 +99,7 @@ extern "C" sp_status sp_attention(const sp_tensor *S, const sp_attention_problem
     forward_args f;
     memset(&f, 0, sizeof(f));
     attn_args &a = f.a;
-    SP_TRY(spmi_attention_check(S, p, 0, &a));
+    SP_TRY(check_problem(S, p, 0, &a));
     if ((a.m > 1 && ldo < a.D) || (a.H > 1 && hdo < a.D)) return SP_ERR_SHAPE;
     if (a.m == 0) return SP_OK;
     const bool pairs = S->nvalues > 0;
@@ -500,12 +116,46 @@ extern "C" sp_status sp_attention(const sp_tensor *S, const sp_attention_problem
     f.part = (float *)workspace;
     f.part_stat = (float *)((char *)workspace + c.part);
     f.groups = c.groups; f.mode = c.mode;
-    const int size = p->dtype == SP_F32 ? 4 : 2;
-    f.vec = a.D * size % 16 == 0;
-    for (int64_t s : {a.ldq, a.hdq, a.ldk, a.hdk, a.ldv, a.hdv, ldo, hdo}) f.vec = f.vec && s * size % 16 == 0;
-    for (const void *x : {a.Q, a.K, a.V, (const void *)O}) f.vec = f.vec && (uintptr_t)x % 16 == 0;
+    attn_alignment rows(a.D, p->dtype == SP_F32 ? 4 : 2);
+    rows.with(a.Q, a.ldq, a.hdq); rows.with(a.K, a.ldk, a.hdk); rows.with(a.V, a.ldv, a.hdv); rows.with(O, ldo, hdo);
+    f.vec = rows.vec;
     hipStream_t st = (hipStream_t)stream;
-    if (p->dtype == SP_F32) return forward_t<float>(plan, f, c, st);
-    if (p->dtype == SP_F16) return forward_t<attn_f16>(plan, f, c, st);
-    return forward_t<attn_bf16>(plan, f, c, st);
+    if (p->dtype == SP_F32) return attn_forward<float>(plan, f, c, st);
+    if (p->dtype == SP_F16) return attn_forward<attn_f16>(plan, f, c, st);
+    return attn_forward<attn_bf16>(plan, f, c, st);
+}
+
+extern "C" sp_status sp_attention_grad(const sp_tensor *S, const sp_attention_problem *p, const sp_attention_grads *g,
+                                       void *workspace, size_t workspaceBytes, void *stream)
+{
+    grad_args f;
+    memset(&f, 0, sizeof(f));
+    attn_args &a = f.a;
+    SP_TRY(check_problem(S, p, 1, &a));
+    if (!g) return SP_ERR_NULL;
+    for (int64_t s : {g->ldo, g->hdo, g->lddo, g->hddo}) if (s < 0) return SP_ERR_SHAPE;
+    if ((a.H > 1 && g->hddq < a.D) || (a.m > 1 && g->lddq < a.D)) return SP_ERR_SHAPE;
+    if ((a.Hk > 1 && (g->hddk < a.D || g->hddv < a.D)) || (a.n > 1 && (g->lddk < a.D || g->lddv < a.D))) return SP_ERR_SHAPE;
+    if (a.buckets && g->dTable && g->lddt < a.H) return SP_ERR_SHAPE;
+    const bool pairs = S->nvalues > 0;
+    if (pairs && (!a.Q || !a.K || !a.V || ((a.buckets || a.causal) && (!a.qpos || !a.kpos)) || (a.buckets && !a.table))) return SP_ERR_NULL;
+    if (a.m > 0 && (!g->O || !g->lse || !g->dO || !g->dQ)) return SP_ERR_NULL;
+    if (a.n > 0 && (!g->dK || !g->dV)) return SP_ERR_NULL;
+    const grad_choice c = choose(S, a);
+    const size_t need = c.delta + c.part + c.table;
+    if (need > 0 && !workspace) return SP_ERR_NULL;
+    if (need > workspaceBytes || ((uintptr_t)workspace & 255)) return SP_ERR_SHAPE;
+    f.g = *g;
+    f.delta = (const float *)workspace;
+    f.part = (float *)((char *)workspace + c.delta);
+    if (a.buckets && g->dTable) f.part_table = (float *)((char *)workspace + c.delta + c.part);
+    attn_alignment rows(a.D, p->dtype == SP_F32 ? 4 : 2);
+    rows.with(a.Q, a.ldq, a.hdq); rows.with(a.K, a.ldk, a.hdk); rows.with(a.V, a.ldv, a.hdv);
+    rows.with(g->O, g->ldo, g->hdo); rows.with(g->dO, g->lddo, g->hddo);
+    rows.with(g->dQ, g->lddq, g->hddq); rows.with(g->dK, g->lddk, g->hddk); rows.with(g->dV, g->lddv, g->hddv);
+    f.vec = rows.vec;
+    hipStream_t st = (hipStream_t)stream;
+    if (p->dtype == SP_F32) return attn_backward<float>(S, f, c, st);
+    if (p->dtype == SP_F16) return attn_backward<attn_f16>(S, f, c, st);
+    return attn_backward<attn_bf16>(S, f, c, st);
 }

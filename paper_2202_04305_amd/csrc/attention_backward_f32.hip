@@ -1,0 +1,3 @@
+#include "attention_backward.h"
+
+template sp_status attn_backward<float>(const sp_tensor *, grad_args &, const grad_choice &, hipStream_t);

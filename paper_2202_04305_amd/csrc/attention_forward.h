@@ -1,0 +1,345 @@
+// Attention over a stored pattern, forward: the kernel that makes O and lse, the join of rows that were cut.  Compiled once for each
+// type (attention_forward_*.hip).
+#pragma once
+#include "attention_tiles.h"
+
+namespace {
+
+// A workgroup takes an item (a block of rows and a stretch of the columns that they store) and one head or a few that share K and V.
+// Per step KT columns' rows of K and V come through registers into LDS, gathered by the plan's list, while the step before is
+// computed; every wave makes the 32 x KW scores of its tile, masks them with the plan's bits, keeps each row's running maximum and sum
+// (f32), and adds the weighted rows of V to its 32 x D sums, which stay in registers.  Weights are rounded to the operands' type
+// for that product (half a step of 16-bit types, as every operand of the matrix cores is); the sum that divides takes them unrounded.
+//
+// WM waves take different tiles over the same columns; WN waves share the columns of one tile and are joined through LDS at the end.
+// POS: with positions (bias, causal); scores are held in units of e then, so that a bias of the type's lowest value stays a number,
+// and as plain products of q and k otherwise.
+template <typename T, int DT, int WM, int WN, int KW, bool POS>
+__global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kernel(forward_args f)
+{
+    typedef attn_tile<T, DT> tile;
+    typedef typename tile::frag frag;
+    constexpr int NT = 64 * WM * WN, KT = KW * WN, TILES = KW / 32;
+    constexpr int PIECES = KT * tile::kGranules / NT;    // granules of K (and of V) a thread fetches for a step
+    constexpr int ROWSTEP = NT / tile::kGranules;
+    constexpr int STEP = KT > kAttnChunk ? KT / kAttnChunk : 1;         // chunks of a step (or one chunk in 64 / KT steps)
+    constexpr int SUB = KT < kAttnChunk ? kAttnChunk / KT : 1;
+    static_assert(KT * tile::kGranules % NT == 0 && NT % tile::kGranules == 0, "every thread fetches the same number of granules");
+    extern __shared__ __align__(16) char lds[];
+    attn_lds *sK = (attn_lds *)lds, *sV = sK + KT * tile::kRow;
+    int *s_kpos = (int *)(lds + 2 * KT * tile::kRow);    // POS: [KT]
+    const attn_args &a = f.a;
+    const attn_plan_view &p = f.p;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = WN > 1 ? wave : 0;
+    const int64_t item_no = blockIdx.x / f.groups;
+    const int group = blockIdx.x % f.groups;
+    const attn_item item(p, item_no);
+
+    const attn_lane me(a, p.br, item.block, f.mode, group, lane, wave, WM);
+    const int64_t row = me.row;
+    const int head = me.head, kv = me.kv, r = me.r;
+    const bool valid = me.valid;
+    const bool busy = __builtin_amdgcn_ballot_w64(valid) != 0;
+    const float cc = POS ? kLog2e : fabsf(a.c);
+
+    frag q[tile::kSteps];
+    tile::load_lane((const T *)a.Q + row * a.ldq + head * a.hdq, a.D, f.vec, valid && item.c1 > item.c0, POS ? 1.f : a.c, q, lane);
+    int qp = 0;
+    attn_bias bias = {nullptr, nullptr, 0, 1, 0};
+    if (POS) {
+        if (a.qpos) qp = a.qpos[row];
+        if (a.buckets) bias = attn_lane_bias<T>(a, lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
+    }
+
+    attn_f32x16 acc[tile::kBlocks];
+#pragma unroll
+    for (int x = 0; x < tile::kBlocks; ++x) acc[x] = (attn_f32x16)(0.f);
+    float top = -INFINITY, total = 0;
+
+    const T *Kh = (const T *)a.K + (int64_t)kv * a.hdk, *Vh = (const T *)a.V + (int64_t)kv * a.hdv;
+    const int my_row = tid / tile::kGranules, my_g = tid % tile::kGranules;
+    const int64_t first = (int64_t)(item.c0 - item.chunk0) * kAttnChunk, steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
+    int32_t at[PIECES], pos_at = 0;
+    frag kf[PIECES], vf[PIECES];
+    int kp_next = 0;
+    auto fetch_columns = [&](int64_t step) {
+        const int64_t x = first + step * KT;
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) at[k] = item.cols.get(x + my_row + k * ROWSTEP);
+        if (POS && tid < KT) pos_at = item.cols.get(x + tid);
+    };
+    auto fetch_rows = [&]() {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            kf[k] = tile::granule(Kh + (int64_t)at[k] * a.ldk, my_g * tile::kPer, a.D, f.vec, true);
+            vf[k] = tile::granule(Vh + (int64_t)at[k] * a.ldv, my_g * tile::kPer, a.D, f.vec, true);
+        }
+        if (POS && a.kpos && tid < KT) kp_next = a.kpos[pos_at];
+    };
+    if (steps > 0) {
+        fetch_columns(0);
+        fetch_rows();
+        if (steps > 1) fetch_columns(1);
+    }
+    for (int64_t step = 0; step < steps; ++step) {
+        __syncthreads();                                 // the step before has been computed
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            tile::put(sK, my_row + k * ROWSTEP, my_g, kf[k]);
+            tile::put(sV, my_row + k * ROWSTEP, my_g, vf[k]);
+        }
+        if (POS && tid < KT) s_kpos[tid] = kp_next;
+        __syncthreads();
+        if (step + 1 < steps) {
+            fetch_rows();
+            if (step + 2 < steps) fetch_columns(step + 2);
+        }
+        const int col0 = (int)(step % SUB) * KT + wn * KW;               // of this wave, from the step's first chunk on
+        const int chunk = item.c0 + (int)(step / SUB) * STEP + col0 / kAttnChunk;
+        if (!busy || chunk >= item.c1) continue;
+        const int state = item.state(p, chunk, r);
+        if (__builtin_amdgcn_readfirstlane(state) == 0) continue;
+        const uint64_t word = item.word(p, chunk, r) >> (col0 % kAttnChunk);
+        const bool all = __builtin_amdgcn_readfirstlane(state) == 2 && !(POS && a.causal);
+
+        attn_f32x16 s[TILES];
+        float up = top;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+            s[t] = tile::scores(sK, wn * KW + 32 * t, q, lane);
+            if (POS) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int *kp = s_kpos + wn * KW + 32 * t + 8 * b + 4 * (lane >> 5);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float v = s[t][4 * b + c] * a.scale;
+                        if (a.buckets) v += bias.at(bias.bucket(kp[c], qp));
+                        if (a.causal && kp[c] > qp) v = -INFINITY;
+                        s[t][4 * b + c] = v;
+                    }
+                }
+            }
+            if (!all) {
+                const uint32_t bits = (uint32_t)(word >> (32 * t)) >> (4 * (lane >> 5));
+#pragma unroll
+                for (int x = 0; x < 16; ++x) s[t][x] = bits >> (8 * (x >> 2) + (x & 3)) & 1 ? s[t][x] : -INFINITY;
+            }
+#pragma unroll
+            for (int x = 0; x < 16; ++x) up = fmaxf(up, s[t][x]);
+        }
+        up = attn_pair_max(up);
+        const float base = up == -INFINITY ? 0.f : up;
+        if (__builtin_amdgcn_ballot_w64(up != top) != 0) {
+            const float old = __builtin_amdgcn_exp2f((top - base) * cc);
+            total *= old;
+#pragma unroll
+            for (int x = 0; x < tile::kBlocks; ++x) acc[x] *= old;
+            top = up;
+        }
+        const float off = -base * cc;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                s[t][x] = __builtin_amdgcn_exp2f(POS ? (s[t][x] - base) * cc : __builtin_fmaf(s[t][x], cc, off));
+                total += s[t][x];
+            }
+            tile::add_rows(acc, sV, wn * KW + 32 * t, s[t], lane);
+        }
+    }
+    total = attn_pair_sum(total);
+    // a row whose sums are not all finite is made again by itself: see attn_row_forward
+    float odd = total * 0.f;
+#pragma unroll
+    for (int x = 0; x < tile::kBlocks; ++x)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) odd += acc[x][k] * 0.f;
+    uint64_t again = __builtin_amdgcn_ballot_w64(valid && !(odd == 0.f));
+    if (!POS && top != -INFINITY) top *= fabsf(a.scale);                  // from here on in units of e
+
+    const int64_t place = ((item.part * a.H + head) * p.br + r);          // of a part
+    float *stat = f.part_stat + 2 * place;
+    T *out = (T *)f.O + row * f.ldo + head * f.hdo;
+    if (WN == 1) {
+        again |= again >> 32;
+        if (valid && !(again >> (lane & 31) & 1)) {
+            const float inv = total == 0 ? 0.f : 1.f / total;
+            if (lane < 32) {
+                if (!item.whole) { stat[0] = top; stat[1] = total; }
+                else if (f.lse) f.lse[head * a.m + row] = total == 0 ? -INFINITY : top + __builtin_amdgcn_logf(total) * kLn2;
+            }
+#pragma unroll
+            for (int x = 0; x < tile::kBlocks; ++x)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const int d = 32 * x + 8 * b + 4 * (lane >> 5);
+                    const attn_f32x4 v = {acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
+                    if (item.whole) attn_store4(out, d, a.D, f.vec, v * inv);
+                    else if (total != 0) attn_store4(f.part + place * a.D, d, a.D, f.vec, v);
+                }
+        }
+    } else {
+        // the waves' shares of the tile meet in LDS, over K and V
+        __syncthreads();
+        float *sums = (float *)lds, *stats = (float *)lds + WN * 32 * DT;        // [WN][32][DT], numbers exchanged by row; [WN][32][3]
+#pragma unroll
+        for (int x = 0; x < tile::kBlocks; ++x)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int g = (8 * x + 2 * b + (lane >> 5)) ^ (lane & 7);
+                *(attn_f32x4 *)(sums + (wn * 32 + (lane & 31)) * DT + 4 * g) = (attn_f32x4){acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
+            }
+        if (lane < 32) {
+            float *st = stats + (wn * 32 + lane) * 3;
+            st[0] = top; st[1] = total;
+            st[2] = (again | again >> 32) >> lane & 1 ? 1.f : 0.f;
+        }
+        __syncthreads();
+        // a row at a time for NT / 32 threads
+        constexpr int LANES = NT / 32, EACH = DT / LANES;
+        const int mine = tid / LANES, part = tid % LANES;
+        float high = -INFINITY, sum = 0, w[WN], bad = 0;
+#pragma unroll
+        for (int x = 0; x < WN; ++x) { high = fmaxf(high, stats[(x * 32 + mine) * 3]); bad += stats[(x * 32 + mine) * 3 + 2]; }
+#pragma unroll
+        for (int x = 0; x < WN; ++x) {
+            w[x] = attn_weight(stats[(x * 32 + mine) * 3], high == -INFINITY ? 0.f : high);
+            sum += stats[(x * 32 + mine) * 3 + 1] * w[x];
+        }
+        // the row's query and head are those of lane `mine` of any wave
+        const int64_t row2 = ((int64_t)__shfl((int)(row >> 32), mine, 64) << 32) | (uint32_t)__shfl((int)row, mine, 64);
+        const int head2 = __shfl(head, mine, 64), r2 = __shfl(r, mine, 64);
+        const bool valid2 = __shfl((int)valid, mine, 64) != 0;
+        const int64_t place2 = (item.part * a.H + head2) * p.br + r2;
+        T *out2 = (T *)f.O + row2 * f.ldo + head2 * f.hdo;
+        if (valid2 && bad == 0) {
+            const float inv = sum == 0 ? 0.f : 1.f / sum;
+            if (part == 0) {
+                if (!item.whole) { f.part_stat[2 * place2] = high; f.part_stat[2 * place2 + 1] = sum; }
+                else if (f.lse) f.lse[head2 * a.m + row2] = sum == 0 ? -INFINITY : high + __builtin_amdgcn_logf(sum) * kLn2;
+            }
+#pragma unroll
+            for (int k = 0; k < EACH; k += 4) {
+                const int d = part * EACH + k;
+                attn_f32x4 v = (attn_f32x4)(0.f);
+#pragma unroll
+                for (int x = 0; x < WN; ++x) v += *(attn_f32x4 *)(sums + (x * 32 + mine) * DT + 4 * ((d >> 2) ^ (mine & 7))) * w[x];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (d + c < a.D) {
+                        if (item.whole) out2[d + c] = (T)(v[c] * inv);
+                        else if (sum != 0) f.part[place2 * a.D + d + c] = v[c];
+                    }
+            }
+        }
+        again = 0;
+        for (int x = 0; x < 32; ++x) {
+            float any = 0;
+            for (int y = 0; y < WN; ++y) any += stats[(y * 32 + x) * 3 + 2];
+            if (any != 0 && x % WN == wn) again |= (uint64_t)1 << x;
+        }
+    }
+    for (again &= 0xffffffffu; again; again &= again - 1) {
+        const int x = __builtin_ctzll(again);
+        const int64_t i = ((int64_t)__builtin_amdgcn_readlane((int)(row >> 32), x) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)row, x);
+        const int h = __builtin_amdgcn_readlane(head, x), rr = __builtin_amdgcn_readlane(r, x);
+        float one[kAttnPer], hi, sum;
+        attn_row_forward<T>(a, p, item.block, rr, item.c0, item.c1, i, h, lane, hi, sum, one);
+        const int64_t at1 = (item.part * a.H + h) * p.br + rr;
+        const float inv = sum == 0 ? 0.f : 1.f / sum;
+        if (lane == 0) {
+            if (!item.whole) { f.part_stat[2 * at1] = hi; f.part_stat[2 * at1 + 1] = sum; }
+            else if (f.lse) f.lse[h * a.m + i] = sum == 0 ? -INFINITY : hi + __builtin_amdgcn_logf(sum) * kLn2;
+        }
+#pragma unroll
+        for (int k = 0; k < kAttnPer; ++k) {
+            const int d = lane + 64 * k;
+            if (d >= a.D) continue;
+            if (item.whole) ((T *)f.O)[i * f.ldo + h * f.hdo + d] = (T)(one[k] * inv);
+            else f.part[at1 * a.D + d] = one[k];
+        }
+    }
+}
+
+// Rows whose columns were cut into several items: a wave for a row and head.  Each part has its maximum and total; the parts' sums are
+// weighted to the largest maximum, in the items' order.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(forward_args f)
+{
+    const attn_args &a = f.a;
+    const attn_plan_view &p = f.p;
+    const int lane = threadIdx.x & 63;
+    const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (x >= a.m * a.H) return;
+    const int64_t i = x / a.H, b = i / p.br;
+    const int h = (int)(x % a.H), r = (int)(i % p.br), first = p.item0[b], parts = p.item0[b + 1] - first;
+    if (parts == 1) return;
+    auto place = [&](int k) { return ((int64_t)(first + k) * a.H + h) * p.br + r; };
+    float top = -INFINITY;
+    for (int k = lane; k < parts; k += 64) top = fmaxf(top, f.part_stat[2 * place(k)]);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float base = top == -INFINITY ? 0.f : top;
+    float acc[kAttnPer] = {0}, total = 0;
+    for (int k = 0; k < parts; ++k) {
+        const float t = f.part_stat[2 * place(k) + 1];
+        if (t == 0) continue;                            // this stretch has nothing of the row, and wrote nothing
+        const float w = attn_weight(f.part_stat[2 * place(k)], base);
+        total += t * w;
+#pragma unroll
+        for (int y = 0; y < kAttnPer; ++y)
+            if (lane + 64 * y < a.D) acc[y] += f.part[place(k) * a.D + lane + 64 * y] * w;
+    }
+    const float inv = total == 0 ? 0.f : 1.f / total;
+#pragma unroll
+    for (int y = 0; y < kAttnPer; ++y)
+        if (lane + 64 * y < a.D) ((T *)f.O)[i * f.ldo + h * f.hdo + lane + 64 * y] = (T)(acc[y] * inv);
+    if (f.lse && lane == 0) f.lse[h * a.m + i] = total == 0 ? -INFINITY : top + __builtin_amdgcn_logf(total) * kLn2;
+}
+
+template <typename T, int DT, int WM, int WN, int KW, bool POS>
+sp_status launch(const forward_args &f, const forward_choice &c, int64_t items, hipStream_t st)
+{
+    constexpr int KT = KW * WN;
+    size_t lds = 2 * (size_t)KT * DT * sizeof(T) + (POS ? KT * 4 + attn_bias_bytes(f.a, c.slots()) : 0);
+    const size_t join = WN > 1 ? (size_t)WN * 32 * (DT + 3) * 4 : 0;
+    if (join > lds) lds = join;
+    auto kernel = forward_kernel<T, DT, WM, WN, KW, POS>;
+    if (lds > 65536) SP_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(items * c.groups)), dim3(64 * WM * WN), lds, st, f);
+    SP_HIP(hipGetLastError());
+    return SP_OK;
+}
+
+template <typename T, int DT, bool POS>
+sp_status launch_mode(const forward_args &f, const forward_choice &c, int64_t items, hipStream_t st)
+{
+    constexpr bool wide = sizeof(T) == 4 && DT == 256;   // K and V of 128 columns would not fit the LDS
+    if (c.wn > 1) return launch<T, DT, 1, wide ? 2 : 4, 32, POS>(f, c, items, st);
+    return launch<T, DT, 4, 1, (DT * (int)sizeof(T) <= 256 ? 64 : 32), POS>(f, c, items, st);
+}
+
+}  // namespace
+
+template <typename T>
+sp_status attn_forward(const sp_attn_plan *plan, forward_args &f, const forward_choice &c, hipStream_t st)
+{
+    // scale 0 goes with the positions: products of q and k by themselves would be scaled by zero after the mask's infinities
+    const bool pos = f.a.buckets || f.a.causal || f.a.scale == 0;
+    const int64_t items = plan->items[c.level];
+    if (items * c.groups >= ((int64_t)1 << 31)) return SP_ERR_TOO_LARGE;
+    sp_status s;
+#define SPMI_FORWARD(DT) s = pos ? launch_mode<T, DT, true>(f, c, items, st) : launch_mode<T, DT, false>(f, c, items, st)
+    if (f.a.D <= 32) SPMI_FORWARD(32);
+    else if (f.a.D <= 64) SPMI_FORWARD(64);
+    else if (f.a.D <= 128) SPMI_FORWARD(128);
+    else SPMI_FORWARD(256);
+#undef SPMI_FORWARD
+    SP_TRY(s);
+    if (c.cut) {
+        hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)ceil_div(f.a.m * f.a.H, 4)), dim3(256), 0, st, f);
+        SP_HIP(hipGetLastError());
+    }
+    return SP_OK;
+}

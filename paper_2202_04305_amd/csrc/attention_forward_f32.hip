@@ -1,0 +1,3 @@
+#include "attention_forward.h"
+
+template sp_status attn_forward<float>(const sp_attn_plan *, forward_args &, const forward_choice &, hipStream_t);

@@ -1,4 +1,4 @@
-// Tiles of 32 x 32 scores on the matrix cores, for attention.hip and attention_grad.hip.
+// Tiles of 32 x 32 scores on the matrix cores, for attention_forward.h and attention_backward.h.
 //
 // Every product is laid out so that the 32 rows that a wave works for (queries; keys in the gradients of K and V) are the lanes:
 // the transposed scores S^T = K Q^T come out with row lane % 32 of the wave in each lane, and 16 of the 32 columns in its registers
@@ -220,3 +220,131 @@ __device__ __forceinline__ attn_bias attn_make_bias(const attn_args &a, char *ld
     }
     return {lut, table, a.last, slots, 0};
 }
+
+// How the 32 rows of a wave's tile are made of queries and heads.
+enum { kRowsOfHead,                      // br = 128: the workgroup's waves take 32 rows each, of one head
+       kHeadsOfRows,                     // br = 32: the workgroup's waves take a head each, of the same 32 rows
+       kRowsTogether,                    // br = 32: one tile, 32 rows of one head; the waves share its columns out
+       kHeadsTogether };                 // br = 1: one tile, up to 32 heads of one row; the waves share its columns out
+
+// A lane's query and head.  group: which heads the workgroup takes, of attn_groups().
+struct attn_lane {
+    int head, kv, r;                     // r: the row's place in its block
+    int64_t row;
+    bool valid;                          // a pair of a row and a head that exists (clamped to one that does)
+    __device__ __forceinline__ attn_lane(const attn_args &a, int br, int64_t block, int mode, int group, int lane, int wave, int waves)
+    {
+        r = lane & 31;
+        valid = true;
+        if (mode == kRowsOfHead || mode == kRowsTogether) {
+            head = group;
+            kv = head / a.G;
+            if (mode == kRowsOfHead) r += 32 * wave;
+        } else {
+            const int per = mode == kHeadsOfRows ? waves : 32, parts = (a.G + per - 1) / per;
+            kv = group / parts;
+            int x = (group % parts) * per + (mode == kHeadsOfRows ? wave : lane & 31);
+            valid = x < a.G;
+            if (!valid) x = a.G - 1;
+            head = kv * a.G + x;
+            if (mode == kHeadsTogether) r = 0;
+        }
+        row = block * br + r;
+        valid = valid && row < a.m;
+        if (row >= a.m) row = a.m - 1;
+    }
+};
+// the bias for the workgroup's heads, its slot for this lane
+template <typename T>
+__device__ __forceinline__ attn_bias attn_lane_bias(const attn_args &a, char *lds, int mode, int group, int lane, int wave, int waves)
+{
+    const int slots = mode == kHeadsTogether ? 32 : mode == kHeadsOfRows ? waves : 1;
+    attn_bias b = attn_make_bias<T>(a, lds, slots, [&](int s) {
+        if (slots == 1) return group;
+        const int parts = (a.G + slots - 1) / slots, x = (group % parts) * slots + s;
+        return x < a.G ? (group / parts) * a.G + x : -1;
+    });
+    b.slot = mode == kHeadsTogether ? lane & 31 : mode == kHeadsOfRows ? wave : 0;
+    return b;
+}
+
+// The mapping for a plan and a problem, and how the plan is cut.
+// A block of 32 rows: with three heads or more to a key, the waves take the heads and K and V are fetched once for them; with
+// fewer, they share the columns out.
+struct attn_mapping {
+    int mode, wm, wn, groups, level;
+    bool cut;                            // some rows have several items
+    int slots() const { return mode == kHeadsTogether ? 32 : mode == kHeadsOfRows ? wm : 1; }
+};
+static inline attn_mapping attn_map(const sp_attn_plan *plan, const attn_args &a)
+{
+    attn_mapping c;
+    if (plan->br == 128) { c.mode = kRowsOfHead; c.groups = a.H; }
+    else if (plan->br == 32 && a.G >= 3) { c.mode = kHeadsOfRows; c.groups = a.Hk * (int)ceil_div(a.G, 4); }
+    else if (plan->br == 32) { c.mode = kRowsTogether; c.groups = a.H; }
+    else { c.mode = kHeadsTogether; c.groups = a.Hk * (int)ceil_div(a.G, 32); }
+    const bool share = c.mode == kRowsTogether || c.mode == kHeadsTogether;
+    c.wm = share ? 1 : 4;
+    c.wn = share ? 4 : 1;
+    c.level = attn_pick_level(plan, c.groups, 1024);
+    c.cut = plan->items[c.level] > plan->nblocks;
+    return c;
+}
+
+// Rows of all tensors made of whole 16-byte granules?
+struct attn_alignment {
+    bool vec;
+    attn_alignment(int D, int size) : vec(D * size % 16 == 0), size_(size) {}
+    void with(const void *x, int64_t ld, int64_t hd) { vec = vec && (uintptr_t)x % 16 == 0 && ld * size_ % 16 == 0 && hd * size_ % 16 == 0; }
+private:
+    int size_;
+};
+
+// Numbers of 4 columns of a row: whole, or cut at D.
+template <typename T>
+__device__ __forceinline__ void attn_store4(T *row, int d, int D, bool vec, attn_f32x4 v)
+{
+    if (vec) {
+        typedef T out4 __attribute__((ext_vector_type(4)));
+        if (d < D) *(out4 *)(row + d) = __builtin_convertvector(v, out4);
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) if (d + c < D) row[d + c] = (T)v[c];
+    }
+}
+
+// ---- what attention.hip hands to the sources of one type ---------------------------------------------------------------------
+struct forward_args {
+    attn_args a;
+    attn_plan_view p;
+    void *O;
+    int64_t ldo, hdo;
+    float *lse;
+    float *part, *part_stat;             // of rows that are cut: [item][head][row of the block][D] and [..][2] (maximum, total)
+    int groups, mode, vec;               // workgroups of an item; mapping; whether rows are made of whole aligned granules
+};
+
+struct forward_choice : attn_mapping {
+    size_t part, part_stat;              // bytes
+};
+template <typename T>
+sp_status attn_forward(const sp_attn_plan *plan, forward_args &f, const forward_choice &c, hipStream_t st);
+
+struct grad_args {
+    attn_args a;
+    attn_plan_view p;
+    sp_attention_grads g;
+    const float *delta;                  // [heads][m]
+    float *part;                         // of rows (keys) that are cut: dq [item][head][row of the block][D]; dkv [item][kv head][key][2][D]
+    float *part_table;                   // [item][head][buckets]
+    int groups, mode, vec;
+};
+
+struct grad_choice {
+    attn_mapping rows;
+    int keys_level;
+    bool keys_cut;
+    size_t delta, part, table;           // bytes; the parts of dQ and of dK, dV use the same place one after the other
+};
+template <typename T>
+sp_status attn_backward(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStream_t st);
