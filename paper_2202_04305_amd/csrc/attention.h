@@ -11,6 +11,13 @@ constexpr int kAttnLevels = 28;
 //
 // A block of many rows reads a row of K and V once for all of them, and is worth it where neighbouring rows store mostly the same
 // columns (bands, sequences, shared prefixes); a row by itself where they do not.
+struct attn_stretch {                    // what a workgroup has to know of its item, in one load
+    int32_t block, chunk0;               // the block and its first chunk
+    int32_t c0, c1;                      // the item's chunks
+    int32_t first, count;                // the block's columns: place of the first one in cols (br = 1: in crd), how many places
+    int32_t whole, pad;                  // the block's only item
+};
+
 struct sp_attn_plan {
     int br;
     int64_t m, n;                        // rows and columns as this plan sees them
@@ -22,29 +29,29 @@ struct sp_attn_plan {
     int32_t *cols;                       // DEVICE [nchunks * 64]; behind a block's last column: that column again, without pairs
     uint64_t *bits;                      // DEVICE [nchunks * br]: bit c of word r of a chunk: row r of the block stores column c
     uint8_t *state;                      // DEVICE [nchunks * br / 32]: of the 32 rows' pairs of a chunk 0 = none, 1 = some, 2 = all are stored
-    // Work items: a block's chunks in stretches of at most `4 << level` of them (a block without any is one item).  The last
-    // level's items are the blocks.
+    // Work items: a block's chunks in stretches of at most attn_level_chunks(level) of them (a block without any is one item).
+    // The last level's items are the blocks.
     int levels;
     int64_t items[kAttnLevels];
     int32_t *item0[kAttnLevels];         // DEVICE [nblocks + 1]: first item of every block
-    int32_t *item_block[kAttnLevels];    // DEVICE [items]
+    attn_stretch *item[kAttnLevels];     // DEVICE [items]
     size_t bytes;
 };
 
-static inline int attn_level_chunks(int level) { return 4 << level; }
+static inline __host__ __device__ int attn_level_chunks(int level) { return 8 << level; }
 
 // A plan at one level, as kernels take it.
 struct attn_plan_view {
-    const int32_t *rowptr, *crd, *chunk0, *cols, *item0, *item_block;
+    const int32_t *rowptr, *crd, *chunk0, *cols, *item0;
+    const attn_stretch *item;
     const uint64_t *bits;
     const uint8_t *state;
     int64_t m, n;
-    int br, per_item;                    // rows of a block, chunks of an item
+    int br;
 };
 static inline attn_plan_view attn_view(const sp_attn_plan *p, int level)
 {
-    return {p->rowptr, p->crd, p->chunk0, p->cols, p->item0[level], p->item_block[level], p->bits, p->state, p->m, p->n, p->br,
-            attn_level_chunks(level)};
+    return {p->rowptr, p->crd, p->chunk0, p->cols, p->item0[level], p->item[level], p->bits, p->state, p->m, p->n, p->br};
 }
 
 // The problem as kernels take it.
@@ -60,12 +67,14 @@ struct attn_args {
     int16_t border[64];                  // far bucket k begins at distance border[k - 1]; distances from `last` on share a bucket
 };
 
-// The level whose items keep the chip busy: at least `want` workgroups where the pattern has as many, and as few parts to be joined
-// as that allows.
-static inline int attn_pick_level(const sp_attn_plan *p, int64_t groups_per_item, int64_t want)
+// How finely the blocks are cut: an item has at most what one of about 512 places for a workgroup (two on each compute unit) gets of
+// the whole work, give or take, so that no long block is left running by itself, and blocks are otherwise left whole: the parts of a
+// row that is cut are written and read again in f32.
+static inline int attn_pick_level(const sp_attn_plan *p, int64_t groups_per_item)
 {
-    int level = p->levels - 1;
-    while (level > 0 && p->items[level] * groups_per_item < want) --level;
+    const double share = 1.25 * (double)p->nchunks * (double)groups_per_item / 512;
+    int level = 0;
+    while (level + 1 < p->levels && attn_level_chunks(level + 1) <= share) ++level;
     return level;
 }
 

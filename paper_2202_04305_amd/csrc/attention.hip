@@ -5,12 +5,14 @@
 
 namespace {
 
+int padded(int D) { return (D + 3) & ~3; }
+
 forward_choice choose(const sp_attn_plan *plan, const attn_args &a)
 {
     forward_choice c;
     (attn_mapping &)c = attn_map(plan, a);
     const size_t rows = c.cut ? (size_t)plan->items[c.level] * a.H * plan->br : 0;
-    c.part = (rows * a.D * 4 + 255) & ~(size_t)255;
+    c.part = (rows * padded(a.D) * 4 + 255) & ~(size_t)255;
     c.part_stat = (rows * 8 + 255) & ~(size_t)255;
     return c;
 }
@@ -20,10 +22,10 @@ grad_choice choose(const sp_tensor *S, const attn_args &a)
     const sp_attn_plan *rows = S->attention[0], *keys = S->attention[1];
     grad_choice c;
     c.rows = attn_map(rows, a);
-    c.keys_level = attn_pick_level(keys, a.Hk, 1024);
+    c.keys_level = attn_pick_level(keys, a.Hk);
     c.keys_cut = keys->items[c.keys_level] > keys->nblocks;
-    const size_t p1 = c.rows.cut ? (size_t)rows->items[c.rows.level] * a.H * rows->br * a.D * 4 : 0;
-    const size_t p2 = c.keys_cut ? (size_t)keys->items[c.keys_level] * a.Hk * keys->br * 2 * a.D * 4 : 0;
+    const size_t p1 = c.rows.cut ? (size_t)rows->items[c.rows.level] * a.H * rows->br * padded(a.D) * 4 : 0;
+    const size_t p2 = c.keys_cut ? (size_t)keys->items[c.keys_level] * a.Hk * keys->br * 2 * padded(a.D) * 4 : 0;
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     c.delta = up((size_t)a.m * a.H * 4);
     c.part = up(p1 > p2 ? p1 : p2);
@@ -115,7 +117,7 @@ extern "C" sp_status sp_attention(const sp_tensor *S, const sp_attention_problem
     f.O = O; f.ldo = ldo; f.hdo = hdo; f.lse = lse;
     f.part = (float *)workspace;
     f.part_stat = (float *)((char *)workspace + c.part);
-    f.groups = c.groups; f.mode = c.mode;
+    f.groups = c.groups; f.mode = c.mode; f.pd = padded(a.D);
     attn_alignment rows(a.D, p->dtype == SP_F32 ? 4 : 2);
     rows.with(a.Q, a.ldq, a.hdq); rows.with(a.K, a.ldk, a.hdk); rows.with(a.V, a.ldv, a.hdv); rows.with(O, ldo, hdo);
     f.vec = rows.vec;
@@ -146,6 +148,7 @@ extern "C" sp_status sp_attention_grad(const sp_tensor *S, const sp_attention_pr
     if (need > 0 && !workspace) return SP_ERR_NULL;
     if (need > workspaceBytes || ((uintptr_t)workspace & 255)) return SP_ERR_SHAPE;
     f.g = *g;
+    f.pd = padded(a.D);
     f.delta = (const float *)workspace;
     f.part = (float *)((char *)workspace + c.delta);
     if (a.buckets && g->dTable) f.part_table = (float *)((char *)workspace + c.delta + c.part);

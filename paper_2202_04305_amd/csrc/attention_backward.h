@@ -202,7 +202,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                     const int d = 32 * x + 8 * b + 4 * (lane >> 5);
                     const attn_f32x4 v = {acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
                     if (item.whole) attn_store4(out, d, a.D, f.vec, v * a.scale);
-                    else attn_store4(f.part + place * a.D, d, a.D, f.vec, v);
+                    else attn_store4(f.part + place * f.pd, d, f.pd, true, v);
                 }
         }
     } else {
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
 #pragma unroll
                 for (int x = 0; x < WN; ++x) v += *(attn_f32x4 *)(sums + (x * 32 + mine) * DT + 4 * ((d >> 2) ^ (mine & 7)));
                 if (item.whole) attn_store4((T *)f.g.dQ + row2 * f.g.lddq + head2 * f.g.hddq, d, a.D, f.vec, v * a.scale);
-                else attn_store4(f.part + place2 * a.D, d, a.D, f.vec, v);
+                else attn_store4(f.part + place2 * f.pd, d, f.pd, true, v);
             }
         }
         again = 0;
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
             const int d = lane + 64 * k;
             if (d >= a.D) continue;
             if (item.whole) ((T *)f.g.dQ)[i * f.g.lddq + h * f.g.hddq + d] = (T)(one[k] * a.scale);
-            else f.part[at1 * a.D + d] = one[k];
+            else f.part[at1 * f.pd + d] = one[k];
         }
     }
 }
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     uint64_t again = __builtin_amdgcn_ballot_w64(valid && !(odd == 0.f));
     again |= again >> 32;
     if (valid && !(again >> (lane & 31) & 1)) {
-        float *part = f.part + ((item.part * a.Hk + kv) * p.br + r) * 2 * a.D;
+        float *part = f.part + ((item.part * a.Hk + kv) * p.br + r) * 2 * f.pd;
 #pragma unroll
         for (int x = 0; x < tile::kBlocks; ++x)
 #pragma unroll
@@ -420,8 +420,8 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
                     attn_store4((T *)f.g.dK + key * f.g.lddk + kv * f.g.hddk, d, a.D, f.vec, k4 * a.scale);
                     attn_store4((T *)f.g.dV + key * f.g.lddv + kv * f.g.hddv, d, a.D, f.vec, v4);
                 } else {
-                    attn_store4(part, d, a.D, f.vec, k4);
-                    attn_store4(part + a.D, d, a.D, f.vec, v4);
+                    attn_store4(part, d, f.pd, true, k4);
+                    attn_store4(part + f.pd, d, f.pd, true, v4);
                 }
             }
     }
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
         float k1[kAttnPer] = {0}, v1[kAttnPer] = {0};
         for (int g = kv * a.G; g < (kv + 1) * a.G; ++g)
             attn_row_dkv<T>(a, p, item.block, rr, item.c0, item.c1, j, g, lane, (const T *)f.g.dO, f.g.lddo, f.g.hddo, f.g.lse, f.delta, k1, v1);
-        float *part = f.part + ((item.part * a.Hk + kv) * p.br + rr) * 2 * a.D;
+        float *part = f.part + ((item.part * a.Hk + kv) * p.br + rr) * 2 * f.pd;
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) {
             const int d = lane + 64 * k;
@@ -442,15 +442,15 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
                 ((T *)f.g.dV)[j * f.g.lddv + kv * f.g.hddv + d] = (T)v1[k];
             } else {
                 part[d] = k1[k];
-                part[a.D + d] = v1[k];
+                part[f.pd + d] = v1[k];
             }
         }
     }
 }
 
-// Rows (dq: of a head; dkv: keys of a kv head) that were cut into several items: their parts added in order.  PER: vectors of D numbers
-// for a row (dq 1: dQ; dkv 2: dK, dV), of which the first is scaled.
-template <typename T, int PER>
+// Rows (dq: of a head; dkv: keys of a kv head) that were cut into several items: their parts added in a fixed order.  PER: vectors of D
+// numbers for a row (dq 1: dQ; dkv 2: dK, dV), of which the first is scaled.
+template <typename T, int LP, int PER>
 __global__ __launch_bounds__(kThreads) void join_kernel(grad_args f, int64_t rows, int heads)
 {
     const attn_plan_view &p = f.p;
@@ -464,11 +464,10 @@ __global__ __launch_bounds__(kThreads) void join_kernel(grad_args f, int64_t row
     for (int v = 0; v < PER; ++v) {
         T *out = PER == 1 ? (T *)f.g.dQ + i * f.g.lddq + h * f.g.hddq
                           : v == 0 ? (T *)f.g.dK + i * f.g.lddk + h * f.g.hddk : (T *)f.g.dV + i * f.g.lddv + h * f.g.hddv;
-        for (int d = lane; d < D; d += 64) {
-            float sum = 0;
-            for (int k = 0; k < parts; ++k) sum += f.part[((((int64_t)(first + k) * heads + h) * p.br + i % p.br) * PER + v) * D + d];
-            out[d] = (T)(v == 0 ? sum * f.a.scale : sum);
-        }
+        const attn_f32x4 sum = attn_add_parts<LP>(parts, f.pd, lane, [&](int k) {
+            return f.part + ((((int64_t)(first + k) * heads + h) * p.br + i % p.br) * PER + v) * f.pd;
+        }, [](int) { return 1.f; });
+        if (lane < LP) attn_store4(out, 4 * lane, D, f.vec, v == 0 ? sum * f.a.scale : sum);
     }
 }
 
@@ -543,7 +542,7 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
         const int64_t items = rows->items[c.rows.level];
         if (pos) SP_TRY((launch_dq_mode<T, DT, true>(f, c.rows, items, st)));
         else SP_TRY((launch_dq_mode<T, DT, false>(f, c.rows, items, st)));
-        if (c.rows.cut) hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)ceil_div(a.m * a.H, 4)), dim3(kThreads), 0, st, f, a.m, a.H);
+        if (c.rows.cut) hipLaunchKernelGGL((join_kernel<T, DT / 4, 1>), dim3((unsigned)ceil_div(a.m * a.H, 4)), dim3(kThreads), 0, st, f, a.m, a.H);
         if (f.part_table) hipLaunchKernelGGL(table_kernel<T>, dim3((unsigned)(a.buckets * a.H)), dim3(kThreads), 0, st, f, items);
         SP_HIP(hipGetLastError());
     }
@@ -552,7 +551,7 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
         const int64_t items = keys->items[c.keys_level];
         if (pos) SP_TRY((launch_dkv_mode<T, DT, true>(f, keys->br, items, st)));
         else SP_TRY((launch_dkv_mode<T, DT, false>(f, keys->br, items, st)));
-        if (c.keys_cut) hipLaunchKernelGGL((join_kernel<T, 2>), dim3((unsigned)ceil_div(a.n * a.Hk, 4)), dim3(kThreads), 0, st, f, a.n, a.Hk);
+        if (c.keys_cut) hipLaunchKernelGGL((join_kernel<T, DT / 4, 2>), dim3((unsigned)ceil_div(a.n * a.Hk, 4)), dim3(kThreads), 0, st, f, a.n, a.Hk);
         SP_HIP(hipGetLastError());
     }
     return SP_OK;

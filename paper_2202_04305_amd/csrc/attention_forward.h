@@ -176,7 +176,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
                     const int d = 32 * x + 8 * b + 4 * (lane >> 5);
                     const attn_f32x4 v = {acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
                     if (item.whole) attn_store4(out, d, a.D, f.vec, v * inv);
-                    else if (total != 0) attn_store4(f.part + place * a.D, d, a.D, f.vec, v);
+                    else if (total != 0) attn_store4(f.part + place * f.pd, d, f.pd, true, v);
                 }
         }
     } else {
@@ -225,12 +225,8 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
                 attn_f32x4 v = (attn_f32x4)(0.f);
 #pragma unroll
                 for (int x = 0; x < WN; ++x) v += *(attn_f32x4 *)(sums + (x * 32 + mine) * DT + 4 * ((d >> 2) ^ (mine & 7))) * w[x];
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (d + c < a.D) {
-                        if (item.whole) out2[d + c] = (T)(v[c] * inv);
-                        else if (sum != 0) f.part[place2 * a.D + d + c] = v[c];
-                    }
+                if (item.whole) attn_store4(out2, d, a.D, f.vec, v * inv);
+                else if (sum != 0) attn_store4(f.part + place2 * f.pd, d, f.pd, true, v);
             }
         }
         again = 0;
@@ -257,44 +253,55 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
             const int d = lane + 64 * k;
             if (d >= a.D) continue;
             if (item.whole) ((T *)f.O)[i * f.ldo + h * f.hdo + d] = (T)(one[k] * inv);
-            else f.part[at1 * a.D + d] = one[k];
+            else f.part[at1 * f.pd + d] = one[k];
         }
     }
 }
 
 // Rows whose columns were cut into several items: a wave for a row and head.  Each part has its maximum and total; the parts' sums are
-// weighted to the largest maximum, in the items' order.
-template <typename T>
+// weighted to the largest maximum and added in a fixed order.  Parts that have nothing of the row wrote no sums and are left out.
+template <typename T, int LP>
 __global__ __launch_bounds__(256) void join_kernel(forward_args f)
 {
+    __shared__ float s_weight[4][64];
+    __shared__ int s_part[4][64];
     const attn_args &a = f.a;
     const attn_plan_view &p = f.p;
-    const int lane = threadIdx.x & 63;
-    const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t x = (int64_t)blockIdx.x * 4 + wave;
     if (x >= a.m * a.H) return;
     const int64_t i = x / a.H, b = i / p.br;
-    const int h = (int)(x % a.H), r = (int)(i % p.br), first = p.item0[b], parts = p.item0[b + 1] - first;
+    const int h = (int)(x % a.H), first = p.item0[b], parts = p.item0[b + 1] - first;
     if (parts == 1) return;
-    auto place = [&](int k) { return ((int64_t)(first + k) * a.H + h) * p.br + r; };
+    auto place = [&](int k) { return ((int64_t)(first + k) * a.H + h) * p.br + i % p.br; };
     float top = -INFINITY;
     for (int k = lane; k < parts; k += 64) top = fmaxf(top, f.part_stat[2 * place(k)]);
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     const float base = top == -INFINITY ? 0.f : top;
-    float acc[kAttnPer] = {0}, total = 0;
-    for (int k = 0; k < parts; ++k) {
-        const float t = f.part_stat[2 * place(k) + 1];
-        if (t == 0) continue;                            // this stretch has nothing of the row, and wrote nothing
-        const float w = attn_weight(f.part_stat[2 * place(k)], base);
+    float total = 0;
+    attn_f32x4 acc = (attn_f32x4)(0.f);
+    for (int k0 = 0; k0 < parts; k0 += 64) {
+        const int k = k0 + lane;
+        const float t = k < parts ? f.part_stat[2 * place(k) + 1] : 0.f;
+        const float w = t == 0 ? 0.f : attn_weight(f.part_stat[2 * place(k)], base);
         total += t * w;
-#pragma unroll
-        for (int y = 0; y < kAttnPer; ++y)
-            if (lane + 64 * y < a.D) acc[y] += f.part[place(k) * a.D + lane + 64 * y] * w;
+        const uint64_t some = __builtin_amdgcn_ballot_w64(t != 0);
+        if (t != 0) {
+            const int n = __builtin_popcountll(some & (((uint64_t)1 << lane) - 1));
+            s_weight[wave][n] = w;
+            s_part[wave][n] = k;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // the list is this wave's own
+        __builtin_amdgcn_wave_barrier();
+        acc += attn_add_parts<LP>(__builtin_popcountll(some), f.pd, lane, [&](int n) { return f.part + place(s_part[wave][n]) * f.pd; },
+                                  [&](int n) { return s_weight[wave][n]; });
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
+    total = attn_wave_sum(total);
     const float inv = total == 0 ? 0.f : 1.f / total;
-#pragma unroll
-    for (int y = 0; y < kAttnPer; ++y)
-        if (lane + 64 * y < a.D) ((T *)f.O)[i * f.ldo + h * f.hdo + lane + 64 * y] = (T)(acc[y] * inv);
+    if (lane < LP) attn_store4((T *)f.O + i * f.ldo + h * f.hdo, 4 * lane, a.D, f.vec, acc * inv);
     if (f.lse && lane == 0) f.lse[h * a.m + i] = total == 0 ? -INFINITY : top + __builtin_amdgcn_logf(total) * kLn2;
 }
 
@@ -329,17 +336,17 @@ sp_status attn_forward(const sp_attn_plan *plan, forward_args &f, const forward_
     const bool pos = f.a.buckets || f.a.causal || f.a.scale == 0;
     const int64_t items = plan->items[c.level];
     if (items * c.groups >= ((int64_t)1 << 31)) return SP_ERR_TOO_LARGE;
-    sp_status s;
-#define SPMI_FORWARD(DT) s = pos ? launch_mode<T, DT, true>(f, c, items, st) : launch_mode<T, DT, false>(f, c, items, st)
+#define SPMI_FORWARD(DT)                                                                                                          \
+    do {                                                                                                                          \
+        if (pos) SP_TRY((launch_mode<T, DT, true>(f, c, items, st)));                                                             \
+        else SP_TRY((launch_mode<T, DT, false>(f, c, items, st)));                                                                \
+        if (c.cut) hipLaunchKernelGGL((join_kernel<T, DT / 4>), dim3((unsigned)ceil_div(f.a.m * f.a.H, 4)), dim3(256), 0, st, f);  \
+    } while (0)
     if (f.a.D <= 32) SPMI_FORWARD(32);
     else if (f.a.D <= 64) SPMI_FORWARD(64);
     else if (f.a.D <= 128) SPMI_FORWARD(128);
     else SPMI_FORWARD(256);
 #undef SPMI_FORWARD
-    SP_TRY(s);
-    if (c.cut) {
-        hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)ceil_div(f.a.m * f.a.H, 4)), dim3(256), 0, st, f);
-        SP_HIP(hipGetLastError());
-    }
+    SP_HIP(hipGetLastError());
     return SP_OK;
 }

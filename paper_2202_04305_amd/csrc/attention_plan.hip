@@ -181,15 +181,27 @@ __global__ __launch_bounds__(kThreads) void items_kernel(const int32_t *__restri
     if (b > nblocks) return;
     const int k = b < nblocks ? chunk0[b + 1] - chunk0[b] : 0;
     for (int l = 0; l < levels; ++l) {
-        const int per = 4 << l;
+        const int per = attn_level_chunks(l);
         t.item0[l][b] = b < nblocks ? (k <= per ? 1 : (k + per - 1) / per) : 0;
     }
 }
-__global__ __launch_bounds__(kThreads) void item_blocks_kernel(const int32_t *__restrict__ item0, int64_t nblocks, int32_t *__restrict__ item_block)
+__global__ __launch_bounds__(kThreads) void stretches_kernel(const int32_t *__restrict__ item0, const int32_t *__restrict__ chunk0,
+                                                             const int32_t *__restrict__ rowptr, int64_t nblocks, int br, int per,
+                                                             attn_stretch *__restrict__ items)
 {
     const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (b >= nblocks) return;
-    for (int32_t x = item0[b]; x < item0[b + 1]; ++x) item_block[x] = (int32_t)b;
+    const int32_t i0 = item0[b], i1 = item0[b + 1], k0 = chunk0[b], k1 = chunk0[b + 1];
+    for (int32_t x = i0; x < i1; ++x) {
+        attn_stretch s;
+        s.block = (int32_t)b; s.chunk0 = k0;
+        s.c0 = k0 + (x - i0) * per;
+        s.c1 = k1 - s.c0 < per ? k1 : s.c0 + per;
+        s.first = br == 1 ? rowptr[b] : k0 * kAttnChunk;
+        s.count = br == 1 ? rowptr[b + 1] - rowptr[b] : (k1 - k0) * kAttnChunk;
+        s.whole = i1 - i0 == 1; s.pad = 0;
+        items[x] = s;
+    }
 }
 
 unsigned blocks_for(int64_t n) { return (unsigned)(n > 0 ? ceil_div(n, kThreads) : 1); }
@@ -207,7 +219,7 @@ struct plan_scope {
     void drop() {
         if (!plan) return;
         mem.put(plan->rowptr); mem.put(plan->crd_own); mem.put(plan->chunk0); mem.put(plan->cols); mem.put(plan->bits); mem.put(plan->state);
-        for (int l = 0; l < kAttnLevels; ++l) { mem.put(plan->item0[l]); mem.put(plan->item_block[l]); }
+        for (int l = 0; l < kAttnLevels; ++l) { mem.put(plan->item0[l]); mem.put(plan->item[l]); }
         delete plan;
         plan = nullptr;
     }
@@ -333,9 +345,10 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
     SP_HIP(hipStreamSynchronize(st));
     for (int l = 0; l < p->levels; ++l) {
         p->items[l] = total[l];
-        p->item_block[l] = (int32_t *)scope.get((size_t)(total[l] > 0 ? total[l] : 1) * 4);
-        if (!p->item_block[l]) return SP_ERR_ALLOC;
-        hipLaunchKernelGGL(item_blocks_kernel, dim3(blocks_for(p->nblocks)), dim3(kThreads), 0, st, p->item0[l], p->nblocks, p->item_block[l]);
+        p->item[l] = (attn_stretch *)scope.get((size_t)(total[l] > 0 ? total[l] : 1) * sizeof(attn_stretch));
+        if (!p->item[l]) return SP_ERR_ALLOC;
+        hipLaunchKernelGGL(stretches_kernel, dim3(blocks_for(p->nblocks)), dim3(kThreads), 0, st, p->item0[l], p->chunk0, p->rowptr, p->nblocks, p->br,
+                           attn_level_chunks(l), p->item[l]);
         SP_HIP(hipGetLastError());
     }
     SP_HIP(hipStreamSynchronize(st));                    // temporaries go back, and another stream may use the plan from now on

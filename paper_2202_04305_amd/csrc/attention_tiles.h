@@ -155,26 +155,16 @@ struct attn_item {
     int64_t part;                        // number among all items
     bool whole;                          // the block's only item
     attn_columns cols;
-    int64_t count;                       // br = 1: columns of the row
+    int64_t count;                       // places of the block's columns; br = 1: columns of the row
 
     __device__ __forceinline__ attn_item(const attn_plan_view &p, int64_t item)
     {
+        const attn_stretch x = p.item[item];
         part = item;
-        block = p.item_block[item];
-        const int first = p.item0[block];
-        chunk0 = p.chunk0[block];
-        const int end = p.chunk0[block + 1];
-        whole = p.item0[block + 1] - first == 1;
-        c0 = chunk0 + (int)(item - first) * p.per_item;
-        c1 = c0 + p.per_item < end ? c0 + p.per_item : end;
-        if (p.br == 1) {
-            const int64_t s = p.rowptr[block];
-            count = p.rowptr[block + 1] - s;
-            cols = {p.crd + s, count - 1};
-        } else {
-            count = 0;
-            cols = {p.cols + (int64_t)chunk0 * kAttnChunk, (int64_t)(end - chunk0) * kAttnChunk - 1};
-        }
+        block = x.block; chunk0 = x.chunk0; c0 = x.c0; c1 = x.c1;
+        whole = x.whole != 0;
+        count = x.count;
+        cols = {(p.br == 1 ? p.crd : p.cols) + x.first, count - 1};
     }
     // the pairs of chunk c and row r of the block, and whether the 32 rows around r have none (0), some (1) or all (2) of them
     __device__ __forceinline__ uint64_t word(const attn_plan_view &p, int c, int r) const
@@ -286,7 +276,7 @@ static inline attn_mapping attn_map(const sp_attn_plan *plan, const attn_args &a
     const bool share = c.mode == kRowsTogether || c.mode == kHeadsTogether;
     c.wm = share ? 1 : 4;
     c.wn = share ? 4 : 1;
-    c.level = attn_pick_level(plan, c.groups, 1024);
+    c.level = attn_pick_level(plan, c.groups);
     c.cut = plan->items[c.level] > plan->nblocks;
     return c;
 }
@@ -320,8 +310,9 @@ struct forward_args {
     void *O;
     int64_t ldo, hdo;
     float *lse;
-    float *part, *part_stat;             // of rows that are cut: [item][head][row of the block][D] and [..][2] (maximum, total)
+    float *part, *part_stat;             // of rows that are cut: [item][head][row of the block][pd] and [..][2] (maximum, total)
     int groups, mode, vec;               // workgroups of an item; mapping; whether rows are made of whole aligned granules
+    int pd;                              // numbers of a row of a part: D rounded up to a multiple of 4
 };
 
 struct forward_choice : attn_mapping {
@@ -335,9 +326,9 @@ struct grad_args {
     attn_plan_view p;
     sp_attention_grads g;
     const float *delta;                  // [heads][m]
-    float *part;                         // of rows (keys) that are cut: dq [item][head][row of the block][D]; dkv [item][kv head][key][2][D]
+    float *part;                         // of rows (keys) that are cut: dq [item][head][row of the block][pd]; dkv [item][kv head][key][2][pd]
     float *part_table;                   // [item][head][buckets]
-    int groups, mode, vec;
+    int groups, mode, vec, pd;
 };
 
 struct grad_choice {
@@ -348,3 +339,32 @@ struct grad_choice {
 };
 template <typename T>
 sp_status attn_backward(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStream_t st);
+
+// ---- parts of rows that were cut ----------------------------------------------------------------------------------------------
+// Sums of f32 rows of pd numbers (a multiple of 4, at most 256), by a wave: LP lanes take a row, 4 numbers each, and 64 / LP rows are
+// taken at a time; `count` rows in all, row k at at(k) with weight weight(k).  The result is in every group of LP lanes.
+template <int LP, typename AT, typename WEIGHT>
+__device__ __forceinline__ attn_f32x4 attn_add_parts(int count, int pd, int lane, AT at, WEIGHT weight)
+{
+    constexpr int S = 64 / LP;
+    const int l = lane % LP, s = lane / LP;
+    attn_f32x4 sum = (attn_f32x4)(0.f);
+    for (int k0 = 0; k0 < count; k0 += 4 * S) {
+        attn_f32x4 v[4];
+        float w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = k0 + u * S + s;
+            const bool there = k < count && 4 * l < pd;
+            w[u] = k < count ? weight(k) : 0.f;
+            v[u] = there ? *(const attn_f32x4 *)(at(k) + 4 * l) : (attn_f32x4)(0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sum += v[u] * w[u];
+    }
+#pragma unroll
+    for (int d = LP; d < 64; d <<= 1)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[c] += __shfl_xor(sum[c], d, 64);
+    return sum;
+}
