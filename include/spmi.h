@@ -183,7 +183,7 @@ sp_status sp_sddmm(const sp_tensor *S, const void *A, int64_t lda, const void *B
 typedef struct sp_attention_problem {
     int dtype;                          /* SP_F32, SP_F16 or SP_BF16: of Q, K, V, O, table and all gradients.  Sums are in f32. */
     int heads, kvHeads;                 /* heads: a multiple of kvHeads                                                  */
-    int headDim;                        /* 1 .. 256                                                                      */
+    int headDim;                        /* 1 .. 256; f32: 1 .. 128                                                       */
     int causal;                         /* 1: only keys with kpos[j] <= qpos[i]                                          */
     int buckets, maxDistance, bidirectional;
     double scale;

@@ -35,15 +35,18 @@ struct sp_attn_plan {
     int64_t items[kAttnLevels];
     int32_t *item0[kAttnLevels];         // DEVICE [nblocks + 1]: first item of every block
     attn_stretch *item[kAttnLevels];     // DEVICE [items]
+    int64_t cut[kAttnLevels];            // blocks of several items,
+    int32_t *cut_block[kAttnLevels];     // DEVICE [cut]: ascending
     size_t bytes;
 };
 
-static inline __host__ __device__ int attn_level_chunks(int level) { return 8 << level; }
+static inline __host__ __device__ int attn_level_chunks(int level) { return 2 << level; }
 
 // A plan at one level, as kernels take it.
 struct attn_plan_view {
     const int32_t *rowptr, *crd, *chunk0, *cols, *item0;
     const attn_stretch *item;
+    const int32_t *cut_block;
     const uint64_t *bits;
     const uint8_t *state;
     int64_t m, n;
@@ -51,7 +54,7 @@ struct attn_plan_view {
 };
 static inline attn_plan_view attn_view(const sp_attn_plan *p, int level)
 {
-    return {p->rowptr, p->crd, p->chunk0, p->cols, p->item0[level], p->item[level], p->bits, p->state, p->m, p->n, p->br};
+    return {p->rowptr, p->crd, p->chunk0, p->cols, p->item0[level], p->item[level], p->cut_block[level], p->bits, p->state, p->m, p->n, p->br};
 }
 
 // The problem as kernels take it.
@@ -67,15 +70,20 @@ struct attn_args {
     int16_t border[64];                  // far bucket k begins at distance border[k - 1]; distances from `last` on share a bucket
 };
 
-// How finely the blocks are cut: an item has at most what one of about 512 places for a workgroup (two on each compute unit) gets of
-// the whole work, give or take, so that no long block is left running by itself, and blocks are otherwise left whole: the parts of a
-// row that is cut are written and read again in f32.
-static inline int attn_pick_level(const sp_attn_plan *p, int64_t groups_per_item)
+// How finely the blocks are cut.  With `groups` workgroups an item, `chunk_us` for a chunk of one and `row_bytes` for a part of one row
+// of one item (written and read again in f32), the level with the least of: what one of 512 places for a workgroup (two on each
+// compute unit) gets of the work, plus the longest item, plus the parts' traffic and the launch that joins them.
+static inline int attn_pick_level(const sp_attn_plan *p, int64_t groups, double chunk_us, double row_bytes)
 {
-    const double share = 1.25 * (double)p->nchunks * (double)groups_per_item / 512;
-    int level = 0;
-    while (level + 1 < p->levels && attn_level_chunks(level + 1) <= share) ++level;
-    return level;
+    int best = p->levels - 1;
+    double least = 0;
+    for (int l = p->levels - 1; l >= 0; --l) {
+        const double longest = p->max_chunks < attn_level_chunks(l) ? (double)p->max_chunks : (double)attn_level_chunks(l);
+        const double extra = p->cut[l] ? 4 + (double)(p->items[l] - p->nblocks + p->cut[l]) * row_bytes * p->br * 2 / 4e6 : 0;
+        const double us = chunk_us * ((double)p->nchunks * (double)groups / 512 + longest) + extra;
+        if (l == p->levels - 1 || us < least) { least = us; best = l; }
+    }
+    return best;
 }
 
 // ---- device -----------------------------------------------------------------------------------------------------------------
@@ -99,20 +107,28 @@ __device__ __forceinline__ int attn_bucket(const attn_args &a, int r)
     return base + b;
 }
 
-// Calls f(column) for every column that row r of block b stores in the block's chunks [c0, c1); for a whole wave, f's argument uniform.
+// The bucket of all distances from the last border on, ahead of the query or behind it.
+__device__ __forceinline__ int attn_far_bucket(const attn_args &a, bool ahead)
+{
+    return ahead ? (a.bidirectional ? 2 * a.side - 1 : 0) : a.side - 1;
+}
+
+// Calls f(column) for every column that row r of block b stores in the block's chunks [c0, c1), until it returns false; for a whole
+// wave, f's argument and answer uniform.
 template <typename F>
 __device__ __forceinline__ void attn_for_columns(const attn_plan_view &p, int64_t b, int r, int c0, int c1, F f)
 {
     if (p.br == 1) {
         const int64_t s = p.rowptr[b], e = p.rowptr[b + 1], first = p.chunk0[b];
         const int64_t lo = s + (c0 - first) * kAttnChunk, hi = s + (c1 - first) * kAttnChunk;
-        for (int64_t x = lo; x < (hi < e ? hi : e); ++x) f(p.crd[x]);
+        for (int64_t x = lo; x < (hi < e ? hi : e); ++x) if (!f(p.crd[x])) return;
         return;
     }
     for (int c = c0; c < c1; ++c) {
         const uint64_t w = p.bits[(int64_t)c * p.br + r];
         uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)w), hi = __builtin_amdgcn_readfirstlane((uint32_t)(w >> 32));
-        for (uint64_t left = ((uint64_t)hi << 32) | lo; left; left &= left - 1) f(p.cols[(int64_t)c * kAttnChunk + __builtin_ctzll(left)]);
+        for (uint64_t left = ((uint64_t)hi << 32) | lo; left; left &= left - 1)
+            if (!f(p.cols[(int64_t)c * kAttnChunk + __builtin_ctzll(left)])) return;
     }
 }
 
@@ -152,6 +168,15 @@ __device__ __forceinline__ float attn_score(const attn_args &a, float dot, int64
 __device__ __forceinline__ float attn_weight(float s, float top) { return __builtin_amdgcn_exp2f((s - top) * kLog2e); }
 __device__ __forceinline__ bool attn_left_out(const attn_args &a, int64_t i, int64_t j) { return a.causal && a.kpos[j] > a.qpos[i]; }
 
+// Is any of a row's D sums still a number?  (What is not a number stays so, and a row of nothing else is done.)
+__device__ __forceinline__ bool attn_any_number(const float (&x)[kAttnPer], int D, int lane)
+{
+    bool any = false;
+#pragma unroll
+    for (int k = 0; k < kAttnPer; ++k) any = any || (lane + 64 * k < D && x[k] == x[k]);
+    return __builtin_amdgcn_ballot_w64(any) != 0;
+}
+
 // top (running maximum), total and acc = sum of e^(s - top) V over a stretch of a row's columns
 template <typename T>
 __device__ __forceinline__ void attn_row_forward(const attn_args &a, const attn_plan_view &p, int64_t b, int r, int c0, int c1, int64_t i, int h,
@@ -164,11 +189,11 @@ __device__ __forceinline__ void attn_row_forward(const attn_args &a, const attn_
 #pragma unroll
     for (int k = 0; k < kAttnPer; ++k) acc[k] = 0;
     attn_for_columns(p, b, r, c0, c1, [&](int64_t j) {
-        if (attn_left_out(a, i, j)) return;
+        if (attn_left_out(a, i, j)) return true;
         float x[kAttnPer];
         attn_load_row((const T *)a.K + j * a.ldk + g * a.hdk, a.D, lane, x);
         const float s = attn_score<T>(a, attn_dot(q, x), i, j, h);
-        if (s == -INFINITY) return;                      // weight 0
+        if (s == -INFINITY) return true;                 // weight 0
         attn_load_row((const T *)a.V + j * a.ldv + g * a.hdv, a.D, lane, x);
         const float up = s > top ? s : top;              // not a number: stays with the old maximum, the weight carries it
         const float old = top == -INFINITY ? 0.f : attn_weight(top, up), w = attn_weight(s, up == -INFINITY ? 0.f : up);
@@ -176,6 +201,7 @@ __device__ __forceinline__ void attn_row_forward(const attn_args &a, const attn_
         total = total * old + w;
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) acc[k] = acc[k] * old + w * x[k];
+        return attn_any_number(acc, a.D, lane);
     });
 }
 
@@ -192,15 +218,16 @@ __device__ __forceinline__ void attn_row_dq(const attn_args &a, const attn_plan_
     for (int k = 0; k < kAttnPer; ++k) acc[k] = 0;
     if (lse == -INFINITY) lse = INFINITY;                // no weight left
     attn_for_columns(p, b, r, c0, c1, [&](int64_t j) {
-        if (attn_left_out(a, i, j)) return;
+        if (attn_left_out(a, i, j)) return true;
         float x[kAttnPer], y[kAttnPer];
         attn_load_row((const T *)a.K + j * a.ldk + g * a.hdk, a.D, lane, x);
         attn_load_row((const T *)a.V + j * a.ldv + g * a.hdv, a.D, lane, y);
         const float s = attn_score<T>(a, attn_dot(q, x), i, j, h);
-        if (s == -INFINITY) return;
+        if (s == -INFINITY) return true;
         const float ds = attn_weight(s, lse) * (attn_dot(go, y) - delta);
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) acc[k] += ds * x[k];
+        return attn_any_number(acc, a.D, lane);
     });
 }
 
@@ -216,16 +243,17 @@ __device__ __forceinline__ void attn_row_dkv(const attn_args &a, const attn_plan
     attn_load_row((const T *)a.K + j * a.ldk + g * a.hdk, a.D, lane, kx);
     attn_load_row((const T *)a.V + j * a.ldv + g * a.hdv, a.D, lane, vx);
     attn_for_columns(p, b, r, c0, c1, [&](int64_t i) {
-        if (attn_left_out(a, i, j)) return;
+        if (attn_left_out(a, i, j)) return true;
         float x[kAttnPer], y[kAttnPer];
         attn_load_row((const T *)a.Q + i * a.ldq + h * a.hdq, a.D, lane, x);
         attn_load_row(dO + i * lddo + h * hddo, a.D, lane, y);
         const float s = attn_score<T>(a, attn_dot(kx, x), i, j, h);
-        if (s == -INFINITY) return;
+        if (s == -INFINITY) return true;
         const float L = lse[h * a.m + i];
         const float w = attn_weight(s, L == -INFINITY ? INFINITY : L);
         const float ds = w * (attn_dot(vx, y) - delta[h * a.m + i]);
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) { dk[k] += ds * x[k]; dv[k] += w * y[k]; }
+        return attn_any_number(dk, a.D, lane) || attn_any_number(dv, a.D, lane);
     });
 }

@@ -7,29 +7,33 @@ namespace {
 
 int padded(int D) { return (D + 3) & ~3; }
 
-forward_choice choose(const sp_attn_plan *plan, const attn_args &a)
+forward_choice choose(const sp_attn_plan *plan, const attn_args &a, int size)
 {
     forward_choice c;
-    (attn_mapping &)c = attn_map(plan, a);
+    (attn_mapping &)c = attn_map(plan, a, size, 2);
     const size_t rows = c.cut ? (size_t)plan->items[c.level] * a.H * plan->br : 0;
     c.part = (rows * padded(a.D) * 4 + 255) & ~(size_t)255;
     c.part_stat = (rows * 8 + 255) & ~(size_t)255;
     return c;
 }
 
-grad_choice choose(const sp_tensor *S, const attn_args &a)
+grad_choice choose(const sp_tensor *S, const attn_args &a, int size, bool table)
 {
     const sp_attn_plan *rows = S->attention[0], *keys = S->attention[1];
     grad_choice c;
-    c.rows = attn_map(rows, a);
-    c.keys_level = attn_pick_level(keys, a.Hk);
-    c.keys_cut = keys->items[c.keys_level] > keys->nblocks;
+    c.rows = attn_map(rows, a, size, 3);
+    // the bias's gradient from sums that need a row's whole D: rows are not cut then, and the sums have to fit the LDS
+    const int row = (a.D <= 32 ? 32 : a.D <= 64 ? 64 : a.D <= 128 ? 128 : 256) * size;
+    c.exact = table && size == 2 && attn_dq_lds(a, c.rows, row, true, true, true) <= kAttnLds;
+    if (c.exact) { c.rows.level = rows->levels - 1; c.rows.cut = false; }
+    c.keys_level = attn_pick_level(keys, a.Hk, attn_chunk_us(a.D, size, 4) * a.G * (keys->br == 128 ? 1 : 0.7), 8.0 * a.D * a.Hk);
+    c.keys_cut = keys->cut[c.keys_level] > 0;
     const size_t p1 = c.rows.cut ? (size_t)rows->items[c.rows.level] * a.H * rows->br * padded(a.D) * 4 : 0;
     const size_t p2 = c.keys_cut ? (size_t)keys->items[c.keys_level] * a.Hk * keys->br * 2 * padded(a.D) * 4 : 0;
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     c.delta = up((size_t)a.m * a.H * 4);
     c.part = up(p1 > p2 ? p1 : p2);
-    c.table = up(a.buckets ? (size_t)rows->items[c.rows.level] * a.H * a.buckets * 4 : 0);
+    c.table = up(table ? (size_t)rows->items[c.rows.level] * a.H * a.buckets * 4 : 0);
     return c;
 }
 
@@ -57,7 +61,8 @@ static sp_status check_problem(const sp_tensor *S, const sp_attention_problem *p
     if (!S || !p) return SP_ERR_NULL;
     if (S->enc.rank != 2) return SP_ERR_RANK;
     if (p->dtype != (int)SP_F32 && p->dtype != (int)SP_F16 && p->dtype != (int)SP_BF16) return SP_ERR_DTYPE;
-    if (p->heads < 1 || p->kvHeads < 1 || p->heads % p->kvHeads || p->headDim < 1 || p->headDim > 256 || p->heads > 65535) return SP_ERR_SHAPE;
+    if (p->heads < 1 || p->kvHeads < 1 || p->heads % p->kvHeads || p->headDim < 1 || p->heads > 65535) return SP_ERR_SHAPE;
+    if (p->headDim > (p->dtype == (int)SP_F32 ? 128 : 256)) return SP_ERR_SHAPE;
     if ((p->causal != 0 && p->causal != 1) || (p->bidirectional != 0 && p->bidirectional != 1)) return SP_ERR_UNSUPPORTED;
     if (p->buckets < 0 || p->buckets > 64) return SP_ERR_SHAPE;
     if (p->buckets) {
@@ -86,10 +91,13 @@ extern "C" sp_status sp_attention_workspace(const sp_tensor *S, const sp_attenti
     attn_args a;
     SP_TRY(check_problem(S, p, grad, &a));
     if (grad) {
-        const grad_choice c = choose(S, a);
-        *bytes = c.delta + c.part + c.table;
+        for (int table = 0; table <= (a.buckets > 0); ++table) {         // with and without the table's gradient
+            const grad_choice c = choose(S, a, p->dtype == SP_F32 ? 4 : 2, table != 0);
+            const size_t need = c.delta + c.part + c.table;
+            if (need > *bytes) *bytes = need;
+        }
     } else {
-        const forward_choice c = choose(S->attention[0], a);
+        const forward_choice c = choose(S->attention[0], a, p->dtype == SP_F32 ? 4 : 2);
         *bytes = c.part + c.part_stat;
     }
     return SP_OK;
@@ -109,7 +117,8 @@ extern "C" sp_status sp_attention(const sp_tensor *S, const sp_attention_problem
     if (!pairs) a.buckets = a.causal = 0;                // nothing is read
     if (!a.buckets && !a.causal) a.qpos = a.kpos = nullptr;
     const sp_attn_plan *plan = S->attention[0];
-    const forward_choice c = choose(plan, a);
+    const int size = p->dtype == SP_F32 ? 4 : 2;
+    const forward_choice c = choose(plan, a, size);
     const size_t need = c.part + c.part_stat;
     if (need > 0 && !workspace) return SP_ERR_NULL;
     if (need > workspaceBytes || ((uintptr_t)workspace & 255)) return SP_ERR_SHAPE;
@@ -118,7 +127,7 @@ extern "C" sp_status sp_attention(const sp_tensor *S, const sp_attention_problem
     f.part = (float *)workspace;
     f.part_stat = (float *)((char *)workspace + c.part);
     f.groups = c.groups; f.mode = c.mode; f.pd = padded(a.D);
-    attn_alignment rows(a.D, p->dtype == SP_F32 ? 4 : 2);
+    attn_alignment rows(a.D, size);
     rows.with(a.Q, a.ldq, a.hdq); rows.with(a.K, a.ldk, a.hdk); rows.with(a.V, a.ldv, a.hdv); rows.with(O, ldo, hdo);
     f.vec = rows.vec;
     hipStream_t st = (hipStream_t)stream;
@@ -143,16 +152,17 @@ extern "C" sp_status sp_attention_grad(const sp_tensor *S, const sp_attention_pr
     if (pairs && (!a.Q || !a.K || !a.V || ((a.buckets || a.causal) && (!a.qpos || !a.kpos)) || (a.buckets && !a.table))) return SP_ERR_NULL;
     if (a.m > 0 && (!g->O || !g->lse || !g->dO || !g->dQ)) return SP_ERR_NULL;
     if (a.n > 0 && (!g->dK || !g->dV)) return SP_ERR_NULL;
-    const grad_choice c = choose(S, a);
+    const int size = p->dtype == SP_F32 ? 4 : 2;
+    const grad_choice c = choose(S, a, size, a.buckets && g->dTable);
     const size_t need = c.delta + c.part + c.table;
     if (need > 0 && !workspace) return SP_ERR_NULL;
     if (need > workspaceBytes || ((uintptr_t)workspace & 255)) return SP_ERR_SHAPE;
     f.g = *g;
-    f.pd = padded(a.D);
+    f.pd = padded(a.D); f.exact = c.exact;
     f.delta = (const float *)workspace;
     f.part = (float *)((char *)workspace + c.delta);
     if (a.buckets && g->dTable) f.part_table = (float *)((char *)workspace + c.delta + c.part);
-    attn_alignment rows(a.D, p->dtype == SP_F32 ? 4 : 2);
+    attn_alignment rows(a.D, size);
     rows.with(a.Q, a.ldq, a.hdq); rows.with(a.K, a.ldk, a.hdk); rows.with(a.V, a.ldv, a.hdv);
     rows.with(g->O, g->ldo, g->hdo); rows.with(g->dO, g->lddo, g->hddo);
     rows.with(g->dQ, g->lddq, g->hddq); rows.with(g->dK, g->lddk, g->hddk); rows.with(g->dV, g->lddv, g->hddv);

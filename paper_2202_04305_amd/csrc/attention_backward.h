@@ -34,15 +34,18 @@ __global__ __launch_bounds__(kThreads) void delta_kernel(grad_args f, float *__r
 }
 
 // dQ: the forward kernel's frame (items, gathered columns through LDS, tiles of 32 rows), with dO beside Q and V read as K is.
-// With a bias its gradient as well: every lane adds its pairs' ds to a place of its own for each bucket in LDS, so that no two
-// lanes ever add to one number; the lanes' sums are added in order at the end.
+//
+// With a bias its gradient as well: every lane adds its pairs' terms to a place of its own for each bucket in LDS, so that no two
+// lanes ever add to one number, and the lanes' sums are added in order at the end; tiles that share a bucket are summed in registers.
+// `exact`: the terms are p dP and p, and ds = p (dP - D) is made of the sums with each row's D = sum p dP.  A bucket's ds almost
+// cancel, and D from an O that was rounded to 16 bits would be most of their error (2.4e-3 of the gradient instead of 1.7e-3, the
+// rounding of the result).  Not exact (f32, whose O is not rounded): the terms are ds.
 template <typename T, int DT, int WM, int WN, int KW, bool POS>
 __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void dq_kernel(grad_args f)
 {
     typedef attn_tile<T, DT> tile;
     typedef typename tile::frag frag;
     constexpr int NT = 64 * WM * WN, KT = KW * WN, TILES = KW / 32;
-    constexpr int PIECES = KT * tile::kGranules / NT, ROWSTEP = NT / tile::kGranules;
     constexpr int STEP = KT > kAttnChunk ? KT / kAttnChunk : 1, SUB = KT < kAttnChunk ? kAttnChunk / KT : 1;
     extern __shared__ __align__(16) char lds[];
     attn_lds *sK = (attn_lds *)lds, *sV = sK + KT * tile::kRow;
@@ -65,16 +68,18 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     if (off == -INFINITY) off = INFINITY;                // no weight left
     if (!POS) off *= kLog2e;
     const float delta = f.delta[me.head * a.m + me.row];
-    int qp = 0;
+    int qp = 0, q_lo = 0, q_hi = 0;
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
-    float *hist = nullptr;
+    float *hist = nullptr;                               // [buckets][64] of ds or p dP, exact: then [buckets][64] of p
+    const int hist_size = a.buckets * 64 * (f.exact ? 2 : 1);
+    float far_x[2] = {0, 0}, far_p[2] = {0, 0};          // the far buckets behind and ahead
     if (POS) {
-        if (a.qpos) qp = a.qpos[me.row];
+        if (a.qpos) { qp = a.qpos[me.row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
         if (a.buckets) {
             bias = attn_lane_bias<T>(a, lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
             if (f.part_table) {
-                hist = (float *)(bias.table + a.buckets * bias.slots) + wave * a.buckets * 64;
-                for (int b = 0; b < a.buckets; ++b) hist[b * 64 + lane] = 0;
+                hist = (float *)(bias.table + a.buckets * bias.slots) + wave * hist_size;
+                for (int b = lane; b < hist_size; b += 64) hist[b] = 0;
             }
         }
     }
@@ -82,72 +87,105 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
 #pragma unroll
     for (int x = 0; x < tile::kBlocks; ++x) acc[x] = (attn_f32x16)(0.f);
 
+    const int64_t steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
+    attn_feed<T, DT, NT, KT, POS> feed;
+    feed.ldx = a.ldk; feed.ldy = a.ldv;
+    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk;
+    feed.pos = a.kpos; feed.sign = a.causal; feed.limit = q_hi;
+    feed.D = a.D; feed.vec = f.vec; feed.row = tid / tile::kGranules; feed.g = tid % tile::kGranules;
     const T *Kh = (const T *)a.K + (int64_t)me.kv * a.hdk, *Vh = (const T *)a.V + (int64_t)me.kv * a.hdv;
-    const int my_row = tid / tile::kGranules, my_g = tid % tile::kGranules;
-    const int64_t first = (int64_t)(item.c0 - item.chunk0) * kAttnChunk, steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
-    int32_t at[PIECES], pos_at = 0;
-    frag kf[PIECES], vf[PIECES];
-    int kp_next = 0;
-    auto fetch_columns = [&](int64_t step) {
-        const int64_t x = first + step * KT;
+    if (POS && a.causal && WM > 1) {
+        if (lane == 0) s_kpos[wave] = q_hi;
+        __syncthreads();
 #pragma unroll
-        for (int k = 0; k < PIECES; ++k) at[k] = item.cols.get(x + my_row + k * ROWSTEP);
-        if (POS && tid < KT) pos_at = item.cols.get(x + tid);
+        for (int w = 0; w < WM; ++w) feed.limit = s_kpos[w] > feed.limit ? s_kpos[w] : feed.limit;
+    }
+    auto my_chunk = [&](int64_t step, int &col0) {
+        col0 = (int)(step % SUB) * KT + wn * KW;
+        const int chunk = item.c0 + (int)(step / SUB) * STEP + col0 / kAttnChunk;
+        return busy && chunk < item.c1 ? chunk : -1;
     };
-    auto fetch_rows = [&]() {
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-            kf[k] = tile::granule(Kh + (int64_t)at[k] * a.ldk, my_g * tile::kPer, a.D, f.vec, true);
-            vf[k] = tile::granule(Vh + (int64_t)at[k] * a.ldv, my_g * tile::kPer, a.D, f.vec, true);
-        }
-        if (POS && a.kpos && tid < KT) kp_next = a.kpos[pos_at];
+    uint64_t word = 0, word_next = 0;
+    int state = 0, state_next = 0;
+    auto fetch_pairs = [&](int64_t step) {
+        int col0;
+        const int chunk = my_chunk(step, col0);
+        state_next = 0;
+        if (chunk >= 0) { state_next = item.state(p, chunk, r); word_next = item.word(p, chunk, r); }
     };
     if (steps > 0) {
-        fetch_columns(0);
-        fetch_rows();
-        if (steps > 1) fetch_columns(1);
+        feed.columns(0);
+        feed.advance();
+        if (steps > 1) feed.columns(1);
+        fetch_pairs(0);
+        feed.rows(Kh, Vh);
     }
     for (int64_t step = 0; step < steps; ++step) {
         __syncthreads();
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-            tile::put(sK, my_row + k * ROWSTEP, my_g, kf[k]);
-            tile::put(sV, my_row + k * ROWSTEP, my_g, vf[k]);
-        }
-        if (POS && tid < KT) s_kpos[tid] = kp_next;
+        feed.put(sK, sV);
+        if (POS && tid < KT) s_kpos[tid] = feed.arrived;
         __syncthreads();
+        word = word_next; state = state_next;
         if (step + 1 < steps) {
-            fetch_rows();
-            if (step + 2 < steps) fetch_columns(step + 2);
+            feed.advance();
+            if (step + 2 < steps) feed.columns(step + 2);
+            fetch_pairs(step + 1);
+            feed.rows(Kh, Vh);
         }
-        const int col0 = (int)(step % SUB) * KT + wn * KW;
-        const int chunk = item.c0 + (int)(step / SUB) * STEP + col0 / kAttnChunk;
-        if (!busy || chunk >= item.c1) continue;
-        const int state = __builtin_amdgcn_readfirstlane(item.state(p, chunk, r));
+        int col0;
+        if (my_chunk(step, col0) < 0) continue;
+        state = __builtin_amdgcn_readfirstlane(state);
         if (state == 0) continue;
-        const uint64_t word = item.word(p, chunk, r) >> (col0 % kAttnChunk);
+        word >>= col0 % kAttnChunk;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
+            const int *kp = s_kpos + wn * KW + 32 * t;
+            attn_near near = {false, false, false, 0};
+            if (POS) {
+                const int col = kp[lane & 31];
+                near = attn_look(a, attn_distance(col, q_hi), attn_distance(col, q_lo));
+                if (near.nothing) continue;
+            }
             attn_f32x16 s = tile::scores(sK, wn * KW + 32 * t, q, lane);
-            const attn_f32x16 dp = tile::scores(sV, wn * KW + 32 * t, go, lane);
+            attn_f32x16 dp = tile::scores(sV, wn * KW + 32 * t, go, lane);
             // what is not stored, and rows that do not exist, add nothing
             const uint32_t bits = (me.valid ? (uint32_t)(word >> (32 * t)) : 0u) >> (4 * (lane >> 5));
+            if (!POS) {
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                bool there = bits >> (8 * (x >> 2) + (x & 3)) & 1;
-                float v = s[x];
-                int bucket = 0;
-                if (POS) {
-                    const int kp = s_kpos[wn * KW + 32 * t + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)];
-                    v *= a.scale;
-                    if (a.buckets) { bucket = bias.bucket(kp, qp); v += bias.at(bucket); }
-                    if (a.causal && kp > qp) there = false;
-                    there = there && v != -INFINITY;     // weight 0, whatever dp is
-                    v = (v - off) * cc;
-                } else v = __builtin_fmaf(v, cc, -off);
-                v = there ? __builtin_amdgcn_exp2f(v) * (dp[x] - delta) : 0.f;
-                if (POS && hist && there) atomicAdd(&hist[bucket * 64 + lane], v);      // a place of this lane's own: one order
-                s[x] = v;
+                for (int x = 0; x < 16; ++x) {
+                    const bool there = bits >> (8 * (x >> 2) + (x & 3)) & 1;
+                    s[x] = there ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], cc, -off)) * (dp[x] - delta) : 0.f;
+                }
+            } else {
+                // weights first, in s; a score of minus infinity has weight 0, whatever dP is
+                const bool one = !a.buckets || near.far;
+                const float all_of = a.buckets && near.far ? bias.at(near.bucket) : 0.f;
+                float sum_x = 0, sum_p = 0;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    const int col = 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3);
+                    bool there = bits >> (8 * (x >> 2) + (x & 3)) & 1;
+                    if (near.ask) there = there && kp[col] <= qp;
+                    int bucket = 0;
+                    float v = all_of;
+                    if (!one) { bucket = bias.bucket(kp[col], qp); v = bias.at(bucket); }
+                    v = __builtin_fmaf(s[x], a.scale, v);
+                    there = there && v != -INFINITY;
+                    const float w = there ? __builtin_amdgcn_exp2f((v - off) * cc) : 0.f;
+                    s[x] = there ? w * (dp[x] - delta) : 0.f;
+                    if (hist) {
+                        const float term = f.exact ? (there ? w * dp[x] : 0.f) : s[x];
+                        if (one) { sum_x += term; sum_p += w; }
+                        else if (there) {
+                            atomicAdd(&hist[bucket * 64 + lane], term);       // a place of this lane's own: one order
+                            if (f.exact) atomicAdd(&hist[(a.buckets + bucket) * 64 + lane], w);
+                        }
+                    }
+                }
+                if (hist && one) {
+                    const int side = near.bucket == a.side - 1 ? 0 : 1;
+                    if (side) { far_x[1] += sum_x; far_p[1] += sum_p; } else { far_x[0] += sum_x; far_p[0] += sum_p; }
+                }
             }
             tile::add_rows(acc, sK, wn * KW + 32 * t, s, lane);
         }
@@ -160,34 +198,49 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     uint64_t again = __builtin_amdgcn_ballot_w64(me.valid && !(odd == 0.f));
 
     if (POS && hist) {
-        // a lane for a bucket (and, where lanes are heads, a head): places added in order
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const int b = attn_far_bucket(a, side == 1);
+            hist[b * 64 + lane] += far_x[side];
+            if (f.exact) hist[(a.buckets + b) * 64 + lane] += far_p[side];
+        }
         __syncthreads();
         const float *all = (const float *)(bias.table + a.buckets * bias.slots);
+        float *s_delta = (float *)lds;                   // over K: [waves][32], each row's D
+        // rows are a wave's own, or (WN) shared by all waves
+        if (f.exact && lane < 32 && (WN == 1 || wave == 0)) {
+            float d = 0;
+            for (int w = wave; w < (WN == 1 ? wave + 1 : WN); ++w)
+                for (int b = 0; b < a.buckets; ++b) d += all[w * hist_size + b * 64 + lane] + all[w * hist_size + b * 64 + 32 + lane];
+            s_delta[wave * 32 + lane] = d;
+        }
+        __syncthreads();
         float *out = f.part_table + item.part * a.H * a.buckets;
-        if (f.mode == kHeadsTogether) {
-            for (int x = tid; x < a.buckets * 32; x += NT) {
-                const int b = x >> 5, h = x & 31, per = 32, parts = (a.G + per - 1) / per, y = (group % parts) * per + h;
-                if (y >= a.G) continue;
-                float sum = 0;
-                for (int w = 0; w < WM * WN; ++w) sum += all[(w * a.buckets + b) * 64 + h] + all[(w * a.buckets + b) * 64 + 32 + h];
-                out[((group / parts) * a.G + y) * a.buckets + b] = sum;
-            }
-        } else {
-            const int waves = f.mode == kHeadsOfRows ? 1 : WM * WN;      // that share a head
-            for (int x = wave; x < a.buckets * (WM * WN / waves); x += WM * WN) {
-                const int b = x % a.buckets, w0 = x / a.buckets * waves;
-                int h = group;
-                if (f.mode == kHeadsOfRows) {
-                    const int parts = (a.G + WM - 1) / WM, y = (group % parts) * WM + w0;
-                    if (y >= a.G) continue;
-                    h = (group / parts) * a.G + y;
+        auto term = [&](int w, int b) {
+            const float x = all[w * hist_size + b * 64 + lane];
+            return f.exact ? x - s_delta[(WN == 1 ? w : 0) * 32 + (lane & 31)] * all[w * hist_size + (a.buckets + b) * 64 + lane] : x;
+        };
+        for (int b = wave; b < a.buckets; b += WM * WN) {
+            float sum = 0;
+            if (f.mode == kHeadsOfRows) {
+                for (int w = 0; w < WM; ++w) {
+                    const int y = group / a.Hk * WM + w;
+                    sum = attn_wave_sum(term(w, b));
+                    if (lane == 0 && y < a.G) out[(group % a.Hk * a.G + y) * a.buckets + b] = sum;
                 }
-                float sum = 0;
-                for (int w = w0; w < w0 + waves; ++w) sum += all[(w * a.buckets + b) * 64 + lane];
+                continue;
+            }
+            for (int w = 0; w < WM * WN; ++w) sum += term(w, b);
+            if (f.mode == kHeadsTogether) {
+                const int y = group / a.Hk * 32 + lane;
+                sum = attn_pair_sum(sum);
+                if (lane < 32 && y < a.G) out[(group % a.Hk * a.G + y) * a.buckets + b] = sum;
+            } else {
                 sum = attn_wave_sum(sum);
-                if (lane == 0) out[h * a.buckets + b] = sum;
+                if (lane == 0) out[(group % a.Hk * a.G + group / a.Hk) * a.buckets + b] = sum;
             }
         }
+        __syncthreads();
     }
 
     const int64_t place = (item.part * a.H + me.head) * p.br + r;
@@ -270,10 +323,8 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
 {
     typedef attn_tile<T, DT> tile;
     typedef typename tile::frag frag;
-    constexpr int NT = 64 * WM, KT = KW, TILES = KW / 32;
-    constexpr int PIECES = KT * tile::kGranules / NT, ROWSTEP = NT / tile::kGranules;
-    constexpr int SUB = kAttnChunk / KT;
-    static_assert(KT <= NT && KT <= kAttnChunk, "a thread for each query of a step");
+    constexpr int NT = 64 * WM, KT = KW, TILES = KW / 32, SUB = kAttnChunk / KT;
+    static_assert(KT <= kAttnChunk, "steps within a chunk");
     extern __shared__ __align__(16) char lds[];
     attn_lds *sQ = (attn_lds *)lds, *sO = sQ + KT * tile::kRow;
     float *s_lse = (float *)(lds + 2 * KT * tile::kRow), *s_delta = s_lse + KT;
@@ -293,11 +344,11 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     frag kx[tile::kSteps], vx[tile::kSteps];
     tile::load_lane((const T *)a.K + key * a.ldk + kv * a.hdk, a.D, f.vec, some, POS ? 1.f : a.c, kx, lane);
     tile::load_lane((const T *)a.V + key * a.ldv + kv * a.hdv, a.D, f.vec, some, 1.f, vx, lane);
-    int kp = 0;
+    int kp = 0, k_lo = 0, k_hi = 0;
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
     float *table = nullptr;
     if (POS) {
-        if (a.kpos) kp = a.kpos[key];
+        if (a.kpos) { kp = a.kpos[key]; k_lo = attn_wave_min(kp); k_hi = attn_wave_max(kp); }
         if (a.buckets) {
             bias = attn_make_bias<T>(a, (char *)(s_qpos + KT), 1, [&](int) { return kv * a.G; });
             table = const_cast<float *>(bias.table);
@@ -307,73 +358,79 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
 #pragma unroll
     for (int x = 0; x < tile::kBlocks; ++x) dk[x] = dv[x] = (attn_f32x16)(0.f);
 
-    const int my_row = tid / tile::kGranules, my_g = tid % tile::kGranules;
-    const int64_t first = (int64_t)(item.c0 - item.chunk0) * kAttnChunk;
     const int64_t per_head = (int64_t)(item.c1 - item.c0) * SUB, steps = per_head * a.G;
-    int32_t at[PIECES], one_at = 0;
-    frag qf[PIECES], of[PIECES];
+    attn_feed<T, DT, NT, KT, POS> feed;
+    feed.ldx = a.ldq; feed.ldy = f.g.lddo;
+    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk;
+    feed.pos = a.qpos; feed.sign = -a.causal; feed.limit = k_lo;
+    feed.D = a.D; feed.vec = f.vec; feed.row = tid / tile::kGranules; feed.g = tid % tile::kGranules;
+    if (POS && a.causal && WM > 1) {
+        if (lane == 0) s_qpos[wave] = k_lo;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WM; ++w) feed.limit = s_qpos[w] < feed.limit ? s_qpos[w] : feed.limit;
+    }
     float lse_next = 0, delta_next = 0;
-    int qp_next = 0;
-    auto fetch_columns = [&](int64_t within) {           // step of a head
-        const int64_t x = first + within * KT;
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) at[k] = item.cols.get(x + my_row + k * ROWSTEP);
-        if (tid < KT) one_at = item.cols.get(x + tid);
-    };
-    auto fetch_rows = [&](int h) {
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-            qf[k] = tile::granule((const T *)a.Q + (int64_t)at[k] * a.ldq + h * a.hdq, my_g * tile::kPer, a.D, f.vec, true);
-            of[k] = tile::granule((const T *)f.g.dO + (int64_t)at[k] * f.g.lddo + h * f.g.hddo, my_g * tile::kPer, a.D, f.vec, true);
+    uint64_t word = 0, word_next = 0;
+    int state = 0, state_next = 0;
+    // a step: the head and the step among the head's
+    struct place { int h; int64_t at; };
+    auto after = [&](place x) { return ++x.at == per_head ? place{x.h + 1, 0} : x; };
+    auto fetch = [&](place x) {
+        if (busy) {
+            const int chunk = item.c0 + (int)(x.at / SUB);
+            state_next = item.state(p, chunk, r);
+            word_next = item.word(p, chunk, r);
         }
         if (tid < KT) {
-            const float l = f.g.lse[h * a.m + one_at];
-            lse_next = l == -INFINITY ? INFINITY : POS ? l : l * kLog2e;
-            delta_next = f.delta[h * a.m + one_at];
-            if (POS && a.qpos) qp_next = a.qpos[one_at];
+            lse_next = f.g.lse[x.h * a.m + feed.one];
+            delta_next = f.delta[x.h * a.m + feed.one];
         }
+        feed.rows((const T *)a.Q + x.h * a.hdq, (const T *)f.g.dO + x.h * f.g.hddo);
     };
-    int64_t within = 0, within2 = 0;                     // of the step at hand, of the columns fetched last
-    int h = kv * a.G, h1 = h;                            // head of the step at hand, of the rows fetched last
-    auto advance = [&](int64_t &w) { if (++w == per_head) w = 0; return w == 0; };
+    place now = {kv * a.G, 0}, soon = after(now), later = after(soon);
     if (steps > 0) {
-        fetch_columns(0);
-        fetch_rows(h);
-        advance(within2);
-        if (steps > 1) fetch_columns(within2);
+        feed.columns(0);
+        feed.advance();
+        if (steps > 1) feed.columns(soon.at);
+        fetch(now);
     }
     for (int64_t step = 0; step < steps; ++step) {
         __syncthreads();
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-            tile::put(sQ, my_row + k * ROWSTEP, my_g, qf[k]);
-            tile::put(sO, my_row + k * ROWSTEP, my_g, of[k]);
-        }
+        feed.put(sQ, sO);
         if (tid < KT) {
-            s_lse[tid] = lse_next;
+            s_lse[tid] = lse_next == -INFINITY ? INFINITY : POS ? lse_next : lse_next * kLog2e;     // no weight left
             s_delta[tid] = delta_next;
-            if (POS) s_qpos[tid] = qp_next;
+            if (POS) s_qpos[tid] = feed.arrived;
         }
-        if (POS && a.buckets && within == 0)
-            for (int b = tid; b < a.buckets; b += NT) table[b] = (float)((const T *)a.table)[(int64_t)b * a.ldt + h];
+        if (POS && a.buckets && now.at == 0)
+            for (int b = tid; b < a.buckets; b += NT) table[b] = (float)((const T *)a.table)[(int64_t)b * a.ldt + now.h];
         __syncthreads();
+        word = word_next; state = state_next;
         if (step + 1 < steps) {
-            if (within2 == 0) ++h1;
-            fetch_rows(h1);
-            advance(within2);
-            if (step + 2 < steps) fetch_columns(within2);
+            feed.advance();
+            if (step + 2 < steps) feed.columns(later.at);
+            fetch(soon);
         }
-        const int col0 = (int)(within % SUB) * KT, chunk = item.c0 + (int)(within / SUB);
-        if (advance(within)) ++h;
+        const int col0 = (int)(now.at % SUB) * KT;
+        now = soon; soon = later; later = after(later);
         if (!busy) continue;
-        const int state = __builtin_amdgcn_readfirstlane(item.state(p, chunk, r));
+        state = __builtin_amdgcn_readfirstlane(state);
         if (state == 0) continue;
-        const uint64_t word = item.word(p, chunk, r) >> col0;
+        word >>= col0;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
+            attn_near near = {false, false, false, 0};
+            if (POS) {
+                const int qp = s_qpos[32 * t + (lane & 31)];
+                near = attn_look(a, attn_distance(k_lo, qp), attn_distance(k_hi, qp));
+                if (near.nothing) continue;
+            }
             attn_f32x16 s = tile::scores(sQ, 32 * t, kx, lane);
             attn_f32x16 dp = tile::scores(sO, 32 * t, vx, lane);
             const uint32_t bits = (valid ? (uint32_t)(word >> (32 * t)) : 0u) >> (4 * (lane >> 5));
+            const bool one = !a.buckets || near.far;
+            const float all_of = POS && a.buckets && near.far ? bias.at(near.bucket) : 0.f;
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int q0 = 32 * t + 8 * b + 4 * (lane >> 5);
@@ -384,10 +441,8 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
                     bool there = bits >> (8 * b + c) & 1;
                     float v = s[x];
                     if (POS) {
-                        const int qp = s_qpos[q0 + c];
-                        v *= a.scale;
-                        if (a.buckets) v += bias.at(bias.bucket(kp, qp));
-                        if (a.causal && kp > qp) there = false;
+                        v = __builtin_fmaf(v, a.scale, one ? all_of : bias.at(bias.bucket(kp, s_qpos[q0 + c])));
+                        if (near.ask) there = there && kp <= s_qpos[q0 + c];
                         there = there && v != -INFINITY;
                         v = (v - lse[c]) * cc;
                     } else v = __builtin_fmaf(v, cc, -lse[c]);
@@ -450,22 +505,24 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
 
 // Rows (dq: of a head; dkv: keys of a kv head) that were cut into several items: their parts added in a fixed order.  PER: vectors of D
 // numbers for a row (dq 1: dQ; dkv 2: dK, dV), of which the first is scaled.
+// The grid: blocks that were cut, rows of a block, heads.
 template <typename T, int LP, int PER>
-__global__ __launch_bounds__(kThreads) void join_kernel(grad_args f, int64_t rows, int heads)
+__global__ __launch_bounds__(kThreads) void join_kernel(grad_args f, int64_t cut, int64_t rows, int heads)
 {
     const attn_plan_view &p = f.p;
     const int lane = threadIdx.x & 63, D = f.a.D;
     const int64_t x = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (x >= rows * heads) return;
-    const int64_t i = x / heads, b = i / p.br;
-    const int h = (int)(x % heads), first = p.item0[b], parts = p.item0[b + 1] - first;
-    if (parts == 1) return;
+    if (x >= cut * p.br * heads) return;
+    const int h = (int)(x % heads), r = (int)(x / heads % p.br);
+    const int64_t b = p.cut_block[x / heads / p.br], i = b * p.br + r;
+    if (i >= rows) return;
+    const int first = p.item0[b], parts = p.item0[b + 1] - first;
 #pragma unroll
     for (int v = 0; v < PER; ++v) {
         T *out = PER == 1 ? (T *)f.g.dQ + i * f.g.lddq + h * f.g.hddq
                           : v == 0 ? (T *)f.g.dK + i * f.g.lddk + h * f.g.hddk : (T *)f.g.dV + i * f.g.lddv + h * f.g.hddv;
         const attn_f32x4 sum = attn_add_parts<LP>(parts, f.pd, lane, [&](int k) {
-            return f.part + ((((int64_t)(first + k) * heads + h) * p.br + i % p.br) * PER + v) * f.pd;
+            return f.part + ((((int64_t)(first + k) * heads + h) * p.br + r) * PER + v) * f.pd;
         }, [](int) { return 1.f; });
         if (lane < LP) attn_store4(out, 4 * lane, D, f.vec, v == 0 ? sum * f.a.scale : sum);
     }
@@ -499,18 +556,16 @@ sp_status launch(K kernel, const grad_args &f, int64_t groups, int threads, size
 template <typename T, int DT, int WM, int WN, int KW, bool POS>
 sp_status launch_dq(const grad_args &f, const attn_mapping &c, int64_t items, hipStream_t st)
 {
-    constexpr int KT = KW * WN;
-    size_t lds = 2 * (size_t)KT * DT * sizeof(T) + (POS ? KT * 4 + attn_bias_bytes(f.a, c.slots()) : 0) + (POS && f.part_table ? (size_t)WM * WN * f.a.buckets * 256 : 0);
+    const size_t lds = attn_dq_lds(f.a, c, DT * (int)sizeof(T), POS, POS && f.part_table, f.exact);
     const size_t join = WN > 1 ? (size_t)WN * 32 * (DT + 1) * 4 : 0;
     return launch(dq_kernel<T, DT, WM, WN, KW, POS>, f, items * c.groups, 64 * WM * WN, lds > join ? lds : join, st);
 }
 template <typename T, int DT, bool POS>
 sp_status launch_dq_mode(const grad_args &f, const attn_mapping &c, int64_t items, hipStream_t st)
 {
-    // K and V of a step and the bias's sums have to fit the LDS together
-    constexpr int kRow = DT * (int)sizeof(T), WN = kRow >= 1024 ? (POS ? 1 : 2) : kRow == 512 && POS ? 2 : 4;
-    if (c.wn > 1) return launch_dq<T, DT, 1, WN, 32, POS>(f, c, items, st);
-    return launch_dq<T, DT, 4, 1, (kRow == 64 ? 64 : 32), POS>(f, c, items, st);
+    constexpr int kRow = DT * (int)sizeof(T);
+    if (c.wn > 1) return launch_dq<T, DT, 1, attn_dq_waves(kRow, POS), 32, POS>(f, c, items, st);
+    return launch_dq<T, DT, 4, 1, attn_dq_columns(kRow), POS>(f, c, items, st);
 }
 template <typename T, int DT, bool POS>
 sp_status launch_dkv_mode(const grad_args &f, int br, int64_t items, hipStream_t st)
@@ -542,7 +597,8 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
         const int64_t items = rows->items[c.rows.level];
         if (pos) SP_TRY((launch_dq_mode<T, DT, true>(f, c.rows, items, st)));
         else SP_TRY((launch_dq_mode<T, DT, false>(f, c.rows, items, st)));
-        if (c.rows.cut) hipLaunchKernelGGL((join_kernel<T, DT / 4, 1>), dim3((unsigned)ceil_div(a.m * a.H, 4)), dim3(kThreads), 0, st, f, a.m, a.H);
+        if (c.rows.cut) hipLaunchKernelGGL((join_kernel<T, DT / 4, 1>), dim3((unsigned)ceil_div(rows->cut[c.rows.level] * rows->br * a.H, 4)), dim3(kThreads), 0, st, f,
+                                           rows->cut[c.rows.level], a.m, a.H);
         if (f.part_table) hipLaunchKernelGGL(table_kernel<T>, dim3((unsigned)(a.buckets * a.H)), dim3(kThreads), 0, st, f, items);
         SP_HIP(hipGetLastError());
     }
@@ -551,7 +607,8 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
         const int64_t items = keys->items[c.keys_level];
         if (pos) SP_TRY((launch_dkv_mode<T, DT, true>(f, keys->br, items, st)));
         else SP_TRY((launch_dkv_mode<T, DT, false>(f, keys->br, items, st)));
-        if (c.keys_cut) hipLaunchKernelGGL((join_kernel<T, DT / 4, 2>), dim3((unsigned)ceil_div(a.n * a.Hk, 4)), dim3(kThreads), 0, st, f, a.n, a.Hk);
+        if (c.keys_cut) hipLaunchKernelGGL((join_kernel<T, DT / 4, 2>), dim3((unsigned)ceil_div(keys->cut[c.keys_level] * keys->br * a.Hk, 4)), dim3(kThreads), 0, st, f,
+                                       keys->cut[c.keys_level], a.n, a.Hk);
         SP_HIP(hipGetLastError());
     }
     return SP_OK;
@@ -565,5 +622,7 @@ sp_status attn_backward(const sp_tensor *S, grad_args &f, const grad_choice &c, 
     if (f.a.D <= 32) return grad_d<T, 32>(S, f, c, st);
     if (f.a.D <= 64) return grad_d<T, 64>(S, f, c, st);
     if (f.a.D <= 128) return grad_d<T, 128>(S, f, c, st);
-    return grad_d<T, 256>(S, f, c, st);
+    // f32 ends at 128: a row and its sums of 256 numbers of 32 bits do not fit a lane's registers
+    if constexpr (sizeof(T) == 2) return grad_d<T, 256>(S, f, c, st);
+    return SP_ERR_SHAPE;
 }

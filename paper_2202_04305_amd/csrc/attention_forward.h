@@ -20,11 +20,8 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     typedef attn_tile<T, DT> tile;
     typedef typename tile::frag frag;
     constexpr int NT = 64 * WM * WN, KT = KW * WN, TILES = KW / 32;
-    constexpr int PIECES = KT * tile::kGranules / NT;    // granules of K (and of V) a thread fetches for a step
-    constexpr int ROWSTEP = NT / tile::kGranules;
     constexpr int STEP = KT > kAttnChunk ? KT / kAttnChunk : 1;         // chunks of a step (or one chunk in 64 / KT steps)
     constexpr int SUB = KT < kAttnChunk ? kAttnChunk / KT : 1;
-    static_assert(KT * tile::kGranules % NT == 0 && NT % tile::kGranules == 0, "every thread fetches the same number of granules");
     extern __shared__ __align__(16) char lds[];
     attn_lds *sK = (attn_lds *)lds, *sV = sK + KT * tile::kRow;
     int *s_kpos = (int *)(lds + 2 * KT * tile::kRow);    // POS: [KT]
@@ -44,10 +41,10 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
 
     frag q[tile::kSteps];
     tile::load_lane((const T *)a.Q + row * a.ldq + head * a.hdq, a.D, f.vec, valid && item.c1 > item.c0, POS ? 1.f : a.c, q, lane);
-    int qp = 0;
+    int qp = 0, q_lo = 0, q_hi = 0;
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
     if (POS) {
-        if (a.qpos) qp = a.qpos[row];
+        if (a.qpos) { qp = a.qpos[row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
         if (a.buckets) bias = attn_lane_bias<T>(a, lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
     }
 
@@ -56,68 +53,88 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     for (int x = 0; x < tile::kBlocks; ++x) acc[x] = (attn_f32x16)(0.f);
     float top = -INFINITY, total = 0;
 
+    const int64_t steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
+    attn_feed<T, DT, NT, KT, POS> feed;
+    feed.ldx = a.ldk; feed.ldy = a.ldv;
+    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk;
+    feed.pos = a.kpos; feed.sign = a.causal; feed.limit = q_hi;
+    feed.D = a.D; feed.vec = f.vec; feed.row = tid / tile::kGranules; feed.g = tid % tile::kGranules;
     const T *Kh = (const T *)a.K + (int64_t)kv * a.hdk, *Vh = (const T *)a.V + (int64_t)kv * a.hdv;
-    const int my_row = tid / tile::kGranules, my_g = tid % tile::kGranules;
-    const int64_t first = (int64_t)(item.c0 - item.chunk0) * kAttnChunk, steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
-    int32_t at[PIECES], pos_at = 0;
-    frag kf[PIECES], vf[PIECES];
-    int kp_next = 0;
-    auto fetch_columns = [&](int64_t step) {
-        const int64_t x = first + step * KT;
+    if (POS && a.causal && WM > 1) {                     // the last position that any row of the block attends to
+        if (lane == 0) s_kpos[wave] = q_hi;
+        __syncthreads();
 #pragma unroll
-        for (int k = 0; k < PIECES; ++k) at[k] = item.cols.get(x + my_row + k * ROWSTEP);
-        if (POS && tid < KT) pos_at = item.cols.get(x + tid);
+        for (int w = 0; w < WM; ++w) feed.limit = s_kpos[w] > feed.limit ? s_kpos[w] : feed.limit;
+    }
+    // this wave's share of a step: columns col0 .. col0 + KW of the step's chunks
+    auto my_chunk = [&](int64_t step, int &col0) {
+        col0 = (int)(step % SUB) * KT + wn * KW;
+        const int chunk = item.c0 + (int)(step / SUB) * STEP + col0 / kAttnChunk;
+        return busy && chunk < item.c1 ? chunk : -1;
     };
-    auto fetch_rows = [&]() {
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-            kf[k] = tile::granule(Kh + (int64_t)at[k] * a.ldk, my_g * tile::kPer, a.D, f.vec, true);
-            vf[k] = tile::granule(Vh + (int64_t)at[k] * a.ldv, my_g * tile::kPer, a.D, f.vec, true);
-        }
-        if (POS && a.kpos && tid < KT) kp_next = a.kpos[pos_at];
+    // its pairs are asked for before the rows of the same step: a wait for them leaves those on their way
+    uint64_t word = 0, word_next = 0;
+    int state = 0, state_next = 0;
+    auto fetch_pairs = [&](int64_t step) {
+        int col0;
+        const int chunk = my_chunk(step, col0);
+        state_next = 0;
+        if (chunk >= 0) { state_next = item.state(p, chunk, r); word_next = item.word(p, chunk, r); }
     };
     if (steps > 0) {
-        fetch_columns(0);
-        fetch_rows();
-        if (steps > 1) fetch_columns(1);
+        feed.columns(0);
+        feed.advance();
+        if (steps > 1) feed.columns(1);
+        fetch_pairs(0);
+        feed.rows(Kh, Vh);
     }
     for (int64_t step = 0; step < steps; ++step) {
         __syncthreads();                                 // the step before has been computed
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-            tile::put(sK, my_row + k * ROWSTEP, my_g, kf[k]);
-            tile::put(sV, my_row + k * ROWSTEP, my_g, vf[k]);
-        }
-        if (POS && tid < KT) s_kpos[tid] = kp_next;
+        feed.put(sK, sV);
+        if (POS && tid < KT) s_kpos[tid] = feed.arrived;
         __syncthreads();
+        word = word_next; state = state_next;
         if (step + 1 < steps) {
-            fetch_rows();
-            if (step + 2 < steps) fetch_columns(step + 2);
+            feed.advance();
+            if (step + 2 < steps) feed.columns(step + 2);
+            fetch_pairs(step + 1);
+            feed.rows(Kh, Vh);
         }
-        const int col0 = (int)(step % SUB) * KT + wn * KW;               // of this wave, from the step's first chunk on
-        const int chunk = item.c0 + (int)(step / SUB) * STEP + col0 / kAttnChunk;
-        if (!busy || chunk >= item.c1) continue;
-        const int state = item.state(p, chunk, r);
-        if (__builtin_amdgcn_readfirstlane(state) == 0) continue;
-        const uint64_t word = item.word(p, chunk, r) >> (col0 % kAttnChunk);
-        const bool all = __builtin_amdgcn_readfirstlane(state) == 2 && !(POS && a.causal);
+        int col0;
+        if (my_chunk(step, col0) < 0) continue;
+        state = __builtin_amdgcn_readfirstlane(state);
+        if (state == 0) continue;
+        word >>= col0 % kAttnChunk;
+        const bool all = state == 2;
 
         attn_f32x16 s[TILES];
         float up = top;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
+            const int *kp = s_kpos + wn * KW + 32 * t;
+            attn_near near = {false, false, false, 0};
+            if (POS) {
+                const int col = kp[lane & 31];
+                near = attn_look(a, attn_distance(col, q_hi), attn_distance(col, q_lo));
+                if (near.nothing) {
+                    s[t] = (attn_f32x16)(-INFINITY);
+                    continue;
+                }
+            }
             s[t] = tile::scores(sK, wn * KW + 32 * t, q, lane);
             if (POS) {
+                if (a.buckets && !near.far) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const int *kp = s_kpos + wn * KW + 32 * t + 8 * b + 4 * (lane >> 5);
+                    for (int x = 0; x < 16; ++x)
+                        s[t][x] = __builtin_fmaf(s[t][x], a.scale, bias.at(bias.bucket(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp)));
+                } else {
+                    const float all_of = a.buckets ? bias.at(near.bucket) : 0.f;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float v = s[t][4 * b + c] * a.scale;
-                        if (a.buckets) v += bias.at(bias.bucket(kp[c], qp));
-                        if (a.causal && kp[c] > qp) v = -INFINITY;
-                        s[t][4 * b + c] = v;
-                    }
+                    for (int x = 0; x < 16; ++x) s[t][x] = __builtin_fmaf(s[t][x], a.scale, all_of);
+                }
+                if (near.ask) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[t][x] = kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)] > qp ? -INFINITY : s[t][x];
                 }
             }
             if (!all) {
@@ -260,8 +277,9 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
 
 // Rows whose columns were cut into several items: a wave for a row and head.  Each part has its maximum and total; the parts' sums are
 // weighted to the largest maximum and added in a fixed order.  Parts that have nothing of the row wrote no sums and are left out.
+// The grid: blocks that were cut, rows of a block, heads.
 template <typename T, int LP>
-__global__ __launch_bounds__(256) void join_kernel(forward_args f)
+__global__ __launch_bounds__(256) void join_kernel(forward_args f, int64_t cut)
 {
     __shared__ float s_weight[4][64];
     __shared__ int s_part[4][64];
@@ -269,11 +287,12 @@ __global__ __launch_bounds__(256) void join_kernel(forward_args f)
     const attn_plan_view &p = f.p;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t x = (int64_t)blockIdx.x * 4 + wave;
-    if (x >= a.m * a.H) return;
-    const int64_t i = x / a.H, b = i / p.br;
-    const int h = (int)(x % a.H), first = p.item0[b], parts = p.item0[b + 1] - first;
-    if (parts == 1) return;
-    auto place = [&](int k) { return ((int64_t)(first + k) * a.H + h) * p.br + i % p.br; };
+    if (x >= cut * p.br * a.H) return;
+    const int h = (int)(x % a.H), r = (int)(x / a.H % p.br);
+    const int64_t b = p.cut_block[x / a.H / p.br], i = b * p.br + r;
+    if (i >= a.m) return;
+    const int first = p.item0[b], parts = p.item0[b + 1] - first;
+    auto place = [&](int k) { return ((int64_t)(first + k) * a.H + h) * p.br + r; };
     float top = -INFINITY;
     for (int k = lane; k < parts; k += 64) top = fmaxf(top, f.part_stat[2 * place(k)]);
 #pragma unroll
@@ -322,8 +341,7 @@ sp_status launch(const forward_args &f, const forward_choice &c, int64_t items, 
 template <typename T, int DT, bool POS>
 sp_status launch_mode(const forward_args &f, const forward_choice &c, int64_t items, hipStream_t st)
 {
-    constexpr bool wide = sizeof(T) == 4 && DT == 256;   // K and V of 128 columns would not fit the LDS
-    if (c.wn > 1) return launch<T, DT, 1, wide ? 2 : 4, 32, POS>(f, c, items, st);
+    if (c.wn > 1) return launch<T, DT, 1, 4, 32, POS>(f, c, items, st);
     return launch<T, DT, 4, 1, (DT * (int)sizeof(T) <= 256 ? 64 : 32), POS>(f, c, items, st);
 }
 
@@ -340,12 +358,13 @@ sp_status attn_forward(const sp_attn_plan *plan, forward_args &f, const forward_
     do {                                                                                                                          \
         if (pos) SP_TRY((launch_mode<T, DT, true>(f, c, items, st)));                                                             \
         else SP_TRY((launch_mode<T, DT, false>(f, c, items, st)));                                                                \
-        if (c.cut) hipLaunchKernelGGL((join_kernel<T, DT / 4>), dim3((unsigned)ceil_div(f.a.m * f.a.H, 4)), dim3(256), 0, st, f);  \
+        if (c.cut) hipLaunchKernelGGL((join_kernel<T, DT / 4>), dim3((unsigned)ceil_div(plan->cut[c.level] * plan->br * f.a.H, 4)), dim3(256), 0, st, f, plan->cut[c.level]); \
     } while (0)
     if (f.a.D <= 32) SPMI_FORWARD(32);
     else if (f.a.D <= 64) SPMI_FORWARD(64);
     else if (f.a.D <= 128) SPMI_FORWARD(128);
-    else SPMI_FORWARD(256);
+    else if constexpr (sizeof(T) == 2) SPMI_FORWARD(256);
+    else return SP_ERR_SHAPE;
 #undef SPMI_FORWARD
     SP_HIP(hipGetLastError());
     return SP_OK;

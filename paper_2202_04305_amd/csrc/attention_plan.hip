@@ -185,6 +185,26 @@ __global__ __launch_bounds__(kThreads) void items_kernel(const int32_t *__restri
         t.item0[l][b] = b < nblocks ? (k <= per ? 1 : (k + per - 1) / per) : 0;
     }
 }
+// the blocks of several items, ascending, by one workgroup
+__global__ __launch_bounds__(1024) void cut_blocks_kernel(const int32_t *__restrict__ item0, int64_t nblocks, int32_t *__restrict__ list,
+                                                          unsigned long long *__restrict__ count)
+{
+    __shared__ int s_wave[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t before = 0;
+    for (int64_t b0 = 0; b0 < nblocks; b0 += 1024) {
+        const int64_t b = b0 + threadIdx.x;
+        const bool cut = b < nblocks && item0[b + 1] - item0[b] > 1;
+        const uint64_t some = __builtin_amdgcn_ballot_w64(cut);
+        if (lane == 0) s_wave[wave] = __builtin_popcountll(some);
+        __syncthreads();
+        int64_t at = before;
+        for (int w = 0; w < 16; ++w) { at += w < wave ? s_wave[w] : 0; before += s_wave[w]; }
+        if (cut && list) list[at + __builtin_popcountll(some & (((uint64_t)1 << lane) - 1))] = (int32_t)b;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *count = (unsigned long long)before;
+}
 __global__ __launch_bounds__(kThreads) void stretches_kernel(const int32_t *__restrict__ item0, const int32_t *__restrict__ chunk0,
                                                              const int32_t *__restrict__ rowptr, int64_t nblocks, int br, int per,
                                                              attn_stretch *__restrict__ items)
@@ -219,7 +239,7 @@ struct plan_scope {
     void drop() {
         if (!plan) return;
         mem.put(plan->rowptr); mem.put(plan->crd_own); mem.put(plan->chunk0); mem.put(plan->cols); mem.put(plan->bits); mem.put(plan->state);
-        for (int l = 0; l < kAttnLevels; ++l) { mem.put(plan->item0[l]); mem.put(plan->item[l]); }
+        for (int l = 0; l < kAttnLevels; ++l) { mem.put(plan->item0[l]); mem.put(plan->item[l]); mem.put(plan->cut_block[l]); }
         delete plan;
         plan = nullptr;
     }
@@ -338,15 +358,23 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
     hipLaunchKernelGGL(items_kernel, dim3(blocks_for(p->nblocks + 1)), dim3(kThreads), 0, st, p->chunk0, p->nblocks, p->levels, table);
     SP_HIP(hipGetLastError());
     int32_t total[kAttnLevels];
+    unsigned long long cut[kAttnLevels];
+    unsigned long long *cuts_dev = (unsigned long long *)tmp.get(kAttnLevels * 8);
+    if (!cuts_dev) return SP_ERR_ALLOC;
     for (int l = 0; l < p->levels; ++l) {
         SP_TRY(spmi_exclusive_scan(p->item0[l], p->nblocks + 1, 32, tmp, st));
+        hipLaunchKernelGGL(cut_blocks_kernel, dim3(1), dim3(1024), 0, st, p->item0[l], p->nblocks, nullptr, cuts_dev + l);
         SP_HIP(hipMemcpyAsync(&total[l], p->item0[l] + p->nblocks, 4, hipMemcpyDeviceToHost, st));
     }
+    SP_HIP(hipMemcpyAsync(cut, cuts_dev, (size_t)p->levels * 8, hipMemcpyDeviceToHost, st));
     SP_HIP(hipStreamSynchronize(st));
     for (int l = 0; l < p->levels; ++l) {
         p->items[l] = total[l];
         p->item[l] = (attn_stretch *)scope.get((size_t)(total[l] > 0 ? total[l] : 1) * sizeof(attn_stretch));
-        if (!p->item[l]) return SP_ERR_ALLOC;
+        p->cut[l] = (int64_t)cut[l];
+        p->cut_block[l] = (int32_t *)scope.get((size_t)(cut[l] > 0 ? cut[l] : 1) * 4);
+        if (!p->item[l] || !p->cut_block[l]) return SP_ERR_ALLOC;
+        if (cut[l]) hipLaunchKernelGGL(cut_blocks_kernel, dim3(1), dim3(1024), 0, st, p->item0[l], p->nblocks, p->cut_block[l], cuts_dev + l);
         hipLaunchKernelGGL(stretches_kernel, dim3(blocks_for(p->nblocks)), dim3(kThreads), 0, st, p->item0[l], p->chunk0, p->rowptr, p->nblocks, p->br,
                            attn_level_chunks(l), p->item[l]);
         SP_HIP(hipGetLastError());

@@ -180,6 +180,103 @@ struct attn_item {
     }
 };
 
+// The rows of two operands (K and V; Q and dO) on their way into LDS: step s of KT columns is fetched into registers while step s - 1 is
+// computed, and its columns' places a step earlier still.  CAUSAL rows whose position no row of the block attends to are not read
+// but set to zero, so that what lies in a cache's free slots does not matter.
+template <typename T, int DT, int NT, int KT, bool POS>
+struct attn_feed {
+    typedef attn_tile<T, DT> tile;
+    typedef typename tile::frag frag;
+    static constexpr int kPieces = KT * tile::kGranules / NT, kRowStep = NT / tile::kGranules;
+    static_assert(KT * tile::kGranules % NT == 0 && NT % tile::kGranules == 0 && KT <= NT, "every thread fetches the same number of granules");
+    const T *X, *Y;
+    int64_t ldx, ldy;
+    attn_columns cols;
+    int64_t x0;                          // the item's first column among its block's
+    const int32_t *pos;                  // positions of the columns, or null
+    int limit, sign;                     // causal: rows are needed where sign * pos <= sign * limit; sign 0: everywhere
+    int D, row, g;
+    bool vec;
+    int32_t at[kPieces], next[kPieces], one, one_next;       // columns of the step fetched next, and of the one after it
+    int32_t kp[kPieces], kp_one;
+    frag x[kPieces], y[kPieces];
+    int32_t arrived, arrived_at;                         // thread tid < KT: the position, and the column, of column tid of the step in x, y
+
+    __device__ __forceinline__ void columns(int64_t step)
+    {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) next[k] = cols.get(x0 + step * KT + row + k * kRowStep);
+        one_next = cols.get(x0 + step * KT + (threadIdx.x < KT ? threadIdx.x : 0));
+    }
+    // the columns asked for last become those of the next rows(); their positions are on the way
+    __device__ __forceinline__ void advance()
+    {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) at[k] = next[k];
+        one = one_next;
+        if (POS && pos) {
+            kp_one = pos[one];
+            if (sign != 0) {
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) kp[k] = pos[at[k]];
+            }
+        }
+    }
+    __device__ __forceinline__ void rows(const T *X, const T *Y)
+    {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            const bool need = !POS || sign == 0 || (sign > 0 ? kp[k] <= limit : kp[k] >= limit);
+            x[k] = tile::granule(X + (int64_t)at[k] * ldx, g * tile::kPer, D, vec, need);
+            y[k] = tile::granule(Y + (int64_t)at[k] * ldy, g * tile::kPer, D, vec, need);
+        }
+        arrived = kp_one;
+        arrived_at = one;
+    }
+    __device__ __forceinline__ void put(attn_lds *tx, attn_lds *ty)
+    {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            tile::put(tx, row + k * kRowStep, g, x[k]);
+            tile::put(ty, row + k * kRowStep, g, y[k]);
+        }
+    }
+};
+
+// Positions of a tile's 32 columns against those of the wave's rows.  A tile that lies wholly past the last border on one side has one
+// bias for each head.
+struct attn_near {
+    bool nothing, ask, far;              // causal leaves nothing / something out; all distances share a bucket
+    int bucket;                          // that bucket
+};
+// col: this lane's column's position (lane % 32).  lo, hi: the least and largest distance that the wave's rows give it; a: borders
+__device__ __forceinline__ attn_near attn_look(const attn_args &a, int lo, int hi)
+{
+    attn_near n = {false, false, false, 0};
+    if (a.causal) {
+        n.ask = __builtin_amdgcn_ballot_w64(hi > 0) != 0;
+        n.nothing = n.ask && __builtin_amdgcn_ballot_w64(lo <= 0) == 0;
+    }
+    if (a.buckets) {
+        const bool ahead = __builtin_amdgcn_ballot_w64(lo < a.last) == 0, behind = __builtin_amdgcn_ballot_w64(hi > -a.last) == 0;
+        n.far = ahead || behind;
+        n.bucket = attn_far_bucket(a, ahead);
+    }
+    return n;
+}
+__device__ __forceinline__ int attn_wave_min(int v)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) { const int o = __shfl_xor(v, d, 64); v = o < v ? o : v; }
+    return v;
+}
+__device__ __forceinline__ int attn_wave_max(int v)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) { const int o = __shfl_xor(v, d, 64); v = o > v ? o : v; }
+    return v;
+}
+
 // The position bias in LDS: the bucket of every distance up to the last border, and the table's columns of the heads at hand.
 struct attn_bias {
     const uint8_t *lut;                  // [2 last + 1]
@@ -217,7 +314,8 @@ enum { kRowsOfHead,                      // br = 128: the workgroup's waves take
        kRowsTogether,                    // br = 32: one tile, 32 rows of one head; the waves share its columns out
        kHeadsTogether };                 // br = 1: one tile, up to 32 heads of one row; the waves share its columns out
 
-// A lane's query and head.  group: which heads the workgroup takes, of attn_groups().
+// A lane's query and head.  group: which of an item's workgroups this is.  The heads of one key head are Hk workgroups apart, so that with 8 key
+// heads or 4 they run on one compute die or two, whose L2 they share K and V in.
 struct attn_lane {
     int head, kv, r;                     // r: the row's place in its block
     int64_t row;
@@ -227,13 +325,13 @@ struct attn_lane {
         r = lane & 31;
         valid = true;
         if (mode == kRowsOfHead || mode == kRowsTogether) {
-            head = group;
-            kv = head / a.G;
+            kv = group % a.Hk;
+            head = kv * a.G + group / a.Hk;
             if (mode == kRowsOfHead) r += 32 * wave;
         } else {
-            const int per = mode == kHeadsOfRows ? waves : 32, parts = (a.G + per - 1) / per;
-            kv = group / parts;
-            int x = (group % parts) * per + (mode == kHeadsOfRows ? wave : lane & 31);
+            const int per = mode == kHeadsOfRows ? waves : 32;
+            kv = group % a.Hk;
+            int x = group / a.Hk * per + (mode == kHeadsOfRows ? wave : lane & 31);
             valid = x < a.G;
             if (!valid) x = a.G - 1;
             head = kv * a.G + x;
@@ -250,9 +348,8 @@ __device__ __forceinline__ attn_bias attn_lane_bias(const attn_args &a, char *ld
 {
     const int slots = mode == kHeadsTogether ? 32 : mode == kHeadsOfRows ? waves : 1;
     attn_bias b = attn_make_bias<T>(a, lds, slots, [&](int s) {
-        if (slots == 1) return group;
-        const int parts = (a.G + slots - 1) / slots, x = (group % parts) * slots + s;
-        return x < a.G ? (group / parts) * a.G + x : -1;
+        const int x = slots == 1 ? group / a.Hk : group / a.Hk * slots + s;
+        return x < a.G ? group % a.Hk * a.G + x : -1;
     });
     b.slot = mode == kHeadsTogether ? lane & 31 : mode == kHeadsOfRows ? wave : 0;
     return b;
@@ -266,7 +363,14 @@ struct attn_mapping {
     bool cut;                            // some rows have several items
     int slots() const { return mode == kHeadsTogether ? 32 : mode == kHeadsOfRows ? wm : 1; }
 };
-static inline attn_mapping attn_map(const sp_attn_plan *plan, const attn_args &a)
+// About what a chunk of 64 columns takes a workgroup of four tiles that has a compute unit to itself, in microseconds, for a number of
+// products (forward 2: 2.0 for 128 numbers of 16 bits; f32 15).
+static inline double attn_chunk_us(int D, int size, int products)
+{
+    const double numbers = D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256;
+    return (size == 4 ? 0.06 : 0.008) * numbers * products;
+}
+static inline attn_mapping attn_map(const sp_attn_plan *plan, const attn_args &a, int size, int products)
 {
     attn_mapping c;
     if (plan->br == 128) { c.mode = kRowsOfHead; c.groups = a.H; }
@@ -276,8 +380,8 @@ static inline attn_mapping attn_map(const sp_attn_plan *plan, const attn_args &a
     const bool share = c.mode == kRowsTogether || c.mode == kHeadsTogether;
     c.wm = share ? 1 : 4;
     c.wn = share ? 4 : 1;
-    c.level = attn_pick_level(plan, c.groups);
-    c.cut = plan->items[c.level] > plan->nblocks;
+    c.level = attn_pick_level(plan, c.groups, attn_chunk_us(a.D, size, products) / (share ? 2 : 1), 4.0 * a.D * a.H);
+    c.cut = plan->cut[c.level] > 0;
     return c;
 }
 
@@ -301,6 +405,18 @@ __device__ __forceinline__ void attn_store4(T *row, int d, int D, bool vec, attn
 #pragma unroll
         for (int c = 0; c < 4; ++c) if (d + c < D) row[d + c] = (T)v[c];
     }
+}
+
+// dq_kernel: how many waves share a tile's columns, and the LDS it takes.  K and V of a step and the bias's sums have to fit together.
+constexpr int kAttnLds = 160 * 1024;
+static constexpr int attn_dq_waves(int row_bytes, bool pos) { return row_bytes == 512 && pos ? 2 : 4; }
+static constexpr int attn_dq_columns(int row_bytes) { return row_bytes == 64 ? 64 : 32; }
+static inline size_t attn_dq_lds(const attn_args &a, const attn_mapping &c, int row_bytes, bool pos, bool table, bool exact)
+{
+    const bool share = c.wn > 1;
+    const int waves = share ? attn_dq_waves(row_bytes, pos) : 4, KT = share ? 32 * waves : attn_dq_columns(row_bytes);
+    const size_t lds = 2 * (size_t)KT * row_bytes + (pos ? KT * 4 + attn_bias_bytes(a, c.slots()) : 0) + (table ? (size_t)waves * a.buckets * (exact ? 512 : 256) : 0);
+    return lds;
 }
 
 // ---- what attention.hip hands to the sources of one type ---------------------------------------------------------------------
@@ -329,10 +445,12 @@ struct grad_args {
     float *part;                         // of rows (keys) that are cut: dq [item][head][row of the block][pd]; dkv [item][kv head][key][2][pd]
     float *part_table;                   // [item][head][buckets]
     int groups, mode, vec, pd;
+    int exact;                           // how the bias's gradient is summed: see dq_kernel
 };
 
 struct grad_choice {
     attn_mapping rows;
+    bool exact;
     int keys_level;
     bool keys_cut;
     size_t delta, part, table;           // bytes; the parts of dQ and of dK, dV use the same place one after the other

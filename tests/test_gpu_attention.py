@@ -109,8 +109,18 @@ def test_patterns(name, dt):
 @pytest.mark.parametrize("D", [1, 7, 8, 31, 32, 40, 64, 80, 100, 128, 136, 192, 256])
 def test_head_sizes(D, dt):
     say("case head size", D, dt)
+    if dt == F32 and D > 128:                            # does not fit a lane's registers: refused
+        with pytest.raises(sp.SpError):
+            check_all(ragged([70, 33], [65, 100]), 2, 1, D, dt)
+        return
     check_all(ragged([70, 33], [65, 100]), 2, 1, D, dt)
     check_all(ragged([1, 1, 1], [300, 17, 64]), 2, 2, D, dt)
+    # with a bias: rows of blocks, single rows, few rows of many heads
+    where = dict(positions=(torch.arange(103) + 20, torch.arange(165)), buckets=32, causal=True, bidirectional=False)
+    check_all(ragged([70, 33], [65, 100]), 2, 1, D, dt, **where)
+    check_all(ragged([70, 33], [65, 100]), 8, 1, D, dt, **where)
+    check_all(ragged([1, 1, 1], [300, 17, 64]), 2, 2, D, dt, positions=(torch.tensor([200, 10, 60]), torch.arange(381)), buckets=64, max_distance=200)
+    check_all(torch.ones(9, 400, dtype=torch.bool), 6, 1, D, dt, positions=(torch.arange(9) * 40, torch.arange(400)), buckets=64, max_distance=200)
 
 
 @pytest.mark.parametrize("heads", [(1, 1), (2, 1), (3, 1), (6, 2), (8, 8), (8, 1), (40, 1), (70, 2)])
