@@ -26,7 +26,7 @@ grad_choice choose(const sp_tensor *S, const attn_args &a, int size, bool table)
     const int row = (a.D <= 32 ? 32 : a.D <= 64 ? 64 : a.D <= 128 ? 128 : 256) * size;
     c.exact = table && size == 2 && attn_dq_lds(a, c.rows, row, true, true, true) <= kAttnLds;
     if (c.exact) { c.rows.level = rows->levels - 1; c.rows.cut = false; }
-    c.keys_level = attn_pick_level(keys, a.Hk, attn_chunk_us(a.D, size, 4) * a.G * (keys->br == 128 ? 1 : 0.7), 8.0 * a.D * a.Hk);
+    c.keys_level = attn_pick_level(keys, a.Hk, attn_chunk_us(a.D, size, 4) * a.G * (keys->br == 128 ? 1 : 0.7), 3, 8.0 * a.D * a.Hk);
     c.keys_cut = keys->cut[c.keys_level] > 0;
     const size_t p1 = c.rows.cut ? (size_t)rows->items[c.rows.level] * a.H * rows->br * padded(a.D) * 4 : 0;
     const size_t p2 = c.keys_cut ? (size_t)keys->items[c.keys_level] * a.Hk * keys->br * 2 * padded(a.D) * 4 : 0;

@@ -48,11 +48,20 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     constexpr int NT = 64 * WM * WN, KT = KW * WN, TILES = KW / 32;
     constexpr int STEP = KT > kAttnChunk ? KT / kAttnChunk : 1, SUB = KT < kAttnChunk ? kAttnChunk / KT : 1;
     extern __shared__ __align__(16) char lds[];
-    attn_lds *sK = (attn_lds *)lds, *sV = sK + KT * tile::kRow;
-    int *s_kpos = (int *)(lds + 2 * KT * tile::kRow);
+    constexpr int FT = WN > 1 ? 64 : NT, FC = WN > 1 ? KW : KT;
     const attn_args &a = f.a;
     const attn_plan_view &p = f.p;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = WN > 1 ? wave : 0;
+    const int ftid = WN > 1 ? lane : tid;
+    attn_lds *sK = (attn_lds *)lds + wn * FC * tile::kRow, *sV = sK + KT * tile::kRow;
+    attn_lds_i32 *s_kpos = (attn_lds_i32 *)((attn_lds *)lds + 2 * KT * tile::kRow) + wn * FC;
+    auto meet = [] {
+        if (WN == 1) __syncthreads();
+        else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
     const int64_t item_no = blockIdx.x / f.groups;
     const int group = blockIdx.x % f.groups;
     const attn_item item(p, item_no);
@@ -70,15 +79,15 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     const float delta = f.delta[me.head * a.m + me.row];
     int qp = 0, q_lo = 0, q_hi = 0;
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
-    float *hist = nullptr;                               // [buckets][64] of ds or p dP, exact: then [buckets][64] of p
+    attn_lds_f32 *hist = nullptr;                             // [buckets][64] of ds or p dP, exact: then [buckets][64] of p
     const int hist_size = a.buckets * 64 * (f.exact ? 2 : 1);
     float far_x[2] = {0, 0}, far_p[2] = {0, 0};          // the far buckets behind and ahead
     if (POS) {
         if (a.qpos) { qp = a.qpos[me.row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
         if (a.buckets) {
-            bias = attn_lane_bias<T>(a, lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
+            bias = attn_lane_bias<T>(a, (attn_lds *)lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
             if (f.part_table) {
-                hist = (float *)(bias.table + a.buckets * bias.slots) + wave * hist_size;
+                hist = bias.table + a.buckets * bias.slots + wave * hist_size;
                 for (int b = lane; b < hist_size; b += 64) hist[b] = 0;
             }
         }
@@ -88,11 +97,12 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     for (int x = 0; x < tile::kBlocks; ++x) acc[x] = (attn_f32x16)(0.f);
 
     const int64_t steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
-    attn_feed<T, DT, NT, KT, POS> feed;
+    if (POS && WN > 1) __syncthreads();
+    attn_feed<T, DT, FT, FC, POS> feed;
     feed.ldx = a.ldk; feed.ldy = a.ldv;
-    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk;
+    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk + wn * FC; feed.step = KT; feed.tid = ftid;
     feed.pos = a.kpos; feed.sign = a.causal; feed.limit = q_hi;
-    feed.D = a.D; feed.vec = f.vec; feed.row = tid / tile::kGranules; feed.g = tid % tile::kGranules;
+    feed.D = a.D; feed.vec = f.vec; feed.row = ftid / tile::kGranules; feed.g = ftid % tile::kGranules;
     const T *Kh = (const T *)a.K + (int64_t)me.kv * a.hdk, *Vh = (const T *)a.V + (int64_t)me.kv * a.hdv;
     if (POS && a.causal && WM > 1) {
         if (lane == 0) s_kpos[wave] = q_hi;
@@ -121,10 +131,10 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         feed.rows(Kh, Vh);
     }
     for (int64_t step = 0; step < steps; ++step) {
-        __syncthreads();
+        meet();
         feed.put(sK, sV);
-        if (POS && tid < KT) s_kpos[tid] = feed.arrived;
-        __syncthreads();
+        if (POS && ftid < FC) s_kpos[ftid] = feed.arrived;
+        meet();
         word = word_next; state = state_next;
         if (step + 1 < steps) {
             feed.advance();
@@ -139,15 +149,15 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         word >>= col0 % kAttnChunk;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
-            const int *kp = s_kpos + wn * KW + 32 * t;
+            const attn_lds_i32 *kp = s_kpos + 32 * t;
             attn_near near = {false, false, false, 0};
             if (POS) {
                 const int col = kp[lane & 31];
                 near = attn_look(a, attn_distance(col, q_hi), attn_distance(col, q_lo));
                 if (near.nothing) continue;
             }
-            attn_f32x16 s = tile::scores(sK, wn * KW + 32 * t, q, lane);
-            attn_f32x16 dp = tile::scores(sV, wn * KW + 32 * t, go, lane);
+            attn_f32x16 s = tile::scores(sK, 32 * t, q, lane);
+            attn_f32x16 dp = tile::scores(sV, 32 * t, go, lane);
             // what is not stored, and rows that do not exist, add nothing
             const uint32_t bits = (me.valid ? (uint32_t)(word >> (32 * t)) : 0u) >> (4 * (lane >> 5));
             if (!POS) {
@@ -157,37 +167,48 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                     s[x] = there ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], cc, -off)) * (dp[x] - delta) : 0.f;
                 }
             } else {
-                // weights first, in s; a score of minus infinity has weight 0, whatever dP is
+                // Loops of one kind of work each, without branches inside, so that the LDS's answers overlap.  A score of minus
+                // infinity has weight 0, whatever dP is.
                 const bool one = !a.buckets || near.far;
-                const float all_of = a.buckets && near.far ? bias.at(near.bucket) : 0.f;
+                uint32_t there = 0;
+                int bucket[16];
+#pragma unroll
+                for (int x = 0; x < 16; ++x) there |= (bits >> (8 * (x >> 2) + (x & 3)) & 1) << x;
+                if (near.ask) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) there &= ~((uint32_t)(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)] > qp) << x);
+                }
+                if (one) {
+                    const float all_of = a.buckets ? bias.at(near.bucket) : 0.f;
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, all_of);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) bucket[x] = bias.bucket(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(bucket[x]));
+                }
                 float sum_x = 0, sum_p = 0;
 #pragma unroll
                 for (int x = 0; x < 16; ++x) {
-                    const int col = 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3);
-                    bool there = bits >> (8 * (x >> 2) + (x & 3)) & 1;
-                    if (near.ask) there = there && kp[col] <= qp;
-                    int bucket = 0;
-                    float v = all_of;
-                    if (!one) { bucket = bias.bucket(kp[col], qp); v = bias.at(bucket); }
-                    v = __builtin_fmaf(s[x], a.scale, v);
-                    there = there && v != -INFINITY;
-                    const float w = there ? __builtin_amdgcn_exp2f((v - off) * cc) : 0.f;
-                    s[x] = there ? w * (dp[x] - delta) : 0.f;
-                    if (hist) {
-                        const float term = f.exact ? (there ? w * dp[x] : 0.f) : s[x];
-                        if (one) { sum_x += term; sum_p += w; }
-                        else if (there) {
-                            atomicAdd(&hist[bucket * 64 + lane], term);       // a place of this lane's own: one order
-                            if (f.exact) atomicAdd(&hist[(a.buckets + bucket) * 64 + lane], w);
-                        }
+                    const bool on = (there >> x & 1) && s[x] != -INFINITY;
+                    const float w = on ? __builtin_amdgcn_exp2f((s[x] - off) * cc) : 0.f;
+                    const float term = on ? w * dp[x] : 0.f;
+                    s[x] = on ? w * (dp[x] - delta) : 0.f;
+                    dp[x] = f.exact ? term : s[x];
+                    if (one) { sum_x += dp[x]; sum_p += w; }
+                    else if (hist) {                     // a place of this lane's own: one order
+                        attn_lds_add(hist + bucket[x] * 64 + lane, dp[x]);
+                        if (f.exact) attn_lds_add(hist + (a.buckets + bucket[x]) * 64 + lane, w);
                     }
                 }
                 if (hist && one) {
-                    const int side = near.bucket == a.side - 1 ? 0 : 1;
-                    if (side) { far_x[1] += sum_x; far_p[1] += sum_p; } else { far_x[0] += sum_x; far_p[0] += sum_p; }
+                    const bool behind = near.bucket == a.side - 1;
+                    far_x[0] += behind ? sum_x : 0.f; far_p[0] += behind ? sum_p : 0.f;
+                    far_x[1] += behind ? 0.f : sum_x; far_p[1] += behind ? 0.f : sum_p;
                 }
             }
-            tile::add_rows(acc, sK, wn * KW + 32 * t, s, lane);
+            tile::add_rows(acc, sK, 32 * t, s, lane);
         }
     }
     float odd = 0;
@@ -198,6 +219,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     uint64_t again = __builtin_amdgcn_ballot_w64(me.valid && !(odd == 0.f));
 
     if (POS && hist) {
+        __syncthreads();                                 // all waves are done with K
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
             const int b = attn_far_bucket(a, side == 1);
@@ -205,8 +227,8 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
             if (f.exact) hist[(a.buckets + b) * 64 + lane] += far_p[side];
         }
         __syncthreads();
-        const float *all = (const float *)(bias.table + a.buckets * bias.slots);
-        float *s_delta = (float *)lds;                   // over K: [waves][32], each row's D
+        const attn_lds_f32 *all = bias.table + a.buckets * bias.slots;
+        attn_lds_f32 *s_delta = (attn_lds_f32 *)(attn_lds *)lds;     // over K: [waves][32], each row's D
         // rows are a wave's own, or (WN) shared by all waves
         if (f.exact && lane < 32 && (WN == 1 || wave == 0)) {
             float d = 0;
@@ -260,13 +282,13 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         }
     } else {
         __syncthreads();
-        float *sums = (float *)lds, *bad = (float *)lds + WN * 32 * DT;
+        attn_lds_f32 *sums = (attn_lds_f32 *)(attn_lds *)lds, *bad = sums + WN * 32 * DT;
 #pragma unroll
         for (int x = 0; x < tile::kBlocks; ++x)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int g = (8 * x + 2 * b + (lane >> 5)) ^ (lane & 7);
-                *(attn_f32x4 *)(sums + (wn * 32 + (lane & 31)) * DT + 4 * g) = (attn_f32x4){acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
+                *(attn_lds_f32x4 *)(sums + (wn * 32 + (lane & 31)) * DT + 4 * g) = (attn_f32x4){acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
             }
         if (lane < 32) bad[wn * 32 + lane] = (again | again >> 32) >> lane & 1 ? 1.f : 0.f;
         __syncthreads();
@@ -285,7 +307,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                 const int d = part * EACH + k;
                 attn_f32x4 v = (attn_f32x4)(0.f);
 #pragma unroll
-                for (int x = 0; x < WN; ++x) v += *(attn_f32x4 *)(sums + (x * 32 + mine) * DT + 4 * ((d >> 2) ^ (mine & 7)));
+                for (int x = 0; x < WN; ++x) v += *(attn_lds_f32x4 *)(sums + (x * 32 + mine) * DT + 4 * ((d >> 2) ^ (mine & 7)));
                 if (item.whole) attn_store4((T *)f.g.dQ + row2 * f.g.lddq + head2 * f.g.hddq, d, a.D, f.vec, v * a.scale);
                 else attn_store4(f.part + place2 * f.pd, d, f.pd, true, v);
             }
@@ -327,8 +349,8 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     static_assert(KT <= kAttnChunk, "steps within a chunk");
     extern __shared__ __align__(16) char lds[];
     attn_lds *sQ = (attn_lds *)lds, *sO = sQ + KT * tile::kRow;
-    float *s_lse = (float *)(lds + 2 * KT * tile::kRow), *s_delta = s_lse + KT;
-    int *s_qpos = (int *)(s_delta + KT);
+    attn_lds_f32 *s_lse = (attn_lds_f32 *)(sQ + 2 * KT * tile::kRow), *s_delta = s_lse + KT;
+    attn_lds_i32 *s_qpos = (attn_lds_i32 *)(s_delta + KT);
     const attn_args &a = f.a;
     const attn_plan_view &p = f.p;                       // of the transposed pattern: rows are keys
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -346,12 +368,12 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     tile::load_lane((const T *)a.V + key * a.ldv + kv * a.hdv, a.D, f.vec, some, 1.f, vx, lane);
     int kp = 0, k_lo = 0, k_hi = 0;
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
-    float *table = nullptr;
+    attn_lds_f32 *table = nullptr;
     if (POS) {
         if (a.kpos) { kp = a.kpos[key]; k_lo = attn_wave_min(kp); k_hi = attn_wave_max(kp); }
         if (a.buckets) {
-            bias = attn_make_bias<T>(a, (char *)(s_qpos + KT), 1, [&](int) { return kv * a.G; });
-            table = const_cast<float *>(bias.table);
+            bias = attn_make_bias<T>(a, (attn_lds *)(s_qpos + KT), 1, [&](int) { return kv * a.G; });
+            table = bias.table;
         }
     }
     attn_f32x16 dk[tile::kBlocks], dv[tile::kBlocks];
@@ -361,7 +383,7 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     const int64_t per_head = (int64_t)(item.c1 - item.c0) * SUB, steps = per_head * a.G;
     attn_feed<T, DT, NT, KT, POS> feed;
     feed.ldx = a.ldq; feed.ldy = f.g.lddo;
-    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk;
+    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk; feed.step = KT; feed.tid = tid;
     feed.pos = a.qpos; feed.sign = -a.causal; feed.limit = k_lo;
     feed.D = a.D; feed.vec = f.vec; feed.row = tid / tile::kGranules; feed.g = tid % tile::kGranules;
     if (POS && a.causal && WM > 1) {
@@ -429,26 +451,36 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
             attn_f32x16 s = tile::scores(sQ, 32 * t, kx, lane);
             attn_f32x16 dp = tile::scores(sO, 32 * t, vx, lane);
             const uint32_t bits = (valid ? (uint32_t)(word >> (32 * t)) : 0u) >> (4 * (lane >> 5));
-            const bool one = !a.buckets || near.far;
-            const float all_of = POS && a.buckets && near.far ? bias.at(near.bucket) : 0.f;
+            uint32_t there = bits;
+            if (POS) {
+                if (near.ask) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x)
+                        there &= ~((uint32_t)(kp > s_qpos[32 * t + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]) << (8 * (x >> 2) + (x & 3)));
+                }
+                if (!a.buckets || near.far) {
+                    const float all_of = a.buckets ? bias.at(near.bucket) : 0.f;
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, all_of);
+                } else {
+                    int bucket[16];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) bucket[x] = bias.bucket(kp, s_qpos[32 * t + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(bucket[x]));
+                }
+            }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int q0 = 32 * t + 8 * b + 4 * (lane >> 5);
-                const attn_f32x4 lse = *(const attn_f32x4 *)(s_lse + q0), delta = *(const attn_f32x4 *)(s_delta + q0);
+                const attn_f32x4 lse = *(const attn_lds_f32x4 *)(s_lse + q0), delta = *(const attn_lds_f32x4 *)(s_delta + q0);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const int x = 4 * b + c;
-                    bool there = bits >> (8 * b + c) & 1;
-                    float v = s[x];
-                    if (POS) {
-                        v = __builtin_fmaf(v, a.scale, one ? all_of : bias.at(bias.bucket(kp, s_qpos[q0 + c])));
-                        if (near.ask) there = there && kp <= s_qpos[q0 + c];
-                        there = there && v != -INFINITY;
-                        v = (v - lse[c]) * cc;
-                    } else v = __builtin_fmaf(v, cc, -lse[c]);
-                    v = there ? __builtin_amdgcn_exp2f(v) : 0.f;
-                    s[x] = v;
-                    dp[x] = there ? v * (dp[x] - delta[c]) : 0.f;
+                    const bool on = (there >> (8 * b + c) & 1) && (!POS || s[x] != -INFINITY);     // a score of minus infinity has weight 0
+                    const float w = on ? __builtin_amdgcn_exp2f(POS ? (s[x] - lse[c]) * cc : __builtin_fmaf(s[x], cc, -lse[c])) : 0.f;
+                    s[x] = w;
+                    dp[x] = on ? w * (dp[x] - delta[c]) : 0.f;
                 }
             }
             tile::add_rows(dv, sO, 32 * t, s, lane);

@@ -23,11 +23,21 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     constexpr int STEP = KT > kAttnChunk ? KT / kAttnChunk : 1;         // chunks of a step (or one chunk in 64 / KT steps)
     constexpr int SUB = KT < kAttnChunk ? kAttnChunk / KT : 1;
     extern __shared__ __align__(16) char lds[];
-    attn_lds *sK = (attn_lds *)lds, *sV = sK + KT * tile::kRow;
-    int *s_kpos = (int *)(lds + 2 * KT * tile::kRow);    // POS: [KT]
+    // WM waves fetch a step together and meet at barriers; WN waves fetch a share of it each, into a place of their own, and do not meet
+    constexpr int FT = WN > 1 ? 64 : NT, FC = WN > 1 ? KW : KT;
     const attn_args &a = f.a;
     const attn_plan_view &p = f.p;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = WN > 1 ? wave : 0;
+    const int ftid = WN > 1 ? lane : tid;
+    attn_lds *sK = (attn_lds *)lds + wn * FC * tile::kRow, *sV = sK + KT * tile::kRow;
+    attn_lds_i32 *s_kpos = (attn_lds_i32 *)((attn_lds *)lds + 2 * KT * tile::kRow) + wn * FC;    // POS: [FC]
+    auto meet = [] {
+        if (WN == 1) __syncthreads();
+        else {                                           // LDS is in order for a wave
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
     const int64_t item_no = blockIdx.x / f.groups;
     const int group = blockIdx.x % f.groups;
     const attn_item item(p, item_no);
@@ -45,7 +55,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
     if (POS) {
         if (a.qpos) { qp = a.qpos[row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
-        if (a.buckets) bias = attn_lane_bias<T>(a, lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
+        if (a.buckets) bias = attn_lane_bias<T>(a, (attn_lds *)lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
     }
 
     attn_f32x16 acc[tile::kBlocks];
@@ -54,11 +64,12 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     float top = -INFINITY, total = 0;
 
     const int64_t steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
-    attn_feed<T, DT, NT, KT, POS> feed;
+    if (POS && WN > 1) __syncthreads();                  // the bias's tables
+    attn_feed<T, DT, FT, FC, POS> feed;
     feed.ldx = a.ldk; feed.ldy = a.ldv;
-    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk;
+    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk + wn * FC; feed.step = KT; feed.tid = ftid;
     feed.pos = a.kpos; feed.sign = a.causal; feed.limit = q_hi;
-    feed.D = a.D; feed.vec = f.vec; feed.row = tid / tile::kGranules; feed.g = tid % tile::kGranules;
+    feed.D = a.D; feed.vec = f.vec; feed.row = ftid / tile::kGranules; feed.g = ftid % tile::kGranules;
     const T *Kh = (const T *)a.K + (int64_t)kv * a.hdk, *Vh = (const T *)a.V + (int64_t)kv * a.hdv;
     if (POS && a.causal && WM > 1) {                     // the last position that any row of the block attends to
         if (lane == 0) s_kpos[wave] = q_hi;
@@ -89,10 +100,10 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
         feed.rows(Kh, Vh);
     }
     for (int64_t step = 0; step < steps; ++step) {
-        __syncthreads();                                 // the step before has been computed
+        meet();                                          // the step before has been computed
         feed.put(sK, sV);
-        if (POS && tid < KT) s_kpos[tid] = feed.arrived;
-        __syncthreads();
+        if (POS && ftid < FC) s_kpos[ftid] = feed.arrived;
+        meet();
         word = word_next; state = state_next;
         if (step + 1 < steps) {
             feed.advance();
@@ -111,7 +122,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
         float up = top;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
-            const int *kp = s_kpos + wn * KW + 32 * t;
+            const attn_lds_i32 *kp = s_kpos + 32 * t;
             attn_near near = {false, false, false, 0};
             if (POS) {
                 const int col = kp[lane & 31];
@@ -121,7 +132,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
                     continue;
                 }
             }
-            s[t] = tile::scores(sK, wn * KW + 32 * t, q, lane);
+            s[t] = tile::scores(sK, 32 * t, q, lane);
             if (POS) {
                 if (a.buckets && !near.far) {
 #pragma unroll
@@ -162,7 +173,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
                 s[t][x] = __builtin_amdgcn_exp2f(POS ? (s[t][x] - base) * cc : __builtin_fmaf(s[t][x], cc, off));
                 total += s[t][x];
             }
-            tile::add_rows(acc, sV, wn * KW + 32 * t, s[t], lane);
+            tile::add_rows(acc, sV, 32 * t, s[t], lane);
         }
     }
     total = attn_pair_sum(total);
@@ -199,16 +210,16 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     } else {
         // the waves' shares of the tile meet in LDS, over K and V
         __syncthreads();
-        float *sums = (float *)lds, *stats = (float *)lds + WN * 32 * DT;        // [WN][32][DT], numbers exchanged by row; [WN][32][3]
+        attn_lds_f32 *sums = (attn_lds_f32 *)(attn_lds *)lds, *stats = sums + WN * 32 * DT;        // [WN][32][DT], numbers exchanged by row; [WN][32][3]
 #pragma unroll
         for (int x = 0; x < tile::kBlocks; ++x)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int g = (8 * x + 2 * b + (lane >> 5)) ^ (lane & 7);
-                *(attn_f32x4 *)(sums + (wn * 32 + (lane & 31)) * DT + 4 * g) = (attn_f32x4){acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
+                *(attn_lds_f32x4 *)(sums + (wn * 32 + (lane & 31)) * DT + 4 * g) = (attn_f32x4){acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
             }
         if (lane < 32) {
-            float *st = stats + (wn * 32 + lane) * 3;
+            attn_lds_f32 *st = stats + (wn * 32 + lane) * 3;
             st[0] = top; st[1] = total;
             st[2] = (again | again >> 32) >> lane & 1 ? 1.f : 0.f;
         }
@@ -241,7 +252,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
                 const int d = part * EACH + k;
                 attn_f32x4 v = (attn_f32x4)(0.f);
 #pragma unroll
-                for (int x = 0; x < WN; ++x) v += *(attn_f32x4 *)(sums + (x * 32 + mine) * DT + 4 * ((d >> 2) ^ (mine & 7))) * w[x];
+                for (int x = 0; x < WN; ++x) v += *(attn_lds_f32x4 *)(sums + (x * 32 + mine) * DT + 4 * ((d >> 2) ^ (mine & 7))) * w[x];
                 if (item.whole) attn_store4(out2, d, a.D, f.vec, v * inv);
                 else if (sum != 0) attn_store4(f.part + place2 * f.pd, d, f.pd, true, v);
             }

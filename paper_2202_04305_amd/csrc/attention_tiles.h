@@ -17,7 +17,12 @@
 typedef float attn_f32x16 __attribute__((ext_vector_type(16)));
 typedef float attn_f32x4 __attribute__((ext_vector_type(4)));
 typedef short attn_s16x4 __attribute__((ext_vector_type(4)));
+// Pointers into LDS say so: through a generic pointer every access would be a flat one, which waits for memory too.
 typedef __attribute__((address_space(3))) char attn_lds;
+typedef __attribute__((address_space(3))) float attn_lds_f32;
+typedef __attribute__((address_space(3))) attn_f32x4 attn_lds_f32x4;
+typedef __attribute__((address_space(3))) int attn_lds_i32;
+typedef __attribute__((address_space(3))) uint8_t attn_lds_u8;
 
 template <typename T> struct attn_mma;
 template <> struct attn_mma<attn_bf16> {
@@ -142,6 +147,9 @@ __device__ __forceinline__ float attn_pair_sum(float v)
     return __uint_as_float(lo) + __uint_as_float(hi);
 }
 
+// *p += v, a number of LDS that only this lane adds to: an instruction without an answer to wait for.
+__device__ __forceinline__ void attn_lds_add(attn_lds_f32 *p, float v) { __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+
 // Where a work item's columns come from: a plan's list of a block, or a row's stretch of crd.
 struct attn_columns {
     const int32_t *at;
@@ -195,18 +203,18 @@ struct attn_feed {
     int64_t x0;                          // the item's first column among its block's
     const int32_t *pos;                  // positions of the columns, or null
     int limit, sign;                     // causal: rows are needed where sign * pos <= sign * limit; sign 0: everywhere
-    int D, row, g;
+    int D, row, g, step, tid;            // step: columns from one step to the next; tid: among the NT threads that fetch together
     bool vec;
     int32_t at[kPieces], next[kPieces], one, one_next;       // columns of the step fetched next, and of the one after it
     int32_t kp[kPieces], kp_one;
     frag x[kPieces], y[kPieces];
-    int32_t arrived, arrived_at;                         // thread tid < KT: the position, and the column, of column tid of the step in x, y
+    int32_t arrived;                     // thread tid < KT: the position of column tid of the step in x, y
 
-    __device__ __forceinline__ void columns(int64_t step)
+    __device__ __forceinline__ void columns(int64_t s)
     {
 #pragma unroll
-        for (int k = 0; k < kPieces; ++k) next[k] = cols.get(x0 + step * KT + row + k * kRowStep);
-        one_next = cols.get(x0 + step * KT + (threadIdx.x < KT ? threadIdx.x : 0));
+        for (int k = 0; k < kPieces; ++k) next[k] = cols.get(x0 + s * step + row + k * kRowStep);
+        one_next = cols.get(x0 + s * step + (tid < KT ? tid : 0));
     }
     // the columns asked for last become those of the next rows(); their positions are on the way
     __device__ __forceinline__ void advance()
@@ -231,7 +239,6 @@ struct attn_feed {
             y[k] = tile::granule(Y + (int64_t)at[k] * ldy, g * tile::kPer, D, vec, need);
         }
         arrived = kp_one;
-        arrived_at = one;
     }
     __device__ __forceinline__ void put(attn_lds *tx, attn_lds *ty)
     {
@@ -279,8 +286,8 @@ __device__ __forceinline__ int attn_wave_max(int v)
 
 // The position bias in LDS: the bucket of every distance up to the last border, and the table's columns of the heads at hand.
 struct attn_bias {
-    const uint8_t *lut;                  // [2 last + 1]
-    const float *table;                  // [buckets][slots]
+    const attn_lds_u8 *lut;              // [2 last + 1]
+    attn_lds_f32 *table;                 // [buckets][slots]
     int last, slots, slot;
     __device__ __forceinline__ int bucket(int kp, int qp) const
     {
@@ -296,10 +303,10 @@ static inline size_t attn_bias_bytes(const attn_args &a, int slots)
 }
 // by the whole workgroup; the caller synchronises.  head(slot): the head of a slot, or -1
 template <typename T, typename HEAD>
-__device__ __forceinline__ attn_bias attn_make_bias(const attn_args &a, char *lds, int slots, HEAD head)
+__device__ __forceinline__ attn_bias attn_make_bias(const attn_args &a, attn_lds *lds, int slots, HEAD head)
 {
-    uint8_t *lut = (uint8_t *)lds;
-    float *table = (float *)(lds + ((2 * a.last + 1 + 15) & ~15));
+    attn_lds_u8 *lut = (attn_lds_u8 *)lds;
+    attn_lds_f32 *table = (attn_lds_f32 *)(lds + ((2 * a.last + 1 + 15) & ~15));
     for (int x = threadIdx.x; x <= 2 * a.last; x += blockDim.x) lut[x] = (uint8_t)attn_bucket(a, x - a.last);
     for (int x = threadIdx.x; x < a.buckets * slots; x += blockDim.x) {
         const int h = head(x % slots);
@@ -344,7 +351,7 @@ struct attn_lane {
 };
 // the bias for the workgroup's heads, its slot for this lane
 template <typename T>
-__device__ __forceinline__ attn_bias attn_lane_bias(const attn_args &a, char *lds, int mode, int group, int lane, int wave, int waves)
+__device__ __forceinline__ attn_bias attn_lane_bias(const attn_args &a, attn_lds *lds, int mode, int group, int lane, int wave, int waves)
 {
     const int slots = mode == kHeadsTogether ? 32 : mode == kHeadsOfRows ? waves : 1;
     attn_bias b = attn_make_bias<T>(a, lds, slots, [&](int s) {
@@ -380,7 +387,7 @@ static inline attn_mapping attn_map(const sp_attn_plan *plan, const attn_args &a
     const bool share = c.mode == kRowsTogether || c.mode == kHeadsTogether;
     c.wm = share ? 1 : 4;
     c.wn = share ? 4 : 1;
-    c.level = attn_pick_level(plan, c.groups, attn_chunk_us(a.D, size, products) / (share ? 2 : 1), 4.0 * a.D * a.H);
+    c.level = attn_pick_level(plan, c.groups, attn_chunk_us(a.D, size, products) / (share ? 2 : 1), share ? 6 : 3, 4.0 * a.D * a.H);
     c.cut = plan->cut[c.level] > 0;
     return c;
 }
