@@ -33,10 +33,39 @@ __global__ __launch_bounds__(kThreads) void delta_kernel(grad_args f, float *__r
     if (l == 0 && x < a.m * a.H) delta[h * a.m + i] = s;
 }
 
+// Adds a lane's 16 pairs to its sums by bucket: hist[(bucket * 64 + lane) * N ...].  Four pairs are read, added and written back at a
+// time; where some of the four share a bucket, the later one goes on from the earlier one's sum, and the last write stays.
+template <int N>
+__device__ __forceinline__ void attn_add_by_bucket(attn_lds_f32 *hist, int lane, const int (&bucket)[16], const attn_f32x16 &x, const attn_f32x16 &y)
+{
+    typedef float sums __attribute__((ext_vector_type(N)));
+    typedef __attribute__((address_space(3))) sums lds_sums;
+#pragma unroll
+    for (int g = 0; g < 16; g += 4) {
+        lds_sums *at[4];
+        sums v[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            at[c] = (lds_sums *)hist + bucket[g + c] * 64 + lane;
+            v[c] = *at[c];
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+            for (int e = 0; e < c; ++e) v[c] = bucket[g + c] == bucket[g + e] ? v[e] : v[c];
+            v[c][0] += x[g + c];
+            if (N == 2) v[c][N - 1] += y[g + c];
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) *at[c] = v[c];
+    }
+}
+
 // dQ: the forward kernel's frame (items, gathered columns through LDS, tiles of 32 rows), with dO beside Q and V read as K is.
 //
 // With a bias its gradient as well: every lane adds its pairs' terms to a place of its own for each bucket in LDS, so that no two
 // lanes ever add to one number, and the lanes' sums are added in order at the end; tiles that share a bucket are summed in registers.
+// (Atomic adds to LDS take a cycle a lane, 64 for an instruction: 273 us for 16 sequences of 512, 12 heads, instead of XXX.)
 // `exact`: the terms are p dP and p, and ds = p (dP - D) is made of the sums with each row's D = sum p dP.  A bucket's ds almost
 // cancel, and D from an O that was rounded to 16 bits would be most of their error (2.4e-3 of the gradient instead of 1.7e-3, the
 // rounding of the result).  Not exact (f32, whose O is not rounded): the terms are ds.
@@ -79,7 +108,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     const float delta = f.delta[me.head * a.m + me.row];
     int qp = 0, q_lo = 0, q_hi = 0;
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
-    attn_lds_f32 *hist = nullptr;                             // [buckets][64] of ds or p dP, exact: then [buckets][64] of p
+    attn_lds_f32 *hist = nullptr;                             // [buckets][64] of ds; exact: of p dP and p
     const int hist_size = a.buckets * 64 * (f.exact ? 2 : 1);
     float far_x[2] = {0, 0}, far_p[2] = {0, 0};          // the far buckets behind and ahead
     if (POS) {
@@ -87,7 +116,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         if (a.buckets) {
             bias = attn_lane_bias<T>(a, (attn_lds *)lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
             if (f.part_table) {
-                hist = bias.table + a.buckets * bias.slots + wave * hist_size;
+                hist = bias.table + ((a.buckets * bias.slots + 3) & ~3) + wave * hist_size;
                 for (int b = lane; b < hist_size; b += 64) hist[b] = 0;
             }
         }
@@ -189,6 +218,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                     for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(bucket[x]));
                 }
                 float sum_x = 0, sum_p = 0;
+                attn_f32x16 weight;
 #pragma unroll
                 for (int x = 0; x < 16; ++x) {
                     const bool on = (there >> x & 1) && s[x] != -INFINITY;
@@ -197,10 +227,11 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                     s[x] = on ? w * (dp[x] - delta) : 0.f;
                     dp[x] = f.exact ? term : s[x];
                     if (one) { sum_x += dp[x]; sum_p += w; }
-                    else if (hist) {                     // a place of this lane's own: one order
-                        attn_lds_add(hist + bucket[x] * 64 + lane, dp[x]);
-                        if (f.exact) attn_lds_add(hist + (a.buckets + bucket[x]) * 64 + lane, w);
-                    }
+                    weight[x] = w;
+                }
+                if (hist && !one) {
+                    if (f.exact) attn_add_by_bucket<2>(hist, lane, bucket, dp, weight);
+                    else attn_add_by_bucket<1>(hist, lane, bucket, dp, weight);
                 }
                 if (hist && one) {
                     const bool behind = near.bucket == a.side - 1;
@@ -223,24 +254,26 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
             const int b = attn_far_bucket(a, side == 1);
-            hist[b * 64 + lane] += far_x[side];
-            if (f.exact) hist[(a.buckets + b) * 64 + lane] += far_p[side];
+            if (f.exact) {
+                hist[(b * 64 + lane) * 2] += far_x[side];
+                hist[(b * 64 + lane) * 2 + 1] += far_p[side];
+            } else hist[b * 64 + lane] += far_x[side];
         }
         __syncthreads();
-        const attn_lds_f32 *all = bias.table + a.buckets * bias.slots;
+        const attn_lds_f32 *all = bias.table + ((a.buckets * bias.slots + 3) & ~3);
         attn_lds_f32 *s_delta = (attn_lds_f32 *)(attn_lds *)lds;     // over K: [waves][32], each row's D
         // rows are a wave's own, or (WN) shared by all waves
         if (f.exact && lane < 32 && (WN == 1 || wave == 0)) {
             float d = 0;
             for (int w = wave; w < (WN == 1 ? wave + 1 : WN); ++w)
-                for (int b = 0; b < a.buckets; ++b) d += all[w * hist_size + b * 64 + lane] + all[w * hist_size + b * 64 + 32 + lane];
+                for (int b = 0; b < a.buckets; ++b) d += all[w * hist_size + (b * 64 + lane) * 2] + all[w * hist_size + (b * 64 + 32 + lane) * 2];
             s_delta[wave * 32 + lane] = d;
         }
         __syncthreads();
         float *out = f.part_table + item.part * a.H * a.buckets;
         auto term = [&](int w, int b) {
-            const float x = all[w * hist_size + b * 64 + lane];
-            return f.exact ? x - s_delta[(WN == 1 ? w : 0) * 32 + (lane & 31)] * all[w * hist_size + (a.buckets + b) * 64 + lane] : x;
+            const attn_lds_f32 *x = all + w * hist_size + (b * 64 + lane) * (f.exact ? 2 : 1);
+            return f.exact ? x[0] - s_delta[(WN == 1 ? w : 0) * 32 + (lane & 31)] * x[1] : x[0];
         };
         for (int b = wave; b < a.buckets; b += WM * WN) {
             float sum = 0;

@@ -147,9 +147,6 @@ __device__ __forceinline__ float attn_pair_sum(float v)
     return __uint_as_float(lo) + __uint_as_float(hi);
 }
 
-// *p += v, a number of LDS that only this lane adds to: an instruction without an answer to wait for.
-__device__ __forceinline__ void attn_lds_add(attn_lds_f32 *p, float v) { __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
-
 // Where a work item's columns come from: a plan's list of a block, or a row's stretch of crd.
 struct attn_columns {
     const int32_t *at;
@@ -299,7 +296,7 @@ struct attn_bias {
 };
 static inline size_t attn_bias_bytes(const attn_args &a, int slots)
 {
-    return a.buckets ? (size_t)((2 * a.last + 1 + 15) & ~15) + (size_t)a.buckets * slots * 4 : 0;
+    return a.buckets ? (size_t)((2 * a.last + 1 + 15) & ~15) + (size_t)((a.buckets * slots * 4 + 15) & ~15) : 0;
 }
 // by the whole workgroup; the caller synchronises.  head(slot): the head of a slot, or -1
 template <typename T, typename HEAD>
