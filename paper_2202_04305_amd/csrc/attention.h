@@ -6,7 +6,8 @@ constexpr int kAttnChunk = 64;           // columns of a chunk: one 64-bit word 
 constexpr int kAttnLevels = 28;
 
 // What sp_prepare_attention makes of a pattern (or of its transpose, where rows are keys and columns are queries).  Rows are
-// taken in blocks of `br`; a block's distinct columns, ascending, are cut into chunks of 64.  br = 1: a block is a row and its
+// taken in blocks of at most `br`, which end where neighbouring rows' columns lie apart (the sequences of a batch) if that takes hardly
+// more chunks than blocks of `br` throughout; a block's distinct columns, ascending, are cut into chunks of 64.  br = 1: a block is a row and its
 // columns are its stretch of crd, no bits are needed.
 //
 // A block of many rows reads a row of K and V once for all of them, and is worth it where neighbouring rows store mostly the same
@@ -15,7 +16,8 @@ struct attn_stretch {                    // what a workgroup has to know of its 
     int32_t block, chunk0;               // the block and its first chunk
     int32_t c0, c1;                      // the item's chunks
     int32_t first, count;                // the block's columns: place of the first one in cols (br = 1: in crd), how many places
-    int32_t whole, pad;                  // the block's only item
+    int32_t row0;                        // the block's first row
+    int32_t rows_whole;                  // 2 * its number of rows + 1 where it is the block's only item
 };
 
 struct sp_attn_plan {
@@ -23,6 +25,7 @@ struct sp_attn_plan {
     int64_t m, n;                        // rows and columns as this plan sees them
     int64_t nblocks, nchunks, max_chunks;
     int32_t *rowptr;                     // DEVICE [m + 1]
+    int32_t *row0;                       // DEVICE [nblocks + 1]: first row of every block; null: b * br
     const int32_t *crd;                  // DEVICE [entries], rows ascending, columns ascending within
     int32_t *crd_own;                    // the same where the plan had to make it
     int32_t *chunk0;                     // DEVICE [nblocks + 1]: first chunk of every block
@@ -44,7 +47,7 @@ static inline __host__ __device__ int attn_level_chunks(int level) { return 2 <<
 
 // A plan at one level, as kernels take it.
 struct attn_plan_view {
-    const int32_t *rowptr, *crd, *chunk0, *cols, *item0;
+    const int32_t *rowptr, *crd, *chunk0, *cols, *item0, *row0;
     const attn_stretch *item;
     const int32_t *cut_block;
     const uint64_t *bits;
@@ -54,7 +57,7 @@ struct attn_plan_view {
 };
 static inline attn_plan_view attn_view(const sp_attn_plan *p, int level)
 {
-    return {p->rowptr, p->crd, p->chunk0, p->cols, p->item0[level], p->item[level], p->cut_block[level], p->bits, p->state, p->m, p->n, p->br};
+    return {p->rowptr, p->crd, p->chunk0, p->cols, p->item0[level], p->row0, p->item[level], p->cut_block[level], p->bits, p->state, p->m, p->n, p->br};
 }
 
 // The problem as kernels take it.
@@ -112,6 +115,13 @@ __device__ __forceinline__ int attn_bucket(const attn_args &a, int r)
 __device__ __forceinline__ int attn_far_bucket(const attn_args &a, bool ahead)
 {
     return ahead ? (a.bidirectional ? 2 * a.side - 1 : 0) : a.side - 1;
+}
+
+// Block b's first row and the one behind its last.
+__host__ __device__ __forceinline__ int64_t attn_first_row(const int32_t *row0, int64_t b, int br, int64_t m)
+{
+    const int64_t x = row0 ? (int64_t)row0[b] : b * br;
+    return x < m ? x : m;
 }
 
 // Calls f(column) for every column that row r of block b stores in the block's chunks [c0, c1), until it returns false; for a whole

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     const int64_t item_no = blockIdx.x / f.groups;
     const int group = blockIdx.x % f.groups;
     const attn_item item(p, item_no);
-    const attn_lane me(a, p.br, item.block, f.mode, group, lane, wave, WM);
+    const attn_lane me(a, item, f.mode, group, lane, wave, WM);
     const int r = me.r;
     const bool busy = __builtin_amdgcn_ballot_w64(me.valid) != 0, some = me.valid && item.c1 > item.c0;
     const float cc = POS ? kLog2e : fabsf(a.c);
@@ -391,9 +391,8 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     const int kv = blockIdx.x % a.Hk;
     const attn_item item(p, item_no);
     const int r = 32 * wave + (lane & 31);
-    int64_t key = item.block * p.br + r;
-    const bool valid = key < a.n;
-    if (!valid) key = a.n - 1;
+    const bool valid = r < item.rows;
+    const int64_t key = item.row0 + (valid ? r : item.rows - 1);
     const bool busy = __builtin_amdgcn_ballot_w64(valid) != 0, some = valid && item.c1 > item.c0;
     const float cc = POS ? kLog2e : fabsf(a.c);
     frag kx[tile::kSteps], vx[tile::kSteps];
@@ -572,15 +571,15 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
 // numbers for a row (dq 1: dQ; dkv 2: dK, dV), of which the first is scaled.
 // The grid: blocks that were cut, rows of a block, heads.
 template <typename T, int LP, int PER>
-__global__ __launch_bounds__(kThreads) void join_kernel(grad_args f, int64_t cut, int64_t rows, int heads)
+__global__ __launch_bounds__(kThreads) void join_kernel(grad_args f, int64_t cut, int heads)
 {
     const attn_plan_view &p = f.p;
     const int lane = threadIdx.x & 63, D = f.a.D;
     const int64_t x = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
     if (x >= cut * p.br * heads) return;
     const int h = (int)(x % heads), r = (int)(x / heads % p.br);
-    const int64_t b = p.cut_block[x / heads / p.br], i = b * p.br + r;
-    if (i >= rows) return;
+    const int64_t b = p.cut_block[x / heads / p.br], i = attn_first_row(p.row0, b, p.br, p.m) + r;
+    if (i >= attn_first_row(p.row0, b + 1, p.br, p.m)) return;
     const int first = p.item0[b], parts = p.item0[b + 1] - first;
 #pragma unroll
     for (int v = 0; v < PER; ++v) {
@@ -663,7 +662,7 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
         if (pos) SP_TRY((launch_dq_mode<T, DT, true>(f, c.rows, items, st)));
         else SP_TRY((launch_dq_mode<T, DT, false>(f, c.rows, items, st)));
         if (c.rows.cut) hipLaunchKernelGGL((join_kernel<T, DT / 4, 1>), dim3((unsigned)ceil_div(rows->cut[c.rows.level] * rows->br * a.H, 4)), dim3(kThreads), 0, st, f,
-                                           rows->cut[c.rows.level], a.m, a.H);
+                                           rows->cut[c.rows.level], a.H);
         if (f.part_table) hipLaunchKernelGGL(table_kernel<T>, dim3((unsigned)(a.buckets * a.H)), dim3(kThreads), 0, st, f, items);
         SP_HIP(hipGetLastError());
     }
@@ -673,7 +672,7 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
         if (pos) SP_TRY((launch_dkv_mode<T, DT, true>(f, keys->br, items, st)));
         else SP_TRY((launch_dkv_mode<T, DT, false>(f, keys->br, items, st)));
         if (c.keys_cut) hipLaunchKernelGGL((join_kernel<T, DT / 4, 2>), dim3((unsigned)ceil_div(keys->cut[c.keys_level] * keys->br * a.Hk, 4)), dim3(kThreads), 0, st, f,
-                                       keys->cut[c.keys_level], a.n, a.Hk);
+                                       keys->cut[c.keys_level], a.Hk);
         SP_HIP(hipGetLastError());
     }
     return SP_OK;

@@ -42,7 +42,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     const int group = blockIdx.x % f.groups;
     const attn_item item(p, item_no);
 
-    const attn_lane me(a, p.br, item.block, f.mode, group, lane, wave, WM);
+    const attn_lane me(a, item, f.mode, group, lane, wave, WM);
     const int64_t row = me.row;
     const int head = me.head, kv = me.kv, r = me.r;
     const bool valid = me.valid;
@@ -300,8 +300,8 @@ __global__ __launch_bounds__(256) void join_kernel(forward_args f, int64_t cut)
     const int64_t x = (int64_t)blockIdx.x * 4 + wave;
     if (x >= cut * p.br * a.H) return;
     const int h = (int)(x % a.H), r = (int)(x / a.H % p.br);
-    const int64_t b = p.cut_block[x / a.H / p.br], i = b * p.br + r;
-    if (i >= a.m) return;
+    const int64_t b = p.cut_block[x / a.H / p.br], i = attn_first_row(p.row0, b, p.br, p.m) + r;
+    if (i >= attn_first_row(p.row0, b + 1, p.br, p.m)) return;
     const int first = p.item0[b], parts = p.item0[b + 1] - first;
     auto place = [&](int k) { return ((int64_t)(first + k) * a.H + h) * p.br + r; };
     float top = -INFINITY;

@@ -46,10 +46,48 @@ __device__ int32_t first_at_least(const int32_t *__restrict__ crd, int32_t s, in
     return s;
 }
 
+// Blocks of at most br rows that end where a row's stretch of columns and the next row's have no column in common, by one workgroup.
+// row0[0 .. count]: their first rows, and m.
+__global__ __launch_bounds__(1024) void blocks_kernel(const int32_t *__restrict__ rowptr, const int32_t *__restrict__ crd, int64_t m, int br,
+                                                      int32_t *__restrict__ row0, unsigned long long *__restrict__ count)
+{
+    __shared__ int32_t s_start[16];
+    __shared__ int s_count[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int32_t start_before = 0;                            // first row of the stretch that reaches into these rows
+    int64_t before = 0;
+    for (int64_t i0 = 0; i0 < m; i0 += 1024) {
+        const int64_t i = i0 + threadIdx.x;
+        bool apart = false;
+        if (i > 0 && i < m) {
+            const int32_t a = rowptr[i - 1], b = rowptr[i], c = rowptr[i + 1];
+            apart = a < b && b < c && (crd[b] > crd[b - 1] || crd[c - 1] < crd[a]);
+        }
+        int32_t start = apart ? (int32_t)i : 0;          // running maximum: the first row of each row's stretch
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) { const int32_t o = __shfl_up(start, d, 64); if (lane >= d && o > start) start = o; }
+        if (lane == 63) s_start[wave] = start;
+        __syncthreads();
+        int32_t carry = start_before;
+        for (int w = 0; w < 16; ++w) { if (w < wave && s_start[w] > carry) carry = s_start[w]; if (s_start[w] > start_before) start_before = s_start[w]; }
+        if (carry > start) start = carry;
+        const bool first = i < m && (i - start) % br == 0;
+        const uint64_t firsts = __builtin_amdgcn_ballot_w64(first);
+        if (lane == 0) s_count[wave] = __builtin_popcountll(firsts);
+        __syncthreads();
+        int64_t at = before;
+        for (int w = 0; w < 16; ++w) { at += w < wave ? s_count[w] : 0; before += s_count[w]; }
+        if (first) row0[at + __builtin_popcountll(firsts & (((uint64_t)1 << lane) - 1))] = (int32_t)i;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) { row0[before] = (int32_t)m; *count = (unsigned long long)before; }
+}
+
 // FILL = false: counts[block * windows + window] = distinct columns.  FILL = true: counts are scanned (exclusive), chunk0 is there;
 // writes cols and bits.
 template <bool FILL>
-__global__ __launch_bounds__(kThreads) void window_kernel(const int32_t *__restrict__ rowptr, const int32_t *__restrict__ crd, int64_t m, int br,
+__global__ __launch_bounds__(kThreads) void window_kernel(const int32_t *__restrict__ rowptr, const int32_t *__restrict__ crd,
+                                                          const int32_t *__restrict__ row0, int64_t m, int br,
                                                           int windows, int wlog, uint32_t *__restrict__ counts, const int32_t *__restrict__ chunk0,
                                                           int32_t *__restrict__ cols, uint32_t *__restrict__ bits)
 {
@@ -63,9 +101,9 @@ __global__ __launch_bounds__(kThreads) void window_kernel(const int32_t *__restr
     const int words = 1 << wlog;                         // of a thread
     for (int i = 0; i < words; ++i) bitmap[tid * words + i] = 0;
     if (tid < br) {
-        const int64_t row = block * br + tid;
+        const int64_t row = attn_first_row(row0, block, br, m) + tid;
         int32_t lo = 0, hi = 0;
-        if (row < m) {
+        if (row < attn_first_row(row0, block + 1, br, m)) {
             lo = rowptr[row]; hi = rowptr[row + 1];
             if (windows > 1) { lo = first_at_least(crd, lo, hi, base); hi = first_at_least(crd, lo, hi, end); }
         }
@@ -153,7 +191,8 @@ __global__ __launch_bounds__(kThreads) void pad_kernel(const uint32_t *__restric
     if (n > 0 && x < end) cols[x] = cols[first + n - 1];
 }
 
-__global__ __launch_bounds__(kThreads) void state_kernel(const uint64_t *__restrict__ bits, const int32_t *__restrict__ chunk0, int64_t nblocks,
+__global__ __launch_bounds__(kThreads) void state_kernel(const uint64_t *__restrict__ bits, const int32_t *__restrict__ chunk0,
+                                                         const int32_t *__restrict__ row0, int64_t nblocks,
                                                          int64_t nchunks, int64_t m, int br, uint8_t *__restrict__ state)
 {
     const int64_t x = (int64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -165,11 +204,12 @@ __global__ __launch_bounds__(kThreads) void state_kernel(const uint64_t *__restr
         const int64_t mid = (lo + hi) >> 1;
         if (chunk0[mid] <= chunk) lo = mid; else hi = mid;
     }
+    const int64_t rows = attn_first_row(row0, lo + 1, br, m) - attn_first_row(row0, lo, br, m);
     uint64_t all = ~(uint64_t)0, any = 0;
     for (int r = 0; r < 32; ++r) {
         const uint64_t w = bits[chunk * br + sub * 32 + r];
         any |= w;
-        if (lo * br + sub * 32 + r < m) all &= w;        // rows behind the last one leave no trace
+        if (sub * 32 + r < rows) all &= w;               // rows behind the block's last one leave no trace
     }
     state[x] = any == 0 ? 0 : all == ~(uint64_t)0 ? 2 : 1;
 }
@@ -206,8 +246,8 @@ __global__ __launch_bounds__(1024) void cut_blocks_kernel(const int32_t *__restr
     if (threadIdx.x == 0) *count = (unsigned long long)before;
 }
 __global__ __launch_bounds__(kThreads) void stretches_kernel(const int32_t *__restrict__ item0, const int32_t *__restrict__ chunk0,
-                                                             const int32_t *__restrict__ rowptr, int64_t nblocks, int br, int per,
-                                                             attn_stretch *__restrict__ items)
+                                                             const int32_t *__restrict__ rowptr, const int32_t *__restrict__ row0, int64_t nblocks,
+                                                             int64_t m, int br, int per, attn_stretch *__restrict__ items)
 {
     const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (b >= nblocks) return;
@@ -219,7 +259,8 @@ __global__ __launch_bounds__(kThreads) void stretches_kernel(const int32_t *__re
         s.c1 = k1 - s.c0 < per ? k1 : s.c0 + per;
         s.first = br == 1 ? rowptr[b] : k0 * kAttnChunk;
         s.count = br == 1 ? rowptr[b + 1] - rowptr[b] : (k1 - k0) * kAttnChunk;
-        s.whole = i1 - i0 == 1; s.pad = 0;
+        s.row0 = (int32_t)attn_first_row(row0, b, br, m);
+        s.rows_whole = 2 * (int32_t)(attn_first_row(row0, b + 1, br, m) - s.row0) + (i1 - i0 == 1);
         items[x] = s;
     }
 }
@@ -238,7 +279,7 @@ struct plan_scope {
     }
     void drop() {
         if (!plan) return;
-        mem.put(plan->rowptr); mem.put(plan->crd_own); mem.put(plan->chunk0); mem.put(plan->cols); mem.put(plan->bits); mem.put(plan->state);
+        mem.put(plan->rowptr); mem.put(plan->row0); mem.put(plan->crd_own); mem.put(plan->chunk0); mem.put(plan->cols); mem.put(plan->bits); mem.put(plan->state);
         for (int l = 0; l < kAttnLevels; ++l) { mem.put(plan->item0[l]); mem.put(plan->item[l]); mem.put(plan->cut_block[l]); }
         delete plan;
         plan = nullptr;
@@ -248,10 +289,10 @@ struct plan_scope {
 
 struct cut { int windows = 1, wlog = 0; int64_t blocks = 0; };
 // at most 2^20 pairs of a block and a window where windows of up to 2^17 columns allow it
-cut cut_for(int64_t m, int64_t n, int br)
+cut cut_for(int64_t blocks, int64_t n)
 {
     cut c;
-    c.blocks = ceil_div(m, br);
+    c.blocks = blocks;
     while (c.wlog < 4 && c.blocks * ceil_div(n, (int64_t)kWindow << c.wlog) > ((int64_t)1 << 20)) ++c.wlog;
     c.windows = (int)(n > 0 ? ceil_div(n, (int64_t)kWindow << c.wlog) : 1);
     return c;
@@ -289,46 +330,74 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
         SP_HIP(hipGetLastError());
         p->crd = p->crd_own;
     }
-    // distinct columns of the blocks, for 128 rows and for 32
+    // Three ways to make blocks: of 128 rows, of 32, and of at most 128 within stretches of rows that have columns in common.  For
+    // each: the distinct columns of its blocks by window, their chunks.
+    struct way { int br; cut c; uint32_t *counts; int32_t *row0, *chunk0; unsigned long long chunks, most; } ways[3];
     unsigned long long *stats = (unsigned long long *)tmp.get(256);
-    if (!stats) return SP_ERR_ALLOC;
-    uint32_t *counts[2] = {nullptr, nullptr};
-    cut cuts[2] = {cut_for(m, n, 128), cut_for(m, n, 32)};
-    for (int k = 0; k < 2; ++k) {
-        const int64_t pairs = cuts[k].blocks * cuts[k].windows;
-        if (pairs >= ((int64_t)1 << 31) - 1) return SP_ERR_TOO_LARGE;
-        counts[k] = (uint32_t *)tmp.get((size_t)(pairs + 1) * 4);
-        if (!counts[k]) return SP_ERR_ALLOC;
-        hipLaunchKernelGGL(fill_kernel, dim3(1), dim3(kThreads), 0, st, counts[k] + pairs, (int64_t)1, 0u);
-        if (pairs > 0)
-            hipLaunchKernelGGL((window_kernel<false>), dim3((unsigned)pairs), dim3(kThreads), (size_t)(kThreads << cuts[k].wlog) * 4, st, p->rowptr,
-                               p->crd, m, k == 0 ? 128 : 32, cuts[k].windows, cuts[k].wlog, counts[k], nullptr, nullptr, nullptr);
+    int32_t *row0 = (int32_t *)tmp.get((size_t)(m + 1) * 4);
+    if (!stats || !row0) return SP_ERR_ALLOC;
+    SP_TRY(spmi_fill_zero(stats, 256, st));
+    unsigned long long within = 0;
+    if (m > 0) {
+        hipLaunchKernelGGL(blocks_kernel, dim3(1), dim3(1024), 0, st, p->rowptr, p->crd, m, 128, row0, stats + 8);
         SP_HIP(hipGetLastError());
-        SP_TRY(spmi_exclusive_scan(counts[k], pairs + 1, 32, tmp, st));
+        SP_HIP(hipMemcpyAsync(&within, stats + 8, 8, hipMemcpyDeviceToHost, st));
+        SP_HIP(hipStreamSynchronize(st));
     }
-    uint32_t distinct[2] = {0, 0};
-    for (int k = 0; k < 2; ++k)
-        SP_HIP(hipMemcpyAsync(&distinct[k], counts[k] + cuts[k].blocks * cuts[k].windows, 4, hipMemcpyDeviceToHost, st));
+    int tried = 2;
+    ways[0].br = 128; ways[0].row0 = nullptr;
+    ways[1].br = 32; ways[1].row0 = nullptr;
+    ways[2].br = 128; ways[2].row0 = row0;
+    if ((int64_t)within > ceil_div(m, 128)) tried = 3;
+    for (int k = 0; k < tried; ++k) {
+        way &w = ways[k];
+        w.c = cut_for(w.row0 ? (int64_t)within : ceil_div(m, w.br), n);
+        const int64_t pairs = w.c.blocks * w.c.windows;
+        if (pairs >= ((int64_t)1 << 31) - 1) return SP_ERR_TOO_LARGE;
+        w.counts = (uint32_t *)tmp.get((size_t)(pairs + 1) * 4);
+        w.chunk0 = (int32_t *)tmp.get((size_t)(w.c.blocks + 1) * 4);
+        if (!w.counts || !w.chunk0) return SP_ERR_ALLOC;
+        hipLaunchKernelGGL(fill_kernel, dim3(1), dim3(kThreads), 0, st, w.counts + pairs, (int64_t)1, 0u);
+        if (pairs > 0)
+            hipLaunchKernelGGL((window_kernel<false>), dim3((unsigned)pairs), dim3(kThreads), (size_t)(kThreads << w.c.wlog) * 4, st, p->rowptr,
+                               p->crd, w.row0, m, w.br, w.c.windows, w.c.wlog, w.counts, nullptr, nullptr, nullptr);
+        SP_HIP(hipGetLastError());
+        SP_TRY(spmi_exclusive_scan(w.counts, pairs + 1, 32, tmp, st));
+        hipLaunchKernelGGL(chunks_kernel, dim3(blocks_for(w.c.blocks + 1)), dim3(kThreads), 0, st, w.counts, w.c.windows, p->rowptr, w.c.blocks, w.chunk0,
+                           stats + 2 * k);
+        SP_HIP(hipGetLastError());
+    }
+    unsigned long long host[6] = {0};
+    SP_HIP(hipMemcpyAsync(host, stats, sizeof(host), hipMemcpyDeviceToHost, st));
     SP_HIP(hipStreamSynchronize(st));
-    // What a block of rows costs for each of its distinct columns: about 64 rows' worth of work to fetch it, and its rows' worth
-    // of work, used or not; a row by itself takes the work of 32 (it shares its tile with the heads of its group only).
-    const double cost128 = (double)distinct[0] * (64 + 128), cost32 = (double)distinct[1] * (64 + 32), cost1 = (double)entries * (64 + 32);
-    if (!transposed && cost1 <= cost32 && cost1 <= cost128) p->br = 1;
-    else p->br = cost32 < cost128 ? 32 : 128;
-    const int k = p->br == 128 ? 0 : 1;
-    const cut &c = cuts[k];
-    p->nblocks = p->br == 1 ? m : c.blocks;
+    for (int k = 0; k < tried; ++k) { ways[k].chunks = host[2 * k]; ways[k].most = host[2 * k + 1]; }
+    // What a block of rows costs for each of its chunks' columns: about 64 rows' worth of work to fetch it, and its rows' worth of work,
+    // used or not; a row by itself takes the work of 32 (it shares its tile with the heads of its group only).
+    const int wide = tried == 3 && ways[2].chunks * 10 <= ways[0].chunks * 11 ? 2 : 0;
+    const double cost128 = (double)ways[wide].chunks * 64 * (64 + 128), cost32 = (double)ways[1].chunks * 64 * (64 + 32), cost1 = (double)entries * (64 + 32);
+    const way *chosen = nullptr;                         // null: rows by themselves
+    if (transposed || cost1 > cost32 || cost1 > cost128) chosen = &ways[cost32 < cost128 ? 1 : wide];
+    p->br = chosen ? chosen->br : 1;
+    p->nblocks = chosen ? chosen->c.blocks : m;
     p->chunk0 = (int32_t *)scope.get((size_t)(p->nblocks + 1) * 4);
     if (!p->chunk0) return SP_ERR_ALLOC;
-    SP_TRY(spmi_fill_zero(stats, 256, st));
-    hipLaunchKernelGGL(chunks_kernel, dim3(blocks_for(p->nblocks + 1)), dim3(kThreads), 0, st, p->br == 1 ? nullptr : counts[k], c.windows, p->rowptr,
-                       p->nblocks, p->chunk0, stats);
-    SP_HIP(hipGetLastError());
+    if (chosen && chosen->row0) {
+        p->row0 = (int32_t *)scope.get((size_t)(p->nblocks + 1) * 4);
+        if (!p->row0) return SP_ERR_ALLOC;
+        SP_HIP(hipMemcpyAsync(p->row0, chosen->row0, (size_t)(p->nblocks + 1) * 4, hipMemcpyDeviceToDevice, st));
+    }
+    if (chosen) {
+        SP_HIP(hipMemcpyAsync(p->chunk0, chosen->chunk0, (size_t)(p->nblocks + 1) * 4, hipMemcpyDeviceToDevice, st));
+        p->nchunks = (int64_t)chosen->chunks; p->max_chunks = (int64_t)chosen->most;
+    } else {
+        SP_TRY(spmi_fill_zero(stats, 256, st));
+        hipLaunchKernelGGL(chunks_kernel, dim3(blocks_for(m + 1)), dim3(kThreads), 0, st, nullptr, 1, p->rowptr, m, p->chunk0, stats);
+        SP_HIP(hipGetLastError());
+        SP_HIP(hipMemcpyAsync(host, stats, 16, hipMemcpyDeviceToHost, st));
+        SP_HIP(hipStreamSynchronize(st));
+        p->nchunks = (int64_t)host[0]; p->max_chunks = (int64_t)host[1];
+    }
     SP_TRY(spmi_exclusive_scan(p->chunk0, p->nblocks + 1, 32, tmp, st));
-    unsigned long long host[2] = {0, 0};
-    SP_HIP(hipMemcpyAsync(host, stats, 16, hipMemcpyDeviceToHost, st));
-    SP_HIP(hipStreamSynchronize(st));
-    p->nchunks = (int64_t)host[0]; p->max_chunks = (int64_t)host[1];
     if (p->nchunks >= ((int64_t)1 << 25)) return SP_ERR_TOO_LARGE;       // 2^31 columns of blocks
     if (p->br > 1) {
         const size_t words = (size_t)p->nchunks * p->br;
@@ -338,11 +407,12 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
         if (!p->cols || !p->bits || !p->state) return SP_ERR_ALLOC;
         if (p->nchunks > 0) {
             SP_TRY(spmi_fill_zero(p->bits, words * 8, st));
+            const cut &c = chosen->c;
             hipLaunchKernelGGL((window_kernel<true>), dim3((unsigned)(c.blocks * c.windows)), dim3(kThreads), (size_t)(kThreads << c.wlog) * 8, st,
-                               p->rowptr, p->crd, m, p->br, c.windows, c.wlog, counts[k], p->chunk0, p->cols, (uint32_t *)p->bits);
-            hipLaunchKernelGGL(pad_kernel, dim3((unsigned)ceil_div(p->nblocks, kThreads / 64)), dim3(kThreads), 0, st, counts[k], c.windows, p->chunk0,
+                               p->rowptr, p->crd, p->row0, m, p->br, c.windows, c.wlog, chosen->counts, p->chunk0, p->cols, (uint32_t *)p->bits);
+            hipLaunchKernelGGL(pad_kernel, dim3((unsigned)ceil_div(p->nblocks, kThreads / 64)), dim3(kThreads), 0, st, chosen->counts, c.windows, p->chunk0,
                                p->nblocks, p->cols);
-            hipLaunchKernelGGL(state_kernel, dim3(blocks_for(p->nchunks * (p->br / 32))), dim3(kThreads), 0, st, p->bits, p->chunk0, p->nblocks,
+            hipLaunchKernelGGL(state_kernel, dim3(blocks_for(p->nchunks * (p->br / 32))), dim3(kThreads), 0, st, p->bits, p->chunk0, p->row0, p->nblocks,
                                p->nchunks, m, p->br, p->state);
             SP_HIP(hipGetLastError());
         }
@@ -375,8 +445,8 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
         p->cut_block[l] = (int32_t *)scope.get((size_t)(cut[l] > 0 ? cut[l] : 1) * 4);
         if (!p->item[l] || !p->cut_block[l]) return SP_ERR_ALLOC;
         if (cut[l]) hipLaunchKernelGGL(cut_blocks_kernel, dim3(1), dim3(1024), 0, st, p->item0[l], p->nblocks, p->cut_block[l], cuts_dev + l);
-        hipLaunchKernelGGL(stretches_kernel, dim3(blocks_for(p->nblocks)), dim3(kThreads), 0, st, p->item0[l], p->chunk0, p->rowptr, p->nblocks, p->br,
-                           attn_level_chunks(l), p->item[l]);
+        hipLaunchKernelGGL(stretches_kernel, dim3(blocks_for(p->nblocks)), dim3(kThreads), 0, st, p->item0[l], p->chunk0, p->rowptr, p->row0, p->nblocks,
+                           m, p->br, attn_level_chunks(l), p->item[l]);
         SP_HIP(hipGetLastError());
     }
     SP_HIP(hipStreamSynchronize(st));                    // temporaries go back, and another stream may use the plan from now on

@@ -159,6 +159,8 @@ struct attn_item {
     int chunk0, c0, c1;                  // the block's first chunk, the item's chunks
     int64_t part;                        // number among all items
     bool whole;                          // the block's only item
+    int64_t row0;                        // the block's first row
+    int rows;                            // and how many it has
     attn_columns cols;
     int64_t count;                       // places of the block's columns; br = 1: columns of the row
 
@@ -167,7 +169,8 @@ struct attn_item {
         const attn_stretch x = p.item[item];
         part = item;
         block = x.block; chunk0 = x.chunk0; c0 = x.c0; c1 = x.c1;
-        whole = x.whole != 0;
+        whole = x.rows_whole & 1;
+        row0 = x.row0; rows = x.rows_whole >> 1;
         count = x.count;
         cols = {(p.br == 1 ? p.crd : p.cols) + x.first, count - 1};
     }
@@ -324,7 +327,7 @@ struct attn_lane {
     int head, kv, r;                     // r: the row's place in its block
     int64_t row;
     bool valid;                          // a pair of a row and a head that exists (clamped to one that does)
-    __device__ __forceinline__ attn_lane(const attn_args &a, int br, int64_t block, int mode, int group, int lane, int wave, int waves)
+    __device__ __forceinline__ attn_lane(const attn_args &a, const attn_item &item, int mode, int group, int lane, int wave, int waves)
     {
         r = lane & 31;
         valid = true;
@@ -341,9 +344,8 @@ struct attn_lane {
             head = kv * a.G + x;
             if (mode == kHeadsTogether) r = 0;
         }
-        row = block * br + r;
-        valid = valid && row < a.m;
-        if (row >= a.m) row = a.m - 1;
+        valid = valid && r < item.rows;
+        row = item.row0 + (r < item.rows ? r : item.rows - 1);
     }
 };
 // the bias for the workgroup's heads, its slot for this lane
