@@ -6,8 +6,7 @@
 namespace {
 
 // A workgroup takes an item (a block of rows and a stretch of the columns that they store) and one head or a few that share K and V.
-// Per step KT columns' rows of K and V come through registers into LDS, gathered by the plan's list, while the step before is
-// computed; every wave makes the 32 x KW scores of its tile, masks them with the plan's bits, keeps each row's running maximum and sum
+// Per step KT columns' rows of K and V come into LDS, gathered by the plan's list, while the step before is computed; every wave makes the 32 x KW scores of its tile, masks them with the plan's bits, keeps each row's running maximum and sum
 // (f32), and adds the weighted rows of V to its 32 x D sums, which stay in registers.  Weights are rounded to the operands' type
 // for that product (half a step of 16-bit types, as every operand of the matrix cores is); the sum that divides takes them unrounded.
 //
@@ -29,15 +28,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     const attn_plan_view &p = f.p;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = WN > 1 ? wave : 0;
     const int ftid = WN > 1 ? lane : tid;
-    attn_lds *sK = (attn_lds *)lds + wn * FC * tile::kRow, *sV = sK + KT * tile::kRow;
-    attn_lds_i32 *s_kpos = (attn_lds_i32 *)((attn_lds *)lds + 2 * KT * tile::kRow) + wn * FC;    // POS: [FC]
-    auto meet = [] {
-        if (WN == 1) __syncthreads();
-        else {                                           // LDS is in order for a wave
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
-    };
+    attn_lds_i32 *s_kpos = (attn_lds_i32 *)((attn_lds *)lds + 4 * KT * tile::kRow) + wn * 2 * FC;    // POS: two places of [FC]
     const int64_t item_no = blockIdx.x / f.groups;
     const int group = blockIdx.x % f.groups;
     const attn_item item(p, item_no);
@@ -55,7 +46,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
     if (POS) {
         if (a.qpos) { qp = a.qpos[row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
-        if (a.buckets) bias = attn_lane_bias<T>(a, (attn_lds *)lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
+        if (a.buckets) bias = attn_lane_bias<T>(a, (attn_lds *)lds + 4 * KT * tile::kRow + 2 * KT * 4, f.mode, group, lane, wave, WM);
     }
 
     attn_f32x16 acc[tile::kBlocks];
@@ -64,19 +55,21 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     float top = -INFINITY, total = 0;
 
     const int64_t steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
-    if (POS && WN > 1) __syncthreads();                  // the bias's tables
-    attn_feed<T, DT, FT, FC, POS> feed;
-    feed.ldx = a.ldk; feed.ldy = a.ldv;
-    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk + wn * FC; feed.step = KT; feed.tid = ftid;
-    feed.pos = a.kpos; feed.sign = a.causal; feed.limit = q_hi;
-    feed.D = a.D; feed.vec = f.vec; feed.row = ftid / tile::kGranules; feed.g = ftid % tile::kGranules;
+    attn_ring<T, DT, FT, FC, POS> ring;
+    ring.lds = (attn_lds *)lds + wn * 4 * FC * tile::kRow;
+    ring.ldx = a.ldk; ring.ldy = a.ldv;
+    ring.cols = item.cols; ring.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk + wn * FC; ring.step = KT; ring.tid = ftid;
+    ring.pos = a.kpos; ring.sign = POS ? a.causal : 0; ring.limit = q_hi;
+    ring.D = a.D; ring.vec = f.vec;
     const T *Kh = (const T *)a.K + (int64_t)kv * a.hdk, *Vh = (const T *)a.V + (int64_t)kv * a.hdv;
+    if (a.D != DT || ring.sign) ring.zero();
     if (POS && a.causal && WM > 1) {                     // the last position that any row of the block attends to
         if (lane == 0) s_kpos[wave] = q_hi;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WM; ++w) feed.limit = s_kpos[w] > feed.limit ? s_kpos[w] : feed.limit;
+        for (int w = 0; w < WM; ++w) ring.limit = s_kpos[w] > ring.limit ? s_kpos[w] : ring.limit;
     }
+    if (POS || a.D != DT) __syncthreads();               // the bias's tables, the zeros
     // this wave's share of a step: columns col0 .. col0 + KW of the step's chunks
     auto my_chunk = [&](int64_t step, int &col0) {
         col0 = (int)(step % SUB) * KT + wn * KW;
@@ -93,23 +86,25 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
         if (chunk >= 0) { state_next = item.state(p, chunk, r); word_next = item.word(p, chunk, r); }
     };
     if (steps > 0) {
-        feed.columns(0);
-        feed.advance();
-        if (steps > 1) feed.columns(1);
+        ring.begin(steps);
         fetch_pairs(0);
-        feed.rows(Kh, Vh);
+        ring.rows(0, Kh, Vh);
     }
     for (int64_t step = 0; step < steps; ++step) {
-        meet();                                          // the step before has been computed
-        feed.put(sK, sV);
-        if (POS && ftid < FC) s_kpos[ftid] = feed.arrived;
-        meet();
+        ring.arrive();
+        if (POS && ftid < FC) s_kpos[(step & 1) * FC + ftid] = ring.kp_one;
+        if (WN == 1) __syncthreads();                    // the step's rows are there, the step before has been computed
+        else {                                           // a wave's own rows; LDS is in order for a wave
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
         word = word_next; state = state_next;
+        const attn_lds *sK = ring.x_of(step), *sV = ring.y_of(step);
         if (step + 1 < steps) {
-            feed.advance();
-            if (step + 2 < steps) feed.columns(step + 2);
+            ring.advance();
+            if (step + ring.kAhead < steps) ring.columns(step + ring.kAhead);
             fetch_pairs(step + 1);
-            feed.rows(Kh, Vh);
+            ring.rows(step + 1, Kh, Vh);
         }
         int col0;
         if (my_chunk(step, col0) < 0) continue;
@@ -122,7 +117,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
         float up = top;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
-            const attn_lds_i32 *kp = s_kpos + 32 * t;
+            const attn_lds_i32 *kp = s_kpos + (step & 1) * FC + 32 * t;
             attn_near near = {false, false, false, 0};
             if (POS) {
                 const int col = kp[lane & 31];
@@ -339,7 +334,7 @@ template <typename T, int DT, int WM, int WN, int KW, bool POS>
 sp_status launch(const forward_args &f, const forward_choice &c, int64_t items, hipStream_t st)
 {
     constexpr int KT = KW * WN;
-    size_t lds = 2 * (size_t)KT * DT * sizeof(T) + (POS ? KT * 4 + attn_bias_bytes(f.a, c.slots()) : 0);
+    size_t lds = 4 * (size_t)KT * DT * sizeof(T) + (POS ? 2 * KT * 4 + attn_bias_bytes(f.a, c.slots()) : 0);
     const size_t join = WN > 1 ? (size_t)WN * 32 * (DT + 3) * 4 : 0;
     if (join > lds) lds = join;
     auto kernel = forward_kernel<T, DT, WM, WN, KW, POS>;
@@ -352,7 +347,7 @@ sp_status launch(const forward_args &f, const forward_choice &c, int64_t items, 
 template <typename T, int DT, bool POS>
 sp_status launch_mode(const forward_args &f, const forward_choice &c, int64_t items, hipStream_t st)
 {
-    if (c.wn > 1) return launch<T, DT, 1, 4, 32, POS>(f, c, items, st);
+    if (c.wn > 1) return launch<T, DT, 1, (DT * (int)sizeof(T) <= 256 ? 4 : 2), 32, POS>(f, c, items, st);   // two places for each wave have to fit the LDS
     return launch<T, DT, 4, 1, (DT * (int)sizeof(T) <= 256 ? 64 : 32), POS>(f, c, items, st);
 }
 

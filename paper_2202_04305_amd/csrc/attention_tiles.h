@@ -250,6 +250,104 @@ struct attn_feed {
     }
 };
 
+// The same straight from memory into LDS (global_load_lds): no registers hold rows on their way, and a step's rows arrive while the step
+// before is computed from the other of two places.  A wave's instruction fills 64 consecutive granules of LDS, so the granules' exchange
+// (attn_tile::place) is made by which granule of memory each lane asks for.  Rows that nobody attends to and numbers past D are
+// left out; the place was zeroed once.  Inline assembly, because for the compiler's own form of this load every later read of LDS waits
+// for it; it has no destination register, and arrive() waits for it before anybody reads.
+__device__ __forceinline__ void attn_to_lds(const void *from, unsigned to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
+}
+template <typename T, int DT, int NT, int KT, bool POS>
+struct attn_ring {
+    typedef attn_tile<T, DT> tile;
+    typedef typename tile::frag frag;
+    static constexpr int kPieces = KT * tile::kGranules / NT, kRowStep = NT / tile::kGranules, kBytes = KT * tile::kRow;
+    static_assert(KT * tile::kGranules % NT == 0 && NT % tile::kGranules == 0 && KT <= NT, "every thread fetches the same number of granules");
+    attn_lds *lds;                       // two places of X and Y each
+    int64_t ldx, ldy;                    // numbers from row to row
+    attn_columns cols;
+    int64_t x0;                          // the item's first column among its block's
+    const int32_t *pos;                  // positions of the columns, or null
+    int limit, sign;                     // causal: rows are needed where sign * pos <= sign * limit; sign 0: everywhere
+    int D, step, tid;                    // step: columns from one step to the next; tid: among the NT threads that fetch together
+    bool vec;
+    int32_t next[kPieces], one_next;     // columns on their way
+    int32_t soon[kPieces], one_soon;     // POS: columns that are there, whose positions are on their way
+    int32_t at[kPieces], one;            // columns of the rows to be fetched next
+    int32_t kp_soon[kPieces], kp_one_soon, kp[kPieces], kp_one;
+
+    __device__ __forceinline__ attn_lds *x_of(int64_t s) const { return lds + (s & 1) * (2 * kBytes); }
+    __device__ __forceinline__ attn_lds *y_of(int64_t s) const { return x_of(s) + kBytes; }
+    __device__ __forceinline__ int row(int k) const { return tid / tile::kGranules + k * kRowStep; }
+    __device__ __forceinline__ void zero()
+    {
+        for (int x = tid; x < 4 * kBytes / 16; x += NT) *(__attribute__((address_space(3))) attn_f32x4 *)(lds + x * 16) = (attn_f32x4)(0.f);
+    }
+    __device__ __forceinline__ void columns(int64_t s)
+    {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) next[k] = cols.get(x0 + s * step + row(k));
+        if (POS) one_next = cols.get(x0 + s * step + (tid < KT ? tid : 0));
+    }
+    // moves the columns up a place: next -> soon (POS: their positions are asked for) -> at
+    __device__ __forceinline__ void advance()
+    {
+        if constexpr (POS) {
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) { at[k] = soon[k]; kp[k] = kp_soon[k]; soon[k] = next[k]; }
+            one = one_soon; kp_one = kp_one_soon; one_soon = one_next;
+            if (pos) {
+                kp_one_soon = pos[one_soon];
+                if (sign != 0) {
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k) kp_soon[k] = pos[soon[k]];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) at[k] = next[k];
+        }
+    }
+    __device__ __forceinline__ void begin(int64_t steps)
+    {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) soon[k] = kp_soon[k] = 0;
+        one_soon = kp_one_soon = 0;
+        columns(0);
+        advance();
+        if (POS) {
+            if (steps > 1) columns(1);
+            advance();
+            if (steps > 2) columns(2);
+        } else if (steps > 1) columns(1);
+    }
+    static constexpr int kAhead = POS ? 3 : 2;           // columns(s + kAhead) is asked for when the rows of s + 1 are
+    __device__ __forceinline__ void rows(int64_t s, const T *X, const T *Y)
+    {
+        const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)x_of(s) + (unsigned)tid / 64 * 1024);
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            const int g = (tid % tile::kGranules) ^ tile::swizzle(row(k));
+            const bool need = !POS || sign == 0 || (sign > 0 ? kp[k] <= limit : kp[k] >= limit);
+            const T *x = X + ((int64_t)at[k] * ldx + g * tile::kPer), *y = Y + ((int64_t)at[k] * ldy + g * tile::kPer);
+            if (vec) {
+                if (need && g * tile::kPer < D) {
+                    attn_to_lds(x, to + k * (NT * 16));
+                    attn_to_lds(y, to + k * (NT * 16) + kBytes);
+                }
+            } else if (need) {
+                attn_lds *place = x_of(s) + (k * NT + tid) * 16;
+                *(__attribute__((address_space(3))) frag *)place = tile::granule(x - g * tile::kPer, g * tile::kPer, D, false, true);
+                *(__attribute__((address_space(3))) frag *)(place + kBytes) = tile::granule(y - g * tile::kPer, g * tile::kPer, D, false, true);
+            }
+        }
+    }
+    // this thread's rows have arrived (the others': after a barrier)
+    static __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+};
+
 // Positions of a tile's 32 columns against those of the wave's rows.  A tile that lies wholly past the last border on one side has one
 // bias for each head.
 struct attn_near {
