@@ -111,10 +111,15 @@ __device__ __forceinline__ int attn_bucket(const attn_args &a, int r)
     return base + b;
 }
 
-// The bucket of all distances from the last border on, ahead of the query or behind it.
-__device__ __forceinline__ int attn_far_bucket(const attn_args &a, bool ahead)
+// Kernels number the buckets without the one that no distance has: of two directions, distance 0 on the upper half.  (That leaves two
+// workgroups on a compute unit for the gradient of 32 buckets, head size 64.)
+__host__ __device__ __forceinline__ int attn_places(const attn_args &a) { return a.buckets - a.bidirectional; }
+__device__ __forceinline__ int attn_place_of(const attn_args &a, int bucket) { return bucket - (a.bidirectional && bucket > a.side ? 1 : 0); }
+__device__ __forceinline__ int attn_bucket_of(const attn_args &a, int place) { return place + (a.bidirectional && place >= a.side ? 1 : 0); }
+// The place of all distances from the last border on, ahead of the query or behind it.
+__device__ __forceinline__ int attn_far_place(const attn_args &a, bool ahead)
 {
-    return ahead ? (a.bidirectional ? 2 * a.side - 1 : 0) : a.side - 1;
+    return ahead ? (a.bidirectional ? 2 * a.side - 2 : 0) : a.side - 1;
 }
 
 // Block b's first row and the one behind its last.

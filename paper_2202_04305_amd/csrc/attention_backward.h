@@ -82,15 +82,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     const attn_plan_view &p = f.p;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = WN > 1 ? wave : 0;
     const int ftid = WN > 1 ? lane : tid;
-    attn_lds *sK = (attn_lds *)lds + wn * FC * tile::kRow, *sV = sK + KT * tile::kRow;
-    attn_lds_i32 *s_kpos = (attn_lds_i32 *)((attn_lds *)lds + 2 * KT * tile::kRow) + wn * FC;
-    auto meet = [] {
-        if (WN == 1) __syncthreads();
-        else {
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
-    };
+    attn_lds_i32 *s_kpos = (attn_lds_i32 *)((attn_lds *)lds + 4 * KT * tile::kRow) + wn * 2 * FC;
     const int64_t item_no = blockIdx.x / f.groups;
     const int group = blockIdx.x % f.groups;
     const attn_item item(p, item_no);
@@ -109,14 +101,14 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     int qp = 0, q_lo = 0, q_hi = 0;
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
     attn_lds_f32 *hist = nullptr;                             // [buckets][64] of ds; exact: of p dP and p
-    const int hist_size = a.buckets * 64 * (f.exact ? 2 : 1);
+    const int places = attn_places(a), hist_size = places * 64 * (f.exact ? 2 : 1);
     float far_x[2] = {0, 0}, far_p[2] = {0, 0};          // the far buckets behind and ahead
     if (POS) {
         if (a.qpos) { qp = a.qpos[me.row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
         if (a.buckets) {
-            bias = attn_lane_bias<T>(a, (attn_lds *)lds + 2 * KT * tile::kRow + KT * 4, f.mode, group, lane, wave, WM);
+            bias = attn_lane_bias<T>(a, (attn_lds *)lds + 4 * KT * tile::kRow + 2 * KT * 4, f.mode, group, lane, wave, WM);
             if (f.part_table) {
-                hist = bias.table + ((a.buckets * bias.slots + 3) & ~3) + wave * hist_size;
+                hist = bias.table + ((places * bias.slots + 3) & ~3) + wave * hist_size;
                 for (int b = lane; b < hist_size; b += 64) hist[b] = 0;
             }
         }
@@ -126,19 +118,21 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     for (int x = 0; x < tile::kBlocks; ++x) acc[x] = (attn_f32x16)(0.f);
 
     const int64_t steps = (int64_t)(item.c1 - item.c0 + STEP - 1) / STEP * SUB;
-    if (POS && WN > 1) __syncthreads();
-    attn_feed<T, DT, FT, FC, POS> feed;
-    feed.ldx = a.ldk; feed.ldy = a.ldv;
-    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk + wn * FC; feed.step = KT; feed.tid = ftid;
-    feed.pos = a.kpos; feed.sign = a.causal; feed.limit = q_hi;
-    feed.D = a.D; feed.vec = f.vec; feed.row = ftid / tile::kGranules; feed.g = ftid % tile::kGranules;
+    attn_ring<T, DT, FT, FC, POS> ring;
+    ring.lds = (attn_lds *)lds + wn * 4 * FC * tile::kRow;
+    ring.ldx = a.ldk; ring.ldy = a.ldv;
+    ring.cols = item.cols; ring.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk + wn * FC; ring.step = KT; ring.tid = ftid;
+    ring.pos = a.kpos; ring.sign = POS ? a.causal : 0; ring.limit = q_hi;
+    ring.D = a.D; ring.vec = f.vec;
     const T *Kh = (const T *)a.K + (int64_t)me.kv * a.hdk, *Vh = (const T *)a.V + (int64_t)me.kv * a.hdv;
+    if (a.D != DT || ring.sign) ring.zero();
     if (POS && a.causal && WM > 1) {
         if (lane == 0) s_kpos[wave] = q_hi;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WM; ++w) feed.limit = s_kpos[w] > feed.limit ? s_kpos[w] : feed.limit;
+        for (int w = 0; w < WM; ++w) ring.limit = s_kpos[w] > ring.limit ? s_kpos[w] : ring.limit;
     }
+    if (POS || a.D != DT) __syncthreads();
     auto my_chunk = [&](int64_t step, int &col0) {
         col0 = (int)(step % SUB) * KT + wn * KW;
         const int chunk = item.c0 + (int)(step / SUB) * STEP + col0 / kAttnChunk;
@@ -153,23 +147,25 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         if (chunk >= 0) { state_next = item.state(p, chunk, r); word_next = item.word(p, chunk, r); }
     };
     if (steps > 0) {
-        feed.columns(0);
-        feed.advance();
-        if (steps > 1) feed.columns(1);
+        ring.begin(steps, [](int64_t s) { return s; });
         fetch_pairs(0);
-        feed.rows(Kh, Vh);
+        ring.rows(0, Kh, Vh);
     }
     for (int64_t step = 0; step < steps; ++step) {
-        meet();
-        feed.put(sK, sV);
-        if (POS && ftid < FC) s_kpos[ftid] = feed.arrived;
-        meet();
+        ring.arrive();
+        if (POS && ftid < FC) s_kpos[(step & 1) * FC + ftid] = ring.kp_one;
+        if (WN == 1) __syncthreads();
+        else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
         word = word_next; state = state_next;
+        const attn_lds *sK = ring.x_of(step), *sV = ring.y_of(step);
         if (step + 1 < steps) {
-            feed.advance();
-            if (step + 2 < steps) feed.columns(step + 2);
+            ring.advance();
+            if (step + ring.kAhead < steps) ring.columns(step + ring.kAhead);
             fetch_pairs(step + 1);
-            feed.rows(Kh, Vh);
+            ring.rows(step + 1, Kh, Vh);
         }
         int col0;
         if (my_chunk(step, col0) < 0) continue;
@@ -178,7 +174,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         word >>= col0 % kAttnChunk;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
-            const attn_lds_i32 *kp = s_kpos + 32 * t;
+            const attn_lds_i32 *kp = s_kpos + (step & 1) * FC + 32 * t;
             attn_near near = {false, false, false, 0};
             if (POS) {
                 const int col = kp[lane & 31];
@@ -200,7 +196,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                 // infinity has weight 0, whatever dP is.
                 const bool one = !a.buckets || near.far;
                 uint32_t there = 0;
-                int bucket[16];
+                int place[16];
 #pragma unroll
                 for (int x = 0; x < 16; ++x) there |= (bits >> (8 * (x >> 2) + (x & 3)) & 1) << x;
                 if (near.ask) {
@@ -208,14 +204,14 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                     for (int x = 0; x < 16; ++x) there &= ~((uint32_t)(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)] > qp) << x);
                 }
                 if (one) {
-                    const float all_of = a.buckets ? bias.at(near.bucket) : 0.f;
+                    const float all_of = a.buckets ? bias.at(near.place) : 0.f;
 #pragma unroll
                     for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, all_of);
                 } else {
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) bucket[x] = bias.bucket(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp);
+                    for (int x = 0; x < 16; ++x) place[x] = bias.place(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp);
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(bucket[x]));
+                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(place[x]));
                 }
                 float sum_x = 0, sum_p = 0;
                 attn_f32x16 weight;
@@ -230,11 +226,11 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                     weight[x] = w;
                 }
                 if (hist && !one) {
-                    if (f.exact) attn_add_by_bucket<2>(hist, lane, bucket, dp, weight);
-                    else attn_add_by_bucket<1>(hist, lane, bucket, dp, weight);
+                    if (f.exact) attn_add_by_bucket<2>(hist, lane, place, dp, weight);
+                    else attn_add_by_bucket<1>(hist, lane, place, dp, weight);
                 }
                 if (hist && one) {
-                    const bool behind = near.bucket == a.side - 1;
+                    const bool behind = near.place == a.side - 1;
                     far_x[0] += behind ? sum_x : 0.f; far_p[0] += behind ? sum_p : 0.f;
                     far_x[1] += behind ? 0.f : sum_x; far_p[1] += behind ? 0.f : sum_p;
                 }
@@ -253,20 +249,20 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         __syncthreads();                                 // all waves are done with K
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
-            const int b = attn_far_bucket(a, side == 1);
+            const int b = attn_far_place(a, side == 1);
             if (f.exact) {
                 hist[(b * 64 + lane) * 2] += far_x[side];
                 hist[(b * 64 + lane) * 2 + 1] += far_p[side];
             } else hist[b * 64 + lane] += far_x[side];
         }
         __syncthreads();
-        const attn_lds_f32 *all = bias.table + ((a.buckets * bias.slots + 3) & ~3);
+        const attn_lds_f32 *all = bias.table + ((places * bias.slots + 3) & ~3);
         attn_lds_f32 *s_delta = (attn_lds_f32 *)(attn_lds *)lds;     // over K: [waves][32], each row's D
         // rows are a wave's own, or (WN) shared by all waves
         if (f.exact && lane < 32 && (WN == 1 || wave == 0)) {
             float d = 0;
             for (int w = wave; w < (WN == 1 ? wave + 1 : WN); ++w)
-                for (int b = 0; b < a.buckets; ++b) d += all[w * hist_size + (b * 64 + lane) * 2] + all[w * hist_size + (b * 64 + 32 + lane) * 2];
+                for (int b = 0; b < places; ++b) d += all[w * hist_size + (b * 64 + lane) * 2] + all[w * hist_size + (b * 64 + 32 + lane) * 2];
             s_delta[wave * 32 + lane] = d;
         }
         __syncthreads();
@@ -275,13 +271,13 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
             const attn_lds_f32 *x = all + w * hist_size + (b * 64 + lane) * (f.exact ? 2 : 1);
             return f.exact ? x[0] - s_delta[(WN == 1 ? w : 0) * 32 + (lane & 31)] * x[1] : x[0];
         };
-        for (int b = wave; b < a.buckets; b += WM * WN) {
+        for (int b = wave; b < places; b += WM * WN) {
             float sum = 0;
             if (f.mode == kHeadsOfRows) {
                 for (int w = 0; w < WM; ++w) {
                     const int y = group / a.Hk * WM + w;
                     sum = attn_wave_sum(term(w, b));
-                    if (lane == 0 && y < a.G) out[(group % a.Hk * a.G + y) * a.buckets + b] = sum;
+                    if (lane == 0 && y < a.G) out[(group % a.Hk * a.G + y) * a.buckets + attn_bucket_of(a, b)] = sum;
                 }
                 continue;
             }
@@ -289,10 +285,10 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
             if (f.mode == kHeadsTogether) {
                 const int y = group / a.Hk * 32 + lane;
                 sum = attn_pair_sum(sum);
-                if (lane < 32 && y < a.G) out[(group % a.Hk * a.G + y) * a.buckets + b] = sum;
+                if (lane < 32 && y < a.G) out[(group % a.Hk * a.G + y) * a.buckets + attn_bucket_of(a, b)] = sum;
             } else {
                 sum = attn_wave_sum(sum);
-                if (lane == 0) out[(group % a.Hk * a.G + group / a.Hk) * a.buckets + b] = sum;
+                if (lane == 0) out[(group % a.Hk * a.G + group / a.Hk) * a.buckets + attn_bucket_of(a, b)] = sum;
             }
         }
         __syncthreads();
@@ -381,9 +377,9 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     constexpr int NT = 64 * WM, KT = KW, TILES = KW / 32, SUB = kAttnChunk / KT;
     static_assert(KT <= kAttnChunk, "steps within a chunk");
     extern __shared__ __align__(16) char lds[];
-    attn_lds *sQ = (attn_lds *)lds, *sO = sQ + KT * tile::kRow;
-    attn_lds_f32 *s_lse = (attn_lds_f32 *)(sQ + 2 * KT * tile::kRow), *s_delta = s_lse + KT;
-    attn_lds_i32 *s_qpos = (attn_lds_i32 *)(s_delta + KT);
+    // behind Q and dO, two places of everything: lse, D and positions of a step's queries, the bias of a head
+    attn_lds_f32 *s_lse = (attn_lds_f32 *)((attn_lds *)lds + 4 * KT * tile::kRow), *s_delta = s_lse + 2 * KT;
+    attn_lds_i32 *s_qpos = (attn_lds_i32 *)(s_delta + 2 * KT);
     const attn_args &a = f.a;
     const attn_plan_view &p = f.p;                       // of the transposed pattern: rows are keys
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -400,12 +396,14 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     tile::load_lane((const T *)a.V + key * a.ldv + kv * a.hdv, a.D, f.vec, some, 1.f, vx, lane);
     int kp = 0, k_lo = 0, k_hi = 0;
     attn_bias bias = {nullptr, nullptr, 0, 1, 0};
-    attn_lds_f32 *table = nullptr;
     if (POS) {
         if (a.kpos) { kp = a.kpos[key]; k_lo = attn_wave_min(kp); k_hi = attn_wave_max(kp); }
         if (a.buckets) {
-            bias = attn_make_bias<T>(a, (attn_lds *)(s_qpos + KT), 1, [&](int) { return kv * a.G; });
-            table = bias.table;
+            // a slot for even heads and one for odd ones: the head at hand and the next
+            bias = attn_make_bias<T>(a, (attn_lds *)(s_qpos + 2 * KT), 2, [&](int s) {
+                const int x = (s ^ kv * a.G) & 1;
+                return x < a.G ? kv * a.G + x : -1;
+            });
         }
     }
     attn_f32x16 dk[tile::kBlocks], dv[tile::kBlocks];
@@ -413,17 +411,20 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     for (int x = 0; x < tile::kBlocks; ++x) dk[x] = dv[x] = (attn_f32x16)(0.f);
 
     const int64_t per_head = (int64_t)(item.c1 - item.c0) * SUB, steps = per_head * a.G;
-    attn_feed<T, DT, NT, KT, POS> feed;
-    feed.ldx = a.ldq; feed.ldy = f.g.lddo;
-    feed.cols = item.cols; feed.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk; feed.step = KT; feed.tid = tid;
-    feed.pos = a.qpos; feed.sign = -a.causal; feed.limit = k_lo;
-    feed.D = a.D; feed.vec = f.vec; feed.row = tid / tile::kGranules; feed.g = tid % tile::kGranules;
+    attn_ring<T, DT, NT, KT, POS, true> ring;
+    ring.lds = (attn_lds *)lds;
+    ring.ldx = a.ldq; ring.ldy = f.g.lddo;
+    ring.cols = item.cols; ring.x0 = (int64_t)(item.c0 - item.chunk0) * kAttnChunk; ring.step = KT; ring.tid = tid;
+    ring.pos = a.qpos; ring.sign = POS ? -a.causal : 0; ring.limit = k_lo;
+    ring.D = a.D; ring.vec = f.vec;
+    if (a.D != DT || ring.sign) ring.zero();
     if (POS && a.causal && WM > 1) {
         if (lane == 0) s_qpos[wave] = k_lo;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WM; ++w) feed.limit = s_qpos[w] < feed.limit ? s_qpos[w] : feed.limit;
+        for (int w = 0; w < WM; ++w) ring.limit = s_qpos[w] < ring.limit ? s_qpos[w] : ring.limit;
     }
+    if (POS || a.D != DT) __syncthreads();
     float lse_next = 0, delta_next = 0;
     uint64_t word = 0, word_next = 0;
     int state = 0, state_next = 0;
@@ -437,37 +438,43 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
             word_next = item.word(p, chunk, r);
         }
         if (tid < KT) {
-            lse_next = f.g.lse[x.h * a.m + feed.one];
-            delta_next = f.delta[x.h * a.m + feed.one];
+            lse_next = f.g.lse[x.h * a.m + ring.one];
+            delta_next = f.delta[x.h * a.m + ring.one];
         }
-        feed.rows((const T *)a.Q + x.h * a.hdq, (const T *)f.g.dO + x.h * f.g.hddo);
     };
-    place now = {kv * a.G, 0}, soon = after(now), later = after(soon);
+    auto rows = [&](int64_t s, place x) { ring.rows(s, (const T *)a.Q + x.h * a.hdq, (const T *)f.g.dO + x.h * f.g.hddo); };
+    place now = {kv * a.G, 0}, soon = after(now), ahead = after(soon);
+    if (ring.kAhead == 3) ahead = after(ahead);          // the step whose columns are asked for
     if (steps > 0) {
-        feed.columns(0);
-        feed.advance();
-        if (steps > 1) feed.columns(soon.at);
+        place x[3] = {now, soon, after(soon)};
+        ring.begin(steps, [&](int64_t s) { return x[s].at; });
         fetch(now);
+        rows(0, now);
     }
     for (int64_t step = 0; step < steps; ++step) {
-        __syncthreads();
-        feed.put(sQ, sO);
+        ring.arrive();
+        const int here = (int)(step & 1) * KT;
         if (tid < KT) {
-            s_lse[tid] = lse_next == -INFINITY ? INFINITY : POS ? lse_next : lse_next * kLog2e;     // no weight left
-            s_delta[tid] = delta_next;
-            if (POS) s_qpos[tid] = feed.arrived;
+            s_lse[here + tid] = lse_next == -INFINITY ? INFINITY : POS ? lse_next : lse_next * kLog2e;     // no weight left
+            s_delta[here + tid] = delta_next;
+            if (POS) s_qpos[here + tid] = ring.kp_one;
         }
-        if (POS && a.buckets && now.at == 0)
-            for (int b = tid; b < a.buckets; b += NT) table[b] = (float)((const T *)a.table)[(int64_t)b * a.ldt + now.h];
+        if (POS && a.buckets && now.at == 0) {           // the slot of the head before the last is free
+            bias.slot = now.h & 1;
+            if (a.G > 2)
+                for (int b = tid; b < attn_places(a); b += NT) bias.table[2 * b + bias.slot] = (float)((const T *)a.table)[(int64_t)attn_bucket_of(a, b) * a.ldt + now.h];
+        }
         __syncthreads();
         word = word_next; state = state_next;
+        const attn_lds *sQ = ring.x_of(step), *sO = ring.y_of(step);
         if (step + 1 < steps) {
-            feed.advance();
-            if (step + 2 < steps) feed.columns(later.at);
+            ring.advance();
+            if (step + ring.kAhead < steps) ring.columns(ahead.at);
             fetch(soon);
+            rows(step + 1, soon);
         }
         const int col0 = (int)(now.at % SUB) * KT;
-        now = soon; soon = later; later = after(later);
+        now = soon; soon = after(soon); ahead = after(ahead);
         if (!busy) continue;
         state = __builtin_amdgcn_readfirstlane(state);
         if (state == 0) continue;
@@ -476,7 +483,7 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
         for (int t = 0; t < TILES; ++t) {
             attn_near near = {false, false, false, 0};
             if (POS) {
-                const int qp = s_qpos[32 * t + (lane & 31)];
+                const int qp = s_qpos[here + 32 * t + (lane & 31)];
                 near = attn_look(a, attn_distance(k_lo, qp), attn_distance(k_hi, qp));
                 if (near.nothing) continue;
             }
@@ -488,23 +495,23 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
                 if (near.ask) {
 #pragma unroll
                     for (int x = 0; x < 16; ++x)
-                        there &= ~((uint32_t)(kp > s_qpos[32 * t + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]) << (8 * (x >> 2) + (x & 3)));
+                        there &= ~((uint32_t)(kp > s_qpos[here + 32 * t + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]) << (8 * (x >> 2) + (x & 3)));
                 }
                 if (!a.buckets || near.far) {
-                    const float all_of = a.buckets ? bias.at(near.bucket) : 0.f;
+                    const float all_of = a.buckets ? bias.at(near.place) : 0.f;
 #pragma unroll
                     for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, all_of);
                 } else {
-                    int bucket[16];
+                    int place[16];
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) bucket[x] = bias.bucket(kp, s_qpos[32 * t + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]);
+                    for (int x = 0; x < 16; ++x) place[x] = bias.place(kp, s_qpos[here + 32 * t + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]);
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(bucket[x]));
+                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(place[x]));
                 }
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-                const int q0 = 32 * t + 8 * b + 4 * (lane >> 5);
+                const int q0 = here + 32 * t + 8 * b + 4 * (lane >> 5);
                 const attn_f32x4 lse = *(const attn_lds_f32x4 *)(s_lse + q0), delta = *(const attn_lds_f32x4 *)(s_delta + q0);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -604,13 +611,15 @@ __global__ __launch_bounds__(kThreads) void table_kernel(grad_args f, int64_t it
     sum = attn_wave_sum(sum);
     if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) ((T *)f.g.dTable)[(int64_t)b * f.g.lddt + h] = (T)(s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]);
+    const bool none = a.bidirectional && b == a.side;    // no distance is in that bucket, and nothing was written for it
+    if (threadIdx.x == 0) ((T *)f.g.dTable)[(int64_t)b * f.g.lddt + h] = (T)(none ? 0.f : s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]);
 }
 
 template <typename K>
 sp_status launch(K kernel, const grad_args &f, int64_t groups, int threads, size_t lds, hipStream_t st)
 {
     if (groups >= ((int64_t)1 << 31)) return SP_ERR_TOO_LARGE;
+    if (lds > (size_t)kAttnLds) return SP_ERR_UNSUPPORTED;
     if (lds > 65536) SP_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), lds, st, f);
     SP_HIP(hipGetLastError());
@@ -629,13 +638,13 @@ sp_status launch_dq_mode(const grad_args &f, const attn_mapping &c, int64_t item
 {
     constexpr int kRow = DT * (int)sizeof(T);
     if (c.wn > 1) return launch_dq<T, DT, 1, attn_dq_waves(kRow, POS), 32, POS>(f, c, items, st);
-    return launch_dq<T, DT, 4, 1, attn_dq_columns(kRow), POS>(f, c, items, st);
+    return launch_dq<T, DT, 4, 1, attn_dq_columns(kRow, POS), POS>(f, c, items, st);
 }
 template <typename T, int DT, bool POS>
 sp_status launch_dkv_mode(const grad_args &f, int br, int64_t items, hipStream_t st)
 {
-    constexpr int KW = DT * (int)sizeof(T) == 64 ? 64 : 32;
-    const size_t lds = 2 * (size_t)KW * DT * sizeof(T) + KW * 12 + (POS ? attn_bias_bytes(f.a, 1) : 0);
+    constexpr int KW = sizeof(T) == 2 && DT <= 128 ? 64 : 32;
+    const size_t lds = 4 * (size_t)KW * DT * sizeof(T) + KW * 24 + (POS ? attn_bias_bytes(f.a, 2) : 0);
     if (br == 128) return launch(dkv_kernel<T, DT, 4, KW, POS>, f, items * f.a.Hk, 256, lds, st);
     return launch(dkv_kernel<T, DT, 1, KW, POS>, f, items * f.a.Hk, 64, lds, st);
 }

@@ -86,7 +86,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
         if (chunk >= 0) { state_next = item.state(p, chunk, r); word_next = item.word(p, chunk, r); }
     };
     if (steps > 0) {
-        ring.begin(steps);
+        ring.begin(steps, [](int64_t s) { return s; });
         fetch_pairs(0);
         ring.rows(0, Kh, Vh);
     }
@@ -132,9 +132,9 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
                 if (a.buckets && !near.far) {
 #pragma unroll
                     for (int x = 0; x < 16; ++x)
-                        s[t][x] = __builtin_fmaf(s[t][x], a.scale, bias.at(bias.bucket(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp)));
+                        s[t][x] = __builtin_fmaf(s[t][x], a.scale, bias.at(bias.place(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp)));
                 } else {
-                    const float all_of = a.buckets ? bias.at(near.bucket) : 0.f;
+                    const float all_of = a.buckets ? bias.at(near.place) : 0.f;
 #pragma unroll
                     for (int x = 0; x < 16; ++x) s[t][x] = __builtin_fmaf(s[t][x], a.scale, all_of);
                 }

@@ -188,70 +188,9 @@ struct attn_item {
     }
 };
 
-// The rows of two operands (K and V; Q and dO) on their way into LDS: step s of KT columns is fetched into registers while step s - 1 is
-// computed, and its columns' places a step earlier still.  CAUSAL rows whose position no row of the block attends to are not read
-// but set to zero, so that what lies in a cache's free slots does not matter.
-template <typename T, int DT, int NT, int KT, bool POS>
-struct attn_feed {
-    typedef attn_tile<T, DT> tile;
-    typedef typename tile::frag frag;
-    static constexpr int kPieces = KT * tile::kGranules / NT, kRowStep = NT / tile::kGranules;
-    static_assert(KT * tile::kGranules % NT == 0 && NT % tile::kGranules == 0 && KT <= NT, "every thread fetches the same number of granules");
-    const T *X, *Y;
-    int64_t ldx, ldy;
-    attn_columns cols;
-    int64_t x0;                          // the item's first column among its block's
-    const int32_t *pos;                  // positions of the columns, or null
-    int limit, sign;                     // causal: rows are needed where sign * pos <= sign * limit; sign 0: everywhere
-    int D, row, g, step, tid;            // step: columns from one step to the next; tid: among the NT threads that fetch together
-    bool vec;
-    int32_t at[kPieces], next[kPieces], one, one_next;       // columns of the step fetched next, and of the one after it
-    int32_t kp[kPieces], kp_one;
-    frag x[kPieces], y[kPieces];
-    int32_t arrived;                     // thread tid < KT: the position of column tid of the step in x, y
-
-    __device__ __forceinline__ void columns(int64_t s)
-    {
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) next[k] = cols.get(x0 + s * step + row + k * kRowStep);
-        one_next = cols.get(x0 + s * step + (tid < KT ? tid : 0));
-    }
-    // the columns asked for last become those of the next rows(); their positions are on the way
-    __device__ __forceinline__ void advance()
-    {
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) at[k] = next[k];
-        one = one_next;
-        if (POS && pos) {
-            kp_one = pos[one];
-            if (sign != 0) {
-#pragma unroll
-                for (int k = 0; k < kPieces; ++k) kp[k] = pos[at[k]];
-            }
-        }
-    }
-    __device__ __forceinline__ void rows(const T *X, const T *Y)
-    {
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-            const bool need = !POS || sign == 0 || (sign > 0 ? kp[k] <= limit : kp[k] >= limit);
-            x[k] = tile::granule(X + (int64_t)at[k] * ldx, g * tile::kPer, D, vec, need);
-            y[k] = tile::granule(Y + (int64_t)at[k] * ldy, g * tile::kPer, D, vec, need);
-        }
-        arrived = kp_one;
-    }
-    __device__ __forceinline__ void put(attn_lds *tx, attn_lds *ty)
-    {
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-            tile::put(tx, row + k * kRowStep, g, x[k]);
-            tile::put(ty, row + k * kRowStep, g, y[k]);
-        }
-    }
-};
-
-// The same straight from memory into LDS (global_load_lds): no registers hold rows on their way, and a step's rows arrive while the step
-// before is computed from the other of two places.  A wave's instruction fills 64 consecutive granules of LDS, so the granules' exchange
+// The rows of two operands (K and V; Q and dO) on their way from memory into LDS (global_load_lds): no registers hold them, and a step's
+// rows arrive while the step before is computed from the other of two places.  (Through registers, 16 sequences of up to 1024 queries over
+// 4096 keys, 16 heads of 128: 600 us instead of 419.)  A wave's instruction fills 64 consecutive granules of LDS, so the granules' exchange
 // (attn_tile::place) is made by which granule of memory each lane asks for.  Rows that nobody attends to and numbers past D are
 // left out; the place was zeroed once.  Inline assembly, because for the compiler's own form of this load every later read of LDS waits
 // for it; it has no destination register, and arrive() waits for it before anybody reads.
@@ -259,7 +198,9 @@ __device__ __forceinline__ void attn_to_lds(const void *from, unsigned to)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
 }
-template <typename T, int DT, int NT, int KT, bool POS>
+// CAUSAL rows that nobody attends to are not read either, so that what lies in a cache's free places does not matter.  ONE: keep each
+// step's columns, one a thread (for positions, and what else belongs to a column).
+template <typename T, int DT, int NT, int KT, bool POS, bool ONE = POS>
 struct attn_ring {
     typedef attn_tile<T, DT> tile;
     typedef typename tile::frag frag;
@@ -289,7 +230,7 @@ struct attn_ring {
     {
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) next[k] = cols.get(x0 + s * step + row(k));
-        if (POS) one_next = cols.get(x0 + s * step + (tid < KT ? tid : 0));
+        if (ONE) one_next = cols.get(x0 + s * step + (tid < KT ? tid : 0));
     }
     // moves the columns up a place: next -> soon (POS: their positions are asked for) -> at
     __device__ __forceinline__ void advance()
@@ -308,20 +249,23 @@ struct attn_ring {
         } else {
 #pragma unroll
             for (int k = 0; k < kPieces; ++k) at[k] = next[k];
+            if (ONE) one = one_next;
         }
     }
-    __device__ __forceinline__ void begin(int64_t steps)
+    // step_at(s): the place of step s among the columns' steps
+    template <typename F>
+    __device__ __forceinline__ void begin(int64_t steps, F step_at)
     {
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) soon[k] = kp_soon[k] = 0;
         one_soon = kp_one_soon = 0;
-        columns(0);
+        columns(step_at(0));
         advance();
         if (POS) {
-            if (steps > 1) columns(1);
+            if (steps > 1) columns(step_at(1));
             advance();
-            if (steps > 2) columns(2);
-        } else if (steps > 1) columns(1);
+            if (steps > 2) columns(step_at(2));
+        } else if (steps > 1) columns(step_at(1));
     }
     static constexpr int kAhead = POS ? 3 : 2;           // columns(s + kAhead) is asked for when the rows of s + 1 are
     __device__ __forceinline__ void rows(int64_t s, const T *X, const T *Y)
@@ -352,7 +296,7 @@ struct attn_ring {
 // bias for each head.
 struct attn_near {
     bool nothing, ask, far;              // causal leaves nothing / something out; all distances share a bucket
-    int bucket;                          // that bucket
+    int place;                           // its place
 };
 // col: this lane's column's position (lane % 32).  lo, hi: the least and largest distance that the wave's rows give it; a: borders
 __device__ __forceinline__ attn_near attn_look(const attn_args &a, int lo, int hi)
@@ -365,7 +309,7 @@ __device__ __forceinline__ attn_near attn_look(const attn_args &a, int lo, int h
     if (a.buckets) {
         const bool ahead = __builtin_amdgcn_ballot_w64(lo < a.last) == 0, behind = __builtin_amdgcn_ballot_w64(hi > -a.last) == 0;
         n.far = ahead || behind;
-        n.bucket = attn_far_bucket(a, ahead);
+        n.place = attn_far_place(a, ahead);
     }
     return n;
 }
@@ -384,20 +328,20 @@ __device__ __forceinline__ int attn_wave_max(int v)
 
 // The position bias in LDS: the bucket of every distance up to the last border, and the table's columns of the heads at hand.
 struct attn_bias {
-    const attn_lds_u8 *lut;              // [2 last + 1]
-    attn_lds_f32 *table;                 // [buckets][slots]
+    const attn_lds_u8 *lut;              // [2 last + 1]: the places of the distances' buckets
+    attn_lds_f32 *table;                 // [places][slots]
     int last, slots, slot;
-    __device__ __forceinline__ int bucket(int kp, int qp) const
+    __device__ __forceinline__ int place(int kp, int qp) const
     {
         int r = attn_distance(kp, qp);
         r = r < -last ? -last : r > last ? last : r;
         return lut[r + last];
     }
-    __device__ __forceinline__ float at(int bucket) const { return table[bucket * slots + slot]; }
+    __device__ __forceinline__ float at(int place) const { return table[place * slots + slot]; }
 };
 static inline size_t attn_bias_bytes(const attn_args &a, int slots)
 {
-    return a.buckets ? (size_t)((2 * a.last + 1 + 15) & ~15) + (size_t)((a.buckets * slots * 4 + 15) & ~15) : 0;
+    return a.buckets ? (size_t)((2 * a.last + 1 + 15) & ~15) + (size_t)((attn_places(a) * slots * 4 + 15) & ~15) : 0;
 }
 // by the whole workgroup; the caller synchronises.  head(slot): the head of a slot, or -1
 template <typename T, typename HEAD>
@@ -405,10 +349,10 @@ __device__ __forceinline__ attn_bias attn_make_bias(const attn_args &a, attn_lds
 {
     attn_lds_u8 *lut = (attn_lds_u8 *)lds;
     attn_lds_f32 *table = (attn_lds_f32 *)(lds + ((2 * a.last + 1 + 15) & ~15));
-    for (int x = threadIdx.x; x <= 2 * a.last; x += blockDim.x) lut[x] = (uint8_t)attn_bucket(a, x - a.last);
-    for (int x = threadIdx.x; x < a.buckets * slots; x += blockDim.x) {
+    for (int x = threadIdx.x; x <= 2 * a.last; x += blockDim.x) lut[x] = (uint8_t)attn_place_of(a, attn_bucket(a, x - a.last));
+    for (int x = threadIdx.x; x < attn_places(a) * slots; x += blockDim.x) {
         const int h = head(x % slots);
-        table[x] = h < 0 ? 0.f : (float)((const T *)a.table)[(int64_t)(x / slots) * a.ldt + h];
+        table[x] = h < 0 ? 0.f : (float)((const T *)a.table)[(int64_t)attn_bucket_of(a, x / slots) * a.ldt + h];
     }
     return {lut, table, a.last, slots, 0};
 }
@@ -513,13 +457,16 @@ __device__ __forceinline__ void attn_store4(T *row, int d, int D, bool vec, attn
 
 // dq_kernel: how many waves share a tile's columns, and the LDS it takes.  K and V of a step and the bias's sums have to fit together.
 constexpr int kAttnLds = 160 * 1024;
-static constexpr int attn_dq_waves(int row_bytes, bool pos) { return row_bytes == 512 && pos ? 2 : 4; }
-static constexpr int attn_dq_columns(int row_bytes) { return row_bytes == 64 ? 64 : 32; }
+static constexpr int attn_dq_waves(int row_bytes, bool pos) { return row_bytes == 512 ? (pos ? 1 : 2) : row_bytes == 256 && pos ? 2 : 4; }
+// Columns of a step for four tiles.  64 take long enough to compute for the next ones to arrive; with the bias's sums in LDS, 32 leave
+// room for a second workgroup.
+static constexpr int attn_dq_columns(int row_bytes, bool pos) { return row_bytes <= (pos ? 64 : 256) ? 64 : 32; }
 static inline size_t attn_dq_lds(const attn_args &a, const attn_mapping &c, int row_bytes, bool pos, bool table, bool exact)
 {
     const bool share = c.wn > 1;
-    const int waves = share ? attn_dq_waves(row_bytes, pos) : 4, KT = share ? 32 * waves : attn_dq_columns(row_bytes);
-    const size_t lds = 2 * (size_t)KT * row_bytes + (pos ? KT * 4 + attn_bias_bytes(a, c.slots()) : 0) + (table ? (size_t)waves * a.buckets * (exact ? 512 : 256) : 0);
+    const int waves = share ? attn_dq_waves(row_bytes, pos) : 4, KT = share ? 32 * waves : attn_dq_columns(row_bytes, pos);
+    const size_t lds = 4 * (size_t)KT * row_bytes + (pos ? 2 * KT * 4 + attn_bias_bytes(a, c.slots()) : 0) +
+                       (table ? (size_t)waves * attn_places(a) * (exact ? 512 : 256) : 0);
     return lds;
 }
 
