@@ -33,6 +33,9 @@ __global__ __launch_bounds__(kThreads) void delta_kernel(grad_args f, float *__r
     if (l == 0 && x < a.m * a.H) delta[h * a.m + i] = s;
 }
 
+// v where bit k of `bits` is set, otherwise 0, whatever v is.
+__device__ __forceinline__ float attn_where(uint32_t bits, int k, float v) { return __uint_as_float(__float_as_uint(v) & (uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1)); }
+
 // Adds a lane's 16 pairs to its sums by bucket: hist[(bucket * 64 + lane) * N ...].  Four pairs are read, added and written back at a
 // time; where some of the four share a bucket, the later one goes on from the earlier one's sum, and the last write stays.
 template <int N>
@@ -76,7 +79,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     typedef typename tile::frag frag;
     constexpr int NT = 64 * WM * WN, KT = KW * WN, TILES = KW / 32;
     constexpr int STEP = KT > kAttnChunk ? KT / kAttnChunk : 1, SUB = KT < kAttnChunk ? kAttnChunk / KT : 1;
-    extern __shared__ __align__(16) char lds[];
+    extern __shared__ __align__(1024) char lds[];
     constexpr int FT = WN > 1 ? 64 : NT, FC = WN > 1 ? KW : KT;
     const attn_args &a = f.a;
     const attn_plan_view &p = f.p;
@@ -187,9 +190,10 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
             const uint32_t bits = (me.valid ? (uint32_t)(word >> (32 * t)) : 0u) >> (4 * (lane >> 5));
             if (!POS) {
 #pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    const bool there = bits >> (8 * (x >> 2) + (x & 3)) & 1;
-                    s[x] = there ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], cc, -off)) * (dp[x] - delta) : 0.f;
+                for (int x = 0; x < 16; ++x) s[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], cc, -off)) * (dp[x] - delta);
+                if (state != 2) {                        // a lane of no row keeps its own nonsense to itself
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[x] = attn_where(bits, 8 * (x >> 2) + (x & 3), s[x]);
                 }
             } else {
                 // Loops of one kind of work each, without branches inside, so that the LDS's answers overlap.  A score of minus
@@ -376,7 +380,7 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     typedef typename tile::frag frag;
     constexpr int NT = 64 * WM, KT = KW, TILES = KW / 32, SUB = kAttnChunk / KT;
     static_assert(KT <= kAttnChunk, "steps within a chunk");
-    extern __shared__ __align__(16) char lds[];
+    extern __shared__ __align__(1024) char lds[];
     // behind Q and dO, two places of everything: lse, D and positions of a step's queries, the bias of a head
     attn_lds_f32 *s_lse = (attn_lds_f32 *)((attn_lds *)lds + 4 * KT * tile::kRow), *s_delta = s_lse + 2 * KT;
     attn_lds_i32 *s_qpos = (attn_lds_i32 *)(s_delta + 2 * KT);
@@ -509,6 +513,10 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
                     for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(place[x]));
                 }
             }
+            if (POS) {                                   // a score of minus infinity has weight 0, whatever dP is
+#pragma unroll
+                for (int x = 0; x < 16; ++x) there = s[x] == -INFINITY ? there & ~(1u << (8 * (x >> 2) + (x & 3))) : there;
+            }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int q0 = here + 32 * t + 8 * b + 4 * (lane >> 5);
@@ -516,10 +524,15 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const int x = 4 * b + c;
-                    const bool on = (there >> (8 * b + c) & 1) && (!POS || s[x] != -INFINITY);     // a score of minus infinity has weight 0
-                    const float w = on ? __builtin_amdgcn_exp2f(POS ? (s[x] - lse[c]) * cc : __builtin_fmaf(s[x], cc, -lse[c])) : 0.f;
-                    s[x] = w;
-                    dp[x] = on ? w * (dp[x] - delta[c]) : 0.f;
+                    s[x] = __builtin_amdgcn_exp2f(POS ? (s[x] - lse[c]) * cc : __builtin_fmaf(s[x], cc, -lse[c]));
+                    dp[x] = s[x] * (dp[x] - delta[c]);
+                }
+            }
+            if (POS || state != 2) {                     // a lane of no key keeps its own nonsense to itself
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    s[x] = attn_where(there, 8 * (x >> 2) + (x & 3), s[x]);
+                    dp[x] = attn_where(there, 8 * (x >> 2) + (x & 3), dp[x]);
                 }
             }
             tile::add_rows(dv, sO, 32 * t, s, lane);

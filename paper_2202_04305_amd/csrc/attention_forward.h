@@ -21,7 +21,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     constexpr int NT = 64 * WM * WN, KT = KW * WN, TILES = KW / 32;
     constexpr int STEP = KT > kAttnChunk ? KT / kAttnChunk : 1;         // chunks of a step (or one chunk in 64 / KT steps)
     constexpr int SUB = KT < kAttnChunk ? kAttnChunk / KT : 1;
-    extern __shared__ __align__(16) char lds[];
+    extern __shared__ __align__(1024) char lds[];
     // WM waves fetch a step together and meet at barriers; WN waves fetch a share of it each, into a place of their own, and do not meet
     constexpr int FT = WN > 1 ? 64 : NT, FC = WN > 1 ? KW : KT;
     const attn_args &a = f.a;

@@ -60,17 +60,18 @@ struct attn_tile {
     }
     static __device__ __forceinline__ int place(int r, int g) { return r * kRow + ((g ^ swizzle(r)) << 4); }
 
-    // 32 rows from row0 (a multiple of 32) on as the first operand, step s
-    static __device__ __forceinline__ frag rows(const attn_lds *t, int row0, int s, int lane)
-    {
-        return *(const __attribute__((address_space(3))) frag *)(t + row0 * kRow + place(lane & 31, 2 * s + (lane >> 5)));
-    }
-    // acc (32 rows x 32 lanes) = the tile's rows row0 ... times the lanes' rows `b`
+    // Addresses are one number of a lane, exchanged by a constant for every read (a step, a block of numbers), plus a constant: the
+    // exchange only touches bits within a row, and tiles begin at multiples of a row.
+    template <typename V>
+    static __device__ __forceinline__ V read(unsigned at) { return *(const __attribute__((address_space(3))) V *)(uintptr_t)at; }
+
+    // acc (32 rows x 32 lanes) = the tile's rows row0 ... (a multiple of 32) times the lanes' rows `b`
     static __device__ __forceinline__ attn_f32x16 scores(const attn_lds *t, int row0, const frag (&b)[kSteps], int lane)
     {
+        const unsigned base = (unsigned)(uintptr_t)t + (unsigned)place(lane & 31, lane >> 5);
         attn_f32x16 acc = (attn_f32x16)(0.f);
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) acc = attn_mma<T>::mul(rows(t, row0, s, lane), b[s], acc);
+        for (int s = 0; s < kSteps; ++s) acc = attn_mma<T>::mul(read<frag>((base ^ (unsigned)(s << 5)) + row0 * kRow), b[s], acc);
         return acc;
     }
     // acc[x] (numbers 32 x ... of a head, 32 lanes) += sum over the tile's 32 rows from row0 on of row[number] * w[row of the lane]
@@ -78,17 +79,16 @@ struct attn_tile {
     {
         const int half = lane >> 5;
         if constexpr (sizeof(T) == 4) {
-            const int l = lane & 31;
+            const unsigned base = (unsigned)(uintptr_t)t + (unsigned)(place(4 * half, (lane & 31) >> 2) + (lane & 3) * 4);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int row = 8 * (r >> 2) + 4 * half + (r & 3);
+                const int row = 8 * (r >> 2) + (r & 3);  // and 4 for the upper half
 #pragma unroll
-                for (int x = 0; x < kBlocks; ++x) {
-                    const float v = *(const __attribute__((address_space(3))) float *)(t + row0 * kRow + place(row, x * 8 + (l >> 2)) + (l & 3) * 4);
-                    acc[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w[r], acc[x], 0, 0, 0);
-                }
+                for (int x = 0; x < kBlocks; ++x)
+                    acc[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(read<float>((base ^ (unsigned)((x * 8 ^ swizzle(row)) << 4)) + (row0 + row) * kRow), w[r], acc[x], 0, 0, 0);
             }
         } else {
+            const unsigned base = (unsigned)(uintptr_t)t + (unsigned)(place(4 * half + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 frag p;
@@ -98,11 +98,9 @@ struct attn_tile {
                 for (int x = 0; x < kBlocks; ++x) {
                     union { attn_s16x4 q[2]; frag f; } v;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int row = 16 * u + 8 * k + 4 * half + ((lane & 15) >> 2);
-                        const int at = place(row, x * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8;
-                        v.q[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) attn_s16x4 *)(t + row0 * kRow + at));
-                    }
+                    for (int k = 0; k < 2; ++k)          // rows 16 u + 8 k on, whose swizzle is that of the first ones exchanged by 2 k
+                        v.q[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) attn_s16x4 *)(uintptr_t)(
+                            (base ^ (unsigned)((4 * x ^ 2 * k) << 4)) + (row0 + 16 * u + 8 * k) * kRow));
                     acc[x] = attn_mma<T>::mul(v.f, p, acc[x]);
                 }
             }
