@@ -36,31 +36,38 @@ __global__ __launch_bounds__(kThreads) void delta_kernel(grad_args f, float *__r
 // v where bit k of `bits` is set, otherwise 0, whatever v is.
 __device__ __forceinline__ float attn_where(uint32_t bits, int k, float v) { return __uint_as_float(__float_as_uint(v) & (uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1)); }
 
-// Adds a lane's 16 pairs to its sums by bucket: hist[(bucket * 64 + lane) * N ...].  Four pairs are read, added and written back at a
-// time; where some of the four share a bucket, the later one goes on from the earlier one's sum, and the last write stays.
+// Adds a lane's 16 pairs to its sums by bucket: hist[(bucket * 64 + lane) * N ...].  Two pairs are read, added and written back at a
+// time; where they share a bucket, the second one goes on from the first one's sum, and the last write stays.  (Four at a time save half
+// of the waiting and cost three times the comparing.)
 template <int N>
-__device__ __forceinline__ void attn_add_by_bucket(attn_lds_f32 *hist, int lane, const int (&bucket)[16], const attn_f32x16 &x, const attn_f32x16 &y)
+__device__ __forceinline__ void attn_add_by_bucket(attn_lds_f32 *hist, int lane, const int (&bucket)[16], const float (&x)[16], const float (&y)[16])
 {
-    typedef float sums __attribute__((ext_vector_type(N)));
+    typedef float sums __attribute__((ext_vector_type(2)));
     typedef __attribute__((address_space(3))) sums lds_sums;
 #pragma unroll
-    for (int g = 0; g < 16; g += 4) {
-        lds_sums *at[4];
-        sums v[4];
+    for (int g = 0; g < 16; g += 2) {
+        attn_lds_f32 *at[2];
+        float u[2], v[2] = {0, 0};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            at[c] = (lds_sums *)hist + bucket[g + c] * 64 + lane;
-            v[c] = *at[c];
+        for (int c = 0; c < 2; ++c) {
+            at[c] = hist + (bucket[g + c] * 64 + lane) * N;
+            if (N == 2) {
+                const sums r = *(lds_sums *)at[c];
+                u[c] = r.x; v[c] = r.y;
+            } else u[c] = *at[c];
         }
+        const bool same = bucket[g] == bucket[g + 1];
+        u[0] += x[g]; v[0] += y[g];
+        u[1] = (same ? u[0] : u[1]) + x[g + 1];
+        v[1] = (same ? v[0] : v[1]) + y[g + 1];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-#pragma unroll
-            for (int e = 0; e < c; ++e) v[c] = bucket[g + c] == bucket[g + e] ? v[e] : v[c];
-            v[c][0] += x[g + c];
-            if (N == 2) v[c][N - 1] += y[g + c];
+        for (int c = 0; c < 2; ++c) {
+            if (N == 2) {
+                sums r;
+                r.x = u[c]; r.y = v[c];
+                *(lds_sums *)at[c] = r;
+            } else *at[c] = u[c];
         }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) *at[c] = v[c];
     }
 }
 
@@ -102,16 +109,17 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     if (!POS) off *= kLog2e;
     const float delta = f.delta[me.head * a.m + me.row];
     int qp = 0, q_lo = 0, q_hi = 0;
-    attn_bias bias = {nullptr, nullptr, 0, 1, 0};
+    attn_bias bias = {};
     attn_lds_f32 *hist = nullptr;                             // [buckets][64] of ds; exact: of p dP and p
     const int places = attn_places(a), hist_size = places * 64 * (f.exact ? 2 : 1);
     float far_x[2] = {0, 0}, far_p[2] = {0, 0};          // the far buckets behind and ahead
+    const float of_term = f.exact ? 0.f : delta;
     if (POS) {
         if (a.qpos) { qp = a.qpos[me.row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
         if (a.buckets) {
             bias = attn_lane_bias<T>(a, (attn_lds *)lds + 4 * KT * tile::kRow + 2 * KT * 4, f.mode, group, lane, wave, WM);
             if (f.part_table) {
-                hist = bias.table + ((places * bias.slots + 3) & ~3) + wave * hist_size;
+                hist = bias.table + (((places << bias.shift) + 3) & ~3) + wave * hist_size;
                 for (int b = lane; b < hist_size; b += 64) hist[b] = 0;
             }
         }
@@ -200,9 +208,8 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                 // infinity has weight 0, whatever dP is.
                 const bool one = !a.buckets || near.far;
                 uint32_t there = 0;
-                int place[16];
 #pragma unroll
-                for (int x = 0; x < 16; ++x) there |= (bits >> (8 * (x >> 2) + (x & 3)) & 1) << x;
+                for (int b = 0; b < 4; ++b) there |= (bits >> 8 * b & 15) << 4 * b;
                 if (near.ask) {
 #pragma unroll
                     for (int x = 0; x < 16; ++x) there &= ~((uint32_t)(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)] > qp) << x);
@@ -211,27 +218,26 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                     const float all_of = a.buckets ? bias.at(near.place) : 0.f;
 #pragma unroll
                     for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, all_of);
-                } else {
+                } else
+                    attn_add_bias(bias, s, a.scale, [&](int x) { return kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]; }, [&](int) { return qp; });
+                if (attn_any_lowest(s)) {
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) place[x] = bias.place(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp);
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(place[x]));
+                    for (int x = 0; x < 16; ++x) there &= ~((uint32_t)(s[x] == -INFINITY) << x);
                 }
-                float sum_x = 0, sum_p = 0;
-                attn_f32x16 weight;
+                float sum_x = 0, sum_p = 0, term[16], weight[16];
 #pragma unroll
                 for (int x = 0; x < 16; ++x) {
-                    const bool on = (there >> x & 1) && s[x] != -INFINITY;
-                    const float w = on ? __builtin_amdgcn_exp2f((s[x] - off) * cc) : 0.f;
-                    const float term = on ? w * dp[x] : 0.f;
-                    s[x] = on ? w * (dp[x] - delta) : 0.f;
-                    dp[x] = f.exact ? term : s[x];
-                    if (one) { sum_x += dp[x]; sum_p += w; }
-                    weight[x] = w;
+                    weight[x] = attn_where(there, x, __builtin_amdgcn_exp2f((s[x] - off) * cc));
+                    s[x] = attn_where(there, x, weight[x] * (dp[x] - delta));
+                    term[x] = attn_where(there, x, weight[x] * (dp[x] - of_term));
+                    sum_x += term[x]; sum_p += weight[x];
                 }
                 if (hist && !one) {
-                    if (f.exact) attn_add_by_bucket<2>(hist, lane, place, dp, weight);
-                    else attn_add_by_bucket<1>(hist, lane, place, dp, weight);
+                    int place[16];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) place[x] = bias.lut[bias.index(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp)];
+                    if (f.exact) attn_add_by_bucket<2>(hist, lane, place, term, weight);
+                    else attn_add_by_bucket<1>(hist, lane, place, term, weight);
                 }
                 if (hist && one) {
                     const bool behind = near.place == a.side - 1;
@@ -260,7 +266,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
             } else hist[b * 64 + lane] += far_x[side];
         }
         __syncthreads();
-        const attn_lds_f32 *all = bias.table + ((places * bias.slots + 3) & ~3);
+        const attn_lds_f32 *all = bias.table + (((places << bias.shift) + 3) & ~3);
         attn_lds_f32 *s_delta = (attn_lds_f32 *)(attn_lds *)lds;     // over K: [waves][32], each row's D
         // rows are a wave's own, or (WN) shared by all waves
         if (f.exact && lane < 32 && (WN == 1 || wave == 0)) {
@@ -399,12 +405,12 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
     tile::load_lane((const T *)a.K + key * a.ldk + kv * a.hdk, a.D, f.vec, some, POS ? 1.f : a.c, kx, lane);
     tile::load_lane((const T *)a.V + key * a.ldv + kv * a.hdv, a.D, f.vec, some, 1.f, vx, lane);
     int kp = 0, k_lo = 0, k_hi = 0;
-    attn_bias bias = {nullptr, nullptr, 0, 1, 0};
+    attn_bias bias = {};
     if (POS) {
         if (a.kpos) { kp = a.kpos[key]; k_lo = attn_wave_min(kp); k_hi = attn_wave_max(kp); }
         if (a.buckets) {
             // a slot for even heads and one for odd ones: the head at hand and the next
-            bias = attn_make_bias<T>(a, (attn_lds *)(s_qpos + 2 * KT), 2, [&](int s) {
+            bias = attn_make_bias<T>(a, (attn_lds *)(s_qpos + 2 * KT), 1, [&](int s) {
                 const int x = (s ^ kv * a.G) & 1;
                 return x < a.G ? kv * a.G + x : -1;
             });
@@ -465,8 +471,12 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
         }
         if (POS && a.buckets && now.at == 0) {           // the slot of the head before the last is free
             bias.slot = now.h & 1;
-            if (a.G > 2)
-                for (int b = tid; b < attn_places(a); b += NT) bias.table[2 * b + bias.slot] = (float)((const T *)a.table)[(int64_t)attn_bucket_of(a, b) * a.ldt + now.h];
+            if (a.G > 2) {
+                auto entry = [&](int bucket) { return (float)((const T *)a.table)[(int64_t)bucket * a.ldt + now.h]; };
+                for (int b = tid; b < attn_places(a); b += NT) bias.table[2 * b + bias.slot] = entry(attn_bucket_of(a, b));
+                if (bias.value)
+                    for (int b = tid; b <= 2 * a.last; b += NT) bias.value[2 * b + bias.slot] = entry(attn_bucket(a, b - a.last));
+            }
         }
         __syncthreads();
         word = word_next; state = state_next;
@@ -506,16 +516,12 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
 #pragma unroll
                     for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, all_of);
                 } else {
-                    int place[16];
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) place[x] = bias.place(kp, s_qpos[here + 32 * t + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]);
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, bias.at(place[x]));
+                    attn_add_bias(bias, s, a.scale, [&](int) { return kp; }, [&](int x) { return s_qpos[here + 32 * t + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]; });
                 }
             }
-            if (POS) {                                   // a score of minus infinity has weight 0, whatever dP is
+            if (POS && attn_any_lowest(s)) {             // a score of minus infinity has weight 0, whatever dP is
 #pragma unroll
-                for (int x = 0; x < 16; ++x) there = s[x] == -INFINITY ? there & ~(1u << (8 * (x >> 2) + (x & 3))) : there;
+                for (int x = 0; x < 16; ++x) there &= ~((uint32_t)(s[x] == -INFINITY) << (8 * (x >> 2) + (x & 3)));
             }
 #pragma unroll
             for (int b = 0; b < 4; ++b) {

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
     frag q[tile::kSteps];
     tile::load_lane((const T *)a.Q + row * a.ldq + head * a.hdq, a.D, f.vec, valid && item.c1 > item.c0, POS ? 1.f : a.c, q, lane);
     int qp = 0, q_lo = 0, q_hi = 0;
-    attn_bias bias = {nullptr, nullptr, 0, 1, 0};
+    attn_bias bias = {};
     if (POS) {
         if (a.qpos) { qp = a.qpos[row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
         if (a.buckets) bias = attn_lane_bias<T>(a, (attn_lds *)lds + 4 * KT * tile::kRow + 2 * KT * 4, f.mode, group, lane, wave, WM);
@@ -130,9 +130,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kerne
             s[t] = tile::scores(sK, 32 * t, q, lane);
             if (POS) {
                 if (a.buckets && !near.far) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x)
-                        s[t][x] = __builtin_fmaf(s[t][x], a.scale, bias.at(bias.place(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp)));
+                    attn_add_bias(bias, s[t], a.scale, [&](int x) { return kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]; }, [&](int) { return qp; });
                 } else {
                     const float all_of = a.buckets ? bias.at(near.place) : 0.f;
 #pragma unroll

@@ -324,35 +324,77 @@ __device__ __forceinline__ int attn_wave_max(int v)
     return v;
 }
 
-// The position bias in LDS: the bucket of every distance up to the last border, and the table's columns of the heads at hand.
+// The position bias in LDS: the place of every distance's bucket up to the last border, the table's columns of the heads at hand (a slot
+// each, 1 << shift of them), and, where that is small, the bias of every distance.
 struct attn_bias {
-    const attn_lds_u8 *lut;              // [2 last + 1]: the places of the distances' buckets
+    const attn_lds_u8 *lut;              // [2 last + 1]
     attn_lds_f32 *table;                 // [places][slots]
-    int last, slots, slot;
-    __device__ __forceinline__ int place(int kp, int qp) const
+    attn_lds_f32 *value;                 // [2 last + 1][slots], or null
+    int last, shift, slot;
+    __device__ __forceinline__ int index(int kp, int qp) const
     {
-        int r = attn_distance(kp, qp);
-        r = r < -last ? -last : r > last ? last : r;
-        return lut[r + last];
+        const int r = attn_distance(kp, qp);
+        return __builtin_elementwise_max(__builtin_elementwise_min(r, last), -last) + last;
     }
-    __device__ __forceinline__ float at(int place) const { return table[place * slots + slot]; }
+    __device__ __forceinline__ float at(int place) const { return table[(place << shift) + slot]; }
+    __device__ __forceinline__ float of(int index) const { return value[(index << shift) + slot]; }
 };
+static inline __host__ __device__ bool attn_bias_direct(const attn_args &a, int slots) { return (2 * a.last + 1) * slots <= 2048; }
 static inline size_t attn_bias_bytes(const attn_args &a, int slots)
 {
-    return a.buckets ? (size_t)((2 * a.last + 1 + 15) & ~15) + (size_t)((attn_places(a) * slots * 4 + 15) & ~15) : 0;
+    if (!a.buckets) return 0;
+    const size_t direct = attn_bias_direct(a, slots) ? (size_t)(((2 * a.last + 1) * slots * 4 + 15) & ~15) : 0;
+    return (size_t)((2 * a.last + 1 + 15) & ~15) + direct + (size_t)((attn_places(a) * slots * 4 + 15) & ~15);
 }
 // by the whole workgroup; the caller synchronises.  head(slot): the head of a slot, or -1
 template <typename T, typename HEAD>
-__device__ __forceinline__ attn_bias attn_make_bias(const attn_args &a, attn_lds *lds, int slots, HEAD head)
+__device__ __forceinline__ attn_bias attn_make_bias(const attn_args &a, attn_lds *lds, int shift, HEAD head)
 {
+    const int slots = 1 << shift, distances = 2 * a.last + 1;
+    const bool direct = attn_bias_direct(a, slots);
+    attn_bias b;
+    b.last = a.last; b.shift = shift; b.slot = 0;
     attn_lds_u8 *lut = (attn_lds_u8 *)lds;
-    attn_lds_f32 *table = (attn_lds_f32 *)(lds + ((2 * a.last + 1 + 15) & ~15));
-    for (int x = threadIdx.x; x <= 2 * a.last; x += blockDim.x) lut[x] = (uint8_t)attn_place_of(a, attn_bucket(a, x - a.last));
-    for (int x = threadIdx.x; x < attn_places(a) * slots; x += blockDim.x) {
-        const int h = head(x % slots);
-        table[x] = h < 0 ? 0.f : (float)((const T *)a.table)[(int64_t)attn_bucket_of(a, x / slots) * a.ldt + h];
+    b.lut = lut;
+    b.value = direct ? (attn_lds_f32 *)(lds + ((distances + 15) & ~15)) : nullptr;
+    b.table = (attn_lds_f32 *)(lds + ((distances + 15) & ~15) + (direct ? (distances * slots * 4 + 15) & ~15 : 0));
+    auto entry = [&](int bucket, int s) {
+        const int h = head(s);
+        return h < 0 ? 0.f : (float)((const T *)a.table)[(int64_t)bucket * a.ldt + h];
+    };
+    for (int x = threadIdx.x; x < distances; x += blockDim.x) {
+        const int bucket = attn_bucket(a, x - a.last);
+        lut[x] = (uint8_t)attn_place_of(a, bucket);
+        if (direct)
+            for (int s = 0; s < slots; ++s) b.value[(x << shift) + s] = entry(bucket, s);
     }
-    return {lut, table, a.last, slots, 0};
+    for (int x = threadIdx.x; x < attn_places(a) * slots; x += blockDim.x) b.table[x] = entry(attn_bucket_of(a, x >> shift), x & (slots - 1));
+    return b;
+}
+// scores of a tile: s * scale + bias, of the distances k(x) - q(x) of its 16 pairs
+template <typename K, typename Q>
+__device__ __forceinline__ void attn_add_bias(const attn_bias &bias, attn_f32x16 &s, float scale, K k, Q q)
+{
+    int i[16];
+#pragma unroll
+    for (int x = 0; x < 16; ++x) i[x] = bias.index(k(x), q(x));
+    if (bias.value) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], scale, bias.of(i[x]));
+    } else {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) i[x] = bias.lut[i[x]];
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], scale, bias.at(i[x]));
+    }
+}
+// Is any of a wave's scores minus infinity?
+__device__ __forceinline__ bool attn_any_lowest(const attn_f32x16 &s)
+{
+    float low = s[0];
+#pragma unroll
+    for (int x = 1; x < 16; ++x) low = fminf(low, s[x]);
+    return __builtin_amdgcn_ballot_w64(low == -INFINITY) != 0;
 }
 
 // How the 32 rows of a wave's tile are made of queries and heads.
@@ -392,9 +434,9 @@ struct attn_lane {
 template <typename T>
 __device__ __forceinline__ attn_bias attn_lane_bias(const attn_args &a, attn_lds *lds, int mode, int group, int lane, int wave, int waves)
 {
-    const int slots = mode == kHeadsTogether ? 32 : mode == kHeadsOfRows ? waves : 1;
-    attn_bias b = attn_make_bias<T>(a, lds, slots, [&](int s) {
-        const int x = slots == 1 ? group / a.Hk : group / a.Hk * slots + s;
+    const int shift = mode == kHeadsTogether ? 5 : mode == kHeadsOfRows ? 2 : 0;         // of four waves
+    attn_bias b = attn_make_bias<T>(a, lds, shift, [&](int s) {
+        const int x = shift == 0 ? group / a.Hk : (group / a.Hk << shift) + s;
         return x < a.G ? group % a.Hk * a.G + x : -1;
     });
     b.slot = mode == kHeadsTogether ? lane & 31 : mode == kHeadsOfRows ? wave : 0;
