@@ -14,7 +14,7 @@ namespace {
 // POS: with positions (bias, causal); scores are held in units of e then, so that a bias of the type's lowest value stays a number,
 // and as plain products of q and k otherwise.
 template <typename T, int DT, int WM, int WN, int KW, bool POS>
-__global__ __launch_bounds__(64 * WM * WN, DT <= 128 ? 2 : 1) void forward_kernel(forward_args f)
+__global__ __launch_bounds__(64 * WM * WN, DT * (int)sizeof(T) <= 128 ? 3 : DT <= 128 ? 2 : 1) void forward_kernel(forward_args f)
 {
     typedef attn_tile<T, DT> tile;
     typedef typename tile::frag frag;

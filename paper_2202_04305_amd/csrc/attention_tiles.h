@@ -324,12 +324,11 @@ __device__ __forceinline__ int attn_wave_max(int v)
     return v;
 }
 
-// The position bias in LDS: the place of every distance's bucket up to the last border, the table's columns of the heads at hand (a slot
-// each, 1 << shift of them), and, where that is small, the bias of every distance.
+// The position bias in LDS: the place of every distance's bucket up to the last border, and the table's columns of the heads at hand (a
+// slot each, 1 << shift of them).  (The bias of every distance instead, one read less, made no difference.)
 struct attn_bias {
     const attn_lds_u8 *lut;              // [2 last + 1]
     attn_lds_f32 *table;                 // [places][slots]
-    attn_lds_f32 *value;                 // [2 last + 1][slots], or null
     int last, shift, slot;
     __device__ __forceinline__ int index(int kp, int qp) const
     {
@@ -337,39 +336,24 @@ struct attn_bias {
         return __builtin_elementwise_max(__builtin_elementwise_min(r, last), -last) + last;
     }
     __device__ __forceinline__ float at(int place) const { return table[(place << shift) + slot]; }
-    __device__ __forceinline__ float of(int index) const { return value[(index << shift) + slot]; }
 };
-static inline __host__ __device__ bool attn_bias_direct(const attn_args &a, int slots) { return (2 * a.last + 1) * slots <= 2048; }
 static inline size_t attn_bias_bytes(const attn_args &a, int slots)
 {
-    if (!a.buckets) return 0;
-    const size_t direct = attn_bias_direct(a, slots) ? (size_t)(((2 * a.last + 1) * slots * 4 + 15) & ~15) : 0;
-    return (size_t)((2 * a.last + 1 + 15) & ~15) + direct + (size_t)((attn_places(a) * slots * 4 + 15) & ~15);
+    return a.buckets ? (size_t)((2 * a.last + 1 + 15) & ~15) + (size_t)((attn_places(a) * slots * 4 + 15) & ~15) : 0;
 }
 // by the whole workgroup; the caller synchronises.  head(slot): the head of a slot, or -1
 template <typename T, typename HEAD>
 __device__ __forceinline__ attn_bias attn_make_bias(const attn_args &a, attn_lds *lds, int shift, HEAD head)
 {
     const int slots = 1 << shift, distances = 2 * a.last + 1;
-    const bool direct = attn_bias_direct(a, slots);
-    attn_bias b;
-    b.last = a.last; b.shift = shift; b.slot = 0;
     attn_lds_u8 *lut = (attn_lds_u8 *)lds;
-    b.lut = lut;
-    b.value = direct ? (attn_lds_f32 *)(lds + ((distances + 15) & ~15)) : nullptr;
-    b.table = (attn_lds_f32 *)(lds + ((distances + 15) & ~15) + (direct ? (distances * slots * 4 + 15) & ~15 : 0));
-    auto entry = [&](int bucket, int s) {
-        const int h = head(s);
-        return h < 0 ? 0.f : (float)((const T *)a.table)[(int64_t)bucket * a.ldt + h];
-    };
-    for (int x = threadIdx.x; x < distances; x += blockDim.x) {
-        const int bucket = attn_bucket(a, x - a.last);
-        lut[x] = (uint8_t)attn_place_of(a, bucket);
-        if (direct)
-            for (int s = 0; s < slots; ++s) b.value[(x << shift) + s] = entry(bucket, s);
+    attn_lds_f32 *table = (attn_lds_f32 *)(lds + ((distances + 15) & ~15));
+    for (int x = threadIdx.x; x < distances; x += blockDim.x) lut[x] = (uint8_t)attn_place_of(a, attn_bucket(a, x - a.last));
+    for (int x = threadIdx.x; x < attn_places(a) * slots; x += blockDim.x) {
+        const int h = head(x & (slots - 1));
+        table[x] = h < 0 ? 0.f : (float)((const T *)a.table)[(int64_t)attn_bucket_of(a, x >> shift) * a.ldt + h];
     }
-    for (int x = threadIdx.x; x < attn_places(a) * slots; x += blockDim.x) b.table[x] = entry(attn_bucket_of(a, x >> shift), x & (slots - 1));
-    return b;
+    return {lut, table, a.last, shift, 0};
 }
 // scores of a tile: s * scale + bias, of the distances k(x) - q(x) of its 16 pairs
 template <typename K, typename Q>
@@ -378,15 +362,10 @@ __device__ __forceinline__ void attn_add_bias(const attn_bias &bias, attn_f32x16
     int i[16];
 #pragma unroll
     for (int x = 0; x < 16; ++x) i[x] = bias.index(k(x), q(x));
-    if (bias.value) {
 #pragma unroll
-        for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], scale, bias.of(i[x]));
-    } else {
+    for (int x = 0; x < 16; ++x) i[x] = bias.lut[i[x]];
 #pragma unroll
-        for (int x = 0; x < 16; ++x) i[x] = bias.lut[i[x]];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], scale, bias.at(i[x]));
-    }
+    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], scale, bias.at(i[x]));
 }
 // Is any of a wave's scores minus infinity?
 __device__ __forceinline__ bool attn_any_lowest(const attn_f32x16 &s)
