@@ -185,6 +185,8 @@ class Encoding:
 class Tensor:
     def __init__(self, handle, allocator, dtype, device):
         self._h, self._allocator, self.dtype, self.device = handle, allocator, dtype, device
+        self._sizes = None               # (rank, m, n), once asked for
+        self._workspaces = {}            # bytes of workspace of the attention problems met so far
 
     def free(self):
         if self._h and _lib is not None:
@@ -338,42 +340,44 @@ def sp_prepare_attention(S, grad=False):
 
 
 def _rows_of_heads(t, name, S, dtype):
-    """The strides of a (tokens, heads, d) tensor: the last dimension is contiguous, the other two are free."""
-    if t.dim() != 3 or t.dtype != dtype or t.device != S.device or (t.shape[2] > 1 and t.stride(2) != 1):
+    """The address and strides of a (tokens, heads, d) tensor: the last dimension is contiguous, the other two are free."""
+    st = t.stride()
+    if len(st) != 3 or t.dtype != dtype or t.device != S.device or (st[2] != 1 and t.shape[2] > 1):
         raise ValueError("%s: a (tokens, heads, d) tensor of %s on %s with a contiguous last dimension, not %s %s strides %s on %s" % (
             name, dtype, S.device, t.dtype, tuple(t.shape), tuple(t.stride()), t.device))
-    return t.data_ptr(), int(t.stride(0)), int(t.stride(1))
+    return t.data_ptr(), st[0], st[1]
 
 
 def _attention_problem(S, Q, K, V, scale, causal, qpos, kpos, bias, max_distance, bidirectional):
-    info = sp_tensor_info(S)
-    if info.rank != 2:
+    if S._sizes is None:
+        info = sp_tensor_info(S)
+        S._sizes = info.rank, info.shape[0], info.shape[1] if info.rank > 1 else 0
+    rank, m, n = S._sizes
+    if rank != 2:
         raise SpError(2, "in sp_attention")
-    m, n = info.shape[0], info.shape[1]
-    if Q.dtype not in _ATTENTION_DT:
-        raise SpError(9, "in sp_attention: %s" % Q.dtype)
-    p = SpAttentionProblem()
-    p.Q, p.ldq, p.hdq = _rows_of_heads(Q, "Q", S, Q.dtype)
-    p.K, p.ldk, p.hdk = _rows_of_heads(K, "K", S, Q.dtype)
-    p.V, p.ldv, p.hdv = _rows_of_heads(V, "V", S, Q.dtype)
-    if Q.shape[0] != m or K.shape[0] != n or V.shape != K.shape or K.shape[2] != Q.shape[2]:
+    dtype = Q.dtype
+    if dtype not in _ATTENTION_DT:
+        raise SpError(9, "in sp_attention: %s" % dtype)
+    q, k, v = _rows_of_heads(Q, "Q", S, dtype), _rows_of_heads(K, "K", S, dtype), _rows_of_heads(V, "V", S, dtype)
+    (rows, heads, d), (cols, kv, dk) = Q.shape, K.shape
+    if rows != m or cols != n or V.shape != K.shape or dk != d:
         raise ValueError("Q %s, K %s, V %s for a pattern of %d x %d" % (tuple(Q.shape), tuple(K.shape), tuple(V.shape), m, n))
-    p.dtype, p.heads, p.kvHeads, p.headDim = _ATTENTION_DT[Q.dtype], int(Q.shape[1]), int(K.shape[1]), int(Q.shape[2])
-    p.scale = float(Q.shape[2]) ** -0.5 if scale is None else float(scale)
-    p.causal = int(bool(causal))
+    at, table = (None, None), (None, 0)
+    buckets = 0
     if causal or bias is not None:
         for name, t, size in (("qpos", qpos, m), ("kpos", kpos, n)):
             if t is None or t.dtype != torch.int32 or t.device != S.device or tuple(t.shape) != (size,) or not t.is_contiguous():
                 raise ValueError("%s: %d contiguous int32 positions on %s" % (name, size, S.device))
-        p.qpos, p.kpos = qpos.data_ptr(), kpos.data_ptr()
+        at = qpos.data_ptr(), kpos.data_ptr()
     if bias is not None:
-        if bias.dim() != 2 or bias.dtype != Q.dtype or bias.device != S.device or bias.shape[1] != Q.shape[1] or (bias.shape[1] > 1 and bias.stride(1) != 1):
-            raise ValueError("bias: a (buckets, heads) tensor of %s on %s" % (Q.dtype, S.device))
-        if bias.shape[0] == 0:
+        if bias.dim() != 2 or bias.dtype != dtype or bias.device != S.device or bias.shape[1] != heads or (heads > 1 and bias.stride(1) != 1):
+            raise ValueError("bias: a (buckets, heads) tensor of %s on %s" % (dtype, S.device))
+        buckets = int(bias.shape[0])
+        if buckets == 0:
             raise SpError(8, "in sp_attention: no buckets")
-        p.table, p.ldt, p.buckets = bias.data_ptr(), max(int(bias.stride(0)), int(bias.shape[1])) if bias.shape[0] == 1 else int(bias.stride(0)), int(bias.shape[0])
-        p.maxDistance, p.bidirectional = int(max_distance), int(bool(bidirectional))
-    return p
+        table = bias.data_ptr(), max(bias.stride(0), heads) if buckets == 1 else bias.stride(0)
+    return SpAttentionProblem(_ATTENTION_DT[dtype], heads, kv, d, 1 if causal else 0, buckets, int(max_distance), 1 if bidirectional else 0,
+                              (float(d) ** -0.5 if d else 1.0) if scale is None else float(scale), *q, *k, *v, *at, *table)
 
 
 def _attention_call(S, f):
@@ -385,9 +389,13 @@ def _attention_call(S, f):
 
 
 def _attention_workspace(L, S, p, grad):
-    need = ctypes.c_size_t()
-    _check(L.sp_attention_workspace(S._h, ctypes.byref(p), grad, ctypes.byref(need)), "in sp_attention_workspace")
-    return torch.empty(need.value, dtype=torch.uint8, device=S.device) if need.value else None, need.value
+    key = (grad, p.dtype, p.heads, p.kvHeads, p.headDim, p.buckets, p.bidirectional, p.maxDistance)
+    size = S._workspaces.get(key)
+    if size is None:
+        need = ctypes.c_size_t()
+        _check(L.sp_attention_workspace(S._h, ctypes.byref(p), grad, ctypes.byref(need)), "in sp_attention_workspace")
+        size = S._workspaces[key] = need.value
+    return torch.empty(size, dtype=torch.uint8, device=S.device) if size else None, size
 
 
 def _attention_output(t, like, name):

@@ -192,8 +192,8 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                 near = attn_look(a, attn_distance(col, q_hi), attn_distance(col, q_lo));
                 if (near.nothing) continue;
             }
-            attn_f32x16 s = tile::scores(sK, 32 * t, q, lane);
-            attn_f32x16 dp = tile::scores(sV, 32 * t, go, lane);
+            attn_f32x16 s = tile::scores(sK, 32 * t, q, a.D, lane);
+            attn_f32x16 dp = tile::scores(sV, 32 * t, go, a.D, lane);
             // what is not stored, and rows that do not exist, add nothing
             const uint32_t bits = (me.valid ? (uint32_t)(word >> (32 * t)) : 0u) >> (4 * (lane >> 5));
             if (!POS) {
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                     far_x[1] += behind ? 0.f : sum_x; far_p[1] += behind ? 0.f : sum_p;
                 }
             }
-            tile::add_rows(acc, sK, 32 * t, s, lane);
+            tile::add_rows(acc, sK, 32 * t, s, a.D, lane);
         }
     }
     float odd = 0;
@@ -376,11 +376,17 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     }
 }
 
+// Does a workgroup of dkv_kernel take a compute unit's registers for itself?  Two sums and two operands of 128 numbers of 16 bits are 192
+// registers; with the positions' work beside them the rest no longer fits half of the 512 (dK, dV of a band of 10763 tokens, 8 heads of
+// 128, with bias: 262 us so, 86 alone), without it, it nearly does (8 sequences of about 860, 16 heads of 128: 446 us for the whole
+// step, 476 alone).
+constexpr bool attn_dkv_alone(int row_bytes, bool pos) { return row_bytes > (pos ? 128 : 256); }
+
 // dK and dV: blocks of keys (lanes) over the queries that attend to them, head by head of the keys' group.  Q and dO come through
 // LDS, K and V stay in registers; the scores are those of the forward kernel with the roles exchanged, so weights and ds are again
 // operands as they lie.  WM waves take 32 keys each.
 template <typename T, int DT, int WM, int KW, bool POS>
-__global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_kernel(grad_args f)
+__global__ __launch_bounds__(64 * WM, attn_dkv_alone(DT * (int)sizeof(T), POS) ? 1 : 2) void dkv_kernel(grad_args f)
 {
     typedef attn_tile<T, DT> tile;
     typedef typename tile::frag frag;
@@ -497,8 +503,8 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
                 near = attn_look(a, attn_distance(k_lo, qp), attn_distance(k_hi, qp));
                 if (near.nothing) continue;
             }
-            attn_f32x16 s = tile::scores(sQ, 32 * t, kx, lane);
-            attn_f32x16 dp = tile::scores(sO, 32 * t, vx, lane);
+            attn_f32x16 s = tile::scores(sQ, 32 * t, kx, a.D, lane);
+            attn_f32x16 dp = tile::scores(sO, 32 * t, vx, a.D, lane);
             const uint32_t bits = (valid ? (uint32_t)(word >> (32 * t)) : 0u) >> (4 * (lane >> 5));
             uint32_t there = bits;
             if (POS) {
@@ -537,8 +543,8 @@ __global__ __launch_bounds__(64 * WM, DT * sizeof(T) <= 256 ? 2 : 1) void dkv_ke
                     dp[x] = attn_where(there, 8 * (x >> 2) + (x & 3), dp[x]);
                 }
             }
-            tile::add_rows(dv, sO, 32 * t, s, lane);
-            tile::add_rows(dk, sQ, 32 * t, dp, lane);
+            tile::add_rows(dv, sO, 32 * t, s, a.D, lane);
+            tile::add_rows(dk, sQ, 32 * t, dp, a.D, lane);
         }
     }
     float odd = 0;
@@ -658,7 +664,7 @@ sp_status launch_dq_mode(const grad_args &f, const attn_mapping &c, int64_t item
 template <typename T, int DT, bool POS>
 sp_status launch_dkv_mode(const grad_args &f, int br, int64_t items, hipStream_t st)
 {
-    constexpr int KW = sizeof(T) == 2 && DT <= 128 ? 64 : 32;
+    constexpr int KW = sizeof(T) == 2 && (DT <= 64 || (DT == 128 && POS)) ? 64 : 32;
     const size_t lds = 4 * (size_t)KW * DT * sizeof(T) + KW * 24 + (POS ? attn_bias_bytes(f.a, 2) : 0);
     if (br == 128) return launch(dkv_kernel<T, DT, 4, KW, POS>, f, items * f.a.Hk, 256, lds, st);
     return launch(dkv_kernel<T, DT, 1, KW, POS>, f, items * f.a.Hk, 64, lds, st);

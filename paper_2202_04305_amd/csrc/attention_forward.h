@@ -127,7 +127,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * (int)sizeof(T) <= 128 ? 3 : DT <
                     continue;
                 }
             }
-            s[t] = tile::scores(sK, 32 * t, q, lane);
+            s[t] = tile::scores(sK, 32 * t, q, a.D, lane);
             if (POS) {
                 if (a.buckets && !near.far) {
                     attn_add_bias(bias, s[t], a.scale, [&](int x) { return kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]; }, [&](int) { return qp; });
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * (int)sizeof(T) <= 128 ? 3 : DT <
                 s[t][x] = __builtin_amdgcn_exp2f(POS ? (s[t][x] - base) * cc : __builtin_fmaf(s[t][x], cc, off));
                 total += s[t][x];
             }
-            tile::add_rows(acc, sV, 32 * t, s[t], lane);
+            tile::add_rows(acc, sV, 32 * t, s[t], a.D, lane);
         }
     }
     total = attn_pair_sum(total);

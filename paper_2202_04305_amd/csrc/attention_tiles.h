@@ -65,44 +65,64 @@ struct attn_tile {
     template <typename V>
     static __device__ __forceinline__ V read(unsigned at) { return *(const __attribute__((address_space(3))) V *)(uintptr_t)at; }
 
+    // Is any of a row's last quarter used?  (Head sizes up to 48, 96 or 192 do without their products.)
+    static constexpr int kQuarter = DT / 4 * 3;
+
     // acc (32 rows x 32 lanes) = the tile's rows row0 ... (a multiple of 32) times the lanes' rows `b`
-    static __device__ __forceinline__ attn_f32x16 scores(const attn_lds *t, int row0, const frag (&b)[kSteps], int lane)
+    static __device__ __forceinline__ attn_f32x16 scores(const attn_lds *t, int row0, const frag (&b)[kSteps], int D, int lane)
     {
         const unsigned base = (unsigned)(uintptr_t)t + (unsigned)place(lane & 31, lane >> 5);
         attn_f32x16 acc = (attn_f32x16)(0.f);
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) acc = attn_mma<T>::mul(read<frag>((base ^ (unsigned)(s << 5)) + row0 * kRow), b[s], acc);
+        for (int s = 0; s < kSteps - kSteps / 4; ++s) acc = attn_mma<T>::mul(read<frag>((base ^ (unsigned)(s << 5)) + row0 * kRow), b[s], acc);
+        if (D > kQuarter) {
+#pragma unroll
+            for (int s = kSteps - kSteps / 4; s < kSteps; ++s) acc = attn_mma<T>::mul(read<frag>((base ^ (unsigned)(s << 5)) + row0 * kRow), b[s], acc);
+        }
         return acc;
     }
     // acc[x] (numbers 32 x ... of a head, 32 lanes) += sum over the tile's 32 rows from row0 on of row[number] * w[row of the lane]
-    static __device__ __forceinline__ void add_rows(attn_f32x16 (&acc)[kBlocks], const attn_lds *t, int row0, const attn_f32x16 &w, int lane)
+    static __device__ __forceinline__ void add_rows(attn_f32x16 (&acc)[kBlocks], const attn_lds *t, int row0, const attn_f32x16 &w, int D, int lane)
     {
+        constexpr int kFirst = kBlocks - kBlocks / 4;    // blocks that are not of the last quarter
         const int half = lane >> 5;
         if constexpr (sizeof(T) == 4) {
             const unsigned base = (unsigned)(uintptr_t)t + (unsigned)(place(4 * half, (lane & 31) >> 2) + (lane & 3) * 4);
+            auto block = [&](int x) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = 8 * (r >> 2) + (r & 3);  // and 4 for the upper half
-#pragma unroll
-                for (int x = 0; x < kBlocks; ++x)
+                for (int r = 0; r < 16; ++r) {
+                    const int row = 8 * (r >> 2) + (r & 3);      // and 4 for the upper half
                     acc[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(read<float>((base ^ (unsigned)((x * 8 ^ swizzle(row)) << 4)) + (row0 + row) * kRow), w[r], acc[x], 0, 0, 0);
+                }
+            };
+#pragma unroll
+            for (int x = 0; x < kFirst; ++x) block(x);
+            if (kFirst < kBlocks && D > kQuarter) {
+#pragma unroll
+                for (int x = kFirst; x < kBlocks; ++x) block(x);
             }
         } else {
             const unsigned base = (unsigned)(uintptr_t)t + (unsigned)(place(4 * half + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8);
+            frag p[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                frag p;
+            for (int k = 0; k < 16; ++k) p[k >> 3][k & 7] = (T)w[k];
+            auto block = [&](int x, int u) {
+                union { attn_s16x4 q[2]; frag f; } v;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) p[k] = (T)w[8 * u + k];
+                for (int k = 0; k < 2; ++k)              // rows 16 u + 8 k on, whose swizzle is that of the first ones exchanged by 2 k
+                    v.q[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) attn_s16x4 *)(uintptr_t)(
+                        (base ^ (unsigned)((4 * x ^ 2 * k) << 4)) + (row0 + 16 * u + 8 * k) * kRow));
+                acc[x] = attn_mma<T>::mul(v.f, p[u], acc[x]);
+            };
 #pragma unroll
-                for (int x = 0; x < kBlocks; ++x) {
-                    union { attn_s16x4 q[2]; frag f; } v;
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)          // rows 16 u + 8 k on, whose swizzle is that of the first ones exchanged by 2 k
-                        v.q[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) attn_s16x4 *)(uintptr_t)(
-                            (base ^ (unsigned)((4 * x ^ 2 * k) << 4)) + (row0 + 16 * u + 8 * k) * kRow));
-                    acc[x] = attn_mma<T>::mul(v.f, p, acc[x]);
-                }
+                for (int x = 0; x < kFirst; ++x) block(x, u);
+            if (kFirst < kBlocks && D > kQuarter) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int x = kFirst; x < kBlocks; ++x) block(x, u);
             }
         }
     }
