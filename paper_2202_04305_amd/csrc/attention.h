@@ -43,7 +43,7 @@ struct sp_attn_plan {
     size_t bytes;
 };
 
-static inline __host__ __device__ int attn_level_chunks(int level) { return 2 << level; }
+static inline __host__ __device__ int attn_level_chunks(int level) { return 1 << level; }
 
 // A plan at one level, as kernels take it.
 struct attn_plan_view {

@@ -159,7 +159,7 @@ extern "C" sp_status sp_attention_grad(const sp_tensor *S, const sp_attention_pr
     if (need > workspaceBytes || ((uintptr_t)workspace & 255)) return SP_ERR_SHAPE;
     f.g = *g;
     f.pd = padded(a.D); f.exact = c.exact;
-    f.delta = (const float *)workspace;
+    f.delta = (float *)workspace;
     f.part = (float *)((char *)workspace + c.delta);
     if (a.buckets && g->dTable) f.part_table = (float *)((char *)workspace + c.delta + c.part);
     attn_alignment rows(a.D, size);

@@ -10,29 +10,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// D[h,i] = sum_d dO[i,h,d] * O[i,h,d]: LPR lanes for a row, 16 bytes of it each
-template <typename T, int LPR>
-__global__ __launch_bounds__(kThreads) void delta_kernel(grad_args f, float *__restrict__ delta)
-{
-    constexpr int V = 16 / (int)sizeof(T);
-    typedef typename attn_mma<T>::frag frag;
-    const attn_args &a = f.a;
-    const int l = threadIdx.x % LPR;
-    const int64_t x = (int64_t)blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
-    float s = 0;
-    const int64_t i = x / a.H;
-    const int h = (int)(x % a.H);
-    if (x < a.m * a.H) {
-        const T *u = (const T *)f.g.O + i * f.g.ldo + h * f.g.hdo, *v = (const T *)f.g.dO + i * f.g.lddo + h * f.g.hddo;
-        const frag p = attn_tile<T, 32>::granule(u, l * V, a.D, f.vec, true), q = attn_tile<T, 32>::granule(v, l * V, a.D, f.vec, true);
-#pragma unroll
-        for (int k = 0; k < V; ++k) s += (float)p[k] * (float)q[k];
-    }
-#pragma unroll
-    for (int d = LPR / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
-    if (l == 0 && x < a.m * a.H) delta[h * a.m + i] = s;
-}
-
 // v where bit k of `bits` is set, otherwise 0, whatever v is.
 __device__ __forceinline__ float attn_where(uint32_t bits, int k, float v) { return __uint_as_float(__float_as_uint(v) & (uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1)); }
 
@@ -103,11 +80,23 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
 
     frag q[tile::kSteps], go[tile::kSteps];
     tile::load_lane((const T *)a.Q + me.row * a.ldq + me.head * a.hdq, a.D, f.vec, some, POS ? 1.f : a.c, q, lane);
-    tile::load_lane((const T *)f.g.dO + me.row * f.g.lddo + me.head * f.g.hddo, a.D, f.vec, some, 1.f, go, lane);
+    tile::load_lane((const T *)f.g.dO + me.row * f.g.lddo + me.head * f.g.hddo, a.D, f.vec, me.valid, 1.f, go, lane);
     float off = f.g.lse[me.head * a.m + me.row];
     if (off == -INFINITY) off = INFINITY;                // no weight left
     if (!POS) off *= kLog2e;
-    const float delta = f.delta[me.head * a.m + me.row];
+    // D = sum dO * O of the lane's row
+    float delta = 0;
+    {
+        const T *o = (const T *)f.g.O + me.row * f.g.ldo + me.head * f.g.hdo;
+#pragma unroll
+        for (int s = 0; s < tile::kSteps; ++s) {
+            const frag u = tile::granule(o, (2 * s + (lane >> 5)) * tile::kPer, a.D, f.vec, me.valid);
+#pragma unroll
+            for (int k = 0; k < tile::kPer; ++k) delta += (float)u[k] * (float)go[s][k];
+        }
+        delta = attn_pair_sum(delta);
+    }
+    float rest = 0;                                      // sum of ds over the row's pairs
     int qp = 0, q_lo = 0, q_hi = 0;
     attn_bias bias = {};
     attn_lds_f32 *hist = nullptr;                             // [buckets][64] of ds; exact: of p dP and p
@@ -245,9 +234,17 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                     far_x[1] += behind ? 0.f : sum_x; far_p[1] += behind ? 0.f : sum_p;
                 }
             }
+            if (sizeof(T) == 2) {
+#pragma unroll
+                for (int x = 0; x < 16; ++x) rest += s[x];
+            }
             tile::add_rows(acc, sK, 32 * t, s, a.D, lane);
         }
     }
+    // For dkv_kernel.  The weights of a row that is whole here sum to 1, so what its ds miss to sum to 0 is the error of a D made of an O
+    // that was rounded to 16 bits.
+    rest = sizeof(T) == 2 && item.whole ? attn_pair_sum(rest) : 0.f;
+    if (WN == 1 && me.valid && lane < 32 && item.c0 == item.chunk0) f.delta[me.head * a.m + me.row] = delta + rest;
     float odd = 0;
 #pragma unroll
     for (int x = 0; x < tile::kBlocks; ++x)
@@ -329,17 +326,22 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                 const int g = (8 * x + 2 * b + (lane >> 5)) ^ (lane & 7);
                 *(attn_lds_f32x4 *)(sums + (wn * 32 + (lane & 31)) * DT + 4 * g) = (attn_f32x4){acc[x][4 * b], acc[x][4 * b + 1], acc[x][4 * b + 2], acc[x][4 * b + 3]};
             }
-        if (lane < 32) bad[wn * 32 + lane] = (again | again >> 32) >> lane & 1 ? 1.f : 0.f;
+        if (lane < 32) {
+            bad[wn * 32 + lane] = (again | again >> 32) >> lane & 1 ? 1.f : 0.f;
+            bad[(WN + wn) * 32 + lane] = rest;
+        }
         __syncthreads();
         constexpr int LANES = NT / 32, EACH = DT / LANES;
         const int mine = tid / LANES, part = tid % LANES;
-        float any = 0;
+        float any = 0, more = 0;
 #pragma unroll
-        for (int x = 0; x < WN; ++x) any += bad[x * 32 + mine];
+        for (int x = 0; x < WN; ++x) { any += bad[x * 32 + mine]; more += bad[(WN + x) * 32 + mine]; }
+        const float delta2 = __shfl(delta, mine, 64);
         const int64_t row2 = ((int64_t)__shfl((int)(me.row >> 32), mine, 64) << 32) | (uint32_t)__shfl((int)me.row, mine, 64);
         const int head2 = __shfl(me.head, mine, 64), r2 = __shfl(r, mine, 64);
         const bool valid2 = __shfl((int)me.valid, mine, 64) != 0;
         const int64_t place2 = (item.part * a.H + head2) * p.br + r2;
+        if (valid2 && part == 0 && item.c0 == item.chunk0) f.delta[head2 * a.m + row2] = delta2 + more;
         if (valid2 && any == 0) {
 #pragma unroll
             for (int k = 0; k < EACH; k += 4) {
@@ -364,7 +366,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         const int h = __builtin_amdgcn_readlane(me.head, x), rr = __builtin_amdgcn_readlane(r, x);
         float one[kAttnPer];
         attn_row_dq<T>(a, p, item.block, rr, item.c0, item.c1, i, h, lane, (const T *)f.g.dO + i * f.g.lddo + h * f.g.hddo, f.g.lse[h * a.m + i],
-                       f.delta[h * a.m + i], one);
+                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(delta), x)), one);
         const int64_t at1 = (item.part * a.H + h) * p.br + rr;
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) {
@@ -651,7 +653,7 @@ template <typename T, int DT, int WM, int WN, int KW, bool POS>
 sp_status launch_dq(const grad_args &f, const attn_mapping &c, int64_t items, hipStream_t st)
 {
     const size_t lds = attn_dq_lds(f.a, c, DT * (int)sizeof(T), POS, POS && f.part_table, f.exact);
-    const size_t join = WN > 1 ? (size_t)WN * 32 * (DT + 1) * 4 : 0;
+    const size_t join = WN > 1 ? (size_t)WN * 32 * (DT + 2) * 4 : 0;
     return launch(dq_kernel<T, DT, WM, WN, KW, POS>, f, items * c.groups, 64 * WM * WN, lds > join ? lds : join, st);
 }
 template <typename T, int DT, bool POS>
@@ -683,9 +685,6 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
     if (!a.buckets && !a.causal) a.qpos = a.kpos = nullptr;
     const bool pos = a.buckets || a.causal || a.scale == 0;
     if (a.m > 0) {
-        constexpr int LPR = DT * (int)sizeof(T) / 16;
-        hipLaunchKernelGGL((delta_kernel<T, LPR>), dim3((unsigned)ceil_div(a.m * a.H, kThreads / LPR)), dim3(kThreads), 0, st, f, (float *)f.delta);
-        SP_HIP(hipGetLastError());
         f.p = attn_view(rows, c.rows.level);
         f.groups = c.rows.groups; f.mode = c.rows.mode;
         const int64_t items = rows->items[c.rows.level];

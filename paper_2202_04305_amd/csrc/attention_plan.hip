@@ -372,9 +372,12 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
     SP_HIP(hipStreamSynchronize(st));
     for (int k = 0; k < tried; ++k) { ways[k].chunks = host[2 * k]; ways[k].most = host[2 * k + 1]; }
     // What a block of rows costs for each of its chunks' columns: about 64 rows' worth of work to fetch it, and its rows' worth of work,
-    // used or not; a row by itself takes the work of 32 (it shares its tile with the heads of its group only).
+    // used or not.  A row by itself fetches its columns for itself, but makes one tile of all heads of a group, where a block makes one for
+    // each head: it is the better choice until a block of 32 rows has every column twice on average, as long as the rows all run at
+    // once; beyond about 512 of them, beginning and ending one costs as much as 400 columns (4096 rows of 96 columns out of 65,536, 8
+    // heads: 95 us in blocks of 32, 378 by themselves; 276 rows of 79 out of 17,791, 8 heads of one key head, f32: 54 and 38).
     const int wide = tried == 3 && ways[2].chunks * 10 <= ways[0].chunks * 11 ? 2 : 0;
-    const double cost128 = (double)ways[wide].chunks * 64 * (64 + 128), cost32 = (double)ways[1].chunks * 64 * (64 + 32), cost1 = (double)entries * (64 + 32);
+    const double cost128 = (double)ways[wide].chunks * 64 * (64 + 128), cost32 = (double)ways[1].chunks * 64 * (64 + 32), cost1 = ((double)entries + 400.0 * (double)(m > 512 ? m - 512 : 0)) * (64 + 32) / 2;
     const way *chosen = nullptr;                         // null: rows by themselves
     if (transposed || cost1 > cost32 || cost1 > cost128) chosen = &ways[cost32 < cost128 ? 1 : wide];
     p->br = chosen ? chosen->br : 1;

@@ -531,7 +531,7 @@ struct grad_args {
     attn_args a;
     attn_plan_view p;
     sp_attention_grads g;
-    const float *delta;                  // [heads][m]
+    float *delta;                        // [heads][m]: D of every row, made by dq_kernel
     float *part;                         // of rows (keys) that are cut: dq [item][head][row of the block][pd]; dkv [item][kv head][key][2][pd]
     float *part_table;                   // [item][head][buckets]
     int groups, mode, vec, pd;
