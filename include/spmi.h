@@ -198,7 +198,8 @@ typedef struct sp_attention_problem {
  * reads instead of pos and crd: the distinct columns of every block of rows with a bit for each pair, and how the blocks are
  * cut into work items.  It serves any number of heads, any head size and type.  Synchronises `stream`; calling it again is a no-op.
  * S: a packed rank-2 tensor, row-major with a compressed innermost level (CSR or DCSR); other encodings give SP_ERR_UNSUPPORTED
- * (convert first).  Errors: NULL, RANK, UNSUPPORTED, TOO_LARGE (2^31 rows, columns or pairs of blocks and column windows), ALLOC, HIP. */
+ * (convert first).  Errors: NULL, RANK, UNSUPPORTED (also while `stream` is being recorded), TOO_LARGE (2^31 rows, columns or pairs of blocks and column
+ * windows), ALLOC, HIP. */
 sp_status sp_prepare_attention(sp_tensor *S, int grad, void *stream);
 
 /* Bytes of workspace that sp_attention (grad = 0) or sp_attention_grad (grad = 1) needs for this problem.  S must have been
@@ -212,7 +213,10 @@ sp_status sp_attention_workspace(const sp_tensor *S, const sp_attention_problem 
  *        `stream` is done.  Calls that may overlap (other streams, graphs that are replayed at the same time) need one each.
  * S must have been prepared with sp_prepare_attention (SP_ERR_UNSUPPORTED otherwise).  Enqueues on `stream`; neither allocates nor
  * synchronises, and keeps no state in the handle, so that calls may overlap and may be recorded into a HIP graph.  Results are the
- * same bits on every call.  Errors: NULL, RANK, DTYPE, SHAPE, UNSUPPORTED, HIP. */
+ * same bits on every call.  16-bit types: weights (and, for the gradients, ds) are rounded to the operands' type before the products they
+ * are operands of, as every operand of the matrix cores is; f16 gradients below 2^-14 lose precision, as elsewhere (scale the loss).
+ * Rows whose sums are not finite in the end are made again pair by pair, which takes longer.
+ * Errors: NULL, RANK, DTYPE, SHAPE, UNSUPPORTED, TOO_LARGE (2^31 workgroups), HIP. */
 sp_status sp_attention(const sp_tensor *S, const sp_attention_problem *p, void *O, int64_t ldo, int64_t hdo, float *lse,
                        void *workspace, size_t workspaceBytes, void *stream);
 

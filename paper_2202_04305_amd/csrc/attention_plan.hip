@@ -489,6 +489,8 @@ extern "C" sp_status sp_prepare_attention(sp_tensor *S, int grad, void *stream)
     if (S->enc.perm[0] != 0 || S->enc.lt[1] != SP_COMPRESSED) return SP_ERR_UNSUPPORTED;   // row-major with a compressed inner level
     if (S->nvalues >= ((int64_t)1 << 31)) return SP_ERR_TOO_LARGE;
     hipStream_t st = (hipStream_t)stream;
+    if (S->attention[0] && (!grad || S->attention[1])) return SP_OK;
+    if (spmi_recording(st)) return SP_ERR_UNSUPPORTED;   // it waits for the stream
     sp_mem mem{S->alloc, S->free_, S->ctx};
     if (!S->attention[0]) SP_TRY(build_plan(S, mem, false, st, &S->attention[0]));
     if (grad && !S->attention[1]) {

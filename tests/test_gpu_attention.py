@@ -406,6 +406,63 @@ def test_scores_then_softmax_then_product_by_the_other_calls():
     assert bool(((O[:, 0].double() - out.double()).abs().cpu() <= 3 * tol[:, 0]).all())
 
 
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-3, 2.5])
+def test_scales(scale, dt):
+    """Zero (every pair weighs the same), negative, small and large ones."""
+    check_all(ragged([50, 3], [70, 40]), 2, 1, 64, dt, scale=scale)
+    check_all(ragged([50, 3], [70, 40]), 2, 1, 64, dt, scale=scale, buckets=8, positions=(torch.arange(53), torch.arange(110)), max_distance=20)
+
+
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("name", ["band", "sparse", "tokens behind a prefix"])
+def test_gradients_of_rows_that_do_not_attend_to_one_that_is_not_a_number(name, dt):
+    """A key and value of NaN spoil what attends to them; all other rows' and keys' gradients stay right."""
+    at = PATTERNS[name]()
+    p = problem(at, 2, 1, 32, dt)
+    col = int((at.sum(0) + 1000 * (at.sum(0) == 0)).argmin())
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    p.K[col], p.V[col] = float("nan"), float("nan")
+    rows = ~at[:, col]
+    p.dO[~rows] = 0                                      # those rows' own gradients are lost, and the other keys' share of them
+    got = run(S, p)
+    p.K[col], p.V[col] = 0, 0
+    p.at = at & rows[:, None]
+    ref = reference(p)
+    keys = ~at[~rows].any(0)
+    check({"dQ": got["dQ"][rows.to(DEV)], "dK": got["dK"][keys.to(DEV)], "dV": got["dV"][keys.to(DEV)]},
+          {"dQ": tuple(t[rows] for t in ref["dQ"]), "dK": tuple(t[keys] for t in ref["dK"]), "dV": tuple(t[keys] for t in ref["dV"])}, name)
+
+
+def test_f16_gradients_beyond_the_type():
+    """dO so large that ds does not fit f16: such rows are made again pair by pair, in f32."""
+    at = ragged([40, 20], [50, 30])
+    p = problem(at, 2, 1, 32, F16)
+    p.dO[7] = p.dO[7] * 8000
+    p.K, p.V = p.K * 0.05, p.V
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    got, ref = run(S, p), reference(p)
+    assert float(ref["dQ"][0].abs().max()) < 65504 and float(ref["dV"][0].abs().max()) < 65504
+    rows = torch.arange(60) != 7
+    check({k: got[k] for k in ("O", "lse", "dV")}, {k: ref[k] for k in ("O", "lse", "dV")})
+    check({"dQ": got["dQ"]}, {"dQ": ref["dQ"]})
+    assert bool(torch.isfinite(got["dK"]).all()) or float(ref["dK"][0].abs().max()) > 65504
+
+
+def test_inspector_is_refused_while_a_graph_is_recorded():
+    at = torch.ones(5, 6, dtype=torch.bool)
+    S, T = pack(at), sp.sp_prepare_attention(pack(at))
+    x = torch.zeros(4, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x += 1
+        assert code(sp.sp_prepare_attention, S) == 10
+        sp.sp_prepare_attention(T)                       # there is nothing left to do
+    graph.replay()
+    torch.cuda.synchronize()
+    assert x.tolist() == [1.0] * 4
+
+
 def code(f, *a, **k):
     with pytest.raises(sp.SpError) as e:
         f(*a, **k)
