@@ -345,7 +345,11 @@ sp_status launch(const forward_args &f, const forward_choice &c, int64_t items, 
 template <typename T, int DT, bool POS>
 sp_status launch_mode(const forward_args &f, const forward_choice &c, int64_t items, hipStream_t st)
 {
-    if (c.wn > 1) return launch<T, DT, 1, (DT * (int)sizeof(T) <= 256 ? 4 : 2), 32, POS>(f, c, items, st);   // two places for each wave have to fit the LDS
+    // Waves that share a tile's columns have two places for their rows each.  Four of them, or two where four would not fit the LDS, or
+    // where two let five workgroups onto a compute unit instead of two (64 rows of 800 to 1500 columns, 16 heads of 64: 73 -> 70 us; 4096
+    // rows of 96 scattered ones: 94 -> 86; with positions to be looked at it is the other way round, 32 -> 49 for caches of 1024).
+    constexpr int row = DT * (int)sizeof(T);
+    if (c.wn > 1) return launch<T, DT, 1, (row == 512 || (row == 128 && !POS) ? 2 : 4), 32, POS>(f, c, items, st);
     return launch<T, DT, 4, 1, (DT * (int)sizeof(T) <= 256 ? 64 : 32), POS>(f, c, items, st);
 }
 

@@ -491,19 +491,25 @@ extern "C" sp_status sp_prepare_attention(sp_tensor *S, int grad, void *stream)
     hipStream_t st = (hipStream_t)stream;
     if (S->attention[0] && (!grad || S->attention[1])) return SP_OK;
     if (spmi_recording(st)) return SP_ERR_UNSUPPORTED;   // it waits for the stream
-    sp_mem mem{S->alloc, S->free_, S->ctx};
-    if (!S->attention[0]) SP_TRY(build_plan(S, mem, false, st, &S->attention[0]));
-    if (grad && !S->attention[1]) {
-        sp_encoding enc = S->enc;
-        enc.lt[0] = SP_DENSE; enc.lt[1] = SP_COMPRESSED;
-        enc.perm[0] = 1; enc.perm[1] = 0;
-        enc.pw = enc.cw = enc.pw_store = enc.cw_store = 32;
-        if (S->shape[0] >= ((int64_t)1 << 31) - 256) return SP_ERR_TOO_LARGE;
-        sp_tensor *T = nullptr;
-        SP_TRY(spmi_repack(S, &enc, st, &T));
-        const sp_status s = build_plan(T, mem, true, st, &S->attention[1]);
+    sp_tensor *T = nullptr;
+    try {
+        sp_mem mem{S->alloc, S->free_, S->ctx};
+        if (!S->attention[0]) SP_TRY(build_plan(S, mem, false, st, &S->attention[0]));
+        if (grad && !S->attention[1]) {
+            sp_encoding enc = S->enc;
+            enc.lt[0] = SP_DENSE; enc.lt[1] = SP_COMPRESSED;
+            enc.perm[0] = 1; enc.perm[1] = 0;
+            enc.pw = enc.cw = enc.pw_store = enc.cw_store = 32;
+            if (S->shape[0] >= ((int64_t)1 << 31) - 256) return SP_ERR_TOO_LARGE;
+            SP_TRY(spmi_repack(S, &enc, st, &T));
+            const sp_status s = build_plan(T, mem, true, st, &S->attention[1]);
+            sp_tensor_free(T);
+            T = nullptr;
+            SP_TRY(s);
+        }
+    } catch (...) {                                      // host memory ran out: no exception leaves a C entry
         sp_tensor_free(T);
-        SP_TRY(s);
+        return SP_ERR_ALLOC;
     }
     return SP_OK;
 }
