@@ -65,8 +65,8 @@ struct attn_tile {
     template <typename V>
     static __device__ __forceinline__ V read(unsigned at) { return *(const __attribute__((address_space(3))) V *)(uintptr_t)at; }
 
-    // Is any of a row's last quarter used?  (Head sizes up to 48, 96 or 192 do without their products.)
-    static constexpr int kQuarter = DT / 4 * 3;
+    // f32, whose products are slow, does without those of a row's last quarter where the head ends before it.
+    static constexpr int kQuarter = sizeof(T) == 4 ? DT / 4 * 3 : 0;
 
     // acc (32 rows x 32 lanes) = the tile's rows row0 ... (a multiple of 32) times the lanes' rows `b`
     static __device__ __forceinline__ attn_f32x16 scores(const attn_lds *t, int row0, const frag (&b)[kSteps], int D, int lane)
@@ -75,7 +75,7 @@ struct attn_tile {
         attn_f32x16 acc = (attn_f32x16)(0.f);
 #pragma unroll
         for (int s = 0; s < kSteps - kSteps / 4; ++s) acc = attn_mma<T>::mul(read<frag>((base ^ (unsigned)(s << 5)) + row0 * kRow), b[s], acc);
-        if (D > kQuarter) {
+        if (sizeof(T) == 2 || D > kQuarter) {
 #pragma unroll
             for (int s = kSteps - kSteps / 4; s < kSteps; ++s) acc = attn_mma<T>::mul(read<frag>((base ^ (unsigned)(s << 5)) + row0 * kRow), b[s], acc);
         }
@@ -84,10 +84,10 @@ struct attn_tile {
     // acc[x] (numbers 32 x ... of a head, 32 lanes) += sum over the tile's 32 rows from row0 on of row[number] * w[row of the lane]
     static __device__ __forceinline__ void add_rows(attn_f32x16 (&acc)[kBlocks], const attn_lds *t, int row0, const attn_f32x16 &w, int D, int lane)
     {
-        constexpr int kFirst = kBlocks - kBlocks / 4;    // blocks that are not of the last quarter
         const int half = lane >> 5;
         if constexpr (sizeof(T) == 4) {
             const unsigned base = (unsigned)(uintptr_t)t + (unsigned)(place(4 * half, (lane & 31) >> 2) + (lane & 3) * 4);
+            constexpr int kFirst = kBlocks - kBlocks / 4;        // blocks that are not of the last quarter
             auto block = [&](int x) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -117,13 +117,7 @@ struct attn_tile {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int x = 0; x < kFirst; ++x) block(x, u);
-            if (kFirst < kBlocks && D > kQuarter) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int x = kFirst; x < kBlocks; ++x) block(x, u);
-            }
+                for (int x = 0; x < kBlocks; ++x) block(x, u);
         }
     }
     // one lane's row as the second operand: numbers past D are zero

@@ -123,6 +123,21 @@ def test_head_sizes(D, dt):
     check_all(torch.ones(9, 400, dtype=torch.bool), 6, 1, D, dt, positions=(torch.arange(9) * 40, torch.arange(400)), buckets=64, max_distance=200)
 
 
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("D", [24, 64, 72, 128, 200, 256])
+@pytest.mark.parametrize("heads", [(2, 2), (2, 1), (6, 1)])
+def test_few_rows_and_few_keys(heads, D, dt):
+    """Blocks of 32 rows, and of 32 keys, over long stretches of the other side that are cut into several items."""
+    if dt == F32 and D > 128:
+        pytest.skip("refused: does not fit a lane's registers")
+    say("case few", heads, D, dt)
+    g = torch.Generator().manual_seed(D)
+    for m, n in ((20, 700), (700, 20)):
+        at = torch.rand(m, n, generator=g) < 0.8
+        check_all(at, heads[0], heads[1], D, dt)
+        check_all(at, heads[0], heads[1], D, dt, buckets=32, positions=(torch.arange(m) * 3, torch.arange(n) * 2 - 40), causal=D % 16 == 0, bidirectional=D != 64)
+
+
 @pytest.mark.parametrize("heads", [(1, 1), (2, 1), (3, 1), (6, 2), (8, 8), (8, 1), (40, 1), (70, 2)])
 @pytest.mark.parametrize("name", ["one row", "ragged batch", "band", "sparse", "tokens behind a prefix"])
 def test_head_layouts(name, heads):
@@ -293,6 +308,25 @@ def test_strides(dt):
     p.K, p.V = p.K[:, :1].expand(-1, 4, -1), p.V[:, :1].expand(-1, 4, -1)
     got, _ = sp.sp_attention(S, p.Q.to(DEV), p.K[:, :1].contiguous().to(DEV).expand(-1, 4, -1), p.V[:, :1].contiguous().to(DEV).expand(-1, 4, -1), **o)
     check({"O": got}, {"O": reference(p, False)["O"]}, "expanded")
+
+
+def test_offsets_beyond_32_bits():
+    """Rows of K and V so far apart that the last ones lie more than 2^32 bytes, and 2^31 numbers, behind the first."""
+    n, ld, D = 150_000, 16_384, 32
+    at = torch.zeros(5, n, dtype=torch.bool)
+    g = torch.Generator().manual_seed(8)
+    at[:, torch.randint(n, (60,), generator=g)] = True
+    at[:3, n - 40:] = True
+    at[3, :] = False
+    p = problem(at, 2, 1, D, BF16, train=False)
+    S = sp.sp_prepare_attention(pack(at))
+    far = torch.empty(n * ld, dtype=BF16, device=DEV)
+    K, V = (far.view(n, ld)[:, o:o + D].unflatten(1, (1, D)) for o in (0, 64))
+    K.copy_(p.K.to(DEV))
+    V.copy_(p.V.to(DEV))
+    assert (n - 1) * K.stride(0) > 2 ** 31
+    O, lse = sp.sp_attention(S, p.Q.to(DEV), K, V)
+    check({"O": O, "lse": lse}, reference(p, False))
 
 
 def test_gradients_against_differences():
