@@ -77,16 +77,17 @@ struct attn_args {
 // loads that depend on each other before the first rows arrive) and `row_bytes` for a part of one row of one item (written and read
 // again in f32), the level with the least of: what one of 512 places for a workgroup (two on each compute unit) gets of the work,
 // plus the longest item, plus the parts' traffic and the launch that joins them.
+static inline double attn_level_us(const sp_attn_plan *p, int level, int64_t groups, double chunk_us, double item_us, double row_bytes)
+{
+    const double longest = p->max_chunks < attn_level_chunks(level) ? (double)p->max_chunks : (double)attn_level_chunks(level);
+    const double extra = p->cut[level] ? 5 + (double)(p->items[level] - p->nblocks + p->cut[level]) * row_bytes * p->br * 2 / 4e6 : 0;
+    return (double)groups / 512 * (chunk_us * (double)p->nchunks + item_us * (double)p->items[level]) + chunk_us * longest + extra;
+}
 static inline int attn_pick_level(const sp_attn_plan *p, int64_t groups, double chunk_us, double item_us, double row_bytes)
 {
     int best = p->levels - 1;
-    double least = 0;
-    for (int l = p->levels - 1; l >= 0; --l) {
-        const double longest = p->max_chunks < attn_level_chunks(l) ? (double)p->max_chunks : (double)attn_level_chunks(l);
-        const double extra = p->cut[l] ? 5 + (double)(p->items[l] - p->nblocks + p->cut[l]) * row_bytes * p->br * 2 / 4e6 : 0;
-        const double us = (double)groups / 512 * (chunk_us * (double)p->nchunks + item_us * (double)p->items[l]) + chunk_us * longest + extra;
-        if (l == p->levels - 1 || us < least) { least = us; best = l; }
-    }
+    for (int l = p->levels - 2; l >= 0; --l)
+        if (attn_level_us(p, l, groups, chunk_us, item_us, row_bytes) < attn_level_us(p, best, groups, chunk_us, item_us, row_bytes)) best = l;
     return best;
 }
 

@@ -22,9 +22,10 @@ grad_choice choose(const sp_tensor *S, const attn_args &a, int size, bool table)
     const sp_attn_plan *rows = S->attention[0], *keys = S->attention[1];
     grad_choice c;
     c.rows = attn_map(rows, a, size, 3);
-    // the bias's gradient from sums that need a row's whole D: rows are not cut then, and the sums have to fit the LDS
+    // the bias's gradient from sums that need a row's whole D: rows are not cut then, unless a few long ones would hold up the rest for
+    // longer than the whole pass takes, and the sums have to fit the LDS
     const int row = (a.D <= 32 ? 32 : a.D <= 64 ? 64 : a.D <= 128 ? 128 : 256) * size;
-    c.exact = table && size == 2 && attn_dq_lds(a, c.rows, row, true, true, true) <= kAttnLds;
+    c.exact = table && size == 2 && c.rows.whole_us <= 2 * c.rows.us + 20 && attn_dq_lds(a, c.rows, row, true, true, true) <= kAttnLds;
     if (c.exact) { c.rows.level = rows->levels - 1; c.rows.cut = false; }
     c.keys_level = attn_pick_level(keys, a.Hk, attn_chunk_us(a.D, size, 4) * a.G * (keys->br == 128 ? 1 : 0.7), 3, 8.0 * a.D * a.Hk);
     c.keys_cut = keys->cut[c.keys_level] > 0;

@@ -142,7 +142,6 @@ struct attn_tile {
         }
         return f;
     }
-    static __device__ __forceinline__ void put(attn_lds *t, int r, int g, frag f) { *(__attribute__((address_space(3))) frag *)(t + place(r, g)) = f; }
 };
 
 // The larger of a lane's value and its partner's 32 lanes on; their sum.
@@ -441,6 +440,7 @@ __device__ __forceinline__ attn_bias attn_lane_bias(const attn_args &a, attn_lds
 // fewer, they share the columns out.
 struct attn_mapping {
     int mode, wm, wn, groups, level;
+    double us, whole_us;                 // modelled time of the level, and with whole blocks
     bool cut;                            // some rows have several items
     int slots() const { return mode == kHeadsTogether ? 32 : mode == kHeadsOfRows ? wm : 1; }
 };
@@ -461,7 +461,10 @@ static inline attn_mapping attn_map(const sp_attn_plan *plan, const attn_args &a
     const bool share = c.mode == kRowsTogether || c.mode == kHeadsTogether;
     c.wm = share ? 1 : 4;
     c.wn = share ? 4 : 1;
-    c.level = attn_pick_level(plan, c.groups, attn_chunk_us(a.D, size, products) / (share ? 2 : 1), share ? 6 : 3, 4.0 * a.D * a.H);
+    const double chunk_us = attn_chunk_us(a.D, size, products) / (share ? 2 : 1), item_us = share ? 6 : 3, row_bytes = 4.0 * a.D * a.H;
+    c.level = attn_pick_level(plan, c.groups, chunk_us, item_us, row_bytes);
+    c.us = attn_level_us(plan, c.level, c.groups, chunk_us, item_us, row_bytes);
+    c.whole_us = attn_level_us(plan, plan->levels - 1, c.groups, chunk_us, item_us, row_bytes);
     c.cut = plan->cut[c.level] > 0;
     return c;
 }

@@ -197,6 +197,16 @@ def test_position_bias(kind, buckets, far, dt):
     check_all(at, 4, 2, 32, dt, buckets=buckets, positions=pos, max_distance=far, **o)
 
 
+def test_position_bias_with_rows_that_attend_to_everything():
+    """A band whose first rows store every column as well: they are cut, their gradients joined."""
+    m = 6000
+    at = band(m, m, 12)
+    at[:3] = True
+    at[:, :2] = True
+    for dt in (BF16, F32):
+        check_all(at, 1, 1, 32, dt, buckets=16, positions=(torch.arange(m), torch.arange(m)), max_distance=40)
+
+
 @pytest.mark.parametrize("name", ["one row", "band", "sparse", "tokens behind a prefix"])
 def test_position_bias_by_pattern(name):
     at = PATTERNS[name]()
@@ -308,6 +318,54 @@ def test_strides(dt):
     p.K, p.V = p.K[:, :1].expand(-1, 4, -1), p.V[:, :1].expand(-1, 4, -1)
     got, _ = sp.sp_attention(S, p.Q.to(DEV), p.K[:, :1].contiguous().to(DEV).expand(-1, 4, -1), p.V[:, :1].contiguous().to(DEV).expand(-1, 4, -1), **o)
     check({"O": got}, {"O": reference(p, False)["O"]}, "expanded")
+
+
+def test_decoding_steps_over_caches_from_one_recorded_graph():
+    """Serving: a pattern with room for 40 tokens of each sequence is packed once; a recorded step appends a key and value where its positions
+    say and attends with bias and causal.  The caches' free places hold NaN.  Then cross attention to states of another length."""
+    B, room, H, Hk, D = 3, 40, 4, 2, 32
+    g = torch.Generator().manual_seed(4)
+    lens = torch.tensor([5, 0, 30])
+    own, cross = ragged([1] * B, [room] * B), ragged([1] * B, [17, 60, 9])
+    S, X = (sp.sp_prepare_attention(pack(a)) for a in (own, cross))
+    bias = torch.randn(16, H, generator=g).to(BF16)
+    K, V = (torch.full((B * room, Hk, D), float("nan"), dtype=BF16) for _ in range(2))
+    for b in range(B):
+        for t in (K, V):
+            t[b * room:b * room + int(lens[b])] = torch.randn(int(lens[b]), Hk, D, generator=g).to(BF16)
+    states = [torch.randn(86, Hk, D, generator=g).to(BF16) for _ in range(2)]
+    kpos = torch.arange(room, dtype=torch.int32).repeat(B)
+    dev = dict(K=K.to(DEV), V=V.to(DEV), q=torch.zeros(B, H, D, dtype=BF16, device=DEV), k=torch.zeros(B, Hk, D, dtype=BF16, device=DEV),
+               v=torch.zeros(B, Hk, D, dtype=BF16, device=DEV), pos=lens.int().to(DEV), kpos=kpos.to(DEV), bias=bias.to(DEV))
+    base = torch.arange(B, device=DEV) * room
+    SK, SV = (t.to(DEV) for t in states)
+
+    def step():
+        at = base + dev["pos"]
+        dev["K"].index_copy_(0, at, dev["k"])
+        dev["V"].index_copy_(0, at, dev["v"])
+        O, _ = sp.sp_attention(S, dev["q"], dev["K"], dev["V"], causal=True, qpos=dev["pos"], kpos=dev["kpos"], bias=dev["bias"], max_distance=20, bidirectional=False)
+        return O, sp.sp_attention(X, O, SK, SV)[0]
+    saved = dev["K"].clone(), dev["V"].clone()
+    step()                                               # warm, then as it was
+    dev["K"].copy_(saved[0]); dev["V"].copy_(saved[1])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        O, Y = step()
+    dev["K"].copy_(saved[0]); dev["V"].copy_(saved[1])
+    for n in range(6):
+        q, k, v = torch.randn(B, H, D, generator=g).to(BF16), torch.randn(B, Hk, D, generator=g).to(BF16), torch.randn(B, Hk, D, generator=g).to(BF16)
+        for name, t in (("q", q), ("k", k), ("v", v)):
+            dev[name].copy_(t)
+        dev["pos"].copy_(lens.int() + n)
+        graph.replay()
+        torch.cuda.synchronize()
+        for b in range(B):
+            K[b * room + int(lens[b]) + n], V[b * room + int(lens[b]) + n] = k[b], v[b]
+        p = Problem(own, q, torch.nan_to_num(K), torch.nan_to_num(V), causal=True, qpos=lens.int() + n, kpos=kpos, bias=bias, max_distance=20, bidirectional=False)
+        check({"O": O}, {"O": reference(p, False)["O"]}, "step %d" % n)
+        check({"O": Y}, {"O": reference(Problem(cross, O.cpu(), *states), False)["O"]}, "step %d, cross" % n)
 
 
 def test_offsets_beyond_32_bits():
