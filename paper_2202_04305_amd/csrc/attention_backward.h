@@ -58,7 +58,8 @@ __device__ __forceinline__ void attn_add_by_bucket(attn_lds_f32 *hist, int lane,
 // (Atomic adds to LDS take a cycle a lane, 64 for an instruction: 273 us for 16 sequences of 512, 12 heads, instead of 94.)
 // `exact`: the terms are p dP and p, and ds = p (dP - D) is made of the sums with each row's D = sum p dP.  A bucket's ds almost
 // cancel, and D from an O that was rounded to 16 bits would be most of their error (2.4e-3 of the gradient instead of 1.7e-3, the
-// rounding of the result).  Not exact (f32, whose O is not rounded): the terms are ds.
+// rounding of the result).  Not exact: the terms are ds.  That is f32, whose O is not rounded, and 16-bit types where rows are cut or the
+// sums do not fit the LDS: D takes O's rounding there.  Either way the order of the sums is fixed.
 template <typename T, int DT, int WM, int WN, int KW, bool POS>
 __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void dq_kernel(grad_args f)
 {
