@@ -186,7 +186,7 @@ typedef struct sp_attention_problem {
     int headDim;                        /* 1 .. 256; f32: 1 .. 128                                                       */
     int causal;                         /* 1: only keys with kpos[j] <= qpos[i]                                          */
     int buckets, maxDistance, bidirectional;
-    double scale;
+    double scale;                       /* scale / ln 2 has to be finite in f32                                          */
     const void *Q; int64_t ldq, hdq;    /* DEVICE: element (i, h, d) at Q[i * ldq + h * hdq + d]; strides >= 0           */
     const void *K; int64_t ldk, hdk;    /* DEVICE: element (j, g, d) at K[j * ldk + g * hdk + d]                         */
     const void *V; int64_t ldv, hdv;

@@ -71,7 +71,8 @@ static sp_status check_problem(const sp_tensor *S, const sp_attention_problem *p
         if (side < 2 || (p->bidirectional && p->buckets % 2) || p->maxDistance <= side / 2 || p->maxDistance > 4096 || p->ldt < p->heads) return SP_ERR_SHAPE;
     }
     for (int64_t s : {p->ldq, p->hdq, p->ldk, p->hdk, p->ldv, p->hdv}) if (s < 0) return SP_ERR_SHAPE;
-    if (!(p->scale - p->scale == 0)) return SP_ERR_SHAPE;            // not finite
+    const float c = (float)(p->scale * 1.4426950408889634);
+    if (!(c - c == 0)) return SP_ERR_SHAPE;                          // the kernels hold it in 32 bits: not finite there
     if (S->enc.perm[0] != 0 || S->enc.lt[1] != SP_COMPRESSED || !S->attention[0] || (grad && !S->attention[1])) return SP_ERR_UNSUPPORTED;
     memset(a, 0, sizeof(*a));
     a->Q = p->Q; a->K = p->K; a->V = p->V; a->table = p->table;
@@ -79,7 +80,7 @@ static sp_status check_problem(const sp_tensor *S, const sp_attention_problem *p
     a->qpos = p->qpos; a->kpos = p->kpos;
     a->m = S->shape[0]; a->n = S->shape[1];
     a->D = p->headDim; a->H = p->heads; a->Hk = p->kvHeads; a->G = p->heads / p->kvHeads;
-    a->scale = (float)p->scale; a->c = (float)(p->scale * 1.4426950408889634);
+    a->scale = (float)p->scale; a->c = c;
     a->buckets = p->buckets; a->bidirectional = p->bidirectional; a->causal = p->causal;
     if (p->buckets) make_borders(p, a);
     return SP_OK;

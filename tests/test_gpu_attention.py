@@ -627,3 +627,15 @@ def test_inspector_out_of_memory_leaves_nothing_behind():
     check(run(S, p), reference(p))
     S.free()
     assert len(alloc.live) == 0 and held > 0
+
+
+@pytest.mark.parametrize("scale", [float("inf"), 3e38, -3e38, 1e300])
+def test_scales_without_a_32_bit_value_are_refused(scale):
+    """The kernels hold the scale, and its product with log2 e, in 32 bits; the largest of either is 3.4e38."""
+    at = torch.ones(6, 8, dtype=torch.bool)
+    p = problem(at, 2, 2, 16, BF16)
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    Q, K, V, dO = (t.to(DEV) for t in (p.Q, p.K, p.V, p.dO))
+    O, lse = sp.sp_attention(S, Q, K, V)
+    assert code(sp.sp_attention, S, Q, K, V, scale=scale) == 8
+    assert code(sp.sp_attention_grad, S, Q, K, V, O, lse, dO, scale=scale) == 8
