@@ -683,7 +683,9 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
     attn_args &a = f.a;
     const sp_attn_plan *rows = S->attention[0], *keys = S->attention[1];
     if (S->nvalues == 0) {                               // no pairs: zeros, and nothing of the problem is read
-        if (f.part_table) hipLaunchKernelGGL(table_kernel<T>, dim3((unsigned)(a.buckets * a.H)), dim3(kThreads), 0, st, f, (int64_t)0);
+        // (by dTable: without rows the workspace has no bytes, and its parts no addresses)
+        if (a.buckets && f.g.dTable) hipLaunchKernelGGL(table_kernel<T>, dim3((unsigned)(a.buckets * a.H)), dim3(kThreads), 0, st, f, (int64_t)0);
+        SP_HIP(hipGetLastError());
         f.part_table = nullptr;
         a.buckets = a.causal = 0;
     }
