@@ -194,7 +194,8 @@ __device__ __forceinline__ bool attn_any_number(const float (&x)[kAttnPer], int 
     return __builtin_amdgcn_ballot_w64(any) != 0;
 }
 
-// top (running maximum), total and acc = sum of e^(s - top) V over a stretch of a row's columns
+// top (running maximum), total and acc = sum of e^(s - top) V over a stretch of a row's columns.  Values that are not numbers spoil acc
+// alone: top and total (lse) go on to the row's end, as the gradients of the row's other keys are weighted by them.
 template <typename T>
 __device__ __forceinline__ void attn_row_forward(const attn_args &a, const attn_plan_view &p, int64_t b, int r, int c0, int c1, int64_t i, int h,
                                                  int lane, float &top, float &total, float (&acc)[kAttnPer])
@@ -203,6 +204,7 @@ __device__ __forceinline__ void attn_row_forward(const attn_args &a, const attn_
     float q[kAttnPer];
     attn_load_row((const T *)a.Q + i * a.ldq + h * a.hdq, a.D, lane, q);
     top = -INFINITY; total = 0;
+    bool sums = true;                                    // is any of acc still a number?
 #pragma unroll
     for (int k = 0; k < kAttnPer; ++k) acc[k] = 0;
     attn_for_columns(p, b, r, c0, c1, [&](int64_t j) {
@@ -211,14 +213,17 @@ __device__ __forceinline__ void attn_row_forward(const attn_args &a, const attn_
         attn_load_row((const T *)a.K + j * a.ldk + g * a.hdk, a.D, lane, x);
         const float s = attn_score<T>(a, attn_dot(q, x), i, j, h);
         if (s == -INFINITY) return true;                 // weight 0
-        attn_load_row((const T *)a.V + j * a.ldv + g * a.hdv, a.D, lane, x);
+        if (sums) attn_load_row((const T *)a.V + j * a.ldv + g * a.hdv, a.D, lane, x);
         const float up = s > top ? s : top;              // not a number: stays with the old maximum, the weight carries it
         const float old = top == -INFINITY ? 0.f : attn_weight(top, up), w = attn_weight(s, up == -INFINITY ? 0.f : up);
         top = up;
         total = total * old + w;
+        if (sums) {
 #pragma unroll
-        for (int k = 0; k < kAttnPer; ++k) acc[k] = acc[k] * old + w * x[k];
-        return attn_any_number(acc, a.D, lane);
+            for (int k = 0; k < kAttnPer; ++k) acc[k] = acc[k] * old + w * x[k];
+            sums = attn_any_number(acc, a.D, lane);
+        }
+        return sums || total == total;
     });
 }
 

@@ -35,3 +35,32 @@ def test_gradients_without_pairs_are_zeros(m, n, dt, poisoned):
         for k in ("dQ", "dK", "dV") + (("dT",) if buckets else ()):
             assert got[k].shape == {"dQ": (m, 2, 16), "dK": (n, 1, 16), "dV": (n, 1, 16), "dT": (8, 2)}[k]
             assert not got[k].any(), (k, got[k])
+
+
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("part", ["all numbers", "some numbers"])
+@pytest.mark.parametrize("name", ["band", "sparse", "half", "ragged batch", "tokens behind a prefix", "one row", "cut rows"])
+def test_values_that_are_not_numbers_leave_lse_and_dv_right(name, part, dt):
+    """lse does not depend on V, and dV = p^T dO not on V either: a V of NaN (its K is a number) spoils O and the gradients that the formula
+    takes from it, and the other numbers of a head's O stay right where only some of V's are spoiled."""
+    at = torch.cat([torch.ones(24, 3000, dtype=torch.bool), ragged([1] * 24, [40] * 24)], 1) if name == "cut rows" else PATTERNS[name]()
+    p = problem(at, 2, 1, 64, dt)
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    cols = at.any(0).nonzero().flatten()
+    col = int(cols[len(cols) // 3])
+    say("case", name, part, dt, "column", col)
+    spoiled = torch.ones(64, dtype=torch.bool) if part == "all numbers" else torch.arange(64) % 5 == 0
+    was = p.V[col].clone()
+    p.V[col, :, spoiled] = float("nan")
+    got = run(S, p)
+    p.V[col] = was
+    ref = reference(p)
+    check({k: got[k] for k in ("lse", "dV")}, {k: ref[k] for k in ("lse", "dV")}, name)
+    rows = at[:, col]
+    nan = torch.isnan(got["O"].cpu())
+    assert bool((nan == (rows[:, None, None] & spoiled)).all())
+    check({"O": got["O"][:, :, (~spoiled).to(DEV)]}, {"O": tuple(t[:, :, ~spoiled] for t in ref["O"])}, name)
+    clean, far = ~rows, ~at[rows].any(0)                 # rows without it, and the keys that none of the others has
+    check({"dQ": got["dQ"][clean.to(DEV)], "dK": got["dK"][far.to(DEV)]},
+          {"dQ": tuple(t[clean] for t in ref["dQ"]), "dK": tuple(t[far] for t in ref["dK"])}, name)
+    assert bool(torch.isnan(got["dQ"][rows.to(DEV)]).all()) and bool(torch.isnan(got["dK"][at[rows].any(0).to(DEV)]).all())
