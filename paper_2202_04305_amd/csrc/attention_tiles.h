@@ -204,10 +204,12 @@ struct attn_item {
 // 4096 keys, 16 heads of 128: 600 us instead of 419.)  A wave's instruction fills 64 consecutive granules of LDS, so the granules' exchange
 // (attn_tile::place) is made by which granule of memory each lane asks for.  Rows that nobody attends to and numbers past D are
 // left out; the place was zeroed once.  Inline assembly, because for the compiler's own form of this load every later read of LDS waits
-// for it; it has no destination register, and arrive() waits for it before anybody reads.
+// for it; it has no destination register, and arrive() waits for it before anybody reads.  The place in LDS is an operand in m0, which the
+// compiler so knows the contents of (a write to m0 that the assembly only lists as clobbered need not be preserved); the load may
+// follow a write to m0 after one cycle at the earliest.
 __device__ __forceinline__ void attn_to_lds(const void *from, unsigned to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory", "m0");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(to), "v"(from) : "memory");
 }
 // CAUSAL rows that nobody attends to are not read either, so that what lies in a cache's free places does not matter.  ONE: keep each
 // step's columns, one a thread (for positions, and what else belongs to a column).
