@@ -226,6 +226,8 @@ sp_status sp_attention(const sp_tensor *S, const sp_attention_problem *p, void *
  *     dQ[i,h] = scale sum_j ds[i,j] K[j,g],   dK[j,g] = scale sum_{h of g} sum_i ds[i,j] Q[i,h],
  *     dTable[b,h] = sum over the pairs (i,j) of bucket b of ds[i,j]
  * O and lse are sp_attention's; the gradients are overwritten (rows and columns without pairs become zero).  dTable may be NULL.
+ * A row's weights p sum to 1 also where a bias puts lse so far from zero that its 32 bits have no room for the logarithm of their
+ * number (a row of nothing but the type's lowest value weighs all its keys alike).
  * S must have been prepared with grad = 1.  Workspace, streams and reproducibility as for sp_attention. */
 typedef struct sp_attention_grads {
     const void *O; int64_t ldo, hdo;

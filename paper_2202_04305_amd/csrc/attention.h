@@ -183,6 +183,13 @@ __device__ __forceinline__ float attn_score(const attn_args &a, float dot, int64
     return s;
 }
 __device__ __forceinline__ float attn_weight(float s, float top) { return __builtin_amdgcn_exp2f((s - top) * kLog2e); }
+// The same in the gradients, where log_sum is log2 of what the row's weights e^(s - lse) sum to (see attn_log_sum).  That is of the tiles' scores;
+// one that is made pair by pair may round to another step, and its weight stays at 1 then.
+__device__ __forceinline__ float attn_weight(float s, float lse, float log_sum)
+{
+    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s - lse, kLog2e, -log_sum));
+    return log_sum != 0 && w > 1.f ? 1.f : w;
+}
 __device__ __forceinline__ bool attn_left_out(const attn_args &a, int64_t i, int64_t j) { return a.causal && a.kpos[j] > a.qpos[i]; }
 
 // Is any of a row's D sums still a number?  (What is not a number stays so, and a row of nothing else is done.)
@@ -230,7 +237,7 @@ __device__ __forceinline__ void attn_row_forward(const attn_args &a, const attn_
 // sum over the stretch of ds K (not yet scaled)
 template <typename T>
 __device__ __forceinline__ void attn_row_dq(const attn_args &a, const attn_plan_view &p, int64_t b, int r, int c0, int c1, int64_t i, int h, int lane,
-                                            const T *dO, float lse, float delta, float (&acc)[kAttnPer])
+                                            const T *dO, float lse, float delta, float log_sum, float (&acc)[kAttnPer])
 {
     const int g = h / a.G;
     float q[kAttnPer], go[kAttnPer];
@@ -246,7 +253,7 @@ __device__ __forceinline__ void attn_row_dq(const attn_args &a, const attn_plan_
         attn_load_row((const T *)a.V + j * a.ldv + g * a.hdv, a.D, lane, y);
         const float s = attn_score<T>(a, attn_dot(q, x), i, j, h);
         if (s == -INFINITY) return true;
-        const float ds = attn_weight(s, lse) * (attn_dot(go, y) - delta);
+        const float ds = attn_weight(s, lse, log_sum) * (attn_dot(go, y) - delta);
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) acc[k] += ds * x[k];
         return attn_any_number(acc, a.D, lane);
@@ -257,7 +264,7 @@ __device__ __forceinline__ void attn_row_dq(const attn_args &a, const attn_plan_
 // p: the plan of the transposed pattern
 template <typename T>
 __device__ __forceinline__ void attn_row_dkv(const attn_args &a, const attn_plan_view &p, int64_t b, int r, int c0, int c1, int64_t j, int h, int lane,
-                                             const T *dO, int64_t lddo, int64_t hddo, const float *lse, const float *delta,
+                                             const T *dO, int64_t lddo, int64_t hddo, const float *lse, const float *delta, const float *log_sum,
                                              float (&dk)[kAttnPer], float (&dv)[kAttnPer])
 {
     const int g = h / a.G;
@@ -272,7 +279,7 @@ __device__ __forceinline__ void attn_row_dkv(const attn_args &a, const attn_plan
         const float s = attn_score<T>(a, attn_dot(kx, x), i, j, h);
         if (s == -INFINITY) return true;
         const float L = lse[h * a.m + i];
-        const float w = attn_weight(s, L == -INFINITY ? INFINITY : L);
+        const float w = attn_weight(s, L == -INFINITY ? INFINITY : L, log_sum ? log_sum[h * a.m + i] : 0.f);
         const float ds = w * (attn_dot(vx, y) - delta[h * a.m + i]);
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) { dk[k] += ds * x[k]; dv[k] += w * y[k]; }

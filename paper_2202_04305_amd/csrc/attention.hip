@@ -33,6 +33,7 @@ grad_choice choose(const sp_tensor *S, const attn_args &a, int size, bool table)
     const size_t p2 = c.keys_cut ? (size_t)keys->items[c.keys_level] * a.Hk * keys->br * 2 * padded(a.D) * 4 : 0;
     auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
     c.delta = up((size_t)a.m * a.H * 4);
+    c.log_sum = a.buckets ? c.delta : 0;
     c.part = up(p1 > p2 ? p1 : p2);
     c.table = up(table ? (size_t)rows->items[c.rows.level] * a.H * a.buckets * 4 : 0);
     return c;
@@ -95,7 +96,7 @@ extern "C" sp_status sp_attention_workspace(const sp_tensor *S, const sp_attenti
     if (grad) {
         for (int table = 0; table <= (a.buckets > 0); ++table) {         // with and without the table's gradient
             const grad_choice c = choose(S, a, p->dtype == SP_F32 ? 4 : 2, table != 0);
-            const size_t need = c.delta + c.part + c.table;
+            const size_t need = c.bytes();
             if (need > *bytes) *bytes = need;
         }
     } else {
@@ -157,14 +158,15 @@ extern "C" sp_status sp_attention_grad(const sp_tensor *S, const sp_attention_pr
     if (a.n > 0 && (!g->dK || !g->dV)) return SP_ERR_NULL;
     const int size = p->dtype == SP_F32 ? 4 : 2;
     const grad_choice c = choose(S, a, size, a.buckets && g->dTable);
-    const size_t need = c.delta + c.part + c.table;
+    const size_t need = c.bytes();
     if (need > 0 && !workspace) return SP_ERR_NULL;
     if (need > workspaceBytes || ((uintptr_t)workspace & 255)) return SP_ERR_SHAPE;
     f.g = *g;
     f.pd = padded(a.D); f.exact = c.exact;
     f.delta = (float *)workspace;
-    f.part = (float *)((char *)workspace + c.delta);
-    if (a.buckets && g->dTable) f.part_table = (float *)((char *)workspace + c.delta + c.part);
+    if (a.buckets) f.log_sum = (float *)((char *)workspace + c.delta);
+    f.part = (float *)((char *)workspace + c.delta + c.log_sum);
+    if (a.buckets && g->dTable) f.part_table = (float *)((char *)f.part + c.part);
     attn_alignment rows(a.D, size);
     rows.with(a.Q, a.ldq, a.hdq); rows.with(a.K, a.ldk, a.hdk); rows.with(a.V, a.ldv, a.hdv);
     rows.with(g->O, g->ldo, g->hdo); rows.with(g->dO, g->lddo, g->hddo);

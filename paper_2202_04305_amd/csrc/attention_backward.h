@@ -48,6 +48,43 @@ __device__ __forceinline__ void attn_add_by_bucket(attn_lds_f32 *hist, int lane,
     }
 }
 
+// log2 of what the weights e^(s - lse) of a lane's whole row sum to.  lse = top + log(total) is rounded to 32 bits, and far from zero that
+// takes the logarithm from it: of n scores of -3.4e38 (a bias of a type's lowest value) every weight would be 1, not 1 / n.  Up to kAttnNearLse
+// the rounding changes a weight by less than 2^-14 and is left alone (0); for tiles with a row beyond, the row's scores are made once more
+// here, by the same instructions in the same order as in the kernels' tiles, so the same bits.  (Where the steps of a score are 64 wide, one
+// that rounds to another step weighs e^64.)  Rows of K come straight from memory, a lane's as it needs them: such tiles are few.
+constexpr float kAttnNearLse = 1024;
+template <typename T, int DT>
+__device__ __forceinline__ float attn_log_sum(const grad_args &f, const attn_item &item, const attn_lane &me, const typename attn_tile<T, DT>::frag (&q)[attn_tile<T, DT>::kSteps],
+                                              int qp, float lse, int lane)
+{
+    typedef attn_tile<T, DT> tile;
+    const attn_args &a = f.a;
+    const attn_plan_view &p = f.p;
+    const T *Kh = (const T *)a.K + (int64_t)me.kv * a.hdk;
+    float sum = 0;
+    for (int chunk = item.chunk0; chunk < p.chunk0[item.block + 1]; ++chunk) {
+        const uint64_t word = item.word(p, chunk, me.r);
+        for (int t = 0; t < 2; ++t) {
+            const int64_t x0 = (int64_t)(chunk - item.chunk0) * kAttnChunk + 32 * t;
+            const T *row = Kh + item.cols.get(x0 + (lane & 31)) * a.ldk;
+            attn_f32x16 s = (attn_f32x16)(0.f);
+#pragma unroll
+            for (int k = 0; k < tile::kSteps; ++k) s = attn_mma<T>::mul(tile::granule(row, (2 * k + (lane >> 5)) * tile::kPer, a.D, f.vec, true), q[k], s);
+            const uint32_t bits = (uint32_t)(word >> (32 * t)) >> (4 * (lane >> 5));
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const int kp = a.kpos[item.cols.get(x0 + 8 * (x >> 2) + 4 * (lane >> 5) + (x & 3))];
+                const float of = (float)((const T *)a.table)[(int64_t)attn_bucket(a, attn_distance(kp, qp)) * a.ldt + me.head];
+                const bool there = bits >> (8 * (x >> 2) + (x & 3)) & 1 && !(a.causal && kp > qp);
+                sum += there ? attn_weight(__builtin_fmaf(s[x], a.scale, of), lse) : 0.f;
+            }
+        }
+    }
+    sum = attn_pair_sum(sum);
+    return me.valid && fabsf(lse) >= kAttnNearLse && sum > 0 ? __builtin_amdgcn_logf(sum) : 0.f;
+}
+
 // dQ: the forward kernel's frame (items, gathered columns through LDS, tiles of 32 rows), with dO beside Q and V read as K is.
 //
 // 16 sequences of 256 to 512 queries over 512 to 1024 keys, 12 heads of 64, bf16: 47 us, 460 TFLOP/s for three products; bound by the
@@ -100,7 +137,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         }
         delta = attn_pair_sum(delta);
     }
-    float rest = 0;                                      // sum of ds over the row's pairs
+    float rest = 0, log_sum = 0;                         // sum of ds over the row's pairs; log2 of that of its weights
     int qp = 0, q_lo = 0, q_hi = 0;
     attn_bias bias = {};
     attn_lds_f32 *hist = nullptr;                             // [buckets][64] of ds; exact: of p dP and p
@@ -110,6 +147,8 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     if (POS) {
         if (a.qpos) { qp = a.qpos[me.row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
         if (a.buckets) {
+            if (__builtin_amdgcn_ballot_w64(me.valid && fabsf(off) >= kAttnNearLse && off - off == 0) != 0)
+                log_sum = attn_log_sum<T, DT>(f, item, me, q, qp, off, lane);
             bias = attn_lane_bias<T>(a, (attn_lds *)lds + 4 * KT * tile::kRow + 2 * KT * 4, f.mode, group, lane, wave, WM);
             if (f.part_table) {
                 hist = bias.table + (((places << bias.shift) + 3) & ~3) + wave * hist_size;
@@ -220,7 +259,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
                 float sum_x = 0, sum_p = 0, term[16], weight[16];
 #pragma unroll
                 for (int x = 0; x < 16; ++x) {
-                    weight[x] = attn_where(there, x, __builtin_amdgcn_exp2f((s[x] - off) * cc));
+                    weight[x] = attn_where(there, x, __builtin_amdgcn_exp2f(__builtin_fmaf(s[x] - off, cc, -log_sum)));
                     s[x] = attn_where(there, x, weight[x] * (dp[x] - delta));
                     term[x] = attn_where(there, x, weight[x] * (dp[x] - of_term));
                     sum_x += term[x]; sum_p += weight[x];
@@ -248,7 +287,10 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     // For dkv_kernel.  The weights of a row that is whole here sum to 1, so what its ds miss to sum to 0 is the error of a D made of an O
     // that was rounded to 16 bits.
     rest = sizeof(T) == 2 && item.whole ? attn_pair_sum(rest) : 0.f;
-    if (WN == 1 && me.valid && lane < 32 && item.c0 == item.chunk0) f.delta[me.head * a.m + me.row] = delta + rest;
+    if (WN == 1 && me.valid && lane < 32 && item.c0 == item.chunk0) {
+        f.delta[me.head * a.m + me.row] = delta + rest;
+        if (POS && f.log_sum) f.log_sum[me.head * a.m + me.row] = log_sum;
+    }
     float odd = 0;
 #pragma unroll
     for (int x = 0; x < tile::kBlocks; ++x)
@@ -340,12 +382,15 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         float any = 0, more = 0;
 #pragma unroll
         for (int x = 0; x < WN; ++x) { any += bad[x * 32 + mine]; more += bad[(WN + x) * 32 + mine]; }
-        const float delta2 = __shfl(delta, mine, 64);
+        const float delta2 = __shfl(delta, mine, 64), log_sum2 = POS ? __shfl(log_sum, mine, 64) : 0.f;
         const int64_t row2 = ((int64_t)__shfl((int)(me.row >> 32), mine, 64) << 32) | (uint32_t)__shfl((int)me.row, mine, 64);
         const int head2 = __shfl(me.head, mine, 64), r2 = __shfl(r, mine, 64);
         const bool valid2 = __shfl((int)me.valid, mine, 64) != 0;
         const int64_t place2 = (item.part * a.H + head2) * p.br + r2;
-        if (valid2 && part == 0 && item.c0 == item.chunk0) f.delta[head2 * a.m + row2] = delta2 + more;
+        if (valid2 && part == 0 && item.c0 == item.chunk0) {
+            f.delta[head2 * a.m + row2] = delta2 + more;
+            if (POS && f.log_sum) f.log_sum[head2 * a.m + row2] = log_sum2;
+        }
         if (valid2 && any == 0) {
 #pragma unroll
             for (int k = 0; k < EACH; k += 4) {
@@ -370,7 +415,8 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         const int h = __builtin_amdgcn_readlane(me.head, x), rr = __builtin_amdgcn_readlane(r, x);
         float one[kAttnPer];
         attn_row_dq<T>(a, p, item.block, rr, item.c0, item.c1, i, h, lane, (const T *)f.g.dO + i * f.g.lddo + h * f.g.hddo, f.g.lse[h * a.m + i],
-                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(delta), x)), one);
+                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(delta), x)), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(log_sum), x)),
+                       one);
         const int64_t at1 = (item.part * a.H + h) * p.br + rr;
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) {
@@ -400,9 +446,10 @@ __global__ __launch_bounds__(64 * WM, attn_dkv_alone(DT * (int)sizeof(T), POS) ?
     constexpr int NT = 64 * WM, KT = KW, TILES = KW / 32, SUB = kAttnChunk / KT;
     static_assert(KT <= kAttnChunk, "steps within a chunk");
     extern __shared__ __align__(1024) char lds[];
-    // behind Q and dO, two places of everything: lse, D and positions of a step's queries, the bias of a head
+    // behind Q and dO, two places of everything: lse and D, with POS positions and attn_log_sum of a step's queries, the bias of a head
     attn_lds_f32 *s_lse = (attn_lds_f32 *)((attn_lds *)lds + 4 * KT * tile::kRow), *s_delta = s_lse + 2 * KT;
     attn_lds_i32 *s_qpos = (attn_lds_i32 *)(s_delta + 2 * KT);
+    attn_lds_f32 *s_log = (attn_lds_f32 *)(s_qpos + 2 * KT);
     const attn_args &a = f.a;
     const attn_plan_view &p = f.p;                       // of the transposed pattern: rows are keys
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -423,7 +470,7 @@ __global__ __launch_bounds__(64 * WM, attn_dkv_alone(DT * (int)sizeof(T), POS) ?
         if (a.kpos) { kp = a.kpos[key]; k_lo = attn_wave_min(kp); k_hi = attn_wave_max(kp); }
         if (a.buckets) {
             // a slot for even heads and one for odd ones: the head at hand and the next
-            bias = attn_make_bias<T>(a, (attn_lds *)(s_qpos + 2 * KT), 1, [&](int s) {
+            bias = attn_make_bias<T>(a, (attn_lds *)(s_log + 2 * KT), 1, [&](int s) {
                 const int x = (s ^ kv * a.G) & 1;
                 return x < a.G ? kv * a.G + x : -1;
             });
@@ -448,7 +495,7 @@ __global__ __launch_bounds__(64 * WM, attn_dkv_alone(DT * (int)sizeof(T), POS) ?
         for (int w = 0; w < WM; ++w) ring.limit = s_qpos[w] < ring.limit ? s_qpos[w] : ring.limit;
     }
     if (POS || a.D != DT) __syncthreads();
-    float lse_next = 0, delta_next = 0;
+    float lse_next = 0, delta_next = 0, log_next = 0;
     uint64_t word = 0, word_next = 0;
     int state = 0, state_next = 0;
     // a step: the head and the step among the head's
@@ -463,6 +510,7 @@ __global__ __launch_bounds__(64 * WM, attn_dkv_alone(DT * (int)sizeof(T), POS) ?
         if (tid < KT) {
             lse_next = f.g.lse[x.h * a.m + ring.one];
             delta_next = f.delta[x.h * a.m + ring.one];
+            if (POS && f.log_sum) log_next = f.log_sum[x.h * a.m + ring.one];
         }
     };
     auto rows = [&](int64_t s, place x) { ring.rows(s, (const T *)a.Q + x.h * a.hdq, (const T *)f.g.dO + x.h * f.g.hddo); };
@@ -480,7 +528,7 @@ __global__ __launch_bounds__(64 * WM, attn_dkv_alone(DT * (int)sizeof(T), POS) ?
         if (tid < KT) {
             s_lse[here + tid] = lse_next == -INFINITY ? INFINITY : POS ? lse_next : lse_next * kLog2e;     // no weight left
             s_delta[here + tid] = delta_next;
-            if (POS) s_qpos[here + tid] = ring.kp_one;
+            if (POS) { s_qpos[here + tid] = ring.kp_one; s_log[here + tid] = log_next; }
         }
         if (POS && a.buckets && now.at == 0) {           // the slot of the head before the last is free
             bias.slot = now.h & 1;
@@ -536,10 +584,11 @@ __global__ __launch_bounds__(64 * WM, attn_dkv_alone(DT * (int)sizeof(T), POS) ?
             for (int b = 0; b < 4; ++b) {
                 const int q0 = here + 32 * t + 8 * b + 4 * (lane >> 5);
                 const attn_f32x4 lse = *(const attn_lds_f32x4 *)(s_lse + q0), delta = *(const attn_lds_f32x4 *)(s_delta + q0);
+                const attn_f32x4 log_sum = POS ? *(const attn_lds_f32x4 *)(s_log + q0) : (attn_f32x4)(0.f);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const int x = 4 * b + c;
-                    s[x] = __builtin_amdgcn_exp2f(POS ? (s[x] - lse[c]) * cc : __builtin_fmaf(s[x], cc, -lse[c]));
+                    s[x] = __builtin_amdgcn_exp2f(POS ? __builtin_fmaf(s[x] - lse[c], cc, -log_sum[c]) : __builtin_fmaf(s[x], cc, -lse[c]));
                     dp[x] = s[x] * (dp[x] - delta[c]);
                 }
             }
@@ -585,7 +634,7 @@ __global__ __launch_bounds__(64 * WM, attn_dkv_alone(DT * (int)sizeof(T), POS) ?
         const int rr = __builtin_amdgcn_readlane(r, x);
         float k1[kAttnPer] = {0}, v1[kAttnPer] = {0};
         for (int g = kv * a.G; g < (kv + 1) * a.G; ++g)
-            attn_row_dkv<T>(a, p, item.block, rr, item.c0, item.c1, j, g, lane, (const T *)f.g.dO, f.g.lddo, f.g.hddo, f.g.lse, f.delta, k1, v1);
+            attn_row_dkv<T>(a, p, item.block, rr, item.c0, item.c1, j, g, lane, (const T *)f.g.dO, f.g.lddo, f.g.hddo, f.g.lse, f.delta, POS ? f.log_sum : nullptr, k1, v1);
         float *part = f.part + ((item.part * a.Hk + kv) * p.br + rr) * 2 * f.pd;
 #pragma unroll
         for (int k = 0; k < kAttnPer; ++k) {
@@ -672,7 +721,7 @@ template <typename T, int DT, bool POS>
 sp_status launch_dkv_mode(const grad_args &f, int br, int64_t items, hipStream_t st)
 {
     constexpr int KW = sizeof(T) == 2 && (DT <= 64 || (DT == 128 && POS)) ? 64 : 32;
-    const size_t lds = 4 * (size_t)KW * DT * sizeof(T) + KW * 24 + (POS ? attn_bias_bytes(f.a, 2) : 0);
+    const size_t lds = 4 * (size_t)KW * DT * sizeof(T) + KW * (POS ? 32 : 16) + (POS ? attn_bias_bytes(f.a, 2) : 0);
     if (br == 128) return launch(dkv_kernel<T, DT, 4, KW, POS>, f, items * f.a.Hk, 256, lds, st);
     return launch(dkv_kernel<T, DT, 1, KW, POS>, f, items * f.a.Hk, 64, lds, st);
 }

@@ -531,6 +531,7 @@ struct grad_args {
     attn_plan_view p;
     sp_attention_grads g;
     float *delta;                        // [heads][m]: D of every row, made by dq_kernel
+    float *log_sum;                      // with a bias, [heads][m]: attn_log_sum of every row, made by dq_kernel
     float *part;                         // of rows (keys) that are cut: dq [item][head][row of the block][pd]; dkv [item][kv head][key][2][pd]
     float *part_table;                   // [item][head][buckets]
     int groups, mode, vec, pd;
@@ -542,7 +543,8 @@ struct grad_choice {
     bool exact;
     int keys_level;
     bool keys_cut;
-    size_t delta, part, table;           // bytes; the parts of dQ and of dK, dV use the same place one after the other
+    size_t delta, log_sum, part, table;  // bytes; the parts of dQ and of dK, dV use the same place one after the other
+    size_t bytes() const { return delta + log_sum + part + table; }
 };
 template <typename T>
 sp_status attn_backward(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStream_t st);

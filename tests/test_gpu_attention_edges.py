@@ -64,3 +64,99 @@ def test_values_that_are_not_numbers_leave_lse_and_dv_right(name, part, dt):
     check({"dQ": got["dQ"][clean.to(DEV)], "dK": got["dK"][far.to(DEV)]},
           {"dQ": tuple(t[clean] for t in ref["dQ"]), "dK": tuple(t[far] for t in ref["dK"])}, name)
     assert bool(torch.isnan(got["dQ"][rows.to(DEV)]).all()) and bool(torch.isnan(got["dK"][at[rows].any(0).to(DEV)]).all())
+
+
+LOWEST = [(F16, -2048.0), (F16, -65504.0), (F32, -65504.0), (BF16, -65504.0), (BF16, -1e7), (F32, -1e8), (F32, -1e9), (BF16, -1e9), (F32, torch.finfo(F32).min),
+          (BF16, torch.finfo(BF16).min)]
+
+
+def far_below(at, H, Hk, D, dt, low, rows, seed=0):
+    """A problem whose bucket 0 holds `low`, of which `rows` have nothing else, and what has to come out of it.  All scores are the bias
+    alone (Q and K have no number in common that is not zero), so they are exact in 32 bits, and what a row of equal scores weighs does not
+    depend on them: those rows are taken with a bias of 0, the others without the pairs of bucket 0, whose weight e^low is 0."""
+    m, n = at.shape
+    kpos = torch.tensor([10, 8, 6, 2])[torch.arange(n) % 4]
+    qpos = torch.full((m,), 9)                           # distances of 1, -1, -3, -7: buckets 0 to 3
+    qpos[rows] = 1                                       # every key ahead: bucket 0
+    p = problem(at, H, Hk, D, dt, seed=seed, buckets=4, positions=(qpos, kpos), max_distance=8, bidirectional=False)
+    p.Q[:, :, D // 2:] = 0
+    p.K[:, :, :D // 2] = 0
+    p.bias[0] = low
+    ahead = (p.kpos[None, :] >= p.qpos[:, None])
+    whole = ~(at & ~ahead).any(1)                        # `rows`, and those of a few entries that all lie ahead
+    lowest, table = p.bias[0].clone(), p.bias
+    p.at, p.bias = at & whole[:, None], torch.zeros_like(table)
+    equal = reference(p)
+    p.at, p.bias = at & ~whole[:, None] & ~ahead, table
+    rest = reference(p)
+    p.at = at
+    ref = {k: tuple(a + b for a, b in zip(equal[k], rest[k])) for k in ("O", "dQ", "dK", "dV", "dT")}
+    lse, tol = (torch.where(whole[None, :], a, b) for a, b in zip(equal["lse"], rest["lse"]))
+    some = whole & at.any(1)
+    assert bool(some[rows].any())
+    lse[:, some] += lowest.double()[:, None]
+    tol[:, some] += 2.0 ** -24 * abs(low)
+    ref["lse"] = lse, tol
+    for k in ("O", "dQ", "dK", "dV"):                    # the bounds say something
+        assert float(ref[k][1].max()) <= 0.3 * float(ref[k][0].abs().max()), k
+    return p, ref
+
+
+@pytest.mark.parametrize("dt,low", LOWEST)
+@pytest.mark.parametrize("name", ["dense", "one row", "sparse", "tokens behind a prefix", "cut rows", "all rows"])
+@pytest.mark.parametrize("heads", [(2, 1), (6, 1), (40, 2)])
+def test_rows_of_nothing_but_the_lowest_bias_weigh_their_keys_alike(heads, name, dt, low):
+    """lse = low + log n is low in 32 bits, so weights e^(s - lse) are all 1 where they should be 1 / n."""
+    at = torch.ones(20, 3000, dtype=torch.bool) if name == "cut rows" else PATTERNS["dense" if name == "all rows" else name]()
+    rows = slice(None) if name in ("all rows", "one row") else [3, 4, 11]
+    p, ref = far_below(at, heads[0], heads[1], 32, dt, low, rows)
+    say("case", name, heads, dt, low)
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    check(run(S, p), ref, "%s %s" % (name, low))
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_rows_far_below_zero_from_a_recorded_graph(dt):
+    at = torch.ones(70, 900, dtype=torch.bool)
+    p, ref = far_below(at, 4, 2, 64, dt, float(torch.finfo(dt).min), [0, 33, 69])
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    o = p.options(DEV)
+    Q, K, V, dO = (t.to(DEV) for t in (p.Q, p.K, p.V, p.dO))
+    eager = run(S, p)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        O, lse = sp.sp_attention(S, Q, K, V, **o)
+        grads = sp.sp_attention_grad(S, Q, K, V, O, lse, dO, **o)
+    for rep in range(3):
+        for t in (O, lse) + grads:
+            t.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = dict(zip(("O", "lse", "dQ", "dK", "dV", "dT"), (O, lse) + grads))
+        check(got, ref, "replay %d" % rep)
+        for k, t in got.items():
+            assert torch.equal(t, eager[k]), k
+
+
+@pytest.mark.parametrize("low", [-3e3, -1e6, -1e7, -1e8, -1e9, 1e6, 1e8])
+@pytest.mark.parametrize("name", ["dense", "sparse", "tokens behind a prefix", "cut rows"])
+def test_weights_sum_to_one_where_scores_have_wide_steps(name, low):
+    """Products of any size beside a bias that leaves them few bits: which weights come out depends on how scores round, but each row's sum
+    to 1, so the rows of dV add up to those of dO.  A weight's exponent is at most 64 where it counts (2^-64 of the sum), rounded to 64 * 2^-24 of
+    the weight, once where the sum is made and once where the weight is; sums of n terms add n * 2^-24."""
+    at = torch.ones(20, 3000, dtype=torch.bool) if name == "cut rows" else PATTERNS[name]()
+    m, n = at.shape
+    p = problem(at, 2, 1, 32, F32, buckets=4, positions=(torch.arange(m), torch.arange(n)), max_distance=8, bidirectional=False)
+    p.Q, p.K = p.Q * 4, p.K * 4
+    p.bias[:] = low
+    say("case", name, low)
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    got = run(S, p)
+    there = at.any(1)
+    want, most = p.dO[there].double().sum((0, 1)), p.dO[there].double().abs().sum((0, 1))
+    tol = (2 * 64 + 2 * max(m, n) + 16) * 2.0 ** -24 * most
+    x = got["dV"].double().cpu().sum((0, 1))
+    assert bool(((x - want).abs() <= tol).all()), float(((x - want).abs() / tol).max())
+    assert bool(torch.isfinite(got["dQ"]).all()) and bool(torch.isfinite(got["dK"]).all())
