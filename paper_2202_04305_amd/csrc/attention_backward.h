@@ -322,7 +322,8 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         float *out = f.part_table + item.part * a.H * a.buckets;
         auto term = [&](int w, int b) {
             const attn_lds_f32 *x = all + w * hist_size + (b * 64 + lane) * (f.exact ? 2 : 1);
-            return f.exact ? x[0] - s_delta[(WN == 1 ? w : 0) * 32 + (lane & 31)] * x[1] : x[0];
+            // (a row without weight in the bucket adds nothing to it, whatever its D is)
+            return f.exact && x[1] != 0 ? x[0] - s_delta[(WN == 1 ? w : 0) * 32 + (lane & 31)] * x[1] : x[0];
         };
         for (int b = wave; b < places; b += WM * WN) {
             float sum = 0;

@@ -160,3 +160,24 @@ def test_weights_sum_to_one_where_scores_have_wide_steps(name, low):
     x = got["dV"].double().cpu().sum((0, 1))
     assert bool(((x - want).abs() <= tol).all()), float(((x - want).abs() / tol).max())
     assert bool(torch.isfinite(got["dQ"]).all()) and bool(torch.isfinite(got["dK"]).all())
+
+
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("name", ["dense", "sparse", "one row", "tokens behind a prefix"])
+def test_a_row_that_is_not_a_number_spoils_the_biases_of_its_own_distances_only(name, dt):
+    """dTable[b] sums over the pairs of bucket b: a row whose dO is NaN reaches the buckets that its pairs have."""
+    at = PATTERNS[name]()
+    m, n = at.shape
+    qpos, kpos = torch.arange(m) % 50, torch.arange(n) % 50
+    row = m // 2
+    qpos[row] = 2000                                     # all of its keys lie far behind: one bucket, the last of that side
+    p = problem(at, 2, 1, 32, dt, buckets=16, positions=(qpos, kpos), max_distance=100)
+    p.dO[row] = 0
+    ref = reference(p)
+    p.dO[row] = float("nan")
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    got = run(S, p)
+    others = torch.arange(16) != 7
+    check({"dT": got["dT"][others.to(DEV)]}, {"dT": tuple(t[others] for t in ref["dT"])}, name)
+    if at[row].any():
+        assert bool(torch.isnan(got["dT"][7]).all())
