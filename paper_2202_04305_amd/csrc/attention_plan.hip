@@ -273,8 +273,9 @@ struct plan_scope {
     sp_attn_plan *plan;
     explicit plan_scope(const sp_mem &m) : mem(m), plan(new sp_attn_plan()) { memset(plan, 0, sizeof(*plan)); }
     void *get(size_t bytes) {
-        void *p = mem.get((bytes + 255) & ~(size_t)255);
-        if (p) plan->bytes += (bytes + 255) & ~(size_t)255;
+        bytes = ((bytes ? bytes : 1) + 255) & ~(size_t)255;      // an allocator that is asked for nothing may give no address
+        void *p = mem.get(bytes);
+        if (p) plan->bytes += bytes;
         return p;
     }
     void drop() {

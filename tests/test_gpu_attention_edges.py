@@ -181,3 +181,25 @@ def test_a_row_that_is_not_a_number_spoils_the_biases_of_its_own_distances_only(
     check({"dT": got["dT"][others.to(DEV)]}, {"dT": tuple(t[others] for t in ref["dT"])}, name)
     if at[row].any():
         assert bool(torch.isnan(got["dT"][7]).all())
+
+
+class _DefaultAllocator:
+    """No callbacks: the library's own allocator."""
+    alloc_cb, free_cb = sp.binding._ALLOC_FN(), sp.binding._FREE_FN()
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("m,n,pairs", [(20, 30, 0), (1000, 30, 0), (0, 4, 0), (4, 0, 0), (0, 0, 0), (200, 100, 500), (1, 1, 1)])
+def test_default_allocator(m, n, pairs, grad):
+    """Nothing stored needs no chunks, and an allocator that is asked for no bytes gives no address."""
+    at = torch.zeros(m, n, dtype=torch.bool)
+    g = torch.Generator().manual_seed(6)
+    if pairs:
+        at[torch.randint(m, (pairs,), generator=g), torch.randint(n, (pairs,), generator=g)] = True
+    rows, cols = (t.to(DEV).contiguous() for t in at.nonzero(as_tuple=True))
+    S = sp.sp_pack(sp.sp_encode((0, 1), None, 32, 32), (m, n), [rows, cols], torch.zeros(rows.numel(), device=DEV), allocator=_DefaultAllocator())
+    sp.sp_prepare_attention(S, grad=grad)
+    p = problem(at, 2, 1, 16, F32)
+    check(run(S, p, grad), reference(p, grad))
+    torch.cuda.synchronize()
+    S.free()
