@@ -182,7 +182,7 @@ sp_status sp_sddmm(const sp_tensor *S, const void *A, int64_t lda, const void *B
  * e < maxDistance <= 4096. */
 typedef struct sp_attention_problem {
     int dtype;                          /* SP_F32, SP_F16 or SP_BF16: of Q, K, V, O, table and all gradients.  Sums are in f32. */
-    int heads, kvHeads;                 /* heads: a multiple of kvHeads                                                  */
+    int heads, kvHeads;                 /* heads: a multiple of kvHeads, at most 65535                                   */
     int headDim;                        /* 1 .. 256; f32: 1 .. 128                                                       */
     int causal;                         /* 1: only keys with kpos[j] <= qpos[i]                                          */
     int buckets, maxDistance, bidirectional;
@@ -216,7 +216,8 @@ sp_status sp_attention_workspace(const sp_tensor *S, const sp_attention_problem 
  * same bits on every call.  16-bit types: weights (and, for the gradients, ds) are rounded to the operands' type before the products they
  * are operands of, as every operand of the matrix cores is; f16 gradients below 2^-14 lose precision, as elsewhere (scale the loss).
  * Rows whose sums are not finite in the end are made again pair by pair, which takes longer.
- * Errors: NULL, RANK, DTYPE, SHAPE, UNSUPPORTED, TOO_LARGE (2^31 workgroups), HIP. */
+ * Errors: NULL, RANK, DTYPE, SHAPE, UNSUPPORTED, TOO_LARGE (2^32 threads of a launch: 2^24 workgroups, each of 128 rows or fewer and one head
+ * or a few), HIP.  A call that is refused has written nothing. */
 sp_status sp_attention(const sp_tensor *S, const sp_attention_problem *p, void *O, int64_t ldo, int64_t hdo, float *lse,
                        void *workspace, size_t workspaceBytes, void *stream);
 

@@ -44,6 +44,8 @@ struct sp_attn_plan {
 };
 
 static inline __host__ __device__ int attn_level_chunks(int level) { return 1 << level; }
+// A launch has fewer than 2^32 threads along a direction.
+static inline bool attn_launches(int64_t groups, int threads) { return groups < ((int64_t)1 << 31) && groups * threads < ((int64_t)1 << 32); }
 
 // A plan at one level, as kernels take it.
 struct attn_plan_view {

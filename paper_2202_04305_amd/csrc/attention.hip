@@ -133,7 +133,7 @@ extern "C" sp_status sp_attention(const sp_tensor *S, const sp_attention_problem
     attn_alignment rows(a.D, size);
     rows.with(a.Q, a.ldq, a.hdq); rows.with(a.K, a.ldk, a.hdk); rows.with(a.V, a.ldv, a.hdv); rows.with(O, ldo, hdo);
     f.vec = rows.vec;
-    if (plan->cut[c.level] * plan->br * a.H / 4 >= ((int64_t)1 << 31) - 1) return SP_ERR_TOO_LARGE;         // workgroups of the join
+    if (!attn_launches(ceil_div(plan->cut[c.level] * plan->br * a.H, 4), 256)) return SP_ERR_TOO_LARGE;     // the join
     hipStream_t st = (hipStream_t)stream;
     if (p->dtype == SP_F32) return attn_forward<float>(plan, f, c, st);
     if (p->dtype == SP_F16) return attn_forward<attn_f16>(plan, f, c, st);
@@ -172,9 +172,9 @@ extern "C" sp_status sp_attention_grad(const sp_tensor *S, const sp_attention_pr
     rows.with(g->O, g->ldo, g->hdo); rows.with(g->dO, g->lddo, g->hddo);
     rows.with(g->dQ, g->lddq, g->hddq); rows.with(g->dK, g->lddk, g->hddk); rows.with(g->dV, g->lddv, g->hddv);
     f.vec = rows.vec;
-    for (const sp_attn_plan *plan : S->attention)
-        for (int l = 0; l < plan->levels; ++l)
-            if (plan->cut[l] * plan->br * a.H / 4 >= ((int64_t)1 << 31) - 1) return SP_ERR_TOO_LARGE;       // workgroups of the joins
+    const sp_attn_plan *rows_plan = S->attention[0], *keys_plan = S->attention[1];
+    if ((c.rows.cut && !attn_launches(ceil_div(rows_plan->cut[c.rows.level] * rows_plan->br * a.H, 4), 256)) ||
+        (c.keys_cut && !attn_launches(ceil_div(keys_plan->cut[c.keys_level] * keys_plan->br * a.Hk, 4), 256))) return SP_ERR_TOO_LARGE;     // the joins
     hipStream_t st = (hipStream_t)stream;
     if (p->dtype == SP_F32) return attn_backward<float>(S, f, c, st);
     if (p->dtype == SP_F16) return attn_backward<attn_f16>(S, f, c, st);

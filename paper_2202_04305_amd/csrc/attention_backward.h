@@ -696,7 +696,7 @@ __global__ __launch_bounds__(kThreads) void table_kernel(grad_args f, int64_t it
 template <typename K>
 sp_status launch(K kernel, const grad_args &f, int64_t groups, int threads, size_t lds, hipStream_t st)
 {
-    if (groups >= ((int64_t)1 << 31)) return SP_ERR_TOO_LARGE;
+    if (!attn_launches(groups, threads)) return SP_ERR_TOO_LARGE;
     if (lds > (size_t)kAttnLds) return SP_ERR_UNSUPPORTED;
     if (lds > 65536) SP_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), lds, st, f);
@@ -732,6 +732,10 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
 {
     attn_args &a = f.a;
     const sp_attn_plan *rows = S->attention[0], *keys = S->attention[1];
+    const bool pos = (S->nvalues > 0 && (a.buckets || a.causal)) || a.scale == 0;
+    const int row_threads = c.rows.wn > 1 ? 64 * attn_dq_waves(DT * (int)sizeof(T), pos) : 256;
+    if (!attn_launches(rows->items[c.rows.level] * c.rows.groups, row_threads) || !attn_launches(keys->items[c.keys_level] * a.Hk, keys->br == 128 ? 256 : 64))
+        return SP_ERR_TOO_LARGE;                         // before anything is written
     if (S->nvalues == 0) {                               // no pairs: zeros, and nothing of the problem is read
         // (by dTable: without rows the workspace has no bytes, and its parts no addresses)
         if (a.buckets && f.g.dTable) hipLaunchKernelGGL(table_kernel<T>, dim3((unsigned)(a.buckets * a.H)), dim3(kThreads), 0, st, f, (int64_t)0);
@@ -740,7 +744,6 @@ sp_status grad_d(const sp_tensor *S, grad_args &f, const grad_choice &c, hipStre
         a.buckets = a.causal = 0;
     }
     if (!a.buckets && !a.causal) a.qpos = a.kpos = nullptr;
-    const bool pos = a.buckets || a.causal || a.scale == 0;
     if (a.m > 0) {
         f.p = attn_view(rows, c.rows.level);
         f.groups = c.rows.groups; f.mode = c.rows.mode;

@@ -341,6 +341,7 @@ sp_status launch(const forward_args &f, const forward_choice &c, int64_t items, 
     const size_t join = WN > 1 ? (size_t)WN * 32 * (DT + 3) * 4 : 0;
     if (join > lds) lds = join;
     auto kernel = forward_kernel<T, DT, WM, WN, KW, POS>;
+    if (!attn_launches(items * c.groups, 64 * WM * WN)) return SP_ERR_TOO_LARGE;
     if (lds > 65536) SP_HIP(hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     hipLaunchKernelGGL(kernel, dim3((unsigned)(items * c.groups)), dim3(64 * WM * WN), lds, st, f);
     SP_HIP(hipGetLastError());
@@ -366,7 +367,6 @@ sp_status attn_forward(const sp_attn_plan *plan, forward_args &f, const forward_
     // scale 0 goes with the positions: products of q and k by themselves would be scaled by zero after the mask's infinities
     const bool pos = f.a.buckets || f.a.causal || f.a.scale == 0;
     const int64_t items = plan->items[c.level];
-    if (items * c.groups >= ((int64_t)1 << 31)) return SP_ERR_TOO_LARGE;
 #define SPMI_FORWARD(DT)                                                                                                          \
     do {                                                                                                                          \
         if (pos) SP_TRY((launch_mode<T, DT, true>(f, c, items, st)));                                                             \

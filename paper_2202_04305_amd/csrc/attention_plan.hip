@@ -86,7 +86,7 @@ __global__ __launch_bounds__(1024) void blocks_kernel(const int32_t *__restrict_
 // FILL = false: counts[block * windows + window] = distinct columns.  FILL = true: counts are scanned (exclusive), chunk0 is there;
 // writes cols and bits.
 template <bool FILL>
-__global__ __launch_bounds__(kThreads) void window_kernel(const int32_t *__restrict__ rowptr, const int32_t *__restrict__ crd,
+__global__ __launch_bounds__(kThreads) void window_kernel(int64_t first, const int32_t *__restrict__ rowptr, const int32_t *__restrict__ crd,
                                                           const int32_t *__restrict__ row0, int64_t m, int br,
                                                           int windows, int wlog, uint32_t *__restrict__ counts, const int32_t *__restrict__ chunk0,
                                                           int32_t *__restrict__ cols, uint32_t *__restrict__ bits)
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kThreads) void window_kernel(const int32_t *__restr
     __shared__ uint32_t s_wave[kThreads / 64];
     uint32_t *rank = bitmap + (kThreads << wlog);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t block = blockIdx.x / windows, window = blockIdx.x % windows;
+    const int64_t pair = first + blockIdx.x, block = pair / windows, window = pair % windows;
     const int64_t base = window * ((int64_t)kWindow << wlog), end = base + ((int64_t)kWindow << wlog);
     const int words = 1 << wlog;                         // of a thread
     for (int i = 0; i < words; ++i) bitmap[tid * words + i] = 0;
@@ -124,12 +124,12 @@ __global__ __launch_bounds__(kThreads) void window_kernel(const int32_t *__restr
     uint32_t before = 0, total = 0;
     for (int w = 0; w < kThreads / 64; ++w) { before += w < wave ? s_wave[w] : 0; total += s_wave[w]; }
     if (!FILL) {
-        if (tid == 0) counts[blockIdx.x] = total;
+        if (tid == 0) counts[pair] = total;
         return;
     }
     if (total == 0) return;                              // the whole workgroup
     // places of this window's columns: behind those of the block's windows before it
-    const uint32_t place = (uint32_t)chunk0[block] * kAttnChunk + (counts[blockIdx.x] - counts[block * windows]);
+    const uint32_t place = (uint32_t)chunk0[block] * kAttnChunk + (counts[pair] - counts[block * windows]);
     uint32_t at = before + upto - mine;
     for (int i = 0; i < words; ++i) {
         const int w = tid * words + i;
@@ -184,11 +184,11 @@ __global__ __launch_bounds__(kThreads) void chunks_kernel(const uint32_t *__rest
 __global__ __launch_bounds__(kThreads) void pad_kernel(const uint32_t *__restrict__ counts, int windows, const int32_t *__restrict__ chunk0,
                                                        int64_t nblocks, int32_t *__restrict__ cols)
 {
-    const int64_t b = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (b >= nblocks) return;
-    const int64_t n = counts[(b + 1) * windows] - counts[b * windows], first = (int64_t)chunk0[b] * kAttnChunk, end = (int64_t)chunk0[b + 1] * kAttnChunk;
-    const int64_t x = first + n + (threadIdx.x & 63);
-    if (n > 0 && x < end) cols[x] = cols[first + n - 1];
+    for (int64_t b = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); b < nblocks; b += (int64_t)gridDim.x * (kThreads / 64)) {
+        const int64_t n = counts[(b + 1) * windows] - counts[b * windows], first = (int64_t)chunk0[b] * kAttnChunk, end = (int64_t)chunk0[b + 1] * kAttnChunk;
+        const int64_t x = first + n + (threadIdx.x & 63);
+        if (n > 0 && x < end) cols[x] = cols[first + n - 1];
+    }
 }
 
 __global__ __launch_bounds__(kThreads) void state_kernel(const uint64_t *__restrict__ bits, const int32_t *__restrict__ chunk0,
@@ -264,6 +264,8 @@ __global__ __launch_bounds__(kThreads) void stretches_kernel(const int32_t *__re
         items[x] = s;
     }
 }
+
+constexpr int64_t kGroups = 1 << 22;     // workgroups of a launch, where there may be more than one has (attn_launches)
 
 unsigned blocks_for(int64_t n) { return (unsigned)(n > 0 ? ceil_div(n, kThreads) : 1); }
 
@@ -359,9 +361,9 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
         w.chunk0 = (int32_t *)tmp.get((size_t)(w.c.blocks + 1) * 4);
         if (!w.counts || !w.chunk0) return SP_ERR_ALLOC;
         hipLaunchKernelGGL(fill_kernel, dim3(1), dim3(kThreads), 0, st, w.counts + pairs, (int64_t)1, 0u);
-        if (pairs > 0)
-            hipLaunchKernelGGL((window_kernel<false>), dim3((unsigned)pairs), dim3(kThreads), (size_t)(kThreads << w.c.wlog) * 4, st, p->rowptr,
-                               p->crd, w.row0, m, w.br, w.c.windows, w.c.wlog, w.counts, nullptr, nullptr, nullptr);
+        for (int64_t first = 0; first < pairs; first += kGroups)
+            hipLaunchKernelGGL((window_kernel<false>), dim3((unsigned)(pairs - first < kGroups ? pairs - first : kGroups)), dim3(kThreads),
+                               (size_t)(kThreads << w.c.wlog) * 4, st, first, p->rowptr, p->crd, w.row0, m, w.br, w.c.windows, w.c.wlog, w.counts, nullptr, nullptr, nullptr);
         SP_HIP(hipGetLastError());
         SP_TRY(spmi_exclusive_scan(w.counts, pairs + 1, 32, tmp, st));
         hipLaunchKernelGGL(chunks_kernel, dim3(blocks_for(w.c.blocks + 1)), dim3(kThreads), 0, st, w.counts, w.c.windows, p->rowptr, w.c.blocks, w.chunk0,
@@ -377,10 +379,12 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
     // each head: it is the better choice until a block of 32 rows has every column twice on average, as long as the rows all run at
     // once; beyond about 512 of them, beginning and ending one costs as much as 400 columns (4096 rows of 96 columns out of 65,536, 8
     // heads: 95 us in blocks of 32, 378 by themselves; 276 rows of 79 out of 17,791, 8 heads of one key head, f32: 54 and 38).
-    const int wide = tried == 3 && ways[2].chunks * 10 <= ways[0].chunks * 11 ? 2 : 0;
+    // Whatever makes more blocks than a launch has workgroups is left out.
+    auto fits = [](int64_t blocks) { return attn_launches(blocks, 256); };
+    const int wide = tried == 3 && ways[2].chunks * 10 <= ways[0].chunks * 11 && fits(ways[2].c.blocks) ? 2 : 0;
     const double cost128 = (double)ways[wide].chunks * 64 * (64 + 128), cost32 = (double)ways[1].chunks * 64 * (64 + 32), cost1 = ((double)entries + 400.0 * (double)(m > 512 ? m - 512 : 0)) * (64 + 32) / 2;
     const way *chosen = nullptr;                         // null: rows by themselves
-    if (transposed || cost1 > cost32 || cost1 > cost128) chosen = &ways[cost32 < cost128 ? 1 : wide];
+    if (transposed || cost1 > cost32 || cost1 > cost128 || !fits(m)) chosen = &ways[cost32 < cost128 && fits(ways[1].c.blocks) ? 1 : wide];
     p->br = chosen ? chosen->br : 1;
     p->nblocks = chosen ? chosen->c.blocks : m;
     p->chunk0 = (int32_t *)scope.get((size_t)(p->nblocks + 1) * 4);
@@ -412,9 +416,12 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
         if (p->nchunks > 0) {
             SP_TRY(spmi_fill_zero(p->bits, words * 8, st));
             const cut &c = chosen->c;
-            hipLaunchKernelGGL((window_kernel<true>), dim3((unsigned)(c.blocks * c.windows)), dim3(kThreads), (size_t)(kThreads << c.wlog) * 8, st,
-                               p->rowptr, p->crd, p->row0, m, p->br, c.windows, c.wlog, chosen->counts, p->chunk0, p->cols, (uint32_t *)p->bits);
-            hipLaunchKernelGGL(pad_kernel, dim3((unsigned)ceil_div(p->nblocks, kThreads / 64)), dim3(kThreads), 0, st, chosen->counts, c.windows, p->chunk0,
+            const int64_t pairs = c.blocks * c.windows, pads = ceil_div(p->nblocks, kThreads / 64);
+            for (int64_t first = 0; first < pairs; first += kGroups)
+                hipLaunchKernelGGL((window_kernel<true>), dim3((unsigned)(pairs - first < kGroups ? pairs - first : kGroups)), dim3(kThreads),
+                                   (size_t)(kThreads << c.wlog) * 8, st, first, p->rowptr, p->crd, p->row0, m, p->br, c.windows, c.wlog, chosen->counts, p->chunk0,
+                                   p->cols, (uint32_t *)p->bits);
+            hipLaunchKernelGGL(pad_kernel, dim3((unsigned)(pads < kGroups ? pads : kGroups)), dim3(kThreads), 0, st, chosen->counts, c.windows, p->chunk0,
                                p->nblocks, p->cols);
             hipLaunchKernelGGL(state_kernel, dim3(blocks_for(p->nchunks * (p->br / 32))), dim3(kThreads), 0, st, p->bits, p->chunk0, p->row0, p->nblocks,
                                p->nchunks, m, p->br, p->state);

@@ -203,3 +203,34 @@ def test_default_allocator(m, n, pairs, grad):
     check(run(S, p, grad), reference(p, grad))
     torch.cuda.synchronize()
     S.free()
+
+
+def test_calls_of_more_workgroups_than_a_launch_has_are_refused():
+    """A launch has fewer than 2^32 threads in a direction: 2^24 workgroups of 256.  2^24 rows in blocks of 128, 128 heads."""
+    m = 1 << 24
+    none = torch.zeros(0, dtype=torch.int64, device=DEV)
+    S = sp.sp_pack(sp.sp_encode((0, 1), None, 32, 32), (m, 8), [none, none], torch.zeros(0, device=DEV))
+    sp.sp_prepare_attention(S, grad=True)
+    row = torch.zeros(1, 128, 1, dtype=BF16, device=DEV)
+    Q, K = row.expand(m, -1, -1), torch.zeros(8, 128, 1, dtype=BF16, device=DEV)
+    O = torch.empty(m, 128, 1, dtype=BF16, device=DEV)
+    lse = torch.empty(128, m, device=DEV)
+    assert code(sp.sp_attention, S, Q, K, K, O=O, lse=lse) == 11
+    assert code(sp.sp_attention_grad, S, Q, K, K, O, lse, O, dQ=O, dK=K, dV=K) == 11
+
+
+def test_more_blocks_of_rows_than_a_launch_has_workgroups():
+    """2^29 rows and a few, of which three store anything: the inspector looks at 2^24 blocks of 32."""
+    m, H = (1 << 29) + 5, 1
+    rows, cols = torch.tensor([7, 7, (1 << 28) + 1, m - 1, m - 1, m - 1]), torch.tensor([1, 5, 0, 0, 3, 7])
+    S = sp.sp_pack(sp.sp_encode((0, 1), None, 32, 32), (m, 8), [rows.to(DEV), cols.to(DEV)], torch.zeros(6, device=DEV))
+    sp.sp_prepare_attention(S)
+    some = torch.unique(rows)
+    at = torch.zeros(3, 8, dtype=torch.bool)
+    at[torch.searchsorted(some, rows), cols] = True
+    p = problem(at, H, 1, 4, BF16, train=False)
+    Q = torch.zeros(m, 1, 4, dtype=BF16, device=DEV)
+    Q[some.to(DEV)] = p.Q.to(DEV)
+    O, lse = sp.sp_attention(S, Q, p.K.to(DEV), p.V.to(DEV))
+    check({"O": O[some.to(DEV)], "lse": lse[:, some.to(DEV)]}, reference(p, False))
+    assert int((lse != float("-inf")).sum()) == 3 and int((O != 0).any(2).sum()) == 3
