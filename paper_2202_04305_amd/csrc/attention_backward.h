@@ -775,7 +775,8 @@ sp_status attn_backward(const sp_tensor *S, grad_args &f, const grad_choice &c, 
     if (f.a.D <= 32) return grad_d<T, 32>(S, f, c, st);
     if (f.a.D <= 64) return grad_d<T, 64>(S, f, c, st);
     if (f.a.D <= 128) return grad_d<T, 128>(S, f, c, st);
-    // f32 ends at 128: a row and its sums of 256 numbers of 32 bits do not fit a lane's registers
+    // f32 ends at 128: a row and its sums of 256 numbers of 32 bits do not fit a lane's registers (0.6 to 2 KB of scratch a lane), nor, with a
+    // bias, a step of K and V and the sums by bucket the LDS
     if constexpr (sizeof(T) == 2) return grad_d<T, 256>(S, f, c, st);
     return SP_ERR_SHAPE;
 }
