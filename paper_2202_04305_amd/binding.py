@@ -335,7 +335,7 @@ _ATTENTION_DT = {torch.float32: SP_F32, torch.float16: SP_F16, torch.bfloat16: S
 def sp_prepare_attention(S, grad=False):
     """The inspector step of sp_attention (grad: and of sp_attention_grad) on the pattern of S; synchronises."""
     L = load_library()
-    _check(L.sp_prepare_attention(S._h, int(bool(grad)), _stream_ptr()), "in sp_prepare_attention")
+    _attention_call(S, lambda: _check(L.sp_prepare_attention(S._h, int(bool(grad)), _stream_ptr()), "in sp_prepare_attention"))
     return S
 
 
