@@ -229,7 +229,8 @@ sp_status sp_attention(const sp_tensor *S, const sp_attention_problem *p, void *
  * O and lse are sp_attention's; the gradients are overwritten (rows and columns without pairs become zero).  dTable may be NULL.
  * A row's weights p sum to 1 also where a bias puts lse so far from zero that its 32 bits have no room for the logarithm of their
  * number (a row of nothing but the type's lowest value weighs all its keys alike).
- * S must have been prepared with grad = 1.  Workspace, streams and reproducibility as for sp_attention. */
+ * Gradients must not overlap each other or an input.  S must have been prepared with grad = 1.  Workspace, streams, errors and
+ * reproducibility as for sp_attention. */
 typedef struct sp_attention_grads {
     const void *O; int64_t ldo, hdo;
     const float *lse;                   /* DEVICE, heads x m                                                             */

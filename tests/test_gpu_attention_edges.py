@@ -6,7 +6,7 @@ import torch
 import paper_2202_04305_amd as sp
 from attention_util import reference
 from gpu_util import say, DEV
-from test_gpu_attention import BF16, F16, F32, PATTERNS, band, check, code, pack, problem, ragged, run
+from test_gpu_attention import BF16, F16, F32, PATTERNS, check, code, pack, problem, ragged, random_pattern, run
 
 pytestmark = pytest.mark.gpu
 
@@ -234,3 +234,150 @@ def test_more_blocks_of_rows_than_a_launch_has_workgroups():
     O, lse = sp.sp_attention(S, Q, p.K.to(DEV), p.V.to(DEV))
     check({"O": O[some.to(DEV)], "lse": lse[:, some.to(DEV)]}, reference(p, False))
     assert int((lse != float("-inf")).sum()) == 3 and int((O != 0).any(2).sum()) == 3
+
+
+def by_abi(S, p, grads=True, **without):
+    """The calls of the C ABI with pointers that may be NULL left out."""
+    from paper_2202_04305_amd import binding
+    import ctypes
+    L, st = sp.load_library(), torch.cuda.current_stream().cuda_stream
+    o = p.options(DEV)
+    Q, K, V, dO = (t.to(DEV) for t in (p.Q, p.K, p.V, p.dO))
+    a = binding._attention_problem(S, Q, K, V, o["scale"], o.get("causal", False), o.get("qpos"), o.get("kpos"), o.get("bias"), o.get("max_distance", 128),
+                                   o.get("bidirectional", True))
+    keep = [o, Q, K, V, dO]
+
+    def work(grad):
+        size = ctypes.c_size_t()
+        assert L.sp_attention_workspace(S._h, ctypes.byref(a), grad, ctypes.byref(size)) == 0
+        keep.append(torch.full((max(size.value, 1),), 255, dtype=torch.uint8, device=DEV))
+        return keep[-1].data_ptr(), size.value
+    out = {"O": torch.empty_like(Q), "lse": torch.empty(Q.shape[1], Q.shape[0], device=DEV)}
+    lse = None if "lse" in without else out["lse"].data_ptr()
+    assert L.sp_attention(S._h, ctypes.byref(a), out["O"].data_ptr(), out["O"].stride(0), out["O"].stride(1), lse, *work(0), st) == 0
+    if lse is None:
+        torch.cuda.synchronize()
+        return {"O": out["O"]}
+    g = binding.SpAttentionGrads()
+    for k, like in (("dQ", Q), ("dK", K), ("dV", V)):
+        out[k] = torch.empty_like(like)
+    for k, ld, hd, t in (("O", "ldo", "hdo", out["O"]), ("dO", "lddo", "hddo", dO), ("dQ", "lddq", "hddq", out["dQ"]), ("dK", "lddk", "hddk", out["dK"]), ("dV", "lddv", "hddv", out["dV"])):
+        setattr(g, k, t.data_ptr()); setattr(g, ld, t.stride(0)); setattr(g, hd, t.stride(1))
+    g.lse = lse
+    assert L.sp_attention_grad(S._h, ctypes.byref(a), ctypes.byref(g), *work(1), st) == 0
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("name", ["band", "sparse", "tokens behind a prefix", "one row"])
+def test_outputs_that_may_be_left_out(name, dt):
+    """lse NULL, and dTable NULL with a bias: the other outputs are the same bits."""
+    at = PATTERNS[name]()
+    p = problem(at, 4, 2, 32, dt, buckets=16, positions=(torch.arange(at.shape[0]), torch.arange(at.shape[1])), max_distance=60)
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    want, ref = run(S, p), reference(p)
+    assert torch.equal(by_abi(S, p, lse=None)["O"], want["O"])
+    got = by_abi(S, p)                                   # rows may be cut otherwise than with the table's gradient
+    del ref["dT"]
+    check(got, ref, name)
+
+
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("D", [8, 32, 40, 64, 96, 128, 160, 256])
+def test_the_largest_tables_fit_beside_every_head_size(D, dt):
+    """64 buckets over distances of up to 4096, in every way of making tiles: the tables and the sums by bucket share the LDS with the rows."""
+    if dt == F32 and D > 128:
+        pytest.skip("refused: does not fit a lane's registers")
+    say("case", D, dt)
+    g = torch.Generator().manual_seed(D)
+    few, many = torch.rand(20, 700, generator=g) < 0.8, ragged([130, 33], [165, 100])
+    for at, heads in ((few, (2, 1)), (few, (6, 1)), (torch.ones(1, 300, dtype=torch.bool), (40, 1)), (many, (2, 1))):
+        m, n = at.shape
+        where = torch.randint(-4500, 4500, (m,), generator=g), torch.randint(-4500, 4500, (n,), generator=g)
+        p = problem(at, heads[0], heads[1], D, dt, buckets=64, positions=where, max_distance=4096, bidirectional=D % 16 == 0)
+        S = sp.sp_prepare_attention(pack(at), grad=True)
+        check(run(S, p), reference(p), "D %d heads %s" % (D, heads))
+
+
+@pytest.mark.parametrize("made", ["sp_convert", "sp_add", "sp_spgemm"])
+def test_patterns_that_other_calls_have_made(made):
+    a, b = random_pattern(90, 70, 0.1, 1), random_pattern(90, 70, 0.1, 2)
+    enc = sp.sp_encode((0, 1), (0, 1), 32, 32)
+
+    def ones(at, order=(0, 1)):
+        rows, cols = (t.to(DEV).contiguous() for t in at.nonzero(as_tuple=True))
+        return sp.sp_pack(sp.sp_encode((0, 1), order, 32, 32), at.shape, [rows, cols], torch.ones(rows.numel(), device=DEV))
+    if made == "sp_convert":
+        at, S = a, sp.sp_convert(ones(a, (1, 0)), enc)
+    elif made == "sp_add":
+        at, S = a | b, sp.sp_add(ones(a), ones(b), enc)
+    else:
+        at, S = (a.float() @ b.t().float()) > 0, sp.sp_spgemm(ones(a), ones(b.t().contiguous()), enc)
+    p = problem(at, 4, 2, 32, BF16)
+    sp.sp_prepare_attention(S, grad=True)
+    check(run(S, p), reference(p), made)
+    assert sp.sp_tensor_info(S).derivedBytes > 0
+
+
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("name", ["one row", "band", "sparse", "half", "ragged batch", "tokens behind a prefix", "empty rows"])
+def test_causal_by_positions_in_no_order(name, dt):
+    at = PATTERNS[name]()
+    g = torch.Generator().manual_seed(11)
+    for heads, buckets in (((2, 2), 0), ((6, 1), 0), ((2, 1), 16), ((6, 1), 16)):
+        where = torch.randint(-60, 60, (at.shape[0],), generator=g), torch.randint(-60, 60, (at.shape[1],), generator=g)
+        p = problem(at, heads[0], heads[1], 40, dt, buckets=buckets, positions=where, causal=True, max_distance=50, bidirectional=heads[1] == 2)
+        S = sp.sp_prepare_attention(pack(at), grad=True)
+        check(run(S, p), reference(p), "%s %s %d" % (name, heads, buckets))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("name", ["dense", "sparse", "one row", "tokens behind a prefix"])
+def test_a_bias_that_is_not_a_number_reaches_the_rows_that_have_its_distances_only(name, dt, bad):
+    at = PATTERNS[name]()
+    m, n = at.shape
+    p = problem(at, 4, 2, 32, dt, buckets=16, positions=(torch.arange(m) % 37, torch.arange(n) % 41), max_distance=100)
+    if m > 1:
+        p.qpos[m // 2] = 2000                            # all of this row's keys in bucket 7, which no other row has
+    else:
+        p.bias[7] = 0
+    p.bias[7] = bad
+    rows = torch.arange(m) != (m // 2 if m > 1 else -1)
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    p.dO[~rows] = 0
+    got = run(S, p)
+    p.bias[7], p.at = 0, at & rows[:, None]
+    ref = reference(p)
+    keys = ~at[~rows].any(0)
+    check({"O": got["O"][rows.to(DEV)], "lse": got["lse"][:, rows.to(DEV)], "dQ": got["dQ"][rows.to(DEV)], "dK": got["dK"][keys.to(DEV)], "dV": got["dV"][keys.to(DEV)]},
+          {"O": tuple(t[rows] for t in ref["O"]), "lse": tuple(t[:, rows] for t in ref["lse"]), "dQ": tuple(t[rows] for t in ref["dQ"]),
+           "dK": tuple(t[keys] for t in ref["dK"]), "dV": tuple(t[keys] for t in ref["dV"])}, name)
+    others = torch.arange(16) != 7
+    check({"dT": got["dT"][others.to(DEV)]}, {"dT": tuple(t[others] for t in ref["dT"])}, name)
+    if m > 1 and at[m // 2].any():
+        assert bool(torch.isnan(got["O"][m // 2]).all())
+
+
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("name", ["band", "sparse", "tokens behind a prefix", "cut rows"])
+def test_infinite_values_and_gradients_stay_with_their_rows(name, dt):
+    """A value of infinity, and a dO of infinity in another row."""
+    at = torch.cat([torch.ones(24, 3000, dtype=torch.bool), ragged([1] * 24, [40] * 24)], 1) if name == "cut rows" else PATTERNS[name]()
+    p = problem(at, 2, 1, 32, dt)
+    col = at.shape[1] - 1 if name != "sparse" and name != "band" else int((at.sum(0) + 1000 * (at.sum(0) == 0)).argmin())
+    row = int((~at[:, col]).nonzero()[0])
+    was = p.V[col].clone(), p.dO[row].clone()
+    p.V[col], p.dO[row] = float("inf"), float("-inf")
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    got = run(S, p)
+    p.V[col], p.dO[row] = was
+    ref = reference(p)
+    has = at[:, col]
+    check({"O": got["O"][(~has).to(DEV)], "lse": got["lse"]}, {"O": tuple(t[~has] for t in ref["O"]), "lse": ref["lse"]}, name)
+    assert not bool(torch.isfinite(got["O"][has.to(DEV)]).any())
+    rows, keys = ~has, ~at[row] & ~at[has].any(0)
+    rows[row] = False
+    check({"dQ": got["dQ"][rows.to(DEV)], "dK": got["dK"][keys.to(DEV)], "dV": got["dV"][(~at[row]).to(DEV)]},
+          {"dQ": tuple(t[rows] for t in ref["dQ"]), "dK": tuple(t[keys] for t in ref["dK"]), "dV": tuple(t[~at[row]] for t in ref["dV"])}, name)
