@@ -22,6 +22,9 @@ grad_choice choose(const sp_tensor *S, const attn_args &a, int size, bool table)
     const sp_attn_plan *rows = S->attention[0], *keys = S->attention[1];
     grad_choice c;
     c.rows = attn_map(rows, a, size, 3);
+    // short 16-bit rows stay whole (see kAttnTwice)
+    if (size == 2 && c.rows.level < kAttnTwiceLevel) c.rows.level = rows->levels - 1 < kAttnTwiceLevel ? rows->levels - 1 : kAttnTwiceLevel;
+    c.rows.cut = rows->cut[c.rows.level] > 0;
     // the bias's gradient from sums that need a row's whole D: rows are not cut then, unless a few long ones would hold up the rest for
     // longer than the whole pass takes, and the sums have to fit the LDS
     const int row = (a.D <= 32 ? 32 : a.D <= 64 ? 64 : a.D <= 128 ? 128 : 256) * size;

@@ -110,7 +110,8 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     const attn_plan_view &p = f.p;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = WN > 1 ? wave : 0;
     const int ftid = WN > 1 ? lane : tid;
-    attn_lds_i32 *s_kpos = (attn_lds_i32 *)((attn_lds *)lds + 4 * KT * tile::kRow) + wn * 2 * FC;
+    constexpr int kShare = WN > 1 ? WN * 128 : 0;        // behind K and V
+    attn_lds_i32 *s_kpos = (attn_lds_i32 *)((attn_lds *)lds + 4 * KT * tile::kRow + kShare) + wn * 2 * FC;
     const int64_t item_no = blockIdx.x / f.groups;
     const int group = blockIdx.x % f.groups;
     const attn_item item(p, item_no);
@@ -143,13 +144,12 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
     attn_lds_f32 *hist = nullptr;                             // [buckets][64] of ds; exact: of p dP and p
     const int places = attn_places(a), hist_size = places * 64 * (f.exact ? 2 : 1);
     float far_x[2] = {0, 0}, far_p[2] = {0, 0};          // the far buckets behind and ahead
-    const float of_term = f.exact ? 0.f : delta;
     if (POS) {
         if (a.qpos) { qp = a.qpos[me.row]; q_lo = attn_wave_min(qp); q_hi = attn_wave_max(qp); }
         if (a.buckets) {
             if (__builtin_amdgcn_ballot_w64(me.valid && fabsf(off) >= kAttnNearLse && off - off == 0) != 0)
                 log_sum = attn_log_sum<T, DT>(f, item, me, q, qp, off, lane);
-            bias = attn_lane_bias<T>(a, (attn_lds *)lds + 4 * KT * tile::kRow + 2 * KT * 4, f.mode, group, lane, wave, WM);
+            bias = attn_lane_bias<T>(a, (attn_lds *)lds + 4 * KT * tile::kRow + kShare + 2 * KT * 4, f.mode, group, lane, wave, WM);
             if (f.part_table) {
                 hist = bias.table + (((places << bias.shift) + 3) & ~3) + wave * hist_size;
                 for (int b = lane; b < hist_size; b += 64) hist[b] = 0;
@@ -189,103 +189,123 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         state_next = 0;
         if (chunk >= 0) { state_next = item.state(p, chunk, r); word_next = item.word(p, chunk, r); }
     };
-    if (steps > 0) {
-        ring.begin(steps, [](int64_t s) { return s; });
-        fetch_pairs(0);
-        ring.rows(0, Kh, Vh);
+    auto walk = [&](auto early) {
+        constexpr bool EARLY = decltype(early)::value;
+        if (steps > 0) {
+            ring.begin(steps, [](int64_t s) { return s; });
+            fetch_pairs(0);
+            ring.rows(0, Kh, Vh);
+        }
+        for (int64_t step = 0; step < steps; ++step) {
+            ring.arrive();
+            if (POS && ftid < FC) s_kpos[(step & 1) * FC + ftid] = ring.kp_one;
+            if (WN == 1) __syncthreads();
+            else {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+            word = word_next; state = state_next;
+            const attn_lds *sK = ring.x_of(step), *sV = ring.y_of(step);
+            if (step + 1 < steps) {
+                ring.advance();
+                if (step + ring.kAhead < steps) ring.columns(step + ring.kAhead);
+                fetch_pairs(step + 1);
+                ring.rows(step + 1, Kh, Vh);
+            }
+            int col0;
+            if (my_chunk(step, col0) < 0) continue;
+            state = __builtin_amdgcn_readfirstlane(state);
+            if (state == 0) continue;
+            word >>= col0 % kAttnChunk;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const attn_lds_i32 *kp = s_kpos + (step & 1) * FC + 32 * t;
+                attn_near near = {false, false, false, 0};
+                if (POS) {
+                    const int col = kp[lane & 31];
+                    near = attn_look(a, attn_distance(col, q_hi), attn_distance(col, q_lo));
+                    if (near.nothing) continue;
+                }
+                attn_f32x16 s = tile::scores(sK, 32 * t, q, a.D, lane);
+                attn_f32x16 dp = tile::scores(sV, 32 * t, go, a.D, lane);
+                // what is not stored, and rows that do not exist, add nothing
+                const uint32_t bits = (me.valid ? (uint32_t)(word >> (32 * t)) : 0u) >> (4 * (lane >> 5));
+                if (!POS) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], cc, -off)) * (dp[x] - delta);
+                    if (state != 2) {                        // a lane of no row keeps its own nonsense to itself
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) s[x] = attn_where(bits, 8 * (x >> 2) + (x & 3), s[x]);
+                    }
+                } else {
+                    // Loops of one kind of work each, without branches inside, so that the LDS's answers overlap.  A score of minus
+                    // infinity has weight 0, whatever dP is.
+                    const bool one = !a.buckets || near.far;
+                    uint32_t there = 0;
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) there |= (bits >> 8 * b & 15) << 4 * b;
+                    if (near.ask) {
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) there &= ~((uint32_t)(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)] > qp) << x);
+                    }
+                    if (one) {
+                        const float all_of = a.buckets ? bias.at(near.place) : 0.f;
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, all_of);
+                    } else
+                        attn_add_bias(bias, s, a.scale, [&](int x) { return kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]; }, [&](int) { return qp; });
+                    if (attn_any_lowest(s)) {
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) there &= ~((uint32_t)(s[x] == -INFINITY) << x);
+                    }
+                    float sum_x = 0, sum_p = 0, term[16], weight[16];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        weight[x] = attn_where(there, x, __builtin_amdgcn_exp2f(__builtin_fmaf(s[x] - off, cc, -log_sum)));
+                        s[x] = attn_where(there, x, weight[x] * (dp[x] - delta));
+                        term[x] = attn_where(there, x, weight[x] * (dp[x] - (f.exact ? 0.f : delta)));
+                        sum_x += term[x]; sum_p += weight[x];
+                    }
+                    if (!EARLY && hist && !one) {
+                        int place[16];
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) place[x] = bias.lut[bias.index(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp)];
+                        if (f.exact) attn_add_by_bucket<2>(hist, lane, place, term, weight);
+                        else attn_add_by_bucket<1>(hist, lane, place, term, weight);
+                    }
+                    if (!EARLY && hist && one) {
+                        const bool behind = near.place == a.side - 1;
+                        far_x[0] += behind ? sum_x : 0.f; far_p[0] += behind ? sum_p : 0.f;
+                        far_x[1] += behind ? 0.f : sum_x; far_p[1] += behind ? 0.f : sum_p;
+                    }
+                }
+                if (sizeof(T) == 2) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) rest += s[x];
+                }
+                if (!EARLY) tile::add_rows(acc, sK, 32 * t, s, a.D, lane);
+            }
+        }
+    };
+    // Short rows go through their steps twice, and the first time their ds only add up to what D misses.
+    if (sizeof(T) == 2 && item.whole && item.c1 - item.c0 <= kAttnTwice) {
+        walk(std::true_type());
+        rest = attn_pair_sum(rest);
+        __syncthreads();
+        if (WN > 1) {                                    // the waves' shares of the tile
+            attn_lds_f32 *share = (attn_lds_f32 *)((attn_lds *)lds + 4 * KT * tile::kRow);
+            share[wn * 32 + (lane & 31)] = rest;
+            __syncthreads();
+            rest = 0;
+#pragma unroll
+            for (int x = 0; x < WN; ++x) rest += share[x * 32 + (lane & 31)];
+        }
+        delta += rest;
+        rest = 0;
     }
-    for (int64_t step = 0; step < steps; ++step) {
-        ring.arrive();
-        if (POS && ftid < FC) s_kpos[(step & 1) * FC + ftid] = ring.kp_one;
-        if (WN == 1) __syncthreads();
-        else {
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
-        word = word_next; state = state_next;
-        const attn_lds *sK = ring.x_of(step), *sV = ring.y_of(step);
-        if (step + 1 < steps) {
-            ring.advance();
-            if (step + ring.kAhead < steps) ring.columns(step + ring.kAhead);
-            fetch_pairs(step + 1);
-            ring.rows(step + 1, Kh, Vh);
-        }
-        int col0;
-        if (my_chunk(step, col0) < 0) continue;
-        state = __builtin_amdgcn_readfirstlane(state);
-        if (state == 0) continue;
-        word >>= col0 % kAttnChunk;
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-            const attn_lds_i32 *kp = s_kpos + (step & 1) * FC + 32 * t;
-            attn_near near = {false, false, false, 0};
-            if (POS) {
-                const int col = kp[lane & 31];
-                near = attn_look(a, attn_distance(col, q_hi), attn_distance(col, q_lo));
-                if (near.nothing) continue;
-            }
-            attn_f32x16 s = tile::scores(sK, 32 * t, q, a.D, lane);
-            attn_f32x16 dp = tile::scores(sV, 32 * t, go, a.D, lane);
-            // what is not stored, and rows that do not exist, add nothing
-            const uint32_t bits = (me.valid ? (uint32_t)(word >> (32 * t)) : 0u) >> (4 * (lane >> 5));
-            if (!POS) {
-#pragma unroll
-                for (int x = 0; x < 16; ++x) s[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x], cc, -off)) * (dp[x] - delta);
-                if (state != 2) {                        // a lane of no row keeps its own nonsense to itself
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) s[x] = attn_where(bits, 8 * (x >> 2) + (x & 3), s[x]);
-                }
-            } else {
-                // Loops of one kind of work each, without branches inside, so that the LDS's answers overlap.  A score of minus
-                // infinity has weight 0, whatever dP is.
-                const bool one = !a.buckets || near.far;
-                uint32_t there = 0;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) there |= (bits >> 8 * b & 15) << 4 * b;
-                if (near.ask) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) there &= ~((uint32_t)(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)] > qp) << x);
-                }
-                if (one) {
-                    const float all_of = a.buckets ? bias.at(near.place) : 0.f;
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) s[x] = __builtin_fmaf(s[x], a.scale, all_of);
-                } else
-                    attn_add_bias(bias, s, a.scale, [&](int x) { return kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)]; }, [&](int) { return qp; });
-                if (attn_any_lowest(s)) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) there &= ~((uint32_t)(s[x] == -INFINITY) << x);
-                }
-                float sum_x = 0, sum_p = 0, term[16], weight[16];
-#pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    weight[x] = attn_where(there, x, __builtin_amdgcn_exp2f(__builtin_fmaf(s[x] - off, cc, -log_sum)));
-                    s[x] = attn_where(there, x, weight[x] * (dp[x] - delta));
-                    term[x] = attn_where(there, x, weight[x] * (dp[x] - of_term));
-                    sum_x += term[x]; sum_p += weight[x];
-                }
-                if (hist && !one) {
-                    int place[16];
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) place[x] = bias.lut[bias.index(kp[8 * (x >> 2) + 4 * (lane >> 5) + (x & 3)], qp)];
-                    if (f.exact) attn_add_by_bucket<2>(hist, lane, place, term, weight);
-                    else attn_add_by_bucket<1>(hist, lane, place, term, weight);
-                }
-                if (hist && one) {
-                    const bool behind = near.place == a.side - 1;
-                    far_x[0] += behind ? sum_x : 0.f; far_p[0] += behind ? sum_p : 0.f;
-                    far_x[1] += behind ? 0.f : sum_x; far_p[1] += behind ? 0.f : sum_p;
-                }
-            }
-            if (sizeof(T) == 2) {
-#pragma unroll
-                for (int x = 0; x < 16; ++x) rest += s[x];
-            }
-            tile::add_rows(acc, sK, 32 * t, s, a.D, lane);
-        }
-    }
-    // For dkv_kernel.  The weights of a row that is whole here sum to 1, so what its ds miss to sum to 0 is the error of a D made of an O
-    // that was rounded to 16 bits.
+    walk(std::false_type());
+    // For dkv_kernel, and what short rows go through their steps twice for.  The weights of a row that is whole here sum to 1, so what its ds
+    // miss to sum to 0 is the error of a D made of an O that was rounded to 16 bits.
     rest = sizeof(T) == 2 && item.whole ? attn_pair_sum(rest) : 0.f;
     if (WN == 1 && me.valid && lane < 32 && item.c0 == item.chunk0) {
         f.delta[me.head * a.m + me.row] = delta + rest;
