@@ -288,7 +288,7 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
         }
     };
     // Short rows go through their steps twice, and the first time their ds only add up to what D misses.
-    if (sizeof(T) == 2 && item.whole && item.c1 - item.c0 <= kAttnTwice) {
+    if (sizeof(T) == 2 && item.whole && item.c1 - item.c0 <= kAttnTwice && p.rowptr[item.row0 + item.rows] - p.rowptr[item.row0] <= kAttnTwicePairs * item.rows) {
         walk(std::true_type());
         rest = attn_pair_sum(rest);
         __syncthreads();
@@ -339,11 +339,25 @@ __global__ __launch_bounds__(64 * WM * WN, DT * sizeof(T) <= 256 ? 2 : 1) void d
             s_delta[wave * 32 + lane] = d;
         }
         __syncthreads();
+        if (f.exact) {                                   // a row whose D is not a number adds nothing to the buckets that it has no weight in
+            bool odd = false;
+            for (int x = lane; x < (WN == 1 ? 32 * WM : 32); x += 64) odd = odd || !(s_delta[x] * 0.f == 0.f);
+            if (__builtin_amdgcn_ballot_w64(odd) != 0) { // the whole workgroup
+                const float d = s_delta[(WN == 1 ? wave : 0) * 32 + (lane & 31)];
+                for (int b = 0; b < places; ++b) {
+                    attn_lds_f32 *x = hist + (b * 64 + lane) * 2;
+                    if (x[1] != 0) x[0] -= d * x[1];
+                    x[1] = 0;
+                }
+                __syncthreads();
+                if (tid < 32 * WM) s_delta[tid] = 0;
+                __syncthreads();
+            }
+        }
         float *out = f.part_table + item.part * a.H * a.buckets;
         auto term = [&](int w, int b) {
             const attn_lds_f32 *x = all + w * hist_size + (b * 64 + lane) * (f.exact ? 2 : 1);
-            // (a row without weight in the bucket adds nothing to it, whatever its D is)
-            return f.exact && x[1] != 0 ? x[0] - s_delta[(WN == 1 ? w : 0) * 32 + (lane & 31)] * x[1] : x[0];
+            return f.exact ? x[0] - s_delta[(WN == 1 ? w : 0) * 32 + (lane & 31)] * x[1] : x[0];
         };
         for (int b = wave; b < places; b += WM * WN) {
             float sum = 0;

@@ -499,10 +499,12 @@ static constexpr int attn_dq_waves(int row_bytes, bool pos) { return row_bytes =
 // Columns of a step for four tiles.  64 take long enough to compute for the next ones to arrive; with the bias's sums in LDS, 32 leave
 // room for a second workgroup.
 static constexpr int attn_dq_columns(int row_bytes, bool pos) { return row_bytes <= (pos ? 64 : 256) ? 64 : 32; }
-// 16-bit rows of up to this many chunks are not cut in dq_kernel, and go through it twice: the first time for what their D misses, which is made
-// of an O that was rounded to 16 bits.  Beside dQ that error is the larger the fewer columns there are: rows of 20 to 30 have an error of
-// 2.8e-3 with it (bf16) and 2.35e-3 without, of which the roundings of ds and dQ make 1.65e-3 each; rows of 250 or more 2.4e-3 at most.
-constexpr int kAttnTwiceLevel = 2, kAttnTwice = 1 << kAttnTwiceLevel;
+// 16-bit rows of up to this many chunks are not cut in dq_kernel; where they also have no more pairs than this on average, a block's rows go
+// through it twice: the first time for what their D misses, which is made of an O that was rounded to 16 bits.  Beside dQ that error is
+// the larger the fewer pairs there are: in units of one rounding of dQ, rows of 20 to 30 have an error of 1.5 to 1.63 with it and of 1.42
+// (ds' rounding and dQ's) without; rows of 128 of 1.46 at most, and 16 sequences of 200 to 512 take 195.4 us instead of 191 if those of up to
+// 256 go twice.
+constexpr int kAttnTwiceLevel = 2, kAttnTwice = 1 << kAttnTwiceLevel, kAttnTwicePairs = 128;
 static inline size_t attn_dq_lds(const attn_args &a, const attn_mapping &c, int row_bytes, bool pos, bool table, bool exact)
 {
     const bool share = c.wn > 1;
