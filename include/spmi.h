@@ -171,7 +171,8 @@ sp_status sp_sddmm(const sp_tensor *S, const void *A, int64_t lda, const void *B
  *     s[i,j] = scale * sum_d Q[i,h,d] * K[j,g,d] + table[bucket(kpos[j] - qpos[i]), h]
  *     lse[h,i] = log sum_j exp(s[i,j]),   O[i,h,d] = sum_j exp(s[i,j] - lse[h,i]) * V[j,g,d]
  * A row that attends to nothing, or whose scores are all minus infinity, gives O = 0 and lse = minus infinity.  What a row does not
- * attend to has no influence on it, whatever it holds (infinities and NaN included).
+ * attend to has no influence on it, whatever it holds (infinities and NaN included).  A score of plus infinity, or one that is not a
+ * number, makes its row's O and lse NaN; a value that is not finite the numbers of O that it is in, and lse stays right.
  * A batch is a block-diagonal pattern: cross attention stores a rectangle for each sequence, of queries times states; tokens that
  * share a prefix store the same columns, which are then read once for all rows of a block.
  *
@@ -199,7 +200,9 @@ typedef struct sp_attention_problem {
  * cut into work items.  It serves any number of heads, any head size and type.  Synchronises `stream`; calling it again is a no-op.
  * S: a packed rank-2 tensor, row-major with a compressed innermost level (CSR or DCSR); other encodings give SP_ERR_UNSUPPORTED
  * (convert first).  Errors: NULL, RANK, UNSUPPORTED (also while `stream` is being recorded), TOO_LARGE (2^31 rows, columns or pairs of blocks and column
- * windows), ALLOC, HIP. */
+ * windows), ALLOC, HIP.  It takes 0.3 to 4 ms (with grad 0.6 to 7) for up to 40 million entries, tens of calls' worth: a pattern is
+ * meant to serve all layers and many steps.  One that changes with every token (tokens appended behind a prefix) is better packed with room
+ * and masked by positions. */
 sp_status sp_prepare_attention(sp_tensor *S, int grad, void *stream);
 
 /* Bytes of workspace that sp_attention (grad = 0) or sp_attention_grad (grad = 1) needs for this problem.  S must have been

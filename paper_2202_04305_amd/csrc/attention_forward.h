@@ -10,7 +10,7 @@ namespace {
 // (f32), and adds the weighted rows of V to its 32 x D sums, which stay in registers.  Weights are rounded to the operands' type
 // for that product (half a step of 16-bit types, as every operand of the matrix cores is); the sum that divides takes them unrounded.
 //
-// 16 sequences of 512 to 1024 queries over 2048 to 4096 keys, 16 heads of 128 over 4, bf16: 427 us, 749 TFLOP/s.  Of the cycles the matrix
+// 16 sequences of 512 to 1024 queries over 2048 to 4096 keys, 16 heads of 128 over 4, bf16: 419 us, 763 TFLOP/s.  Of the cycles the matrix
 // cores work 31 % and the vector units 47 %: an exponential takes four vector cycles, 32 of them a lane and step, beside 32 products,
 // and two waves a SIMD (256 registers each) overlap them only in part.  Single tokens are bound by the rows of K and V: 64 of them over
 // 800 to 1500 columns, 16 heads of 64, f16: 70 us, 4.1 TB/s.

@@ -376,8 +376,9 @@ sp_status build_plan(const sp_tensor *t, const sp_mem &mem, bool transposed, hip
     for (int k = 0; k < tried; ++k) { ways[k].chunks = host[2 * k]; ways[k].most = host[2 * k + 1]; }
     // What a block of rows costs for each of its chunks' columns: about 64 rows' worth of work to fetch it, and its rows' worth of work,
     // used or not.  A row by itself fetches its columns for itself, but makes one tile of all heads of a group, where a block makes one for
-    // each head: it is the better choice until a block of 32 rows has every column twice on average, as long as the rows all run at
-    // once; beyond about 512 of them, beginning and ending one costs as much as 400 columns (4096 rows of 96 columns out of 65,536, 8
+    // each head: it is the better choice until a block of 32 rows has every column twice on average, as long as the rows run at
+    // once.  How many do depends on the heads, which a plan does not know; beyond 512 rows, beginning and ending one is taken to cost as
+    // much as 400 columns (measured at these two: 4096 rows of 96 columns out of 65,536, 8
     // heads: 95 us in blocks of 32, 378 by themselves; 276 rows of 79 out of 17,791, 8 heads of one key head, f32: 54 and 38).
     // Whatever makes more blocks than a launch has workgroups is left out.
     auto fits = [](int64_t blocks) { return attn_launches(blocks, 256); };

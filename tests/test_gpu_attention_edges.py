@@ -403,3 +403,21 @@ def test_dq_of_short_rows_has_two_roundings(kind, heads, dt):
         say(k, float(error / one))
         assert float(error) <= 1.5 * float(one), (k, float(error / one))
     check(got, ref, kind)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("name", ["dense", "sparse", "one row", "tokens behind a prefix"])
+def test_a_score_of_infinity_makes_its_row_nan_and_no_other(name, dt):
+    at = PATTERNS[name]()
+    p = problem(at, 2, 1, 32, dt, train=False)
+    col = int((at.sum(0) + 1000 * (at.sum(0) == 0)).argmin())
+    p.Q[:, :, 0] = p.Q[:, :, 0].abs() + 4
+    p.K[col] = 0
+    p.K[col, :, 0] = 3e38
+    p.scale = 1.0
+    S = sp.sp_prepare_attention(pack(at))
+    got = run(S, p, False)
+    p.K[col] = 0
+    ref, rows = reference(p, False), ~at[:, col]
+    check({"O": got["O"][rows.to(DEV)], "lse": got["lse"][:, rows.to(DEV)]}, {"O": tuple(t[rows] for t in ref["O"]), "lse": tuple(t[:, rows] for t in ref["lse"])}, name)
+    assert bool(torch.isnan(got["O"][(~rows).to(DEV)]).all()) and bool(torch.isnan(got["lse"][:, (~rows).to(DEV)]).all())
