@@ -52,7 +52,8 @@ __device__ __forceinline__ void attn_add_by_bucket(attn_lds_f32 *hist, int lane,
 // takes the logarithm from it: of n scores of -3.4e38 (a bias of a type's lowest value) every weight would be 1, not 1 / n.  Up to kAttnNearLse
 // the rounding changes a weight by less than 2^-14 and is left alone (0); for tiles with a row beyond, the row's scores are made once more
 // here, by the same instructions in the same order as in the kernels' tiles, so the same bits.  (Where the steps of a score are 64 wide, one
-// that rounds to another step weighs e^64.)  Rows of K come straight from memory, a lane's as it needs them: such tiles are few.
+// that rounds to another step weighs e^64.)  Rows of K come straight from memory, a lane's as it needs them: such tiles are few.  (All of them,
+// by a bias 2048 higher, and the steps take 2.6 times as long: 16 sequences of 200 to 512, 12 heads of 64: 197 and 499 us.)
 constexpr float kAttnNearLse = 1024;
 template <typename T, int DT>
 __device__ __forceinline__ float attn_log_sum(const grad_args &f, const attn_item &item, const attn_lane &me, const typename attn_tile<T, DT>::frag (&q)[attn_tile<T, DT>::kSteps],

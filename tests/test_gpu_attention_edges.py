@@ -421,3 +421,31 @@ def test_a_score_of_infinity_makes_its_row_nan_and_no_other(name, dt):
     ref, rows = reference(p, False), ~at[:, col]
     check({"O": got["O"][rows.to(DEV)], "lse": got["lse"][:, rows.to(DEV)]}, {"O": tuple(t[rows] for t in ref["O"]), "lse": tuple(t[:, rows] for t in ref["lse"])}, name)
     assert bool(torch.isnan(got["O"][(~rows).to(DEV)]).all()) and bool(torch.isnan(got["lse"][:, (~rows).to(DEV)]).all())
+
+
+@pytest.mark.parametrize("buckets", [0, 8])
+def test_gradients_at_offsets_beyond_32_bits(buckets):
+    """Keys' rows more than 2^31 numbers behind the first, queries' rows 2^30 numbers apart, gradients among them; nothing else is written."""
+    n, ld, D, m = 150_000, 16_384, 32, 5
+    at = torch.zeros(m, n, dtype=torch.bool)
+    g = torch.Generator().manual_seed(9)
+    at[:, torch.randint(n, (60,), generator=g)] = True
+    at[:3, n - 40:] = True
+    at[3] = False
+    p = problem(at, 2, 1, D, BF16, buckets=buckets, positions=(torch.arange(m) * 30_000, torch.arange(n)), max_distance=2000)
+    S = sp.sp_prepare_attention(pack(at), grad=True)
+    wide = torch.empty(n * ld, dtype=BF16, device=DEV).view(n, ld)
+    K, V, dK, dV = (wide[:, o:o + D].unflatten(1, (1, D)) for o in (0, 64, 128, 192))
+    tall = torch.empty((m - 1) * (1 << 30) + 1024, dtype=BF16, device=DEV)
+    Q, dO, O, dQ = (tall.as_strided((m, 2, D), (1 << 30, D, 1), o) for o in (0, 128, 256, 384))
+    guard = [wide[:, o:o + 16] for o in (32, 96, 160, 224)] + [tall.as_strided((m, 32), (1 << 30, 1), o) for o in (64, 192, 320, 448)]
+    for t in guard:
+        t.fill_(7)
+    for t, x in ((K, p.K), (V, p.V), (Q, p.Q), (dO, p.dO)):
+        t.copy_(x.to(DEV))
+    o = p.options(DEV)
+    _, lse = sp.sp_attention(S, Q, K, V, O=O, **o)
+    _, _, _, dT = sp.sp_attention_grad(S, Q, K, V, O, lse, dO, dQ=dQ, dK=dK, dV=dV, **o)
+    ref = reference(p)
+    check({"O": O, "lse": lse, "dQ": dQ, "dK": dK, "dV": dV, **({"dT": dT} if buckets else {})}, ref)
+    assert all(bool((t == 7).all()) for t in guard)
