@@ -23,7 +23,7 @@ grad_choice choose(const sp_tensor *S, const attn_args &a, int size, bool table)
     grad_choice c;
     c.rows = attn_map(rows, a, size, 3);
     // short 16-bit rows stay whole (see kAttnTwice)
-    if (size == 2 && c.rows.level < kAttnTwiceLevel) c.rows.level = rows->levels - 1 < kAttnTwiceLevel ? rows->levels - 1 : kAttnTwiceLevel;
+    if (size == 2 && S->nvalues <= kAttnTwicePairs * a.m && c.rows.level < kAttnTwiceLevel) c.rows.level = rows->levels - 1 < kAttnTwiceLevel ? rows->levels - 1 : kAttnTwiceLevel;
     c.rows.cut = rows->cut[c.rows.level] > 0;
     // the bias's gradient from sums that need a row's whole D: rows are not cut then, unless a few long ones would hold up the rest for
     // longer than the whole pass takes, and the sums have to fit the LDS

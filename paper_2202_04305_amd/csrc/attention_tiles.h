@@ -499,12 +499,12 @@ static constexpr int attn_dq_waves(int row_bytes, bool pos) { return row_bytes =
 // Columns of a step for four tiles.  64 take long enough to compute for the next ones to arrive; with the bias's sums in LDS, 32 leave
 // room for a second workgroup.
 static constexpr int attn_dq_columns(int row_bytes, bool pos) { return row_bytes <= (pos ? 64 : 256) ? 64 : 32; }
-// 16-bit rows of up to this many chunks are not cut in dq_kernel; where they also have no more pairs than this on average, a block's rows go
-// through it twice: the first time for what their D misses, which is made of an O that was rounded to 16 bits.  Beside dQ that error is
+// 16-bit rows of up to this many pairs, on average over a block of up to this many chunks, go through dq_kernel twice: the first time for what
+// their D misses, which is made of an O that was rounded to 16 bits.  (A pattern of such rows is not cut finer.)  Beside dQ that error is
 // the larger the fewer pairs there are: in units of one rounding of dQ, rows of 20 to 30 have an error of 1.5 to 1.63 with it and of 1.42
 // (ds' rounding and dQ's) without; rows of 128 of 1.46 at most.  The second pass takes a tenth of such a step (64 sequences of 64 to 128: 52.4
 // and 58.1 us; 16384 rows of a band of 65: 224 and 260); 16 sequences of 200 to 512 would take 195.4 us instead of 191 with it up to 256.
-constexpr int kAttnTwiceLevel = 2, kAttnTwice = 1 << kAttnTwiceLevel, kAttnTwicePairs = 128;
+constexpr int kAttnTwiceLevel = 3, kAttnTwice = 1 << kAttnTwiceLevel, kAttnTwicePairs = 128;
 static inline size_t attn_dq_lds(const attn_args &a, const attn_mapping &c, int row_bytes, bool pos, bool table, bool exact)
 {
     const bool share = c.wn > 1;
