@@ -40,7 +40,7 @@ typedef enum {
 typedef enum { SP_DENSE = 0, SP_COMPRESSED = 1 } sp_level_type;
 typedef enum {
     SP_F32 = 0, SP_F64 = 1,  /* the values of a tensor and the operands of its products     */
-    SP_F16 = 2, SP_BF16 = 3  /* operands of sp_attention only: sp_pack refuses them         */
+    SP_F16 = 2, SP_BF16 = 3  /* operands of attention, rotary positions and the cache: sp_pack refuses them */
 } sp_dtype;
 #define SP_MAX_RANK 8
 
@@ -245,6 +245,120 @@ typedef struct sp_attention_grads {
 } sp_attention_grads;
 sp_status sp_attention_grad(const sp_tensor *S, const sp_attention_problem *p, const sp_attention_grads *g,
                             void *workspace, size_t workspaceBytes, void *stream);
+
+/* Rotary positions: pairs of numbers of a head, turned by an angle that grows with the token's position.  Pair k < rotDim / 2 is (x, y) =
+ * numbers (k, k + rotDim / 2) of the head, or (2k, 2k + 1) where interleaved = 1; numbers from rotDim on stay as they are.  With
+ * a = position * frequency[k]
+ *     x' = scale (x cos a - y sin a),   y' = scale (x sin a + y cos a)
+ * Angles are formed and brought into one turn in 64 bits, so positions may be any 32-bit numbers.  Q and K are two tensors that are turned
+ * in one launch (kvHeads = 0: Q alone).  An output may be its input (the same address and strides); otherwise outputs must not overlap
+ * each other or an input. */
+typedef struct sp_rotary_problem {
+    int dtype;                          /* SP_F32, SP_F16 or SP_BF16                                                     */
+    int headDim, rotDim;                /* rotDim: even, 0 .. headDim                                                    */
+    int interleaved;
+    double scale;                       /* finite in f32                                                                 */
+    int64_t tokens;
+    const int32_t *position;            /* DEVICE: tokens positions                                                      */
+    const double *frequency;            /* DEVICE: rotDim / 2 angles a position, in radians                              */
+    int heads, kvHeads;                 /* kvHeads may be 0                                                              */
+    const void *Q; int64_t ldq, hdq;    /* DEVICE: element (i, h, d) at Q[i * ldq + h * hdq + d]; strides >= 0           */
+    const void *K; int64_t ldk, hdk;
+    void *Qout; int64_t ldqo, hdqo;
+    void *Kout; int64_t ldko, hdko;
+} sp_rotary_problem;
+
+/* The frequencies base^(-2k / rotDim) for k < rotDim / 2 (HOST, 64 bits), for contexts longer than a model was trained on made smaller: by
+ * `factor` where trained = 0; otherwise with n = trained * frequency / (2 pi) turns in the trained length and c = (n - low) / (high - low) cut
+ * to [0, 1], (1 - c) / factor + c times as large: fast pairs stay, slow ones are stretched.  Errors: NULL, SHAPE (rotDim odd or negative;
+ * base or factor not positive and finite; trained negative; high <= low where trained > 0). */
+sp_status sp_rotary_frequencies(int rotDim, double base, double factor, int64_t trained, double low, double high, double *frequency /* HOST */);
+
+/* Turns Q and K; sp_rotary_grad: the gradients with respect to Q and K, given those with respect to the results in the places of Q and K (the
+ * same with -a for a).  Enqueues on `stream`; neither allocates nor synchronises.  Each result is rounded once.  Errors, in this order:
+ * NULL (p), DTYPE, SHAPE, UNSUPPORTED (interleaved neither 0 nor 1), NULL, HIP. */
+sp_status sp_rotary(const sp_rotary_problem *p, void *stream);
+sp_status sp_rotary_grad(const sp_rotary_problem *p, void *stream);
+
+/* A cache of keys and values held in 4 bits, in pages that requests own: in the storage's terms a dense level of requests, a compressed level of
+ * pages (a request's row of the block table has their numbers) and a dense level of the tokens of a page.  Slot s is token s % pageTokens of
+ * page s / pageTokens.  A token's head is cut into blocks of 32 numbers (the last one filled up with zeros) that share a power of two: the
+ * least 2^e with e in [-100, 125] that leaves the block's largest magnitude at 7 or below.  A number is held as one of 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * times 2^e with a sign: the nearest, of two as near the even one in that order, at most 6.  A block with a number that is not finite
+ * is NaN as a whole.  What a cache holds is exact in bf16 (and in f32).
+ * The caller owns the memory; one such cache for each layer, and one block table for all of them. */
+typedef struct sp_cache {
+    void *data;                         /* DEVICE, aligned to 256 bytes: sp_cache_bytes of it; any contents to begin with */
+    int64_t pages;                      /* pages * pageTokens < 2^31                                                     */
+    int pageTokens;                     /* a multiple of 16                                                              */
+    int kvHeads, headDim;               /* headDim 1 .. 256                                                              */
+} sp_cache;
+sp_status sp_cache_bytes(const sp_cache *c, size_t *bytes);
+
+/* The pages and slots of a step, from the requests' lengths, on the GPU.  Request r has length[r] tokens in its pages and gets added[r] more
+ * (negative numbers count as 0).  Pages that it needs for them are taken from freePages, in the order of requests and
+ * of positions, from number *taken on, and are appended to its row of the table.
+ *   start[r]      the first row of request r among the step's tokens, start[requests] their number
+ *   position, slot  of every token of the step, in order of requests
+ *   lengthOut[r]  length[r] + added[r];   *takenOut = *taken + pages needed
+ * Rows behind the last token up to `tokens` get position -1 and slot -1 (a batch padded to a size that graphs were recorded for); tokens behind
+ * row tokens - 1 get no row.  Where freePages ends (*takenOut > freeCount says so), where the table's row ends, or where a page's number is
+ * not in [0, pages), the table gets -1 where it has room and the tokens get slot -1, which sp_cache_store leaves out.
+ * The table is read and written in place; other outputs must not overlap each other or an input.  Enqueues on `stream`, one launch; neither
+ * allocates nor synchronises.  Sums must stay below 2^31.  Errors: NULL, SHAPE (pageTokens, negative sizes, ldt < width), TOO_LARGE (pages *
+ * pageTokens, requests or tokens of 2^31 or more), HIP. */
+typedef struct sp_cache_step {
+    int64_t requests, tokens;
+    int64_t pages;
+    int pageTokens;
+    const int32_t *length, *added;      /* DEVICE: requests numbers each                                                 */
+    const int32_t *freePages; int64_t freeCount;    /* DEVICE                                                            */
+    const int32_t *taken;               /* DEVICE: one number                                                            */
+    int32_t *table; int64_t ldt, width; /* DEVICE: requests rows of `width` pages, ldt >= width                          */
+    int32_t *lengthOut, *start;         /* DEVICE: requests and requests + 1 numbers                                     */
+    int32_t *position, *slot;           /* DEVICE: tokens numbers each                                                   */
+    int32_t *takenOut;                  /* DEVICE: one number                                                            */
+} sp_cache_step;
+sp_status sp_cache_map(const sp_cache_step *s, void *stream);
+
+/* Keys and values into the cache, and back: row i of K and V (element (i, g, d) at K[i * ldk + g * hdk + d], SP_F32, SP_F16 or SP_BF16) belongs to
+ * slot[i] (DEVICE).  Rows whose slot is not in [0, pages * pageTokens) are not stored, and are loaded as zeros.  No slot may be
+ * given twice in a call that stores (it would hold a mixture of the rows).  sp_cache_load rounds to `dtype` (SP_F32 and SP_BF16: exact).
+ * Enqueue on `stream`; neither allocate nor synchronise.  Errors, in this order: NULL (c), DTYPE, SHAPE, TOO_LARGE (pages * pageTokens or tokens of
+ * 2^31 or more), NULL, HIP. */
+sp_status sp_cache_store(const sp_cache *c, int dtype, int64_t tokens, const int32_t *slot, const void *K, int64_t ldk, int64_t hdk,
+                         const void *V, int64_t ldv, int64_t hdv, void *stream);
+sp_status sp_cache_load(const sp_cache *c, int dtype, int64_t tokens, const int32_t *slot, void *K, int64_t ldk, int64_t hdk,
+                        void *V, int64_t ldv, int64_t hdv, void *stream);
+
+/* Attention over the cache: a request's queries are the last n = start[r + 1] - start[r] of its length[r] tokens (the step's own are stored before
+ * the call), rows start[r] .. start[r + 1] - 1 of Q.  Query i of the request attends to the tokens t < length[r], with causal set only where
+ * t <= length[r] - n + i; for every head h, which reads head g = h / (heads / kvHeads) of the cache:
+ *     s[t] = scale * sum_d Q[i,h,d] * K[t,g,d],   lse[h,i] = log sum_t exp(s[t]),   O[i,h,d] = sum_t exp(s[t] - lse[h,i]) * V[t,g,d]
+ * Single tokens, prompts (or pieces of them) and mixtures of both are the same call.  Tokens whose page is not in [0, pages) and tokens behind
+ * width * pageTokens are not attended to.  Rows, infinities and NaN as for sp_attention: a row that attends to nothing gives O = 0 and lse =
+ * minus infinity, and what a row does not attend to has no influence on it, whatever it holds.  start ascends from 0 or more to `tokens` or
+ * less; rows that belong to no request are left as they were.
+ *   O    DEVICE: element (i, h, d) at O[i * ldo + h * hdo + d]; rows must not overlap each other or an input.
+ *   lse  DEVICE, heads x tokens, f32; may be NULL.
+ *   workspace  as for sp_attention: sp_cache_attention_workspace bytes, aligned to 256, one for each of the calls that may overlap.
+ * Enqueues on `stream`; neither allocates nor synchronises, reads lengths, rows and pages on the GPU (a recorded graph serves other ones), and
+ * gives the same bits on every call.  The numbers of the cache are exact in the products; Q is, too (in as many parts of bf16 as its type
+ * has room for); weights are rounded to Q's type before their product.  Errors, in this order: NULL (c, p), DTYPE, SHAPE, UNSUPPORTED (causal neither 0
+ * nor 1), TOO_LARGE (pages * pageTokens, tokens, or requests of 2^31 or more, or more workgroups than a launch has), NULL, SHAPE (workspace), HIP. */
+typedef struct sp_cache_problem {
+    int dtype;                          /* SP_F32, SP_F16 or SP_BF16: of Q and O                                         */
+    int heads;                          /* a multiple of the cache's kvHeads, at most 65535                              */
+    int causal;
+    double scale;                       /* scale / ln 2 has to be finite in f32                                          */
+    int64_t requests, tokens;           /* tokens: rows of Q                                                             */
+    const void *Q; int64_t ldq, hdq;    /* DEVICE: element (i, h, d) at Q[i * ldq + h * hdq + d]; strides >= 0           */
+    const int32_t *table; int64_t ldt, width;       /* DEVICE: requests rows of `width` pages, ldt >= width              */
+    const int32_t *length, *start;      /* DEVICE: requests and requests + 1 numbers                                     */
+} sp_cache_problem;
+sp_status sp_cache_attention_workspace(const sp_cache *c, const sp_cache_problem *p, size_t *bytes);
+sp_status sp_cache_attention(const sp_cache *c, const sp_cache_problem *p, void *O, int64_t ldo, int64_t hdo, float *lse,
+                             void *workspace, size_t workspaceBytes, void *stream);
 
 /* Matricized tensor times Khatri-Rao product A[i,j] = sum_{k,l} B[i,k,l] * D[l,j] * C[k,j] (Section 6.3, the MTTKRP
  * kernel), B a packed rank-3 tensor of shape I x K x L.

@@ -16,7 +16,8 @@ STATUS_NAMES = ["SP_OK", "SP_ERR_NULL", "SP_ERR_RANK", "SP_ERR_LEVEL_TYPE", "SP_
                 "SP_ERR_TOO_LARGE", "SP_ERR_ALLOC", "SP_ERR_HIP"]
 
 EXPORTS = ["sp_encode", "sp_encoding_free", "sp_pack", "sp_tensor_free", "sp_prepare", "sp_matmul", "sp_matmul_noalloc", "sp_pos", "sp_crd", "sp_values",
-           "sp_unpack", "sp_convert", "sp_sddmm", "sp_prepare_attention", "sp_attention_workspace", "sp_attention", "sp_attention_grad", "sp_mttkrp", "sp_spgemm", "sp_add", "sp_tensor_info", "sp_tensor_tune", "sp_profile_read", "sp_stream_copy", "sp_stream_read", "sp_pack_sort_mode", "sp_status_str", "sp_last_hip_error"]
+           "sp_unpack", "sp_convert", "sp_sddmm", "sp_prepare_attention", "sp_attention_workspace", "sp_attention", "sp_attention_grad", "sp_rotary", "sp_rotary_grad", "sp_rotary_frequencies",
+           "sp_cache_bytes", "sp_cache_map", "sp_cache_store", "sp_cache_load", "sp_cache_attention_workspace", "sp_cache_attention", "sp_mttkrp", "sp_spgemm", "sp_add", "sp_tensor_info", "sp_tensor_tune", "sp_profile_read", "sp_stream_copy", "sp_stream_read", "sp_pack_sort_mode", "sp_status_str", "sp_last_hip_error"]
 
 _ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p)
 _FREE_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_void_p)
@@ -46,6 +47,32 @@ class SpAttentionGrads(ctypes.Structure):
                 ("dK", ctypes.c_void_p), ("lddk", ctypes.c_int64), ("hddk", ctypes.c_int64),
                 ("dV", ctypes.c_void_p), ("lddv", ctypes.c_int64), ("hddv", ctypes.c_int64),
                 ("dTable", ctypes.c_void_p), ("lddt", ctypes.c_int64)]
+
+
+class SpRotaryProblem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("headDim", ctypes.c_int), ("rotDim", ctypes.c_int), ("interleaved", ctypes.c_int), ("scale", ctypes.c_double),
+                ("tokens", ctypes.c_int64), ("position", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("heads", ctypes.c_int), ("kvHeads", ctypes.c_int),
+                ("Q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("hdq", ctypes.c_int64),
+                ("K", ctypes.c_void_p), ("ldk", ctypes.c_int64), ("hdk", ctypes.c_int64),
+                ("Qout", ctypes.c_void_p), ("ldqo", ctypes.c_int64), ("hdqo", ctypes.c_int64),
+                ("Kout", ctypes.c_void_p), ("ldko", ctypes.c_int64), ("hdko", ctypes.c_int64)]
+
+
+class SpCache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("pageTokens", ctypes.c_int), ("kvHeads", ctypes.c_int), ("headDim", ctypes.c_int)]
+
+
+class SpCacheStep(ctypes.Structure):
+    _fields_ = [("requests", ctypes.c_int64), ("tokens", ctypes.c_int64), ("pages", ctypes.c_int64), ("pageTokens", ctypes.c_int),
+                ("length", ctypes.c_void_p), ("added", ctypes.c_void_p), ("freePages", ctypes.c_void_p), ("freeCount", ctypes.c_int64),
+                ("taken", ctypes.c_void_p), ("table", ctypes.c_void_p), ("ldt", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("lengthOut", ctypes.c_void_p), ("start", ctypes.c_void_p), ("position", ctypes.c_void_p), ("slot", ctypes.c_void_p), ("takenOut", ctypes.c_void_p)]
+
+
+class SpCacheProblem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("heads", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_double),
+                ("requests", ctypes.c_int64), ("tokens", ctypes.c_int64), ("Q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("hdq", ctypes.c_int64),
+                ("table", ctypes.c_void_p), ("ldt", ctypes.c_int64), ("width", ctypes.c_int64), ("length", ctypes.c_void_p), ("start", ctypes.c_void_p)]
 
 
 class SpError(RuntimeError):
@@ -109,6 +136,23 @@ def load_library():
     L.sp_attention.argtypes = [vp, problem, vp, i64, i64, vp, vp, size, vp]
     L.sp_attention_grad.restype = ci
     L.sp_attention_grad.argtypes = [vp, problem, grads, vp, size, vp]
+    L.sp_rotary_frequencies.restype = ci
+    L.sp_rotary_frequencies.argtypes = [ci, ctypes.c_double, ctypes.c_double, i64, ctypes.c_double, ctypes.c_double, vp]
+    for f in (L.sp_rotary, L.sp_rotary_grad):
+        f.restype = ci
+        f.argtypes = [ctypes.POINTER(SpRotaryProblem), vp]
+    cache, cached = ctypes.POINTER(SpCache), ctypes.POINTER(SpCacheProblem)
+    L.sp_cache_bytes.restype = ci
+    L.sp_cache_bytes.argtypes = [cache, ctypes.POINTER(size)]
+    L.sp_cache_map.restype = ci
+    L.sp_cache_map.argtypes = [ctypes.POINTER(SpCacheStep), vp]
+    for f in (L.sp_cache_store, L.sp_cache_load):
+        f.restype = ci
+        f.argtypes = [cache, ci, i64, vp, vp, i64, i64, vp, i64, i64, vp]
+    L.sp_cache_attention_workspace.restype = ci
+    L.sp_cache_attention_workspace.argtypes = [cache, cached, ctypes.POINTER(size)]
+    L.sp_cache_attention.restype = ci
+    L.sp_cache_attention.argtypes = [cache, cached, vp, i64, i64, vp, vp, size, vp]
     L.sp_convert.restype = ci
     L.sp_convert.argtypes = [vp, vp, vp, ctypes.POINTER(vp)]
     L.sp_tensor_info.restype = ci
@@ -453,6 +497,181 @@ def sp_attention_grad(S, Q, K, V, O, lse, dO, scale=None, causal=False, qpos=Non
         _check(L.sp_attention_grad(S._h, ctypes.byref(p), ctypes.byref(g), work.data_ptr() if size else None, size, _stream_ptr()), "in sp_attention_grad")
         return out[0], out[1], out[2], dbias
     return _attention_call(S, call)
+
+
+def _rotary(grad, position, frequencies, Q, K, interleaved, scale, Q_out, K_out):
+    L = load_library()
+    if Q.dtype not in _ATTENTION_DT:
+        raise SpError(9, "in sp_rotary: %s" % Q.dtype)
+
+    def call():
+        q = _rows_of_heads(Q, "Q", Q, Q.dtype)
+        (tokens, heads, d), half = Q.shape, frequencies.numel()
+        if position.dtype != torch.int32 or position.device != Q.device or tuple(position.shape) != (tokens,) or not position.is_contiguous():
+            raise ValueError("position: %d contiguous int32 positions on %s" % (tokens, Q.device))
+        if frequencies.dtype != torch.float64 or frequencies.device != Q.device or frequencies.dim() != 1 or not frequencies.is_contiguous():
+            raise ValueError("frequencies: contiguous float64 numbers on %s" % Q.device)
+        q_out = _attention_output(Q_out, Q, "Q_out")
+        qo, k, ko, k_out = _rows_of_heads(q_out, "Q_out", Q, Q.dtype), (None, 0, 0), (None, 0, 0), None
+        if K is not None:
+            k = _rows_of_heads(K, "K", Q, Q.dtype)
+            if K.shape[0] != tokens or K.shape[2] != d:
+                raise ValueError("K %s beside Q %s" % (tuple(K.shape), tuple(Q.shape)))
+            k_out = _attention_output(K_out, K, "K_out")
+            ko = _rows_of_heads(k_out, "K_out", Q, Q.dtype)
+        p = SpRotaryProblem(_ATTENTION_DT[Q.dtype], d, 2 * half, 1 if interleaved else 0, float(scale), tokens, position.data_ptr(),
+                            frequencies.data_ptr(), heads, 0 if K is None else K.shape[1], *q, *k, *qo, *ko)
+        f = L.sp_rotary_grad if grad else L.sp_rotary
+        _check(f(ctypes.byref(p), _stream_ptr()), "in sp_rotary_grad" if grad else "in sp_rotary")
+        return q_out if K is None else (q_out, k_out)
+    return _attention_call(Q, call)
+
+
+def sp_rotary(position, frequencies, Q, K=None, interleaved=False, scale=1.0, Q_out=None, K_out=None):
+    """Q (tokens, heads, d) and, if given, K (tokens, kv heads, d) with their pairs turned by position * frequencies (int32 positions, f64 angles a
+    position; the first 2 * len(frequencies) numbers of a head turn).  Returns the turned Q, or (Q, K): new tensors, or Q_out and K_out, which may
+    be Q and K."""
+    return _rotary(False, position, frequencies, Q, K, interleaved, scale, Q_out, K_out)
+
+
+def sp_rotary_grad(position, frequencies, dQ, dK=None, interleaved=False, scale=1.0, dQ_out=None, dK_out=None):
+    """The gradients with respect to sp_rotary's Q and K, given those with respect to its results (the same arguments otherwise)."""
+    return _rotary(True, position, frequencies, dQ, dK, interleaved, scale, dQ_out, dK_out)
+
+
+def sp_rotary_frequencies(rot_dim, base=10000.0, factor=1.0, trained=0, low=1.0, high=32.0, device=None):
+    """base^(-2k / rot_dim) for k < rot_dim / 2 as f64 on `device` (the current GPU unless given), made smaller by `factor` for long contexts:
+    all of them, or with trained > 0 those that make fewer than `high` turns in so many positions (wholly below `low`, partly between)."""
+    rot_dim = int(rot_dim)
+    f = (ctypes.c_double * max(1, rot_dim // 2))()
+    _check(load_library().sp_rotary_frequencies(rot_dim, float(base), float(factor), int(trained), float(low), float(high), f), "in sp_rotary_frequencies")
+    return torch.tensor(f[:rot_dim // 2], dtype=torch.float64, device="cuda" if device is None else device)
+
+
+class Cache:
+    """Keys and values in 4 bits: the pages' memory (`data`) and their description."""
+
+    def __init__(self, data, spec):
+        self.data, self._spec, self.device = data, spec, data.device
+        self._ref = ctypes.byref(spec)
+        self._workspaces = {}            # bytes of workspace of the attention problems met so far
+
+    pages = property(lambda self: self._spec.pages)
+    page_tokens = property(lambda self: self._spec.pageTokens)
+    kv_heads = property(lambda self: self._spec.kvHeads)
+    head_dim = property(lambda self: self._spec.headDim)
+
+
+def sp_cache(pages, page_tokens, kv_heads, head_dim, device=None):
+    """A cache of `pages` pages of page_tokens tokens (a multiple of 16), filled with zeros, on `device` (the current GPU unless given)."""
+    spec, size = SpCache(None, int(pages), int(page_tokens), int(kv_heads), int(head_dim)), ctypes.c_size_t()
+    _check(load_library().sp_cache_bytes(ctypes.byref(spec), ctypes.byref(size)), "in sp_cache")
+    data = torch.zeros(max(1, size.value), dtype=torch.uint8, device="cuda" if device is None else device)
+    spec.data = data.data_ptr()
+    return Cache(data, spec)
+
+
+def _whole_numbers(t, name, size, device):
+    """The address of `size` contiguous int32 numbers."""
+    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != (size,) or not t.is_contiguous():
+        raise ValueError("%s: %d contiguous int32 numbers on %s, not %s %s on %s" % (name, size, device, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+def _block_table(t, requests, device):
+    """The address, row stride and width of a block table."""
+    st = t.stride()
+    if t.dtype != torch.int32 or t.device != device or t.dim() != 2 or t.shape[0] != requests or (t.shape[1] > 1 and st[1] != 1):
+        raise ValueError("table: int32 pages (%d, width) on %s with contiguous rows, not %s %s strides %s on %s" % (
+            requests, device, t.dtype, tuple(t.shape), st, t.device))
+    return t.data_ptr(), st[0] if requests > 1 else max(st[0], t.shape[1]), t.shape[1]
+
+
+def sp_cache_map(lengths, added, free, taken, table, page_tokens, pages, tokens):
+    """The pages and slots of a step.  lengths, added: (requests) int32, what each request has in the cache and gets; free: int32 pages to hand
+    out, from number taken[0] on; table: (requests, width) int32, updated in place; tokens: rows of the step (sum of added, or more).
+    Returns (lengths + added, start (requests + 1), position (tokens), slot (tokens), taken)."""
+    L = load_library()
+
+    def call():
+        n, dev = lengths.shape[0], lengths.device
+        out = [torch.empty(k, dtype=torch.int32, device=dev) for k in (n, n + 1, int(tokens), int(tokens), 1)]
+        s = SpCacheStep(n, int(tokens), int(pages), int(page_tokens), _whole_numbers(lengths, "lengths", n, dev), _whole_numbers(added, "added", n, dev),
+                        _whole_numbers(free, "free", free.shape[0], dev), free.shape[0], _whole_numbers(taken, "taken", 1, dev),
+                        *_block_table(table, n, dev), *[t.data_ptr() for t in out])
+        _check(L.sp_cache_map(ctypes.byref(s), _stream_ptr()), "in sp_cache_map")
+        return tuple(out)
+    return _attention_call(lengths, call)
+
+
+def _cache_rows(cache, t, name, tokens, dtype):
+    row = _rows_of_heads(t, name, cache, dtype)
+    if tuple(t.shape) != (tokens, cache.kv_heads, cache.head_dim):
+        raise ValueError("%s: shape %s, not %s" % (name, (tokens, cache.kv_heads, cache.head_dim), tuple(t.shape)))
+    return row
+
+
+def sp_cache_store(cache, K, V, slots):
+    """K and V (tokens, kv heads, d), f32, f16 or bf16, into the cache's slots (int32; -1: not stored), in 4 bits."""
+    L = load_library()
+    if K.dtype not in _ATTENTION_DT:
+        raise SpError(9, "in sp_cache_store: %s" % K.dtype)
+
+    def call():
+        n = K.shape[0]
+        k, v = _cache_rows(cache, K, "K", n, K.dtype), _cache_rows(cache, V, "V", n, K.dtype)
+        _check(L.sp_cache_store(cache._ref, _ATTENTION_DT[K.dtype], n, _whole_numbers(slots, "slots", n, cache.device), *k, *v, _stream_ptr()), "in sp_cache_store")
+    _attention_call(cache, call)
+
+
+def sp_cache_load(cache, slots, dtype=torch.bfloat16, K=None, V=None):
+    """What the cache's slots hold (int32; -1: zeros): K and V (tokens, kv heads, d) of `dtype`, new tensors or the given ones."""
+    L = load_library()
+    if dtype not in _ATTENTION_DT:
+        raise SpError(9, "in sp_cache_load: %s" % dtype)
+
+    def call():
+        n = slots.shape[0]
+        out = [torch.empty(n, cache.kv_heads, cache.head_dim, dtype=dtype, device=cache.device) if t is None else t for t in (K, V)]
+        k, v = _cache_rows(cache, out[0], "K", n, dtype), _cache_rows(cache, out[1], "V", n, dtype)
+        _check(L.sp_cache_load(cache._ref, _ATTENTION_DT[dtype], n, _whole_numbers(slots, "slots", n, cache.device), *k, *v, _stream_ptr()), "in sp_cache_load")
+        return out[0], out[1]
+    return _attention_call(cache, call)
+
+
+def sp_cache_attention(cache, Q, table, lengths, start, scale=None, causal=True, O=None, lse=None):
+    """Attention over the cache.  Q: (tokens, heads, d), f32, f16 or bf16; request r's queries are rows start[r] .. start[r + 1] - 1, the last of its
+    lengths[r] tokens in the pages of table[r] (all int32); scale: 1 / sqrt(d) unless given.  Returns O (tokens, heads, d) and lse (heads, tokens)
+    f32; rows of no request are left as they were."""
+    L = load_library()
+    if Q.dtype not in _ATTENTION_DT:
+        raise SpError(9, "in sp_cache_attention: %s" % Q.dtype)
+
+    def call():
+        dev, dt = cache.device, Q.dtype
+        q = _rows_of_heads(Q, "Q", cache, dt)
+        tokens, heads, d = Q.shape
+        if d != cache.head_dim:
+            raise ValueError("Q %s for a cache of heads of %d" % (tuple(Q.shape), cache.head_dim))
+        n = lengths.shape[0]
+        at = _block_table(table, n, dev)
+        p = SpCacheProblem(_ATTENTION_DT[dt], heads, 1 if causal else 0, float(d) ** -0.5 if scale is None else float(scale), n, tokens, *q,
+                           *at, _whole_numbers(lengths, "lengths", n, dev), _whole_numbers(start, "start", n + 1, dev))
+        out = _attention_output(O, Q, "O")
+        logs = torch.empty((heads, tokens), dtype=torch.float32, device=dev) if lse is None else lse
+        if lse is not None and (tuple(lse.shape) != (heads, tokens) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev):
+            raise ValueError("lse: a contiguous f32 tensor of (heads, tokens)")
+        o = _rows_of_heads(out, "O", cache, dt)
+        key = (dt, heads, n, tokens, at[2])
+        size = cache._workspaces.get(key)
+        if size is None:
+            need = ctypes.c_size_t()
+            _check(L.sp_cache_attention_workspace(cache._ref, ctypes.byref(p), ctypes.byref(need)), "in sp_cache_attention")
+            size = cache._workspaces[key] = need.value
+        work = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+        _check(L.sp_cache_attention(cache._ref, ctypes.byref(p), *o, logs.data_ptr(), work.data_ptr() if size else None, size, _stream_ptr()), "in sp_cache_attention")
+        return out, logs
+    return _attention_call(cache, call)
 
 
 def sp_mttkrp(B, C, D, A=None, accumulate=False):
