@@ -1,0 +1,703 @@
+// Attention over the 4-bit cache: the kernels (cache_attention_*.hip instantiate them, cache_attention.hip calls them).
+//
+// Scores are computed transposed, S^T = K Q^T, in 16 x 16 tiles of the matrix cores (v_mfma_f32_16x16x32_bf16): a column is a query and
+// head, a row a token.  Lane l of a wave has column l % 16 and rows 4 (l / 16) .. + 3 of a tile, so a column's weights are, as they lie,
+// the second operand of O^T = V^T P^T over the 32 tokens of two tiles.  The cache's layout is that of the first operands: a lane turns the
+// words that it loads into bf16 (v_cvt_scalef32_pk_bf16_fp4, which multiplies by the block's power of two), and keys and values go
+// from memory to the matrix cores without passing the LDS.
+#pragma once
+#include "cache.h"
+#include <math.h>
+
+constexpr float kCacheLog2e = 1.4426950408889634f, kCacheLn2 = 0.6931471805599453f;
+
+struct cache_attn_args {
+    cache_view c;
+    const void *Q;
+    void *O;
+    float *lse;
+    const int32_t *table, *length, *start;
+    int64_t ldq, hdq, ldo, hdo, ldt, width, requests, tokens;
+    int H, R, causal;                    // R = H / G heads share a head of the cache
+    float scale, step;                   // step = |scale| log2(e); the scale's sign goes into Q
+    int vec;                             // rows of Q and O are aligned to 8 numbers
+    uint32_t page_mul, page_shift;       // records of a page: x / (P / 16) = mulhi(x, page_mul) >> page_shift, or x >> page_shift where page_mul = 0
+    float *part;                         // workspace: [slot][head of the cache][column][32 nb] sums
+    float2 *stat;                        //            [slot][head of the cache][column]: running maximum (in units of log 2) and total
+    uint32_t slots;                      // slots there is room for
+};
+
+// ---- work ------------------------------------------------------------------------------------------------------------------
+// The columns of a request (its queries times the heads that share a head of the cache) are cut into tiles, its tokens into chunks, and an
+// item is a tile, a chunk and a head of the cache.  Lengths are known on the GPU alone, so every workgroup finds its item by a scan over
+// the requests.  Chunks are as long as makes about kCacheTarget items of all work, at least kCacheLeast tokens.
+constexpr int kCacheTarget = 1024, kCacheLeast = 256;
+
+struct cache_request { uint32_t n, columns, tiles, tokens; int64_t last; };         // last: position of the last query
+struct cache_item {
+    int64_t r, row0;                     // request; its first row
+    cache_request q;
+    uint32_t tile, chunk, chunks, slot;  // slot: of the tile's first chunk; the next one's is q.tiles further on
+};
+
+static inline __host__ __device__ int64_t cache_limit(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+__device__ __forceinline__ cache_request cache_request_of(const cache_attn_args &a, int64_t r, int cols)
+{
+    cache_request q = {0, 0, 0, 0, 0};
+    if (r >= a.requests) return q;
+    const int64_t s0 = cache_limit(a.start[r], 0, a.tokens), s1 = cache_limit(a.start[r + 1], 0, a.tokens), len = a.length[r];
+    if (s1 <= s0) return q;
+    q.n = (uint32_t)(s1 - s0);
+    q.columns = q.n * (uint32_t)a.R;
+    q.tiles = (q.columns + cols - 1) / cols;
+    q.tokens = (uint32_t)cache_limit(len, 0, a.width * a.c.P);
+    q.last = len - 1;
+    return q;
+}
+
+__device__ __forceinline__ uint32_t cache_wave_scan(uint32_t v, int lane)           // sum of lanes 0 .. lane
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { const uint32_t o = __shfl_up(v, d, 64); v += lane >= d ? o : 0; }
+    return v;
+}
+
+// Tokens of a chunk: by the work of all requests.
+__device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a, int cols, int lane)
+{
+    uint64_t work = 0;
+    for (int64_t r = lane; r < a.requests; r += 64) {
+        const cache_request q = cache_request_of(a, r, cols);
+        work += (uint64_t)q.tiles * q.tokens;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) work += __shfl_xor(work, d, 64);
+    const uint64_t c = (work * a.c.G + kCacheTarget - 1) / kCacheTarget;
+    return c < kCacheLeast ? kCacheLeast : c > 0x7fffff00u ? 0x7fffff00u : ((uint32_t)c + 127) & ~127u;
+}
+// Chunks longer than the work's share make fewer than 2 kCacheTarget / G slots: a request of more than one has chunks < 2 tokens / length.
+static inline int64_t cache_slots(int G) { return ceil_div(2 * kCacheTarget, G); }
+
+// Item `index` of all (joined = false), or tile `index` of those that have more than one chunk.  For a whole wave; false: there is none.
+__device__ __forceinline__ bool cache_find(const cache_attn_args &a, int cols, uint32_t index, bool joined, int lane, cache_item *item)
+{
+    const uint32_t len = __builtin_amdgcn_readfirstlane(cache_chunk_tokens(a, cols, lane));
+    uint32_t items = 0, slots = 0;
+    for (int64_t base = 0; base < a.requests; base += 64) {
+        const cache_request q = cache_request_of(a, base + lane, cols);
+        const uint32_t chunks = q.tokens <= len ? 1 : (q.tokens + len - 1) / len;
+        const uint32_t mine = joined ? (chunks > 1 ? q.tiles : 0) : q.tiles * chunks, room = chunks > 1 ? q.tiles * chunks : 0;
+        const uint32_t upto = items + cache_wave_scan(mine, lane), slot = slots + cache_wave_scan(room, lane);
+        const uint64_t behind = __builtin_amdgcn_ballot_w64(upto > index);
+        if (behind) {
+            const int k = __builtin_ctzll(behind);
+            auto of = [k](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, k); };
+            const uint32_t rest = index - (of(upto) - of(mine));
+            item->r = base + k;
+            item->row0 = cache_limit(a.start[item->r], 0, a.tokens);
+            item->q.n = of(q.n); item->q.columns = of(q.columns); item->q.tiles = of(q.tiles); item->q.tokens = of(q.tokens);
+            item->q.last = (int64_t)a.length[item->r] - 1;
+            item->chunks = of(chunks);
+            item->tile = rest % item->q.tiles;
+            item->chunk = rest / item->q.tiles;
+            item->slot = of(slot) - of(room) + item->tile;
+            return item->tile < item->q.tiles && item->chunk < item->chunks;
+        }
+        items = __builtin_amdgcn_readlane(upto, 63);
+        slots = __builtin_amdgcn_readlane(slot, 63);
+    }
+    return false;
+}
+
+// ---- one column by itself ---------------------------------------------------------------------------------------------------
+
+constexpr int kCachePer = 4;             // numbers of a lane: head sizes up to 256
+
+__device__ __forceinline__ float cache_wave_sum(float v)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// top (running maximum, in units of log 2), total and acc = sum of 2^(s - top) V over the tokens [t0, t1) of request r, for one row and head; a
+// wave, lanes across the head's numbers.  Every token is looked at alone, so that nothing that the row does not attend to can reach it: the
+// tiles fall back on it where a sum is not finite, as a token that other columns attend to is multiplied with zero there, which
+// infinities and NaN survive.
+template <typename T>
+__device__ __forceinline__ void cache_row(const cache_attn_args &a, int64_t r, int64_t i, int h, uint32_t t0, uint32_t t1, int lane,
+                                       float &top, float &total, float (&acc)[kCachePer])
+{
+    const int g = h / a.R, D = a.c.D;
+    const T *row = (const T *)a.Q + i * a.ldq + h * a.hdq;
+    const float step = a.scale < 0 ? -a.step : a.step;
+    float q[kCachePer];
+#pragma unroll
+    for (int k = 0; k < kCachePer; ++k) { q[k] = lane + 64 * k < D ? (float)row[lane + 64 * k] : 0.f; acc[k] = 0; }
+    top = -INFINITY; total = 0;
+#pragma unroll 1
+    for (uint32_t t = t0; t < t1; ++t) {
+        const int64_t page = a.table[r * a.ldt + t / (uint32_t)a.c.P];
+        if (page < 0 || page >= a.c.pages) continue;
+        const int u = (int)(t % (uint32_t)a.c.P);
+        const uint8_t *rec = a.c.record(page, g, u);
+        float s = 0;
+#pragma unroll
+        for (int k = 0; k < kCachePer; ++k) if (lane + 64 * k < D) s += q[k] * cache_key(a.c, rec, u % kCacheTile, lane + 64 * k);
+        s = cache_wave_sum(s) * step;
+        if (s == -INFINITY) continue;                    // weight 0
+        const float up = s > top ? s : top;              // not a number: stays with the old maximum, the weight carries it
+        const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - up), w = __builtin_amdgcn_exp2f(s - (up == -INFINITY ? 0.f : up));
+        top = up;
+        total = total * old + w;
+#pragma unroll
+        for (int k = 0; k < kCachePer; ++k) if (lane + 64 * k < D) acc[k] = acc[k] * old + w * cache_value(a.c, rec, u % kCacheTile, lane + 64 * k);
+    }
+}
+
+// ---- tiles ------------------------------------------------------------------------------------------------------------------
+
+typedef float cache_f4 __attribute__((ext_vector_type(4)));
+typedef __bf16 cache_b8 __attribute__((ext_vector_type(8)));
+typedef __bf16 cache_b2 __attribute__((ext_vector_type(2)));
+typedef uint32_t cache_u4 __attribute__((ext_vector_type(4)));
+
+// Q and weights as sums of bf16 numbers: 8 bits each, so that three hold all of f32.
+template <typename T> struct cache_parts { static constexpr int n = sizeof(T) == 4 ? 3 : 2; };
+template <> struct cache_parts<cache_bf16> { static constexpr int n = 1; };
+
+template <int N>
+__device__ __forceinline__ void cache_words(const uint8_t *p, uint32_t (&w)[N])     // 4-byte aligned
+{
+    typedef uint32_t v4 __attribute__((ext_vector_type(4), aligned(4)));
+    typedef uint32_t v2 __attribute__((ext_vector_type(2), aligned(4)));
+    const uint32_t *x = (const uint32_t *)p;
+    int k = 0;
+#pragma unroll
+    for (; k + 4 <= N; k += 4) { const v4 v = *(const v4 *)(x + k); w[k] = v[0]; w[k + 1] = v[1]; w[k + 2] = v[2]; w[k + 3] = v[3]; }
+    if constexpr (N % 4 >= 2) { const v2 v = *(const v2 *)(x + k); w[k] = v[0]; w[k + 1] = v[1]; k += 2; }
+    if constexpr (N % 2) w[k] = x[k];
+}
+template <int BYTE>
+__device__ __forceinline__ uint32_t cache_convert(uint32_t word, float scale)       // two codes -> two numbers
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, BYTE));
+}
+__device__ __forceinline__ uint32_t cache_pair(float x, float y)                    // rounded to bf16
+{
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){x, y}, cache_b2));
+}
+
+// What a lane holds of 32 tokens: of each half its words of K and V and their scales.
+template <int NB>
+struct cache_tokens {
+    static constexpr int SB = NB <= 2 ? NB : NB <= 4 ? 4 : 8, KS = (SB + 3) / 4;
+    uint32_t k[2][NB], v[2][NB], ks[2][KS], vs[2][SB];
+    __device__ __forceinline__ void load(const uint8_t *rec, int half, int lane)
+    {
+        constexpr int record = 512 * NB;
+        const int t = lane & 15, g = lane >> 4;
+        cache_words(rec + (t * 4 + g) * (NB * 4), k[half]);
+        if constexpr (SB == 1) ks[half][0] = rec[record + t];
+        else if constexpr (SB == 2) ks[half][0] = *(const uint16_t *)(rec + record + t * 2);
+        else cache_words(rec + record + t * SB, ks[half]);
+        cache_words(rec + 256 * NB + (g * 16 + t) * (NB * 4), v[half]);
+        cache_words(rec + record + 16 * SB + g * 4 * SB, vs[half]);
+    }
+    __device__ __forceinline__ float k_scale(int half, int s) const { return __uint_as_float(((ks[half][s / 4] >> (8 * (s % 4))) & 255) << 23); }
+    __device__ __forceinline__ float v_scale(int half, int token, int s) const
+    {
+        const int b = token * SB + s;
+        return __uint_as_float(((vs[half][b / 4] >> (8 * (b % 4))) & 255) << 23);
+    }
+};
+
+// 16 NQ columns of one tile over some of its tokens, by one wave.
+template <typename T, int NB, int NQ>
+struct cache_wave {
+    static constexpr int parts = cache_parts<T>::n;
+    cache_b8 q[NQ][parts][NB];
+    cache_f4 o[NQ][2 * NB];
+    float top[NQ], mu[NQ], total[NQ];    // running maximum (the same in the four lanes of a column); what is taken off; a lane's own share of the total
+    uint32_t end[NQ];                    // the column attends to tokens before this one
+
+    // Q's column: 8 numbers of every block
+    __device__ __forceinline__ void load_q(const cache_attn_args &a, const cache_item &it, uint32_t first, int g, int lane)
+    {
+        const int D = a.c.D;
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+            const uint32_t col = first + 16 * k + (lane & 15);
+            const bool there = col < it.q.columns;
+            const uint32_t i = there ? col / (uint32_t)a.R : 0, hh = there ? col % (uint32_t)a.R : 0;
+            const T *row = (const T *)a.Q + (it.row0 + i) * a.ldq + (int64_t)(g * a.R + hh) * a.hdq;
+            const int64_t e = a.causal ? it.q.last - it.q.n + 2 + i : (int64_t)it.q.tokens;
+            end[k] = there ? (uint32_t)cache_limit(e, 0, it.q.tokens) : it.q.tokens;
+            top[k] = -INFINITY; mu[k] = 0; total[k] = 0;
+#pragma unroll
+            for (int s = 0; s < 2 * NB; ++s) o[k][s] = (cache_f4)(0.f);
+#pragma unroll
+            for (int s = 0; s < NB; ++s) {
+                const int d0 = 32 * s + 8 * (lane >> 4);
+                float x[8];
+                if (a.vec) {
+                    typedef T row8 __attribute__((ext_vector_type(8)));
+                    row8 v = {};
+                    if (there && d0 < D) v = *(const row8 *)(row + d0);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = there && d0 + j < D ? (float)row[d0 + j] : 0.f;
+                }
+                // cut off (not rounded) to 8 bits, part after part: nothing is lost and nothing overflows
+                uint32_t w[parts][4] = {};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float y = a.scale < 0 ? -x[j] : x[j];
+                    const bool finite = y - y == 0;
+#pragma unroll
+                    for (int p = 0; p < parts; ++p) {
+                        uint32_t u = __float_as_uint(y);
+                        if (p == 0 && !finite) u = y == y ? u : 0x7fc00000u;
+                        if (p > 0 && !finite) u = 0;
+                        w[p][j / 2] |= j % 2 ? u & 0xffff0000u : u >> 16;
+                        y -= __uint_as_float(u & 0xffff0000u);
+                    }
+                }
+#pragma unroll
+                for (int p = 0; p < parts; ++p) q[k][p][s] = __builtin_bit_cast(cache_b8, (cache_u4){w[p][0], w[p][1], w[p][2], w[p][3]});
+            }
+        }
+    }
+
+    // 32 tokens from t on.  MASKED: some column attends to some of them only; there: which halves' pages exist; tokens: the request's
+    template <bool MASKED>
+    __device__ __forceinline__ void tokens32(const cache_tokens<NB> &x, float step, uint32_t t, uint32_t tokens, uint32_t there, int lane)
+    {
+        const int g = lane >> 4;
+        cache_f4 s[NQ][2];
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) s[k][0] = s[k][1] = (cache_f4)(0.f);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const float f = x.k_scale(half, b);
+                const uint32_t w = x.k[half][b];
+                const cache_b8 key = __builtin_bit_cast(cache_b8, (cache_u4){cache_convert<0>(w, f), cache_convert<1>(w, f), cache_convert<2>(w, f), cache_convert<3>(w, f)});
+#pragma unroll
+                for (int k = 0; k < NQ; ++k)
+#pragma unroll
+                    for (int p = 0; p < parts; ++p) s[k][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[k][p][b], s[k][half], 0, 0, 0);
+            }
+        cache_b8 w[NQ][parts];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+            // The maximum that is taken off lags behind by up to 8 (a factor of 256): moving it costs a pass over the sums, and it moves in
+            // the first tokens of a chunk, hardly later.
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                y[j] = s[k][j / 4][j % 4];
+                if (MASKED) {
+                    const uint32_t at = t + 16 * (j / 4) + 4 * g + j % 4;
+                    y[j] = at < end[k] && ((there >> (j / 4)) & 1) ? y[j] * step : -INFINITY;
+                }
+            }
+            float most = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+            if (!MASKED) most *= step;
+            if (__builtin_amdgcn_ballot_w64(most > top[k] + 8)) {
+                most = fmaxf(most, __shfl_xor(most, 16, 64));
+                most = fmaxf(most, __shfl_xor(most, 32, 64));
+                const float up = fmaxf(top[k], most), now = up == -INFINITY ? 0.f : up;
+                const float f = top[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mu[k] - now);
+                top[k] = up; mu[k] = now;
+                total[k] *= f;
+#pragma unroll
+                for (int b = 0; b < 2 * NB; ++b) o[k][b] *= f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(MASKED ? y[j] - mu[k] : __builtin_fmaf(y[j], step, -mu[k]));
+            total[k] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+#pragma unroll
+            for (int p = 0; p < parts; ++p) {
+                cache_u4 u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    u[j] = cache_pair(y[2 * j], y[2 * j + 1]);
+                    y[2 * j] -= __uint_as_float(u[j] << 16);
+                    y[2 * j + 1] -= __uint_as_float(u[j] & 0xffff0000u);
+                }
+                w[k][p] = __builtin_bit_cast(cache_b8, u);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            uint32_t lo[4], hi[4];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float f[4];
+                uint32_t word = x.v[half][b];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    f[j] = x.v_scale(half, j, b);
+                    if (MASKED && (t + 16 * half + 4 * g + j >= tokens || !((there >> half) & 1))) {      // behind the request's tokens: anything may be there
+                        f[j] = 1.f;
+                        word &= ~(255u << (8 * j));
+                    }
+                }
+                const uint32_t c0 = cache_convert<0>(word, f[0]), c1 = cache_convert<1>(word, f[1]), c2 = cache_convert<2>(word, f[2]), c3 = cache_convert<3>(word, f[3]);
+                lo[2 * half] = __builtin_amdgcn_perm(c1, c0, 0x05040100);
+                lo[2 * half + 1] = __builtin_amdgcn_perm(c3, c2, 0x05040100);
+                hi[2 * half] = __builtin_amdgcn_perm(c1, c0, 0x07060302);
+                hi[2 * half + 1] = __builtin_amdgcn_perm(c3, c2, 0x07060302);
+            }
+            const cache_b8 vl = __builtin_bit_cast(cache_b8, (cache_u4){lo[0], lo[1], lo[2], lo[3]});
+            const cache_b8 vh = __builtin_bit_cast(cache_b8, (cache_u4){hi[0], hi[1], hi[2], hi[3]});
+#pragma unroll
+            for (int k = 0; k < NQ; ++k)
+#pragma unroll
+                for (int p = 0; p < parts; ++p) {
+                    o[k][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vl, w[k][p], o[k][2 * b], 0, 0, 0);
+                    o[k][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vh, w[k][p], o[k][2 * b + 1], 0, 0, 0);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    // The tokens from t on, 32 at a time every `stride`, up to `to`; `whole`: all columns attend to all tokens before it.
+    __device__ __forceinline__ void run(const cache_attn_args &a, const cache_item &it, int g, uint32_t t, uint32_t stride, uint32_t to, uint32_t whole, int lane)
+    {
+        if (t >= to) return;
+        const int32_t *table = a.table + it.r * a.ldt;
+        const uint32_t per = (uint32_t)a.c.P / kCacheTile;
+        const int64_t head = (int64_t)per * a.c.lay.record();
+        auto page_of = [&](uint32_t record) { return a.page_mul ? __umulhi(record, a.page_mul) >> a.page_shift : record >> a.page_shift; };
+        auto pages = [&](uint32_t at, int32_t (&p)[2]) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint32_t n = page_of(at / kCacheTile + half);
+                p[half] = n < a.width ? table[n] : -1;
+            }
+        };
+        auto fetch = [&](uint32_t at, const int32_t (&p)[2], cache_tokens<NB> &x) {
+            uint32_t there = 0;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint32_t record = at / kCacheTile + half, in = record - page_of(record) * per;
+                const bool ok = p[half] >= 0 && p[half] < a.c.pages;
+                there |= ok ? 1u << half : 0;
+                x.load(a.c.data + (ok ? (p[half] * (int64_t)a.c.G + g) * head + in * (int64_t)a.c.lay.record() : 0), half, lane);
+            }
+            return there;
+        };
+        int32_t p[2];
+        cache_tokens<NB> now, next;
+        pages(t, p);
+        uint32_t there = fetch(t, p, now);
+        pages(t + stride, p);
+        while (true) {
+            const bool more = t + stride < to;
+            uint32_t next_there = 0;
+            if (more) {
+                next_there = fetch(t + stride, p, next);
+                pages(t + 2 * stride, p);
+            }
+            if (t + 32 <= whole && there == 3) tokens32<false>(now, a.step, t, it.q.tokens, there, lane);
+            else tokens32<true>(now, a.step, t, it.q.tokens, there, lane);
+            if (!more) break;
+            now = next;
+            there = next_there;
+            t += stride;
+        }
+    }
+};
+
+// The tokens of an item and of them those that its columns, `first` and `count - 1` more, attend to.
+struct cache_span { uint32_t from, to, whole; };
+__device__ __forceinline__ cache_span cache_span_of(const cache_attn_args &a, const cache_item &it, uint32_t first, uint32_t count)
+{
+    const uint32_t each = it.chunks == 1 ? it.q.tokens : ((it.q.tokens + it.chunks - 1) / it.chunks + 31) & ~31u;
+    cache_span s;
+    const uint64_t from = (uint64_t)it.chunk * each, to = from + each;
+    s.from = (uint32_t)(from < it.q.tokens ? from : it.q.tokens);
+    s.to = (uint32_t)(to < it.q.tokens ? to : it.q.tokens);
+    s.whole = it.q.tokens;
+    if (a.causal) {
+        const int64_t before = it.q.last - it.q.n + 2;   // what the request's first query attends to, at least
+        const uint32_t end = (uint32_t)cache_limit(before + (first + count - 1) / (uint32_t)a.R, 0, it.q.tokens);
+        s.whole = (uint32_t)cache_limit(before + first / (uint32_t)a.R, 0, it.q.tokens);
+        if (end < s.to) s.to = end;
+    }
+    return s;
+}
+
+// A column's result: O and lse, or a part of them for the join.
+template <typename T, int NB>
+struct cache_column {
+    T *out;
+    float *lse, *part;
+    float2 *stat;
+    __device__ __forceinline__ cache_column(const cache_attn_args &a, const cache_item &it, int g, uint32_t col, uint32_t cols)
+    {
+        const uint32_t i = col / (uint32_t)a.R, h = g * a.R + col % (uint32_t)a.R;
+        out = (T *)a.O + (it.row0 + i) * a.ldo + (int64_t)h * a.hdo;
+        lse = a.lse ? a.lse + (int64_t)h * a.tokens + it.row0 + i : nullptr;
+        const int64_t at = ((int64_t)(it.slot + it.chunk * it.q.tiles) * a.c.G + g) * cols + col % cols;
+        part = it.chunks > 1 ? a.part + at * (32 * NB) : nullptr;
+        stat = a.stat + at;
+    }
+    __device__ __forceinline__ void numbers(const cache_attn_args &a, int d, cache_f4 x, float total) const       // d a multiple of 4
+    {
+        if (part) { *(cache_f4 *)(part + d) = x; return; }
+        const float f = total == 0 ? 0.f : 1 / total;
+        typedef T v4 __attribute__((ext_vector_type(4)));
+        if (a.vec) { if (d < a.c.D) *(v4 *)(out + d) = (v4){(T)(x[0] * f), (T)(x[1] * f), (T)(x[2] * f), (T)(x[3] * f)}; }
+        else
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (d + j < a.c.D) out[d + j] = (T)(x[j] * f);
+    }
+    __device__ __forceinline__ void total(float top, float sum) const
+    {
+        if (part) *stat = {top, sum};
+        else if (lse) *lse = sum == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kCacheLn2;
+    }
+};
+
+// A column whose sums are not finite although its total is, made again.
+template <typename T, int NB>
+__device__ __forceinline__ void cache_again(const cache_attn_args &a, const cache_item &it, int g, uint32_t col, uint32_t cols, uint32_t from, uint32_t to, int lane)
+{
+    const uint32_t i = col / (uint32_t)a.R;
+    const cache_span s = cache_span_of(a, it, col, 1);
+    float top, total, acc[kCachePer];
+    cache_row<T>(a, it.r, it.row0 + i, g * a.R + col % (uint32_t)a.R, from, to < s.to ? to : s.to, lane, top, total, acc);
+    const cache_column<T, NB> c(a, it, g, col, cols);
+#pragma unroll
+    for (int k = 0; k < kCachePer; ++k) {
+        const int d = lane + 64 * k;
+        if (c.part) { if (d < 32 * NB) c.part[d] = d < a.c.D ? acc[k] : 0.f; }
+        else if (d < a.c.D) c.out[d] = (T)(total == 0 ? 0.f : acc[k] / total);
+    }
+    if (lane == 0) c.total(top, total);
+}
+
+// Few columns for each request: a workgroup takes 16 of them, its four waves 32 tokens in turn, and they meet in the LDS.
+template <typename T, int NB>
+__global__ __launch_bounds__(256, NB <= 4 ? 3 : 2) void cache_few_kernel(cache_attn_args a)
+{
+    constexpr int row = 32 * NB + 4;
+    __shared__ float sums[4][16][row];
+    __shared__ float2 stats[4][16];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y;
+    cache_item it;
+    if (!cache_find(a, 16, blockIdx.x, false, lane, &it)) return;
+    if (it.chunks > 1 && it.slot + it.chunk * it.q.tiles >= a.slots) return;
+    const uint32_t first = it.tile * 16, count = it.q.columns - first < 16 ? it.q.columns - first : 16;
+    const cache_span span = cache_span_of(a, it, first, count);
+    cache_wave<T, NB, 1> x;
+    x.load_q(a, it, first, g, lane);
+    x.run(a, it, g, span.from + 32 * w, 128, span.to, span.whole, lane);
+    float total = x.total[0];
+    total += __shfl_xor(total, 16, 64);
+    total += __shfl_xor(total, 32, 64);
+    const int q = lane & 15;
+    if (lane < 16) stats[w][q] = {x.top[0], total};
+#pragma unroll
+    for (int b = 0; b < 2 * NB; ++b) *(cache_f4 *)&sums[w][q][16 * b + 4 * (lane >> 4)] = x.o[0][b];
+    __syncthreads();
+    const uint32_t c = threadIdx.x >> 4;                 // a column for every 16 threads
+    float top = -INFINITY, f[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, stats[k][c].x);
+    total = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        f[k] = stats[k][c].y == 0 ? 0.f : __builtin_amdgcn_exp2f(stats[k][c].x - top);
+        total += stats[k][c].y == 0 ? 0.f : stats[k][c].y * f[k];
+    }
+    const bool there = c < count;
+    cache_f4 y[(8 * NB + 15) / 16];
+    bool fine = true;
+#pragma unroll
+    for (int j = 0; j < (8 * NB + 15) / 16; ++j) {
+        const int d = 4 * (q + 16 * j);
+        if (d < 32 * NB) {
+            y[j] = (cache_f4)(0.f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) if (!(stats[k][c].y == 0)) y[j] += *(const cache_f4 *)&sums[k][c][d] * f[k];
+            fine = fine && y[j][0] - y[j][0] == 0 && y[j][1] - y[j][1] == 0 && y[j][2] - y[j][2] == 0 && y[j][3] - y[j][3] == 0;
+        }
+    }
+    const uint64_t spoilt = __builtin_amdgcn_ballot_w64(there && !fine && total == total);
+    if (there && !((spoilt >> (lane & 48)) & 0xffff)) {
+        const cache_column<T, NB> out(a, it, g, first + c, 16);
+#pragma unroll
+        for (int j = 0; j < (8 * NB + 15) / 16; ++j) {
+            const int d = 4 * (q + 16 * j);
+            if (d < 32 * NB) out.numbers(a, d, y[j], total);
+        }
+        if (q == 0) out.total(top == -INFINITY ? 0.f : top, total);
+    }
+#pragma unroll 1
+    for (int k = 0; k < 4; ++k)
+        if ((spoilt >> (16 * k)) & 0xffff) cache_again<T, NB>(a, it, g, first + 4 * w + k, 16, span.from, span.to, lane);
+}
+
+// Many columns: every wave takes 16 NQ of them and all tokens of its chunk.
+template <typename T, int NB, int NQ>
+__global__ __launch_bounds__(256, 1) void cache_many_kernel(cache_attn_args a)
+{
+    constexpr uint32_t cols = 16 * NQ;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y;
+    cache_item it;
+    if (!cache_find(a, cols, blockIdx.x * 4 + w, false, lane, &it)) return;
+    if (it.chunks > 1 && it.slot + it.chunk * it.q.tiles >= a.slots) return;
+    const uint32_t first = it.tile * cols, count = it.q.columns - first < cols ? it.q.columns - first : cols;
+    const cache_span span = cache_span_of(a, it, first, count);
+    uint64_t spoilt = 0;                                 // 16 columns a group
+    auto finish = [&](auto &x, auto groups) {
+#pragma unroll
+        for (int k = 0; k < groups; ++k) {
+            float total = x.total[k];
+            total += __shfl_xor(total, 16, 64);
+            total += __shfl_xor(total, 32, 64);
+            bool fine = true;
+#pragma unroll
+            for (int b = 0; b < 2 * NB; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) fine = fine && x.o[k][b][j] - x.o[k][b][j] == 0;
+            const uint32_t col = 16 * k + (lane & 15);
+            const bool there = col < count;
+            const uint64_t bad = __builtin_amdgcn_ballot_w64(there && !fine && total == total);
+            const uint32_t mine = (uint32_t)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffff;
+            spoilt |= (uint64_t)mine << (16 * k);
+            if (there && !((mine >> (lane & 15)) & 1)) {
+                const cache_column<T, NB> out(a, it, g, first + col, cols);
+#pragma unroll
+                for (int b = 0; b < 2 * NB; ++b) out.numbers(a, 16 * b + 4 * (lane >> 4), x.o[k][b], total);
+                if (lane < 16) out.total(x.mu[k], total);
+            }
+        }
+    };
+    if (count <= 16) {
+        cache_wave<T, NB, 1> x;
+        x.load_q(a, it, first, g, lane);
+        x.run(a, it, g, span.from, 32, span.to, span.whole, lane);
+        finish(x, std::integral_constant<int, 1>());
+    } else {
+        cache_wave<T, NB, NQ> x;
+        x.load_q(a, it, first, g, lane);
+        x.run(a, it, g, span.from, 32, span.to, span.whole, lane);
+        finish(x, std::integral_constant<int, NQ>());
+    }
+    for (; spoilt; spoilt &= spoilt - 1) cache_again<T, NB>(a, it, g, first + __builtin_ctzll(spoilt), cols, span.from, span.to, lane);
+}
+
+// Joins the chunks of the tiles that have several: a workgroup for each column, its waves a quarter of the chunks each.
+template <typename T, int NB>
+__global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int cols)
+{
+    constexpr int pad = 32 * NB, per = (pad + 63) / 64;
+    __shared__ float sums[4][pad];
+    __shared__ float2 stats[4];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y;
+    cache_item it;
+    if (!cache_find(a, cols, blockIdx.x, true, lane, &it)) return;
+    const uint32_t column = blockIdx.z, col = it.tile * cols + column;
+    if (col >= it.q.columns || it.slot + (it.chunks - 1) * it.q.tiles >= a.slots) return;
+    const int64_t step = (int64_t)it.q.tiles * a.c.G * cols, base = ((int64_t)it.slot * a.c.G + g) * cols + column;
+    float top = -INFINITY, total = 0, acc[per] = {};
+    for (uint32_t k = w; k < it.chunks; k += 4) {
+        const float2 s = a.stat[base + k * step];
+        if (s.y == 0) continue;                          // no weight
+        const float up = fmaxf(top, s.x), old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - up), f = __builtin_amdgcn_exp2f(s.x - up);
+        top = up;
+        total = total * old + s.y * f;
+        const float *part = a.part + (base + k * step) * pad;
+#pragma unroll
+        for (int j = 0; j < per; ++j) if (lane + 64 * j < pad) acc[j] = acc[j] * old + part[lane + 64 * j] * f;
+    }
+    if (lane == 0) stats[w] = {top, total};
+#pragma unroll
+    for (int j = 0; j < per; ++j) if (lane + 64 * j < pad) sums[w][lane + 64 * j] = acc[j];
+    __syncthreads();
+    float most = -INFINITY, all = 0, f[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) most = fmaxf(most, stats[k].x);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        f[k] = stats[k].y == 0 ? 0.f : __builtin_amdgcn_exp2f(stats[k].x - most);
+        all += stats[k].y == 0 ? 0.f : stats[k].y * f[k];
+    }
+    const uint32_t i = col / (uint32_t)a.R, h = g * a.R + col % (uint32_t)a.R;
+    T *out = (T *)a.O + (it.row0 + i) * a.ldo + (int64_t)h * a.hdo;
+    for (int d = threadIdx.x; d < a.c.D; d += 256) {
+        float x = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (!(stats[k].y == 0)) x += sums[k][d] * f[k];
+        out[d] = (T)(all == 0 ? 0.f : x / all);
+    }
+    if (a.lse && threadIdx.x == 0) a.lse[(int64_t)h * a.tokens + it.row0 + i] = all == 0 ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kCacheLn2;
+}
+
+// ---- launch -----------------------------------------------------------------------------------------------------------------
+
+// What a call launches; by sizes that the host knows.
+struct cache_choice {
+    bool few;                            // 16 columns a workgroup, or 16 NQ a wave
+    int cols;
+    int64_t items, slots;                // upper bounds; slots = 0: no request can have more than one chunk
+    size_t part, stat;                   // bytes
+};
+
+template <typename T> constexpr int cache_nq(int nb) { return cache_parts<T>::n == 1 ? (nb <= 4 ? 4 : 2) : cache_parts<T>::n == 2 ? (nb <= 4 ? 2 : 1) : (nb <= 4 ? 2 : 1); }
+
+template <typename T>
+cache_choice cache_choose(const cache_attn_args &a)
+{
+    cache_choice c;
+    const int64_t requests = a.requests < a.tokens ? a.requests : a.tokens, columns = a.tokens * a.R;
+    c.few = columns <= 16 * requests || cache_nq<T>(a.c.lay.nb) == 1;
+    c.cols = c.few ? 16 : 16 * cache_nq<T>(a.c.lay.nb);
+    c.slots = a.width * a.c.P <= kCacheLeast ? 0 : cache_slots(a.c.G);
+    c.items = columns / c.cols + requests + (c.slots ? ceil_div(kCacheTarget, a.c.G) : 0);
+    const size_t rows = (size_t)c.slots * a.c.G * c.cols;
+    c.part = rows * 32 * a.c.lay.nb * sizeof(float);
+    c.stat = (rows * sizeof(float2) + 255) & ~(size_t)255;
+    return c;
+}
+
+template <typename T, int NB>
+void cache_launch(const cache_attn_args &a, const cache_choice &c, hipStream_t st)
+{
+    constexpr int NQ = cache_nq<T>(NB);
+    if (c.few) cache_few_kernel<T, NB><<<dim3((unsigned)c.items, a.c.G), 256, 0, st>>>(a);
+    else if constexpr (NQ > 1) cache_many_kernel<T, NB, NQ><<<dim3((unsigned)ceil_div(c.items, 4), a.c.G), 256, 0, st>>>(a);
+    if (c.slots) cache_join_kernel<T, NB><<<dim3((unsigned)ceil_div(c.slots, 2), a.c.G, c.cols), 256, 0, st>>>(a, c.cols);
+}
+
+template <typename T> sp_status cache_attention(const cache_attn_args &a, const cache_choice &c, hipStream_t st);
+template <typename T> cache_choice cache_choice_of(const cache_attn_args &a);
+
+#define CACHE_ATTENTION_OF(T)                                                                        \
+    template <> sp_status cache_attention<T>(const cache_attn_args &a, const cache_choice &c, hipStream_t st) \
+    {                                                                                                \
+        switch (a.c.lay.nb) {                                                                        \
+        case 1: cache_launch<T, 1>(a, c, st); break;                                                 \
+        case 2: cache_launch<T, 2>(a, c, st); break;                                                 \
+        case 3: cache_launch<T, 3>(a, c, st); break;                                                 \
+        case 4: cache_launch<T, 4>(a, c, st); break;                                                 \
+        case 5: cache_launch<T, 5>(a, c, st); break;                                                 \
+        case 6: cache_launch<T, 6>(a, c, st); break;                                                 \
+        case 7: cache_launch<T, 7>(a, c, st); break;                                                 \
+        default: cache_launch<T, 8>(a, c, st);                                                       \
+        }                                                                                            \
+        SP_HIP(hipGetLastError());                                                                   \
+        return SP_OK;                                                                                \
+    }                                                                                                \
+    template <> cache_choice cache_choice_of<T>(const cache_attn_args &a) { return cache_choose<T>(a); }

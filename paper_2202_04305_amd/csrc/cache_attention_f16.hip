@@ -1,0 +1,3 @@
+// The kernels of attention over the 4-bit cache for f16.
+#include "cache_attention.h"
+CACHE_ATTENTION_OF(cache_f16)
