@@ -19,9 +19,9 @@ struct cache_attn_args {
     const int32_t *table, *length, *start;
     int64_t ldq, hdq, ldo, hdo, ldt, width, requests, tokens;
     int H, R, causal;                    // R = H / G heads share a head of the cache
-    float scale, step;                   // step = |scale| log2(e); the scale's sign goes into Q
+    float sign, step;                    // scale log2(e) = sign step; sign = -1, 0, 1 goes into Q, step > 0
     int vec;                             // rows of Q and O are aligned to 8 numbers
-    uint32_t page_mul, page_shift;       // records of a page: x / (P / 16) = mulhi(x, page_mul) >> page_shift, or x >> page_shift where page_mul = 0
+    uint32_t page_mul, page_shift;       // x / (P / 16) = x page_mul >> page_shift, the product in 64 bits
     float *part;                         // workspace: [slot][head of the cache][column][32 nb] sums
     float2 *stat;                        //            [slot][head of the cache][column]: running maximum (in units of log 2) and total
     uint32_t slots;                      // slots there is room for
@@ -33,9 +33,9 @@ struct cache_attn_args {
 // the requests.  Chunks are as long as makes about kCacheTarget items of all work, at least kCacheLeast tokens.
 constexpr int kCacheTarget = 1024, kCacheLeast = 256;
 
-struct cache_request { uint32_t n, columns, tiles, tokens; int64_t last; };         // last: position of the last query
+struct cache_request { uint32_t n, columns, tiles, tokens, row0; int32_t last; };   // row0: its first row; last: position of its last query, -1 or more
 struct cache_item {
-    int64_t r, row0;                     // request; its first row
+    int64_t r, row0;                     // the request and its first row
     cache_request q;
     uint32_t tile, chunk, chunks, slot;  // slot: of the tile's first chunk; the next one's is q.tiles further on
 };
@@ -44,7 +44,7 @@ static inline __host__ __device__ int64_t cache_limit(int64_t x, int64_t lo, int
 
 __device__ __forceinline__ cache_request cache_request_of(const cache_attn_args &a, int64_t r, int cols)
 {
-    cache_request q = {0, 0, 0, 0, 0};
+    cache_request q = {0, 0, 0, 0, 0, -1};
     if (r >= a.requests) return q;
     const int64_t s0 = cache_limit(a.start[r], 0, a.tokens), s1 = cache_limit(a.start[r + 1], 0, a.tokens), len = a.length[r];
     if (s1 <= s0) return q;
@@ -52,7 +52,8 @@ __device__ __forceinline__ cache_request cache_request_of(const cache_attn_args 
     q.columns = q.n * (uint32_t)a.R;
     q.tiles = (q.columns + cols - 1) / cols;
     q.tokens = (uint32_t)cache_limit(len, 0, a.width * a.c.P);
-    q.last = len - 1;
+    q.row0 = (uint32_t)s0;
+    q.last = (int32_t)(len < 0 ? 0 : len) - 1;
     return q;
 }
 
@@ -63,11 +64,12 @@ __device__ __forceinline__ uint32_t cache_wave_scan(uint32_t v, int lane)       
     return v;
 }
 
-// Tokens of a chunk: by the work of all requests.
-__device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a, int cols, int lane)
+// Tokens of a chunk: by the work of all requests.  own: the lane's among the first 64
+__device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a, int cols, int lane, const cache_request &own)
 {
-    uint64_t work = 0;
-    for (int64_t r = lane; r < a.requests; r += 64) {
+    if (a.slots == 0) return 0x7fffff00u;
+    uint64_t work = (uint64_t)own.tiles * own.tokens;
+    for (int64_t r = lane + 64; r < a.requests; r += 64) {
         const cache_request q = cache_request_of(a, r, cols);
         work += (uint64_t)q.tiles * q.tokens;
     }
@@ -77,15 +79,16 @@ __device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a,
     return c < kCacheLeast ? kCacheLeast : c > 0x7fffff00u ? 0x7fffff00u : ((uint32_t)c + 127) & ~127u;
 }
 // Chunks longer than the work's share make fewer than 2 kCacheTarget / G slots: a request of more than one has chunks < 2 tokens / length.
-static inline int64_t cache_slots(int G) { return ceil_div(2 * kCacheTarget, G); }
+static inline int64_t cache_slots(int G) { return 2 * ceil_div(kCacheTarget, G); }
 
 // Item `index` of all (joined = false), or tile `index` of those that have more than one chunk.  For a whole wave; false: there is none.
 __device__ __forceinline__ bool cache_find(const cache_attn_args &a, int cols, uint32_t index, bool joined, int lane, cache_item *item)
 {
-    const uint32_t len = __builtin_amdgcn_readfirstlane(cache_chunk_tokens(a, cols, lane));
+    cache_request q = cache_request_of(a, lane, cols);
+    const uint32_t len = __builtin_amdgcn_readfirstlane(cache_chunk_tokens(a, cols, lane, q));
     uint32_t items = 0, slots = 0;
     for (int64_t base = 0; base < a.requests; base += 64) {
-        const cache_request q = cache_request_of(a, base + lane, cols);
+        if (base) q = cache_request_of(a, base + lane, cols);
         const uint32_t chunks = q.tokens <= len ? 1 : (q.tokens + len - 1) / len;
         const uint32_t mine = joined ? (chunks > 1 ? q.tiles : 0) : q.tiles * chunks, room = chunks > 1 ? q.tiles * chunks : 0;
         const uint32_t upto = items + cache_wave_scan(mine, lane), slot = slots + cache_wave_scan(room, lane);
@@ -95,9 +98,9 @@ __device__ __forceinline__ bool cache_find(const cache_attn_args &a, int cols, u
             auto of = [k](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, k); };
             const uint32_t rest = index - (of(upto) - of(mine));
             item->r = base + k;
-            item->row0 = cache_limit(a.start[item->r], 0, a.tokens);
+            item->row0 = of(q.row0);
             item->q.n = of(q.n); item->q.columns = of(q.columns); item->q.tiles = of(q.tiles); item->q.tokens = of(q.tokens);
-            item->q.last = (int64_t)a.length[item->r] - 1;
+            item->q.last = (int64_t)(int32_t)of((uint32_t)q.last);
             item->chunks = of(chunks);
             item->tile = rest % item->q.tiles;
             item->chunk = rest / item->q.tiles;
@@ -109,6 +112,8 @@ __device__ __forceinline__ bool cache_find(const cache_attn_args &a, int cols, u
     }
     return false;
 }
+
+__device__ __forceinline__ uint32_t cache_page_of(const cache_attn_args &a, uint32_t record) { return (uint32_t)((uint64_t)record * a.page_mul >> a.page_shift); }
 
 // ---- one column by itself ---------------------------------------------------------------------------------------------------
 
@@ -131,7 +136,7 @@ __device__ __forceinline__ void cache_row(const cache_attn_args &a, int64_t r, i
 {
     const int g = h / a.R, D = a.c.D;
     const T *row = (const T *)a.Q + i * a.ldq + h * a.hdq;
-    const float step = a.scale < 0 ? -a.step : a.step;
+    const float step = a.sign * a.step;
     float q[kCachePer];
 #pragma unroll
     for (int k = 0; k < kCachePer; ++k) { q[k] = lane + 64 * k < D ? (float)row[lane + 64 * k] : 0.f; acc[k] = 0; }
@@ -190,28 +195,85 @@ __device__ __forceinline__ uint32_t cache_pair(float x, float y)                
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){x, y}, cache_b2));
 }
 
-// What a lane holds of 32 tokens: of each half its words of K and V and their scales.
+// What a lane holds of a record, 16 tokens: its words of K and V and their scales.
+template <int NB>
+struct cache_record {
+    static constexpr int SB = NB <= 2 ? NB : NB <= 4 ? 4 : 8, KS = (SB + 3) / 4;
+    uint32_t k[NB], v[NB], ks[KS], vs[SB];
+    __device__ __forceinline__ void load(const uint8_t *rec, int lane)
+    {
+        constexpr int scales = 512 * NB;
+        const int t = lane & 15, g = lane >> 4;
+        cache_words(rec + (t * 4 + g) * (NB * 4), k);
+        if constexpr (SB == 1) ks[0] = rec[scales + t];
+        else if constexpr (SB == 2) ks[0] = *(const uint16_t *)(rec + scales + t * 2);
+        else cache_words(rec + scales + t * SB, ks);
+        cache_words(rec + 256 * NB + (g * 16 + t) * (NB * 4), v);
+        cache_words(rec + scales + 16 * SB + g * 4 * SB, vs);
+    }
+    // A scale as the conversion takes it, which looks at the exponent (bits 23 to 30) alone: the byte is moved there, whatever lies beside it.
+    static __device__ __forceinline__ float scale(uint32_t w, int b) { return __uint_as_float(b == 3 ? w >> 1 : w << (23 - 8 * b)); }
+    __device__ __forceinline__ cache_b8 key(int b) const                // the operand of block b of K
+    {
+        const float f = scale(ks[b / 4], b % 4);
+        return __builtin_bit_cast(cache_b8, (cache_u4){cache_convert<0>(k[b], f), cache_convert<1>(k[b], f), cache_convert<2>(k[b], f), cache_convert<3>(k[b], f)});
+    }
+    __device__ __forceinline__ float v_scale(int token, int b) const { return scale(vs[(token * SB + b) / 4], (token * SB + b) % 4); }
+    // half of the operands of block b of V: numbers 0 .. 15 and 16 .. 31 of four tokens
+    __device__ __forceinline__ void values(int b, uint32_t (&lo)[2], uint32_t (&hi)[2]) const
+    {
+        const uint32_t c0 = cache_convert<0>(v[b], v_scale(0, b)), c1 = cache_convert<1>(v[b], v_scale(1, b));
+        const uint32_t c2 = cache_convert<2>(v[b], v_scale(2, b)), c3 = cache_convert<3>(v[b], v_scale(3, b));
+        lo[0] = __builtin_amdgcn_perm(c1, c0, 0x05040100);
+        lo[1] = __builtin_amdgcn_perm(c3, c2, 0x05040100);
+        hi[0] = __builtin_amdgcn_perm(c1, c0, 0x07060302);
+        hi[1] = __builtin_amdgcn_perm(c3, c2, 0x07060302);
+    }
+    __device__ __forceinline__ void blank(int token)                   // the token's values are zeros
+    {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) v[b] &= ~(255u << (8 * token));
+        if constexpr (SB >= 4) {
+#pragma unroll
+            for (int b = 0; b < SB / 4; ++b) vs[token * (SB / 4) + b] = 0x7f7f7f7f;
+        } else {
+            constexpr uint32_t ones = SB == 2 ? 0xffff : 0xff;
+            uint32_t &w = vs[token * SB / 4];
+            const int at = 8 * (token * SB % 4);
+            w = (w & ~(ones << at)) | ((0x7f7f & ones) << at);
+        }
+    }
+};
+
+// 32 tokens in registers.
 template <int NB>
 struct cache_tokens {
-    static constexpr int SB = NB <= 2 ? NB : NB <= 4 ? 4 : 8, KS = (SB + 3) / 4;
-    uint32_t k[2][NB], v[2][NB], ks[2][KS], vs[2][SB];
-    __device__ __forceinline__ void load(const uint8_t *rec, int half, int lane)
+    cache_record<NB> half[2];
+    __device__ __forceinline__ cache_b8 key(int h, int b, int) const { return half[h].key(b); }
+    __device__ __forceinline__ void values(int b, int, cache_b8 &lo, cache_b8 &hi) const
     {
-        constexpr int record = 512 * NB;
-        const int t = lane & 15, g = lane >> 4;
-        cache_words(rec + (t * 4 + g) * (NB * 4), k[half]);
-        if constexpr (SB == 1) ks[half][0] = rec[record + t];
-        else if constexpr (SB == 2) ks[half][0] = *(const uint16_t *)(rec + record + t * 2);
-        else cache_words(rec + record + t * SB, ks[half]);
-        cache_words(rec + 256 * NB + (g * 16 + t) * (NB * 4), v[half]);
-        cache_words(rec + record + 16 * SB + g * 4 * SB, vs[half]);
+        uint32_t l[2][2], h[2][2];
+        half[0].values(b, l[0], h[0]);
+        half[1].values(b, l[1], h[1]);
+        lo = __builtin_bit_cast(cache_b8, (cache_u4){l[0][0], l[0][1], l[1][0], l[1][1]});
+        hi = __builtin_bit_cast(cache_b8, (cache_u4){h[0][0], h[0][1], h[1][0], h[1][1]});
     }
-    __device__ __forceinline__ float k_scale(int half, int s) const { return __uint_as_float(((ks[half][s / 4] >> (8 * (s % 4))) & 255) << 23); }
-    __device__ __forceinline__ float v_scale(int half, int token, int s) const
+    __device__ __forceinline__ void blank(int h, int token) { half[h].blank(token); }
+};
+
+// The same as operands in LDS, where the waves of a workgroup share them: 32 tokens of a stretch of 64.
+template <int NB>
+struct cache_staged {
+    static constexpr int kv = 4 * NB * 1024;             // bytes of the operands of K (and of V) of 64 tokens
+    const char *k, *v;                                   // of these 32 tokens
+    __device__ __forceinline__ cache_staged(const char *stage, int pair) : k(stage + pair * 2 * NB * 1024), v(stage + kv + pair * 2 * NB * 1024) {}
+    __device__ __forceinline__ cache_b8 key(int half, int b, int lane) const { return *(const cache_b8 *)(k + (half * NB + b) * 1024 + lane * 16); }
+    __device__ __forceinline__ void values(int b, int lane, cache_b8 &lo, cache_b8 &hi) const
     {
-        const int b = token * SB + s;
-        return __uint_as_float(((vs[half][b / 4] >> (8 * (b % 4))) & 255) << 23);
+        lo = *(const cache_b8 *)(v + b * 2048 + lane * 16);
+        hi = *(const cache_b8 *)(v + b * 2048 + 1024 + lane * 16);
     }
+    __device__ __forceinline__ void blank(int, int) {}   // done where they were written
 };
 
 // 16 NQ columns of one tile over some of its tokens, by one wave.
@@ -233,7 +295,7 @@ struct cache_wave {
             const bool there = col < it.q.columns;
             const uint32_t i = there ? col / (uint32_t)a.R : 0, hh = there ? col % (uint32_t)a.R : 0;
             const T *row = (const T *)a.Q + (it.row0 + i) * a.ldq + (int64_t)(g * a.R + hh) * a.hdq;
-            const int64_t e = a.causal ? it.q.last - it.q.n + 2 + i : (int64_t)it.q.tokens;
+            const int64_t e = a.causal ? (int64_t)it.q.last - it.q.n + 2 + i : (int64_t)it.q.tokens;
             end[k] = there ? (uint32_t)cache_limit(e, 0, it.q.tokens) : it.q.tokens;
             top[k] = -INFINITY; mu[k] = 0; total[k] = 0;
 #pragma unroll
@@ -256,7 +318,7 @@ struct cache_wave {
                 uint32_t w[parts][4] = {};
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    float y = a.scale < 0 ? -x[j] : x[j];
+                    float y = x[j] * a.sign;
                     const bool finite = y - y == 0;
 #pragma unroll
                     for (int p = 0; p < parts; ++p) {
@@ -273,9 +335,10 @@ struct cache_wave {
         }
     }
 
-    // 32 tokens from t on.  MASKED: some column attends to some of them only; there: which halves' pages exist; tokens: the request's
-    template <bool MASKED>
-    __device__ __forceinline__ void tokens32(const cache_tokens<NB> &x, float step, uint32_t t, uint32_t tokens, uint32_t there, int lane)
+    // 32 tokens from t on.  partial: some column attends to some of them only; there: which halves' pages exist; tokens: the request's.
+    // One path for both, as two would be merged by the compiler into one that keeps everything of both at once.
+    template <typename S>
+    __device__ __forceinline__ void tokens32(S &x, float step, uint32_t t, uint32_t tokens, uint32_t there, bool partial, int lane)
     {
         const int g = lane >> 4;
         cache_f4 s[NQ][2];
@@ -285,31 +348,31 @@ struct cache_wave {
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const float f = x.k_scale(half, b);
-                const uint32_t w = x.k[half][b];
-                const cache_b8 key = __builtin_bit_cast(cache_b8, (cache_u4){cache_convert<0>(w, f), cache_convert<1>(w, f), cache_convert<2>(w, f), cache_convert<3>(w, f)});
+                const cache_b8 key = x.key(half, b, lane);
 #pragma unroll
                 for (int k = 0; k < NQ; ++k)
 #pragma unroll
                     for (int p = 0; p < parts; ++p) s[k][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[k][p][b], s[k][half], 0, 0, 0);
             }
+        if (partial) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t at = t + 16 * half + 4 * g + j;
+                    const bool page = (there >> half) & 1;
+#pragma unroll
+                    for (int k = 0; k < NQ; ++k) s[k][half][j] = page && at < end[k] ? s[k][half][j] : -INFINITY;
+                    if (!page || at >= tokens) x.blank(half, j);        // behind the request's tokens: anything may be there
+                }
+        }
         cache_b8 w[NQ][parts];
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < NQ; ++k) {
             // The maximum that is taken off lags behind by up to 8 (a factor of 256): moving it costs a pass over the sums, and it moves in
             // the first tokens of a chunk, hardly later.
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                y[j] = s[k][j / 4][j % 4];
-                if (MASKED) {
-                    const uint32_t at = t + 16 * (j / 4) + 4 * g + j % 4;
-                    y[j] = at < end[k] && ((there >> (j / 4)) & 1) ? y[j] * step : -INFINITY;
-                }
-            }
-            float most = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-            if (!MASKED) most *= step;
+            float most = fmaxf(fmaxf(fmaxf(s[k][0][0], s[k][0][1]), fmaxf(s[k][0][2], s[k][0][3])), fmaxf(fmaxf(s[k][1][0], s[k][1][1]), fmaxf(s[k][1][2], s[k][1][3])));
+            most *= step;
             if (__builtin_amdgcn_ballot_w64(most > top[k] + 8)) {
                 most = fmaxf(most, __shfl_xor(most, 16, 64));
                 most = fmaxf(most, __shfl_xor(most, 32, 64));
@@ -320,8 +383,9 @@ struct cache_wave {
 #pragma unroll
                 for (int b = 0; b < 2 * NB; ++b) o[k][b] *= f;
             }
+            float y[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(MASKED ? y[j] - mu[k] : __builtin_fmaf(y[j], step, -mu[k]));
+            for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][j / 4][j % 4], step, -mu[k]));
             total[k] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
 #pragma unroll
             for (int p = 0; p < parts; ++p) {
@@ -337,27 +401,8 @@ struct cache_wave {
         }
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            uint32_t lo[4], hi[4];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float f[4];
-                uint32_t word = x.v[half][b];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    f[j] = x.v_scale(half, j, b);
-                    if (MASKED && (t + 16 * half + 4 * g + j >= tokens || !((there >> half) & 1))) {      // behind the request's tokens: anything may be there
-                        f[j] = 1.f;
-                        word &= ~(255u << (8 * j));
-                    }
-                }
-                const uint32_t c0 = cache_convert<0>(word, f[0]), c1 = cache_convert<1>(word, f[1]), c2 = cache_convert<2>(word, f[2]), c3 = cache_convert<3>(word, f[3]);
-                lo[2 * half] = __builtin_amdgcn_perm(c1, c0, 0x05040100);
-                lo[2 * half + 1] = __builtin_amdgcn_perm(c3, c2, 0x05040100);
-                hi[2 * half] = __builtin_amdgcn_perm(c1, c0, 0x07060302);
-                hi[2 * half + 1] = __builtin_amdgcn_perm(c3, c2, 0x07060302);
-            }
-            const cache_b8 vl = __builtin_bit_cast(cache_b8, (cache_u4){lo[0], lo[1], lo[2], lo[3]});
-            const cache_b8 vh = __builtin_bit_cast(cache_b8, (cache_u4){hi[0], hi[1], hi[2], hi[3]});
+            cache_b8 vl, vh;
+            x.values(b, lane, vl, vh);
 #pragma unroll
             for (int k = 0; k < NQ; ++k)
 #pragma unroll
@@ -365,7 +410,6 @@ struct cache_wave {
                     o[k][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vl, w[k][p], o[k][2 * b], 0, 0, 0);
                     o[k][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vh, w[k][p], o[k][2 * b + 1], 0, 0, 0);
                 }
-            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
@@ -376,12 +420,13 @@ struct cache_wave {
         const int32_t *table = a.table + it.r * a.ldt;
         const uint32_t per = (uint32_t)a.c.P / kCacheTile;
         const int64_t head = (int64_t)per * a.c.lay.record();
-        auto page_of = [&](uint32_t record) { return a.page_mul ? __umulhi(record, a.page_mul) >> a.page_shift : record >> a.page_shift; };
+        auto page_of = [&](uint32_t record) { return cache_page_of(a, record); };
+        // Tokens before `to` have a page in the table; the second 16 of 32 may lie behind the table's end, and are behind the request's then.
         auto pages = [&](uint32_t at, int32_t (&p)[2]) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint32_t n = page_of(at / kCacheTile + half);
-                p[half] = n < a.width ? table[n] : -1;
+                p[half] = table[n < a.width ? n : a.width - 1];
             }
         };
         auto fetch = [&](uint32_t at, const int32_t (&p)[2], cache_tokens<NB> &x) {
@@ -391,28 +436,30 @@ struct cache_wave {
                 const uint32_t record = at / kCacheTile + half, in = record - page_of(record) * per;
                 const bool ok = p[half] >= 0 && p[half] < a.c.pages;
                 there |= ok ? 1u << half : 0;
-                x.load(a.c.data + (ok ? (p[half] * (int64_t)a.c.G + g) * head + in * (int64_t)a.c.lay.record() : 0), half, lane);
+                x.half[half].load(a.c.data + (ok ? (p[half] * (int64_t)a.c.G + g) * head + in * (int64_t)a.c.lay.record() : 0), lane);
             }
             return there;
         };
+        // Two places, one filled while the other is worked on; pages a step ahead of that.  At the end the last tokens are loaded again: no
+        // branches in between.
+        const uint32_t last = t + (to - 1 - t) / stride * stride;
         int32_t p[2];
-        cache_tokens<NB> now, next;
+        cache_tokens<NB> x[2];
+        uint32_t next = t < last ? t + stride : last, there[2];
         pages(t, p);
-        uint32_t there = fetch(t, p, now);
-        pages(t + stride, p);
+        there[0] = fetch(t, p, x[0]);
+        pages(next, p);
         while (true) {
-            const bool more = t + stride < to;
-            uint32_t next_there = 0;
-            if (more) {
-                next_there = fetch(t + stride, p, next);
-                pages(t + 2 * stride, p);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                there[1 - k] = fetch(next, p, x[1 - k]);
+                const uint32_t then = next < last ? next + stride : last;
+                pages(then, p);
+                tokens32(x[k], a.step, t, it.q.tokens, there[k], t + 32 > whole || there[k] != 3, lane);
+                if (t == last) return;
+                t = next;
+                next = then;
             }
-            if (t + 32 <= whole && there == 3) tokens32<false>(now, a.step, t, it.q.tokens, there, lane);
-            else tokens32<true>(now, a.step, t, it.q.tokens, there, lane);
-            if (!more) break;
-            now = next;
-            there = next_there;
-            t += stride;
         }
     }
 };
@@ -428,7 +475,7 @@ __device__ __forceinline__ cache_span cache_span_of(const cache_attn_args &a, co
     s.to = (uint32_t)(to < it.q.tokens ? to : it.q.tokens);
     s.whole = it.q.tokens;
     if (a.causal) {
-        const int64_t before = it.q.last - it.q.n + 2;   // what the request's first query attends to, at least
+        const int64_t before = (int64_t)it.q.last - it.q.n + 2;   // what the request's first query attends to, at least
         const uint32_t end = (uint32_t)cache_limit(before + (first + count - 1) / (uint32_t)a.R, 0, it.q.tokens);
         s.whole = (uint32_t)cache_limit(before + first / (uint32_t)a.R, 0, it.q.tokens);
         if (end < s.to) s.to = end;
@@ -486,18 +533,14 @@ __device__ __forceinline__ void cache_again(const cache_attn_args &a, const cach
     if (lane == 0) c.total(top, total);
 }
 
-// Few columns for each request: a workgroup takes 16 of them, its four waves 32 tokens in turn, and they meet in the LDS.
+// 16 columns or fewer: the four waves of a workgroup take 32 tokens in turn, and they meet in the LDS.
 template <typename T, int NB>
-__global__ __launch_bounds__(256, NB <= 4 ? 3 : 2) void cache_few_kernel(cache_attn_args a)
+struct cache_meeting { float sums[4][16][32 * NB + 4]; float2 stats[4][16]; };
+
+template <typename T, int NB>
+__device__ __forceinline__ void cache_few(const cache_attn_args &a, const cache_item &it, int g, uint32_t cols, int w, int lane, cache_meeting<T, NB> &m)
 {
-    constexpr int row = 32 * NB + 4;
-    __shared__ float sums[4][16][row];
-    __shared__ float2 stats[4][16];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y;
-    cache_item it;
-    if (!cache_find(a, 16, blockIdx.x, false, lane, &it)) return;
-    if (it.chunks > 1 && it.slot + it.chunk * it.q.tiles >= a.slots) return;
-    const uint32_t first = it.tile * 16, count = it.q.columns - first < 16 ? it.q.columns - first : 16;
+    const uint32_t first = it.tile * cols, count = it.q.columns - first < 16 ? it.q.columns - first : 16;
     const cache_span span = cache_span_of(a, it, first, count);
     cache_wave<T, NB, 1> x;
     x.load_q(a, it, first, g, lane);
@@ -506,38 +549,42 @@ __global__ __launch_bounds__(256, NB <= 4 ? 3 : 2) void cache_few_kernel(cache_a
     total += __shfl_xor(total, 16, 64);
     total += __shfl_xor(total, 32, 64);
     const int q = lane & 15;
-    if (lane < 16) stats[w][q] = {x.top[0], total};
+    if (lane < 16) m.stats[w][q] = {x.top[0], total};
 #pragma unroll
-    for (int b = 0; b < 2 * NB; ++b) *(cache_f4 *)&sums[w][q][16 * b + 4 * (lane >> 4)] = x.o[0][b];
+    for (int b = 0; b < 2 * NB; ++b) *(cache_f4 *)&m.sums[w][q][16 * b + 4 * (lane >> 4)] = x.o[0][b];
     __syncthreads();
     const uint32_t c = threadIdx.x >> 4;                 // a column for every 16 threads
     float top = -INFINITY, f[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) top = fmaxf(top, stats[k][c].x);
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, m.stats[k][c].x);
     total = 0;
+    bool some[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        f[k] = stats[k][c].y == 0 ? 0.f : __builtin_amdgcn_exp2f(stats[k][c].x - top);
-        total += stats[k][c].y == 0 ? 0.f : stats[k][c].y * f[k];
+        const float2 s = m.stats[k][c];
+        some[k] = !(s.y == 0);                           // sums without weight may hold anything
+        f[k] = __builtin_amdgcn_exp2f(s.x - top);
+        total += some[k] ? s.y * f[k] : 0.f;
     }
     const bool there = c < count;
-    cache_f4 y[(8 * NB + 15) / 16];
+    constexpr int each = (8 * NB + 15) / 16;
+    cache_f4 y[each];
     bool fine = true;
 #pragma unroll
-    for (int j = 0; j < (8 * NB + 15) / 16; ++j) {
+    for (int j = 0; j < each; ++j) {
         const int d = 4 * (q + 16 * j);
+        y[j] = (cache_f4)(0.f);
         if (d < 32 * NB) {
-            y[j] = (cache_f4)(0.f);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) if (!(stats[k][c].y == 0)) y[j] += *(const cache_f4 *)&sums[k][c][d] * f[k];
+            for (int k = 0; k < 4; ++k) if (some[k]) y[j] += *(const cache_f4 *)&m.sums[k][c][d] * f[k];
             fine = fine && y[j][0] - y[j][0] == 0 && y[j][1] - y[j][1] == 0 && y[j][2] - y[j][2] == 0 && y[j][3] - y[j][3] == 0;
         }
     }
     const uint64_t spoilt = __builtin_amdgcn_ballot_w64(there && !fine && total == total);
     if (there && !((spoilt >> (lane & 48)) & 0xffff)) {
-        const cache_column<T, NB> out(a, it, g, first + c, 16);
+        const cache_column<T, NB> out(a, it, g, first + c, cols);
 #pragma unroll
-        for (int j = 0; j < (8 * NB + 15) / 16; ++j) {
+        for (int j = 0; j < each; ++j) {
             const int d = 4 * (q + 16 * j);
             if (d < 32 * NB) out.numbers(a, d, y[j], total);
         }
@@ -545,127 +592,228 @@ __global__ __launch_bounds__(256, NB <= 4 ? 3 : 2) void cache_few_kernel(cache_a
     }
 #pragma unroll 1
     for (int k = 0; k < 4; ++k)
-        if ((spoilt >> (16 * k)) & 0xffff) cache_again<T, NB>(a, it, g, first + 4 * w + k, 16, span.from, span.to, lane);
+        if ((spoilt >> (16 * k)) & 0xffff) cache_again<T, NB>(a, it, g, first + 4 * w + k, cols, span.from, span.to, lane);
 }
 
-// Many columns: every wave takes 16 NQ of them and all tokens of its chunk.
-template <typename T, int NB, int NQ>
-__global__ __launch_bounds__(256, 1) void cache_many_kernel(cache_attn_args a)
+// Single tokens of requests (and other steps of few columns a request).
+template <typename T, int NB>
+__global__ __launch_bounds__(256, NB <= 4 ? 3 : 2) void cache_few_kernel(cache_attn_args a)
 {
-    constexpr uint32_t cols = 16 * NQ;
+    __shared__ cache_meeting<T, NB> meeting;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    cache_item it;
+    if (!cache_find(a, 16, blockIdx.x, false, lane, &it)) return;
+    if (it.chunks > 1 && it.slot + it.chunk * it.q.tiles >= a.slots) return;
+    cache_few<T, NB>(a, it, blockIdx.y, 16, w, lane, meeting);
+}
+
+// Prompts: the four waves of a workgroup take 16 NQ columns each and all tokens of the chunk, 64 at a time.  A wave turns 16 of the 64 into
+// operands, which the four share in LDS: in registers of their own the conversions would take as long as the exponentials.  Two places: one
+// is filled while the other is worked on.  (NB > 4: one place, there is no room for two workgroups otherwise.)
+template <typename T, int NB, int NQ>
+__global__ __launch_bounds__(256, 2) void cache_many_kernel(cache_attn_args a)
+{
+    constexpr uint32_t cols = 64 * NQ;
+    constexpr int places = NB <= 4 ? 2 : 1, stage = 2 * cache_staged<NB>::kv;
+    __shared__ union {
+        cache_meeting<T, NB> meeting;
+        struct { char at[places][stage]; uint32_t there[places][4]; } staged;
+    } lds;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y;
     cache_item it;
-    if (!cache_find(a, cols, blockIdx.x * 4 + w, false, lane, &it)) return;
+    if (!cache_find(a, cols, blockIdx.x, false, lane, &it)) return;
     if (it.chunks > 1 && it.slot + it.chunk * it.q.tiles >= a.slots) return;
-    const uint32_t first = it.tile * cols, count = it.q.columns - first < cols ? it.q.columns - first : cols;
-    const cache_span span = cache_span_of(a, it, first, count);
-    uint64_t spoilt = 0;                                 // 16 columns a group
-    auto finish = [&](auto &x, auto groups) {
+    if (it.q.columns <= 16) { cache_few<T, NB>(a, it, g, cols, w, lane, lds.meeting); return; }
+    const uint32_t tile0 = it.tile * cols, tile_count = it.q.columns - tile0 < cols ? it.q.columns - tile0 : cols;
+    const cache_span all = cache_span_of(a, it, tile0, tile_count);
+    const uint32_t first = tile0 + 16 * NQ * w, mine = tile_count > 16 * NQ * w ? tile_count - 16 * NQ * w : 0, count = mine < 16 * NQ ? mine : 16 * NQ;
+    const cache_span span = cache_span_of(a, it, count ? first : tile0, count ? count : 1);
+    cache_wave<T, NB, NQ> x;
+    x.load_q(a, it, first, g, lane);
+
+    const int32_t *table = a.table + it.r * a.ldt;
+    const uint32_t per = (uint32_t)a.c.P / kCacheTile;
+    const int64_t head = (int64_t)per * a.c.lay.record();
+    // a wave's 16 of the 64 tokens from t on; behind the table's end the request has none
+    auto page = [&](uint32_t t) {
+        const uint32_t n = cache_page_of(a, t / kCacheTile + w);
+        return table[n < a.width ? n : a.width - 1];
+    };
+    cache_record<NB> rec;
+    auto fetch = [&](uint32_t t, int32_t p) {
+        const uint32_t record = t / kCacheTile + w, in = record - cache_page_of(a, record) * per;
+        const bool ok = p >= 0 && p < a.c.pages;
+        rec.load(a.c.data + (ok ? (p * (int64_t)a.c.G + g) * head + in * (int64_t)a.c.lay.record() : 0), lane);
+        return ok;
+    };
+    auto put = [&](int place, uint32_t t, bool ok) {
+        char *to = lds.staged.at[place];
+        if (!ok || t + 16 * w + 16 > it.q.tokens)
 #pragma unroll
-        for (int k = 0; k < groups; ++k) {
-            float total = x.total[k];
-            total += __shfl_xor(total, 16, 64);
-            total += __shfl_xor(total, 32, 64);
-            bool fine = true;
+            for (int j = 0; j < 4; ++j) if (!ok || t + 16 * w + 4 * (lane >> 4) + j >= it.q.tokens) rec.blank(j);
 #pragma unroll
-            for (int b = 0; b < 2 * NB; ++b)
+        for (int b = 0; b < NB; ++b) {
+            *(cache_b8 *)(to + (w * NB + b) * 1024 + lane * 16) = rec.key(b);
+            uint32_t lo[2], hi[2];
+            rec.values(b, lo, hi);
+            char *v = to + cache_staged<NB>::kv + ((w >> 1) * NB + b) * 2048 + lane * 16 + (w & 1) * 8;
+            *(uint2 *)v = {lo[0], lo[1]};
+            *(uint2 *)(v + 1024) = {hi[0], hi[1]};
+        }
+        if (lane == 0) lds.staged.there[place][w] = ok;
+    };
+    auto work = [&](int place, uint32_t t) {
+        const uint4 f = *(const uint4 *)lds.staged.there[place];
+        const uint32_t there = __builtin_amdgcn_readfirstlane(f.x | f.y << 1 | f.z << 2 | f.w << 3);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) fine = fine && x.o[k][b][j] - x.o[k][b][j] == 0;
-            const uint32_t col = 16 * k + (lane & 15);
-            const bool there = col < count;
-            const uint64_t bad = __builtin_amdgcn_ballot_w64(there && !fine && total == total);
-            const uint32_t mine = (uint32_t)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffff;
-            spoilt |= (uint64_t)mine << (16 * k);
-            if (there && !((mine >> (lane & 15)) & 1)) {
-                const cache_column<T, NB> out(a, it, g, first + col, cols);
-#pragma unroll
-                for (int b = 0; b < 2 * NB; ++b) out.numbers(a, 16 * b + 4 * (lane >> 4), x.o[k][b], total);
-                if (lane < 16) out.total(x.mu[k], total);
-            }
+        for (int pair = 0; pair < 2; ++pair) {
+            const uint32_t at = t + 32 * pair;
+            if (at >= span.to || !count) break;
+            cache_staged<NB> src(lds.staged.at[place], pair);
+            const uint32_t both = (there >> (2 * pair)) & 3;
+            x.tokens32(src, a.step, at, it.q.tokens, both, at + 32 > span.whole || both != 3, lane);
         }
     };
-    if (count <= 16) {
-        cache_wave<T, NB, 1> x;
-        x.load_q(a, it, first, g, lane);
-        x.run(a, it, g, span.from, 32, span.to, span.whole, lane);
-        finish(x, std::integral_constant<int, 1>());
-    } else {
-        cache_wave<T, NB, NQ> x;
-        x.load_q(a, it, first, g, lane);
-        x.run(a, it, g, span.from, 32, span.to, span.whole, lane);
-        finish(x, std::integral_constant<int, NQ>());
+    if (all.from < all.to) {
+        const uint32_t last = all.from + (all.to - 1 - all.from) / 64 * 64;
+        uint32_t t = all.from, next = t < last ? t + 64 : last;
+        bool ok = fetch(t, page(t));
+        put(0, t, ok);
+        int32_t p = page(next);
+        ok = fetch(next, p);
+        __syncthreads();
+        if constexpr (places == 2) {
+            for (int place = 0;; place ^= 1) {
+                if (t != last) {
+                    const uint32_t then = next < last ? next + 64 : last;
+                    p = page(then);
+                    put(place ^ 1, next, ok);
+                    ok = fetch(then, p);
+                }
+                work(place, t);
+                if (t == last) break;
+                __syncthreads();
+                t = next;
+                next = next < last ? next + 64 : last;
+            }
+        } else {
+            while (true) {
+                work(0, t);
+                if (t == last) break;
+                __syncthreads();
+                put(0, next, ok);
+                t = next;
+                next = next < last ? next + 64 : last;
+                ok = fetch(next, page(next));
+                __syncthreads();
+            }
+        }
     }
-    for (; spoilt; spoilt &= spoilt - 1) cache_again<T, NB>(a, it, g, first + __builtin_ctzll(spoilt), cols, span.from, span.to, lane);
+    uint64_t spoilt = 0;                                 // a bit a column
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) {
+        float total = x.total[k];
+        total += __shfl_xor(total, 16, 64);
+        total += __shfl_xor(total, 32, 64);
+        bool fine = true;
+#pragma unroll
+        for (int b = 0; b < 2 * NB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) fine = fine && x.o[k][b][j] - x.o[k][b][j] == 0;
+        const uint32_t col = 16 * k + (lane & 15);
+        const bool there = col < count;
+        const uint64_t bad = __builtin_amdgcn_ballot_w64(there && !fine && total == total);
+        const uint32_t these = (uint32_t)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffff;
+        spoilt |= (uint64_t)these << (16 * k);
+        if (there && !((these >> (lane & 15)) & 1)) {
+            const cache_column<T, NB> out(a, it, g, first + col, cols);
+#pragma unroll
+            for (int b = 0; b < 2 * NB; ++b) out.numbers(a, 16 * b + 4 * (lane >> 4), x.o[k][b], total);
+            if (lane < 16) out.total(x.mu[k], total);
+        }
+    }
+#pragma unroll 1
+    for (; spoilt; spoilt &= spoilt - 1) cache_again<T, NB>(a, it, g, first + __builtin_ctzll(spoilt), cols, all.from, all.to, lane);
 }
 
-// Joins the chunks of the tiles that have several: a workgroup for each column, its waves a quarter of the chunks each.
+// Joins the chunks of the tiles that have several: a workgroup for each column (or some of them in turn).  The chunks' factors first, then the
+// sums, a quarter of the chunks a wave: loads that do not wait for each other.
 template <typename T, int NB>
 __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int cols)
 {
     constexpr int pad = 32 * NB, per = (pad + 63) / 64;
-    __shared__ float sums[4][pad];
-    __shared__ float2 stats[4];
+    __shared__ float factor[2 * kCacheTarget], sums[4][pad];
+    __shared__ float stats[2][4];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y;
     cache_item it;
     if (!cache_find(a, cols, blockIdx.x, true, lane, &it)) return;
-    const uint32_t column = blockIdx.z, col = it.tile * cols + column;
-    if (col >= it.q.columns || it.slot + (it.chunks - 1) * it.q.tiles >= a.slots) return;
-    const int64_t step = (int64_t)it.q.tiles * a.c.G * cols, base = ((int64_t)it.slot * a.c.G + g) * cols + column;
-    float top = -INFINITY, total = 0, acc[per] = {};
-    for (uint32_t k = w; k < it.chunks; k += 4) {
-        const float2 s = a.stat[base + k * step];
-        if (s.y == 0) continue;                          // no weight
-        const float up = fmaxf(top, s.x), old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - up), f = __builtin_amdgcn_exp2f(s.x - up);
-        top = up;
-        total = total * old + s.y * f;
-        const float *part = a.part + (base + k * step) * pad;
+    if (it.slot + (it.chunks - 1) * it.q.tiles >= a.slots) return;       // so there are at most 2 kCacheTarget chunks
+    const int64_t step = (int64_t)it.q.tiles * a.c.G * cols;
+    for (uint32_t column = blockIdx.z; column < (uint32_t)cols && it.tile * cols + column < it.q.columns; column += gridDim.z) {
+        const uint32_t col = it.tile * cols + column;
+        const int64_t base = ((int64_t)it.slot * a.c.G + g) * cols + column;
+        float top = -INFINITY, total = 0;
+        for (uint32_t k = threadIdx.x; k < it.chunks; k += 256) top = fmaxf(top, a.stat[base + k * step].x);
 #pragma unroll
-        for (int j = 0; j < per; ++j) if (lane + 64 * j < pad) acc[j] = acc[j] * old + part[lane + 64 * j] * f;
+        for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+        if (lane == 0) stats[0][w] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(stats[0][0], stats[0][1]), fmaxf(stats[0][2], stats[0][3]));
+        for (uint32_t k = threadIdx.x; k < it.chunks; k += 256) {
+            const float2 s = a.stat[base + k * step];
+            const float f = s.y == 0 ? 0.f : __builtin_amdgcn_exp2f(s.x - top);      // (sums without weight are zeros)
+            factor[k] = f;
+            total += s.y == 0 ? 0.f : s.y * f;
+        }
+        total = cache_wave_sum(total);
+        if (lane == 0) stats[1][w] = total;
+        __syncthreads();
+        total = (stats[1][0] + stats[1][1]) + (stats[1][2] + stats[1][3]);
+        float acc[per] = {};
+#pragma unroll 8
+        for (uint32_t k = w; k < it.chunks; k += 4) {
+            const float *part = a.part + (base + k * step) * pad;
+#pragma unroll
+            for (int j = 0; j < per; ++j) if (pad % 64 == 0 || lane + 64 * j < pad) acc[j] += part[lane + 64 * j] * factor[k];
+        }
+#pragma unroll
+        for (int j = 0; j < per; ++j) if (pad % 64 == 0 || lane + 64 * j < pad) sums[w][lane + 64 * j] = acc[j];
+        __syncthreads();
+        const uint32_t i = col / (uint32_t)a.R, h = g * a.R + col % (uint32_t)a.R;
+        T *out = (T *)a.O + (it.row0 + i) * a.ldo + (int64_t)h * a.hdo;
+        if ((int)threadIdx.x < a.c.D) {
+            const int d = threadIdx.x;
+            out[d] = (T)(total == 0 ? 0.f : ((sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d])) / total);
+        }
+        if (a.lse && threadIdx.x == 0) a.lse[(int64_t)h * a.tokens + it.row0 + i] = total == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kCacheLn2;
+        __syncthreads();
     }
-    if (lane == 0) stats[w] = {top, total};
-#pragma unroll
-    for (int j = 0; j < per; ++j) if (lane + 64 * j < pad) sums[w][lane + 64 * j] = acc[j];
-    __syncthreads();
-    float most = -INFINITY, all = 0, f[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) most = fmaxf(most, stats[k].x);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        f[k] = stats[k].y == 0 ? 0.f : __builtin_amdgcn_exp2f(stats[k].x - most);
-        all += stats[k].y == 0 ? 0.f : stats[k].y * f[k];
-    }
-    const uint32_t i = col / (uint32_t)a.R, h = g * a.R + col % (uint32_t)a.R;
-    T *out = (T *)a.O + (it.row0 + i) * a.ldo + (int64_t)h * a.hdo;
-    for (int d = threadIdx.x; d < a.c.D; d += 256) {
-        float x = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) if (!(stats[k].y == 0)) x += sums[k][d] * f[k];
-        out[d] = (T)(all == 0 ? 0.f : x / all);
-    }
-    if (a.lse && threadIdx.x == 0) a.lse[(int64_t)h * a.tokens + it.row0 + i] = all == 0 ? -INFINITY : (most + __builtin_amdgcn_logf(all)) * kCacheLn2;
 }
 
 // ---- launch -----------------------------------------------------------------------------------------------------------------
 
 // What a call launches; by sizes that the host knows.
 struct cache_choice {
-    bool few;                            // 16 columns a workgroup, or 16 NQ a wave
+    bool few;                            // tiles of 16 columns, or of 64 NQ
     int cols;
     int64_t items, slots;                // upper bounds; slots = 0: no request can have more than one chunk
+    int64_t joins;                       // tiles of requests with more than one chunk, at most
     size_t part, stat;                   // bytes
 };
 
-template <typename T> constexpr int cache_nq(int nb) { return cache_parts<T>::n == 1 ? (nb <= 4 ? 4 : 2) : cache_parts<T>::n == 2 ? (nb <= 4 ? 2 : 1) : (nb <= 4 ? 2 : 1); }
+template <typename T> constexpr int cache_nq(int nb) { return nb <= 4 || cache_parts<T>::n == 1 ? 2 : 1; }
 
 template <typename T>
 cache_choice cache_choose(const cache_attn_args &a)
 {
     cache_choice c;
     const int64_t requests = a.requests < a.tokens ? a.requests : a.tokens, columns = a.tokens * a.R;
-    c.few = columns <= 16 * requests || cache_nq<T>(a.c.lay.nb) == 1;
-    c.cols = c.few ? 16 : 16 * cache_nq<T>(a.c.lay.nb);
+    c.few = columns <= 16 * requests;
+    c.cols = c.few ? 16 : 64 * cache_nq<T>(a.c.lay.nb);
     c.slots = a.width * a.c.P <= kCacheLeast ? 0 : cache_slots(a.c.G);
-    c.items = columns / c.cols + requests + (c.slots ? ceil_div(kCacheTarget, a.c.G) : 0);
+    const int64_t tiles = columns / c.cols + requests;
+    c.joins = tiles < c.slots / 2 ? tiles : c.slots / 2;
+    c.items = tiles + (c.slots ? ceil_div(kCacheTarget, a.c.G) : 0);
     const size_t rows = (size_t)c.slots * a.c.G * c.cols;
     c.part = rows * 32 * a.c.lay.nb * sizeof(float);
     c.stat = (rows * sizeof(float2) + 255) & ~(size_t)255;
@@ -677,8 +825,8 @@ void cache_launch(const cache_attn_args &a, const cache_choice &c, hipStream_t s
 {
     constexpr int NQ = cache_nq<T>(NB);
     if (c.few) cache_few_kernel<T, NB><<<dim3((unsigned)c.items, a.c.G), 256, 0, st>>>(a);
-    else if constexpr (NQ > 1) cache_many_kernel<T, NB, NQ><<<dim3((unsigned)ceil_div(c.items, 4), a.c.G), 256, 0, st>>>(a);
-    if (c.slots) cache_join_kernel<T, NB><<<dim3((unsigned)ceil_div(c.slots, 2), a.c.G, c.cols), 256, 0, st>>>(a, c.cols);
+    else cache_many_kernel<T, NB, NQ><<<dim3((unsigned)c.items, a.c.G), 256, 0, st>>>(a);
+    if (c.slots) cache_join_kernel<T, NB><<<dim3((unsigned)c.joins, a.c.G, c.joins * a.c.G * c.cols <= 4096 ? c.cols : 4), 256, 0, st>>>(a, c.cols);
 }
 
 template <typename T> sp_status cache_attention(const cache_attn_args &a, const cache_choice &c, hipStream_t st);
