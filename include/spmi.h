@@ -276,7 +276,7 @@ sp_status sp_rotary_frequencies(int rotDim, double base, double factor, int64_t 
 
 /* Turns Q and K; sp_rotary_grad: the gradients with respect to Q and K, given those with respect to the results in the places of Q and K (the
  * same with -a for a).  Enqueues on `stream`; neither allocates nor synchronises.  Each result is rounded once.  Errors, in this order:
- * NULL (p), DTYPE, SHAPE, UNSUPPORTED (interleaved neither 0 nor 1), NULL, HIP. */
+ * NULL (p), DTYPE, SHAPE, UNSUPPORTED (interleaved neither 0 nor 1), TOO_LARGE (a token of 2^31 numbers or more), NULL, HIP. */
 sp_status sp_rotary(const sp_rotary_problem *p, void *stream);
 sp_status sp_rotary_grad(const sp_rotary_problem *p, void *stream);
 
@@ -325,7 +325,7 @@ sp_status sp_cache_map(const sp_cache_step *s, void *stream);
  * slot[i] (DEVICE).  Rows whose slot is not in [0, pages * pageTokens) are not stored, and are loaded as zeros.  No slot may be
  * given twice in a call that stores (it would hold a mixture of the rows).  sp_cache_load rounds to `dtype` (SP_F32 and SP_BF16: exact).
  * Enqueue on `stream`; neither allocate nor synchronise.  Errors, in this order: NULL (c), DTYPE, SHAPE, TOO_LARGE (pages * pageTokens or tokens of
- * 2^31 or more), NULL, HIP. */
+ * 2^31 or more, tokens * kvHeads of 2^29 or more), NULL, HIP. */
 sp_status sp_cache_store(const sp_cache *c, int dtype, int64_t tokens, const int32_t *slot, const void *K, int64_t ldk, int64_t hdk,
                          const void *V, int64_t ldv, int64_t hdv, void *stream);
 sp_status sp_cache_load(const sp_cache *c, int dtype, int64_t tokens, const int32_t *slot, void *K, int64_t ldk, int64_t hdk,

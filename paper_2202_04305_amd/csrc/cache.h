@@ -54,6 +54,12 @@ static inline bool cache_has_memory(const cache_view &v) { return v.pages == 0 |
 typedef __bf16 cache_bf16;
 typedef _Float16 cache_f16;
 
+template <int BYTE>
+__device__ __forceinline__ uint32_t cache_convert(uint32_t word, float scale)       // two codes -> two numbers
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, BYTE));
+}
+
 // What a code and a scale stand for.
 __device__ __forceinline__ float cache_number(uint32_t code, uint32_t scale)
 {

@@ -16,77 +16,98 @@ extern "C" sp_status sp_cache_bytes(const sp_cache *c, size_t *bytes)
 namespace {
 
 __device__ __forceinline__ int64_t at_least_0(int32_t x) { return x < 0 ? 0 : x; }
-__device__ __forceinline__ int32_t saturated(int64_t x) { return x > INT32_MAX ? INT32_MAX : (int32_t)x; }
+__device__ __forceinline__ int32_t saturated(int64_t x) { return x > INT32_MAX ? INT32_MAX : x < INT32_MIN ? INT32_MIN : (int32_t)x; }
 
-constexpr int kMapGroup = 64;            // requests of a workgroup
+constexpr int kMapGroup = 64;            // requests of a workgroup: a wave scans them
+
+__device__ __forceinline__ int64_t map_scan(int64_t v, int lane)             // sum of lanes 0 .. lane
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { const int64_t o = __shfl_up(v, d, 64); v += lane >= d ? o : 0; }
+    return v;
+}
 
 // One launch: workgroup (b, y) sums up the requests before its 64, scans its own, and writes slice y of their pages and tokens.  No
 // workgroup reads what another writes: a token in a new page takes the page from the list, as whoever writes the table does.
-__global__ __launch_bounds__(256) void map_kernel(sp_cache_step s)
+// A launch's latency bounds it (four loads that depend on each other), beyond 100000 tokens the search for a token's request.
+__global__ __launch_bounds__(256) void map_kernel(sp_cache_step s, spmi_divisor32 by_page)
 {
-    __shared__ int64_t sum[2][256];
-    __shared__ int64_t first_token[kMapGroup + 1], first_page[kMapGroup + 1], length[kMapGroup];
-    const int64_t r0 = (int64_t)blockIdx.x * kMapGroup, P = s.pageTokens;
-    const int count = (int)(s.requests - r0 < kMapGroup ? s.requests - r0 : kMapGroup), tid = threadIdx.x;
+    __shared__ int64_t before[2][4];
+    __shared__ int64_t first_token[kMapGroup + 1], first_page[kMapGroup + 1];
+    __shared__ uint32_t length[kMapGroup];
+    const int64_t r0 = (int64_t)blockIdx.x * kMapGroup;
+    const uint32_t P = s.pageTokens;
+    const int count = (int)(s.requests - r0 < kMapGroup ? s.requests - r0 : kMapGroup), tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    // pages of `tokens` < 2^32 tokens
+    auto pages_of = [&](int64_t tokens) { return tokens <= INT32_MAX - (int64_t)P ? (int64_t)spmi_div_by32((uint32_t)tokens + P - 1, by_page) : (tokens + P - 1) / P; };
+    auto needed = [&](int64_t len, int64_t add) { return pages_of(len + add) - pages_of(len); };
     int64_t tokens = 0, pages = 0;
     for (int64_t r = tid; r < r0; r += 256) {
         const int64_t len = at_least_0(s.length[r]), add = at_least_0(s.added[r]);
         tokens += add;
-        pages += (len + add + P - 1) / P - (len + P - 1) / P;
+        pages += needed(len, add);
     }
-    sum[0][tid] = tokens; sum[1][tid] = pages;
-    __syncthreads();
-    for (int d = 128; d >= 1; d >>= 1) {
-        if (tid < d) { sum[0][tid] += sum[0][tid + d]; sum[1][tid] += sum[1][tid + d]; }
-        __syncthreads();
-    }
-    if (tid == 0) {
-        int64_t t = sum[0][0], p = sum[1][0];
-        for (int k = 0; k < count; ++k) {
-            const int64_t len = at_least_0(s.length[r0 + k]), add = at_least_0(s.added[r0 + k]);
-            first_token[k] = t; first_page[k] = p; length[k] = len;
-            t += add;
-            p += (len + add + P - 1) / P - (len + P - 1) / P;
-        }
-        first_token[count] = t; first_page[count] = p;
-    }
-    __syncthreads();
     const int64_t taken = *s.taken;
+    int64_t len = 0, add = 0;
+    if (w == 0 && lane < count) { len = at_least_0(s.length[r0 + lane]); add = at_least_0(s.added[r0 + lane]); }
+    if (r0) {
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) { tokens += __shfl_xor(tokens, d, 64); pages += __shfl_xor(pages, d, 64); }
+        if (lane == 0) { before[0][w] = tokens; before[1][w] = pages; }
+        __syncthreads();
+        tokens = (before[0][0] + before[0][1]) + (before[0][2] + before[0][3]);
+        pages = (before[1][0] + before[1][1]) + (before[1][2] + before[1][3]);
+    }
+    if (w == 0) {
+        const int64_t more = needed(len, add);
+        const int64_t t = tokens + map_scan(add, lane), p = pages + map_scan(more, lane);
+        first_token[lane] = t - add; first_page[lane] = p - more;
+        length[lane] = (uint32_t)len;
+        if (lane == 63) { first_token[64] = t; first_page[64] = p; }
+    }
+    __syncthreads();
+    const int64_t all_tokens = first_token[64], all_pages = first_page[64];          // requests beyond `count` have neither
     auto free_page = [&](int64_t k) -> int64_t {
         k += taken;
         const int64_t page = k >= 0 && k < s.freeCount ? s.freePages[k] : -1;
         return page >= 0 && page < s.pages ? page : -1;
     };
     auto request_of = [&](const int64_t *first, int64_t x) {             // the last one that begins at x or before
-        int lo = 0, hi = count;
-        while (hi - lo > 1) { const int mid = (lo + hi) / 2; if (first[mid] <= x) lo = mid; else hi = mid; }
-        return lo;
+        int k = 0;
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) k += k + d < count && first[k + d] <= x ? d : 0;
+        return k;
     };
     const int64_t step = (int64_t)gridDim.y * 256, me = (int64_t)blockIdx.y * 256 + tid;
-    for (int64_t x = first_page[0] + me; x < first_page[count]; x += step) {
+    for (int64_t x = first_page[0] + me; x < all_pages; x += step) {
         const int k = request_of(first_page, x);
-        const int64_t at = (length[k] + P - 1) / P + x - first_page[k];
+        const int64_t at = pages_of(length[k]) + x - first_page[k];
         if (at < s.width) s.table[(r0 + k) * s.ldt + at] = (int32_t)free_page(x);
     }
-    const int64_t end = first_token[count] < s.tokens ? first_token[count] : s.tokens;
+    const int64_t end = all_tokens < s.tokens ? all_tokens : s.tokens;
     for (int64_t x = first_token[0] + me; x < end; x += step) {
         const int k = request_of(first_token, x);
-        const int64_t position = length[k] + x - first_token[k], at = position / P, held = (length[k] + P - 1) / P;
-        int64_t page = -1;
-        if (at < s.width) page = at >= held ? free_page(first_page[k] + at - held) : s.table[(r0 + k) * s.ldt + at];
+        const int64_t position = length[k] + x - first_token[k], held = pages_of(length[k]);
+        int64_t slot = -1;
+        if (position <= INT32_MAX) {
+            const uint32_t at = spmi_div_by32((uint32_t)position, by_page);
+            int64_t page = -1;
+            if (at < s.width) page = at >= held ? free_page(first_page[k] + at - held) : s.table[(r0 + k) * s.ldt + at];
+            if (page >= 0 && page < s.pages) slot = page * P + (uint32_t)position - at * P;
+        }
         s.position[x] = saturated(position);
-        s.slot[x] = page >= 0 && page < s.pages ? (int32_t)(page * P + position % P) : -1;
+        s.slot[x] = (int32_t)slot;
     }
     const bool last = r0 + count == s.requests;
     if (last) for (int64_t x = end + me; x < s.tokens; x += step) s.position[x] = s.slot[x] = -1;
     if (blockIdx.y == 0) {
-        if (tid < count) {
-            s.start[r0 + tid] = saturated(first_token[tid]);
-            s.lengthOut[r0 + tid] = saturated(length[tid] + at_least_0(s.added[r0 + tid]));
+        if (w == 0 && lane < count) {
+            s.start[r0 + lane] = saturated(first_token[lane]);
+            s.lengthOut[r0 + lane] = saturated(len + add);
         }
         if (last && tid == 0) {
-            s.start[s.requests] = saturated(first_token[count]);
-            *s.takenOut = saturated(taken + first_page[count]);
+            s.start[s.requests] = saturated(all_tokens);
+            *s.takenOut = saturated(taken + all_pages);
         }
     }
 }
@@ -102,11 +123,12 @@ extern "C" sp_status sp_cache_map(const sp_cache_step *s, void *stream)
     if (s->pages >= ceil_div(top, s->pageTokens) || s->requests >= top || s->tokens >= top) return SP_ERR_TOO_LARGE;
     if (!s->taken || !s->takenOut || !s->start || (s->requests && (!s->length || !s->added || !s->lengthOut || (s->width && !s->table))) ||
         (s->freeCount && !s->freePages) || (s->tokens && (!s->position || !s->slot))) return SP_ERR_NULL;
-    // a workgroup for each 64 requests (one where there are none), cut into slices of 2048 tokens of what the step has room for
+    // a workgroup for each 64 requests (one where there are none), cut into slices of 1024 tokens of what the step has room for
     const int64_t groups = s->requests ? ceil_div(s->requests, kMapGroup) : 1;
-    int64_t slices = ceil_div(ceil_div(s->tokens, groups), 2048);
+    int64_t slices = ceil_div(ceil_div(s->tokens, groups), 1024);
     slices = slices < 1 ? 1 : slices > 256 ? 256 : slices;
-    map_kernel<<<dim3((unsigned)groups, (unsigned)slices), 256, 0, (hipStream_t)stream>>>(*s);
+    if (groups >= (int64_t)1 << 24) return SP_ERR_TOO_LARGE;
+    map_kernel<<<dim3((unsigned)groups, (unsigned)slices), 256, 0, (hipStream_t)stream>>>(*s, spmi_make_divisor32(s->pageTokens));
     SP_HIP(hipGetLastError());
     return SP_OK;
 }
@@ -133,68 +155,138 @@ __device__ __forceinline__ int cache_exponent(float top)
     return e < kCacheMinExp ? kCacheMinExp : e > kCacheMaxExp ? kCacheMaxExp : e;
 }
 
-// A thread for each block of 32 numbers of K or V.
+constexpr int kStoreTokens = 32;         // of a workgroup, which takes one head of them
+
+// Eight numbers of a row, zeros behind its end.
 template <typename T>
-__global__ __launch_bounds__(256) void store_kernel(cache_rows a)
+__device__ __forceinline__ void load8(const T *row, int d0, int D, bool vec, float (&x)[8])
 {
-    const cache_view &c = a.c;
-    const int nb = c.lay.nb;
-    const int64_t n = a.tokens * c.G * 2 * nb;
-    for (int64_t x = blockIdx.x * (int64_t)256 + threadIdx.x; x < n; x += (int64_t)gridDim.x * 256) {
-        const int s = (int)(x % nb), which = (int)(x / nb % 2), g = (int)(x / (2 * nb) % c.G);
-        const int64_t i = x / (2 * nb) / c.G;
-        const int64_t slot = a.slot[i];
-        if (slot < 0 || slot >= c.pages * c.P) continue;
-        const T *in = which ? (const T *)a.V + i * a.ldv + g * a.hdv : (const T *)a.K + i * a.ldk + g * a.hdk;
-        float v[kCacheBlock], top = 0;
-        bool finite = true;
-        for (int d = 0; d < kCacheBlock; ++d) {
-            v[d] = 32 * s + d < c.D ? (float)in[32 * s + d] : 0.f;
-            top = fmaxf(top, fabsf(v[d]));
-            finite = finite && v[d] - v[d] == 0;
-        }
-        const int e = cache_exponent(finite ? top : 0.f);
-        const float scale = __uint_as_float((uint32_t)(e + 127) << 23);
-        uint32_t code[4];
-        for (int w = 0; w < 4; ++w) {
-            uint32_t q = 0;
-            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w], v[8 * w + 1], scale, 0);
-            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w + 2], v[8 * w + 3], scale, 1);
-            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w + 4], v[8 * w + 5], scale, 2);
-            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[8 * w + 6], v[8 * w + 7], scale, 3);
-            code[w] = q;
-        }
-        const int t = (int)(slot % c.P);
-        uint8_t *rec = c.record(slot / c.P, g, t);
-        const int u = t % kCacheTile;
-        rec[(which ? c.lay.v_scales() : c.lay.k_scales()) + u * c.lay.sb + s] = finite ? (uint8_t)(e + 127) : (uint8_t)kCacheNaN;
-        if (!which) for (int w = 0; w < 4; ++w) ((uint32_t *)rec)[(u * 4 + w) * nb + s] = code[w];
-        else for (int k = 0; k < 16; ++k) {
-            const uint32_t lo = (code[k / 8] >> (4 * (k % 8))) & 15, hi = (code[2 + k / 8] >> (4 * (k % 8))) & 15;
-            rec[c.lay.v_codes() + (((u >> 2) * 16 + k) * nb + s) * 4 + (u & 3)] = (uint8_t)(lo | hi << 4);
-        }
+    if (vec) {
+        typedef T row8 __attribute__((ext_vector_type(8)));
+        row8 v = {};
+        if (d0 < D) v = *(const row8 *)(row + d0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = d0 + j < D ? (float)row[d0 + j] : 0.f;
     }
 }
 
-// A thread for each number of K and of V.
-template <typename T>
-__global__ __launch_bounds__(256) void load_kernel(cache_rows a)
+// Rows into the pages.  Their bytes bound it.  Four neighbouring lanes have a block of 32 numbers, 8 each, which are a word of K as they lie.  A
+// token's values are every fourth byte of 64 NB, so the tokens of a workgroup meet in the LDS, from where four that are neighbours in the
+// pages (aligned to four) go out as words, others as bytes.
+template <typename T, int NB>
+__global__ __launch_bounds__(256) void store_kernel(cache_rows a, int vec)
 {
+    constexpr int words = 4 * NB, row = 16 * NB;         // lanes of a token; bytes of a token's values
+    __shared__ uint8_t bytes[kStoreTokens][row];
+    __shared__ int32_t slots[kStoreTokens + 3];
     const cache_view &c = a.c;
-    const int64_t n = a.tokens * c.G * c.D;
-    for (int64_t x = blockIdx.x * (int64_t)256 + threadIdx.x; x < n; x += (int64_t)gridDim.x * 256) {
-        const int d = (int)(x % c.D), g = (int)(x / c.D % c.G);
-        const int64_t i = x / c.D / c.G;
-        const int64_t slot = a.slot[i];
-        float k = 0, v = 0;
-        if (slot >= 0 && slot < c.pages * c.P) {
-            const int t = (int)(slot % c.P);
-            const uint8_t *rec = c.record(slot / c.P, g, t);
-            k = cache_key(c, rec, t % kCacheTile, d);
-            v = cache_value(c, rec, t % kCacheTile, d);
+    const uint32_t window = blockIdx.x / (uint32_t)c.G, head = blockIdx.x - window * (uint32_t)c.G;
+    const int64_t i0 = (int64_t)window * kStoreTokens, room = c.pages * c.P;
+    const int tokens = (int)(a.tokens - i0 < kStoreTokens ? a.tokens - i0 : kStoreTokens), g = (int)head;
+    if (threadIdx.x < kStoreTokens + 3) {
+        const int32_t slot = (int)threadIdx.x < tokens ? a.slot[i0 + threadIdx.x] : -1;
+        slots[threadIdx.x] = slot < room ? slot : -1;
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < tokens * words; x += 256) {            // the four lanes of a block stay together
+        const int i = x / words, s = (x % words) / 4, q = x & 3, d0 = 32 * s + 8 * q;
+        const int32_t slot = slots[i];
+        if (slot < 0) continue;
+        const int t = (int)((uint32_t)slot % (uint32_t)c.P);
+        uint8_t *rec = c.record((uint32_t)slot / (uint32_t)c.P, g, t);
+        const int u = t % kCacheTile;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float v[8];
+            load8<T>(which ? (const T *)a.V + (i0 + i) * a.ldv + g * a.hdv : (const T *)a.K + (i0 + i) * a.ldk + g * a.hdk, d0, c.D, vec, v);
+            float top = 0, none = 0;                     // none: 0, or not a number
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { top = fmaxf(top, fabsf(v[j])); none += v[j] - v[j]; }
+            top = fmaxf(top, __shfl_xor(top, 1, 64)); none += __shfl_xor(none, 1, 64);
+            top = fmaxf(top, __shfl_xor(top, 2, 64)); none += __shfl_xor(none, 2, 64);
+            const bool finite = none == 0;
+            const int e = cache_exponent(finite ? top : 0.f);
+            const float scale = __uint_as_float((uint32_t)(e + 127) << 23);
+            uint32_t code = 0;
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[0], v[1], scale, 0);
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[2], v[3], scale, 1);
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[4], v[5], scale, 2);
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[6], v[7], scale, 3);
+            if (q == 0) rec[(which ? c.lay.v_scales() : c.lay.k_scales()) + u * c.lay.sb + s] = finite ? (uint8_t)(e + 127) : (uint8_t)kCacheNaN;
+            if (!which) ((uint32_t *)rec)[(u * 4 + q) * NB + s] = code;
+            else {
+                // numbers 32 s + n and 32 s + 16 + n share a byte: lanes q and q + 2
+                const uint32_t other = __shfl_xor(code, 2, 64), lo = q < 2 ? code : other, hi = q < 2 ? other : code;
+                // this lane's four bytes of the eight: n = 8 (q & 1) + 4 (q >> 1) + 0 .. 3
+                const uint32_t l = q < 2 ? lo & 0xffff : lo >> 16, h = q < 2 ? hi & 0xffff : hi >> 16;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    bytes[i][(8 * (q & 1) + 4 * (q >> 1) + j) * NB + s] = (uint8_t)(((l >> (4 * j)) & 15) | ((h >> (4 * j)) & 15) << 4);
+            }
         }
-        ((T *)a.Kout)[i * a.ldk + g * a.hdk + d] = (T)k;
-        ((T *)a.Vout)[i * a.ldv + g * a.hdv + d] = (T)v;
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < tokens * row; x += 256) {
+        const int i = x / row, k = x % row, slot = slots[i];
+        if (slot < 0) continue;
+        // four neighbours, of which this is the first, or another one that the first takes along
+        const int lead = i - (slot & 3);
+        const bool four = lead >= 0 && slots[lead] == (slot & ~3) && slots[lead + 1] == (slot & ~3) + 1 && slots[lead + 2] == (slot & ~3) + 2 && slots[lead + 3] == (slot & ~3) + 3;
+        if (four && lead != i) continue;
+        const int t = (int)((uint32_t)slot % (uint32_t)c.P);
+        uint8_t *at = c.record((uint32_t)slot / (uint32_t)c.P, g, t) + c.lay.v_codes() + ((t % kCacheTile >> 2) * row + k) * 4;
+        if (four) *(uint32_t *)at = bytes[i][k] | bytes[i + 1][k] << 8 | bytes[i + 2][k] << 16 | (uint32_t)bytes[i + 3][k] << 24;
+        else at[t & 3] = bytes[i][k];
+    }
+}
+
+// Eight codes, to pairs of bf16.
+__device__ __forceinline__ void cache_eight(uint32_t word, float scale, uint32_t (&x)[4])
+{
+    x[0] = cache_convert<0>(word, scale); x[1] = cache_convert<1>(word, scale); x[2] = cache_convert<2>(word, scale); x[3] = cache_convert<3>(word, scale);
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *row, int d0, int D, bool vec, const uint32_t (&x)[4])
+{
+    typedef T row8 __attribute__((ext_vector_type(8)));
+    row8 v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (T)__uint_as_float(j % 2 ? x[j / 2] & 0xffff0000u : x[j / 2] << 16);
+    if (vec) { if (d0 < D) *(row8 *)(row + d0) = v; }
+    else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (d0 + j < D) row[d0 + j] = v[j];
+}
+
+// Rows out of the pages: a lane for 8 numbers of K and of V.
+template <typename T, int NB>
+__global__ __launch_bounds__(256) void load_kernel(cache_rows a, int vec)
+{
+    constexpr int words = 4 * NB;
+    const cache_view &c = a.c;
+    const int64_t n = a.tokens * c.G * words;
+    for (int64_t x = blockIdx.x * (int64_t)256 + threadIdx.x; x < n; x += (int64_t)gridDim.x * 256) {
+        const int64_t r = x / words, i = n <= INT32_MAX ? (uint32_t)r / (uint32_t)c.G : r / c.G;
+        const int g = (int)(r - i * c.G), s = (int)(x % words) / 4, q = (int)(x & 3), d0 = 32 * s + 8 * q;
+        const int64_t slot = a.slot[i];
+        uint32_t k[4] = {}, v[4] = {};                   // as pairs of bf16
+        if (slot >= 0 && slot < c.pages * c.P) {
+            const int t = (int)((uint32_t)slot % (uint32_t)c.P), u = t % kCacheTile;
+            const uint8_t *rec = c.record((uint32_t)slot / (uint32_t)c.P, g, t);
+            const uint32_t kw = ((const uint32_t *)rec)[(u * 4 + q) * NB + s];
+            const uint8_t *b = rec + c.lay.v_codes() + (((u >> 2) * 16 + 8 * (q & 1)) * NB + s) * 4 + (u & 3);
+            uint32_t vw = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) vw |= (((uint32_t)b[j * NB * 4] >> (q & 2 ? 4 : 0)) & 15) << (4 * j);
+            const float ks = __uint_as_float((uint32_t)rec[c.lay.k_scales() + u * c.lay.sb + s] << 23), vs = __uint_as_float((uint32_t)rec[c.lay.v_scales() + u * c.lay.sb + s] << 23);
+            cache_eight(kw, ks, k);
+            cache_eight(vw, vs, v);
+        }
+        store8<T>((T *)a.Kout + i * a.ldk + g * a.hdk, d0, c.D, vec, k);
+        store8<T>((T *)a.Vout + i * a.ldv + g * a.hdv, d0, c.D, vec, v);
     }
 }
 
@@ -207,13 +299,53 @@ sp_status check_rows(const sp_cache *c, int dtype, int64_t tokens, bool out, cac
     if (out ? (tokens > 1 && (a->ldk < least || a->ldv < least)) || (c->kvHeads > 1 && (a->hdk < least || a->hdv < least))
             : a->ldk < 0 || a->ldv < 0 || a->hdk < 0 || a->hdv < 0) return SP_ERR_SHAPE;
     SP_TRY(cache_check(c, &a->c));
-    if (tokens >= (int64_t)1 << 31) return SP_ERR_TOO_LARGE;
+    if (tokens >= (int64_t)1 << 31 || ceil_div(tokens, kStoreTokens) * c->kvHeads >= (int64_t)1 << 24) return SP_ERR_TOO_LARGE;        // 2^32 threads of a launch
     a->tokens = tokens;
     if (tokens && (!a->slot || !cache_has_memory(a->c) || (out ? !a->Kout || !a->Vout : !a->K || !a->V))) return SP_ERR_NULL;
     return SP_OK;
 }
 
-int grid(int64_t threads) { const int64_t b = ceil_div(threads, 256); return (int)(b < 65536 ? b : 65536); }
+// Can rows be read and written 8 numbers at a time?
+bool aligned(const cache_rows &a, int size)
+{
+    const int64_t stray = (uintptr_t)a.K | (uintptr_t)a.V | (uintptr_t)a.Kout | (uintptr_t)a.Vout | (uintptr_t)(size * (a.ldk | a.hdk | a.ldv | a.hdv));
+    return a.c.D % 8 == 0 && stray % 16 == 0;
+}
+
+template <typename T, int NB>
+void launch_rows(const cache_rows &a, bool store, hipStream_t st)
+{
+    const int vec = aligned(a, sizeof(T));
+    if (store) store_kernel<T, NB><<<(unsigned)(ceil_div(a.tokens, kStoreTokens) * a.c.G), 256, 0, st>>>(a, vec);
+    else {
+        const int64_t blocks = ceil_div(a.tokens * a.c.G * 4 * NB, 256);
+        load_kernel<T, NB><<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(a, vec);
+    }
+}
+
+template <typename T>
+void launch_rows_of(const cache_rows &a, bool store, hipStream_t st)
+{
+    switch (a.c.lay.nb) {
+    case 1: return launch_rows<T, 1>(a, store, st);
+    case 2: return launch_rows<T, 2>(a, store, st);
+    case 3: return launch_rows<T, 3>(a, store, st);
+    case 4: return launch_rows<T, 4>(a, store, st);
+    case 5: return launch_rows<T, 5>(a, store, st);
+    case 6: return launch_rows<T, 6>(a, store, st);
+    case 7: return launch_rows<T, 7>(a, store, st);
+    default: return launch_rows<T, 8>(a, store, st);
+    }
+}
+
+sp_status run_rows(const cache_rows &a, int dtype, bool store, hipStream_t st)
+{
+    if (dtype == SP_F32) launch_rows_of<float>(a, store, st);
+    else if (dtype == SP_F16) launch_rows_of<cache_f16>(a, store, st);
+    else launch_rows_of<cache_bf16>(a, store, st);
+    SP_HIP(hipGetLastError());
+    return SP_OK;
+}
 
 }  // namespace
 
@@ -223,13 +355,7 @@ extern "C" sp_status sp_cache_store(const sp_cache *c, int dtype, int64_t tokens
     cache_rows a = {{}, slot, 0, K, V, nullptr, nullptr, ldk, hdk, ldv, hdv};
     SP_TRY(check_rows(c, dtype, tokens, false, &a));
     if (tokens == 0 || a.c.pages == 0) return SP_OK;
-    const int n = grid(tokens * a.c.G * 2 * a.c.lay.nb);
-    hipStream_t st = (hipStream_t)stream;
-    if (dtype == SP_F32) store_kernel<float><<<n, 256, 0, st>>>(a);
-    else if (dtype == SP_F16) store_kernel<cache_f16><<<n, 256, 0, st>>>(a);
-    else store_kernel<cache_bf16><<<n, 256, 0, st>>>(a);
-    SP_HIP(hipGetLastError());
-    return SP_OK;
+    return run_rows(a, dtype, true, (hipStream_t)stream);
 }
 
 extern "C" sp_status sp_cache_load(const sp_cache *c, int dtype, int64_t tokens, const int32_t *slot, void *K, int64_t ldk, int64_t hdk,
@@ -238,11 +364,5 @@ extern "C" sp_status sp_cache_load(const sp_cache *c, int dtype, int64_t tokens,
     cache_rows a = {{}, slot, 0, nullptr, nullptr, K, V, ldk, hdk, ldv, hdv};
     SP_TRY(check_rows(c, dtype, tokens, true, &a));
     if (tokens == 0) return SP_OK;
-    const int n = grid(tokens * a.c.G * a.c.D);
-    hipStream_t st = (hipStream_t)stream;
-    if (dtype == SP_F32) load_kernel<float><<<n, 256, 0, st>>>(a);
-    else if (dtype == SP_F16) load_kernel<cache_f16><<<n, 256, 0, st>>>(a);
-    else load_kernel<cache_bf16><<<n, 256, 0, st>>>(a);
-    SP_HIP(hipGetLastError());
-    return SP_OK;
+    return run_rows(a, dtype, false, (hipStream_t)stream);
 }

@@ -21,7 +21,7 @@ struct cache_attn_args {
     int H, R, causal;                    // R = H / G heads share a head of the cache
     float sign, step;                    // scale log2(e) = sign step; sign = -1, 0, 1 goes into Q, step > 0
     int vec;                             // rows of Q and O are aligned to 8 numbers
-    uint32_t page_mul, page_shift;       // x / (P / 16) = x page_mul >> page_shift, the product in 64 bits
+    spmi_divisor32 records;              // of a page: P / 16
     float *part;                         // workspace: [slot][head of the cache][column][32 nb] sums
     float2 *stat;                        //            [slot][head of the cache][column]: running maximum (in units of log 2) and total
     uint32_t slots;                      // slots there is room for
@@ -31,9 +31,9 @@ struct cache_attn_args {
 // The columns of a request (its queries times the heads that share a head of the cache) are cut into tiles, its tokens into chunks, and an
 // item is a tile, a chunk and a head of the cache.  Lengths are known on the GPU alone, so every workgroup finds its item by a scan over
 // the requests.  Chunks are as long as makes about kCacheTarget items of all work, at least kCacheLeast tokens.
-constexpr int kCacheTarget = 1024, kCacheLeast = 256;
+constexpr int kCacheTarget = 512, kCacheLeast = 256;
 
-struct cache_request { uint32_t n, columns, tiles, tokens, row0; int32_t last; };   // row0: its first row; last: position of its last query, -1 or more
+struct cache_request { uint32_t n, columns, tiles, tokens, row0; int32_t last; uint32_t r; };      // row0: its first row; last: position of its last query, -1 or more; r: its number
 struct cache_item {
     int64_t r, row0;                     // the request and its first row
     cache_request q;
@@ -44,7 +44,7 @@ static inline __host__ __device__ int64_t cache_limit(int64_t x, int64_t lo, int
 
 __device__ __forceinline__ cache_request cache_request_of(const cache_attn_args &a, int64_t r, int cols)
 {
-    cache_request q = {0, 0, 0, 0, 0, -1};
+    cache_request q = {0, 0, 0, 0, 0, -1, (uint32_t)r};
     if (r >= a.requests) return q;
     const int64_t s0 = cache_limit(a.start[r], 0, a.tokens), s1 = cache_limit(a.start[r + 1], 0, a.tokens), len = a.length[r];
     if (s1 <= s0) return q;
@@ -78,8 +78,22 @@ __device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a,
     const uint64_t c = (work * a.c.G + kCacheTarget - 1) / kCacheTarget;
     return c < kCacheLeast ? kCacheLeast : c > 0x7fffff00u ? 0x7fffff00u : ((uint32_t)c + 127) & ~127u;
 }
+// The heads of the cache of one item are neighbours: workgroups go to the eight XCDs in turn, so that with 8 heads (or 4, 16, ..) what one L2 holds
+// of the pages serves all tiles of a request.
 // Chunks longer than the work's share make fewer than 2 kCacheTarget / G slots: a request of more than one has chunks < 2 tokens / length.
 static inline int64_t cache_slots(int G) { return 2 * ceil_div(kCacheTarget, G); }
+
+// The lanes' requests in the order of their tokens, the longest first, so that a launch does not end with the longest alone.
+__device__ __forceinline__ void cache_longest_first(cache_request *q, int lane)
+{
+    uint32_t rank = 0;
+    for (int k = 0; k < 64; ++k) {
+        const uint32_t other = __builtin_amdgcn_readlane(q->tokens, k);
+        rank += other > q->tokens || (other == q->tokens && k < lane) ? 1 : 0;
+    }
+    auto move = [rank](uint32_t x) { return (uint32_t)__builtin_amdgcn_ds_permute((int)rank * 4, (int)x); };
+    *q = {move(q->n), move(q->columns), move(q->tiles), move(q->tokens), move(q->row0), (int32_t)move((uint32_t)q->last), move(q->r)};
+}
 
 // Item `index` of all (joined = false), or tile `index` of those that have more than one chunk.  For a whole wave; false: there is none.
 __device__ __forceinline__ bool cache_find(const cache_attn_args &a, int cols, uint32_t index, bool joined, int lane, cache_item *item)
@@ -89,6 +103,8 @@ __device__ __forceinline__ bool cache_find(const cache_attn_args &a, int cols, u
     uint32_t items = 0, slots = 0;
     for (int64_t base = 0; base < a.requests; base += 64) {
         if (base) q = cache_request_of(a, base + lane, cols);
+        if (joined && !__builtin_amdgcn_ballot_w64(q.tokens > len && q.tiles)) continue;         // no chunks to join here
+        if (cols > 16) cache_longest_first(&q, lane);
         const uint32_t chunks = q.tokens <= len ? 1 : (q.tokens + len - 1) / len;
         const uint32_t mine = joined ? (chunks > 1 ? q.tiles : 0) : q.tiles * chunks, room = chunks > 1 ? q.tiles * chunks : 0;
         const uint32_t upto = items + cache_wave_scan(mine, lane), slot = slots + cache_wave_scan(room, lane);
@@ -97,7 +113,7 @@ __device__ __forceinline__ bool cache_find(const cache_attn_args &a, int cols, u
             const int k = __builtin_ctzll(behind);
             auto of = [k](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, k); };
             const uint32_t rest = index - (of(upto) - of(mine));
-            item->r = base + k;
+            item->r = of(q.r);
             item->row0 = of(q.row0);
             item->q.n = of(q.n); item->q.columns = of(q.columns); item->q.tiles = of(q.tiles); item->q.tokens = of(q.tokens);
             item->q.last = (int64_t)(int32_t)of((uint32_t)q.last);
@@ -113,7 +129,7 @@ __device__ __forceinline__ bool cache_find(const cache_attn_args &a, int cols, u
     return false;
 }
 
-__device__ __forceinline__ uint32_t cache_page_of(const cache_attn_args &a, uint32_t record) { return (uint32_t)((uint64_t)record * a.page_mul >> a.page_shift); }
+__device__ __forceinline__ uint32_t cache_page_of(const cache_attn_args &a, uint32_t record) { return spmi_div_by32(record, a.records); }
 
 // ---- one column by itself ---------------------------------------------------------------------------------------------------
 
@@ -184,11 +200,6 @@ __device__ __forceinline__ void cache_words(const uint8_t *p, uint32_t (&w)[N]) 
     if constexpr (N % 4 >= 2) { const v2 v = *(const v2 *)(x + k); w[k] = v[0]; w[k + 1] = v[1]; k += 2; }
     if constexpr (N % 2) w[k] = x[k];
 }
-template <int BYTE>
-__device__ __forceinline__ uint32_t cache_convert(uint32_t word, float scale)       // two codes -> two numbers
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, BYTE));
-}
 __device__ __forceinline__ uint32_t cache_pair(float x, float y)                    // rounded to bf16
 {
     typedef float f2 __attribute__((ext_vector_type(2)));
@@ -198,7 +209,7 @@ __device__ __forceinline__ uint32_t cache_pair(float x, float y)                
 // What a lane holds of a record, 16 tokens: its words of K and V and their scales.
 template <int NB>
 struct cache_record {
-    static constexpr int SB = NB <= 2 ? NB : NB <= 4 ? 4 : 8, KS = (SB + 3) / 4;
+    static constexpr int SB = NB <= 2 ? NB : NB <= 4 ? 4 : 8, KS = (SB + 3) / 4, bytes = 512 * NB + 32 * SB;
     uint32_t k[NB], v[NB], ks[KS], vs[SB];
     __device__ __forceinline__ void load(const uint8_t *rec, int lane)
     {
@@ -249,8 +260,7 @@ struct cache_record {
 template <int NB>
 struct cache_tokens {
     cache_record<NB> half[2];
-    __device__ __forceinline__ cache_b8 key(int h, int b, int) const { return half[h].key(b); }
-    __device__ __forceinline__ void values(int b, int, cache_b8 &lo, cache_b8 &hi) const
+    __device__ __forceinline__ void values(int b, cache_b8 &lo, cache_b8 &hi) const
     {
         uint32_t l[2][2], h[2][2];
         half[0].values(b, l[0], h[0]);
@@ -258,23 +268,10 @@ struct cache_tokens {
         lo = __builtin_bit_cast(cache_b8, (cache_u4){l[0][0], l[0][1], l[1][0], l[1][1]});
         hi = __builtin_bit_cast(cache_b8, (cache_u4){h[0][0], h[0][1], h[1][0], h[1][1]});
     }
-    __device__ __forceinline__ void blank(int h, int token) { half[h].blank(token); }
 };
 
-// The same as operands in LDS, where the waves of a workgroup share them: 32 tokens of a stretch of 64.
-template <int NB>
-struct cache_staged {
-    static constexpr int kv = 4 * NB * 1024;             // bytes of the operands of K (and of V) of 64 tokens
-    const char *k, *v;                                   // of these 32 tokens
-    __device__ __forceinline__ cache_staged(const char *stage, int pair) : k(stage + pair * 2 * NB * 1024), v(stage + kv + pair * 2 * NB * 1024) {}
-    __device__ __forceinline__ cache_b8 key(int half, int b, int lane) const { return *(const cache_b8 *)(k + (half * NB + b) * 1024 + lane * 16); }
-    __device__ __forceinline__ void values(int b, int lane, cache_b8 &lo, cache_b8 &hi) const
-    {
-        lo = *(const cache_b8 *)(v + b * 2048 + lane * 16);
-        hi = *(const cache_b8 *)(v + b * 2048 + 1024 + lane * 16);
-    }
-    __device__ __forceinline__ void blank(int, int) {}   // done where they were written
-};
+// A number that all lanes share, in a vector register.
+__device__ __forceinline__ float cache_spread(float x) { asm volatile("" : "+v"(x)); return x; }
 
 // 16 NQ columns of one tile over some of its tokens, by one wave.
 template <typename T, int NB, int NQ>
@@ -282,7 +279,8 @@ struct cache_wave {
     static constexpr int parts = cache_parts<T>::n;
     cache_b8 q[NQ][parts][NB];
     cache_f4 o[NQ][2 * NB];
-    float top[NQ], mu[NQ], total[NQ];    // running maximum (the same in the four lanes of a column); what is taken off; a lane's own share of the total
+    float top[NQ], mu[NQ], most[NQ];     // running maximum (the same in the four lanes of a column); what is taken off; sum of weights that moves it
+    float total[NQ];                     // a lane's own share of the total
     uint32_t end[NQ];                    // the column attends to tokens before this one
 
     // Q's column: 8 numbers of every block
@@ -297,7 +295,7 @@ struct cache_wave {
             const T *row = (const T *)a.Q + (it.row0 + i) * a.ldq + (int64_t)(g * a.R + hh) * a.hdq;
             const int64_t e = a.causal ? (int64_t)it.q.last - it.q.n + 2 + i : (int64_t)it.q.tokens;
             end[k] = there ? (uint32_t)cache_limit(e, 0, it.q.tokens) : it.q.tokens;
-            top[k] = -INFINITY; mu[k] = 0; total[k] = 0;
+            top[k] = -INFINITY; mu[k] = 0; most[k] = -1; total[k] = 0;
 #pragma unroll
             for (int s = 0; s < 2 * NB; ++s) o[k][s] = (cache_f4)(0.f);
 #pragma unroll
@@ -335,58 +333,63 @@ struct cache_wave {
         }
     }
 
-    // 32 tokens from t on.  partial: some column attends to some of them only; there: which halves' pages exist; tokens: the request's.
-    // One path for both, as two would be merged by the compiler into one that keeps everything of both at once.
-    template <typename S>
-    __device__ __forceinline__ void tokens32(S &x, float step, uint32_t t, uint32_t tokens, uint32_t there, bool partial, int lane)
+    // S^T of 32 tokens; key(half, b): the operands of K
+    template <typename F>
+    __device__ __forceinline__ void scores(cache_f4 (&s)[NQ][2], F key) const
     {
-        const int g = lane >> 4;
-        cache_f4 s[NQ][2];
 #pragma unroll
         for (int k = 0; k < NQ; ++k) s[k][0] = s[k][1] = (cache_f4)(0.f);
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int b = 0; b < NB; ++b) {
+            const cache_b8 x[2] = {key(0, b), key(1, b)};
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const cache_b8 key = x.key(half, b, lane);
+            for (int p = 0; p < parts; ++p)
 #pragma unroll
                 for (int k = 0; k < NQ; ++k)
 #pragma unroll
-                    for (int p = 0; p < parts; ++p) s[k][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[k][p][b], s[k][half], 0, 0, 0);
-            }
-        if (partial) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t at = t + 16 * half + 4 * g + j;
-                    const bool page = (there >> half) & 1;
-#pragma unroll
-                    for (int k = 0; k < NQ; ++k) s[k][half][j] = page && at < end[k] ? s[k][half][j] : -INFINITY;
-                    if (!page || at >= tokens) x.blank(half, j);        // behind the request's tokens: anything may be there
-                }
+                    for (int half = 0; half < 2; ++half)         // sums that do not wait for each other
+                        s[k][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[half], q[k][p][b], s[k][half], 0, 0, 0);
         }
-        cache_b8 w[NQ][parts];
+    }
+    // Where some column attends to some of the 32 tokens from t on only; there: which halves' pages exist
+    __device__ __forceinline__ void leave_out(cache_f4 (&s)[NQ][2], uint32_t t, uint32_t there, int lane) const
+    {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t at = t + 16 * half + 4 * (lane >> 4) + j;
+#pragma unroll
+                for (int k = 0; k < NQ; ++k) s[k][half][j] = ((there >> half) & 1) && at < end[k] ? s[k][half][j] : -INFINITY;
+            }
+    }
+    // The weights as operands, and their sums.
+    __device__ __forceinline__ void weights(const cache_f4 (&s)[NQ][2], float step, cache_b8 (&w)[NQ][parts])
+    {
 #pragma unroll
         for (int k = 0; k < NQ; ++k) {
-            // The maximum that is taken off lags behind by up to 8 (a factor of 256): moving it costs a pass over the sums, and it moves in
-            // the first tokens of a chunk, hardly later.
-            float most = fmaxf(fmaxf(fmaxf(s[k][0][0], s[k][0][1]), fmaxf(s[k][0][2], s[k][0][3])), fmaxf(fmaxf(s[k][1][0], s[k][1][1]), fmaxf(s[k][1][2], s[k][1][3])));
-            most *= step;
-            if (__builtin_amdgcn_ballot_w64(most > top[k] + 8)) {
-                most = fmaxf(most, __shfl_xor(most, 16, 64));
-                most = fmaxf(most, __shfl_xor(most, 32, 64));
-                const float up = fmaxf(top[k], most), now = up == -INFINITY ? 0.f : up;
-                const float f = top[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mu[k] - now);
+            // The maximum that is taken off lags behind by up to 8 (a factor of 256), which the sum of the weights says: moving it costs a pass
+            // over the sums, and it moves in the first tokens of a chunk, hardly later.
+            float y[8], sum;
+            auto exponentials = [&]() {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][j / 4][j % 4], step, -mu[k]));
+                sum = ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+            };
+            exponentials();
+            if (__builtin_amdgcn_ballot_w64(sum > most[k])) {
+                float up = fmaxf(fmaxf(fmaxf(s[k][0][0], s[k][0][1]), fmaxf(s[k][0][2], s[k][0][3])), fmaxf(fmaxf(s[k][1][0], s[k][1][1]), fmaxf(s[k][1][2], s[k][1][3])));
+                up = fmaxf(up, __shfl_xor(up, 16, 64));
+                up = fmaxf(top[k], fmaxf(up, __shfl_xor(up, 32, 64)) * step);
+                const float now = up == -INFINITY ? 0.f : up, f = top[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mu[k] - now);
                 top[k] = up; mu[k] = now;
+                most[k] = up == -INFINITY ? -1.f : 256.f;        // the first score that is not minus infinity moves it
                 total[k] *= f;
 #pragma unroll
                 for (int b = 0; b < 2 * NB; ++b) o[k][b] *= f;
+                exponentials();
             }
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][j / 4][j % 4], step, -mu[k]));
-            total[k] += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+            total[k] += sum;
 #pragma unroll
             for (int p = 0; p < parts; ++p) {
                 cache_u4 u;
@@ -399,17 +402,38 @@ struct cache_wave {
                 w[k][p] = __builtin_bit_cast(cache_b8, u);
             }
         }
+    }
+    // O^T += V^T P^T for numbers 16 b .. 16 b + 15
+    __device__ __forceinline__ void sums(int b, cache_b8 value, const cache_b8 (&w)[NQ][parts])
+    {
+#pragma unroll
+        for (int k = 0; k < NQ; ++k)
+#pragma unroll
+            for (int p = 0; p < parts; ++p) o[k][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, w[k][p], o[k][b], 0, 0, 0);
+    }
+
+    // 32 tokens from t on, in registers.  partial: some column attends to some of them only; tokens: the request's.
+    // One path for both, as two would be merged by the compiler into one that keeps everything of both at once.
+    __device__ __forceinline__ void tokens32(cache_tokens<NB> &x, float step, uint32_t t, uint32_t tokens, uint32_t there, bool partial, int lane)
+    {
+        cache_f4 s[NQ][2];
+        scores(s, [&](int half, int b) { return x.half[half].key(b); });
+        if (partial) {
+            leave_out(s, t, there, lane);
+#pragma unroll
+            for (int half = 0; half < 2; ++half)         // behind the request's tokens anything may be there
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (!((there >> half) & 1) || t + 16 * half + 4 * (lane >> 4) + j >= tokens) x.half[half].blank(j);
+        }
+        cache_b8 w[NQ][parts];
+        weights(s, step, w);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            cache_b8 vl, vh;
-            x.values(b, lane, vl, vh);
-#pragma unroll
-            for (int k = 0; k < NQ; ++k)
-#pragma unroll
-                for (int p = 0; p < parts; ++p) {
-                    o[k][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vl, w[k][p], o[k][2 * b], 0, 0, 0);
-                    o[k][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vh, w[k][p], o[k][2 * b + 1], 0, 0, 0);
-                }
+            cache_b8 lo, hi;
+            x.values(b, lo, hi);
+            sums(2 * b, lo, w);
+            sums(2 * b + 1, hi, w);
         }
     }
 
@@ -418,8 +442,9 @@ struct cache_wave {
     {
         if (t >= to) return;
         const int32_t *table = a.table + it.r * a.ldt;
-        const uint32_t per = (uint32_t)a.c.P / kCacheTile;
-        const int64_t head = (int64_t)per * a.c.lay.record();
+        const uint32_t per = (uint32_t)a.c.P / kCacheTile, count = (uint32_t)a.c.pages;
+        const int64_t page_bytes = (int64_t)per * a.c.G * cache_record<NB>::bytes;
+        const uint8_t *data = a.c.data + g * (int64_t)per * cache_record<NB>::bytes;
         auto page_of = [&](uint32_t record) { return cache_page_of(a, record); };
         // Tokens before `to` have a page in the table; the second 16 of 32 may lie behind the table's end, and are behind the request's then.
         auto pages = [&](uint32_t at, int32_t (&p)[2]) {
@@ -434,9 +459,9 @@ struct cache_wave {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint32_t record = at / kCacheTile + half, in = record - page_of(record) * per;
-                const bool ok = p[half] >= 0 && p[half] < a.c.pages;
+                const bool ok = (uint32_t)p[half] < count;
                 there |= ok ? 1u << half : 0;
-                x.half[half].load(a.c.data + (ok ? (p[half] * (int64_t)a.c.G + g) * head + in * (int64_t)a.c.lay.record() : 0), lane);
+                x.half[half].load(data + ((ok ? (uint32_t)p[half] : 0u) * page_bytes + in * cache_record<NB>::bytes), lane);
             }
             return there;
         };
@@ -468,7 +493,7 @@ struct cache_wave {
 struct cache_span { uint32_t from, to, whole; };
 __device__ __forceinline__ cache_span cache_span_of(const cache_attn_args &a, const cache_item &it, uint32_t first, uint32_t count)
 {
-    const uint32_t each = it.chunks == 1 ? it.q.tokens : ((it.q.tokens + it.chunks - 1) / it.chunks + 31) & ~31u;
+    const uint32_t each = it.chunks == 1 ? it.q.tokens : ((it.q.tokens + it.chunks - 1) / it.chunks + 63) & ~63u;      // whole steps
     cache_span s;
     const uint64_t from = (uint64_t)it.chunk * each, to = from + each;
     s.from = (uint32_t)(from < it.q.tokens ? from : it.q.tokens);
@@ -533,6 +558,14 @@ __device__ __forceinline__ void cache_again(const cache_attn_args &a, const cach
     if (lane == 0) c.total(top, total);
 }
 
+// The kernel's arguments (its first ones), to be loaded where they are used: kept from the kernel's beginning on they would not fit the scalar registers.
+__device__ __forceinline__ const cache_attn_args &cache_late()
+{
+    typedef const __attribute__((address_space(4))) cache_attn_args *pointer;
+    pointer p = (pointer)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const cache_attn_args *)p;
+}
 // 16 columns or fewer: the four waves of a workgroup take 32 tokens in turn, and they meet in the LDS.
 template <typename T, int NB>
 struct cache_meeting { float sums[4][16][32 * NB + 4]; float2 stats[4][16]; };
@@ -545,6 +578,7 @@ __device__ __forceinline__ void cache_few(const cache_attn_args &a, const cache_
     cache_wave<T, NB, 1> x;
     x.load_q(a, it, first, g, lane);
     x.run(a, it, g, span.from + 32 * w, 128, span.to, span.whole, lane);
+    const cache_attn_args &late = cache_late();
     float total = x.total[0];
     total += __shfl_xor(total, 16, 64);
     total += __shfl_xor(total, 32, 64);
@@ -582,17 +616,17 @@ __device__ __forceinline__ void cache_few(const cache_attn_args &a, const cache_
     }
     const uint64_t spoilt = __builtin_amdgcn_ballot_w64(there && !fine && total == total);
     if (there && !((spoilt >> (lane & 48)) & 0xffff)) {
-        const cache_column<T, NB> out(a, it, g, first + c, cols);
+        const cache_column<T, NB> out(late, it, g, first + c, cols);
 #pragma unroll
         for (int j = 0; j < each; ++j) {
             const int d = 4 * (q + 16 * j);
-            if (d < 32 * NB) out.numbers(a, d, y[j], total);
+            if (d < 32 * NB) out.numbers(late, d, y[j], total);
         }
         if (q == 0) out.total(top == -INFINITY ? 0.f : top, total);
     }
 #pragma unroll 1
     for (int k = 0; k < 4; ++k)
-        if ((spoilt >> (16 * k)) & 0xffff) cache_again<T, NB>(a, it, g, first + 4 * w + k, cols, span.from, span.to, lane);
+        if ((spoilt >> (16 * k)) & 0xffff) cache_again<T, NB>(late, it, g, first + 4 * w + k, cols, span.from, span.to, lane);
 }
 
 // Single tokens of requests (and other steps of few columns a request).
@@ -602,9 +636,10 @@ __global__ __launch_bounds__(256, NB <= 4 ? 3 : 2) void cache_few_kernel(cache_a
     __shared__ cache_meeting<T, NB> meeting;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     cache_item it;
-    if (!cache_find(a, 16, blockIdx.x, false, lane, &it)) return;
+    const uint32_t index = blockIdx.x / (uint32_t)a.c.G, g = blockIdx.x - index * a.c.G;
+    if (!cache_find(a, 16, index, false, lane, &it)) return;
     if (it.chunks > 1 && it.slot + it.chunk * it.q.tiles >= a.slots) return;
-    cache_few<T, NB>(a, it, blockIdx.y, 16, w, lane, meeting);
+    cache_few<T, NB>(a, it, (int)g, 16, w, lane, meeting);
 }
 
 // Prompts: the four waves of a workgroup take 16 NQ columns each and all tokens of the chunk, 64 at a time.  A wave turns 16 of the 64 into
@@ -614,14 +649,16 @@ template <typename T, int NB, int NQ>
 __global__ __launch_bounds__(256, 2) void cache_many_kernel(cache_attn_args a)
 {
     constexpr uint32_t cols = 64 * NQ;
-    constexpr int places = NB <= 4 ? 2 : 1, stage = 2 * cache_staged<NB>::kv;
-    __shared__ union {
+    constexpr int places = NB <= 4 ? 2 : 1, kv = 4 * NB * 1024, stage = 2 * kv;      // kv: bytes of the operands of K (and of V) of 64 tokens
+    __shared__ union __align__(16) {
         cache_meeting<T, NB> meeting;
         struct { char at[places][stage]; uint32_t there[places][4]; } staged;
     } lds;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t index = blockIdx.x / (uint32_t)a.c.G;
+    const int g = (int)(blockIdx.x - index * a.c.G);
     cache_item it;
-    if (!cache_find(a, cols, blockIdx.x, false, lane, &it)) return;
+    if (!cache_find(a, cols, index, false, lane, &it)) return;
     if (it.chunks > 1 && it.slot + it.chunk * it.q.tiles >= a.slots) return;
     if (it.q.columns <= 16) { cache_few<T, NB>(a, it, g, cols, w, lane, lds.meeting); return; }
     const uint32_t tile0 = it.tile * cols, tile_count = it.q.columns - tile0 < cols ? it.q.columns - tile0 : cols;
@@ -630,10 +667,12 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(cache_attn_args a)
     const cache_span span = cache_span_of(a, it, count ? first : tile0, count ? count : 1);
     cache_wave<T, NB, NQ> x;
     x.load_q(a, it, first, g, lane);
+    const float step = cache_spread(a.step);
 
     const int32_t *table = a.table + it.r * a.ldt;
-    const uint32_t per = (uint32_t)a.c.P / kCacheTile;
-    const int64_t head = (int64_t)per * a.c.lay.record();
+    const uint32_t per = (uint32_t)a.c.P / kCacheTile, count_pages = (uint32_t)a.c.pages;
+    const int64_t page_bytes = (int64_t)per * a.c.G * cache_record<NB>::bytes;
+    const uint8_t *data = a.c.data + g * (int64_t)per * cache_record<NB>::bytes;
     // a wave's 16 of the 64 tokens from t on; behind the table's end the request has none
     auto page = [&](uint32_t t) {
         const uint32_t n = cache_page_of(a, t / kCacheTile + w);
@@ -642,8 +681,8 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(cache_attn_args a)
     cache_record<NB> rec;
     auto fetch = [&](uint32_t t, int32_t p) {
         const uint32_t record = t / kCacheTile + w, in = record - cache_page_of(a, record) * per;
-        const bool ok = p >= 0 && p < a.c.pages;
-        rec.load(a.c.data + (ok ? (p * (int64_t)a.c.G + g) * head + in * (int64_t)a.c.lay.record() : 0), lane);
+        const bool ok = (uint32_t)p < count_pages;
+        rec.load(data + ((ok ? (uint32_t)p : 0u) * page_bytes + in * cache_record<NB>::bytes), lane);
         return ok;
     };
     auto put = [&](int place, uint32_t t, bool ok) {
@@ -656,22 +695,37 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(cache_attn_args a)
             *(cache_b8 *)(to + (w * NB + b) * 1024 + lane * 16) = rec.key(b);
             uint32_t lo[2], hi[2];
             rec.values(b, lo, hi);
-            char *v = to + cache_staged<NB>::kv + ((w >> 1) * NB + b) * 2048 + lane * 16 + (w & 1) * 8;
+            char *v = to + kv + ((w >> 1) * NB + b) * 2048 + lane * 16 + (w & 1) * 8;
             *(uint2 *)v = {lo[0], lo[1]};
             *(uint2 *)(v + 1024) = {hi[0], hi[1]};
         }
         if (lane == 0) lds.staged.there[place][w] = ok;
     };
+    // Operands are asked for a product ahead of their use: of V before the exponentials, of the next K before the product with V.
     auto work = [&](int place, uint32_t t) {
+        const char *at = lds.staged.at[place] + lane * 16;
         const uint4 f = *(const uint4 *)lds.staged.there[place];
+        cache_b8 key[2 * NB], value[2 * NB], w[NQ][cache_parts<T>::n];
+        cache_f4 s[NQ][2];
+#pragma unroll
+        for (int b = 0; b < 2 * NB; ++b) key[b] = *(const cache_b8 *)(at + b * 1024);
         const uint32_t there = __builtin_amdgcn_readfirstlane(f.x | f.y << 1 | f.z << 2 | f.w << 3);
 #pragma unroll
         for (int pair = 0; pair < 2; ++pair) {
-            const uint32_t at = t + 32 * pair;
-            if (at >= span.to || !count) break;
-            cache_staged<NB> src(lds.staged.at[place], pair);
+            x.scores(s, [&](int half, int b) { return key[half * NB + b]; });
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int b = 0; b < 2 * NB; ++b) value[b] = *(const cache_b8 *)(at + kv + (pair * 2 * NB + b) * 1024);
             const uint32_t both = (there >> (2 * pair)) & 3;
-            x.tokens32(src, a.step, at, it.q.tokens, both, at + 32 > span.whole || both != 3, lane);
+            if (t + 32 * pair + 32 > span.whole || both != 3) x.leave_out(s, t + 32 * pair, both, lane);
+            x.weights(s, step, w);
+            __builtin_amdgcn_sched_barrier(0);
+            if (pair == 0)
+#pragma unroll
+                for (int b = 0; b < 2 * NB; ++b) key[b] = *(const cache_b8 *)(at + (2 * NB + b) * 1024);
+#pragma unroll
+            for (int b = 0; b < 2 * NB; ++b) x.sums(b, value[b], w);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
     if (all.from < all.to) {
@@ -709,6 +763,7 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(cache_attn_args a)
             }
         }
     }
+    const cache_attn_args &late = cache_late();
     uint64_t spoilt = 0;                                 // a bit a column
 #pragma unroll
     for (int k = 0; k < NQ; ++k) {
@@ -726,14 +781,14 @@ __global__ __launch_bounds__(256, 2) void cache_many_kernel(cache_attn_args a)
         const uint32_t these = (uint32_t)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffff;
         spoilt |= (uint64_t)these << (16 * k);
         if (there && !((these >> (lane & 15)) & 1)) {
-            const cache_column<T, NB> out(a, it, g, first + col, cols);
+            const cache_column<T, NB> out(late, it, g, first + col, cols);
 #pragma unroll
-            for (int b = 0; b < 2 * NB; ++b) out.numbers(a, 16 * b + 4 * (lane >> 4), x.o[k][b], total);
+            for (int b = 0; b < 2 * NB; ++b) out.numbers(late, 16 * b + 4 * (lane >> 4), x.o[k][b], total);
             if (lane < 16) out.total(x.mu[k], total);
         }
     }
 #pragma unroll 1
-    for (; spoilt; spoilt &= spoilt - 1) cache_again<T, NB>(a, it, g, first + __builtin_ctzll(spoilt), cols, all.from, all.to, lane);
+    for (; spoilt; spoilt &= spoilt - 1) cache_again<T, NB>(late, it, g, first + __builtin_ctzll(spoilt), cols, all.from, all.to, lane);
 }
 
 // Joins the chunks of the tiles that have several: a workgroup for each column (or some of them in turn).  The chunks' factors first, then the
@@ -744,12 +799,14 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int 
     constexpr int pad = 32 * NB, per = (pad + 63) / 64;
     __shared__ float factor[2 * kCacheTarget], sums[4][pad];
     __shared__ float stats[2][4];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t index = blockIdx.x / (uint32_t)a.c.G;
+    const int g = (int)(blockIdx.x - index * a.c.G);
     cache_item it;
-    if (!cache_find(a, cols, blockIdx.x, true, lane, &it)) return;
+    if (!cache_find(a, cols, index, true, lane, &it)) return;
     if (it.slot + (it.chunks - 1) * it.q.tiles >= a.slots) return;       // so there are at most 2 kCacheTarget chunks
     const int64_t step = (int64_t)it.q.tiles * a.c.G * cols;
-    for (uint32_t column = blockIdx.z; column < (uint32_t)cols && it.tile * cols + column < it.q.columns; column += gridDim.z) {
+    for (uint32_t column = blockIdx.y; column < (uint32_t)cols && it.tile * cols + column < it.q.columns; column += gridDim.y) {
         const uint32_t col = it.tile * cols + column;
         const int64_t base = ((int64_t)it.slot * a.c.G + g) * cols + column;
         float top = -INFINITY, total = 0;
@@ -824,9 +881,9 @@ template <typename T, int NB>
 void cache_launch(const cache_attn_args &a, const cache_choice &c, hipStream_t st)
 {
     constexpr int NQ = cache_nq<T>(NB);
-    if (c.few) cache_few_kernel<T, NB><<<dim3((unsigned)c.items, a.c.G), 256, 0, st>>>(a);
-    else cache_many_kernel<T, NB, NQ><<<dim3((unsigned)c.items, a.c.G), 256, 0, st>>>(a);
-    if (c.slots) cache_join_kernel<T, NB><<<dim3((unsigned)c.joins, a.c.G, c.joins * a.c.G * c.cols <= 4096 ? c.cols : 4), 256, 0, st>>>(a, c.cols);
+    if (c.few) cache_few_kernel<T, NB><<<(unsigned)(c.items * a.c.G), 256, 0, st>>>(a);
+    else cache_many_kernel<T, NB, NQ><<<(unsigned)(c.items * a.c.G), 256, 0, st>>>(a);
+    if (c.slots) cache_join_kernel<T, NB><<<dim3((unsigned)(c.joins * a.c.G), c.joins * a.c.G * c.cols <= 4096 ? c.cols : 4), 256, 0, st>>>(a, c.cols);
 }
 
 template <typename T> sp_status cache_attention(const cache_attn_args &a, const cache_choice &c, hipStream_t st);

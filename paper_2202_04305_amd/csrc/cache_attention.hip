@@ -10,15 +10,6 @@ template <> sp_status cache_attention<cache_bf16>(const cache_attn_args &a, cons
 
 namespace {
 
-// The records of a page as a divisor d of numbers x below 2^31: with 2^s < d < 2^(s + 1), mul = floor(2^(32 + s) / d) + 1 exceeds 2^(32 + s) / d by
-// at most 1, which moves x mul / 2^(32 + s) by less than 1 / d.
-void make_divisor(uint32_t d, cache_attn_args *a)
-{
-    const int s = 31 - __builtin_clz(d);
-    if (d & (d - 1)) { a->page_mul = (uint32_t)(((uint64_t)1 << (32 + s)) / d + 1); a->page_shift = 32 + s; }
-    else { a->page_mul = 1u << 31; a->page_shift = 31 + s; }
-}
-
 sp_status check_problem(const sp_cache *c, const sp_cache_problem *p, cache_attn_args *a, cache_choice *choice)
 {
     if (!c || !p) return SP_ERR_NULL;
@@ -37,9 +28,9 @@ sp_status check_problem(const sp_cache *c, const sp_cache_problem *p, cache_attn
     a->Q = p->Q; a->table = p->table; a->length = p->length; a->start = p->start;
     a->ldq = p->ldq; a->hdq = p->hdq; a->ldt = p->ldt; a->width = c->pages ? p->width : 0; a->requests = p->requests; a->tokens = p->tokens;
     a->H = p->heads; a->R = p->heads / c->kvHeads; a->causal = p->causal; a->sign = step < 0 ? -1.f : step > 0 ? 1.f : 0.f; a->step = step == 0 ? 1.f : fabsf(step);
-    make_divisor(c->pageTokens / kCacheTile, a);
+    a->records = spmi_make_divisor32(c->pageTokens / kCacheTile);
     *choice = p->dtype == SP_F32 ? cache_choice_of<float>(*a) : p->dtype == SP_F16 ? cache_choice_of<cache_f16>(*a) : cache_choice_of<cache_bf16>(*a);
-    if (a->tokens * a->R >= top || choice->items >= (int64_t)1 << 24) return SP_ERR_TOO_LARGE;        // 2^32 threads of a launch
+    if (a->tokens * a->R >= top || choice->items * a->c.G >= (int64_t)1 << 24) return SP_ERR_TOO_LARGE;        // 2^32 threads of a launch
     return SP_OK;
 }
 

@@ -381,6 +381,18 @@ struct spmi_long_sum<float, V> {
 // order, and with rows of 64 a fixed place would be the same one of every row (a full last column would never be seen).
 __device__ __forceinline__ uint32_t spmi_sampled_place(uint32_t group) { return (group * 2654435761u) >> 26; }
 
+// Division of numbers below 2^31 by d > 0: x mul >> shift, the product in 64 bits.  With 2^s < d < 2^(s + 1), mul = floor(2^(32 + s) / d) + 1 exceeds
+// 2^(32 + s) / d by at most 1, which moves the quotient by less than 1 / d; powers of two are shifts.
+struct spmi_divisor32 { uint32_t mul, shift; };
+static inline spmi_divisor32 spmi_make_divisor32(uint32_t d)
+{
+    const uint32_t s = 31 - __builtin_clz(d);
+    if (d & (d - 1)) return {(uint32_t)(((uint64_t)1 << (32 + s)) / d + 1), 32 + s};
+    return {1u << 31, 31 + s};
+}
+__host__ __device__ inline uint32_t spmi_div_by32(uint32_t x, const spmi_divisor32 &d) { return (uint32_t)((uint64_t)x * d.mul >> d.shift); }
+
+
 // Division of a key by a level's stride or size, which the host knows when it launches: a shift when the divisor is a
 // power of two, a multiplication by the reciprocal in double plus a one-step correction while the dividend is below
 // 2^52 (the estimate is then within one of the quotient), the hardware's 64-bit division otherwise.

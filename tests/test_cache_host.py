@@ -72,7 +72,7 @@ def rotary(**more):
     (dict(scale=math.nan), SHAPE), (dict(ldq=-1), SHAPE), (dict(hdk=-1), SHAPE), (dict(ldqo=63), SHAPE), (dict(hdqo=63), SHAPE), (dict(ldko=63), SHAPE), (dict(hdko=63), SHAPE),
     (dict(interleaved=2), UNSUPPORTED), (dict(position=None), NULL), (dict(frequency=None), NULL), (dict(Q=None), NULL), (dict(K=None), NULL),
     (dict(Qout=None), NULL), (dict(Kout=None), NULL), (dict(dtype=1, headDim=0, interleaved=2, Q=None), DTYPE), (dict(headDim=0, interleaved=2, Q=None), SHAPE),
-    (dict(interleaved=2, Q=None), UNSUPPORTED)])
+    (dict(interleaved=2, Q=None), UNSUPPORTED), (dict(heads=1 << 25), TOO_LARGE), (dict(heads=(1 << 31) - 1, kvHeads=(1 << 31) - 1), TOO_LARGE)])
 def test_rotary_refusals(more, code):
     L = sp.load_library()
     assert L.sp_rotary(ref(rotary(**more)), None) == code
