@@ -1,6 +1,7 @@
 """ctypes binding of libspmi.so.  Same names as the C ABI; argument marshalling only."""
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -140,19 +141,19 @@ def load_library():
     L.sp_rotary_frequencies.argtypes = [ci, ctypes.c_double, ctypes.c_double, i64, ctypes.c_double, ctypes.c_double, vp]
     for f in (L.sp_rotary, L.sp_rotary_grad):
         f.restype = ci
-        f.argtypes = [ctypes.POINTER(SpRotaryProblem), vp]
-    cache, cached = ctypes.POINTER(SpCache), ctypes.POINTER(SpCacheProblem)
+        f.argtypes = [vp, vp]                # structures, or their bytes
+    cache = ctypes.POINTER(SpCache)
     L.sp_cache_bytes.restype = ci
     L.sp_cache_bytes.argtypes = [cache, ctypes.POINTER(size)]
     L.sp_cache_map.restype = ci
-    L.sp_cache_map.argtypes = [ctypes.POINTER(SpCacheStep), vp]
+    L.sp_cache_map.argtypes = [vp, vp]
     for f in (L.sp_cache_store, L.sp_cache_load):
         f.restype = ci
         f.argtypes = [cache, ci, i64, vp, vp, i64, i64, vp, i64, i64, vp]
     L.sp_cache_attention_workspace.restype = ci
-    L.sp_cache_attention_workspace.argtypes = [cache, cached, ctypes.POINTER(size)]
+    L.sp_cache_attention_workspace.argtypes = [cache, vp, ctypes.POINTER(size)]
     L.sp_cache_attention.restype = ci
-    L.sp_cache_attention.argtypes = [cache, cached, vp, i64, i64, vp, vp, size, vp]
+    L.sp_cache_attention.argtypes = [cache, vp, vp, i64, i64, vp, vp, size, vp]
     L.sp_convert.restype = ci
     L.sp_convert.argtypes = [vp, vp, vp, ctypes.POINTER(vp)]
     L.sp_tensor_info.restype = ci
@@ -499,44 +500,86 @@ def sp_attention_grad(S, Q, K, V, O, lse, dO, scale=None, causal=False, qpos=Non
     return _attention_call(S, call)
 
 
-def _rotary(grad, position, frequencies, Q, K, interleaved, scale, Q_out, K_out):
-    L = load_library()
-    if Q.dtype not in _ATTENTION_DT:
-        raise SpError(9, "in sp_rotary: %s" % Q.dtype)
+# The same bytes as the structures above, made in a third of the time; a step of a serving loop makes one for each call.
+_ROTARY, _STEP, _PROBLEM = struct.Struct("@iiiidqPPii" + "Pqq" * 4), struct.Struct("@qqqi" + "PPPqPPqqPPPPP"), struct.Struct("@iiidqqPqqPqqPP")
 
-    def call():
-        q = _rows_of_heads(Q, "Q", Q, Q.dtype)
-        (tokens, heads, d), half = Q.shape, frequencies.numel()
-        if position.dtype != torch.int32 or position.device != Q.device or tuple(position.shape) != (tokens,) or not position.is_contiguous():
-            raise ValueError("position: %d contiguous int32 positions on %s" % (tokens, Q.device))
-        if frequencies.dtype != torch.float64 or frequencies.device != Q.device or frequencies.dim() != 1 or not frequencies.is_contiguous():
-            raise ValueError("frequencies: contiguous float64 numbers on %s" % Q.device)
-        q_out = _attention_output(Q_out, Q, "Q_out")
-        qo, k, ko, k_out = _rows_of_heads(q_out, "Q_out", Q, Q.dtype), (None, 0, 0), (None, 0, 0), None
-        if K is not None:
-            k = _rows_of_heads(K, "K", Q, Q.dtype)
-            if K.shape[0] != tokens or K.shape[2] != d:
-                raise ValueError("K %s beside Q %s" % (tuple(K.shape), tuple(Q.shape)))
-            k_out = _attention_output(K_out, K, "K_out")
-            ko = _rows_of_heads(k_out, "K_out", Q, Q.dtype)
-        p = SpRotaryProblem(_ATTENTION_DT[Q.dtype], d, 2 * half, 1 if interleaved else 0, float(scale), tokens, position.data_ptr(),
-                            frequencies.data_ptr(), heads, 0 if K is None else K.shape[1], *q, *k, *qo, *ko)
-        f = L.sp_rotary_grad if grad else L.sp_rotary
-        _check(f(ctypes.byref(p), _stream_ptr()), "in sp_rotary_grad" if grad else "in sp_rotary")
-        return q_out if K is None else (q_out, k_out)
-    return _attention_call(Q, call)
+
+def _heads_of(t, name, dtype, index):
+    """_rows_of_heads for a tensor on GPU number `index`, with little work where all is well."""
+    st = t.stride()
+    if len(st) != 3 or t.dtype is not dtype or t.get_device() != index or (st[2] != 1 and t.shape[2] > 1):
+        raise ValueError("%s: a (tokens, heads, d) tensor of %s on GPU %d with a contiguous last dimension, not %s %s strides %s on %s" % (
+            name, dtype, index, t.dtype, tuple(t.shape), tuple(st), t.device))
+    return t.data_ptr(), st[0], st[1]
+
+
+def _output_like(t, like, name):
+    """An output of `like`'s shape: a new one, or the caller's (its rows must not overlap)."""
+    if t is None:
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
+    if t.shape != like.shape:
+        raise ValueError("%s: shape %s, not %s" % (name, tuple(like.shape), tuple(t.shape)))
+    return t
+
+
+def _whole_numbers(t, name, size, index):
+    """The address of `size` contiguous int32 numbers on GPU number `index`."""
+    if t.dtype is not torch.int32 or t.get_device() != index or t.dim() != 1 or t.numel() != size or not t.is_contiguous():
+        raise ValueError("%s: %d contiguous int32 numbers on GPU %d, not %s %s on %s" % (name, size, index, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+def _gpu_of(t):
+    """The number of a tensor's GPU."""
+    index = t.get_device()
+    if index < 0:
+        raise ValueError("a tensor on a GPU, not on %s" % t.device)
+    return index
+
+
+def _on_gpu(index, f, *args):
+    """f(*args) with that GPU current: the stream, the workspace and the launches are that device's."""
+    if index == torch.cuda.current_device():
+        return f(*args)
+    with torch.cuda.device(index):
+        return f(*args)
+
+
+def _rotary(grad, index, position, frequencies, Q, K, interleaved, scale, Q_out, K_out):
+    L, dt = load_library(), Q.dtype
+    code = _ATTENTION_DT.get(dt)
+    if code is None:
+        raise SpError(9, "in sp_rotary: %s" % dt)
+    q = _heads_of(Q, "Q", dt, index)
+    (tokens, heads, d), half = Q.shape, frequencies.numel()
+    if frequencies.dtype is not torch.float64 or frequencies.get_device() != index or frequencies.dim() != 1 or not frequencies.is_contiguous():
+        raise ValueError("frequencies: contiguous float64 numbers on GPU %d" % index)
+    at = _whole_numbers(position, "position", tokens, index)
+    q_out = _output_like(Q_out, Q, "Q_out")
+    qo, k, ko, k_out, kv = _heads_of(q_out, "Q_out", dt, index), (0, 0, 0), (0, 0, 0), None, 0
+    if K is not None:
+        k = _heads_of(K, "K", dt, index)
+        n, kv, dk = K.shape
+        if n != tokens or dk != d:
+            raise ValueError("K %s beside Q %s" % (tuple(K.shape), tuple(Q.shape)))
+        k_out = _output_like(K_out, K, "K_out")
+        ko = _heads_of(k_out, "K_out", dt, index)
+    f = L.sp_rotary_grad if grad else L.sp_rotary
+    _check(f(_ROTARY.pack(code, d, 2 * half, 1 if interleaved else 0, scale, tokens, at, frequencies.data_ptr(), heads, kv, *q, *k, *qo, *ko),
+             _stream_ptr()), "in sp_rotary_grad" if grad else "in sp_rotary")
+    return q_out if K is None else (q_out, k_out)
 
 
 def sp_rotary(position, frequencies, Q, K=None, interleaved=False, scale=1.0, Q_out=None, K_out=None):
     """Q (tokens, heads, d) and, if given, K (tokens, kv heads, d) with their pairs turned by position * frequencies (int32 positions, f64 angles a
     position; the first 2 * len(frequencies) numbers of a head turn).  Returns the turned Q, or (Q, K): new tensors, or Q_out and K_out, which may
     be Q and K."""
-    return _rotary(False, position, frequencies, Q, K, interleaved, scale, Q_out, K_out)
+    return _on_gpu(_gpu_of(Q), _rotary, False, Q.get_device(), position, frequencies, Q, K, interleaved, scale, Q_out, K_out)
 
 
 def sp_rotary_grad(position, frequencies, dQ, dK=None, interleaved=False, scale=1.0, dQ_out=None, dK_out=None):
     """The gradients with respect to sp_rotary's Q and K, given those with respect to its results (the same arguments otherwise)."""
-    return _rotary(True, position, frequencies, dQ, dK, interleaved, scale, dQ_out, dK_out)
+    return _on_gpu(_gpu_of(dQ), _rotary, True, dQ.get_device(), position, frequencies, dQ, dK, interleaved, scale, dQ_out, dK_out)
 
 
 def sp_rotary_frequencies(rot_dim, base=10000.0, factor=1.0, trained=0, low=1.0, high=32.0, device=None):
@@ -553,13 +596,9 @@ class Cache:
 
     def __init__(self, data, spec):
         self.data, self._spec, self.device = data, spec, data.device
-        self._ref = ctypes.byref(spec)
+        self.pages, self.page_tokens, self.kv_heads, self.head_dim = spec.pages, spec.pageTokens, spec.kvHeads, spec.headDim
+        self._ref, self._index = ctypes.byref(spec), data.get_device()
         self._workspaces = {}            # bytes of workspace of the attention problems met so far
-
-    pages = property(lambda self: self._spec.pages)
-    page_tokens = property(lambda self: self._spec.pageTokens)
-    kv_heads = property(lambda self: self._spec.kvHeads)
-    head_dim = property(lambda self: self._spec.headDim)
 
 
 def sp_cache(pages, page_tokens, kv_heads, head_dim, device=None):
@@ -571,107 +610,110 @@ def sp_cache(pages, page_tokens, kv_heads, head_dim, device=None):
     return Cache(data, spec)
 
 
-def _whole_numbers(t, name, size, device):
-    """The address of `size` contiguous int32 numbers."""
-    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != (size,) or not t.is_contiguous():
-        raise ValueError("%s: %d contiguous int32 numbers on %s, not %s %s on %s" % (name, size, device, t.dtype, tuple(t.shape), t.device))
-    return t.data_ptr()
-
-
-def _block_table(t, requests, device):
+def _block_table(t, requests, index):
     """The address, row stride and width of a block table."""
     st = t.stride()
-    if t.dtype != torch.int32 or t.device != device or t.dim() != 2 or t.shape[0] != requests or (t.shape[1] > 1 and st[1] != 1):
-        raise ValueError("table: int32 pages (%d, width) on %s with contiguous rows, not %s %s strides %s on %s" % (
-            requests, device, t.dtype, tuple(t.shape), st, t.device))
-    return t.data_ptr(), st[0] if requests > 1 else max(st[0], t.shape[1]), t.shape[1]
+    if t.dtype is not torch.int32 or t.get_device() != index or len(st) != 2 or t.shape[0] != requests or (st[1] != 1 and t.shape[1] > 1):
+        raise ValueError("table: int32 pages (%d, width) on GPU %d with contiguous rows, not %s %s strides %s on %s" % (
+            requests, index, t.dtype, tuple(t.shape), st, t.device))
+    width = t.shape[1]
+    return t.data_ptr(), st[0] if requests > 1 else max(st[0], width), width
 
 
 def sp_cache_map(lengths, added, free, taken, table, page_tokens, pages, tokens):
     """The pages and slots of a step.  lengths, added: (requests) int32, what each request has in the cache and gets; free: int32 pages to hand
     out, from number taken[0] on; table: (requests, width) int32, updated in place; tokens: rows of the step (sum of added, or more).
     Returns (lengths + added, start (requests + 1), position (tokens), slot (tokens), taken)."""
-    L = load_library()
+    return _on_gpu(_gpu_of(lengths), _cache_map, lengths, added, free, taken, table, page_tokens, pages, tokens)
 
-    def call():
-        n, dev = lengths.shape[0], lengths.device
-        out = [torch.empty(k, dtype=torch.int32, device=dev) for k in (n, n + 1, int(tokens), int(tokens), 1)]
-        s = SpCacheStep(n, int(tokens), int(pages), int(page_tokens), _whole_numbers(lengths, "lengths", n, dev), _whole_numbers(added, "added", n, dev),
-                        _whole_numbers(free, "free", free.shape[0], dev), free.shape[0], _whole_numbers(taken, "taken", 1, dev),
-                        *_block_table(table, n, dev), *[t.data_ptr() for t in out])
-        _check(L.sp_cache_map(ctypes.byref(s), _stream_ptr()), "in sp_cache_map")
-        return tuple(out)
-    return _attention_call(lengths, call)
+
+def _cache_map(lengths, added, free, taken, table, page_tokens, pages, tokens):
+    n, nfree, index, new = lengths.shape[0], free.shape[0], lengths.get_device(), lengths.new_empty
+    at = (_whole_numbers(lengths, "lengths", n, index), _whole_numbers(added, "added", n, index), _whole_numbers(free, "free", nfree, index), nfree,
+          _whole_numbers(taken, "taken", 1, index), *_block_table(table, n, index))
+    if tokens < 0:
+        raise SpError(8, "in sp_cache_map: %d tokens" % tokens)
+    out = new(n), new(n + 1), new(tokens), new(tokens), new(1)
+    _check(load_library().sp_cache_map(_STEP.pack(n, tokens, pages, page_tokens, *at, *[t.data_ptr() for t in out]), _stream_ptr()), "in sp_cache_map")
+    return out
 
 
 def _cache_rows(cache, t, name, tokens, dtype):
-    row = _rows_of_heads(t, name, cache, dtype)
-    if tuple(t.shape) != (tokens, cache.kv_heads, cache.head_dim):
+    row = _heads_of(t, name, dtype, cache._index)
+    if t.shape[0] != tokens or t.shape[1] != cache.kv_heads or t.shape[2] != cache.head_dim:
         raise ValueError("%s: shape %s, not %s" % (name, (tokens, cache.kv_heads, cache.head_dim), tuple(t.shape)))
     return row
 
 
 def sp_cache_store(cache, K, V, slots):
     """K and V (tokens, kv heads, d), f32, f16 or bf16, into the cache's slots (int32; -1: not stored), in 4 bits."""
-    L = load_library()
-    if K.dtype not in _ATTENTION_DT:
-        raise SpError(9, "in sp_cache_store: %s" % K.dtype)
+    _on_gpu(cache._index, _cache_store, cache, K, V, slots)
 
-    def call():
-        n = K.shape[0]
-        k, v = _cache_rows(cache, K, "K", n, K.dtype), _cache_rows(cache, V, "V", n, K.dtype)
-        _check(L.sp_cache_store(cache._ref, _ATTENTION_DT[K.dtype], n, _whole_numbers(slots, "slots", n, cache.device), *k, *v, _stream_ptr()), "in sp_cache_store")
-    _attention_call(cache, call)
+
+def _cache_store(cache, K, V, slots):
+    n, dt = K.shape[0], K.dtype
+    code = _ATTENTION_DT.get(dt)
+    if code is None:
+        raise SpError(9, "in sp_cache_store: %s" % dt)
+    k, v = _cache_rows(cache, K, "K", n, dt), _cache_rows(cache, V, "V", n, dt)
+    _check(load_library().sp_cache_store(cache._ref, code, n, _whole_numbers(slots, "slots", n, cache._index), *k, *v, _stream_ptr()), "in sp_cache_store")
 
 
 def sp_cache_load(cache, slots, dtype=torch.bfloat16, K=None, V=None):
     """What the cache's slots hold (int32; -1: zeros): K and V (tokens, kv heads, d) of `dtype`, new tensors or the given ones."""
-    L = load_library()
-    if dtype not in _ATTENTION_DT:
-        raise SpError(9, "in sp_cache_load: %s" % dtype)
+    return _on_gpu(cache._index, _cache_load, cache, slots, dtype, K, V)
 
-    def call():
-        n = slots.shape[0]
-        out = [torch.empty(n, cache.kv_heads, cache.head_dim, dtype=dtype, device=cache.device) if t is None else t for t in (K, V)]
-        k, v = _cache_rows(cache, out[0], "K", n, dtype), _cache_rows(cache, out[1], "V", n, dtype)
-        _check(L.sp_cache_load(cache._ref, _ATTENTION_DT[dtype], n, _whole_numbers(slots, "slots", n, cache.device), *k, *v, _stream_ptr()), "in sp_cache_load")
-        return out[0], out[1]
-    return _attention_call(cache, call)
+
+def _cache_load(cache, slots, dtype, K, V):
+    code = _ATTENTION_DT.get(dtype)
+    if code is None:
+        raise SpError(9, "in sp_cache_load: %s" % dtype)
+    n = slots.shape[0]
+    at = _whole_numbers(slots, "slots", n, cache._index)
+    if K is None:
+        K = torch.empty((n, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.device)
+    if V is None:
+        V = torch.empty((n, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.device)
+    k, v = _cache_rows(cache, K, "K", n, dtype), _cache_rows(cache, V, "V", n, dtype)
+    _check(load_library().sp_cache_load(cache._ref, code, n, at, *k, *v, _stream_ptr()), "in sp_cache_load")
+    return K, V
 
 
 def sp_cache_attention(cache, Q, table, lengths, start, scale=None, causal=True, O=None, lse=None):
     """Attention over the cache.  Q: (tokens, heads, d), f32, f16 or bf16; request r's queries are rows start[r] .. start[r + 1] - 1, the last of its
     lengths[r] tokens in the pages of table[r] (all int32); scale: 1 / sqrt(d) unless given.  Returns O (tokens, heads, d) and lse (heads, tokens)
     f32; rows of no request are left as they were."""
-    L = load_library()
-    if Q.dtype not in _ATTENTION_DT:
-        raise SpError(9, "in sp_cache_attention: %s" % Q.dtype)
+    return _on_gpu(cache._index, _cache_attention, cache, Q, table, lengths, start, scale, causal, O, lse)
 
-    def call():
-        dev, dt = cache.device, Q.dtype
-        q = _rows_of_heads(Q, "Q", cache, dt)
-        tokens, heads, d = Q.shape
-        if d != cache.head_dim:
-            raise ValueError("Q %s for a cache of heads of %d" % (tuple(Q.shape), cache.head_dim))
-        n = lengths.shape[0]
-        at = _block_table(table, n, dev)
-        p = SpCacheProblem(_ATTENTION_DT[dt], heads, 1 if causal else 0, float(d) ** -0.5 if scale is None else float(scale), n, tokens, *q,
-                           *at, _whole_numbers(lengths, "lengths", n, dev), _whole_numbers(start, "start", n + 1, dev))
-        out = _attention_output(O, Q, "O")
-        logs = torch.empty((heads, tokens), dtype=torch.float32, device=dev) if lse is None else lse
-        if lse is not None and (tuple(lse.shape) != (heads, tokens) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev):
-            raise ValueError("lse: a contiguous f32 tensor of (heads, tokens)")
-        o = _rows_of_heads(out, "O", cache, dt)
-        key = (dt, heads, n, tokens, at[2])
-        size = cache._workspaces.get(key)
-        if size is None:
-            need = ctypes.c_size_t()
-            _check(L.sp_cache_attention_workspace(cache._ref, ctypes.byref(p), ctypes.byref(need)), "in sp_cache_attention")
-            size = cache._workspaces[key] = need.value
-        work = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
-        _check(L.sp_cache_attention(cache._ref, ctypes.byref(p), *o, logs.data_ptr(), work.data_ptr() if size else None, size, _stream_ptr()), "in sp_cache_attention")
-        return out, logs
-    return _attention_call(cache, call)
+
+def _cache_attention(cache, Q, table, lengths, start, scale, causal, O, lse):
+    L, dt, index = load_library(), Q.dtype, cache._index
+    code = _ATTENTION_DT.get(dt)
+    if code is None:
+        raise SpError(9, "in sp_cache_attention: %s" % dt)
+    q = _heads_of(Q, "Q", dt, index)
+    tokens, heads, d = Q.shape
+    if d != cache.head_dim:
+        raise ValueError("Q %s for a cache of heads of %d" % (tuple(Q.shape), cache.head_dim))
+    n = lengths.shape[0]
+    at = _block_table(table, n, index)
+    p = _PROBLEM.pack(code, heads, 1 if causal else 0, float(d) ** -0.5 if scale is None else scale, n, tokens, *q, *at,
+                      _whole_numbers(lengths, "lengths", n, index), _whole_numbers(start, "start", n + 1, index))
+    O = _output_like(O, Q, "O")
+    if lse is None:
+        lse = torch.empty((heads, tokens), dtype=torch.float32, device=cache.device)
+    elif tuple(lse.shape) != (heads, tokens) or lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.get_device() != index:
+        raise ValueError("lse: a contiguous f32 tensor of (heads, tokens)")
+    o = _heads_of(O, "O", dt, index)
+    key = (code, heads, n, tokens, at[2])
+    size = cache._workspaces.get(key)
+    if size is None:
+        need = ctypes.c_size_t()
+        _check(L.sp_cache_attention_workspace(cache._ref, p, ctypes.byref(need)), "in sp_cache_attention")
+        size = cache._workspaces[key] = need.value
+    work = torch.empty(size, dtype=torch.uint8, device=cache.device) if size else None
+    _check(L.sp_cache_attention(cache._ref, p, *o, lse.data_ptr(), work.data_ptr() if size else None, size, _stream_ptr()), "in sp_cache_attention")
+    return O, lse
 
 
 def sp_mttkrp(B, C, D, A=None, accumulate=False):

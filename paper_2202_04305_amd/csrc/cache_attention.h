@@ -566,6 +566,11 @@ __device__ __forceinline__ const cache_attn_args &cache_late()
     asm volatile("" : "+s"(p));
     return *(const cache_attn_args *)p;
 }
+// Groups of 16 columns of a wave, and waves on a SIMD, so that nothing is kept in scratch memory.
+template <typename T> constexpr int cache_nq(int nb) { return nb <= (cache_parts<T>::n == 3 ? 3 : 4) ? 2 : 1; }
+template <typename T> constexpr int cache_few_waves(int nb) { return nb <= (cache_parts<T>::n == 3 ? 3 : 4) ? 3 : nb <= (cache_parts<T>::n == 1 ? 8 : 9 - cache_parts<T>::n) ? 2 : 1; }
+template <typename T> constexpr int cache_many_waves(int nb) { return nb <= (cache_parts<T>::n == 1 ? 8 : 9 - cache_parts<T>::n) ? 2 : 1; }
+
 // 16 columns or fewer: the four waves of a workgroup take 32 tokens in turn, and they meet in the LDS.
 template <typename T, int NB>
 struct cache_meeting { float sums[4][16][32 * NB + 4]; float2 stats[4][16]; };
@@ -631,7 +636,7 @@ __device__ __forceinline__ void cache_few(const cache_attn_args &a, const cache_
 
 // Single tokens of requests (and other steps of few columns a request).
 template <typename T, int NB>
-__global__ __launch_bounds__(256, NB <= 4 ? 3 : 2) void cache_few_kernel(cache_attn_args a)
+__global__ __launch_bounds__(256, cache_few_waves<T>(NB)) void cache_few_kernel(cache_attn_args a)
 {
     __shared__ cache_meeting<T, NB> meeting;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -646,7 +651,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 3 : 2) void cache_few_kernel(cache_a
 // operands, which the four share in LDS: in registers of their own the conversions would take as long as the exponentials.  Two places: one
 // is filled while the other is worked on.  (NB > 4: one place, there is no room for two workgroups otherwise.)
 template <typename T, int NB, int NQ>
-__global__ __launch_bounds__(256, 2) void cache_many_kernel(cache_attn_args a)
+__global__ __launch_bounds__(256, cache_many_waves<T>(NB)) void cache_many_kernel(cache_attn_args a)
 {
     constexpr uint32_t cols = 64 * NQ;
     constexpr int places = NB <= 4 ? 2 : 1, kv = 4 * NB * 1024, stage = 2 * kv;      // kv: bytes of the operands of K (and of V) of 64 tokens
@@ -858,7 +863,6 @@ struct cache_choice {
     size_t part, stat;                   // bytes
 };
 
-template <typename T> constexpr int cache_nq(int nb) { return nb <= 4 || cache_parts<T>::n == 1 ? 2 : 1; }
 
 template <typename T>
 cache_choice cache_choose(const cache_attn_args &a)

@@ -36,6 +36,13 @@ def test_structures_match_the_header(name, mirror):
     assert fields(name) == list(mirror._fields_)
 
 
+@pytest.mark.parametrize("pack,mirror", [(B._ROTARY, B.SpRotaryProblem), (B._STEP, B.SpCacheStep), (B._PROBLEM, B.SpCacheProblem)])
+def test_packed_bytes_are_the_structures(pack, mirror):
+    """The binding packs the bytes of these structures: the same ones, field by field (padding aside, which both leave zero)."""
+    numbers = [k + 1 for k in range(len(mirror._fields_))]
+    assert pack.size == ctypes.sizeof(mirror) and pack.pack(*numbers) == bytes(mirror(*numbers))
+
+
 def ref(s):
     return ctypes.byref(s)
 
