@@ -710,6 +710,8 @@ def _cache_attention(cache, Q, table, lengths, start, scale, causal, O, lse):
     if size is None:
         need = ctypes.c_size_t()
         _check(L.sp_cache_attention_workspace(cache._ref, p, ctypes.byref(need)), "in sp_cache_attention")
+        if len(cache._workspaces) >= 1000:               # steps of ever other sizes
+            cache._workspaces.clear()
         size = cache._workspaces[key] = need.value
     work = torch.empty(size, dtype=torch.uint8, device=cache.device) if size else None
     _check(L.sp_cache_attention(cache._ref, p, *o, lse.data_ptr(), work.data_ptr() if size else None, size, _stream_ptr()), "in sp_cache_attention")

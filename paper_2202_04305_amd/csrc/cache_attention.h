@@ -25,12 +25,15 @@ struct cache_attn_args {
     float *part;                         // workspace: [slot][head of the cache][column][32 nb] sums
     float2 *stat;                        //            [slot][head of the cache][column]: running maximum (in units of log 2) and total
     uint32_t slots;                      // slots there is room for
+    uint32_t *plan;                      // of more than 64 requests: see cache_plan_kernel
 };
 
 // ---- work ------------------------------------------------------------------------------------------------------------------
 // The columns of a request (its queries times the heads that share a head of the cache) are cut into tiles, its tokens into chunks, and an
 // item is a tile, a chunk and a head of the cache.  Lengths are known on the GPU alone, so every workgroup finds its item by a scan over
-// the requests.  Chunks are as long as makes about kCacheTarget items of all work, at least kCacheLeast tokens.
+// the requests: 64 at a time, of which a plan says the right ones where there are more.  The heads of one item are neighbours: workgroups go
+// to the eight XCDs in turn, so that with 8 heads (or 4, 16, ..) what one L2 holds of the pages serves all tiles of a request.
+// Chunks are as long as makes about kCacheTarget items of all work, at least kCacheLeast tokens.
 constexpr int kCacheTarget = 512, kCacheLeast = 256;
 
 struct cache_request { uint32_t n, columns, tiles, tokens, row0; int32_t last; uint32_t r; };      // row0: its first row; last: position of its last query, -1 or more; r: its number
@@ -42,7 +45,10 @@ struct cache_item {
 
 static inline __host__ __device__ int64_t cache_limit(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-__device__ __forceinline__ cache_request cache_request_of(const cache_attn_args &a, int64_t r, int cols)
+// Columns of a request's tiles in a launch of tiles of `cols`: a quarter where few fill at most half of one (see cache_many_kernel).
+__device__ __forceinline__ uint32_t cache_width(uint32_t columns, uint32_t cols) { return cols > 16 && columns * 2 <= cols ? cols / 4 : cols; }
+
+__device__ __forceinline__ cache_request cache_request_of(const cache_attn_args &a, int64_t r, uint32_t cols)
 {
     cache_request q = {0, 0, 0, 0, 0, -1, (uint32_t)r};
     if (r >= a.requests) return q;
@@ -50,7 +56,8 @@ __device__ __forceinline__ cache_request cache_request_of(const cache_attn_args 
     if (s1 <= s0) return q;
     q.n = (uint32_t)(s1 - s0);
     q.columns = q.n * (uint32_t)a.R;
-    q.tiles = (q.columns + cols - 1) / cols;
+    const uint32_t width = cache_width(q.columns, cols);
+    q.tiles = (q.columns + width - 1) / width;
     q.tokens = (uint32_t)cache_limit(len, 0, a.width * a.c.P);
     q.row0 = (uint32_t)s0;
     q.last = (int32_t)(len < 0 ? 0 : len) - 1;
@@ -63,25 +70,69 @@ __device__ __forceinline__ uint32_t cache_wave_scan(uint32_t v, int lane)       
     for (int d = 1; d < 64; d <<= 1) { const uint32_t o = __shfl_up(v, d, 64); v += lane >= d ? o : 0; }
     return v;
 }
-
-// Tokens of a chunk: by the work of all requests.  own: the lane's among the first 64
-__device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a, int cols, int lane, const cache_request &own)
+template <typename V>
+__device__ __forceinline__ V cache_wave_total(V v)
 {
-    if (a.slots == 0) return 0x7fffff00u;
-    uint64_t work = (uint64_t)own.tiles * own.tokens;
-    for (int64_t r = lane + 64; r < a.requests; r += 64) {
-        const cache_request q = cache_request_of(a, r, cols);
-        work += (uint64_t)q.tiles * q.tokens;
-    }
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) work += __shfl_xor(work, d, 64);
-    const uint64_t c = (work * a.c.G + kCacheTarget - 1) / kCacheTarget;
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// Tokens of a chunk; work = sum over the requests of tiles * tokens.  A head's share of the items is T.  Few columns: there are places for more
+// workgroups than T heads' items, so chunks of work / T do.  Prompts: a workgroup that comes after all places are taken has them wait for it,
+// so tiles and chunks together stay within T (chunks of work / (T - tiles)) as long as that makes chunks less than twice as long.
+// Either way chunks are no shorter than work / T, so those of requests that have several (less than 2 tokens / length) are fewer than 2 T.
+__device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a, uint32_t cols, uint64_t work, uint64_t tiles)
+{
+    const uint64_t T = ((uint32_t)kCacheTarget + a.c.G - 1) / (uint32_t)a.c.G, half = (T + 1) / 2, parts = cols == 16 ? T : tiles + half < T ? T - tiles : half;
+    const uint64_t c = (work + parts - 1) / parts;
     return c < kCacheLeast ? kCacheLeast : c > 0x7fffff00u ? 0x7fffff00u : ((uint32_t)c + 127) & ~127u;
 }
-// The heads of the cache of one item are neighbours: workgroups go to the eight XCDs in turn, so that with 8 heads (or 4, 16, ..) what one L2 holds
-// of the pages serves all tiles of a request.
-// Chunks longer than the work's share make fewer than 2 kCacheTarget / G slots: a request of more than one has chunks < 2 tokens / length.
 static inline int64_t cache_slots(int G) { return 2 * ceil_div(kCacheTarget, G); }
+
+struct cache_counts { uint32_t chunks, items, slots, joins; };           // of a request; joins: tiles with more than one chunk
+__device__ __forceinline__ cache_counts cache_counts_of(const cache_request &q, uint32_t length)
+{
+    const uint32_t chunks = q.tokens <= length ? 1 : (q.tokens + length - 1) / length, items = q.tiles * chunks;
+    return {chunks, items, chunks > 1 ? items : 0, chunks > 1 ? q.tiles : 0};
+}
+
+// The plan of more than 64 requests, by one workgroup: the length of chunks, then for every 64 requests the items, the slots and the joins before
+// them.  (A scan over all requests in every workgroup took 230 of the 320 us of a step of 1024 requests of up to 512 tokens.)
+__global__ __launch_bounds__(1024) static void cache_plan_kernel(cache_attn_args a, uint32_t cols)
+{
+    __shared__ uint64_t sums[2][16];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint32_t blocks = (uint32_t)((a.requests + 63) / 64);
+    uint64_t work = 0, tiles = 0;
+    for (int64_t r = threadIdx.x; r < a.requests; r += 1024) {
+        const cache_request q = cache_request_of(a, r, cols);
+        work += (uint64_t)q.tiles * q.tokens;
+        tiles += q.tiles;
+    }
+    work = cache_wave_total(work); tiles = cache_wave_total(tiles);
+    if (lane == 0) { sums[0][w] = work; sums[1][w] = tiles; }
+    __syncthreads();
+    work = tiles = 0;
+    for (int k = 0; k < 16; ++k) { work += sums[0][k]; tiles += sums[1][k]; }
+    const uint32_t length = a.slots ? cache_chunk_tokens(a, cols, work, tiles) : 0x7fffff00u;
+    if (threadIdx.x == 0) a.plan[0] = length;
+    uint32_t *items = a.plan + 1, *slots = items + blocks, *joins = slots + blocks;
+    for (uint32_t b = w; b < blocks; b += 16) {
+        const cache_counts c = cache_counts_of(cache_request_of(a, (int64_t)b * 64 + lane, cols), length);
+        const uint32_t x = cache_wave_total(c.items), y = cache_wave_total(c.slots), z = cache_wave_total(c.joins);
+        if (lane == 0) { items[b] = x; slots[b] = y; joins[b] = z; }
+    }
+    __syncthreads();
+    if (w < 3) {
+        uint32_t *of = w == 0 ? items : w == 1 ? slots : joins, before = 0;
+        for (uint32_t b = 0; b < blocks; b += 64) {
+            const uint32_t v = b + lane < blocks ? of[b + lane] : 0, upto = before + cache_wave_scan(v, lane);
+            if (b + lane < blocks) of[b + lane] = upto - v;
+            before = __builtin_amdgcn_readlane(upto, 63);
+        }
+    }
+}
 
 // The lanes' requests in the order of their tokens, the longest first, so that a launch does not end with the longest alone.
 __device__ __forceinline__ void cache_longest_first(cache_request *q, int lane)
@@ -96,37 +147,44 @@ __device__ __forceinline__ void cache_longest_first(cache_request *q, int lane)
 }
 
 // Item `index` of all (joined = false), or tile `index` of those that have more than one chunk.  For a whole wave; false: there is none.
-__device__ __forceinline__ bool cache_find(const cache_attn_args &a, int cols, uint32_t index, bool joined, int lane, cache_item *item)
+__device__ __forceinline__ bool cache_find(const cache_attn_args &a, uint32_t cols, uint32_t index, bool joined, int lane, cache_item *item)
 {
-    cache_request q = cache_request_of(a, lane, cols);
-    const uint32_t len = __builtin_amdgcn_readfirstlane(cache_chunk_tokens(a, cols, lane, q));
-    uint32_t items = 0, slots = 0;
-    for (int64_t base = 0; base < a.requests; base += 64) {
-        if (base) q = cache_request_of(a, base + lane, cols);
-        if (joined && !__builtin_amdgcn_ballot_w64(q.tokens > len && q.tiles)) continue;         // no chunks to join here
-        if (cols > 16) cache_longest_first(&q, lane);
-        const uint32_t chunks = q.tokens <= len ? 1 : (q.tokens + len - 1) / len;
-        const uint32_t mine = joined ? (chunks > 1 ? q.tiles : 0) : q.tiles * chunks, room = chunks > 1 ? q.tiles * chunks : 0;
-        const uint32_t upto = items + cache_wave_scan(mine, lane), slot = slots + cache_wave_scan(room, lane);
-        const uint64_t behind = __builtin_amdgcn_ballot_w64(upto > index);
-        if (behind) {
-            const int k = __builtin_ctzll(behind);
-            auto of = [k](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, k); };
-            const uint32_t rest = index - (of(upto) - of(mine));
-            item->r = of(q.r);
-            item->row0 = of(q.row0);
-            item->q.n = of(q.n); item->q.columns = of(q.columns); item->q.tiles = of(q.tiles); item->q.tokens = of(q.tokens);
-            item->q.last = (int64_t)(int32_t)of((uint32_t)q.last);
-            item->chunks = of(chunks);
-            item->tile = rest % item->q.tiles;
-            item->chunk = rest / item->q.tiles;
-            item->slot = of(slot) - of(room) + item->tile;
-            return item->tile < item->q.tiles && item->chunk < item->chunks;
+    cache_request q;
+    uint32_t length = 0x7fffff00u, items = 0, slots = 0;
+    if (a.requests <= 64) {
+        q = cache_request_of(a, lane, cols);
+        if (a.slots) length = cache_chunk_tokens(a, cols, cache_wave_total((uint64_t)q.tiles * q.tokens), cache_wave_total(q.tiles));
+    } else {
+        const uint32_t blocks = (uint32_t)((a.requests + 63) / 64), *before = a.plan + 1 + (joined ? 2 * blocks : 0);
+        uint32_t block = 0;                              // the last one that begins at the index or before
+        for (uint32_t b = 0; b < blocks; b += 64) {
+            const uint64_t some = __builtin_amdgcn_ballot_w64(b + lane < blocks && before[b + lane < blocks ? b + lane : 0] <= index);
+            if (!some) break;
+            block = b + 63 - __builtin_clzll(some);
         }
-        items = __builtin_amdgcn_readlane(upto, 63);
-        slots = __builtin_amdgcn_readlane(slot, 63);
+        length = a.plan[0];
+        items = before[block];
+        slots = a.plan[1 + blocks + block];
+        q = cache_request_of(a, (int64_t)block * 64 + lane, cols);
     }
-    return false;
+    length = __builtin_amdgcn_readfirstlane(length);
+    if (joined && !__builtin_amdgcn_ballot_w64(q.tokens > length && q.tiles)) return false;         // no chunks to join here
+    if (cols > 16) cache_longest_first(&q, lane);
+    const cache_counts c = cache_counts_of(q, length);
+    const uint32_t mine = joined ? c.joins : c.items, upto = items + cache_wave_scan(mine, lane), slot = slots + cache_wave_scan(c.slots, lane);
+    const uint64_t behind = __builtin_amdgcn_ballot_w64(upto > index);
+    if (!behind) return false;
+    const int k = __builtin_ctzll(behind);
+    auto of = [k](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, k); };
+    const uint32_t rest = index - (of(upto) - of(mine));
+    item->r = of(q.r);
+    item->row0 = of(q.row0);
+    item->q = {of(q.n), of(q.columns), of(q.tiles), of(q.tokens), of(q.row0), (int32_t)of((uint32_t)q.last), of(q.r)};
+    item->chunks = of(c.chunks);
+    item->tile = rest % item->q.tiles;
+    item->chunk = rest / item->q.tiles;
+    item->slot = of(slot) - of(c.slots) + item->tile;
+    return item->tile < item->q.tiles && item->chunk < item->chunks;
 }
 
 __device__ __forceinline__ uint32_t cache_page_of(const cache_attn_args &a, uint32_t record) { return spmi_div_by32(record, a.records); }
@@ -519,7 +577,7 @@ struct cache_column {
         const uint32_t i = col / (uint32_t)a.R, h = g * a.R + col % (uint32_t)a.R;
         out = (T *)a.O + (it.row0 + i) * a.ldo + (int64_t)h * a.hdo;
         lse = a.lse ? a.lse + (int64_t)h * a.tokens + it.row0 + i : nullptr;
-        const int64_t at = ((int64_t)(it.slot + it.chunk * it.q.tiles) * a.c.G + g) * cols + col % cols;
+        const int64_t at = ((it.slot + (int64_t)it.chunk * it.q.tiles) * a.c.G + g) * cols + col % cols;
         part = it.chunks > 1 ? a.part + at * (32 * NB) : nullptr;
         stat = a.stat + at;
     }
@@ -571,92 +629,100 @@ template <typename T> constexpr int cache_nq(int nb) { return nb <= (cache_parts
 template <typename T> constexpr int cache_few_waves(int nb) { return nb <= (cache_parts<T>::n == 3 ? 3 : 4) ? 3 : nb <= (cache_parts<T>::n == 1 ? 8 : 9 - cache_parts<T>::n) ? 2 : 1; }
 template <typename T> constexpr int cache_many_waves(int nb) { return nb <= (cache_parts<T>::n == 1 ? 8 : 9 - cache_parts<T>::n) ? 2 : 1; }
 
-// 16 columns or fewer: the four waves of a workgroup take 32 tokens in turn, and they meet in the LDS.
-template <typename T, int NB>
-struct cache_meeting { float sums[4][16][32 * NB + 4]; float2 stats[4][16]; };
+// 16 NQ columns or fewer: the four waves of a workgroup take 32 tokens in turn, and they meet in the LDS.
+template <typename T, int NB, int NQ>
+struct cache_meeting { float sums[4][16 * NQ][32 * NB + 4]; float2 stats[4][16 * NQ]; };
 
-template <typename T, int NB>
-__device__ __forceinline__ void cache_few(const cache_attn_args &a, const cache_item &it, int g, uint32_t cols, int w, int lane, cache_meeting<T, NB> &m)
+template <typename T, int NB, int NQ>
+__device__ __forceinline__ void cache_few(const cache_attn_args &a, const cache_item &it, int g, uint32_t cols, int w, int lane, cache_meeting<T, NB, NQ> &m)
 {
-    const uint32_t first = it.tile * cols, count = it.q.columns - first < 16 ? it.q.columns - first : 16;
+    const uint32_t width = cache_width(it.q.columns, cols), first = it.tile * width, count = it.q.columns - first < width ? it.q.columns - first : width;
     const cache_span span = cache_span_of(a, it, first, count);
-    cache_wave<T, NB, 1> x;
-    x.load_q(a, it, first, g, lane);
-    x.run(a, it, g, span.from + 32 * w, 128, span.to, span.whole, lane);
-    const cache_attn_args &late = cache_late();
-    float total = x.total[0];
-    total += __shfl_xor(total, 16, 64);
-    total += __shfl_xor(total, 32, 64);
     const int q = lane & 15;
-    if (lane < 16) m.stats[w][q] = {x.top[0], total};
+    {
+        cache_wave<T, NB, NQ> x;
+        x.load_q(a, it, first, g, lane);
+        x.run(a, it, g, span.from + 32 * w, 128, span.to, span.whole, lane);
 #pragma unroll
-    for (int b = 0; b < 2 * NB; ++b) *(cache_f4 *)&m.sums[w][q][16 * b + 4 * (lane >> 4)] = x.o[0][b];
-    __syncthreads();
-    const uint32_t c = threadIdx.x >> 4;                 // a column for every 16 threads
-    float top = -INFINITY, f[4];
+        for (int k = 0; k < NQ; ++k) {
+            float total = x.total[k];
+            total += __shfl_xor(total, 16, 64);
+            total += __shfl_xor(total, 32, 64);
+            if (lane < 16) m.stats[w][16 * k + q] = {x.top[k], total};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) top = fmaxf(top, m.stats[k][c].x);
-    total = 0;
-    bool some[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const float2 s = m.stats[k][c];
-        some[k] = !(s.y == 0);                           // sums without weight may hold anything
-        f[k] = __builtin_amdgcn_exp2f(s.x - top);
-        total += some[k] ? s.y * f[k] : 0.f;
-    }
-    const bool there = c < count;
-    constexpr int each = (8 * NB + 15) / 16;
-    cache_f4 y[each];
-    bool fine = true;
-#pragma unroll
-    for (int j = 0; j < each; ++j) {
-        const int d = 4 * (q + 16 * j);
-        y[j] = (cache_f4)(0.f);
-        if (d < 32 * NB) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) if (some[k]) y[j] += *(const cache_f4 *)&m.sums[k][c][d] * f[k];
-            fine = fine && y[j][0] - y[j][0] == 0 && y[j][1] - y[j][1] == 0 && y[j][2] - y[j][2] == 0 && y[j][3] - y[j][3] == 0;
+            for (int b = 0; b < 2 * NB; ++b) *(cache_f4 *)&m.sums[w][16 * k + q][16 * b + 4 * (lane >> 4)] = x.o[k][b];
         }
     }
-    const uint64_t spoilt = __builtin_amdgcn_ballot_w64(there && !fine && total == total);
-    if (there && !((spoilt >> (lane & 48)) & 0xffff)) {
-        const cache_column<T, NB> out(late, it, g, first + c, cols);
+    __syncthreads();
+    const cache_attn_args &late = cache_late();
+    for (uint32_t group = 0; group < count; group += 16) {
+        const uint32_t c = group + (threadIdx.x >> 4);   // a column for every 16 threads
+        float top = -INFINITY, total = 0, f[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top = fmaxf(top, m.stats[k][c].x);
+        bool some[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 s = m.stats[k][c];
+            some[k] = !(s.y == 0);                       // sums without weight may hold anything
+            f[k] = __builtin_amdgcn_exp2f(s.x - top);
+            total += some[k] ? s.y * f[k] : 0.f;
+        }
+        const bool there = c < count;
+        constexpr int each = (8 * NB + 15) / 16;
+        cache_f4 y[each];
+        bool fine = true;
 #pragma unroll
         for (int j = 0; j < each; ++j) {
             const int d = 4 * (q + 16 * j);
-            if (d < 32 * NB) out.numbers(late, d, y[j], total);
+            y[j] = (cache_f4)(0.f);
+            if (d < 32 * NB) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) if (some[k]) y[j] += *(const cache_f4 *)&m.sums[k][c][d] * f[k];
+                fine = fine && y[j][0] - y[j][0] == 0 && y[j][1] - y[j][1] == 0 && y[j][2] - y[j][2] == 0 && y[j][3] - y[j][3] == 0;
+            }
         }
-        if (q == 0) out.total(top == -INFINITY ? 0.f : top, total);
-    }
+        const uint64_t spoilt = __builtin_amdgcn_ballot_w64(there && !fine && total == total);
+        if (there && !((spoilt >> (lane & 48)) & 0xffff)) {
+            const cache_column<T, NB> out(late, it, g, first + c, cols);
+#pragma unroll
+            for (int j = 0; j < each; ++j) {
+                const int d = 4 * (q + 16 * j);
+                if (d < 32 * NB) out.numbers(late, d, y[j], total);
+            }
+            if (q == 0) out.total(top == -INFINITY ? 0.f : top, total);
+        }
 #pragma unroll 1
-    for (int k = 0; k < 4; ++k)
-        if ((spoilt >> (16 * k)) & 0xffff) cache_again<T, NB>(late, it, g, first + 4 * w + k, cols, span.from, span.to, lane);
+        for (int k = 0; k < 4; ++k)
+            if ((spoilt >> (16 * k)) & 0xffff) cache_again<T, NB>(late, it, g, first + group + 4 * w + k, cols, span.from, span.to, lane);
+    }
 }
 
 // Single tokens of requests (and other steps of few columns a request).
 template <typename T, int NB>
 __global__ __launch_bounds__(256, cache_few_waves<T>(NB)) void cache_few_kernel(cache_attn_args a)
 {
-    __shared__ cache_meeting<T, NB> meeting;
+    __shared__ cache_meeting<T, NB, 1> meeting;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     cache_item it;
     const uint32_t index = blockIdx.x / (uint32_t)a.c.G, g = blockIdx.x - index * a.c.G;
     if (!cache_find(a, 16, index, false, lane, &it)) return;
-    if (it.chunks > 1 && it.slot + it.chunk * it.q.tiles >= a.slots) return;
-    cache_few<T, NB>(a, it, (int)g, 16, w, lane, meeting);
+    if (it.chunks > 1 && it.slot + (uint64_t)it.chunk * it.q.tiles >= a.slots) return;       // (rows of requests that overlap)
+    cache_few<T, NB, 1>(a, it, (int)g, 16, w, lane, meeting);
 }
 
 // Prompts: the four waves of a workgroup take 16 NQ columns each and all tokens of the chunk, 64 at a time.  A wave turns 16 of the 64 into
 // operands, which the four share in LDS: in registers of their own the conversions would take as long as the exponentials.  Two places: one
-// is filled while the other is worked on.  (NB > 4: one place, there is no room for two workgroups otherwise.)
+// is filled while the other is worked on.  (NB > 4: one place, there is no room for two workgroups otherwise.)  Requests whose columns would
+// leave two waves or more without any are dealt with as single tokens are, 16 NQ columns (or 16) a workgroup.
 template <typename T, int NB, int NQ>
 __global__ __launch_bounds__(256, cache_many_waves<T>(NB)) void cache_many_kernel(cache_attn_args a)
 {
     constexpr uint32_t cols = 64 * NQ;
     constexpr int places = NB <= 4 ? 2 : 1, kv = 4 * NB * 1024, stage = 2 * kv;      // kv: bytes of the operands of K (and of V) of 64 tokens
     __shared__ union __align__(16) {
-        cache_meeting<T, NB> meeting;
+        cache_meeting<T, NB, 1> meeting;
+        cache_meeting<T, NB, NQ> wide;
         struct { char at[places][stage]; uint32_t there[places][4]; } staged;
     } lds;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -664,8 +730,9 @@ __global__ __launch_bounds__(256, cache_many_waves<T>(NB)) void cache_many_kerne
     const int g = (int)(blockIdx.x - index * a.c.G);
     cache_item it;
     if (!cache_find(a, cols, index, false, lane, &it)) return;
-    if (it.chunks > 1 && it.slot + it.chunk * it.q.tiles >= a.slots) return;
-    if (it.q.columns <= 16) { cache_few<T, NB>(a, it, g, cols, w, lane, lds.meeting); return; }
+    if (it.chunks > 1 && it.slot + (uint64_t)it.chunk * it.q.tiles >= a.slots) return;       // (rows of requests that overlap)
+    if (it.q.columns <= 16) { cache_few<T, NB, 1>(a, it, g, cols, w, lane, lds.meeting); return; }
+    if (cache_width(it.q.columns, cols) < cols) { cache_few<T, NB, NQ>(a, it, g, cols, w, lane, lds.wide); return; }
     const uint32_t tile0 = it.tile * cols, tile_count = it.q.columns - tile0 < cols ? it.q.columns - tile0 : cols;
     const cache_span all = cache_span_of(a, it, tile0, tile_count);
     const uint32_t first = tile0 + 16 * NQ * w, mine = tile_count > 16 * NQ * w ? tile_count - 16 * NQ * w : 0, count = mine < 16 * NQ ? mine : 16 * NQ;
@@ -809,11 +876,12 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int 
     const int g = (int)(blockIdx.x - index * a.c.G);
     cache_item it;
     if (!cache_find(a, cols, index, true, lane, &it)) return;
-    if (it.slot + (it.chunks - 1) * it.q.tiles >= a.slots) return;       // so there are at most 2 kCacheTarget chunks
+    if (it.slot + (uint64_t)(it.chunks - 1) * it.q.tiles >= a.slots) return;       // so there are at most 2 kCacheTarget chunks
     const int64_t step = (int64_t)it.q.tiles * a.c.G * cols;
-    for (uint32_t column = blockIdx.y; column < (uint32_t)cols && it.tile * cols + column < it.q.columns; column += gridDim.y) {
-        const uint32_t col = it.tile * cols + column;
-        const int64_t base = ((int64_t)it.slot * a.c.G + g) * cols + column;
+    const uint32_t width = cache_width(it.q.columns, cols);
+    for (uint32_t column = blockIdx.y; column < width && it.tile * width + column < it.q.columns; column += gridDim.y) {
+        const uint32_t col = it.tile * width + column;
+        const int64_t base = ((int64_t)it.slot * a.c.G + g) * cols + col % (uint32_t)cols;
         float top = -INFINITY, total = 0;
         for (uint32_t k = threadIdx.x; k < it.chunks; k += 256) top = fmaxf(top, a.stat[base + k * step].x);
 #pragma unroll
@@ -860,7 +928,8 @@ struct cache_choice {
     int cols;
     int64_t items, slots;                // upper bounds; slots = 0: no request can have more than one chunk
     int64_t joins;                       // tiles of requests with more than one chunk, at most
-    size_t part, stat;                   // bytes
+    size_t part, stat, plan;             // bytes
+    size_t bytes() const { return part + stat + plan; }
 };
 
 
@@ -872,12 +941,13 @@ cache_choice cache_choose(const cache_attn_args &a)
     c.few = columns <= 16 * requests;
     c.cols = c.few ? 16 : 64 * cache_nq<T>(a.c.lay.nb);
     c.slots = a.width * a.c.P <= kCacheLeast ? 0 : cache_slots(a.c.G);
-    const int64_t tiles = columns / c.cols + requests;
+    const int64_t tiles = columns / c.cols + (c.few ? 1 : 2) * requests;
     c.joins = tiles < c.slots / 2 ? tiles : c.slots / 2;
     c.items = tiles + (c.slots ? ceil_div(kCacheTarget, a.c.G) : 0);
     const size_t rows = (size_t)c.slots * a.c.G * c.cols;
     c.part = rows * 32 * a.c.lay.nb * sizeof(float);
     c.stat = (rows * sizeof(float2) + 255) & ~(size_t)255;
+    c.plan = a.requests > 64 ? ((1 + 3 * (((size_t)a.requests + 63) / 64)) * sizeof(uint32_t) + 255) & ~(size_t)255 : 0;
     return c;
 }
 
@@ -885,6 +955,7 @@ template <typename T, int NB>
 void cache_launch(const cache_attn_args &a, const cache_choice &c, hipStream_t st)
 {
     constexpr int NQ = cache_nq<T>(NB);
+    if (c.plan) cache_plan_kernel<<<1, 1024, 0, st>>>(a, c.cols);
     if (c.few) cache_few_kernel<T, NB><<<(unsigned)(c.items * a.c.G), 256, 0, st>>>(a);
     else cache_many_kernel<T, NB, NQ><<<(unsigned)(c.items * a.c.G), 256, 0, st>>>(a);
     if (c.slots) cache_join_kernel<T, NB><<<dim3((unsigned)(c.joins * a.c.G), c.joins * a.c.G * c.cols <= 4096 ? c.cols : 4), 256, 0, st>>>(a, c.cols);

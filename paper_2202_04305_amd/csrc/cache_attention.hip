@@ -43,7 +43,7 @@ extern "C" sp_status sp_cache_attention_workspace(const sp_cache *c, const sp_ca
     cache_attn_args a;
     cache_choice choice;
     SP_TRY(check_problem(c, p, &a, &choice));
-    *bytes = choice.part + choice.stat;
+    *bytes = choice.bytes();
     return SP_OK;
 }
 
@@ -56,12 +56,13 @@ extern "C" sp_status sp_cache_attention(const sp_cache *c, const sp_cache_proble
     if ((a.tokens > 1 && ldo < a.c.D) || (a.H > 1 && hdo < a.c.D)) return SP_ERR_SHAPE;
     if (a.tokens == 0 || a.requests == 0) return SP_OK;
     if (!O || !a.Q || !a.length || !a.start || (a.width && !a.table) || !cache_has_memory(a.c)) return SP_ERR_NULL;
-    const size_t need = choice.part + choice.stat;
+    const size_t need = choice.bytes();
     if (need > 0 && !workspace) return SP_ERR_NULL;
     if (need > workspaceBytes || ((uintptr_t)workspace & 255)) return SP_ERR_SHAPE;
     a.O = O; a.ldo = ldo; a.hdo = hdo; a.lse = lse;
     a.stat = (float2 *)workspace;
-    a.part = (float *)((char *)workspace + choice.stat);
+    a.plan = (uint32_t *)((char *)workspace + choice.stat);
+    a.part = (float *)((char *)workspace + choice.stat + choice.plan);
     a.slots = (uint32_t)choice.slots;
     const int size = p->dtype == SP_F32 ? 4 : 2;
     const int64_t stray = (uintptr_t)a.Q | (uintptr_t)O | (uintptr_t)(size * (a.ldq | a.hdq | ldo | hdo));

@@ -339,6 +339,30 @@ def test_long(length, n, H, G, P):
     check_all([length, 50], [n, 1], H, G, 64, BF16, P=P)
 
 
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_thousands_of_requests(dt):
+    """More than 64 times 64 requests, most of one token, with long ones and prompts among them."""
+    r = random.Random(5)
+    lengths = [r.choice([0, 1, 16, 40]) for _ in range(4500)]
+    lengths[7], lengths[2100], lengths[4499] = 3000, 2000, 900
+    check_all(lengths, [1] * 4500, 2, 1, 32, dt)
+    n = [r.choice([0, 0, 1]) for _ in range(4500)]
+    n[100], n[2100], n[4300] = 90, 300, 40
+    lengths[100], lengths[4300] = 90, 600
+    check_all(lengths, n, 2, 1, 32, dt)
+    check_all(lengths, [k and max(k, 30) for k in n[:300]] + [0] * 4200, 2, 2, 32, dt)
+
+
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_a_few_tokens_of_each_request(d, dt):
+    """Drafted tokens: 17 to 64 columns a request, beside prompts and single tokens, short and over chunks."""
+    say("case few tokens", d, dt)
+    check_all([300, 33, 8, 1500, 5, 100, 64], [5, 8, 8, 7, 5, 6, 1], 8, 2, d, dt)
+    check_all([9000, 30], [6, 200], 4, 1, d, dt, P=64)
+    check_all([2000, 700], [33, 16], 2, 2, d, dt, causal=False)
+
+
 def test_layouts_and_rows_of_no_request():
     """Strides, rows before the first and behind the last request, which stay as they are; lse given and left out."""
     p = Pages([50, 90], 2, 64, 16)
