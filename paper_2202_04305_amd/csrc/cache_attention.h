@@ -25,7 +25,7 @@ struct cache_attn_args {
     float *part;                         // workspace: [slot][head of the cache][column][32 nb] sums
     float2 *stat;                        //            [slot][head of the cache][column]: running maximum (in units of log 2) and total
     uint32_t slots;                      // slots there is room for
-    uint32_t *plan;                      // of more than 64 requests: see cache_plan_kernel
+    uint32_t *plan;                      // see cache_plan_kernel; null: workgroups do without
 };
 
 // ---- work ------------------------------------------------------------------------------------------------------------------
@@ -78,14 +78,12 @@ __device__ __forceinline__ V cache_wave_total(V v)
     return v;
 }
 
-// Tokens of a chunk; work = sum over the requests of tiles * tokens.  A head's share of the items is T.  Few columns: there are places for more
-// workgroups than T heads' items, so chunks of work / T do.  Prompts: a workgroup that comes after all places are taken has them wait for it,
-// so tiles and chunks together stay within T (chunks of work / (T - tiles)) as long as that makes chunks less than twice as long.
-// Either way chunks are no shorter than work / T, so those of requests that have several (less than 2 tokens / length) are fewer than 2 T.
-__device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a, uint32_t cols, uint64_t work, uint64_t tiles)
+// Tokens of a chunk; work = sum over the requests of tiles * tokens, of which T items of a head get equal shares.  Chunks are no shorter than that,
+// so those of requests that have several (less than 2 tokens / length) are fewer than 2 T.
+__device__ __forceinline__ uint32_t cache_share(const cache_attn_args &a) { return ((uint32_t)kCacheTarget + a.c.G - 1) / (uint32_t)a.c.G; }
+__device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a, uint64_t work)
 {
-    const uint64_t T = ((uint32_t)kCacheTarget + a.c.G - 1) / (uint32_t)a.c.G, half = (T + 1) / 2, parts = cols == 16 ? T : tiles + half < T ? T - tiles : half;
-    const uint64_t c = (work + parts - 1) / parts;
+    const uint64_t T = cache_share(a), c = (work + T - 1) / T;
     return c < kCacheLeast ? kCacheLeast : c > 0x7fffff00u ? 0x7fffff00u : ((uint32_t)c + 127) & ~127u;
 }
 static inline int64_t cache_slots(int G) { return 2 * ceil_div(kCacheTarget, G); }
@@ -97,40 +95,61 @@ __device__ __forceinline__ cache_counts cache_counts_of(const cache_request &q, 
     return {chunks, items, chunks > 1 ? items : 0, chunks > 1 ? q.tiles : 0};
 }
 
-// The plan of more than 64 requests, by one workgroup: the length of chunks, then for every 64 requests the items, the slots and the joins before
-// them.  (A scan over all requests in every workgroup took 230 of the 320 us of a step of 1024 requests of up to 512 tokens.)
+// The plan of a step of prompts, or of more than 64 requests, by one workgroup: the length of chunks, the number of joins, then for every 64
+// requests the items, the slots and the joins before them.  (A scan over all requests in every workgroup took 230 of the 320 us of a step of 1024
+// requests of up to 512 tokens.)
+// Prompts: a workgroup that comes after all places are taken has them wait for it, so chunks grow by quarters, up to twice, until there is a place
+// for every item.  (Single tokens leave room for half as many workgroups again, and more chunks finish closer together.)
 __global__ __launch_bounds__(1024) static void cache_plan_kernel(cache_attn_args a, uint32_t cols)
 {
-    __shared__ uint64_t sums[2][16];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    __shared__ uint64_t sums[16];
+    __shared__ uint32_t counts[16];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const uint32_t blocks = (uint32_t)((a.requests + 63) / 64);
-    uint64_t work = 0, tiles = 0;
-    for (int64_t r = threadIdx.x; r < a.requests; r += 1024) {
-        const cache_request q = cache_request_of(a, r, cols);
-        work += (uint64_t)q.tiles * q.tokens;
-        tiles += q.tiles;
+    uint32_t length = 0x7fffff00u;
+    if (a.slots) {
+        uint64_t work = 0;
+        for (int64_t r = threadIdx.x; r < a.requests; r += blockDim.x) {
+            const cache_request q = cache_request_of(a, r, cols);
+            work += (uint64_t)q.tiles * q.tokens;
+        }
+        work = cache_wave_total(work);
+        if (lane == 0) sums[w] = work;
+        __syncthreads();
+        work = 0;
+        for (int k = 0; k < waves; ++k) work += sums[k];
+        length = cache_chunk_tokens(a, work);
+        if (cols > 16) {
+            const uint32_t more = (length / 4 + 63) & ~63u;
+            for (int tries = 0; tries < 5; ++tries) {
+                uint32_t items = 0;
+                for (int64_t r = threadIdx.x; r < a.requests; r += blockDim.x) items += cache_counts_of(cache_request_of(a, r, cols), length + more * tries).items;
+                items = cache_wave_total(items);
+                __syncthreads();
+                if (lane == 0) counts[w] = items;
+                __syncthreads();
+                items = 0;
+                for (int k = 0; k < waves; ++k) items += counts[k];
+                if (items <= cache_share(a)) { length += more * tries; break; }
+                if (tries == 0 && items > 2 * cache_share(a)) break;      // tiles enough as they are
+            }
+        }
     }
-    work = cache_wave_total(work); tiles = cache_wave_total(tiles);
-    if (lane == 0) { sums[0][w] = work; sums[1][w] = tiles; }
-    __syncthreads();
-    work = tiles = 0;
-    for (int k = 0; k < 16; ++k) { work += sums[0][k]; tiles += sums[1][k]; }
-    const uint32_t length = a.slots ? cache_chunk_tokens(a, cols, work, tiles) : 0x7fffff00u;
-    if (threadIdx.x == 0) a.plan[0] = length;
-    uint32_t *items = a.plan + 1, *slots = items + blocks, *joins = slots + blocks;
-    for (uint32_t b = w; b < blocks; b += 16) {
+    uint32_t *items = a.plan + 2, *slots = items + blocks, *joins = slots + blocks;
+    for (uint32_t b = w; b < blocks; b += waves) {
         const cache_counts c = cache_counts_of(cache_request_of(a, (int64_t)b * 64 + lane, cols), length);
         const uint32_t x = cache_wave_total(c.items), y = cache_wave_total(c.slots), z = cache_wave_total(c.joins);
         if (lane == 0) { items[b] = x; slots[b] = y; joins[b] = z; }
     }
     __syncthreads();
-    if (w < 3) {
-        uint32_t *of = w == 0 ? items : w == 1 ? slots : joins, before = 0;
+    for (int which = w; which < 3; which += waves) {
+        uint32_t *of = which == 0 ? items : which == 1 ? slots : joins, before = 0;
         for (uint32_t b = 0; b < blocks; b += 64) {
             const uint32_t v = b + lane < blocks ? of[b + lane] : 0, upto = before + cache_wave_scan(v, lane);
             if (b + lane < blocks) of[b + lane] = upto - v;
             before = __builtin_amdgcn_readlane(upto, 63);
         }
+        if (which == 2 && lane == 0) { a.plan[0] = length; a.plan[1] = before; }
     }
 }
 
@@ -151,20 +170,22 @@ __device__ __forceinline__ bool cache_find(const cache_attn_args &a, uint32_t co
 {
     cache_request q;
     uint32_t length = 0x7fffff00u, items = 0, slots = 0;
-    if (a.requests <= 64) {
+    if (!a.plan) {
         q = cache_request_of(a, lane, cols);
-        if (a.slots) length = cache_chunk_tokens(a, cols, cache_wave_total((uint64_t)q.tiles * q.tokens), cache_wave_total(q.tiles));
+        if (a.slots) length = cache_chunk_tokens(a, cache_wave_total((uint64_t)q.tiles * q.tokens));
     } else {
-        const uint32_t blocks = (uint32_t)((a.requests + 63) / 64), *before = a.plan + 1 + (joined ? 2 * blocks : 0);
+        if (joined && index >= a.plan[1]) return false;
+        const uint32_t blocks = (uint32_t)((a.requests + 63) / 64), *before = a.plan + 2 + (joined ? 2 * blocks : 0);
         uint32_t block = 0;                              // the last one that begins at the index or before
-        for (uint32_t b = 0; b < blocks; b += 64) {
-            const uint64_t some = __builtin_amdgcn_ballot_w64(b + lane < blocks && before[b + lane < blocks ? b + lane : 0] <= index);
-            if (!some) break;
-            block = b + 63 - __builtin_clzll(some);
-        }
+        if (blocks > 1)
+            for (uint32_t b = 0; b < blocks; b += 64) {
+                const uint64_t some = __builtin_amdgcn_ballot_w64(b + lane < blocks && before[b + lane < blocks ? b + lane : 0] <= index);
+                if (!some) break;
+                block = b + 63 - __builtin_clzll(some);
+            }
         length = a.plan[0];
         items = before[block];
-        slots = a.plan[1 + blocks + block];
+        slots = a.plan[2 + blocks + block];
         q = cache_request_of(a, (int64_t)block * 64 + lane, cols);
     }
     length = __builtin_amdgcn_readfirstlane(length);
@@ -863,7 +884,7 @@ __global__ __launch_bounds__(256, cache_many_waves<T>(NB)) void cache_many_kerne
     for (; spoilt; spoilt &= spoilt - 1) cache_again<T, NB>(late, it, g, first + __builtin_ctzll(spoilt), cols, all.from, all.to, lane);
 }
 
-// Joins the chunks of the tiles that have several: a workgroup for each column (or some of them in turn).  The chunks' factors first, then the
+// Joins the chunks of the tiles that have several: of up to 16 chunks a wave for each column, of more a workgroup (or some columns in turn).  The chunks' factors first, then the
 // sums, a quarter of the chunks a wave: loads that do not wait for each other.
 template <typename T, int NB>
 __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int cols)
@@ -878,8 +899,44 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int 
     if (!cache_find(a, cols, index, true, lane, &it)) return;
     if (it.slot + (uint64_t)(it.chunks - 1) * it.q.tiles >= a.slots) return;       // so there are at most 2 kCacheTarget chunks
     const int64_t step = (int64_t)it.q.tiles * a.c.G * cols;
-    const uint32_t width = cache_width(it.q.columns, cols);
-    for (uint32_t column = blockIdx.y; column < width && it.tile * width + column < it.q.columns; column += gridDim.y) {
+    const uint32_t width = cache_width(it.q.columns, cols), most = it.q.columns - it.tile * width, columns = most < width ? most : width;
+    if (it.chunks <= 16) {                               // a wave for each column
+        for (uint32_t column = blockIdx.y + w * gridDim.y; column < columns; column += 4 * gridDim.y) {
+            const uint32_t col = it.tile * width + column;
+            const int64_t base = ((int64_t)it.slot * a.c.G + g) * cols + col % (uint32_t)cols;
+            const float2 s = (uint32_t)lane < it.chunks ? a.stat[base + lane * step] : make_float2(-INFINITY, 0);
+            float top = s.x;
+#pragma unroll
+            for (int d = 8; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+            const float f = s.y == 0 ? 0.f : __builtin_amdgcn_exp2f(s.x - top);      // (sums without weight are zeros)
+            float total = s.y == 0 ? 0.f : s.y * f, acc[per] = {};
+#pragma unroll
+            for (int d = 8; d >= 1; d >>= 1) total += __shfl_xor(total, d, 64);
+            total = __shfl(total, 0, 64); top = __shfl(top, 0, 64);
+            for (uint32_t k0 = 0; k0 < it.chunks; k0 += 4) {             // four at a time; behind the last one that one again, without weight
+                float x[4][per];
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    const float *part = a.part + (base + (k0 + k < it.chunks ? k0 + k : it.chunks - 1) * step) * pad;
+#pragma unroll
+                    for (int j = 0; j < per; ++j) x[k][j] = pad % 64 == 0 || lane + 64 * j < pad ? part[lane + 64 * j] : 0.f;
+                }
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    const float fk = __shfl(f, (int)(k0 + k), 64);
+#pragma unroll
+                    for (int j = 0; j < per; ++j) acc[j] += x[k][j] * fk;
+                }
+            }
+            const uint32_t i = col / (uint32_t)a.R, h = g * a.R + col % (uint32_t)a.R;
+            T *out = (T *)a.O + (it.row0 + i) * a.ldo + (int64_t)h * a.hdo;
+#pragma unroll
+            for (int j = 0; j < per; ++j) if (lane + 64 * j < a.c.D) out[lane + 64 * j] = (T)(total == 0 ? 0.f : acc[j] / total);
+            if (a.lse && lane == 0) a.lse[(int64_t)h * a.tokens + it.row0 + i] = total == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kCacheLn2;
+        }
+        return;
+    }
+    for (uint32_t column = blockIdx.y; column < columns; column += gridDim.y) {
         const uint32_t col = it.tile * width + column;
         const int64_t base = ((int64_t)it.slot * a.c.G + g) * cols + col % (uint32_t)cols;
         float top = -INFINITY, total = 0;
@@ -947,7 +1004,7 @@ cache_choice cache_choose(const cache_attn_args &a)
     const size_t rows = (size_t)c.slots * a.c.G * c.cols;
     c.part = rows * 32 * a.c.lay.nb * sizeof(float);
     c.stat = (rows * sizeof(float2) + 255) & ~(size_t)255;
-    c.plan = a.requests > 64 ? ((1 + 3 * (((size_t)a.requests + 63) / 64)) * sizeof(uint32_t) + 255) & ~(size_t)255 : 0;
+    c.plan = a.requests > 64 || (!c.few && c.slots) ? ((2 + 3 * (((size_t)a.requests + 63) / 64)) * sizeof(uint32_t) + 255) & ~(size_t)255 : 0;
     return c;
 }
 
@@ -955,10 +1012,10 @@ template <typename T, int NB>
 void cache_launch(const cache_attn_args &a, const cache_choice &c, hipStream_t st)
 {
     constexpr int NQ = cache_nq<T>(NB);
-    if (c.plan) cache_plan_kernel<<<1, 1024, 0, st>>>(a, c.cols);
+    if (c.plan) cache_plan_kernel<<<1, a.requests <= 64 ? 64 : 1024, 0, st>>>(a, c.cols);
     if (c.few) cache_few_kernel<T, NB><<<(unsigned)(c.items * a.c.G), 256, 0, st>>>(a);
     else cache_many_kernel<T, NB, NQ><<<(unsigned)(c.items * a.c.G), 256, 0, st>>>(a);
-    if (c.slots) cache_join_kernel<T, NB><<<dim3((unsigned)(c.joins * a.c.G), c.joins * a.c.G * c.cols <= 4096 ? c.cols : 4), 256, 0, st>>>(a, c.cols);
+    if (c.slots) cache_join_kernel<T, NB><<<dim3((unsigned)(c.joins * a.c.G), c.few ? (c.joins * a.c.G <= 256 ? 16 : 4) : c.cols / 8), 256, 0, st>>>(a, c.cols);
 }
 
 template <typename T> sp_status cache_attention(const cache_attn_args &a, const cache_choice &c, hipStream_t st);

@@ -61,7 +61,7 @@ extern "C" sp_status sp_cache_attention(const sp_cache *c, const sp_cache_proble
     if (need > workspaceBytes || ((uintptr_t)workspace & 255)) return SP_ERR_SHAPE;
     a.O = O; a.ldo = ldo; a.hdo = hdo; a.lse = lse;
     a.stat = (float2 *)workspace;
-    a.plan = (uint32_t *)((char *)workspace + choice.stat);
+    if (choice.plan) a.plan = (uint32_t *)((char *)workspace + choice.stat);
     a.part = (float *)((char *)workspace + choice.stat + choice.plan);
     a.slots = (uint32_t)choice.slots;
     const int size = p->dtype == SP_F32 ? 4 : 2;

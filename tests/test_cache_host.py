@@ -4,6 +4,7 @@ import ctypes
 import math
 import os
 import re
+import subprocess
 
 import pytest
 import torch
@@ -11,6 +12,8 @@ import torch
 import paper_2202_04305_amd as sp
 import cache_util as U
 from paper_2202_04305_amd import binding as B
+from paper_2202_04305_amd import build
+from test_device_assembly import OBJDUMP, lost_registers
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 TYPES = {"int": ctypes.c_int, "int64_t": ctypes.c_int64, "double": ctypes.c_double}
@@ -224,3 +227,20 @@ def test_reference_attention():
             assert abs(got["lse"][0][h, row] - torch.logsumexp(s, 0)) < 1e-12
     assert (got["O"][0][4:6] == 0).all() and (got["lse"][0][:, 4:6] == float("-inf")).all() and torch.isnan(got["O"][0][6]).all()
     assert all(bool((tol[:6] if k == "O" else tol[:, :6]).isfinite().all()) for k, (_, tol) in got.items())
+
+
+def test_no_kernel_of_the_cache_loses_what_it_keeps_aside(tmp_path):
+    """As for the kernels of attention over a pattern: what the compiler keeps in accumulation registers or scratch is fetched again, all of it."""
+    lib = tmp_path / "lib.so"
+    build.is_stale() and build.build()
+    lib.write_bytes(open(build.LIB, "rb").read())
+    subprocess.check_call([OBJDUMP, "--offloading", str(lib)], stdout=subprocess.DEVNULL, cwd=tmp_path)
+    kernels = 0
+    for part in sorted(tmp_path.glob("lib.so.*gfx950")):
+        names = subprocess.run([OBJDUMP, "-t", str(part)], stdout=subprocess.PIPE, text=True, check=True).stdout
+        if not re.search(r"cache_(few|many|join)_kernel", names):
+            continue
+        asm = subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", str(part)], stdout=subprocess.PIPE, text=True, check=True).stdout.splitlines()
+        kernels += sum(bool(re.match(r"[0-9a-f]+ <\S*cache_(few|many|join)_kernel", l)) for l in asm)
+        assert lost_registers(asm) == {}
+    assert kernels == 3 * 8 * 3, kernels
