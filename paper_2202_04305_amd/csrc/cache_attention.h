@@ -540,7 +540,7 @@ struct cache_wave {
                 const uint32_t record = at / kCacheTile + half, in = record - page_of(record) * per;
                 const bool ok = (uint32_t)p[half] < count;
                 there |= ok ? 1u << half : 0;
-                x.half[half].load(data + ((ok ? (uint32_t)p[half] : 0u) * page_bytes + in * cache_record<NB>::bytes), lane);
+                x.half[half].load(data + ((ok ? (uint32_t)p[half] : 0u) * page_bytes + in * (int64_t)cache_record<NB>::bytes), lane);
             }
             return there;
         };
@@ -775,7 +775,7 @@ __global__ __launch_bounds__(256, cache_many_waves<T>(NB)) void cache_many_kerne
     auto fetch = [&](uint32_t t, int32_t p) {
         const uint32_t record = t / kCacheTile + w, in = record - cache_page_of(a, record) * per;
         const bool ok = (uint32_t)p < count_pages;
-        rec.load(data + ((ok ? (uint32_t)p : 0u) * page_bytes + in * cache_record<NB>::bytes), lane);
+        rec.load(data + ((ok ? (uint32_t)p : 0u) * page_bytes + in * (int64_t)cache_record<NB>::bytes), lane);
         return ok;
     };
     auto put = [&](int place, uint32_t t, bool ok) {

@@ -551,6 +551,26 @@ def test_offsets_beyond_32_bits():
         check(got, U.attended(U.held(K), U.held(V), Q, small, lengths, start, P, 6))
 
 
+def test_a_page_beyond_32_bits():
+    """Tokens that lie beyond 2^32 bytes of their page: of 16 million zeros before them nothing is left beside scores of 100 and more."""
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GiB")
+    P, d = 1 << 24, 256
+    c = sp.sp_cache(1, P, 1, d)
+    for n in (1, 40):
+        length = P - 100 * n
+        slots = torch.arange(length - 50, length)
+        K, V = 7 + normal((50, 1, d), BF16, 1).abs(), normal((50, 1, d), BF16, n)
+        sp.sp_cache_store(c, K.to(DEV), V.to(DEV), slots.int().to(DEV))
+        assert same(sp.sp_cache_load(c, slots.int().to(DEV), F32)[1], U.held(V), F32)
+        Q = torch.ones(n, 2, d).to(BF16)
+        got = sp.sp_cache_attention(c, Q.to(DEV), ints([[0]]).to(DEV), ints([length]).to(DEV), ints([0, n]).to(DEV), causal=False)
+        pad = torch.zeros(14, 1, d, dtype=torch.float64)
+        want = U.attended(torch.cat([U.held(K), pad]), torch.cat([U.held(V), pad]), Q, torch.tensor([[0, 1, 2, 3]]), [50], [0, n], 16, 4, causal=False)
+        assert (want["lse"][0] > 100).all()
+        check(dict(zip(("O", "lse"), got)), want)
+
+
 def test_attention_refused_arguments():
     p = Pages([20, 30], 2, 64, 16)
     Q, table, lengths, start = normal((2, 4, 64), BF16, 1).to(DEV), p.table.to(DEV), ints([20, 30]).to(DEV), ints([0, 1, 2]).to(DEV)
