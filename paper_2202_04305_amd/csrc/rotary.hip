@@ -34,14 +34,15 @@ __device__ __forceinline__ float2 rotary_turn(int position, double f)
 
 constexpr int kRotaryPairs = 1024;       // pairs of a workgroup's tokens that the LDS has room for
 
-// V numbers at a time (16 bytes of them where everything is aligned to that, single ones otherwise).  An item of a head is V pairs, of numbers
-// that lie half apart or side by side, or V numbers that stay.  Where the pairs do not fit the LDS (heads beyond 2 kRotaryPairs numbers) every
+// V pairs at a time and W of the numbers that stay (16 bytes of them where everything is aligned to that, single ones otherwise).  An item of a
+// head is V pairs, of numbers that lie half apart or side by side, or W numbers that stay.  Where the pairs do not fit the LDS (heads beyond 2 kRotaryPairs numbers) every
 // item makes its own.
-template <typename T, int V, bool INTERLEAVED>
+template <typename T, int V, int W, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotary_kernel(rotary_args a)
 {
     typedef T row __attribute__((ext_vector_type(V)));
     typedef T row2 __attribute__((ext_vector_type(2 * V)));
+    typedef T rest __attribute__((ext_vector_type(W)));
     __shared__ float2 turn[kRotaryPairs];
     const int turning = a.half / V;
     const bool kept = a.half <= kRotaryPairs;
@@ -66,8 +67,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(rotary_args a)
         const T *in = (const T *)s.in + (i0 + i) * s.ld + h * s.hd;
         T *out = (T *)s.out + (i0 + i) * s.ldo + h * s.hdo;
         if (k >= turning) {                              // behind the turning numbers
-            const int d = 2 * a.half + (k - turning) * V;
-            *(row *)(out + d) = *(const row *)(in + d);
+            const int d = 2 * a.half + (k - turning) * W;
+            *(rest *)(out + d) = *(const rest *)(in + d);
             continue;
         }
         float u[V], v[V];
@@ -108,10 +109,10 @@ __global__ __launch_bounds__(256) void rotary_kernel(rotary_args a)
     }
 }
 
-template <typename T, int V>
+template <typename T, int V, int W>
 void launch(rotary_args a, hipStream_t st)
 {
-    a.per_head = (a.D - a.half) / V;
+    a.per_head = a.half / V + (a.D - 2 * a.half) / W;
     const int heads = a.side[0].heads + a.side[1].heads;
     a.items = heads * a.per_head;
     a.by_head = spmi_make_divisor32(a.per_head);
@@ -123,22 +124,30 @@ void launch(rotary_args a, hipStream_t st)
     a.group = (int)(group > most ? most : group < 1 ? 1 : group);
     const int64_t blocks = ceil_div(a.tokens, a.group), each = ceil_div((int64_t)a.group * a.items, 256), more = ceil_div(512, blocks);
     const dim3 grid((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20), (unsigned)(each < more ? each : more < 1 ? 1 : more));
-    if (a.interleaved) rotary_kernel<T, V, true><<<grid, 256, 0, st>>>(a);
-    else rotary_kernel<T, V, false><<<grid, 256, 0, st>>>(a);
+    if (a.interleaved) rotary_kernel<T, V, W, true><<<grid, 256, 0, st>>>(a);
+    else rotary_kernel<T, V, W, false><<<grid, 256, 0, st>>>(a);
 }
 
-// The most numbers at a time that sizes, strides and addresses allow: 16 bytes, or half of that, or a quarter, ...
+// Are addresses and strides of all tensors multiples of so many numbers?
+bool aligned(const rotary_args &a, int64_t numbers, int64_t size)
+{
+    for (const rotary_side &s : a.side)
+        if (s.heads && ((((uintptr_t)s.in | (uintptr_t)s.out) % (numbers * size)) || s.ld % numbers || s.hd % numbers || s.ldo % numbers || s.hdo % numbers)) return false;
+    return true;
+}
+
+// The most numbers at a time that sizes, strides and addresses allow: 16 bytes, or half of that, or a quarter, ...; of those that stay 16 bytes or
+// as many as of the pairs.
 template <typename T, int V>
 void launch_widest(const rotary_args &a, hipStream_t st)
 {
+    constexpr int most = 16 / sizeof(T);
+    const int64_t run = a.interleaved ? 2 * V : V, rest = a.D - 2 * a.half;
     if constexpr (V > 1) {
-        const int64_t run = a.interleaved ? 2 * V : V;
-        bool fits = a.half % V == 0 && (a.D - 2 * a.half) % V == 0 && run * (int64_t)sizeof(T) <= 16;
-        for (const rotary_side &s : a.side)
-            if (s.heads) fits = fits && (((uintptr_t)s.in | (uintptr_t)s.out) % (run * sizeof(T)) == 0) && s.ld % run == 0 && s.hd % run == 0 && s.ldo % run == 0 && s.hdo % run == 0;
-        if (!fits) return launch_widest<T, V / 2>(a, st);
+        if (a.half % V || run > most || rest % V || !aligned(a, run, sizeof(T))) return launch_widest<T, V / 2>(a, st);
     }
-    launch<T, V>(a, st);
+    if (V < most && rest && rest % most == 0 && 2 * a.half % most == 0 && aligned(a, most, sizeof(T))) launch<T, V, most>(a, st);
+    else launch<T, V, V>(a, st);
 }
 
 sp_status rotary(const sp_rotary_problem *p, float sign, void *stream)
