@@ -158,53 +158,73 @@ __device__ __forceinline__ int cache_exponent(float top)
 constexpr int kStoreTokens = 32;         // of a workgroup, which takes one head of them
 
 // Eight numbers of a row, zeros behind its end.
+template <typename T> using cache_row8 = T __attribute__((ext_vector_type(8)));
 template <typename T>
-__device__ __forceinline__ void load8(const T *row, int d0, int D, bool vec, float (&x)[8])
+__device__ __forceinline__ cache_row8<T> load8(const T *row, int d0, int D, bool vec)
 {
-    if (vec) {
-        typedef T row8 __attribute__((ext_vector_type(8)));
-        row8 v = {};
-        if (d0 < D) v = *(const row8 *)(row + d0);
+    cache_row8<T> v = {};
+    if (vec) { if (d0 < D) v = *(const cache_row8<T> *)(row + d0); }
+    else
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = d0 + j < D ? (float)row[d0 + j] : 0.f;
-    }
+        for (int j = 0; j < 8; ++j) if (d0 + j < D) v[j] = row[d0 + j];
+    return v;
 }
 
-// Rows into the pages.  Their bytes bound it.  Four neighbouring lanes have a block of 32 numbers, 8 each, which are a word of K as they lie.  A
-// token's values are every fourth byte of 64 NB, so the tokens of a workgroup meet in the LDS, from where four that are neighbours in the
-// pages (aligned to four) go out as words, others as bytes.
+// Rows into the pages.  Four neighbouring lanes have a block of 32 numbers, 8 each, which are a word of K as they lie.  A token's values are
+// every fourth byte of 64 NB, so the tokens of a workgroup meet in the LDS: neighbours that share the words of four tokens there are a group, which
+// goes out as words if it has all four, as bytes otherwise.  The rows' bytes and the instructions (400 a wave) bound it alike.
 template <typename T, int NB>
 __global__ __launch_bounds__(256) void store_kernel(cache_rows a, int vec)
 {
-    constexpr int words = 4 * NB, row = 16 * NB;         // lanes of a token; bytes of a token's values
-    __shared__ uint8_t bytes[kStoreTokens][row];
-    __shared__ int32_t slots[kStoreTokens + 3];
+    constexpr int words = 4 * NB, row = 16 * NB;         // lanes of a token; words of four tokens' values
+    __shared__ uint32_t values[kStoreTokens][row];       // [group]
+    __shared__ uint8_t *record[kStoreTokens], *to[kStoreTokens];         // of a token (null: not stored); of a group
+    __shared__ uint32_t place[kStoreTokens], mask[kStoreTokens];         // of a token: its number in the record + 16 * its group; of a group
     const cache_view &c = a.c;
     const uint32_t window = blockIdx.x / (uint32_t)c.G, head = blockIdx.x - window * (uint32_t)c.G;
-    const int64_t i0 = (int64_t)window * kStoreTokens, room = c.pages * c.P;
+    const int64_t i0 = (int64_t)window * kStoreTokens;
     const int tokens = (int)(a.tokens - i0 < kStoreTokens ? a.tokens - i0 : kStoreTokens), g = (int)head;
-    if (threadIdx.x < kStoreTokens + 3) {
-        const int32_t slot = (int)threadIdx.x < tokens ? a.slot[i0 + threadIdx.x] : -1;
-        slots[threadIdx.x] = slot < room ? slot : -1;
+    const int lane = threadIdx.x & 63;
+    int64_t slot = -1;
+    if ((int)threadIdx.x < tokens) slot = a.slot[i0 + threadIdx.x];
+    // all rows are asked for at once, before it is known where they go
+    constexpr int each = (kStoreTokens * words + 255) / 256;
+    cache_row8<T> in[each][2];
+#pragma unroll
+    for (int k = 0; k < each; ++k) {
+        const int x = threadIdx.x + 256 * k, i = x / words, d0 = x % words * 8;
+        if (i >= tokens) continue;
+        in[k][0] = load8<T>((const T *)a.K + (i0 + i) * a.ldk + g * a.hdk, d0, c.D, vec);
+        in[k][1] = load8<T>((const T *)a.V + (i0 + i) * a.ldv + g * a.hdv, d0, c.D, vec);
+    }
+    if (threadIdx.x < 64) {
+        if (slot >= c.pages * c.P) slot = -1;
+        if (lane < kStoreTokens) mask[lane] = 0;
+        const int four = slot < 0 ? -1 : (int)(slot >> 2), before = __shfl_up(four, 1, 64);
+        const bool first = lane == 0 || four < 0 || four != before;
+        const int group = __popcll(__builtin_amdgcn_ballot_w64(first) & (~0ull >> (63 - lane))) - 1;
+        if (lane < tokens) {
+            const uint32_t t = slot < 0 ? 0 : (uint32_t)slot % (uint32_t)c.P, u = t % kCacheTile;
+            uint8_t *rec = slot < 0 ? nullptr : c.record((uint32_t)slot / (uint32_t)c.P, g, (int)t);
+            record[lane] = rec;
+            place[lane] = u + 16 * group;
+            if (first && rec) to[group] = rec + c.lay.v_codes() + (u >> 2) * (row * 4);
+            if (rec) atomicOr(&mask[group], 1u << (u & 3));
+        }
     }
     __syncthreads();
-    for (int x = threadIdx.x; x < tokens * words; x += 256) {            // the four lanes of a block stay together
-        const int i = x / words, s = (x % words) / 4, q = x & 3, d0 = 32 * s + 8 * q;
-        const int32_t slot = slots[i];
-        if (slot < 0) continue;
-        const int t = (int)((uint32_t)slot % (uint32_t)c.P);
-        uint8_t *rec = c.record((uint32_t)slot / (uint32_t)c.P, g, t);
-        const int u = t % kCacheTile;
+#pragma unroll
+    for (int k = 0; k < each; ++k) {                     // the four lanes of a block stay together
+        const int x = threadIdx.x + 256 * k, i = x / words, s = (x % words) / 4, q = x & 3;
+        if (i >= tokens) continue;
+        uint8_t *rec = record[i];
+        if (!rec) continue;
+        const int u = place[i] & 15, group = place[i] >> 4;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            float v[8];
-            load8<T>(which ? (const T *)a.V + (i0 + i) * a.ldv + g * a.hdv : (const T *)a.K + (i0 + i) * a.ldk + g * a.hdk, d0, c.D, vec, v);
-            float top = 0, none = 0;                     // none: 0, or not a number
+            float v[8], top = 0, none = 0;               // none: 0, or not a number
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { top = fmaxf(top, fabsf(v[j])); none += v[j] - v[j]; }
+            for (int j = 0; j < 8; ++j) { v[j] = (float)in[k][which][j]; top = fmaxf(top, fabsf(v[j])); none += v[j] - v[j]; }
             top = fmaxf(top, __shfl_xor(top, 1, 64)); none += __shfl_xor(none, 1, 64);
             top = fmaxf(top, __shfl_xor(top, 2, 64)); none += __shfl_xor(none, 2, 64);
             const bool finite = none == 0;
@@ -218,28 +238,26 @@ __global__ __launch_bounds__(256) void store_kernel(cache_rows a, int vec)
             if (q == 0) rec[(which ? c.lay.v_scales() : c.lay.k_scales()) + u * c.lay.sb + s] = finite ? (uint8_t)(e + 127) : (uint8_t)kCacheNaN;
             if (!which) ((uint32_t *)rec)[(u * 4 + q) * NB + s] = code;
             else {
-                // numbers 32 s + n and 32 s + 16 + n share a byte: lanes q and q + 2
-                const uint32_t other = __shfl_xor(code, 2, 64), lo = q < 2 ? code : other, hi = q < 2 ? other : code;
-                // this lane's four bytes of the eight: n = 8 (q & 1) + 4 (q >> 1) + 0 .. 3
-                const uint32_t l = q < 2 ? lo & 0xffff : lo >> 16, h = q < 2 ? hi & 0xffff : hi >> 16;
+                // numbers 32 s + n and 32 s + 16 + n share a byte: lanes q and q + 2, of which each writes four, n = 8 (q & 1) + 4 (q >> 1) + 0 .. 3
+                const uint32_t other = __shfl_xor(code, 2, 64), lo = q < 2 ? code & 0xffff : other >> 16, hi = q < 2 ? other & 0xffff : code >> 16;
+                uint8_t *at = (uint8_t *)&values[group][(8 * (q & 1) + 4 * (q >> 1)) * NB + s] + (u & 3);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    bytes[i][(8 * (q & 1) + 4 * (q >> 1) + j) * NB + s] = (uint8_t)(((l >> (4 * j)) & 15) | ((h >> (4 * j)) & 15) << 4);
+                for (int j = 0; j < 4; ++j) at[j * NB * 4] = (uint8_t)(((lo >> (4 * j)) & 15) | ((hi >> (4 * j)) & 15) << 4);
             }
         }
     }
     __syncthreads();
+#pragma unroll 1
     for (int x = threadIdx.x; x < tokens * row; x += 256) {
-        const int i = x / row, k = x % row, slot = slots[i];
-        if (slot < 0) continue;
-        // four neighbours, of which this is the first, or another one that the first takes along
-        const int lead = i - (slot & 3);
-        const bool four = lead >= 0 && slots[lead] == (slot & ~3) && slots[lead + 1] == (slot & ~3) + 1 && slots[lead + 2] == (slot & ~3) + 2 && slots[lead + 3] == (slot & ~3) + 3;
-        if (four && lead != i) continue;
-        const int t = (int)((uint32_t)slot % (uint32_t)c.P);
-        uint8_t *at = c.record((uint32_t)slot / (uint32_t)c.P, g, t) + c.lay.v_codes() + ((t % kCacheTile >> 2) * row + k) * 4;
-        if (four) *(uint32_t *)at = bytes[i][k] | bytes[i + 1][k] << 8 | bytes[i + 2][k] << 16 | (uint32_t)bytes[i + 3][k] << 24;
-        else at[t & 3] = bytes[i][k];
+        const int group = x / row, k = x % row;
+        const uint32_t some = mask[group];
+        if (!some) continue;                             // there are fewer groups than tokens, or its token is not stored
+        uint8_t *at = to[group] + k * 4;
+        const uint32_t word = values[group][k];
+        if (some == 15) *(uint32_t *)at = word;
+        else
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if ((some >> j) & 1) at[j] = (uint8_t)(word >> (8 * j));
     }
 }
 
