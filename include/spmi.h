@@ -337,15 +337,16 @@ sp_status sp_cache_load(const sp_cache *c, int dtype, int64_t tokens, const int3
  *     s[t] = scale * sum_d Q[i,h,d] * K[t,g,d],   lse[h,i] = log sum_t exp(s[t]),   O[i,h,d] = sum_t exp(s[t] - lse[h,i]) * V[t,g,d]
  * Single tokens, prompts (or pieces of them) and mixtures of both are the same call.  Tokens whose page is not in [0, pages) and tokens behind
  * width * pageTokens are not attended to.  Rows, infinities and NaN as for sp_attention: a row that attends to nothing gives O = 0 and lse =
- * minus infinity, and what a row does not attend to has no influence on it, whatever it holds.  start ascends from 0 or more to `tokens` or
- * less; rows that belong to no request are left as they were.
+ * minus infinity, and what a row does not attend to has no influence on it, whatever it holds.  start ascends from 0 or more; rows
+ * that belong to no request are left as they were, and requests' rows behind row tokens - 1 are not looked at.
  *   O    DEVICE: element (i, h, d) at O[i * ldo + h * hdo + d]; rows must not overlap each other or an input.
  *   lse  DEVICE, heads x tokens, f32; may be NULL.
  *   workspace  as for sp_attention: sp_cache_attention_workspace bytes, aligned to 256, one for each of the calls that may overlap.
  * Enqueues on `stream`; neither allocates nor synchronises, reads lengths, rows and pages on the GPU (a recorded graph serves other ones), and
  * gives the same bits on every call.  The numbers of the cache are exact in the products; Q is, too (in as many parts of bf16 as its type
  * has room for); weights are rounded to Q's type before their product.  Errors, in this order: NULL (c, p), DTYPE, SHAPE, UNSUPPORTED (causal neither 0
- * nor 1), TOO_LARGE (pages * pageTokens, tokens, or requests of 2^31 or more, or more workgroups than a launch has), NULL, SHAPE (workspace), HIP. */
+ * nor 1), TOO_LARGE (pages * pageTokens, width * pageTokens, requests, or tokens * heads / kvHeads of 2^31
+ * or more, or more workgroups than a launch has), NULL, SHAPE (workspace), HIP. */
 typedef struct sp_cache_problem {
     int dtype;                          /* SP_F32, SP_F16 or SP_BF16: of Q and O                                         */
     int heads;                          /* a multiple of the cache's kvHeads, at most 65535                              */

@@ -54,8 +54,8 @@ __device__ __forceinline__ cache_request cache_request_of(const cache_attn_args 
     if (r >= a.requests) return q;
     const int64_t s0 = cache_limit(a.start[r], 0, a.tokens), s1 = cache_limit(a.start[r + 1], 0, a.tokens), len = a.length[r];
     if (s1 <= s0) return q;
-    q.n = (uint32_t)(s1 - s0);
-    q.columns = q.n * (uint32_t)a.R;
+    q.n = (uint32_t)((int64_t)a.start[r + 1] - a.start[r]);              // rows behind the last one of Q are queries, too
+    q.columns = (uint32_t)(s1 - s0) * (uint32_t)a.R;
     const uint32_t width = cache_width(q.columns, cols);
     q.tiles = (q.columns + width - 1) / width;
     q.tokens = (uint32_t)cache_limit(len, 0, a.width * a.c.P);

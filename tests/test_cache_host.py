@@ -1,5 +1,6 @@
 """The cache held in 4 bits and rotary positions, without a GPU: the binding's structures against the header, every refusal (they come before
 anything is launched), frequencies, and the definitions that the GPU tests compare with."""
+import contextlib
 import ctypes
 import math
 import os
@@ -57,6 +58,37 @@ def cache(**more):
 BAD_CACHES = [(dict(pages=-1), SHAPE), (dict(pageTokens=0), SHAPE), (dict(pageTokens=24), SHAPE), (dict(pageTokens=-16), SHAPE), (dict(kvHeads=0), SHAPE),
               (dict(kvHeads=65536), SHAPE), (dict(headDim=0), SHAPE), (dict(headDim=257), SHAPE), (dict(pages=1 << 27), TOO_LARGE),
               (dict(pages=1 << 62), TOO_LARGE)]
+
+
+class _OnGpu3:
+    """What the entry points ask of a tensor before they make its device current."""
+    dtype, _index = torch.int32, 3
+
+    def get_device(self):
+        return 3
+
+
+@pytest.mark.parametrize("call", [
+    lambda t: sp.sp_rotary(t, t, t), lambda t: sp.sp_rotary_grad(t, t, t), lambda t: sp.sp_cache_map(t, t, t, t, t, 16, 4, 5), lambda t: sp.sp_cache_store(t, t, t, t),
+    lambda t: sp.sp_cache_load(t, t), lambda t: sp.sp_cache_attention(t, t, t, t, t)])
+def test_entry_points_make_the_tensors_device_current(call, monkeypatch):
+    """Without a GPU: torch's device functions are stood in for; whatever the call does first is done with the tensors' device current."""
+    now, seen = [0], []
+
+    @contextlib.contextmanager
+    def device(d):
+        before, now[0] = now[0], d
+        yield
+        now[0] = before
+
+    def inner(*args, **more):
+        seen.append(now[0])
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    for name in ("_rotary", "_cache_map", "_cache_store", "_cache_load", "_cache_attention"):
+        monkeypatch.setattr(B, name, inner)
+    call(_OnGpu3())
+    assert seen == [3] and now == [0]
 
 
 def test_cache_bytes():

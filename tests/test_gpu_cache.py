@@ -1,5 +1,6 @@
 """The cache held in 4 bits: pages and slots, rows into the pages and back, attention over the pages, and a serving loop of all of them, against
 the definitions in 64 bits (tests/cache_util.py, which also derives the bounds)."""
+import ctypes
 import random
 
 import pytest
@@ -8,6 +9,7 @@ import torch
 import paper_2202_04305_amd as sp
 import cache_util as U
 from gpu_util import say, DEV
+from paper_2202_04305_amd import binding as B
 
 pytestmark = pytest.mark.gpu
 
@@ -386,6 +388,38 @@ def test_layouts_and_rows_of_no_request():
             same_rows = p.run(one, start)
             want = p.wanted(Q[:1].expand(m, 4, 64), start)
             check({"O": same_rows["O"][rows]}, {"O": [t[rows] for t in want["O"]]})
+
+
+def test_rows_behind_the_last_one():
+    """A step that has fewer rows than its requests have queries: those that are there are what they are in the whole step."""
+    for n, m in (([20, 30, 5], 33), ([1, 1, 1], 2), ([200, 3, 9], 130)):
+        p, start = Pages([300, 200, 50], 2, 64, 16), starts(n)
+        Q = normal((start[-1], 4, 64), BF16, 1)
+        want = p.wanted(Q, start)
+        got = p.run(Q[:m].contiguous(), start)
+        check(got, {"O": [t[:m] for t in want["O"]], "lse": [t[:, :m] for t in want["lse"]]}, n)
+
+
+def test_without_lse_and_refused_workspaces():
+    """Through the C ABI: no lse, and a workspace that is missing, too small or not aligned, which leaves O as it was."""
+    L = sp.load_library()
+    for n in (1, 50):
+        p, start = Pages([5000], 2, 64, 64), [0, n]
+        Q, table, lengths, begin = normal((n, 8, 64), BF16, 1).to(DEV), p.table.to(DEV), ints([5000]).to(DEV), ints(start).to(DEV)
+        O = torch.full_like(Q, 7.0)
+        packed = B._PROBLEM.pack(sp.SP_BF16, 8, 1, 0.125, 1, n, Q.data_ptr(), 512, 64, table.data_ptr(), table.shape[1], table.shape[1], lengths.data_ptr(), begin.data_ptr())
+        need = ctypes.c_size_t()
+        assert L.sp_cache_attention_workspace(p.cache._ref, packed, ctypes.byref(need)) == 0 and need.value > 0
+        work = torch.empty(need.value + 256, dtype=torch.uint8, device=DEV)
+        stream = torch.cuda.current_stream().cuda_stream
+
+        def call(at, size):
+            return L.sp_cache_attention(p.cache._ref, packed, O.data_ptr(), 512, 64, None, at, size, stream)
+        assert call(None, need.value) == 1 and call(work.data_ptr(), need.value - 1) == 8 and call(work.data_ptr() + 128, need.value) == 8
+        torch.cuda.synchronize()
+        assert (O == 7).all()
+        assert call(work.data_ptr(), need.value) == 0
+        check({"O": O}, {"O": p.wanted(Q.cpu(), start, scale=0.125)["O"]})
 
 
 def test_pages_that_do_not_exist_are_left_out():
