@@ -490,6 +490,44 @@ def test_numbers_that_are_not_finite(d, dt):
             check({"x": o}, {"x": w})
 
 
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("d", [16, 33, 64, 80, 128, 250])
+def test_requests_cut_into_chunks(d, dt):
+    """A table with room for more than 1024 tokens: requests are cut, lengths around the cuts, also where a chunk is left with nothing."""
+    say("case chunks", d, dt)
+    for n in ([1, 1, 1, 1, 1, 1, 1], [1, 0, 3, 20, 70, 2, 1]):
+        start = starts(n)
+        p, Q = Pages([255, 256, 257, 300, 1030, 0, 513], 2, d, 16, 5, width=90), normal((start[-1], 6, d), dt, 3)
+        check(p.run(Q, start), p.wanted(Q, start), (d, dt, n))
+
+
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("d", [64, 128, 80])
+def test_numbers_that_are_not_finite_in_chunks(d, dt):
+    """In one chunk of several: rows that attend to it lose their result, rows that do not keep theirs; queries that are not finite lose their own rows."""
+    say("case chunks, not finite", d, dt)
+    lengths = [1500, 300, 700]
+    for n in ([1, 1, 1], [100, 40, 2]):
+        plain, start = Pages(lengths, 2, d, 16, width=100), starts(n)
+        Q = normal((start[-1], 4, d), dt, 3)
+        for name, spots in (("late", [(0, 1499), (1, 270)]), ("early", [(0, 3), (2, 600)]), ("a run", [(0, t) for t in range(500, 800)])):
+            for where in ("K", "V"):
+                def make(tokens):
+                    x = normal((tokens, 2, d), BF16, 17)
+                    for k, (r, t) in enumerate(spots):
+                        x[int(plain.table[r, t // 16]) * 16 + t % 16, k % 2, (7 * k) % d] = float("nan") if k % 3 else float("inf")
+                    return x
+                p = Pages(lengths, 2, d, 16, width=100, **{where: make})
+                check(p.run(Q, start), p.wanted(Q, start), (name, where, n))
+        Q[0, 1, 3] = float("nan")
+        got, want = plain.run(Q, start), plain.wanted(normal((start[-1], 4, d), dt, 3), start)
+        assert torch.isnan(got["O"][0, 1]).all() and torch.isnan(got["lse"][1, 0])
+        for o, w in ((got["O"], want["O"]), (got["lse"].t(), [t.t() for t in want["lse"]])):
+            o = o.cpu().clone()
+            o[0, 1] = w[0][0, 1].to(o.dtype)
+            check({"x": o}, {"x": w})
+
+
 def test_large_and_small_scores():
     """Scores of hundreds to either side, rows whose largest score comes last, a scale of zero, a negative one."""
     for n in ([1, 1], [33, 60]):
@@ -518,6 +556,25 @@ def test_scores_beyond_f32():
         got = p.run(Q, [0, n], scale=1.0)
         assert (got["O"][:, 0] == 0).all() and (got["lse"][0] == float("-inf")).all()
         assert torch.isnan(got["O"][:, 1]).all() and torch.isnan(got["lse"][1]).all()
+
+
+def test_chunks_that_weigh_nothing():
+    """Scores of minus infinity in whole chunks: what is left decides, and a row of nothing else attends to nothing."""
+    def mixed(n):
+        x = torch.zeros(n, 1, 32)
+        x[:1040] = 1e38
+        return x.to(BF16)
+    for n in (1, 40):
+        for length in (1000, 2000):
+            p = Pages([length], 1, 32, 16, K=mixed, spare=128)
+            p.table = torch.arange(128, dtype=torch.int32)[None].contiguous()
+            got = p.run(torch.full((n, 2, 32), -1e3), [0, n], scale=1.0, causal=False)
+            if length < 1040:
+                assert (got["O"] == 0).all() and (got["lse"] == float("-inf")).all()
+            else:                                        # tokens 1040 to 1999, all of one weight: 960 V of 4 bits, sums of 960 roundings to 32 bits, 3 parts of a weight
+                want = U.held(p.V)[1040:length, 0].mean(0)
+                assert (got["O"].cpu().double() - want).abs().max() < 2000 * 2.0 ** -24 * U.held(p.V).abs().max()
+                assert (got["lse"].cpu() - torch.tensor(960.0).log()).abs().max() < 1e-5          # some 20 roundings of a number below 8
 
 
 def test_the_same_bits_every_time_and_other_streams():
