@@ -34,8 +34,8 @@ struct cache_attn_args {
 // the requests: 64 at a time, of which a plan says the right ones where there are more.  The heads of one item are neighbours: workgroups go
 // to the eight XCDs in turn, so that with 8 heads (or 4, 16, ..) what one L2 holds of the pages serves all tiles of a request.
 // Chunks are as long as makes about kCacheTarget items of all work, at least kCacheLeast tokens.  Where the table has room for kCacheWhole tokens
-// or fewer, nothing is cut and one launch does: 4 requests of up to 1000 tokens 12.0 us instead of 15 to 17 with chunks of 256 or 512 and a join, 2 prompts of
-// 200 behind 1000 33 instead of 41; from there on (8 requests of up to 2048) chunks of 256 and 512 take 16 us, of 1024 17.
+// or fewer, nothing is cut and one launch does: 4 requests of up to 1000 tokens (f32) 12.0 us instead of 15 to 17 with chunks of 256 or 512 and a join, 2 prompts of
+// 200 behind 1000 33 instead of 41; beyond, chunks are worth their join: one request of 2000 15.9 us with chunks of 256 (512: 17.5, 1024: 17.0), of 8192 14.9 (16.6, 17.3).
 constexpr int kCacheTarget = 512, kCacheLeast = 256, kCacheWhole = 1024;
 
 struct cache_request { uint32_t n, columns, tiles, tokens, row0; int32_t last; uint32_t r; };      // row0: its first row; last: position of its last query, -1 or more; r: its number
