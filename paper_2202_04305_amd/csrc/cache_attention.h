@@ -23,7 +23,7 @@ struct cache_attn_args {
     int vec;                             // rows of Q and O are aligned to 8 numbers
     spmi_divisor32 records;              // of a page: P / 16
     float *part;                         // workspace: [slot][head of the cache][column][32 nb] sums
-    float2 *stat;                        //            [slot][head of the cache][column]: running maximum (in units of log 2) and total
+    float2 *stat;                        //            [slot][head of the cache][column]: running maximum (in units of log 2; minus infinity: no weight) and total
     uint32_t slots;                      // slots there is room for
     uint32_t *plan;                      // see cache_plan_kernel; null: workgroups do without
 };
@@ -614,6 +614,7 @@ struct cache_column {
 #pragma unroll
             for (int j = 0; j < 4; ++j) if (d + j < a.c.D) out[d + j] = (T)(x[j] * f);
     }
+    // top: minus infinity where nothing weighs, so that the join's maximum is that of the chunks that do
     __device__ __forceinline__ void total(float top, float sum) const
     {
         if (part) *stat = {top, sum};
@@ -713,7 +714,7 @@ __device__ __forceinline__ void cache_few(const cache_attn_args &a, const cache_
                 const int d = 4 * (q + 16 * j);
                 if (d < 32 * NB) out.numbers(late, d, y[j], total);
             }
-            if (q == 0) out.total(top == -INFINITY ? 0.f : top, total);
+            if (q == 0) out.total(top, total);
         }
 #pragma unroll 1
         for (int k = 0; k < 4; ++k)
@@ -883,7 +884,7 @@ __global__ __launch_bounds__(256, cache_many_waves<T>(NB)) void cache_many_kerne
             const cache_column<T, NB> out(late, it, g, first + col, cols);
 #pragma unroll
             for (int b = 0; b < 2 * NB; ++b) out.numbers(late, 16 * b + 4 * (lane >> 4), x.o[k][b], total);
-            if (lane < 16) out.total(x.mu[k], total);
+            if (lane < 16) out.total(x.top[k], total);
         }
     }
 #pragma unroll 1

@@ -577,6 +577,40 @@ def test_chunks_that_weigh_nothing():
                 assert (got["lse"].cpu() - torch.tensor(960.0).log()).abs().max() < 1e-5          # some 20 roundings of a number below 8
 
 
+# Requests cut into 5 to 25 chunks, in some of which a column has no weight: lengths, queries, heads, heads of the cache, and pages of the first request's
+# table that do not exist.
+WEIGHTLESS = {
+    "a prompt longer than a chunk": ([2000, 30], [2000, 30], 2, 1, ()),
+    "a prompt behind many chunks": ([6000, 50], [300, 50], 2, 1, ()),
+    "drafted tokens across a cut": ([1026, 1026, 40], [4, 2, 1], 4, 2, ()),
+    "drafted tokens of many heads": ([1026, 1030, 40], [4, 10, 1], 8, 1, ()),
+    "drafted tokens behind many chunks": ([6146, 40], [4, 1], 4, 2, ()),
+    "missing pages": ([2000, 1300], [1, 1], 4, 2, range(32, 64)),
+    "the first pages missing": ([2000, 1300], [1, 1], 4, 2, range(0, 16)),
+    "missing pages of many chunks": ([6000, 1300], [1, 1], 4, 2, range(48, 80)),
+    "missing pages of a prompt": ([2000, 1300], [40, 70], 4, 1, range(32, 64)),
+}
+
+
+@pytest.mark.parametrize("name", WEIGHTLESS)
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+def test_low_scores_beside_chunks_without_weight(name, dt):
+    """Scores of -90 to -1000 in the chunks that a row attends to, nothing in the others: those have no say in the row's maximum."""
+    say("case low scores", name, dt)
+    lengths, n, H, G, gone = WEIGHTLESS[name]
+
+    def positive(count):
+        return 1 + normal((count, G, 64), BF16, 31).abs()
+    p, start = Pages(lengths, G, 64, 16, 3, width=70, K=positive), starts(n)
+    p.table[0, list(gone)] = -1
+    Q = -(1 + normal((start[-1], H, 64), F32, 5).abs()) * torch.linspace(1.3, 8, H)[None, :, None]
+    Q = Q.to(dt)
+    want = p.wanted(Q, start, scale=0.5)
+    lse = want["lse"][0]
+    assert (lse < -87).all() and (lse > -1000).all()     # the case is what it says
+    check(p.run(Q, start, scale=0.5), want, (name, dt))
+
+
 def test_the_same_bits_every_time_and_other_streams():
     for n in ([1] * 6, [1, 30, 1, 200, 64, 3]):
         p = Pages([3000, 30, 4000, 200, 500, 1000], 2, 128, 64)
