@@ -595,17 +595,20 @@ class Cache:
     """Keys and values in 4 bits: the pages' memory (`data`) and their description."""
 
     def __init__(self, data, spec):
+        self._ref, self._index = ctypes.byref(spec), _gpu_of(data)       # tensors of the calls have to be on that GPU
         self.data, self._spec, self.device = data, spec, data.device
         self.pages, self.page_tokens, self.kv_heads, self.head_dim = spec.pages, spec.pageTokens, spec.kvHeads, spec.headDim
-        self._ref, self._index = ctypes.byref(spec), data.get_device()
         self._workspaces = {}            # bytes of workspace of the attention problems met so far
 
 
 def sp_cache(pages, page_tokens, kv_heads, head_dim, device=None):
-    """A cache of `pages` pages of page_tokens tokens (a multiple of 16), filled with zeros, on `device` (the current GPU unless given)."""
+    """A cache of `pages` pages of page_tokens tokens (a multiple of 16), filled with zeros, on `device`, a GPU (the current one unless given)."""
+    device = torch.device("cuda" if device is None else device)
+    if device.type != "cuda":
+        raise ValueError("a cache on a GPU, not on %s" % device)
     spec, size = SpCache(None, int(pages), int(page_tokens), int(kv_heads), int(head_dim)), ctypes.c_size_t()
     _check(load_library().sp_cache_bytes(ctypes.byref(spec), ctypes.byref(size)), "in sp_cache")
-    data = torch.zeros(max(1, size.value), dtype=torch.uint8, device="cuda" if device is None else device)
+    data = torch.zeros(max(1, size.value), dtype=torch.uint8, device=device)
     spec.data = data.data_ptr()
     return Cache(data, spec)
 

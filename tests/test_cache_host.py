@@ -103,6 +103,15 @@ def test_cache_bytes():
     assert L.sp_cache_bytes(None, ref(size)) == NULL and L.sp_cache_bytes(ref(cache()), None) == NULL
 
 
+@pytest.mark.parametrize("device", ["cpu", torch.device("cpu"), "meta"])
+def test_a_cache_is_on_a_gpu(device):
+    """Kernels would be given the address of memory that they cannot read: no such cache is made, nor any of its tensors looked at."""
+    with pytest.raises(ValueError):
+        sp.sp_cache(4, 16, 2, 64, device=device)
+    with pytest.raises(ValueError):
+        sp.Cache(torch.zeros(1 << 16, dtype=torch.uint8, device=device), cache())
+
+
 def rotary(**more):
     return B.SpRotaryProblem(**{**dict(dtype=3, headDim=64, rotDim=32, interleaved=0, scale=1.0, tokens=5, position=SOME, frequency=SOME, heads=4, kvHeads=2,
                                        Q=SOME, ldq=256, hdq=64, K=SOME, ldk=128, hdk=64, Qout=SOME, ldqo=256, hdqo=64, Kout=SOME, ldko=128, hdko=64), **more})
