@@ -343,7 +343,8 @@ sp_status sp_cache_load(const sp_cache *c, int dtype, int64_t tokens, const int3
  *   lse  DEVICE, heads x tokens, f32; may be NULL.
  *   workspace  as for sp_attention: sp_cache_attention_workspace bytes, aligned to 256, one for each of the calls that may overlap.
  * Enqueues on `stream`; neither allocates nor synchronises, reads lengths, rows and pages on the GPU (a recorded graph serves other ones), and
- * gives the same bits on every call.  The numbers of the cache are exact in the products; Q is, too (in as many parts of bf16 as its type
+ * gives the same bits on every call.  Sums are in f32.  Rows whose sums are not finite in the end are made again token by token, which takes longer;
+ * means of values that the cache holds are finite, however large these are.  The numbers of the cache are exact in the products; Q is, too (in as many parts of bf16 as its type
  * has room for); weights are rounded to Q's type before their product.  Errors, in this order: NULL (c, p), DTYPE, SHAPE, UNSUPPORTED (causal neither 0
  * nor 1), TOO_LARGE (pages * pageTokens, width * pageTokens, requests, or tokens * heads / kvHeads of 2^31
  * or more, or more workgroups than a launch has), NULL, SHAPE (workspace), HIP. */

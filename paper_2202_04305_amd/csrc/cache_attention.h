@@ -223,13 +223,14 @@ __device__ __forceinline__ float cache_wave_sum(float v)
     return v;
 }
 
-// top (running maximum, in units of log 2), total and acc = sum of 2^(s - top) V over the tokens [t0, t1) of request r, for one row and head; a
-// wave, lanes across the head's numbers.  Every token is looked at alone, so that nothing that the row does not attend to can reach it: the
-// tiles fall back on it where a sum is not finite, as a token that other columns attend to is multiplied with zero there, which
-// infinities and NaN survive.
+// For the tokens [t0, t1) of request r, one row and head: top, the maximum of the scores s in units of log 2, and total and acc, the sums of
+// 2^(s - top - far) and of that times V; a wave, lanes across the head's numbers.  Every token is looked at alone, so that nothing that the row does
+// not attend to can reach it: the tiles fall back on it where a sum is not finite, as a token that other columns attend to is multiplied
+// with zero there, which infinities and NaN survive, or as sums of large values leave the range of f32.  Here they do not: a weight is half at
+// most (far >= 1), and the sums are halved whenever the total gets past a half, so that acc stays below the largest value.
 template <typename T>
 __device__ __forceinline__ void cache_row(const cache_attn_args &a, int64_t r, int64_t i, int h, uint32_t t0, uint32_t t1, int lane,
-                                       float &top, float &total, float (&acc)[kCachePer])
+                                       float &top, int &far, float &total, float (&acc)[kCachePer])
 {
     const int g = h / a.R, D = a.c.D;
     const T *row = (const T *)a.Q + i * a.ldq + h * a.hdq;
@@ -237,7 +238,7 @@ __device__ __forceinline__ void cache_row(const cache_attn_args &a, int64_t r, i
     float q[kCachePer];
 #pragma unroll
     for (int k = 0; k < kCachePer; ++k) { q[k] = lane + 64 * k < D ? (float)row[lane + 64 * k] : 0.f; acc[k] = 0; }
-    top = -INFINITY; total = 0;
+    top = -INFINITY; total = 0; far = 1;
 #pragma unroll 1
     for (uint32_t t = t0; t < t1; ++t) {
         const int64_t page = a.table[r * a.ldt + t / (uint32_t)a.c.P];
@@ -250,11 +251,16 @@ __device__ __forceinline__ void cache_row(const cache_attn_args &a, int64_t r, i
         s = cache_wave_sum(s) * step;
         if (s == -INFINITY) continue;                    // weight 0
         const float up = s > top ? s : top;              // not a number: stays with the old maximum, the weight carries it
-        const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - up), w = __builtin_amdgcn_exp2f(s - (up == -INFINITY ? 0.f : up));
+        const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - up), w = ldexpf(__builtin_amdgcn_exp2f(s - (up == -INFINITY ? 0.f : up)), -far);
         top = up;
         total = total * old + w;
 #pragma unroll
         for (int k = 0; k < kCachePer; ++k) if (lane + 64 * k < D) acc[k] = acc[k] * old + w * cache_value(a.c, rec, u % kCacheTile, lane + 64 * k);
+        if (total > 0.5f) {
+            total *= 0.5f; ++far;
+#pragma unroll
+            for (int k = 0; k < kCachePer; ++k) acc[k] *= 0.5f;
+        }
     }
 }
 
@@ -629,7 +635,8 @@ __device__ __forceinline__ void cache_again(const cache_attn_args &a, const cach
     const uint32_t i = col / (uint32_t)a.R;
     const cache_span s = cache_span_of(a, it, col, 1);
     float top, total, acc[kCachePer];
-    cache_row<T>(a, it.r, it.row0 + i, g * a.R + col % (uint32_t)a.R, from, to < s.to ? to : s.to, lane, top, total, acc);
+    int far;
+    cache_row<T>(a, it.r, it.row0 + i, g * a.R + col % (uint32_t)a.R, from, to < s.to ? to : s.to, lane, top, far, total, acc);
     const cache_column<T, NB> c(a, it, g, col, cols);
 #pragma unroll
     for (int k = 0; k < kCachePer; ++k) {
@@ -637,7 +644,8 @@ __device__ __forceinline__ void cache_again(const cache_attn_args &a, const cach
         if (c.part) { if (d < 32 * NB) c.part[d] = d < a.c.D ? acc[k] : 0.f; }
         else if (d < a.c.D) c.out[d] = (T)(total == 0 ? 0.f : acc[k] / total);
     }
-    if (lane == 0) c.total(top, total);
+    // a part's sums go with its total as they are; what was taken off them counts as maximum
+    if (lane == 0) c.total(c.part ? top + (float)far : top, c.part ? total : ldexpf(total, far));
 }
 
 // The kernel's arguments (its first ones), to be loaded where they are used: kept from the kernel's beginning on they would not fit the scalar registers.
@@ -921,6 +929,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int 
 #pragma unroll
             for (int d = 8; d >= 1; d >>= 1) total += __shfl_xor(total, d, 64);
             total = __shfl(total, 0, 64); top = __shfl(top, 0, 64);
+            const float share = total == 0 ? 0.f : f / total;            // before the sums, which are no larger than the values then
             for (uint32_t k0 = 0; k0 < it.chunks; k0 += 4) {             // four at a time; behind the last one that one again, without weight
                 float x[4][per];
 #pragma unroll
@@ -931,7 +940,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int 
                 }
 #pragma unroll
                 for (uint32_t k = 0; k < 4; ++k) {
-                    const float fk = __shfl(f, (int)(k0 + k), 64);
+                    const float fk = __shfl(share, (int)(k0 + k), 64);
 #pragma unroll
                     for (int j = 0; j < per; ++j) acc[j] += x[k][j] * fk;
                 }
@@ -939,7 +948,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int 
             const uint32_t i = col / (uint32_t)a.R, h = g * a.R + col % (uint32_t)a.R;
             T *out = (T *)a.O + (it.row0 + i) * a.ldo + (int64_t)h * a.hdo;
 #pragma unroll
-            for (int j = 0; j < per; ++j) if (lane + 64 * j < a.c.D) out[lane + 64 * j] = (T)(total == 0 ? 0.f : acc[j] / total);
+            for (int j = 0; j < per; ++j) if (lane + 64 * j < a.c.D) out[lane + 64 * j] = (T)acc[j];
             if (a.lse && lane == 0) a.lse[(int64_t)h * a.tokens + it.row0 + i] = total == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kCacheLn2;
         }
         return;
@@ -964,12 +973,13 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int 
         if (lane == 0) stats[1][w] = total;
         __syncthreads();
         total = (stats[1][0] + stats[1][1]) + (stats[1][2] + stats[1][3]);
+        const float inverse = total == 0 ? 0.f : 1 / total;              // before the sums, as above
         float acc[per] = {};
 #pragma unroll 8
         for (uint32_t k = w; k < it.chunks; k += 4) {
             const float *part = a.part + (base + k * step) * pad;
 #pragma unroll
-            for (int j = 0; j < per; ++j) if (pad % 64 == 0 || lane + 64 * j < pad) acc[j] += part[lane + 64 * j] * factor[k];
+            for (int j = 0; j < per; ++j) if (pad % 64 == 0 || lane + 64 * j < pad) acc[j] += part[lane + 64 * j] * (factor[k] * inverse);
         }
 #pragma unroll
         for (int j = 0; j < per; ++j) if (pad % 64 == 0 || lane + 64 * j < pad) sums[w][lane + 64 * j] = acc[j];
@@ -978,7 +988,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attn_args a, int 
         T *out = (T *)a.O + (it.row0 + i) * a.ldo + (int64_t)h * a.hdo;
         if ((int)threadIdx.x < a.c.D) {
             const int d = threadIdx.x;
-            out[d] = (T)(total == 0 ? 0.f : ((sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d])) / total);
+            out[d] = (T)((sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]));
         }
         if (a.lse && threadIdx.x == 0) a.lse[(int64_t)h * a.tokens + it.row0 + i] = total == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kCacheLn2;
         __syncthreads();

@@ -611,6 +611,32 @@ def test_low_scores_beside_chunks_without_weight(name, dt):
     check(p.run(Q, start, scale=0.5), want, (name, dt))
 
 
+@pytest.mark.parametrize("lengths,n", [([70, 1500, 300], [1, 1, 1]), ([70, 300], [1, 1]), ([70, 1500], [40, 70]), ([70, 300], [40, 70]), ([6000], [1]), ([700, 30], [300, 6])])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_the_largest_values(lengths, n, dt):
+    """Means of values close to the largest that a cache holds are finite, and right, whatever the sums would be."""
+    say("case largest values", lengths, n, dt)
+
+    def alike(count):
+        return torch.full((count, 2, 64), 2.0 ** 127).to(BF16)
+
+    def mixed(count):
+        return (normal((count, 2, 64), F32, 3).clamp(-7, 7) * 2.0 ** 125).to(BF16)
+
+    def sixes(count):
+        x = torch.full((count, 2, 64), 6 * 2.0 ** 125)
+        x[:, 1, ::2] = -3e-20
+        return x.to(BF16)
+    start = starts(n)
+    Q = normal((start[-1], 4, 64), dt, 9)
+    for name, V in (("alike", alike), ("mixed", mixed), ("sixes", sixes)):
+        for scale in (0.0, 0.125, 1.0):
+            p = Pages(lengths, 2, 64, 16, 1, V=V)
+            got, want = p.run(Q, start, scale=scale), p.wanted(Q, start, scale=scale)
+            assert torch.isfinite(got["O"]).all(), (name, scale)
+            check(got, want, (name, scale))
+
+
 def test_the_same_bits_every_time_and_other_streams():
     for n in ([1] * 6, [1, 30, 1, 200, 64, 3]):
         p = Pages([3000, 30, 4000, 200, 500, 1000], 2, 128, 64)
