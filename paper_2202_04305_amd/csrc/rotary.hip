@@ -42,7 +42,8 @@ template <typename T, int V, int W, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotary_kernel(rotary_args a)
 {
     typedef T row __attribute__((ext_vector_type(V)));
-    typedef T row2 __attribute__((ext_vector_type(2 * V)));
+    typedef T row2 __attribute__((ext_vector_type(2 * V), aligned(V == 1 ? sizeof(T) : 2 * V * sizeof(T))));
+    static_assert(V > 1 || alignof(row2) == alignof(T), "V = 1 takes strides and addresses of any number of elements");
     typedef T rest __attribute__((ext_vector_type(W)));
     __shared__ float2 turn[kRotaryPairs];
     const int turning = a.half / V;

@@ -99,6 +99,36 @@ def test_layouts(interleaved, dt):
     close(sp.sp_rotary_grad(at.to(DEV), f.to(DEV), same, **turn), *rotated(Q[:1].expand(40, 5, 48), at, f, interleaved, back=True))
 
 
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_pairs_at_any_number_of_elements(interleaved, dt):
+    """Heads and rows an odd number of elements apart, and addresses moved by one: pairs begin anywhere; in place too."""
+    say("case rotary, odd strides", interleaved, dt)
+    at, f = places(29, 3000), sp.sp_rotary_frequencies(22, device="cpu")
+    for first in (0, 1):
+        whole = torch.full((first + 29 * 5 * 33 + 4,), 7.0, dtype=dt, device=DEV)
+        view, Q = whole[first:first + 29 * 5 * 33].view(29, 5, 33), rows(29, 5, 33, dt, first)
+        for grad, call in ((False, sp.sp_rotary), (True, sp.sp_rotary_grad)):
+            view.copy_(Q)
+            close(call(at.to(DEV), f.to(DEV), view, interleaved=interleaved), *rotated(Q, at, f, interleaved, back=grad))
+            call(at.to(DEV), f.to(DEV), view, None, interleaved, 1.0, view)
+            close(view, *rotated(Q, at, f, interleaved, back=grad))
+            assert (whole[:first] == 7).all() and (whole[first + 29 * 5 * 33:] == 7).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rot", [(2048, 2048), (2050, 2050), (4100, 4096), (2307, 2306)])
+def test_heads_of_more_pairs_than_are_kept(d, rot, interleaved, dt):
+    """1024 pairs have room in the LDS; of more every item makes its own cosines.  Both sides of the border, both pairings, the gradient."""
+    say("case rotary, many pairs", d, rot, interleaved, dt)
+    Q, K, at, f = rows(37, 2, d, dt), rows(37, 1, d, dt, 2), places(37, 5000), sp.sp_rotary_frequencies(rot, device="cpu")
+    for grad, call in ((False, sp.sp_rotary), (True, sp.sp_rotary_grad)):
+        q, k = call(at.to(DEV), f.to(DEV), Q.to(DEV), K.to(DEV), interleaved=interleaved, scale=0.75)
+        close(q, *rotated(Q, at, f, interleaved, 0.75, back=grad), "Q")
+        close(k, *rotated(K, at, f, interleaved, 0.75, back=grad), "K")
+
+
 def test_gradient_against_differentiation():
     """<dY, rotary(X)> differentiated by torch in 64 bits, and by differences of the kernel's own results (which are linear in X)."""
     for interleaved in (False, True):
