@@ -51,6 +51,11 @@ static inline sp_status cache_check(const sp_cache *c, cache_view *v)
 // Is the memory of a cache with pages there, where it may be?
 static inline bool cache_has_memory(const cache_view &v) { return v.pages == 0 || v.data; }
 
+// Eight numbers of a row, which rows aligned to 16 bytes are read and written in.
+template <typename T> struct cache_eight_of { typedef T type __attribute__((ext_vector_type(8), aligned(16))); };
+template <typename T> using cache_row8 = typename cache_eight_of<T>::type;
+static_assert(alignof(cache_row8<float>) == 16, "");
+
 typedef __bf16 cache_bf16;
 typedef _Float16 cache_f16;
 

@@ -158,7 +158,6 @@ __device__ __forceinline__ int cache_exponent(float top)
 constexpr int kStoreTokens = 32;         // of a workgroup, which takes one head of them
 
 // Eight numbers of a row, zeros behind its end.
-template <typename T> using cache_row8 = T __attribute__((ext_vector_type(8)));
 template <typename T>
 __device__ __forceinline__ cache_row8<T> load8(const T *row, int d0, int D, bool vec)
 {
@@ -270,11 +269,10 @@ __device__ __forceinline__ void cache_eight(uint32_t word, float scale, uint32_t
 template <typename T>
 __device__ __forceinline__ void store8(T *row, int d0, int D, bool vec, const uint32_t (&x)[4])
 {
-    typedef T row8 __attribute__((ext_vector_type(8)));
-    row8 v;
+    cache_row8<T> v;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (T)__uint_as_float(j % 2 ? x[j / 2] & 0xffff0000u : x[j / 2] << 16);
-    if (vec) { if (d0 < D) *(row8 *)(row + d0) = v; }
+    if (vec) { if (d0 < D) *(cache_row8<T> *)(row + d0) = v; }
     else
 #pragma unroll
         for (int j = 0; j < 8; ++j) if (d0 + j < D) row[d0 + j] = v[j];

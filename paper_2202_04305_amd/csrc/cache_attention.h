@@ -390,9 +390,8 @@ struct cache_wave {
                 const int d0 = 32 * s + 8 * (lane >> 4);
                 float x[8];
                 if (a.vec) {
-                    typedef T row8 __attribute__((ext_vector_type(8)));
-                    row8 v = {};
-                    if (there && d0 < D) v = *(const row8 *)(row + d0);
+                    cache_row8<T> v = {};
+                    if (there && d0 < D) v = *(const cache_row8<T> *)(row + d0);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
                 } else {

@@ -390,6 +390,32 @@ def test_layouts_and_rows_of_no_request():
             check({"O": same_rows["O"][rows]}, {"O": [t[rows] for t in want["O"]]})
 
 
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+@pytest.mark.parametrize("first", [0, 1, 4, 8])
+def test_addresses_moved_by_a_few_numbers(first, dt):
+    """Rows of Q, K, V and O at 4, 8, 16 bytes and more from a multiple of 32, heads of 40 next to each other."""
+    say("case moved", first, dt)
+
+    def moved(x):
+        whole = torch.full((first + x.numel() + 8,), 7.0, dtype=x.dtype, device=DEV)
+        view = whole[first:first + x.numel()].view(x.shape)
+        view.copy_(x)
+        return whole, view
+    p, n = Pages([70, 33, 200], 2, 40, 16), [1, 33, 5]
+    slots = torch.arange(p.pages * 16, dtype=torch.int32, device=DEV)
+    K, V = (moved(x.to(dt))[1] for x in (p.K, p.V))
+    sp.sp_cache_store(p.cache, K, V, slots)
+    (kw, k), (vw, v) = (moved(torch.zeros(p.K.shape, dtype=dt)) for _ in range(2))
+    sp.sp_cache_load(p.cache, slots, dt, K=k, V=v)
+    p.K, p.V = p.K.to(dt), p.V.to(dt)
+    assert same(k, U.held(p.K), dt) and same(v, U.held(p.V), dt)
+    Q = normal((sum(n), 4, 40), dt, 3)
+    whole, O = moved(torch.zeros_like(Q))
+    check(p.run(moved(Q)[1], starts(n), O=O), p.wanted(Q, starts(n)))
+    for w in (kw, vw, whole):
+        assert (w[:first] == 7).all() and (w[-8:] == 7).all()
+
+
 def test_rows_behind_the_last_one():
     """A step that has fewer rows than its requests have queries: those that are there are what they are in the whole step."""
     for n, m in (([20, 30, 5], 33), ([1, 1, 1], 2), ([200, 3, 9], 130)):
