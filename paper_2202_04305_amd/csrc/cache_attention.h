@@ -82,16 +82,23 @@ __device__ __forceinline__ V cache_wave_total(V v)
 
 // Tokens of a chunk; work = sum over the requests of tiles * tokens, of which T items of a head get equal shares.  Chunks are no shorter than that,
 // so those of requests that have several (less than 2 tokens / length) are fewer than 2 T.
-__device__ __forceinline__ uint32_t cache_share(const cache_attn_args &a) { return ((uint32_t)kCacheTarget + a.c.G - 1) / (uint32_t)a.c.G; }
-__device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a, uint64_t work)
+constexpr uint32_t kCacheUncut = 1u << 31;           // no request has as many
+__host__ __device__ __forceinline__ uint32_t cache_share(const cache_attn_args &a) { return ((uint32_t)kCacheTarget + a.c.G - 1) / (uint32_t)a.c.G; }
+__host__ __device__ __forceinline__ uint32_t cache_chunk_tokens(const cache_attn_args &a, uint64_t work)
 {
     const uint64_t T = cache_share(a), c = (work + T - 1) / T;
-    return c < kCacheLeast ? kCacheLeast : c > 0x7fffff00u ? 0x7fffff00u : ((uint32_t)c + 127) & ~127u;
+    return c < kCacheLeast ? kCacheLeast : c > kCacheUncut ? kCacheUncut : ((uint32_t)c + 127) & ~127u;
+}
+// `times` quarters longer
+__host__ __device__ __forceinline__ uint32_t cache_grown(uint32_t length, int times)
+{
+    const uint64_t c = length + (uint64_t)((length / 4 + 63) & ~63u) * times;
+    return c > kCacheUncut ? kCacheUncut : (uint32_t)c;
 }
 static inline int64_t cache_slots(int G) { return 2 * ceil_div(kCacheTarget, G); }
 
 struct cache_counts { uint32_t chunks, items, slots, joins; };           // of a request; joins: tiles with more than one chunk
-__device__ __forceinline__ cache_counts cache_counts_of(const cache_request &q, uint32_t length)
+__host__ __device__ __forceinline__ cache_counts cache_counts_of(const cache_request &q, uint32_t length)
 {
     const uint32_t chunks = q.tokens <= length ? 1 : (q.tokens + length - 1) / length, items = q.tiles * chunks;
     return {chunks, items, chunks > 1 ? items : 0, chunks > 1 ? q.tiles : 0};
@@ -108,7 +115,7 @@ __global__ __launch_bounds__(1024) static void cache_plan_kernel(cache_attn_args
     __shared__ uint32_t counts[16];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const uint32_t blocks = (uint32_t)((a.requests + 63) / 64);
-    uint32_t length = 0x7fffff00u;
+    uint32_t length = kCacheUncut;
     if (a.slots) {
         uint64_t work = 0;
         for (int64_t r = threadIdx.x; r < a.requests; r += blockDim.x) {
@@ -122,17 +129,16 @@ __global__ __launch_bounds__(1024) static void cache_plan_kernel(cache_attn_args
         for (int k = 0; k < waves; ++k) work += sums[k];
         length = cache_chunk_tokens(a, work);
         if (cols > 16) {
-            const uint32_t more = (length / 4 + 63) & ~63u;
             for (int tries = 0; tries < 5; ++tries) {
                 uint32_t items = 0;
-                for (int64_t r = threadIdx.x; r < a.requests; r += blockDim.x) items += cache_counts_of(cache_request_of(a, r, cols), length + more * tries).items;
+                for (int64_t r = threadIdx.x; r < a.requests; r += blockDim.x) items += cache_counts_of(cache_request_of(a, r, cols), cache_grown(length, tries)).items;
                 items = cache_wave_total(items);
                 __syncthreads();
                 if (lane == 0) counts[w] = items;
                 __syncthreads();
                 items = 0;
                 for (int k = 0; k < waves; ++k) items += counts[k];
-                if (items <= cache_share(a)) { length += more * tries; break; }
+                if (items <= cache_share(a)) { length = cache_grown(length, tries); break; }
                 if (tries == 0 && items > 2 * cache_share(a)) break;      // tiles enough as they are
             }
         }
@@ -171,7 +177,7 @@ __device__ __forceinline__ void cache_longest_first(cache_request *q, int lane)
 __device__ __forceinline__ bool cache_find(const cache_attn_args &a, uint32_t cols, uint32_t index, bool joined, int lane, cache_item *item)
 {
     cache_request q;
-    uint32_t length = 0x7fffff00u, items = 0, slots = 0;
+    uint32_t length = kCacheUncut, items = 0, slots = 0;
     if (!a.plan) {
         q = cache_request_of(a, lane, cols);
         if (a.slots) length = cache_chunk_tokens(a, cache_wave_total((uint64_t)q.tiles * q.tokens));

@@ -285,3 +285,54 @@ def test_no_kernel_of_the_cache_loses_what_it_keeps_aside(tmp_path):
         kernels += sum(bool(re.match(r"[0-9a-f]+ <\S*cache_(few|many|join)_kernel", l)) for l in asm)
         assert lost_registers(asm) == {}
     assert kernels == 3 * 8 * 3, kernels
+
+
+CHUNKS = r"""
+#include "cache_attention.h"
+#include <stdio.h>
+#include <stdlib.h>
+// argv: heads of the cache, quarters of growth, then tiles and tokens of requests.  Prints the chunks' length and every request's counts.
+int main(int argc, char **argv)
+{
+    cache_attn_args a = {};
+    a.c.G = atoi(argv[1]);
+    uint64_t work = 0;
+    for (int k = 3; k < argc; k += 2) work += strtoull(argv[k], 0, 10) * strtoull(argv[k + 1], 0, 10);
+    const uint32_t length = cache_grown(cache_chunk_tokens(a, work), atoi(argv[2]));
+    printf("%u %lld\n", length, (long long)cache_slots(a.c.G));
+    for (int k = 3; k < argc; k += 2) {
+        cache_request q = {};
+        q.tiles = (uint32_t)strtoul(argv[k], 0, 10); q.tokens = (uint32_t)strtoul(argv[k + 1], 0, 10);
+        const cache_counts c = cache_counts_of(q, length);
+        printf("%u %u %u %u\n", c.chunks, c.items, c.slots, c.joins);
+    }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def chunks(tmp_path_factory):
+    """The attention's own arithmetic of chunks, as a program of the host."""
+    d = tmp_path_factory.mktemp("chunks")
+    (d / "chunks.hip").write_text(CHUNKS)
+    subprocess.check_call(["hipcc", "--offload-arch=gfx950", "-std=c++17", "-O1", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+                           "-I", os.path.join(ROOT, "include"), "-I", os.path.join(os.path.dirname(build.LIB), "csrc"), "-o", str(d / "chunks"), str(d / "chunks.hip")],
+                          stderr=subprocess.DEVNULL)
+
+    def run(*numbers):
+        out = subprocess.run([str(d / "chunks")] + [str(x) for x in numbers], stdout=subprocess.PIPE, text=True, check=True).stdout.split()
+        return int(out[0]), int(out[1]), [tuple(map(int, out[k:k + 4])) for k in range(2, len(out), 4)]
+    return run
+
+
+@pytest.mark.parametrize("requests", [[(1, 2000)], [(128, 2 ** 31 - 1)], [(1, 2 ** 31 - 1)] * 3, [(5000, 2 ** 31 - 1), (1, 1)], [(3, 2 ** 31 - 256), (70, 2 ** 31 - 255)],
+                                      [(300, 8000), (1, 1 << 20), (1, 0), (7, 300)], [(1 << 20, 2 ** 31 - 1)], [(40, 2 ** 31 - 1)] * 2])
+@pytest.mark.parametrize("G", [1, 8, 100, 512, 65535])
+def test_chunks_have_room(requests, G, chunks):
+    """The workspace has a slot for every chunk of a request that is cut, and chunks cover their request, up to the longest that there may be."""
+    for times in range(5):
+        length, room, counts = chunks(G, times, *[x for r in requests for x in r])
+        assert 256 <= length <= 1 << 31 and length % 64 == 0
+        assert sum(c[2] for c in counts) < room or not any(c[2] for c in counts), (times, length, counts)
+        for (tiles, tokens), (n, items, slots, joins) in zip(requests, counts):
+            assert n == max(1, -(-tokens // length)) and items == tiles * n and (slots, joins) == ((items, tiles) if n > 1 else (0, 0))
