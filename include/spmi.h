@@ -271,7 +271,8 @@ typedef struct sp_rotary_problem {
 /* The frequencies base^(-2k / rotDim) for k < rotDim / 2 (HOST, 64 bits), for contexts longer than a model was trained on made smaller: by
  * `factor` where trained = 0; otherwise with n = trained * frequency / (2 pi) turns in the trained length and c = (n - low) / (high - low) cut
  * to [0, 1], (1 - c) / factor + c times as large: fast pairs stay, slow ones are stretched.  Errors: NULL, SHAPE (rotDim odd or negative;
- * base or factor not positive and finite; trained negative; high <= low where trained > 0). */
+ * base or factor not positive and finite; trained negative; high <= low where trained > 0; a
+ * frequency that is not finite). */
 sp_status sp_rotary_frequencies(int rotDim, double base, double factor, int64_t trained, double low, double high, double *frequency /* HOST */);
 
 /* Turns Q and K; sp_rotary_grad: the gradients with respect to Q and K, given those with respect to the results in the places of Q and K (the

@@ -194,6 +194,7 @@ extern "C" sp_status sp_rotary_frequencies(int rotDim, double base, double facto
             keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
         }
         frequency[k] = (1 - keep) * f / factor + keep * f;
+        if (!(frequency[k] - frequency[k] == 0)) return SP_ERR_SHAPE;
     }
     return SP_OK;
 }

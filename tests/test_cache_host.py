@@ -157,6 +157,17 @@ def test_frequencies():
     assert L.sp_rotary_frequencies(16, 1e4, 1.0, 0, 5.0, 5.0, out) == 0          # the borders play no part then
 
 
+def test_frequencies_are_finite():
+    """Borders, bases and factors that would give NaN or infinity are refused, those that give numbers are not."""
+    L, out = sp.load_library(), (ctypes.c_double * 8)()
+    for args in ((16, 1e4, 1.0, 9, -math.inf, 32.0), (16, 1e4, 1.0, 9, -math.inf, math.inf), (16, 5e-324, 1.0, 0, 1.0, 32.0), (16, 1e4, 1e-310, 0, 1.0, 32.0)):
+        assert L.sp_rotary_frequencies(*args, out) == SHAPE, args
+        with pytest.raises(sp.SpError):
+            sp.sp_rotary_frequencies(*args, device="cpu")
+    for args in ((16, 1e4, 2.0, 9, 1.0, math.inf), (16, 1e-300, 1.0, 0, 1.0, 32.0), (16, 1e4, 1e308, 0, -math.inf, 32.0)):
+        assert L.sp_rotary_frequencies(*args, out) == 0 and all(math.isfinite(x) for x in out), args
+
+
 def step(**more):
     return B.SpCacheStep(**{**dict(requests=3, tokens=5, pages=10, pageTokens=16, length=SOME, added=SOME, freePages=SOME, freeCount=4, taken=SOME, table=SOME, ldt=4,
                                    width=4, lengthOut=SOME, start=SOME, position=SOME, slot=SOME, takenOut=SOME), **more})
