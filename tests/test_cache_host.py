@@ -159,13 +159,14 @@ def test_frequencies():
 
 def test_frequencies_are_finite():
     """Borders, bases and factors that would give NaN or infinity are refused, those that give numbers are not."""
-    L, out = sp.load_library(), (ctypes.c_double * 8)()
-    for args in ((16, 1e4, 1.0, 9, -math.inf, 32.0), (16, 1e4, 1.0, 9, -math.inf, math.inf), (16, 5e-324, 1.0, 0, 1.0, 32.0), (16, 1e4, 1e-310, 0, 1.0, 32.0)):
+    L, out = sp.load_library(), (ctypes.c_double * 32)()
+    # the least base is 2^-1074: its power -2k / rotDim is at most 2^939.75 for 16 numbers, and past 2^1024 from k = 31 of 64 on
+    for args in ((16, 1e4, 1.0, 9, -math.inf, 32.0), (16, 1e4, 1.0, 9, -math.inf, math.inf), (64, 5e-324, 1.0, 0, 1.0, 32.0), (16, 1e4, 1e-310, 0, 1.0, 32.0)):
         assert L.sp_rotary_frequencies(*args, out) == SHAPE, args
         with pytest.raises(sp.SpError):
             sp.sp_rotary_frequencies(*args, device="cpu")
-    for args in ((16, 1e4, 2.0, 9, 1.0, math.inf), (16, 1e-300, 1.0, 0, 1.0, 32.0), (16, 1e4, 1e308, 0, -math.inf, 32.0)):
-        assert L.sp_rotary_frequencies(*args, out) == 0 and all(math.isfinite(x) for x in out), args
+    for args in ((16, 1e4, 2.0, 9, 1.0, math.inf), (16, 5e-324, 1.0, 0, 1.0, 32.0), (16, 1e-300, 1.0, 0, 1.0, 32.0), (16, 1e4, 1e308, 0, -math.inf, 32.0)):
+        assert L.sp_rotary_frequencies(*args, out) == 0 and all(math.isfinite(x) for x in out[:8]), args
 
 
 def step(**more):
