@@ -307,7 +307,7 @@ sp_status sp_cache_bytes(const sp_cache *c, size_t *bytes);
  * not in [0, pages), the table gets -1 where it has room and the tokens get slot -1, which sp_cache_store leaves out.
  * The table is read and written in place; other outputs must not overlap each other or an input.  Enqueues on `stream`, one launch; neither
  * allocates nor synchronises.  Sums must stay below 2^31.  Errors: NULL, SHAPE (pageTokens, negative sizes, ldt < width), TOO_LARGE (pages *
- * pageTokens, requests or tokens of 2^31 or more), HIP. */
+ * pageTokens or tokens of 2^31 or more, requests beyond 2^30 - 64), HIP. */
 typedef struct sp_cache_step {
     int64_t requests, tokens;
     int64_t pages;
@@ -326,7 +326,7 @@ sp_status sp_cache_map(const sp_cache_step *s, void *stream);
  * slot[i] (DEVICE).  Rows whose slot is not in [0, pages * pageTokens) are not stored, and are loaded as zeros.  No slot may be
  * given twice in a call that stores (it would hold a mixture of the rows).  sp_cache_load rounds to `dtype` (SP_F32 and SP_BF16: exact).
  * Enqueue on `stream`; neither allocate nor synchronise.  Errors, in this order: NULL (c), DTYPE, SHAPE, TOO_LARGE (pages * pageTokens or tokens of
- * 2^31 or more, tokens * kvHeads of 2^29 or more), NULL, HIP. */
+ * 2^31 or more, ceil(tokens / 32) * kvHeads of 2^24 or more), NULL, HIP. */
 sp_status sp_cache_store(const sp_cache *c, int dtype, int64_t tokens, const int32_t *slot, const void *K, int64_t ldk, int64_t hdk,
                          const void *V, int64_t ldv, int64_t hdv, void *stream);
 sp_status sp_cache_load(const sp_cache *c, int dtype, int64_t tokens, const int32_t *slot, void *K, int64_t ldk, int64_t hdk,
@@ -346,7 +346,8 @@ sp_status sp_cache_load(const sp_cache *c, int dtype, int64_t tokens, const int3
  * Enqueues on `stream`; neither allocates nor synchronises, reads lengths, rows and pages on the GPU (a recorded graph serves other ones), and
  * gives the same bits on every call.  Sums are in f32.  Rows whose sums are not finite in the end are made again token by token, which takes longer;
  * means of values that the cache holds are finite, however large these are.  The numbers of the cache are exact in the products; Q is, too (in as many parts of bf16 as its type
- * has room for); weights are rounded to Q's type before their product.  Errors, in this order: NULL (c, p), DTYPE, SHAPE, UNSUPPORTED (causal neither 0
+ * has room for); weights have as many parts:
+ * bf16's are rounded to the one that they have (8 bits), f16's to two (16 bits), f32's to three.  Errors, in this order: NULL (c, p), DTYPE, SHAPE, UNSUPPORTED (causal neither 0
  * nor 1), TOO_LARGE (pages * pageTokens, width * pageTokens, requests, or tokens * heads / kvHeads of 2^31
  * or more, or more workgroups than a launch has), NULL, SHAPE (workspace), HIP. */
 typedef struct sp_cache_problem {

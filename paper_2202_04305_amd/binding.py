@@ -500,7 +500,8 @@ def sp_attention_grad(S, Q, K, V, O, lse, dO, scale=None, causal=False, qpos=Non
     return _attention_call(S, call)
 
 
-# The same bytes as the structures above, made in a third of the time; a step of a serving loop makes one for each call.
+# The same bytes as SpRotaryProblem, SpCacheStep and SpCacheProblem, made in a third of the time; a step of a serving loop makes one for each call.
+# The structures name the fields: tests hold them to the header, and these formats to them.
 _ROTARY, _STEP, _PROBLEM = struct.Struct("@iiiidqPPii" + "Pqq" * 4), struct.Struct("@qqqi" + "PPPqPPqqPPPPP"), struct.Struct("@iiidqqPqqPqqPP")
 
 

@@ -206,6 +206,17 @@ def test_store_and_load_refusals():
     assert both(cache(pages=0, data=None))[0] == 0                             # nowhere to store to
 
 
+def test_limits_of_a_launch():
+    """Both sides of what the header says: 2^24 workgroups of 32 rows and one head, or of 64 requests.  (A cache without pages: nothing is launched.)"""
+    L = sp.load_library()
+    for heads, tokens in ((1 << 15, 511 * 32), (1, (1 << 29) - 32), (65535, 256 * 32), (8192, 2047 * 32)):
+        row = (SOME, heads * 64, 64, SOME, heads * 64, 64, None)
+        wide = cache(kvHeads=heads, pages=0)
+        assert L.sp_cache_store(ref(wide), 3, tokens, SOME, *row) == 0, (heads, tokens)
+        assert L.sp_cache_store(ref(wide), 3, tokens + 1, SOME, *row) == TOO_LARGE and L.sp_cache_load(ref(wide), 3, tokens + 1, SOME, *row) == TOO_LARGE, (heads, tokens)
+    assert L.sp_cache_map(ref(step(requests=(1 << 30) - 63)), None) == TOO_LARGE
+
+
 def problem(**more):
     return B.SpCacheProblem(**{**dict(dtype=3, heads=4, causal=1, scale=0.1, requests=3, tokens=5, Q=SOME, ldq=256, hdq=64, table=SOME, ldt=4, width=4, length=SOME,
                                       start=SOME), **more})
