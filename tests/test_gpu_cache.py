@@ -211,6 +211,48 @@ def test_slots_that_do_not_exist_and_layouts():
         assert same(sp.sp_cache_load(c, slots.to(DEV), dt)[0], torch.where(there, U.held(K[:1]).expand(n, G, d), 0.0), dt)
 
 
+@pytest.mark.parametrize("dt", [F32, F16, BF16])
+@pytest.mark.parametrize("d", [40, 96, 128])
+def test_stored_again_the_bytes_stay(d, dt):
+    """What is held is stored as it is held, bit for bit: a block's largest number is 4 or 6 times its power of two (or the block is at the least one)."""
+    say("case stored again", d, dt)
+    n, G, P, pages = 100, 2, 64, 5
+    c, slots = sp.sp_cache(pages, P, G, d), torch.randperm(pages * P, generator=torch.Generator().manual_seed(3))[:n].int().to(DEV)
+    sp.sp_cache_store(c, rows_of(n, G, d, dt, 1).to(DEV), rows_of(n, G, d, dt, 2).to(DEV), slots)
+    before = c.data.clone()
+    assert before.any()
+    k, v = sp.sp_cache_load(c, slots, F32)
+    sp.sp_cache_store(c, k, v, slots)
+    assert torch.equal(c.data, before)
+    sp.sp_cache_store(c, v, k, slots)
+    assert not torch.equal(c.data, before)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("d", [33, 64, 128])
+def test_what_lies_beside_the_pages(d, dt):
+    """A cache in the middle of other memory: rows for slots that do not exist go nowhere, those that do only into their own page."""
+    say("case beside the pages", d, dt)
+    n, G, P, pages = 64, 2, 16, 4
+    page = sp.sp_cache(1, P, G, d).data.numel()
+    before, size = 1 << 16, pages * page
+    whole = torch.full((before + size + (1 << 16),), 0xAB, dtype=torch.uint8, device=DEV)
+    inside = whole[before:before + size]
+    assert inside.data_ptr() % 256 == 0
+    c = sp.Cache(inside, B.SpCache(inside.data_ptr(), pages, P, G, d))
+    K, V = rows_of(n, G, d, dt, 1), rows_of(n, G, d, dt, 2)
+    outside = ints([-1, -2, -16, -17, -64, -2 ** 31, 64, 65, 79, 80, 127, 128, 4096, 2 ** 31 - 1] * 5)[:n]
+    sp.sp_cache_store(c, K.to(DEV), V.to(DEV), outside.to(DEV))
+    assert (whole == 0xAB).all()
+    slots = torch.where(torch.arange(n) % 3 == 0, outside, torch.arange(n).int() % 16 + 32)     # page 2 alone
+    slots[torch.arange(n) >= 16] = -1
+    sp.sp_cache_store(c, K.to(DEV), V.to(DEV), slots.to(DEV))
+    assert (whole[:before + 2 * page] == 0xAB).all() and (whole[before + 3 * page:] == 0xAB).all() and not (inside[2 * page:3 * page] == 0xAB).all()
+    k, v = sp.sp_cache_load(c, slots.to(DEV), F32)
+    there = (slots >= 32)[:, None, None] & (slots < 48)[:, None, None]
+    assert same(k, torch.where(there, U.held(K), 0.0), F32) and same(v, torch.where(there, U.held(V), 0.0), F32)
+
+
 def test_store_refused_arguments():
     c, K, at = sp.sp_cache(4, 16, 2, 64), torch.zeros(3, 2, 64, device=DEV), ints([0, 1, 2]).to(DEV)
     for k, v, s in ((K.half(), K, at), (K, K[:2], at), (K[:, :1], K[:, :1], at), (K[..., :32], K, at), (K, K, at.long()), (K, K, at[:2]), (K, K, at.cpu()),
