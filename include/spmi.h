@@ -271,8 +271,7 @@ typedef struct sp_rotary_problem {
 /* The frequencies base^(-2k / rotDim) for k < rotDim / 2 (HOST, 64 bits), for contexts longer than a model was trained on made smaller: by
  * `factor` where trained = 0; otherwise with n = trained * frequency / (2 pi) turns in the trained length and c = (n - low) / (high - low) cut
  * to [0, 1], (1 - c) / factor + c times as large: fast pairs stay, slow ones are stretched.  Errors: NULL, SHAPE (rotDim odd or negative;
- * base or factor not positive and finite; trained negative; high <= low where trained > 0; a
- * frequency that is not finite). */
+ * base or factor not positive and finite; trained negative; high <= low where trained > 0; a frequency that is not finite). */
 sp_status sp_rotary_frequencies(int rotDim, double base, double factor, int64_t trained, double low, double high, double *frequency /* HOST */);
 
 /* Turns Q and K; sp_rotary_grad: the gradients with respect to Q and K, given those with respect to the results in the places of Q and K (the
@@ -344,12 +343,12 @@ sp_status sp_cache_load(const sp_cache *c, int dtype, int64_t tokens, const int3
  *   lse  DEVICE, heads x tokens, f32; may be NULL.
  *   workspace  as for sp_attention: sp_cache_attention_workspace bytes, aligned to 256, one for each of the calls that may overlap.
  * Enqueues on `stream`; neither allocates nor synchronises, reads lengths, rows and pages on the GPU (a recorded graph serves other ones), and
- * gives the same bits on every call.  Sums are in f32.  Rows whose sums are not finite in the end are made again token by token, which takes longer;
- * means of values that the cache holds are finite, however large these are.  The numbers of the cache are exact in the products; Q is, too (in as many parts of bf16 as its type
- * has room for); weights have as many parts:
- * bf16's are rounded to the one that they have (8 bits), f16's to two (16 bits), f32's to three.  Errors, in this order: NULL (c, p), DTYPE, SHAPE, UNSUPPORTED (causal neither 0
- * nor 1), TOO_LARGE (pages * pageTokens, width * pageTokens, requests, or tokens * heads / kvHeads of 2^31
- * or more, or more workgroups than a launch has), NULL, SHAPE (workspace), HIP. */
+ * gives the same bits on every call.  Sums are in f32.  Rows whose sums are not finite in the end are made again token by token, which takes
+ * longer; means of values that the cache holds are finite, however large these are.  The numbers of the cache are exact in the products; Q is, too
+ * (in as many parts of bf16 as its type has room for); weights have as many parts: bf16's are rounded to the one that they have (8 bits), f16's
+ * to two (16 bits), f32's to three.  Errors, in this order: NULL (c, p), DTYPE, SHAPE, UNSUPPORTED (causal neither 0 nor 1), TOO_LARGE (pages *
+ * pageTokens, width * pageTokens, requests, or tokens * heads / kvHeads of 2^31 or more, or more workgroups than a launch has), NULL, SHAPE
+ * (workspace), HIP. */
 typedef struct sp_cache_problem {
     int dtype;                          /* SP_F32, SP_F16 or SP_BF16: of Q and O                                         */
     int heads;                          /* a multiple of the cache's kvHeads, at most 65535                              */
